@@ -17,7 +17,8 @@
  * generation counts, fetch new tokens).
  *
  * All functions return 0 on success or a negative BLINK_ERR_* code. Nothing throws.
- * All pointers are HOST pointers. The engine owns every byte of device memory; the caller
+ * All pointers are HOST pointers, but for those of the operators on device memory at the end of
+ * this file. The engine owns every byte of device memory; the caller
  * owns `weights`, `prompt` and event buffers, which are copied before the call returns.
  * Threads: one thread may call blink_submit while another calls blink_poll_outputs and the
  * device loop runs; all other calls are made from one control thread.
@@ -306,6 +307,88 @@ int blink_sample_rows(int32_t device, const float* logits, uint32_t n_rows, uint
  * overlap on one GPU from different processes do not share the array (each process has its own copy). */
 int blink_sample_rows_static(int32_t device, const float* logits, uint32_t n_rows, uint32_t vocab, const blink_sampling* params,
                              const uint32_t* token_index, int32_t* tokens_out);
+/* ---- operators on device memory ------------------------------------------------------------------------------------
+ * The cache of an iteration and the attention over it, for callers that bring their own model or loop. Every call checks its
+ * arguments, enqueues its kernels on `stream` (a hipStream_t of `device`, null: the default stream) and returns; it allocates nothing,
+ * waits for nothing, leaves the thread's current device as it was, and can be captured into a graph. The pointers
+ * below are device pointers of `device` (its own memory, not checked). Calls from several threads may overlap if they share no output, cache place or workspace.
+ * What lies in device memory (positions, slots, lengths, block ids) is checked by the kernels: nothing outside the tensors
+ * described is read or written, whatever it holds. */
+enum { BLINK_TYPE_FLOAT = 0, BLINK_TYPE_HALF = 1, BLINK_TYPE_BF16 = 2 };
+
+/* One layer of a paged cache: blocks of 16 tokens, data aligned to 256 bytes.
+ * 16 bits: halves, keys [block][kv head][token][dim], behind all of them values [block][kv head][dim][token] (the layout of the engine).
+ * 4 bits: per block and kv head a record of 17 head_dim bytes: codes of the keys [token][head_dim / 2], codes of the values [token / 4][16]
+ * [token % 4][head_dim / 32], where the pair (j, m) holds the dimensions 2 (j head_dim / 32 + m) and the next, scales of the keys
+ * [head_dim / 32][token], scales of the values [head_dim / 32][token]. A code is an e2m1 number (0 0.5 1 1.5 2 3 4 6, bit 3: the sign),
+ * the lower half of a byte the lower dimension. A scale byte is 127 + the exponent of the power of two that 32 neighbouring dimensions of one
+ * token share, -23 .. 13 (every value is a half, exactly); 255: not a number. */
+typedef struct {
+  void* data;
+  uint32_t n_blocks, n_kv_heads;
+  uint32_t head_dim;           /* 64 or 128 */
+  uint32_t bits;               /* 16 or 4 */
+} blink_kv_cache;
+int blink_kv_cache_bytes(uint32_t n_blocks, uint32_t n_kv_heads, uint32_t head_dim, uint32_t bits, uint64_t* bytes);
+
+/* Queries and keys normed per head, rotated and stored, in one pass. Of every token t, with its position p and its place s (block * 16 +
+ * offset) in the cache: x <- x / sqrt(mean(x^2) + eps) * gain for every query and key head (only where the gain is given); dimensions i and
+ * i + head_dim / 2 as a pair (a, b) <- (a c - b s, b c + a s) with (c, s) = rope_table[p][i]; queries times q_scale to q_out as halves;
+ * keys and the untouched values into the cache: rounded to nearest halves (beyond 65504: that), or to 4 bits: the scale of a group is the
+ * power of two that puts its largest magnitude into (3.5, 7], codes to nearest, ties to even, 7 to 6. Between inputs and the one rounding all is
+ * computed in 32 bits, keys on their way to 4 bits in 64 (their codes do not depend on an order of summation). A group of 32 with an
+ * infinity or NaN reads as NaN from 4 bits.
+ * A token whose position is not in [0, rope_rows) is skipped: none of its rows is written. One whose slot lies outside the
+ * cache (-1, padding) leaves the cache alone. The same slot twice: one of the tokens, which one is not defined. */
+typedef struct {
+  blink_kv_cache cache;
+  uint32_t n_q_heads, n_tokens;
+  uint32_t in_type;            /* BLINK_TYPE_* of q, k, v */
+  uint32_t rope_rows;
+  const void *q, *k, *v;       /* [n_tokens][heads][head_dim], rows aligned to 16 bytes */
+  uint64_t q_stride, k_stride, v_stride;   /* elements from token to token (parts of one fused projection: its width) */
+  const float *q_gain, *k_gain;            /* [head_dim], null: not normed */
+  const int32_t *positions, *slots;        /* [n_tokens] */
+  const float* rope_table;                 /* [rope_rows][head_dim / 2][2]: cosine, sine */
+  void* q_out;                             /* halves [n_tokens][n_q_heads][head_dim] */
+  uint64_t q_out_stride;
+  float eps, q_scale;
+} blink_qk_norm_rope_args;
+int blink_qk_norm_rope(int32_t device, const blink_qk_norm_rope_args* args, void* stream);
+
+/* Reads tokens back: k_out, v_out, halves [n_tokens][n_kv_heads][head_dim], of the places `slots`. Rows of places outside the cache
+ * stay as they are. */
+int blink_kv_cache_read(int32_t device, const blink_kv_cache* cache, const int32_t* slots, uint32_t n_tokens, void* k_out, void* v_out, void* stream);
+
+/* Attention over the cache. Sequence s has the tokens cu_seqlens[s] .. cu_seqlens[s + 1] of q, the last ones of its context of
+ * seq_lens[s] tokens, which lie in the blocks block_tables[s][0 ..]. A query at position p sees the keys j <= p with j > p - window or
+ * j < sinks (window 0: all j <= p): out = softmax(scale q.k) v over those, query head h with kv head h / (n_q_heads / n_kv_heads). A query that sees no
+ * key (an unused batch slot: a token and a length of 0) gives zeros; what lies in masked places, in unused places of the last
+ * block or in no block's place does not matter, infinities and NaN included. Scores, maxima and sums in 32 bits, probabilities as halves.
+ * max_q: no sequence has more queries than this (further ones are not computed). Single tokens, drafts and prompts may be mixed; calls whose
+ * sequences have few queries (max_q n_q_heads / n_kv_heads <= 16) are the fastest for those. Rows of `out` that no sequence has stay as they are.
+ * Block ids outside the cache: their keys are not seen. Results do not depend on how the work falls on the chip.
+ * The workspace holds zeros before its first call and is left so that the next one can use it; two calls that may run at the same time (two
+ * streams, two graphs in flight) need one each. BLINK_ERR_TOO_LARGE with more than 1024 sequences, or 2^31 blocks of keys. */
+typedef struct {
+  blink_kv_cache cache;
+  uint32_t n_q_heads;
+  uint32_t n_seqs, n_tokens;   /* sequences; tokens of q and out */
+  uint32_t max_q;
+  uint32_t max_blocks;         /* width of block_tables */
+  uint32_t window, sinks;
+  float scale;
+  const void* q;               /* halves [n_tokens][n_q_heads][head_dim], rows aligned to 16 bytes */
+  void* out;                   /* the same */
+  uint64_t q_stride, out_stride;
+  const int32_t *cu_seqlens, *seq_lens, *block_tables;   /* [n_seqs + 1], [n_seqs], [n_seqs][max_blocks] */
+  void* workspace;             /* aligned to 256 bytes */
+  uint64_t workspace_bytes;
+} blink_paged_attention_args;
+int blink_paged_attention(int32_t device, const blink_paged_attention_args* args, void* stream);
+/* What blink_paged_attention needs for any call with these numbers (and any smaller max_q or n_seqs). */
+int blink_attention_workspace_bytes(int32_t device, const blink_kv_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t max_q, uint64_t* bytes);
+
 /* Message of the last error on the calling thread ("" if none). The pointer stays valid until the next call. */
 const char* blink_last_error(void);
 

@@ -13,7 +13,8 @@ EVENT_FIRST, EVENT_LAST = 1, 2
 
 EXPORTS = ["blink_init", "blink_submit", "blink_run", "blink_set_exit_when_idle", "blink_wait", "blink_stop", "blink_poll_outputs", "blink_shutdown",
            "blink_get_trace", "blink_get_stats", "blink_debug_read", "blink_time_phase", "blink_get_phase_times", "blink_calibration_copy",
-           "blink_calibration_rates", "blink_clock_sync", "blink_sample_rows", "blink_sample_rows_static", "blink_last_error"]
+           "blink_calibration_rates", "blink_clock_sync", "blink_sample_rows", "blink_sample_rows_static", "blink_kv_cache_bytes", "blink_qk_norm_rope",
+           "blink_kv_cache_read", "blink_paged_attention", "blink_attention_workspace_bytes", "blink_last_error"]
 
 
 class DBG:
@@ -32,6 +33,23 @@ class Config(C.Structure):
 
 class Sampling(C.Structure):
     _fields_ = [("temperature", C.c_float), ("top_k", C.c_uint32), ("top_p", C.c_float), ("seed", C.c_uint64)]
+
+
+class CacheDesc(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n_blocks", C.c_uint32), ("n_kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("bits", C.c_uint32)]
+
+
+class QkNormRopeArgs(C.Structure):
+    _fields_ = [("cache", CacheDesc)] + [(n, C.c_uint32) for n in ("n_q_heads", "n_tokens", "in_type", "rope_rows")] + [
+        (n, C.c_void_p) for n in ("q", "k", "v")] + [(n, C.c_uint64) for n in ("q_stride", "k_stride", "v_stride")] + [
+        (n, C.c_void_p) for n in ("q_gain", "k_gain", "positions", "slots", "rope_table", "q_out")] + [
+        ("q_out_stride", C.c_uint64), ("eps", C.c_float), ("q_scale", C.c_float)]
+
+
+class PagedAttentionArgs(C.Structure):
+    _fields_ = [("cache", CacheDesc)] + [(n, C.c_uint32) for n in ("n_q_heads", "n_seqs", "n_tokens", "max_q", "max_blocks", "window", "sinks")] + [
+        ("scale", C.c_float), ("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_uint64), ("out_stride", C.c_uint64)] + [
+        (n, C.c_void_p) for n in ("cu_seqlens", "seq_lens", "block_tables", "workspace")] + [("workspace_bytes", C.c_uint64)]
 
 
 class Stats(C.Structure):
@@ -93,6 +111,11 @@ def load_library():
     lib.blink_clock_sync.argtypes = [vp, C.POINTER(u64), C.POINTER(u64), C.POINTER(u64)]
     lib.blink_sample_rows.argtypes = [C.c_int32, vp, u32, u32, vp, vp, vp]
     lib.blink_sample_rows_static.argtypes = [C.c_int32, vp, u32, u32, vp, vp, vp]
+    lib.blink_kv_cache_bytes.argtypes = [u32, u32, u32, u32, C.POINTER(u64)]
+    lib.blink_qk_norm_rope.argtypes = [C.c_int32, vp, vp]
+    lib.blink_kv_cache_read.argtypes = [C.c_int32, vp, vp, u32, vp, vp, vp]
+    lib.blink_paged_attention.argtypes = [C.c_int32, vp, vp]
+    lib.blink_attention_workspace_bytes.argtypes = [C.c_int32, vp, u32, u32, u32, C.POINTER(u64)]
     lib.blink_last_error.restype = C.c_char_p
     for n in EXPORTS[:-1]:
         getattr(lib, n).restype = C.c_int
@@ -126,6 +149,127 @@ def sample_rows(logits, params, token_index, device=0):
 def sample_rows_static(logits, params, token_index, device=0):
     """blink_sample_rows_static: as sample_rows, staging in the library's static device array (no allocation)."""
     return _sample_rows("blink_sample_rows_static", logits, params, token_index, device)
+
+
+# ---- operators on device memory: any tensors with data_ptr(), shape, stride(), dtype and device (torch's, for instance) ----
+_TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}
+
+
+def _tensor(name, t, device, dtypes, shape):
+    """Address of a device tensor whose dimensions behind the first are dense. `shape`: its sizes, None for any."""
+    if t.device.type != "cuda" or (t.device.index or 0) != device:
+        raise ValueError(f"{name} is on {t.device}, not on device {device}")
+    if str(t.dtype) not in dtypes:
+        raise ValueError(f"{name} is {t.dtype}, not one of {', '.join(dtypes)}")
+    if len(t.shape) != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
+        raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {shape}")
+    dense = 1
+    for n, s in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if s != dense and n != 1:
+            raise ValueError(f"{name}: the dimensions of a row must be contiguous")
+        dense *= n
+    if t.shape[0] > 1 and t.stride()[0] < dense:
+        raise ValueError(f"{name}: rows overlap")
+    return t.data_ptr()
+
+
+def _row_stride(t):
+    """Elements from one row to the next (of a single row: its length)."""
+    if t.shape[0] > 1:
+        return t.stride()[0]
+    n = 1
+    for m in t.shape[1:]:
+        n *= m
+    return n
+
+
+def _dense(name, t):
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+_HALF, _INT = ("torch.float16",), ("torch.int32",)
+
+
+def kv_cache_bytes(n_blocks, n_kv_heads, head_dim, bits=16):
+    """Bytes of one layer of a paged cache with `n_blocks` blocks of 16 tokens."""
+    lib, n = load_library(), C.c_uint64()
+    _check(lib, lib.blink_kv_cache_bytes(n_blocks, n_kv_heads, head_dim, bits, C.byref(n)))
+    return n.value
+
+
+class KVCache:
+    """One layer of a paged cache in a contiguous device tensor `data` of kv_cache_bytes(...) bytes, of any type (blink_kv_cache)."""
+
+    def __init__(self, data, n_blocks, n_kv_heads, head_dim, bits=16):
+        need = kv_cache_bytes(n_blocks, n_kv_heads, head_dim, bits)
+        if data.device.type != "cuda":
+            raise ValueError(f"data is on {data.device}")
+        _dense("data", data)
+        if data.numel() * data.element_size() != need:
+            raise ValueError(f"data has {data.numel() * data.element_size()} bytes, the cache {need}")
+        self.data, self.device = data, data.device.index or 0
+        self.desc = CacheDesc(data.data_ptr(), n_blocks, n_kv_heads, head_dim, bits)
+
+
+def qk_norm_rope(q, k, v, positions, slots, rope_table, cache, q_out, q_gain=None, k_gain=None, eps=1e-6, q_scale=1.0, stream=0):
+    """blink_qk_norm_rope: q [tokens, q heads, hd], k and v [tokens, kv heads, hd] (float32, float16 or bfloat16, rows may be parts
+    of wider ones), int32 positions and slots [tokens], float32 rope_table [rows, hd / 2, 2] -> q_out float16 like q, keys and
+    values into `cache`. Gains: float32 [hd] or None. stream: a stream's handle."""
+    lib, d, dev = load_library(), cache.desc, cache.device
+    T, hd, nkv = q.shape[0], d.head_dim, d.n_kv_heads
+    a = QkNormRopeArgs(cache=d, n_tokens=T, q_scale=q_scale, eps=eps)
+    a.q = _tensor("q", q, dev, _TYPES, (T, None, hd))
+    same = (str(q.dtype),)
+    a.k, a.v = _tensor("k", k, dev, same, (T, nkv, hd)), _tensor("v", v, dev, same, (T, nkv, hd))
+    a.n_q_heads, a.in_type, a.rope_rows = q.shape[1], _TYPES[same[0]], rope_table.shape[0]
+    a.q_out = _tensor("q_out", q_out, dev, _HALF, (T, q.shape[1], hd))
+    a.q_stride, a.k_stride, a.v_stride, a.q_out_stride = _row_stride(q), _row_stride(k), _row_stride(v), _row_stride(q_out)
+    a.positions, a.slots = _tensor("positions", positions, dev, _INT, (T,)), _tensor("slots", slots, dev, _INT, (T,))
+    a.rope_table = _tensor("rope_table", rope_table, dev, ("torch.float32",), (None, hd // 2, 2))
+    for name, t in (("positions", positions), ("slots", slots), ("rope_table", rope_table)):
+        _dense(name, t)
+    for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
+        if t is not None:
+            setattr(a, name, _tensor(name, t, dev, ("torch.float32",), (hd,)))
+            _dense(name, t)
+    _check(lib, lib.blink_qk_norm_rope(dev, C.byref(a), stream))
+
+
+def kv_cache_read(cache, slots, k_out, v_out, stream=0):
+    """blink_kv_cache_read: the tokens at int32 slots [tokens] into k_out, v_out, contiguous float16 [tokens, kv heads, hd]."""
+    lib, d, dev = load_library(), cache.desc, cache.device
+    shape = (slots.shape[0], d.n_kv_heads, d.head_dim)
+    at = [_tensor("slots", slots, dev, _INT, shape[:1]), _tensor("k_out", k_out, dev, _HALF, shape), _tensor("v_out", v_out, dev, _HALF, shape)]
+    for name, t in (("slots", slots), ("k_out", k_out), ("v_out", v_out)):
+        _dense(name, t)
+    _check(lib, lib.blink_kv_cache_read(dev, C.byref(d), at[0], shape[0], at[1], at[2], stream))
+
+
+def attention_workspace_bytes(n_q_heads, cache, n_seqs, max_q=1):
+    """Bytes of the workspace of paged_attention for up to n_seqs sequences of up to max_q queries. It holds zeros before its first call."""
+    lib, n = load_library(), C.c_uint64()
+    _check(lib, lib.blink_attention_workspace_bytes(cache.device, C.byref(cache.desc), n_q_heads, n_seqs, max_q, C.byref(n)))
+    return n.value
+
+
+def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q=1, window=0, sinks=0, scale=1.0, stream=0):
+    """blink_paged_attention: q, out float16 [tokens, q heads, hd]; int32 block_tables [seqs, blocks], seq_lens [seqs], cu_seqlens
+    [seqs + 1]; workspace: a contiguous tensor of attention_workspace_bytes(...) bytes. stream: a stream's handle."""
+    lib, d, dev = load_library(), cache.desc, cache.device
+    T, S = q.shape[0], seq_lens.shape[0]
+    a = PagedAttentionArgs(cache=d, n_q_heads=q.shape[1], n_seqs=S, n_tokens=T, max_q=max_q, max_blocks=block_tables.shape[-1], window=window, sinks=sinks, scale=scale)
+    a.q = _tensor("q", q, dev, _HALF, (T, None, d.head_dim))
+    a.out = _tensor("out", out, dev, _HALF, (T, q.shape[1], d.head_dim))
+    a.q_stride, a.out_stride = _row_stride(q), _row_stride(out)
+    a.block_tables, a.seq_lens = _tensor("block_tables", block_tables, dev, _INT, (S, None)), _tensor("seq_lens", seq_lens, dev, _INT, (S,))
+    a.cu_seqlens = _tensor("cu_seqlens", cu_seqlens, dev, _INT, (S + 1,))
+    for name, t in (("block_tables", block_tables), ("seq_lens", seq_lens), ("cu_seqlens", cu_seqlens), ("workspace", workspace)):
+        _dense(name, t)
+    if workspace.device.type != "cuda" or (workspace.device.index or 0) != dev:
+        raise ValueError(f"workspace is on {workspace.device}, not on device {dev}")
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(lib, lib.blink_paged_attention(dev, C.byref(a), stream))
 
 
 class Engine:

@@ -1483,4 +1483,7 @@ extern "C" int blink_sample_rows_static(int32_t device, const float* logits, uin
   return sample_rows_on(g_scratch_ptr[device], nullptr, logits, n_rows, vocab, params, token_index, tokens_out);
 }
 
+// ---- operators on device memory ---------------------------------------------------------------------------------
+#include "operators.h"
+
 extern "C" const char* blink_last_error(void) { return g_err.c_str(); }

@@ -1,0 +1,863 @@
+// Attention over the paged cache with a sliding window and first tokens that stay visible, the cache in halves or in 4 bits (layouts:
+// kv_store.h). A query at position p sees the keys j <= p of its sequence with j > p - window or j < sinks (window 0: all j <= p).
+// A row that sees nothing gives zeros. Softmax in fp32 with a running maximum and sum; the maximum follows only where a score is
+// more than 2^8 above it (a probability of up to 256 is a half as exact as one below 1), which spares most tiles the rescale
+// and the steps across lanes.
+//
+// Rows of a sequence and kv head are its queries times the G query heads that share the head: row = query * G + head. Sixteen of
+// them are the columns of the matrix products S[key][row] = K q and O^T[dim][row] = V^T P^T; the accumulator of S (column = lane % 16, keys
+// 4 (lane / 16) + i) is the operand P^T as it stands. In 4 bits a lane holds 8 neighbouring dimensions of 4 keys, so a register pair of
+// the converted values is two dimensions of one key, and each of the two products that take it has zeros for the other one's dimension
+// in its P: twice the matrix instructions, which decode has to spare, in place of exchanging halves between registers, which it has not.
+#pragma once
+#include "attention_mfma.h"
+#include "kv_store.h"
+
+struct PagedArgs {
+  const f16_t* q;                 // [token][q head][hd]
+  u64 qs;                         // elements between tokens
+  f16_t* out;                     // [token][q head][hd], or packed GEMM operand (out_tbs != 0)
+  u64 os;
+  u32 out_tbs;
+  const i32 *cu, *lens;           // first token of every sequence (n_seqs + 1), its context with them
+  const u32* tables;              // [row][max_blocks] block ids
+  const u32* table_row;           // row of every sequence (null: its number)
+  const void* cache;
+  u32 n_blocks, max_blocks;
+  u32 nq, nkv, G;
+  u32 n_seqs, n_tokens, max_q;    // sequences; tokens of q and out; queries of a sequence that are looked at
+  u32 window, sinks;
+  float c;                        // scale of the scores * log2(e)
+  u32 short_rows;                 // sequences with at most so many rows are the short part's
+  u32 n_splits;                   // most parts of a prompt item's keys
+  u32* ctr;                       // zeros between launches: [n_seqs][nkv] pieces done; then next prompt item, workgroups done
+  float* part;                    // partial results
+};
+
+// One sequence: its tokens, where its queries stand, and which blocks they see
+struct SeqView { u32 t0, n; i32 pos0; };
+__device__ __forceinline__ SeqView seq_view(const PagedArgs& a, u32 s) {
+  SeqView v;
+  const i32 c0 = max(0, min(a.cu[s], (i32)a.n_tokens)), c1 = max(c0, min(a.cu[s + 1], (i32)a.n_tokens));
+  v.t0 = (u32)c0;
+  v.n = min((u32)(c1 - c0), a.max_q);
+  v.pos0 = max(0, min(a.lens[s], (i32)(a.max_blocks * 16))) - (c1 - c0);
+  return v;
+}
+// Visible tiles of TK keys of the queries at positions p0 .. p1 (p1 >= 0): the first `zb` ones, then those from `wlo` to `hi`
+struct Seen { u32 zb, wlo, n; };
+template <u32 TK>
+__device__ __forceinline__ Seen seen_tiles(const PagedArgs& a, i32 p0, i32 p1) {
+  Seen r;
+  r.wlo = a.window && p0 >= (i32)a.window ? (u32)(p0 - (i32)a.window + 1) / TK : 0u;
+  r.zb = min((a.sinks + TK - 1) / TK, r.wlo);
+  r.n = p1 < 0 ? 0u : r.zb + (u32)p1 / TK + 1 - r.wlo;
+  return r;
+}
+
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32 f16x2_bits(f16x2_t v) { return *(const u32*)&v; }
+__device__ __forceinline__ f16x8_t f16x8_of(u32 a, u32 b, u32 c, u32 d) { const uint4 v = make_uint4(a, b, c, d); return *(const f16x8_t*)&v; }
+// Values that are not finite, where some row of the tile must not see them (0 times one would not be 0): the products take the finite ones
+// (only_finite), and a product of strange_codes with the mask (1 where a row sees a key) tells per row and dimension what else it sees:
+// 1 for every +inf, 64 for every -inf, both for NaN (exact: at most 32 keys a product). Tiles that no mask touches need none of it.
+__device__ __forceinline__ u32 only_finite(u32 w) {
+  const u32 lo = (w & 0x7C00u) == 0x7C00u ? 0u : w & 0xFFFFu, hi = (w & 0x7C000000u) == 0x7C000000u ? 0u : w & 0xFFFF0000u;
+  return lo | hi;
+}
+__device__ __forceinline__ u32 strange_codes(u32 w) {
+  auto one = [&](u32 h) { return (h & 0x7C00u) != 0x7C00u ? 0u : (h & 0x3FFu) ? 0x5410u : h >> 15 ? 0x5400u : 0x3C00u; };      // 65, 64, 1
+  return one(w & 0xFFFFu) | one(w >> 16) << 16;
+}
+__device__ __forceinline__ float strange_sum(float n) {
+  const float neg = floorf(n * (1.0f / 64.0f)), pos = n - 64.0f * neg;
+  return (pos > 0.f ? INFINITY : 0.f) + (neg > 0.f ? -INFINITY : 0.f);
+}
+__device__ __forceinline__ bool any_nan(const floatx4_t& z) { return __ballot(z[0] != 0.f || z[1] != 0.f || z[2] != 0.f || z[3] != 0.f) != 0; }
+// bit i: the row at position p (-1: no row) sees the key k + i, i < 8
+__device__ __forceinline__ u32 sees(const PagedArgs& a, i32 p, i32 k) {
+  auto below = [](i32 n) { return (1u << (u32)max(0, min(8, n))) - 1u; };
+  u32 seen = below(p + 1 - k);
+  if (a.window) seen &= ~below(p + 1 - (i32)a.window - k) | below((i32)a.sinks - k);
+  return seen;
+}
+
+// ---- few rows: decoding sequences, drafted tokens --------------------------------------------------------------------------
+// A wave's tile: 16 keys and values of a kv head.
+template <int HD, int BITS> struct CacheTile;
+template <int HD>
+struct CacheTile<HD, 16> {
+  f16x8_t k[HD / 32];
+  uint2 v[HD / 16];
+  __device__ __forceinline__ void load(const PagedArgs& a, u32 id, u32 g) {
+    const u32 lane = threadIdx.x & 63, lg = lane >> 4, lc = lane & 15;
+    const f16_t* kp = (const f16_t*)a.cache + ((u64)id * a.nkv + g) * (16 * HD);
+    const f16_t* vp = kp + (u64)a.n_blocks * a.nkv * (16 * HD);
+#pragma unroll
+    for (int s = 0; s < HD / 32; ++s) k[s] = ld_tile(kp + lc * HD + s * 32 + lg * 8);
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) v[d] = *(const uint2*)(vp + (d * 16 + lc) * 16 + lg * 4);
+  }
+  // dimension of a query's operand, step s
+  static __device__ __forceinline__ u32 q_dim(u32 s, u32 lg) { return s * 32 + lg * 8; }
+  struct Keys { f16x8_t k[HD / 32]; };
+  __device__ __forceinline__ Keys keys() const {
+    Keys r;
+#pragma unroll
+    for (int s = 0; s < HD / 32; ++s) r.k[s] = k[s];
+    return r;
+  }
+  struct Probs { f16x4_t p; };
+  static __device__ __forceinline__ Probs probs(const float (&p)[4]) { return {f16x4_t{(_Float16)p[0], (_Float16)p[1], (_Float16)p[2], (_Float16)p[3]}}; }
+  static __device__ __forceinline__ floatx4_t product(const uint2& w, const Probs& p, int, const floatx4_t& o) { return __builtin_amdgcn_mfma_f32_16x16x16f16(*(const f16x4_t*)&w, p.p, o, 0, 0, 0); }
+  struct Values { uint2 w[HD / 16]; };
+  __device__ __forceinline__ Values values() const {
+    Values r;
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) r.w[d] = v[d];
+    return r;
+  }
+  static constexpr int NW = 2, NV = HD / 16;                         // words of an operand of values, operands
+  static __device__ __forceinline__ constexpr int of(int d) { return d; }          // operand of the dimensions' tile d
+  static __device__ __forceinline__ u32& word(Values& r, int d, int k) { return k ? r.w[d].y : r.w[d].x; }
+  // the 4 dimensions of accumulator tile d, or 4 of the 8 (or 4) neighbouring ones: register i of tile d is dimension
+  static __device__ __forceinline__ u32 o_dim(int d, u32 lg, int i) { return d * 16 + lg * 4 + i; }
+};
+template <int HD>
+struct CacheTile<HD, 4> {
+  u32 k[HD / 32];                 // HD / 4 dimensions of a key: lane % 16, dimensions lane / 16 * HD / 4 ..
+  u32 v[HD / 32];                 // HD / 16 dimensions of 4 values
+  u32 ks, vs;                     // scale of the key's dimensions; of the 4 values'
+  __device__ __forceinline__ void load(const PagedArgs& a, u32 id, u32 g) {
+    const u32 lane = threadIdx.x & 63, lg = lane >> 4, lc = lane & 15;
+    const unsigned char* r = (const unsigned char*)a.cache + ((u64)id * a.nkv + g) * (17 * HD);
+    if constexpr (HD == 128) {
+      const uint4 x = *(const uint4*)(r + lane_key_off(lc, lg)), y = *(const uint4*)(r + 8 * HD + (lg * 16 + lc) * 16);
+      k[0] = x.x; k[1] = x.y; k[2] = x.z; k[3] = x.w;
+      v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w;
+      ks = r[16 * HD + lg * 16 + lc];
+      vs = *(const u32*)(r + 16 * HD + HD / 2 + (lc >> 2) * 16 + lg * 4);
+    } else {
+      const uint2 x = *(const uint2*)(r + lane_key_off(lc, lg)), y = *(const uint2*)(r + 8 * HD + (lg * 16 + lc) * 8);
+      k[0] = x.x; k[1] = x.y;
+      v[0] = y.x; v[1] = y.y;
+      ks = r[16 * HD + (lg >> 1) * 16 + lc];
+      vs = *(const u32*)(r + 16 * HD + HD / 2 + (lc >> 3) * 16 + lg * 4);
+    }
+  }
+  static __device__ __forceinline__ u32 lane_key_off(u32 lc, u32 lg) { return lc * (HD / 2) + lg * (HD / 8); }
+  static __device__ __forceinline__ u32 q_dim(u32 s, u32 lg) { return lg * (HD / 4) + s * 8; }
+  struct Keys { f16x8_t k[HD / 32]; };
+  __device__ __forceinline__ Keys keys() const {
+    const float sc = __uint_as_float(ks << 23);
+    Keys r;
+#pragma unroll
+    for (int s = 0; s < HD / 32; ++s)
+      r.k[s] = f16x8_of(f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(k[s], sc, 0)), f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(k[s], sc, 1)),
+                        f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(k[s], sc, 2)), f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(k[s], sc, 3)));
+    return r;
+  }
+  struct Probs { f16x8_t even, odd; };                               // the probability at the lower, at the upper half of each word
+  static __device__ __forceinline__ Probs probs(const float (&p)[4]) {
+    u32 e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const _Float16 h = (_Float16)p[i]; e[i] = *(const uint16_t*)&h; }
+    return {f16x8_of(e[0], e[1], e[2], e[3]), f16x8_of(e[0] << 16, e[1] << 16, e[2] << 16, e[3] << 16)};
+  }
+  struct Values { u32 w[HD / 32][4]; };                              // [pair of dimensions][value]
+  __device__ __forceinline__ Values values() const {
+    Values r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float sc = __uint_as_float((vs >> (8 * i) & 0xFFu) << 23);
+      if constexpr (HD == 128) {
+        r.w[0][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[i], sc, 0)); r.w[1][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[i], sc, 1));
+        r.w[2][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[i], sc, 2)); r.w[3][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[i], sc, 3));
+      } else {
+        const u32 w = i & 1 ? v[i / 2] >> 16 : v[i / 2];
+        r.w[0][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 0)); r.w[1][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 1));
+      }
+    }
+    return r;
+  }
+  static __device__ __forceinline__ floatx4_t product(const u32 (&w)[4], const Probs& p, int d, const floatx4_t& o) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(w[0], w[1], w[2], w[3]), d & 1 ? p.odd : p.even, o, 0, 0, 0);
+  }
+  static constexpr int NW = 4, NV = HD / 32;
+  static __device__ __forceinline__ constexpr int of(int d) { return d / 2; }
+  static __device__ __forceinline__ u32& word(Values& r, int d, int k) { return r.w[d][k]; }
+  static __device__ __forceinline__ u32 o_dim(int d, u32 lg, int i) { return (lg * 4 + i) * (HD / 16) + d; }
+};
+
+#define PAGED_WAVES 8
+#define PAGED_MAX_SEQS 1024u       // sequences whose views a workgroup keeps in LDS
+template <int HD>
+struct ShortShared {
+  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], last;
+  SeqView view[PAGED_MAX_SEQS];
+  float m[PAGED_WAVES][16], l[PAGED_WAVES][16];
+  float o[PAGED_WAVES][16][HD + 4];
+};
+
+// exclusive prefix sums of f(0 .. n) into pre[0 .. n], by eight waves
+template <typename F>
+__device__ __forceinline__ void prefix_sums(u32* pre, u32* wave_sum, u32 n, F f) {
+  const u32 lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  u32 base = 0;
+  for (u32 i0 = 0; i0 < n; i0 += 64 * PAGED_WAVES) {
+    const u32 i = i0 + threadIdx.x;
+    u32 v = i < n ? f(i) : 0u;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const u32 x = __shfl_up(v, o); if (lane >= (u32)o) v += x; }
+    __syncthreads();
+    if (lane == 63) wave_sum[w] = v;
+    __syncthreads();
+    u32 before = base;
+    for (u32 k = 0; k < PAGED_WAVES; ++k) { if (k < w) before += wave_sum[k]; base += wave_sum[k]; }
+    if (i < n) pre[i + 1] = before + v;
+  }
+  if (threadIdx.x == 0) pre[0] = 0;
+  __syncthreads();
+}
+__device__ __forceinline__ u32 last_at_most(const u32* pre, u32 n, u32 x) {     // last s < n with pre[s] <= x
+  u32 lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const u32 mid = (lo + hi) / 2;
+    if (pre[mid] <= x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// running maximum, sum and output of one tile of 16 rows, and one tile of keys and values added to them
+template <int HD, int BITS>
+struct ShortAcc {
+  typedef CacheTile<HD, BITS> Tile;
+  floatx4_t o[HD / 16];
+  float m, l;
+  __device__ __forceinline__ void init() {
+    m = -INFINITY; l = 0.f;
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) o[d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  // vis: bit i of the lane's four keys seen by the lane's row (used where `edge`)
+  __device__ __forceinline__ void add(const typename Tile::Keys& key, const typename Tile::Values& val, const f16x8_t (&q)[HD / 32], float c, bool edge, u32 vis) {
+    floatx4_t s = floatx4_t{0.f, 0.f, 0.f, 0.f}, s2 = s;             // two chains
+#pragma unroll
+    for (int i = 0; i < HD / 32; i += 2) {
+      s = __builtin_amdgcn_mfma_f32_16x16x32_f16(key.k[i], q[i], s, 0, 0, 0);
+      s2 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key.k[i + 1], q[i + 1], s2, 0, 0, 0);
+    }
+    s = (s + s2) * c;
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = vis >> i & 1u ? s[i] : -INFINITY;
+    }
+    float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    if (__ballot(top > m + 8.f)) {
+      top = quad_max(top);
+      const float mn = fmaxf(m, top);
+      const float f = mn == m || m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);      // (nothing yet but an infinity, maybe: not times 0)
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) o[d] *= f;
+      m = mn;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    float p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { p[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += p[i]; }      // exp2(-inf) = 0
+    const typename Tile::Probs pp = Tile::probs(p);
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) o[d] = Tile::product(val.w[Tile::of(d)], pp, d, o[d]);
+  }
+};
+// takes the values that are not finite out of a tile that some row does not see as a whole, and gives them to the rows that see them
+template <int HD, int BITS, int CT>
+__device__ __forceinline__ void strange_values(typename CacheTile<HD, BITS>::Values& val, ShortAcc<HD, BITS> (&acc)[CT], const u32 (&vis)[CT]) {
+  typedef CacheTile<HD, BITS> Tile;
+  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+  const typename Tile::Probs none = Tile::probs(zero);
+  floatx4_t z = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int v = 0; v < Tile::NV; ++v) z = Tile::product(val.w[v], none, 0, z);       // 0 unless something is not finite
+  if (!any_nan(z)) return;
+#pragma unroll
+  for (int d = 0; d < HD / 16; ++d) {
+    typename Tile::Values odd;
+#pragma unroll
+    for (int k = 0; k < Tile::NW; ++k) Tile::word(odd, Tile::of(d), k) = strange_codes(Tile::word(val, Tile::of(d), k));
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const float see[4] = {vis[c] & 1u ? 1.f : 0.f, vis[c] & 2u ? 1.f : 0.f, vis[c] & 4u ? 1.f : 0.f, vis[c] & 8u ? 1.f : 0.f};
+      const floatx4_t n = Tile::product(odd.w[Tile::of(d)], Tile::probs(see), d, floatx4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[c].o[d][i] += strange_sum(n[i]);
+    }
+    __builtin_amdgcn_sched_barrier(0);               // (rare: no registers for it)
+  }
+#pragma unroll
+  for (int v = 0; v < Tile::NV; ++v)
+#pragma unroll
+    for (int k = 0; k < Tile::NW; ++k) Tile::word(val, v, k) = only_finite(Tile::word(val, v, k));
+}
+
+__device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqView& v) {     // tiles of a sequence and kv head; 0: not this part's, 1 at least else
+  if (!v.n || v.n * a.G > a.short_rows) return 0;
+  return max(1u, seen_tiles<16>(a, v.pos0, v.pos0 + (i32)v.n - 1).n);
+}
+
+__device__ __forceinline__ void put_out(const PagedArgs& a, u32 tok, u32 k, float v) {
+  const u32 h = half_pair(v, 0.f);
+  if (a.out_tbs) a.out[packed_off(tok, k, a.out_tbs)] = (f16_t)h;
+  else a.out[(u64)tok * a.os + k] = (f16_t)h;
+}
+
+// All tiles of all (sequence, kv head) pairs are one line of units, cut into equal runs, one per workgroup: whatever the lengths,
+// every workgroup reads the same number of bytes. A pair whose tiles lie in several runs leaves a partial result in each, and the workgroup
+// that finishes the last of them adds them up in their order. Inside a run the eight waves take a pair's tiles in turn, NT of them on
+// their way at a time, and the next ones are asked for while these are used, over the border between two pairs too.
+#define SHORT_QUANTUM 8u
+template <int HD, int BITS, int CT, int NT>
+__device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD>& sh, u32 wg, u32 nwg) {
+  typedef CacheTile<HD, BITS> Tile;
+  constexpr u32 NW = PAGED_WAVES, ROWS = 16 * CT, SLOT = ROWS * (HD + 2);
+  const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
+  prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return short_unit_count(a, sh.view[s] = seq_view(a, s)) * a.nkv; });
+  const u32 U = (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]);
+  const u32 quantum = max(SHORT_QUANTUM, (U + nwg - 1) / nwg);
+  u32 u = wg * quantum;
+  const u32 u_end = min(u + quantum, U);
+  if (u >= u_end) return;
+  typedef const __attribute__((address_space(4))) u32 const_u32;
+  // a piece: the run's tiles of one pair, [lo, hi) of its nv; a round: up to NW * NT of them
+  struct Piece { u32 s, g, lo, hi, nv, t0, n, row, zb, wlo; i32 pos0; };
+  auto piece_at = [&](u32 at) {
+    Piece p;
+    const u32 s = (u32)__builtin_amdgcn_readfirstlane(last_at_most(sh.pre, a.n_seqs, at));
+    const SeqView v = sh.view[s];
+    const u32 in = at - (u32)__builtin_amdgcn_readfirstlane(sh.pre[s]);
+    p.s = s;
+    p.t0 = (u32)__builtin_amdgcn_readfirstlane(v.t0); p.n = (u32)__builtin_amdgcn_readfirstlane(v.n);
+    p.pos0 = __builtin_amdgcn_readfirstlane(v.pos0);
+    const Seen e = seen_tiles<16>(a, p.pos0, p.pos0 + (i32)p.n - 1);
+    p.zb = (u32)__builtin_amdgcn_readfirstlane(e.zb); p.wlo = (u32)__builtin_amdgcn_readfirstlane(e.wlo);
+    p.nv = (u32)__builtin_amdgcn_readfirstlane(max(1u, e.n));
+    p.g = (u32)__builtin_amdgcn_readfirstlane(in / p.nv);
+    p.lo = in - p.g * p.nv;
+    p.hi = min(p.nv, p.lo + (u_end - at));
+    p.row = a.table_row ? (u32)__builtin_amdgcn_readfirstlane(a.table_row[s]) : s;
+    return p;
+  };
+  u32 at[NT], id[NT], id_next[NT], at_next[NT];
+  auto ids_of = [&](const Piece& p, u32 r, u32 (&at)[NT], u32 (&id)[NT]) {    // tiles and block ids of the round that begins at tile r (past its end: its first)
+    const_u32* const bt = (const_u32*)(u64)uniform_ptr(a.tables + (u64)p.row * a.max_blocks);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const u32 l = r + w + j * NW < p.hi ? r + w + j * NW : r;
+      at[j] = (u32)__builtin_amdgcn_readfirstlane(l < p.zb ? l : p.wlo + l - p.zb);
+      id[j] = p.pos0 + (i32)p.n > 0 ? bt[at[j]] : ~0u;                        // (no query sees a key: no block either)
+    }
+  };
+  f16x8_t q[CT][HD / 32];
+  i32 qpos[CT];                                                              // position of the lane's row (no row: before every key)
+  auto load_q = [&](const Piece& p) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const u32 r = c * 16 + lc, rr = min(r, p.n * a.G - 1), tok = rr / a.G, h = rr - tok * a.G;
+      qpos[c] = r < p.n * a.G ? p.pos0 + (i32)tok : -1;
+      const f16_t* qp = a.q + (u64)(p.t0 + tok) * a.qs + (u64)(p.g * a.G + h) * HD;
+#pragma unroll
+      for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(qp + Tile::q_dim(s, lg));
+    }
+  };
+  Tile tile[NT];
+  ShortAcc<HD, BITS> acc[CT];
+  Piece cur = piece_at(u);
+  u32 r = cur.lo;
+  ids_of(cur, r, at, id);
+  load_q(cur);
+#pragma unroll
+  for (int j = 0; j < NT; ++j) tile[j].load(a, min(id[j], a.n_blocks - 1), cur.g);
+#pragma unroll
+  for (int c = 0; c < CT; ++c) acc[c].init();
+  for (;;) {
+    // what comes next: the piece's next round or the first one of the next piece
+    const bool piece_ends = r + NW * NT >= cur.hi, run_ends = piece_ends && u + (cur.hi - cur.lo) >= u_end;
+    Piece nxt = cur;
+    u32 rn = r + NW * NT;
+    if (piece_ends && !run_ends) { nxt = piece_at(u + (cur.hi - cur.lo)); rn = nxt.lo; }
+    if (!run_ends) ids_of(nxt, rn, at_next, id_next);
+    const i32 p1 = cur.pos0 + (i32)cur.n - 1;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      if (r + w + j * NW < cur.hi && p1 >= 0) {
+        const u32 k0 = at[j] * 16;
+        const typename Tile::Keys key = tile[j].keys();
+        typename Tile::Values val = tile[j].values();
+        const bool edge = !((i32)k0 + 15 <= cur.pos0 && id[j] < a.n_blocks && (!a.window || (i32)k0 > p1 - (i32)a.window || k0 + 16 <= a.sinks));
+        u32 vis[CT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) vis[c] = 0;
+        if (edge) {
+          if (id[j] < a.n_blocks) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) vis[c] = sees(a, qpos[c], (i32)(k0 + lg * 4));
+          }
+          strange_values<HD, BITS, CT>(val, acc, vis);
+        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[c].add(key, val, q[c], a.c, edge, vis[c]);
+      }
+      if (!run_ends) tile[j].load(a, min(id_next[j], a.n_blocks - 1), nxt.g);
+    }
+    if (piece_ends) {
+      const u32 rows = cur.n * a.G;
+      const bool whole = cur.hi - cur.lo == cur.nv;
+      const u32 first = u - cur.lo;                                          // the pair's first unit
+      float* const slot = a.part + (u64)(2 * wg + (cur.lo ? 0u : 1u)) * SLOT;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        __syncthreads();
+        const float l = quad_sum(acc[c].l);
+        if (lg == 0) { sh.m[w][lc] = acc[c].m; sh.l[w][lc] = l; }
+        if (c * 16 + lc < rows) {
+          if constexpr (BITS == 16) {
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)&sh.o[w][lc][d * 16 + lg * 4] = acc[c].o[d];
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int d = 0; d < HD / 16; d += 4)
+                *(floatx4_t*)&sh.o[w][lc][Tile::o_dim(d, lg, i)] = floatx4_t{acc[c].o[d][i], acc[c].o[d + 1][i], acc[c].o[d + 2][i], acc[c].o[d + 3][i]};
+          }
+        }
+        __syncthreads();
+        const u32 here = min(16u, rows > c * 16u ? rows - c * 16u : 0u);
+        for (u32 i = threadIdx.x; i < here * HD; i += 64 * NW) {
+          const u32 row = i / HD, d = i % HD;
+          float M = -INFINITY, L = 0.f, O = 0.f;
+#pragma unroll
+          for (u32 x = 0; x < NW; ++x) M = fmaxf(M, sh.m[x][row]);
+          const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+          for (u32 x = 0; x < NW; ++x) {
+            const float f = __builtin_amdgcn_exp2f(sh.m[x][row] - ref);
+            L += sh.l[x][row] * f;
+            O += sh.o[x][row][d] * f;
+          }
+          const u32 rr = c * 16 + row;
+          if (whole) {
+            const u32 tok = rr / a.G, h = rr - tok * a.G;
+            put_out(a, cur.t0 + tok, (cur.g * a.G + h) * HD + d, L == 0.f ? 0.f : O / L);
+          } else {
+            st_past_caches(slot + ROWS * 2 + rr * HD + d, O);
+            if (d == 0) { st_past_caches(slot + rr * 2, M); st_past_caches(slot + rr * 2 + 1, L); }
+          }
+        }
+        acc[c].init();
+      }
+      if (!whole) {
+        // every store has been written past the caches before the count; the last workgroup adds the pieces up (see merge_chunks)
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        __syncthreads();
+        const u32 w0 = first / quantum, np = (first + cur.nv - 1) / quantum - w0 + 1;
+        if (threadIdx.x == 0) {
+          u32* const ctr = a.ctr + (u64)cur.s * a.nkv + cur.g;
+          const u32 before = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          sh.last = before == np - 1;
+          if (before == np - 1) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (__builtin_amdgcn_readfirstlane(sh.last)) {
+          auto at_piece = [&](u32 p) { return a.part + (u64)(2 * (w0 + p) + (p ? 0u : 1u)) * SLOT; };
+          for (u32 i = threadIdx.x; i < rows * HD; i += 64 * NW) {
+            const u32 rr = i / HD, d = i % HD;
+            float M = -INFINITY, L = 0.f, O = 0.f;
+            for (u32 p0 = 0; p0 < np; p0 += 8) {
+              float m[8];
+#pragma unroll
+              for (u32 x = 0; x < 8; ++x) m[x] = ld_past_caches(at_piece(min(p0 + x, np - 1)) + rr * 2);
+#pragma unroll
+              for (u32 x = 0; x < 8; ++x) M = fmaxf(M, m[x]);
+            }
+            const float ref = M == -INFINITY ? 0.f : M;
+            for (u32 p0 = 0; p0 < np; p0 += 8) {
+              float m[8], l[8], o[8];
+#pragma unroll
+              for (u32 x = 0; x < 8; ++x) {
+                const float* b = at_piece(min(p0 + x, np - 1));
+                m[x] = ld_past_caches(b + rr * 2); l[x] = ld_past_caches(b + rr * 2 + 1); o[x] = ld_past_caches(b + ROWS * 2 + rr * HD + d);
+              }
+#pragma unroll
+              for (u32 x = 0; x < 8; ++x) {
+                const float f = __builtin_amdgcn_exp2f(m[x] - ref);
+                L = p0 + x < np ? L + l[x] * f : L;
+                O = p0 + x < np ? O + o[x] * f : O;
+              }
+            }
+            const u32 tok = rr / a.G, h = rr - tok * a.G;
+            put_out(a, cur.t0 + tok, (cur.g * a.G + h) * HD + d, L == 0.f ? 0.f : O / L);
+          }
+        }
+      }
+      if (run_ends) return;
+      u += cur.hi - cur.lo;
+      load_q(nxt);
+    }
+    cur = nxt;
+    r = rn;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) { at[j] = at_next[j]; id[j] = id_next[j]; }
+  }
+}
+
+// ---- many rows: prompts and their chunks -------------------------------------------------------------------------------------
+// One workgroup (eight waves of CT tiles of 16 rows) per (sequence, kv head, 128 CT rows): keys and values come once per workgroup, 64
+// keys a step, into a ring in LDS that every wave reads its operands from (order in LDS, products and why: attn_prompt). Halves are
+// fetched straight into the ring, three steps ahead. 4-bit tiles come into registers a step ahead, and half of the
+// waves each turn keys and values into halves in that same order, so that a value is converted once per workgroup and not once per wave.
+// The keys of a step: those of the sinks, then from the first one that the item's first query sees to the last one of its last; a
+// wave skips the steps that none of its own rows see. Items come from a counter, the last queries first. With fewer items than workgroups the
+// keys of each are cut into parts, whose results a second kernel adds up.
+#define PROMPT_CT 2u
+#define PROMPT_ROWS (128u * PROMPT_CT)
+#define PROMPT_RING (128u * 1024u)
+#define PROMPT_SLOT(HD) (PROMPT_ROWS * ((HD) + 2u))      // floats of a part's result: maximum and sum of every row, then its output
+struct PromptShared {
+  alignas(256) unsigned char ring[PROMPT_RING];
+  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], next_item;
+};
+__device__ __forceinline__ u32 prompt_items(const PagedArgs& a, u32 s) {
+  const SeqView v = seq_view(a, s);
+  return v.n * a.G <= a.short_rows ? 0u : (v.n * a.G + PROMPT_ROWS - 1) / PROMPT_ROWS;
+}
+// parts of every item's keys: as many as there are workgroups for
+__device__ __forceinline__ u32 prompt_parts(const PagedArgs& a, u32 items, u32 nwg) { return items && items < nwg ? max(1u, min(a.n_splits, nwg / items)) : 1u; }
+
+struct PromptItem { u32 s, g, r0, rows, t0; i32 p0, p1; };   // rows r0 .. r0 + rows of the sequence's, queries at positions p0 .. p1
+__device__ __forceinline__ PromptItem prompt_item(const PagedArgs& a, const u32* pre, u32 item) {
+  PromptItem it;
+  const u32 gi = pre[a.n_seqs] - 1 - item / a.nkv;             // the last queries (the longest walks) first
+  it.g = item % a.nkv;
+  it.s = last_at_most(pre, a.n_seqs, gi);
+  const SeqView v = seq_view(a, it.s);
+  it.r0 = (gi - pre[it.s]) * PROMPT_ROWS;
+  it.rows = min(PROMPT_ROWS, v.n * a.G - it.r0);
+  it.t0 = v.t0;
+  it.p0 = v.pos0 + (i32)(it.r0 / a.G);
+  it.p1 = v.pos0 + (i32)((it.r0 + it.rows - 1) / a.G);
+  return it;
+}
+
+template <int HD, int BITS>
+__device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& sh, u32 wg, u32 nwg) {
+  constexpr int CT = PROMPT_CT;
+  constexpr u32 BLK = 16 * HD * 2, NB = 4, STAGE = 2 * NB * BLK, NS = BITS == 4 ? 2 : (PROMPT_RING / STAGE > 6 ? 6 : PROMPT_RING / STAGE), TPW = BLK / 1024;
+  const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
+  prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return prompt_items(a, s); });
+  const u32 items = (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]) * a.nkv, parts = prompt_parts(a, items, nwg), total = items * parts;
+  u32* const ctr = a.ctr + (u64)a.n_seqs * a.nkv;
+  const u32 lds0 = (u32)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sh.ring;
+  // fetching halves: waves 0-3 the K of a block each, waves 4-7 the V (places in LDS: attn_prompt)
+  const bool fk = w < 4;
+  const u32 fb = w & 3u, f_lds = lds0 + w * BLK;
+  const u32 k_tok = (lc & 4) * 2 + (lc & 3) + (((lc >> 3) ^ fb) & 1u) * 4;    // the key that lies at this lane's place of a K tile
+  u32 voff[TPW];
+#pragma unroll
+  for (u32 r = 0; r < TPW; ++r) voff[r] = fk ? k_tok * (HD * 2) + r * 64 + lg * 16 : (r * 32 + (lg >> 1) * 16 + lc) * 32 + (lg & 1) * 16;
+  const u32 k_at[2] = {(lc >> 3) * BLK + lg * 256 + (lc >> 3) * 128 + (lc & 7) * 16, (lc >> 3) * BLK + lg * 256 + ((lc >> 3) ^ 1u) * 128 + (lc & 7) * 16};
+  const u32 v_at = NB * BLK + (lg >> 1) * BLK + (lg & 1) * 256 + lc * 16;
+  typedef const __attribute__((address_space(4))) u32 const_u32;
+  for (u32 turn = wg; turn < total;) {
+    const u32 item = turn / parts, part = turn - item * parts;
+    PromptItem it = prompt_item(a, sh.pre, item);
+    it.s = (u32)__builtin_amdgcn_readfirstlane(it.s); it.g = (u32)__builtin_amdgcn_readfirstlane(it.g); it.r0 = (u32)__builtin_amdgcn_readfirstlane(it.r0);
+    it.rows = (u32)__builtin_amdgcn_readfirstlane(it.rows); it.t0 = (u32)__builtin_amdgcn_readfirstlane(it.t0);
+    it.p0 = __builtin_amdgcn_readfirstlane(it.p0); it.p1 = __builtin_amdgcn_readfirstlane(it.p1);
+    const Seen e = seen_tiles<64>(a, it.p0, it.p1);
+    const u32 zb = (u32)__builtin_amdgcn_readfirstlane(e.zb), wlo = (u32)__builtin_amdgcn_readfirstlane(e.wlo), n_steps = (u32)__builtin_amdgcn_readfirstlane(e.n);
+    const u32 per = (n_steps + parts - 1) / parts, s_lo = min(part * per, n_steps), s_hi = min(s_lo + per, n_steps);
+    const u32 last_block = (u32)max(0, it.p1) / 16;
+    const u32 row = a.table_row ? (u32)__builtin_amdgcn_readfirstlane(a.table_row[it.s]) : it.s;
+    const_u32* const bt = (const_u32*)(u64)uniform_ptr(a.tables + (u64)row * a.max_blocks);
+    auto tile_of = [&](u32 s) { return s < zb ? s : wlo + s - zb; };          // 64 keys from 64 times this
+    auto block_id = [&](u32 s, u32 b) { return bt[min(NB * tile_of(min(s, n_steps ? n_steps - 1 : 0u)) + b, last_block)]; };
+    // this wave's rows
+    const u32 wr = w * (16 * CT);
+    const bool live = wr < it.rows;
+    const i32 wp0 = it.p0 + (i32)((it.r0 % a.G + wr) / a.G), wp1 = it.p0 + (i32)((it.r0 % a.G + min(wr + 16 * CT, it.rows) - 1) / a.G);
+    f16x8_t q[CT][HD / 32];
+    i32 qpos[CT];
+    u32 otok[CT], ocol[CT];
+    bool colv[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const u32 r = wr + c * 16 + lc, rr = it.r0 + min(r, it.rows - 1), tok = rr / a.G, h = rr - tok * a.G;
+      colv[c] = r < it.rows;
+      qpos[c] = colv[c] ? it.p0 - (i32)(it.r0 / a.G) + (i32)tok : -1;
+      otok[c] = it.t0 + tok; ocol[c] = (it.g * a.G + h) * HD;
+#pragma unroll
+      for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(a.q + (u64)otok[c] * a.qs + ocol[c] + s * 32 + lg * 8);
+    }
+    floatx4_t o[CT][HD / 16];
+    float m[CT], l[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      m[c] = -INFINITY; l[c] = 0.f;
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) o[c][d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    u32 id[NB], bad_ahead = 0;                       // ids of the stage to fetch next; which blocks of the stages in the ring are outside the cache, 4 bits each
+#pragma unroll
+    for (u32 b = 0; b < NB; ++b) id[b] = block_id(s_lo, b);
+    auto next_ids = [&](u32 s) {                     // notes the stage being fetched, asks for the ids of stage s
+#pragma unroll
+      for (u32 b = 0; b < NB; ++b) { bad_ahead = bad_ahead << 1 | (id[b] < a.n_blocks ? 0u : 1u); id[b] = block_id(s, b); }
+    };
+    auto my_block = [&]() { return min(fb == 0 ? id[0] : fb == 1 ? id[1] : fb == 2 ? id[2] : id[3], a.n_blocks - 1); };
+    auto fetch = [&](u32 s) {                        // stage s (past the last: that one again, not used) into its place of the ring
+      const unsigned char* src = (const unsigned char*)uniform_ptr((const f16_t*)a.cache + (((u64)(fk ? 0u : a.n_blocks) + my_block()) * a.nkv + it.g) * (16 * HD));
+      const u32 at = f_lds + (s % NS) * STAGE;
+#pragma unroll
+      for (u32 r = 0; r < TPW; ++r) dma_tile<false>(at + r * 1024, src, voff[r]);
+      next_ids(s + 1);
+    };
+    // 4 bits: waves 0-3 a block's values each, waves 4-7 its keys
+    u32 raw[8], raw_s[4];
+    auto fetch4 = [&](u32 s) {
+      const unsigned char* rec = (const unsigned char*)uniform_ptr((const unsigned char*)a.cache + ((u64)my_block() * a.nkv + it.g) * (17 * HD));
+      const u32 th = (lane >> 4) & 1;                // tokens 8 th ..
+      if (!fk) {
+#pragma unroll
+        for (u32 r = 0; r < HD / 32; ++r) {
+          raw[r] = *(const u32*)(rec + k_tok * (HD / 2) + r * 16 + lg * 4);
+          raw_s[r] = rec[16 * HD + r * 16 + k_tok];
+        }
+      } else if constexpr (HD == 128) {
+        const uint4 x = *(const uint4*)(rec + 8 * HD + (th * 32 + lc) * 16), y = *(const uint4*)(rec + 8 * HD + (th * 32 + 16 + lc) * 16);
+        raw[0] = x.x; raw[1] = x.y; raw[2] = x.z; raw[3] = x.w; raw[4] = y.x; raw[5] = y.y; raw[6] = y.z; raw[7] = y.w;
+        const uint2 z = *(const uint2*)(rec + 16 * HD + HD / 2 + (lc >> 2) * 16 + th * 8);
+        raw_s[0] = z.x; raw_s[1] = z.y;
+      } else {
+        const uint2 x = *(const uint2*)(rec + 8 * HD + (th * 32 + lc) * 8), y = *(const uint2*)(rec + 8 * HD + (th * 32 + 16 + lc) * 8);
+        raw[0] = x.x; raw[1] = x.y; raw[2] = y.x; raw[3] = y.y;
+        const uint2 z = *(const uint2*)(rec + 16 * HD + HD / 2 + (lc >> 3) * 16 + th * 8);
+        raw_s[0] = z.x; raw_s[1] = z.y;
+      }
+      next_ids(s + 1);
+    };
+    auto convert4 = [&](u32 s) {                     // what fetch4 brought, as halves into the ring
+      unsigned char* const st = sh.ring + (s % NS) * STAGE;
+      if (!fk) {
+        unsigned char* const to = st + fb * BLK + lane * 16;
+#pragma unroll
+        for (u32 r = 0; r < HD / 32; ++r) {
+          const float sc = __uint_as_float(raw_s[r] << 23);
+          *(uint4*)(to + r * 1024) = make_uint4(f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[r], sc, 0)), f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[r], sc, 1)),
+                                                f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[r], sc, 2)), f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[r], sc, 3)));
+        }
+      } else if (HD == 128 || lane < 32) {
+        // a lane: 8 tokens x 4 dimensions (of heads of 128 the lower or upper 4 of 8)
+        const u32 th = (lane >> 4) & 1, dq = lane >> 5;
+        u32 pr[8][2];                                // [token][pair of dimensions]
+#pragma unroll
+        for (u32 i = 0; i < 8; ++i) {
+          const float sc = __uint_as_float((raw_s[i / 4] >> (8 * (i % 4)) & 0xFFu) << 23);
+          const u32 x = HD == 128 ? (dq ? raw[i] >> 16 : raw[i]) : (i & 1 ? raw[i / 2] >> 16 : raw[i / 2]);
+          pr[i][0] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 0));
+          pr[i][1] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 1));
+        }
+#pragma unroll
+        for (u32 x = 0; x < 4; ++x) {
+          const u32 D = HD == 128 ? lc * 8 + dq * 4 + x : lc * 4 + x;
+          const u32 sel = x & 1 ? 0x07060302u : 0x05040100u;
+          u32 v[4];
+#pragma unroll
+          for (u32 i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(pr[2 * i + 1][x / 2], pr[2 * i][x / 2], sel);
+          *(uint4*)(st + (NB + fb) * BLK + (D / 32) * 1024 + (((D % 32) / 16 * 2 + th) * 16 + D % 16) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+      }
+    };
+    if constexpr (BITS == 16) {
+#pragma unroll 1
+      for (u32 s = 0; s < NS - 1; ++s) fetch(s_lo + s);
+      wait_loads();      // (left to the compiler, the wait for the queries stands in the loop and empties the ring in every step)
+    } else {
+      fetch4(s_lo);
+    }
+    for (u32 s = s_lo; s < s_hi; ++s) {
+      u32 bad;
+      if constexpr (BITS == 16) {
+        wait_dma_barrier<(int)((NS - 2) * TPW)>();             // stage s is in LDS for everyone, stage s - 1 has been read by everyone
+        bad = bad_ahead >> (4 * (NS - 2)) & 15u;
+        fetch(s + NS - 1);
+      } else {
+        bad = bad_ahead & 15u;
+        convert4(s);                                           // (everyone has read what lay there, step s - 2, before the last barrier)
+        fetch4(s + 1);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+      }
+      const u32 k0 = tile_of(s) * 64;
+      if (!live || (i32)k0 > wp1 || (a.window && (i32)k0 + 63 <= wp0 - (i32)a.window && k0 >= a.sinks)) continue;
+      const unsigned char* const st0 = sh.ring + (s % NS) * STAGE;
+      floatx4_t sc[CT][NB];
+#pragma unroll
+      for (u32 b = 0; b < NB; ++b) {
+        f16x8_t ka[HD / 32];
+#pragma unroll
+        for (int st = 0; st < HD / 32; ++st) ka[st] = as_f16x8(*(const uint4*)(st0 + (b & 2) * BLK + st * 1024 + k_at[b & 1]));
+#pragma unroll
+        for (int c = 0; c < CT; ++c) sc[c][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[0], q[c][0], floatx4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+        for (int st = 1; st < HD / 32; ++st)
+#pragma unroll
+          for (int c = 0; c < CT; ++c) sc[c][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[st], q[c][st], sc[c][b], 0, 0, 0);
+      }
+      const bool edge = (i32)k0 + 63 > wp0 || wr + 16 * CT > it.rows || bad || (a.window && (i32)k0 <= wp1 - (i32)a.window && k0 + 64 > a.sinks);
+      u32 vis[CT] = {};                                        // bit 8 h + i: this lane's row sees its key i of the step's pair of blocks h
+      if (edge) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+#pragma unroll
+          for (u32 h = 0; h < NB / 2; ++h)
+            if (!(bad >> (NB - 1 - (2 * h + (lg >> 1))) & 1u)) vis[c] |= sees(a, qpos[c], (i32)(k0 + h * 32 + lg * 8)) << (8 * h);
+#pragma unroll
+          for (u32 b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[c][b][i] = vis[c] >> (b * 4 + i) & 1u ? sc[c][b][i] : -INFINITY;
+        }
+      }
+      f16x8_t pb[CT][NB / 2];
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        float top = -INFINITY;
+#pragma unroll
+        for (u32 b = 0; b < NB; ++b) top = fmaxf(top, fmaxf(fmaxf(sc[c][b][0], sc[c][b][1]), fmaxf(sc[c][b][2], sc[c][b][3])));
+        top *= a.c;
+        if (__ballot(top > m[c] + 8.f)) {
+          top = quad_max(top);
+          const float mn = fmaxf(m[c], top);
+          const float f = mn == m[c] || m[c] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[c] - mn);
+          l[c] *= f;
+#pragma unroll
+          for (int d = 0; d < HD / 16; ++d) o[c][d] *= f;
+          m[c] = mn;
+        }
+        const float nm = m[c] == -INFINITY ? 0.f : -m[c];
+        float ps = 0.f;
+#pragma unroll
+        for (u32 b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][b][i], a.c, nm));
+            ps += p;
+            pb[c][b / 2][(b & 1) * 4 + i] = (_Float16)p;
+          }
+        l[c] += ps;
+      }
+      const unsigned char* const sv = st0 + v_at;
+      auto value_bits = [&](int d, u32 h) { return *(const uint4*)(sv + 2 * h * BLK + (d >> 1) * 1024 + (d & 1) * 512); };
+      bool strange = false;                                    // some value of the step is not finite
+      if (edge) {
+        const f16x8_t none = f16x8_of(0, 0, 0, 0);
+        floatx4_t z = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+          for (u32 h = 0; h < NB / 2; ++h) z = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_f16x8(value_bits(d, h)), none, z, 0, 0, 0);
+        strange = any_nan(z);
+      }
+      if (!strange) {
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+          for (u32 h = 0; h < NB / 2; ++h) {
+            const f16x8_t va = as_f16x8(value_bits(d, h));
+#pragma unroll
+            for (int c = 0; c < CT; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pb[c][h], o[c][d], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+          for (u32 h = 0; h < NB / 2; ++h) {
+            const uint4 x = value_bits(d, h);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+              o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(only_finite(x.x), only_finite(x.y), only_finite(x.z), only_finite(x.w)), pb[c][h], o[c][d], 0, 0, 0);
+              u32 see[4];
+#pragma unroll
+              for (u32 k = 0; k < 4; ++k) see[k] = (vis[c] >> (8 * h + 2 * k) & 1u ? 0x3C00u : 0u) | (vis[c] >> (8 * h + 2 * k + 1) & 1u ? 0x3C000000u : 0u);
+              const floatx4_t n = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(strange_codes(x.x), strange_codes(x.y), strange_codes(x.z), strange_codes(x.w)),
+                                                                         f16x8_of(see[0], see[1], see[2], see[3]), floatx4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[c][d][i] += strange_sum(n[i]);
+              __builtin_amdgcn_sched_barrier(0);     // (rare: no registers for it)
+            }
+          }
+      }
+    }
+    if (threadIdx.x == 0) sh.next_item = nwg + __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const float sum = quad_sum(l[c]);
+      if (parts == 1) {
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        if (colv[c]) {
+#pragma unroll
+          for (int d = 0; d < HD / 16; ++d) {
+            const u32 k = ocol[c] + d * 16 + lg * 4;
+            f16_t* to = a.out_tbs ? a.out + packed_off(otok[c], k, a.out_tbs) : a.out + (u64)otok[c] * a.os + k;
+            *(uint2*)to = make_uint2(half_pair(o[c][d][0] * inv, o[c][d][1] * inv), half_pair(o[c][d][2] * inv, o[c][d][3] * inv));
+          }
+        }
+      } else if (colv[c]) {
+        float* const slot = a.part + (u64)turn * PROMPT_SLOT(HD);
+        const u32 r = wr + c * 16 + lc;
+        if (lg == 0) *(float2*)(slot + 2 * r) = make_float2(m[c], sum);
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(slot + 2 * PROMPT_ROWS + r * HD + d * 16 + lg * 4) = o[c][d];
+      }
+    }
+    if constexpr (BITS == 16) wait_dma_barrier<0>();           // no fetch of this item is on its way any more, and next_item is there
+    else __syncthreads();
+    turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item);
+    __syncthreads();                                           // (read by everyone before it is written again)
+  }
+  // the last workgroup out leaves the counters as it found them
+  if (threadIdx.x == 0 && __hip_atomic_fetch_add(ctr + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == nwg - 1) {
+    __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(ctr + 1, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+
+// The parts of the prompt items added up: a wave per row, its lanes along the dimensions. `nwg_prompt`: workgroups of the launch before.
+struct PromptMergeShared { u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES]; };
+template <int HD>
+__device__ __forceinline__ void prompt_merge(const PagedArgs& a, PromptMergeShared& sh, u32 wg, u32 nwg, u32 nwg_prompt) {
+  prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return prompt_items(a, s); });
+  const u32 items = sh.pre[a.n_seqs] * a.nkv, parts = prompt_parts(a, items, nwg_prompt), lane = threadIdx.x & 63;
+  if (parts < 2) return;
+  for (u32 i = wg * PAGED_WAVES + (threadIdx.x >> 6); i < items * PROMPT_ROWS; i += nwg * PAGED_WAVES) {
+    const u32 item = i / PROMPT_ROWS, r = i % PROMPT_ROWS;
+    const PromptItem it = prompt_item(a, sh.pre, item);
+    if (r >= it.rows) continue;
+    const float* const base = a.part + (u64)item * parts * PROMPT_SLOT(HD);
+    float M = -INFINITY, L = 0.f, O[HD / 64];
+#pragma unroll
+    for (int d = 0; d < HD / 64; ++d) O[d] = 0.f;
+    for (u32 p = 0; p < parts; ++p) M = fmaxf(M, base[(u64)p * PROMPT_SLOT(HD) + 2 * r]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    for (u32 p = 0; p < parts; ++p) {
+      const float* const b = base + (u64)p * PROMPT_SLOT(HD);
+      const float f = __builtin_amdgcn_exp2f(b[2 * r] - ref);
+      L += b[2 * r + 1] * f;
+#pragma unroll
+      for (int d = 0; d < HD / 64; ++d) O[d] += b[2 * PROMPT_ROWS + r * HD + d * 64 + lane] * f;
+    }
+    const u32 rr = it.r0 + r, tok = rr / a.G, h = rr - tok * a.G;
+#pragma unroll
+    for (int d = 0; d < HD / 64; ++d) put_out(a, it.t0 + tok, (it.g * a.G + h) * HD + d * 64 + lane, L == 0.f ? 0.f : O[d] / L);
+  }
+}
