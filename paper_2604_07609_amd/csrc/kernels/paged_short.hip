@@ -3,7 +3,7 @@
 
 #define SHORT_KERNEL(HD, BITS, CT, NT)                                                                                                              \
   template <> __global__ void __launch_bounds__(512) __attribute__((amdgpu_num_vgpr(120))) k_paged_short<HD, BITS, CT>(PagedArgs a) { \
-    __shared__ ShortShared<HD> sh;                                                                                                                  \
+    __shared__ ShortShared<HD, CT> sh;                                                                                                                  \
     paged_short<HD, BITS, CT, NT>(a, sh, blockIdx.x, gridDim.x);                                                                                    \
   }
 SHORT_KERNEL(64, 16, 1, 4)

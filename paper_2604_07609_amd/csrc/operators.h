@@ -146,7 +146,7 @@ static PagedPlan paged_plan(u32 hd, u32 nq, u32 nkv, u32 n_seqs, u32 n_tokens, u
   const bool few = (u64)n_tokens * G / PROMPT_ROWS * nkv < p.prompt_wgs;
   p.n_splits = p.prompt && few ? std::max(1u, key_steps / 4) : 1u;
   p.ctr_bytes = (((u64)n_seqs * nkv + 2) * 4 + 255) / 256 * 256;
-  const u64 short_part = p.ct ? 2ull * p.short_wgs * 16 * p.ct * (hd + 2) * 4 : 0, prompt_part = p.prompt ? (u64)p.prompt_wgs * PROMPT_SLOT(hd) * 4 : 0;
+  const u64 short_part = p.ct ? 2ull * p.short_wgs * p.ct * (128 + 16 * hd) * 4 : 0, prompt_part = p.prompt ? (u64)p.prompt_wgs * PROMPT_SLOT(hd) * 4 : 0;
   p.part_bytes = std::max(short_part, prompt_part);
   return p;
 }

@@ -191,12 +191,12 @@ struct CacheTile<HD, 4> {
 
 #define PAGED_WAVES 8
 #define PAGED_MAX_SEQS 1024u       // sequences whose views a workgroup keeps in LDS
-template <int HD>
+template <int HD, int CT>
 struct ShortShared {
-  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], last;
+  floatx4_t o[PAGED_WAVES][CT][HD / 16][64];         // a result that one wave leaves for another, as its registers hold it
+  float m[PAGED_WAVES][CT][16], l[PAGED_WAVES][CT][16];
   SeqView view[PAGED_MAX_SEQS];
-  float m[PAGED_WAVES][16], l[PAGED_WAVES][16];
-  float o[PAGED_WAVES][16][HD + 4];
+  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], last[2];
 };
 
 // exclusive prefix sums of f(0 .. n) into pre[0 .. n], by eight waves
@@ -239,6 +239,13 @@ struct ShortAcc {
 #pragma unroll
     for (int d = 0; d < HD / 16; ++d) o[d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   }
+  // maximum and sum with another result's; the factors of this one's output and of the other's
+  __device__ __forceinline__ void join(float m2, float l2, float& mine, float& other) {
+    const float mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.f : mn;
+    mine = __builtin_amdgcn_exp2f(m - ref); other = __builtin_amdgcn_exp2f(m2 - ref);
+    l = l * mine + l2 * other;
+    m = mn;
+  }
   // vis: bit i of the lane's four keys seen by the lane's row (used where `edge`)
   __device__ __forceinline__ void add(const typename Tile::Keys& key, const typename Tile::Values& val, const f16x8_t (&q)[HD / 32], float c, bool edge, u32 vis) {
     floatx4_t s = floatx4_t{0.f, 0.f, 0.f, 0.f}, s2 = s;             // two chains
@@ -271,6 +278,67 @@ struct ShortAcc {
     for (int d = 0; d < HD / 16; ++d) o[d] = Tile::product(val.w[Tile::of(d)], pp, d, o[d]);
   }
 };
+template <int HD, int BITS, int CT>
+__device__ __forceinline__ void leave_in_lds(ShortShared<HD, CT>& sh, u32 at, const ShortAcc<HD, BITS> (&acc)[CT]) {
+  const u32 lane = threadIdx.x & 63;
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const float l = quad_sum(acc[c].l);
+    if (lane < 16) { sh.m[at][c][lane] = acc[c].m; sh.l[at][c][lane] = l; }
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) sh.o[at][c][d][lane] = acc[c].o[d];
+  }
+}
+template <int HD, int BITS, int CT>
+__device__ __forceinline__ void add_from_lds(const ShortShared<HD, CT>& sh, u32 at, ShortAcc<HD, BITS> (&acc)[CT]) {
+  const u32 lane = threadIdx.x & 63;
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    float mine, other;
+    acc[c].join(sh.m[at][c][lane & 15], lane < 16 ? sh.l[at][c][lane] : 0.f, mine, other);       // (a sum is that of the row's four lanes)
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) acc[c].o[d] = acc[c].o[d] * mine + sh.o[at][c][d][lane] * other;
+  }
+}
+// a result in global memory, for another workgroup (see merge_chunks for why past the caches): maxima, sums, outputs as registers hold them
+template <int HD, int CT> __device__ __forceinline__ constexpr u32 short_slot() { return CT * (128 + HD * 16); }     // floats
+template <int HD, int BITS, int CT>
+__device__ __forceinline__ void leave_past_caches(float* slot, const ShortAcc<HD, BITS> (&acc)[CT], u32 rows) {
+  const u32 lane = threadIdx.x & 63;
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    if (c * 16 + (lane & 15) >= rows) continue;
+    float* const p = slot + c * (128 + HD * 16);
+    st_past_caches(p + lane, acc[c].m); st_past_caches(p + 64 + lane, acc[c].l);
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) {
+      u64* const q = (u64*)(p + 128 + (d * 64 + lane) * 4);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        __hip_atomic_store(q + h, ((u64)__float_as_uint(acc[c].o[d][2 * h + 1]) << 32) | __float_as_uint(acc[c].o[d][2 * h]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+}
+template <int HD, int BITS, int CT>
+__device__ __forceinline__ void add_past_caches(const float* slot, ShortAcc<HD, BITS> (&acc)[CT], u32 rows) {
+  const u32 lane = threadIdx.x & 63;
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    if (c * 16 + (lane & 15) >= rows) continue;
+    const float* const p = slot + c * (128 + HD * 16);
+    u64 v[HD / 16][2];
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) v[d][h] = __hip_atomic_load((const u64*)(p + 128 + (d * 64 + lane) * 4) + h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    float mine, other;
+    acc[c].join(ld_past_caches(p + lane), ld_past_caches(p + 64 + lane), mine, other);
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[c].o[d][i] = acc[c].o[d][i] * mine + __uint_as_float((u32)(v[d][i >> 1] >> (32 * (i & 1)))) * other;
+  }
+}
 // takes the values that are not finite out of a tile that some row does not see as a whole, and gives them to the rows that see them
 template <int HD, int BITS, int CT>
 __device__ __forceinline__ void strange_values(typename CacheTile<HD, BITS>::Values& val, ShortAcc<HD, BITS> (&acc)[CT], const u32 (&vis)[CT]) {
@@ -306,61 +374,53 @@ __device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqVie
   return max(1u, seen_tiles<16>(a, v.pos0, v.pos0 + (i32)v.n - 1).n);
 }
 
-__device__ __forceinline__ void put_out(const PagedArgs& a, u32 tok, u32 k, float v) {
-  const u32 h = half_pair(v, 0.f);
-  if (a.out_tbs) a.out[packed_off(tok, k, a.out_tbs)] = (f16_t)h;
-  else a.out[(u64)tok * a.os + k] = (f16_t)h;
-}
+__device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { return a.out_tbs ? a.out + packed_off(tok, k, a.out_tbs) : a.out + (u64)tok * a.os + k; }
 
-// All tiles of all (sequence, kv head) pairs are one line of units, cut into equal runs, one per workgroup: whatever the lengths,
-// every workgroup reads the same number of bytes. A pair whose tiles lie in several runs leaves a partial result in each, and the workgroup
-// that finishes the last of them adds them up in their order. Inside a run the eight waves take a pair's tiles in turn, NT of them on
-// their way at a time, and the next ones are asked for while these are used, over the border between two pairs too.
-#define SHORT_QUANTUM 8u
+// All tiles of all (sequence, kv head) pairs are one line of units, cut into equal runs, one per wave: whatever the lengths, every
+// wave reads the same number of bytes, with NT tiles on their way across the borders between pairs, and waits for nobody until its run ends.
+// A pair inside a run is finished where it is. One that several waves of a workgroup share is added up by the wave it begins in (in
+// LDS, after the one barrier); one that several workgroups share leaves a result of each in the workspace, and the workgroup that comes
+// last adds them up, its waves an eighth of them each. All sums in the order of the runs: results do not depend on who comes when.
+#define SHORT_QUANTUM 4u
 template <int HD, int BITS, int CT, int NT>
-__device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD>& sh, u32 wg, u32 nwg) {
+__device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, CT>& sh, u32 wg, u32 nwg) {
   typedef CacheTile<HD, BITS> Tile;
-  constexpr u32 NW = PAGED_WAVES, ROWS = 16 * CT, SLOT = ROWS * (HD + 2);
+  constexpr u32 NW = PAGED_WAVES;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
+  auto scalar = [](u32 x) { return (u32)__builtin_amdgcn_readfirstlane(x); };
   prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return short_unit_count(a, sh.view[s] = seq_view(a, s)) * a.nkv; });
-  const u32 U = (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]);
-  const u32 quantum = max(SHORT_QUANTUM, (U + nwg - 1) / nwg);
-  u32 u = wg * quantum;
-  const u32 u_end = min(u + quantum, U);
-  if (u >= u_end) return;
+  const u32 U = scalar(sh.pre[a.n_seqs]);
+  const u32 quantum = max(SHORT_QUANTUM, (U + nwg * NW - 1) / (nwg * NW)), wg_units = quantum * NW;
+  if (wg * wg_units >= U) return;                    // (all its waves: the counts below are of workgroups with units)
+  if (threadIdx.x < 2) sh.last[threadIdx.x] = 0;
+  const u32 u0 = min((wg * NW + w) * quantum, U), u1 = min(u0 + quantum, U);
   typedef const __attribute__((address_space(4))) u32 const_u32;
-  // a piece: the run's tiles of one pair, [lo, hi) of its nv; a round: up to NW * NT of them
-  struct Piece { u32 s, g, lo, hi, nv, t0, n, row, zb, wlo; i32 pos0; };
-  auto piece_at = [&](u32 at) {
-    Piece p;
-    const u32 s = (u32)__builtin_amdgcn_readfirstlane(last_at_most(sh.pre, a.n_seqs, at));
+  // a pair of a sequence and a kv head: its first unit and number of tiles, its rows, and which tiles those are
+  struct Pair { u32 s, g, first, nv, t0, n, row, zb, wlo; i32 pos0; };
+  auto pair_of = [&](u32 s, u32 g) {
+    Pair p;
     const SeqView v = sh.view[s];
-    const u32 in = at - (u32)__builtin_amdgcn_readfirstlane(sh.pre[s]);
-    p.s = s;
-    p.t0 = (u32)__builtin_amdgcn_readfirstlane(v.t0); p.n = (u32)__builtin_amdgcn_readfirstlane(v.n);
-    p.pos0 = __builtin_amdgcn_readfirstlane(v.pos0);
+    p.s = s; p.g = g;
+    p.t0 = scalar(v.t0); p.n = scalar(v.n); p.pos0 = (i32)scalar((u32)v.pos0);
     const Seen e = seen_tiles<16>(a, p.pos0, p.pos0 + (i32)p.n - 1);
-    p.zb = (u32)__builtin_amdgcn_readfirstlane(e.zb); p.wlo = (u32)__builtin_amdgcn_readfirstlane(e.wlo);
-    p.nv = (u32)__builtin_amdgcn_readfirstlane(max(1u, e.n));
-    p.g = (u32)__builtin_amdgcn_readfirstlane(in / p.nv);
-    p.lo = in - p.g * p.nv;
-    p.hi = min(p.nv, p.lo + (u_end - at));
-    p.row = a.table_row ? (u32)__builtin_amdgcn_readfirstlane(a.table_row[s]) : s;
+    p.zb = scalar(e.zb); p.wlo = scalar(e.wlo); p.nv = scalar(max(1u, e.n));
+    p.first = scalar(sh.pre[s]) + g * p.nv;
+    p.row = a.table_row ? scalar(a.table_row[s]) : s;
     return p;
   };
-  u32 at[NT], id[NT], id_next[NT], at_next[NT];
-  auto ids_of = [&](const Piece& p, u32 r, u32 (&at)[NT], u32 (&id)[NT]) {    // tiles and block ids of the round that begins at tile r (past its end: its first)
-    const_u32* const bt = (const_u32*)(u64)uniform_ptr(a.tables + (u64)p.row * a.max_blocks);
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const u32 l = r + w + j * NW < p.hi ? r + w + j * NW : r;
-      at[j] = (u32)__builtin_amdgcn_readfirstlane(l < p.zb ? l : p.wlo + l - p.zb);
-      id[j] = p.pos0 + (i32)p.n > 0 ? bt[at[j]] : ~0u;                        // (no query sees a key: no block either)
-    }
+  auto pair_at = [&](u32 u) {
+    const u32 s = scalar(last_at_most(sh.pre, a.n_seqs, u)), in = u - scalar(sh.pre[s]);
+    return pair_of(s, in / (scalar(sh.pre[s + 1] - sh.pre[s]) / a.nkv));
+  };
+  auto pair_after = [&](const Pair& p) {             // (there is one)
+    if (p.g + 1 < a.nkv) { Pair q = p; ++q.g; q.first += q.nv; return q; }
+    u32 s = p.s + 1;
+    while (scalar(sh.pre[s + 1]) == scalar(sh.pre[s])) ++s;
+    return pair_of(s, 0);
   };
   f16x8_t q[CT][HD / 32];
-  i32 qpos[CT];                                                              // position of the lane's row (no row: before every key)
-  auto load_q = [&](const Piece& p) {
+  i32 qpos[CT];                                      // position of the lane's row (no row: before every key)
+  auto load_q = [&](const Pair& p) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const u32 r = c * 16 + lc, rr = min(r, p.n * a.G - 1), tok = rr / a.G, h = rr - tok * a.G;
@@ -370,145 +430,148 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD>&
       for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(qp + Tile::q_dim(s, lg));
     }
   };
-  Tile tile[NT];
   ShortAcc<HD, BITS> acc[CT];
-  Piece cur = piece_at(u);
-  u32 r = cur.lo;
-  ids_of(cur, r, at, id);
-  load_q(cur);
+  auto clear = [&]() {
 #pragma unroll
-  for (int j = 0; j < NT; ++j) tile[j].load(a, min(id[j], a.n_blocks - 1), cur.g);
+    for (int c = 0; c < CT; ++c) acc[c].init();
+  };
+  auto finish = [&](const Pair& p) {
 #pragma unroll
-  for (int c = 0; c < CT; ++c) acc[c].init();
-  for (;;) {
-    // what comes next: the piece's next round or the first one of the next piece
-    const bool piece_ends = r + NW * NT >= cur.hi, run_ends = piece_ends && u + (cur.hi - cur.lo) >= u_end;
-    Piece nxt = cur;
-    u32 rn = r + NW * NT;
-    if (piece_ends && !run_ends) { nxt = piece_at(u + (cur.hi - cur.lo)); rn = nxt.lo; }
-    if (!run_ends) ids_of(nxt, rn, at_next, id_next);
-    const i32 p1 = cur.pos0 + (i32)cur.n - 1;
+    for (int c = 0; c < CT; ++c) {
+      const float l = quad_sum(acc[c].l), inv = l == 0.f ? 0.f : 1.0f / l;
+      const u32 r = c * 16 + lc, tok = r / a.G, k = (p.g * a.G + r - tok * a.G) * HD;
+      if (r >= p.n * a.G) continue;
+      if constexpr (BITS == 16) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      if (r + w + j * NW < cur.hi && p1 >= 0) {
-        const u32 k0 = at[j] * 16;
-        const typename Tile::Keys key = tile[j].keys();
-        typename Tile::Values val = tile[j].values();
-        const bool edge = !((i32)k0 + 15 <= cur.pos0 && id[j] < a.n_blocks && (!a.window || (i32)k0 > p1 - (i32)a.window || k0 + 16 <= a.sinks));
-        u32 vis[CT];
+        for (int d = 0; d < HD / 16; ++d)
+          *(uint2*)out_at(a, p.t0 + tok, k + d * 16 + lg * 4) =
+              make_uint2(half_pair(acc[c].o[d][0] * inv, acc[c].o[d][1] * inv), half_pair(acc[c].o[d][2] * inv, acc[c].o[d][3] * inv));
+      } else {
 #pragma unroll
-        for (int c = 0; c < CT; ++c) vis[c] = 0;
-        if (edge) {
-          if (id[j] < a.n_blocks) {
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int c = 0; c < CT; ++c) vis[c] = sees(a, qpos[c], (i32)(k0 + lg * 4));
-          }
-          strange_values<HD, BITS, CT>(val, acc, vis);
-        }
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c].add(key, val, q[c], a.c, edge, vis[c]);
+          for (int d = 0; d < HD / 16; d += 4)
+            *(uint2*)out_at(a, p.t0 + tok, k + Tile::o_dim(d, lg, i)) =
+                make_uint2(half_pair(acc[c].o[d][i] * inv, acc[c].o[d + 1][i] * inv), half_pair(acc[c].o[d + 2][i] * inv, acc[c].o[d + 3][i] * inv));
       }
-      if (!run_ends) tile[j].load(a, min(id_next[j], a.n_blocks - 1), nxt.g);
     }
-    if (piece_ends) {
-      const u32 rows = cur.n * a.G;
-      const bool whole = cur.hi - cur.lo == cur.nv;
-      const u32 first = u - cur.lo;                                          // the pair's first unit
-      float* const slot = a.part + (u64)(2 * wg + (cur.lo ? 0u : 1u)) * SLOT;
-#pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        __syncthreads();
-        const float l = quad_sum(acc[c].l);
-        if (lg == 0) { sh.m[w][lc] = acc[c].m; sh.l[w][lc] = l; }
-        if (c * 16 + lc < rows) {
-          if constexpr (BITS == 16) {
-#pragma unroll
-            for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)&sh.o[w][lc][d * 16 + lg * 4] = acc[c].o[d];
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int d = 0; d < HD / 16; d += 4)
-                *(floatx4_t*)&sh.o[w][lc][Tile::o_dim(d, lg, i)] = floatx4_t{acc[c].o[d][i], acc[c].o[d + 1][i], acc[c].o[d + 2][i], acc[c].o[d + 3][i]};
-          }
-        }
-        __syncthreads();
-        const u32 here = min(16u, rows > c * 16u ? rows - c * 16u : 0u);
-        for (u32 i = threadIdx.x; i < here * HD; i += 64 * NW) {
-          const u32 row = i / HD, d = i % HD;
-          float M = -INFINITY, L = 0.f, O = 0.f;
-#pragma unroll
-          for (u32 x = 0; x < NW; ++x) M = fmaxf(M, sh.m[x][row]);
-          const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-          for (u32 x = 0; x < NW; ++x) {
-            const float f = __builtin_amdgcn_exp2f(sh.m[x][row] - ref);
-            L += sh.l[x][row] * f;
-            O += sh.o[x][row][d] * f;
-          }
-          const u32 rr = c * 16 + row;
-          if (whole) {
-            const u32 tok = rr / a.G, h = rr - tok * a.G;
-            put_out(a, cur.t0 + tok, (cur.g * a.G + h) * HD + d, L == 0.f ? 0.f : O / L);
-          } else {
-            st_past_caches(slot + ROWS * 2 + rr * HD + d, O);
-            if (d == 0) { st_past_caches(slot + rr * 2, M); st_past_caches(slot + rr * 2 + 1, L); }
-          }
-        }
-        acc[c].init();
+  };
+  Pair cur{};
+  if (u0 < u1) {
+    cur = pair_at(u0);
+    // the tile to ask for next: its unit, pair and block id (asked for a tile ahead)
+    Pair ap = cur;
+    u32 au = u0, aid = 0, ak = 0;
+    auto next_id = [&]() {
+      const u32 l = au - ap.first;
+      const u32 t = l < ap.zb ? l : ap.wlo + l - ap.zb;
+      ak = t * 16;
+      aid = ~0u;                                     // (a pair without keys has no block either)
+      if (ap.pos0 + (i32)ap.n > 0) aid = ((const_u32*)(u64)uniform_ptr(a.tables + (u64)ap.row * a.max_blocks))[t];
+    };
+    Tile tile[NT];
+    u32 k0[NT];
+    bool in_cache[NT];
+    auto ask = [&](int j) {                          // into slot j, unless the run has been asked for
+      if (au >= u1) return;
+      k0[j] = ak;
+      in_cache[j] = aid < a.n_blocks;
+      tile[j].load(a, min(aid, a.n_blocks - 1), ap.g);
+      if (++au < u1) {
+        if (au == ap.first + ap.nv) ap = pair_after(ap);
+        next_id();
       }
-      if (!whole) {
-        // every store has been written past the caches before the count; the last workgroup adds the pieces up (see merge_chunks)
-        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        __syncthreads();
-        const u32 w0 = first / quantum, np = (first + cur.nv - 1) / quantum - w0 + 1;
-        if (threadIdx.x == 0) {
-          u32* const ctr = a.ctr + (u64)cur.s * a.nkv + cur.g;
-          const u32 before = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          sh.last = before == np - 1;
-          if (before == np - 1) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (__builtin_amdgcn_readfirstlane(sh.last)) {
-          auto at_piece = [&](u32 p) { return a.part + (u64)(2 * (w0 + p) + (p ? 0u : 1u)) * SLOT; };
-          for (u32 i = threadIdx.x; i < rows * HD; i += 64 * NW) {
-            const u32 rr = i / HD, d = i % HD;
-            float M = -INFINITY, L = 0.f, O = 0.f;
-            for (u32 p0 = 0; p0 < np; p0 += 8) {
-              float m[8];
+    };
+    load_q(cur);
+    next_id();
 #pragma unroll
-              for (u32 x = 0; x < 8; ++x) m[x] = ld_past_caches(at_piece(min(p0 + x, np - 1)) + rr * 2);
+    for (int j = 0; j < NT; ++j) ask(j);
+    clear();
+    for (u32 u = u0; u < u1;) {
 #pragma unroll
-              for (u32 x = 0; x < 8; ++x) M = fmaxf(M, m[x]);
+      for (int j = 0; j < NT; ++j) {
+        if (u >= u1) break;
+        const i32 p1 = cur.pos0 + (i32)cur.n - 1;
+        if (p1 >= 0) {
+          const typename Tile::Keys key = tile[j].keys();
+          typename Tile::Values val = tile[j].values();
+          const i32 k = (i32)k0[j];
+          const bool edge = !(k + 15 <= cur.pos0 && in_cache[j] && (!a.window || k > p1 - (i32)a.window || (u32)k + 16 <= a.sinks));
+          u32 vis[CT];
+#pragma unroll
+          for (int c = 0; c < CT; ++c) vis[c] = 0;
+          if (edge) {
+            if (in_cache[j]) {
+#pragma unroll
+              for (int c = 0; c < CT; ++c) vis[c] = sees(a, qpos[c], k + (i32)(lg * 4));
             }
-            const float ref = M == -INFINITY ? 0.f : M;
-            for (u32 p0 = 0; p0 < np; p0 += 8) {
-              float m[8], l[8], o[8];
-#pragma unroll
-              for (u32 x = 0; x < 8; ++x) {
-                const float* b = at_piece(min(p0 + x, np - 1));
-                m[x] = ld_past_caches(b + rr * 2); l[x] = ld_past_caches(b + rr * 2 + 1); o[x] = ld_past_caches(b + ROWS * 2 + rr * HD + d);
-              }
-#pragma unroll
-              for (u32 x = 0; x < 8; ++x) {
-                const float f = __builtin_amdgcn_exp2f(m[x] - ref);
-                L = p0 + x < np ? L + l[x] * f : L;
-                O = p0 + x < np ? O + o[x] * f : O;
-              }
-            }
-            const u32 tok = rr / a.G, h = rr - tok * a.G;
-            put_out(a, cur.t0 + tok, (cur.g * a.G + h) * HD + d, L == 0.f ? 0.f : O / L);
+            strange_values<HD, BITS, CT>(val, acc, vis);
           }
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[c].add(key, val, q[c], a.c, edge, vis[c]);
+        }
+        ask(j);
+        ++u;
+        if (u == cur.first + cur.nv) {               // the pair ends: finished here, or its beginning is another wave's
+          if (cur.first >= u0) finish(cur);
+          else leave_in_lds<HD, BITS, CT>(sh, w, acc);
+          if (u < u1) { cur = pair_after(cur); load_q(cur); }
+          clear();
         }
       }
-      if (run_ends) return;
-      u += cur.hi - cur.lo;
-      load_q(nxt);
     }
-    cur = nxt;
-    r = rn;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) { at[j] = at_next[j]; id[j] = id_next[j]; }
+    if (u1 < cur.first + cur.nv && cur.first < u0) leave_in_lds<HD, BITS, CT>(sh, w, acc);      // (the whole run inside a pair)
+  }
+  __syncthreads();
+  // The rest is a workgroup's end, once per launch. This wave's pair that goes on behind its run, if it began there; wave 0 also the
+  // pair that the workgroup's run begins inside of.
+  const u32 wg0 = wg * wg_units, wg1 = min(wg0 + wg_units, U);
+  auto others = [&](const Pair& p, u32 x) {          // what the waves from x on have of the pair
+#pragma unroll 1
+    for (; x < NW && wg0 + x * quantum < min(p.first + p.nv, wg1); ++x) add_from_lds<HD, BITS, CT>(sh, x, acc);
+  };
+  auto hand_on = [&](const Pair& p, u32 which) {     // the workgroup's share of the pair to the workspace; who comes last is told
+    leave_past_caches<HD, BITS, CT>(a.part + (u64)(2 * wg + which) * short_slot<HD, CT>(), acc, p.n * a.G);
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    const u32 np = (p.first + p.nv - 1) / wg_units - p.first / wg_units + 1;
+    if (lane == 0) {
+      u32* const ctr = a.ctr + (u64)p.s * a.nkv + p.g;
+      const u32 before = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      sh.last[which] = before == np - 1;
+      if (before == np - 1) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  };
+  if (u0 < u1 && cur.first >= u0 && u1 < cur.first + cur.nv) {
+    others(cur, w + 1);
+    if (cur.first + cur.nv <= wg1) finish(cur); else hand_on(cur, 1);
+  }
+  if (w == 0) {
+    const Pair p = pair_at(wg0);
+    if (p.first < wg0) {
+      clear();
+      others(p, 0);
+      hand_on(p, 0);
+    }
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (u32 which = 0; which < 2; ++which) {
+    if (!scalar(sh.last[which])) continue;
+    const Pair p = pair_at(which ? wg1 - 1 : wg0);
+    const u32 w0 = p.first / wg_units, np = (p.first + p.nv - 1) / wg_units - w0 + 1, per = (np + NW - 1) / NW;
+    clear();
+#pragma unroll 1
+    for (u32 x = w * per; x < min(np, (w + 1) * per); ++x)
+      add_past_caches<HD, BITS, CT>(a.part + (u64)(2 * (w0 + x) + (x ? 0u : 1u)) * short_slot<HD, CT>(), acc, p.n * a.G);
+    leave_in_lds<HD, BITS, CT>(sh, w, acc);
+    __syncthreads();
+    if (w == 0) {
+      clear();
+#pragma unroll 1
+      for (u32 x = 0; x < NW; ++x) add_from_lds<HD, BITS, CT>(sh, x, acc);
+      finish(p);
+    }
+    __syncthreads();
   }
 }
 
@@ -858,6 +921,6 @@ __device__ __forceinline__ void prompt_merge(const PagedArgs& a, PromptMergeShar
     }
     const u32 rr = it.r0 + r, tok = rr / a.G, h = rr - tok * a.G;
 #pragma unroll
-    for (int d = 0; d < HD / 64; ++d) put_out(a, it.t0 + tok, (it.g * a.G + h) * HD + d * 64 + lane, L == 0.f ? 0.f : O[d] / L);
+    for (int d = 0; d < HD / 64; ++d) *out_at(a, it.t0 + tok, (it.g * a.G + h) * HD + d * 64 + lane) = (f16_t)half_pair(L == 0.f ? 0.f : O[d] / L, 0.f);
   }
 }
