@@ -221,6 +221,19 @@ enum {
  * afterwards; of the measurement helpers only blink_calibration_rates allocates (and frees) buffers of its own. */
 int blink_init(const blink_config* cfg, blink_engine** out);
 
+/* blink_init of models whose attention is of another kind, or whose KV cache is smaller (the paper fixes neither); bf16 models only.
+ * Null options, or all zeros: blink_init. With any of them the rotary embedding and the KV write are a kernel of their own behind
+ * the QKV projection (phase 3 of blink_time_phase), and the attention is blink_paged_attention's (phase 4); every mode of the scheduler,
+ * the flags and the results of the other calls are as without. All blocks of a context stay allocated, those behind a window too. */
+typedef struct {
+  uint32_t qk_norm;            /* 1: queries and keys are normed per head ahead of the rotation, x / sqrt(mean(x^2) + rms_eps) * gain. The
+                                  weights then have, behind wv of every layer, gq[head_dim] gk[head_dim], fp32 */
+  uint32_t window, sinks;      /* window > 0: a position sees itself, the window - 1 positions before it and the first `sinks` ones */
+  uint32_t kv_bits;            /* 0 or 16: halves; 4: the cache holds e2m1 codes with a power-of-two scale per 32 dimensions of a
+                                  token's key or value (blink_kv_cache): 17 / 64 of the bytes */
+} blink_attention_options;
+int blink_init_attention(const blink_config* cfg, const blink_attention_options* options, blink_engine** out);
+
 /* Ring write (section 4.4 "RDMA datapath"): copies the descriptor and the prompt into the slot of the next
  * ticket, then sets the slot state to PREFILL_PENDING. request_id_out receives the ticket (0,1,2,.. in
  * submission order, which is the FCFS order). BLINK_ERR_FULL when that slot has not been emptied yet. */
@@ -268,7 +281,7 @@ int blink_debug_read(blink_engine* e, uint32_t what, void* buf, uint64_t cap_byt
  * chunks (13 to 15: no kernels); a mixture-of-experts model runs, in place of 7 and 8: 16 router GEMM, 17 expert selection, 18 grouped gate/up GEMMs,
  * 19 grouped down GEMMs, 20 weighted sum + residual, and 21 (between 17 and 18) the experts' operand gathered by
  * expert; -1 none). There
- * are no kernels for phases 1, 3, 6 and 9 (fused into the GEMMs; their time is 0). While a phase is selected, the loop
+ * are no kernels for phases 1, 6 and 9, and for 3 only with blink_init_attention's options (fused into the GEMMs; their time is 0). While a phase is selected, the loop
  * brackets every launch of that phase's kernel with HIP events on the compute stream. After the loop has
  * stopped, blink_get_phase_times returns, per iteration enqueued in the last window and in enqueue order, the
  * summed duration in milliseconds of that kernel's launches (one per layer for per-layer phases). */

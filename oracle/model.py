@@ -15,6 +15,10 @@ renormalised over the selected ones, is the same thing); the layer adds sum_j w_
 integer decision taken from floating-point values: a caller may force it (`routing`) and receives the oracle's own choice
 and its margin (`route_log`), so that a test can require agreement wherever the margin exceeds the tolerance.
 
+Attention variants (keys of the configuration, all optional): qk_norm, queries and keys are RMS-normed per head with gains gq, gk
+[hd] ahead of the rotation; window > 0, a position sees itself, the window - 1 positions before it and the first `sinks`
+ones; kv_bits = 4, cached keys and values are what their 4-bit codes stand for (oracle.paged).
+
 Three variants compute the same function:
   forward_dense: the definition. All positions at once, dense causal attention, no cache.
   CachedModel:   contiguous per-sequence KV cache, prefill then one token at a time.
@@ -23,6 +27,7 @@ Three variants compute the same function:
 """
 import numpy as np
 
+from oracle import paged
 from synth.weights import bf16_bits_to_f32
 
 
@@ -72,12 +77,20 @@ def _qkv(cfg, W, l, x, pos):
     q = (h @ W[f"l{l}.wq"].T).reshape(T, nq, hd)
     k = (h @ W[f"l{l}.wk"].T).reshape(T, nkv, hd)
     v = (h @ W[f"l{l}.wv"].T).reshape(T, nkv, hd)
-    return rope(q, pos, cfg["rope_theta"]), rope(k, pos, cfg["rope_theta"]), v
+    if cfg.get("qk_norm", 0):
+        q, k = rmsnorm(q, W[f"l{l}.gq"], cfg["rms_eps"]), rmsnorm(k, W[f"l{l}.gk"], cfg["rms_eps"])
+    q, k = rope(q, pos, cfg["rope_theta"]), rope(k, pos, cfg["rope_theta"])
+    if cfg.get("kv_bits", 16) == 4:
+        k, v = paged.decode4(*paged.encode4(k)), paged.decode4(*paged.encode4(v))
+    return q, k, v
 
 
 def _attend(cfg, q, K, V):
-    """q: [nq, hd] at the last of the positions held in K, V: [n, nkv, hd]. Softmax over all n."""
+    """q: [nq, hd] at the last of the positions held in K, V: [n, nkv, hd]. Softmax over all n, or those the window leaves."""
     nq, nkv, hd = cfg["n_q_heads"], cfg["n_kv_heads"], cfg["head_dim"]
+    if cfg.get("window", 0):
+        seen = paged.visible(len(K) - 1, cfg["window"], cfg.get("sinks", 0))
+        K, V = K[seen], V[seen]
     out = np.empty((nq, hd))
     for h in range(nq):
         kvh = h // (nq // nkv)
@@ -142,6 +155,8 @@ def forward_dense(cfg, W, tokens, all_positions=True):
     nq, nkv, hd = cfg["n_q_heads"], cfg["n_kv_heads"], cfg["head_dim"]
     pos = np.arange(T)
     future = pos[None, :] > pos[:, None]
+    if cfg.get("window", 0):
+        future |= (pos[None, :] <= pos[:, None] - cfg["window"]) & (pos[None, :] >= cfg.get("sinks", 0))
     x = W["embed"][tokens]
     for l in range(cfg["n_layers"]):
         q, k, v = _qkv(cfg, W, l, x, pos)

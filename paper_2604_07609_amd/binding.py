@@ -11,7 +11,7 @@ FLAG_HOST_STEP = 512
 ERR_INVAL, ERR_TOO_LARGE, ERR_FULL, ERR_DEVICE, ERR_STATE = -1, -2, -3, -4, -5
 EVENT_FIRST, EVENT_LAST = 1, 2
 
-EXPORTS = ["blink_init", "blink_submit", "blink_run", "blink_set_exit_when_idle", "blink_wait", "blink_stop", "blink_poll_outputs", "blink_shutdown",
+EXPORTS = ["blink_init", "blink_init_attention", "blink_submit", "blink_run", "blink_set_exit_when_idle", "blink_wait", "blink_stop", "blink_poll_outputs", "blink_shutdown",
            "blink_get_trace", "blink_get_stats", "blink_debug_read", "blink_time_phase", "blink_get_phase_times", "blink_calibration_copy",
            "blink_calibration_rates", "blink_clock_sync", "blink_sample_rows", "blink_sample_rows_static", "blink_kv_cache_bytes", "blink_qk_norm_rope",
            "blink_kv_cache_read", "blink_paged_attention", "blink_attention_workspace_bytes", "blink_last_error"]
@@ -29,6 +29,10 @@ class Config(C.Structure):
         ("max_prefill_tokens", C.c_uint32), ("ring_slots", C.c_uint32), ("eos_token_id", C.c_int32), ("device", C.c_int32),
         ("flags", C.c_uint32), ("trace_capacity", C.c_uint32), ("idle_poll_us", C.c_uint32), ("pump_depth", C.c_uint32),
         ("tune", C.c_uint32), ("n_experts", C.c_uint32), ("n_active", C.c_uint32), ("spec_tokens", C.c_uint32)]
+
+
+class AttentionOptions(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("qk_norm", "window", "sinks", "kv_bits")]
 
 
 class Sampling(C.Structure):
@@ -94,6 +98,7 @@ def load_library():
     lib = C.CDLL(p)
     vp, u32, u64 = C.c_void_p, C.c_uint32, C.c_uint64
     lib.blink_init.argtypes = [C.POINTER(Config), C.POINTER(vp)]
+    lib.blink_init_attention.argtypes = [C.POINTER(Config), C.POINTER(AttentionOptions), C.POINTER(vp)]
     lib.blink_submit.argtypes = [vp, vp, u32, u32, C.POINTER(Sampling), C.POINTER(u64)]
     lib.blink_run.argtypes = [vp, u64]
     lib.blink_wait.argtypes = [vp]
@@ -273,7 +278,8 @@ def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace
 
 
 class Engine:
-    """One serving engine on one GPU. model/engine: dicts as in synth.configs; blob: uint8 array (synth.pack_blob)."""
+    """One serving engine on one GPU. model/engine: dicts as in synth.configs (model: also qk_norm, window, sinks, kv_bits of
+    blink_attention_options); blob: uint8 array (synth.pack_blob)."""
 
     def __init__(self, model, engine, blob, flags=0, device=0, trace_capacity=0, idle_poll_us=0, pump_depth=0, tune=0):
         self.lib = load_library()
@@ -299,7 +305,8 @@ class Engine:
         cfg.pump_depth, cfg.tune = pump_depth, tune
         cfg.n_experts, cfg.n_active = model.get("n_experts", 0), model.get("n_active", 0)
         self.h = C.c_void_p()
-        _check(self.lib, self.lib.blink_init(C.byref(cfg), C.byref(self.h)))
+        opt = AttentionOptions(*(int(model.get(k, 0)) for k in ("qk_norm", "window", "sinks", "kv_bits")))
+        _check(self.lib, self.lib.blink_init_attention(C.byref(cfg), C.byref(opt), C.byref(self.h)))
 
     def submit(self, prompt, max_new_tokens, temperature=0.0, top_k=0, top_p=1.0, seed=0):
         p = np.ascontiguousarray(prompt, dtype=np.int32)

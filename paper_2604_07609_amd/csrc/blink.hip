@@ -3,6 +3,7 @@
 #include "../../include/blink.h"
 #include "blink_device.h"
 #include "phase_kernels.h"
+#include "paged_kernels.h"
 
 #include <algorithm>
 #include <atomic>
@@ -58,6 +59,20 @@ static phase_kernel_t phase_kernel(int ph, bool f32) {
     case PH_MOE_PERMUTE: return k_moe_permute;
     default: return k_sample_publish;
   }
+}
+
+// the kernels of an engine whose rotation and KV write are a phase of their own (DevCtx::paged)
+template <int HD, int BITS>
+static phase_kernel_t paged_phase_kernel(int ph, bool more) {
+  if (ph == PH_QKV) return k_qkv_plain;
+  if (ph == PH_ROPE) return k_store_phase<HD, BITS>;
+  return more ? k_attention_phase<HD, BITS, SHORT_MORE(HD)> : k_attention_phase<HD, BITS, 1>;
+}
+static phase_kernel_t engine_kernel(const DevCtx& c, int ph) {
+  if (!c.paged || (ph != PH_QKV && ph != PH_ROPE && ph != PH_ATTN)) return phase_kernel(ph, c.dtype == 0);
+  const bool more = c.nq / c.nkv * (1 + c.spec_k) > 16;       // drafts: more rows than one tile of them
+  if (c.hd == 64) return c.kv_bits == 4 ? paged_phase_kernel<64, 4>(ph, more) : paged_phase_kernel<64, 16>(ph, more);
+  return c.kv_bits == 4 ? paged_phase_kernel<128, 4>(ph, more) : paged_phase_kernel<128, 16>(ph, more);
 }
 
 // (cos, sin) of pos * theta^(-2i/hd), evaluated in fp64 and rounded once
@@ -387,12 +402,12 @@ static int halloc(blink_engine* e, T** p, u64 count) {
   return 0;
 }
 
-static u64 expected_weight_bytes(const blink_config* c) {
+static u64 expected_weight_bytes(const blink_config* c, const blink_attention_options& o) {
   const u64 es = c->dtype == 1 ? 2 : 4;
   const u64 d = c->d_model, hd = c->head_dim, nq = c->n_q_heads, nkv = c->n_kv_heads, F = c->d_ffn, V = c->vocab;
   const u64 E = c->n_experts;
   const u64 ffn = E ? E * d + E * 3 * F * d : 3 * F * d;   // router and E experts, or the one dense FFN
-  const u64 per_layer = 4 * d + 4 * d + es * ((nq + 2 * nkv) * hd * d + d * nq * hd + ffn);
+  const u64 per_layer = 4 * d + 4 * d + (o.qk_norm ? 2 * 4 * hd : 0) + es * ((nq + 2 * nkv) * hd * d + d * nq * hd + ffn);
   return es * V * d * 2 + c->n_layers * per_layer + 4 * d;
 }
 
@@ -411,7 +426,7 @@ static void free_all(blink_engine* e) {
 
 static int build_graph(blink_engine* e);
 
-static int init_impl(const blink_config* cfg, blink_engine* e) {
+static int init_impl(const blink_config* cfg, const blink_attention_options& opt, blink_engine* e) {
   HIPCHK(hipSetDevice(cfg->device));
   hipDeviceProp_t prop;
   HIPCHK(hipGetDeviceProperties(&prop, cfg->device));
@@ -436,6 +451,8 @@ static int init_impl(const blink_config* cfg, blink_engine* e) {
   c.spec_k = (cfg->flags & BLINK_FLAG_SPECULATIVE) ? cfg->spec_tokens : 0u;
   const u64 rows_cap = (u64)c.max_batch * (c.spec_k + 1);
   c.maxT = std::max<u32>(c.maxT, (u32)rows_cap);
+  c.window = opt.window; c.sinks = opt.sinks; c.kv_bits = opt.kv_bits ? opt.kv_bits : 16;
+  c.paged = opt.qk_norm || opt.window || c.kv_bits == 4;
   const u64 es = c.dtype == 1 ? 2 : 4;
 
   // ---- ring ----
@@ -588,16 +605,22 @@ static int init_impl(const blink_config* cfg, blink_engine* e) {
       };
       auto all = [&]() -> int {
         if (int rc = dalloc(e, &embed, 2 * V * d, false)) return rc;
-        if (int rc = dalloc(e, &gains, (2 * (u64)c.n_layers + 1) * d, false)) return rc;
+        const u64 n_gains = (2 * (u64)c.n_layers + 1) * d, n_head_gains = opt.qk_norm ? 2 * hd * c.n_layers : 0;
+        if (int rc = dalloc(e, &gains, n_gains + n_head_gains, false)) return rc;
         HIPCHK(hipMemcpy(embed, hsrc + off, 2 * V * d, hipMemcpyHostToDevice));
         c.embed = embed; off += 2 * V * d;
-        e->weight_bytes = 2 * V * d + (2 * (u64)c.n_layers + 1) * d * 4;
+        e->weight_bytes = 2 * V * d + (n_gains + n_head_gains) * 4;
         for (u32 l = 0; l < c.n_layers; ++l) {
           float* g1 = gains + (2 * (u64)l) * d;
           float* g2 = g1 + d;
           HIPCHK(hipMemcpy(g1, hsrc + off, 4 * d, hipMemcpyHostToDevice)); off += 4 * d;
-          if (int rc = pack(off, c.qkv_n, c.d, 0, c.hd, &lp[l].wqkv)) return rc;
+          if (int rc = pack(off, c.qkv_n, c.d, 0, c.paged ? 0 : c.hd, &lp[l].wqkv)) return rc;
           off += 2 * (nq + 2 * nkv) * hd * d;
+          if (opt.qk_norm) {
+            float* gq = gains + n_gains + 2 * (u64)l * hd;
+            HIPCHK(hipMemcpy(gq, hsrc + off, 2 * 4 * hd, hipMemcpyHostToDevice)); off += 2 * 4 * hd;
+            lw[l].gq = gq; lw[l].gk = gq + hd;
+          }
           if (int rc = pack(off, c.d, c.nq * c.hd, 0, 0, &lp[l].wo)) return rc;
           off += 2 * d * nq * hd;
           HIPCHK(hipMemcpy(g2, hsrc + off, 4 * d, hipMemcpyHostToDevice)); off += 4 * d;
@@ -671,7 +694,8 @@ static int init_impl(const blink_config* cfg, blink_engine* e) {
     } else if (int rc = dalloc(e, &c.hq, tile_tokens * k_pad(c.F))) return rc;
     if (int rc = dalloc(e, &c.ssq, tile_tokens * (c.d / 16))) return rc;
     {
-      const std::vector<GemmPlan> plan = gemm_plan_table(c.maxT, c.qkv_n, c.d, c.nq * c.hd, c.F, c.V, c.n_experts != 0, (u32)e->n_cu, cfg->tune);
+      const std::vector<GemmPlan> plan = gemm_plan_table(c.maxT, c.qkv_n, c.d, c.nq * c.hd, c.F, c.V, c.n_experts != 0, (u32)e->n_cu, cfg->tune,
+                                                         c.paged ? EPI_SCALED_STORE : EPI_QKV_ROPE);
       u64* dev;
       static_assert(sizeof(GemmPlan) == 8, "an entry is one word");
       if (int rc = dalloc(e, &dev, plan.size())) return rc;
@@ -697,12 +721,18 @@ static int init_impl(const blink_config* cfg, blink_engine* e) {
       if (int rc = dalloc(e, &c.attn_merge_ctr, (u64)c.max_batch * c.nkv)) return rc;
     }
   }
+  if (c.paged) {
+    if (int rc = dalloc(e, &c.qkv, (u64)c.maxT * c.qkv_n, false)) return rc;
+    if (int rc = dalloc(e, &c.paged_ctr, (u64)c.max_batch * c.nkv + 2)) return rc;
+    if (int rc = dalloc(e, &c.paged_part, 2ull * e->n_cu * SHORT_MORE(c.hd) * (128 + 16 * c.hd), false)) return rc;
+  }
   if (int rc = dalloc(e, &e->calib_src, e->calib_bytes)) return rc;
   if (int rc = dalloc(e, &e->calib_dst, e->calib_bytes)) return rc;
   // ---- KV pool ----
   c.kv_kv_stride = (u64)c.n_blocks * c.nkv * c.bs * c.hd;
   c.kv_layer_stride = 2 * c.kv_kv_stride;
-  e->kv_bytes = (u64)c.n_layers * c.kv_layer_stride * es;
+  c.kv_layer_bytes = c.kv_bits == 4 ? (u64)c.n_blocks * c.nkv * 17 * c.hd : c.kv_layer_stride * es;
+  e->kv_bytes = (u64)c.n_layers * c.kv_layer_bytes;
   char* kv;
   if (int rc = dalloc(e, &kv, e->kv_bytes, true)) return rc;   // zeroed: masked keys multiply cached values by 0
   c.kv = kv;
@@ -737,9 +767,12 @@ static int init_impl(const blink_config* cfg, blink_engine* e) {
   return 0;
 }
 
-extern "C" int blink_init(const blink_config* cfg, blink_engine** out) {
+extern "C" int blink_init(const blink_config* cfg, blink_engine** out) { return blink_init_attention(cfg, nullptr, out); }
+
+extern "C" int blink_init_attention(const blink_config* cfg, const blink_attention_options* options, blink_engine** out) {
   g_err.clear();
   if (!cfg || !out) return fail(BLINK_ERR_INVAL, "null argument");
+  const blink_attention_options opt = options ? *options : blink_attention_options{};
   *out = nullptr;
   if (!cfg->weights) return fail(BLINK_ERR_INVAL, "weights is null");
   if (cfg->dtype > 1) return fail(BLINK_ERR_INVAL, "dtype must be 0 (fp32) or 1 (bf16)");
@@ -760,6 +793,10 @@ extern "C" int blink_init(const blink_config* cfg, blink_engine** out) {
     if (cfg->n_experts > MOE_MAX_EXPERTS || !cfg->n_active || cfg->n_active > MOE_MAX_ACTIVE || cfg->n_active > cfg->n_experts)
       return fail(BLINK_ERR_INVAL, "n_experts must be at most %d and n_active in [1, min(%d, n_experts)]", MOE_MAX_EXPERTS, MOE_MAX_ACTIVE);
   }
+  if (opt.kv_bits != 0 && opt.kv_bits != 4 && opt.kv_bits != 16) return fail(BLINK_ERR_INVAL, "kv_bits must be 16 or 4");
+  if (opt.sinks && !opt.window) return fail(BLINK_ERR_INVAL, "sinks without a window");
+  if (opt.window > (1u << 30) || opt.sinks > (1u << 30)) return fail(BLINK_ERR_INVAL, "window and sinks must be at most 2^30");
+  if ((opt.qk_norm || opt.window || opt.kv_bits) && cfg->dtype != 1) return fail(BLINK_ERR_INVAL, "per-head norms, windows and kv_bits are built for dtype 1 (bf16 weights) only");
   if (cfg->vocab >= (1u << 24)) return fail(BLINK_ERR_INVAL, "vocab must be below 2^24");
   if (cfg->kv_block_size != 16) return fail(BLINK_ERR_INVAL, "kv_block_size must be 16");
   if (!cfg->kv_num_blocks || !cfg->max_batch || cfg->max_batch > SCHED_MAX_BATCH)
@@ -781,16 +818,16 @@ extern "C" int blink_init(const blink_config* cfg, blink_engine** out) {
       return fail(BLINK_ERR_INVAL, "speculative decoding: spec_tokens must be in [1, %u]", SPEC_MAX_DRAFTS - 1);
   }
   if (!cfg->ring_slots || (cfg->ring_slots & (cfg->ring_slots - 1))) return fail(BLINK_ERR_INVAL, "ring_slots must be a power of two");
-  if (cfg->weights_bytes != expected_weight_bytes(cfg))
+  if (cfg->weights_bytes != expected_weight_bytes(cfg, opt))
     return fail(BLINK_ERR_INVAL, "weights_bytes is %llu, the model needs %llu", (unsigned long long)cfg->weights_bytes,
-                (unsigned long long)expected_weight_bytes(cfg));
+                (unsigned long long)expected_weight_bytes(cfg, opt));
   int n_dev = 0;
   if (hipGetDeviceCount(&n_dev) != hipSuccess || n_dev <= 0) return fail(BLINK_ERR_DEVICE, "no HIP device available");
   if (cfg->device < 0 || cfg->device >= n_dev) return fail(BLINK_ERR_INVAL, "device %d out of range", cfg->device);
   blink_engine* e = new blink_engine(cfg->ring_slots);
   e->cfg = *cfg;
   e->cfg.weights = nullptr;
-  const int rc = init_impl(cfg, e);
+  const int rc = init_impl(cfg, opt, e);
   if (rc) {
     const std::string keep = g_err;
     free_all(e);
@@ -864,7 +901,8 @@ static int launch_phase(blink_engine* e, const DevCtx& ctx, hipStream_t st, int 
   const bool bf16 = e->ctx.dtype == 1;
   const bool down_f32 = !bf16 && ph == PH_DOWN;
   const u32 threads = down_f32 ? 64u * F32_DOWN_WAVES : bf16 && (gemm || ph == PH_ATTN) ? 512u : (u32)BLK_THREADS;
-  HIPCHK(launch(phase_kernel(ph, !bf16), (bf16 && gemm) || down_f32 ? (u32)e->n_cu : e->grid, threads, st, ctx, layer));
+  const bool one_per_cu = (bf16 && gemm) || down_f32 || (ctx.paged && ph == PH_ATTN);
+  HIPCHK(launch(engine_kernel(ctx, ph), one_per_cu ? (u32)e->n_cu : e->grid, threads, st, ctx, layer));
   if (timed) HIPCHK(hipEventRecord(b, st));
   return 0;
 }
@@ -882,13 +920,14 @@ static int enqueue_iteration_kernels(blink_engine* e, hipStream_t st, u64 enq_in
   if (c.spec_k) HIPCHK(launch(k_spec_draft, (c.max_batch + 3) / 4, BLK_THREADS, st, c));
   HIPCHK(launch(k_sched, 1, BLK_THREADS, st, c));
   if (int rc = launch_phase(e, c, st, PH_EMBED, 0, enq_index)) return rc;
-  // the phases of a layer; the norms and the rotary step have no kernels of their own
-  static const int dense[] = {PH_QKV, PH_ATTN, PH_ATTN_COMBINE, PH_OPROJ, PH_GATEUP, PH_DOWN};
-  static const int experts[] = {PH_QKV, PH_ATTN, PH_ATTN_COMBINE, PH_OPROJ, PH_ROUTER, PH_ROUTE, PH_MOE_PERMUTE, PH_MOE_GATEUP, PH_MOE_DOWN, PH_MOE_COMBINE};
+  // the phases of a layer; the norms have no kernels of their own, the rotary step only in some models
+  static const int dense[] = {PH_QKV, PH_ROPE, PH_ATTN, PH_ATTN_COMBINE, PH_OPROJ, PH_GATEUP, PH_DOWN};
+  static const int experts[] = {PH_QKV, PH_ROPE, PH_ATTN, PH_ATTN_COMBINE, PH_OPROJ, PH_ROUTER, PH_ROUTE, PH_MOE_PERMUTE, PH_MOE_GATEUP, PH_MOE_DOWN, PH_MOE_COMBINE};
   const int *const chain = c.n_experts ? experts : dense, n = (int)(c.n_experts ? sizeof experts : sizeof dense) / (int)sizeof(int);
   for (u32 l = 0; l < c.n_layers; ++l)
     for (int i = 0; i < n; ++i) {
-      if (chain[i] == PH_ATTN_COMBINE && (c.dtype == 0 || kind != CHAIN_MERGE_KERNEL)) continue;
+      if (chain[i] == PH_ATTN_COMBINE && (c.dtype == 0 || c.paged || kind != CHAIN_MERGE_KERNEL)) continue;
+      if (chain[i] == PH_ROPE && !c.paged) continue;
       if (int rc = launch_phase(e, c, st, chain[i], l, enq_index)) return rc;
     }
   if (int rc = launch_phase(e, c, st, PH_LM_HEAD, 0, enq_index)) return rc;
@@ -909,11 +948,11 @@ static int capture_chain(blink_engine* e, Chain kind, hipGraphExec_t* out) {
 
 static int build_graph(blink_engine* e) {
   // The chain for whole contexts exists where the scheduler can make whole contexts the items of every decode iteration: bf16
-  // models in the plain mode, unless the tuning word forces chunk items or the static kernel (bits 15, 23) or rules
+  // models with the engine's own attention in the plain mode, unless the tuning word forces chunk items or the static kernel (bits 15, 23) or rules
   // the chain out (bit 5). The one that merges in the attention kernel exists in every mode (not with bits 5 and 23).
   const u32 ext = BLINK_FLAG_CHUNKED_PREFILL | BLINK_FLAG_PREEMPTION | BLINK_FLAG_PREFIX_CACHE | BLINK_FLAG_SPECULATIVE;
-  e->whole_chain_ok = e->ctx.dtype == 1 && e->ctx.chunk_rec && !(e->cfg.flags & ext) && !(e->cfg.tune & 0x808020u);
-  e->merge_in_ok = e->ctx.dtype == 1 && e->ctx.chunk_rec && !(e->cfg.tune & 0x800020u);
+  e->whole_chain_ok = e->ctx.dtype == 1 && !e->ctx.paged && e->ctx.chunk_rec && !(e->cfg.flags & ext) && !(e->cfg.tune & 0x808020u);
+  e->merge_in_ok = e->ctx.dtype == 1 && !e->ctx.paged && e->ctx.chunk_rec && !(e->cfg.tune & 0x800020u);
   if (e->cfg.flags & BLINK_FLAG_NO_GRAPH) return 0;
   // (the one with the merge kernel is never taken where the attention kernel merges whatever the number of items)
   if (!e->merge_in_ok || !((e->cfg.tune & 0x8u) || merge_in_attention(~0u, e->ctx.hd, (u32)e->n_cu)))

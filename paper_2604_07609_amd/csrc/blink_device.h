@@ -214,6 +214,7 @@ struct LayerW {
   const void* wqkv;     // [ (nq+2nkv)*hd ][d]
   const void* wo;       // [d][nq*hd]
   const float* g2;
+  const float *gq, *gk; // [hd] gains of the per-head norms (null: none)
   const void* wgu;      // [2F][d]: gate rows then up rows
   const void* wd;       // [d][F]
 };
@@ -331,6 +332,12 @@ struct DevCtx {
   // decode attention: partial (max, sum, output) of every chunk of a context longer than one chunk
   float* attn_part_o;   // [chunk][kv head][G][hd]
   float* attn_part_ml;  // [chunk][kv head][G][2]
+  // models with per-head norms, a window or a 4-bit cache (blink_init_attention): the QKV projection leaves fp32 rows in qkv, the store kernel
+  // norms, rotates and stores them, and the attention is that of paged_attention.h
+  u32 paged, window, sinks, kv_bits;
+  u64 kv_layer_bytes;   // of the KV pool
+  u32* paged_ctr;       // [max_batch][nkv] + 2 (zeros between launches)
+  float* paged_part;    // results of sequences that several workgroups share
   u32* attn_merge_ctr;  // [max_batch][nkv] chunks of a context that are done, where the attention kernel merges them itself (zeros between launches)
 };
 

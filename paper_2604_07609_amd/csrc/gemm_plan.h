@@ -103,11 +103,11 @@ static inline unsigned char gemm_plan(int epi, u32 N, u32 K, u32 T, bool ordered
 // The table: an entry per token count up to 64 and one per 64 tokens beyond (every tile is a multiple of 64 tokens wide), for as many tokens
 // as an iteration can have. No entry serves any other count: K in slices holds only while there is at most one item per compute unit.
 constexpr u32 gemm_plan_entry(u32 T) { return T <= 64 ? T : 64 + (T - 1) / 64; }
-static inline std::vector<GemmPlan> gemm_plan_table(u32 max_tokens, u32 qkv_rows, u32 d, u32 q_width, u32 F, u32 V, bool experts, u32 ncu, u32 tune) {
+static inline std::vector<GemmPlan> gemm_plan_table(u32 max_tokens, u32 qkv_rows, u32 d, u32 q_width, u32 F, u32 V, bool experts, u32 ncu, u32 tune, int qkv_epi = EPI_QKV_ROPE) {
   std::vector<GemmPlan> plan(gemm_plan_entry(max_tokens) + 1);
   for (u32 i = 1; i < plan.size(); ++i) {
     const u32 t = i <= 64 ? i : (i - 64) * 64 + 1;
-    plan[i].qkv = gemm_plan(EPI_QKV_ROPE, qkv_rows, d, t, experts, ncu, tune);
+    plan[i].qkv = gemm_plan(qkv_epi, qkv_rows, d, t, experts, ncu, tune);
     plan[i].oproj = gemm_plan(EPI_RESIDUAL, d, q_width, t, experts, ncu, tune);
     plan[i].gateup = gemm_plan(EPI_SILU_GATE, 2 * F, d, t, false, ncu, tune);
     plan[i].down = gemm_plan(EPI_RESIDUAL, d, F, t, experts, ncu, tune);

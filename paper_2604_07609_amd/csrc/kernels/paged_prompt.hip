@@ -1,10 +1,10 @@
 // attention over the paged cache, many rows per sequence
 #include "../paged_kernels.h"
 
-#define PROMPT_KERNEL(HD, BITS)                                                                                                                 \
-  template <> __global__ void __launch_bounds__(512) __attribute__((amdgpu_num_vgpr(120))) k_paged_prompt<HD, BITS>(PagedArgs a) {                \
-    __shared__ PromptShared sh;                                                                                                                 \
-    paged_prompt<HD, BITS>(a, sh, blockIdx.x, gridDim.x);                                                                                       \
+#define PROMPT_KERNEL(HD, BITS)                                                                        \
+  template <> __global__ void PAGED_BOUNDS k_paged_prompt<HD, BITS>(PagedArgs a) {                     \
+    __shared__ PromptShared sh;                                                                        \
+    paged_prompt<HD, BITS>(a, sh, blockIdx.x, gridDim.x, false);                                       \
   }
 PROMPT_KERNEL(64, 16)
 PROMPT_KERNEL(128, 16)

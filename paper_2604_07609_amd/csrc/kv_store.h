@@ -292,6 +292,12 @@ __device__ __forceinline__ void store_values4(const StoreArgs& a, u32 wg) {
   if (j % 4 == 0) rec[16 * HD + HD / 2 + j / 4 * 16 + off] = fine ? (unsigned char)(e + 127) : (unsigned char)255;
 }
 
+// tokens of a wave of the values' part: as many as there are when the chip has waves enough, else few, so that there are
+__host__ __device__ __forceinline__ u32 store_group(u32 T, u32 nkv, u32 n_cu) {
+  u32 g = STORE_GROUP;
+  while (g > 4 && (u64)T * nkv / g < 8ull * n_cu) g /= 2;
+  return g;
+}
 // workgroups of the values' part (they come first: theirs are the longer chains) and of the rows' part
 __host__ __device__ __forceinline__ u32 store_value_wgs(u32 T, u32 nkv, u32 hd, u32 bits, u32 group) {
   return bits == 16 ? ((T + group - 1) / group * nkv + 3) / 4 : (T * nkv + 2048 / hd - 1) / (2048 / hd);

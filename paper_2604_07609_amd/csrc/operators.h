@@ -62,13 +62,6 @@ static hipError_t launch_store(const StoreArgs& s, u32 hd, u32 bits, u32 grid, h
   if (hd == 64) return bits == 16 ? launch(k_kv_store<T, 64, 16>, grid, BLK_THREADS, st, s) : launch(k_kv_store<T, 64, 4>, grid, BLK_THREADS, st, s);
   return bits == 16 ? launch(k_kv_store<T, 128, 16>, grid, BLK_THREADS, st, s) : launch(k_kv_store<T, 128, 4>, grid, BLK_THREADS, st, s);
 }
-// tokens of a wave of the values' part: as many as there are when the chip has waves enough, else few, so that there are
-static u32 store_group(u32 T, u32 nkv, u32 n_cu) {
-  u32 g = STORE_GROUP;
-  while (g > 4 && (u64)T * nkv / g < 8ull * n_cu) g /= 2;
-  return g;
-}
-
 extern "C" int blink_qk_norm_rope(int32_t device, const blink_qk_norm_rope_args* a, void* stream) {
   g_err.clear();
   if (!a) return fail(BLINK_ERR_INVAL, "null argument");
@@ -124,15 +117,15 @@ extern "C" int blink_kv_cache_read(int32_t device, const blink_kv_cache* c, cons
 // ---- attention ------------------------------------------------------------------------------------------------------------------
 // Which kernels a call takes, from what the host knows: its longest run of queries, and not which sequences have it.
 struct PagedPlan {
-  u32 ct;                 // row tiles of the short part (0: it is not launched)
+  u32 ct;                 // row tiles of the short part (0: there is none)
   u32 short_rows;         // sequences with at most so many rows are its
-  bool prompt;            // the prompt part is launched
-  u32 short_wgs, prompt_wgs, n_splits;
-  u64 ctr_bytes, part_bytes;
+  bool prompt;            // there is a prompt part (with a short one: in one launch)
+  u32 wgs, n_splits;
+  u64 ctr_bytes, part_bytes, prompt_bytes;
 };
 static PagedPlan paged_plan(u32 hd, u32 nq, u32 nkv, u32 n_seqs, u32 n_tokens, u32 max_q, u32 key_steps, u32 n_cu) {
   PagedPlan p{};
-  const u32 G = nq / nkv, most = hd == 64 ? 64u : 32u;       // rows that the short part's registers hold
+  const u32 G = nq / nkv, most = 16u * SHORT_MORE(hd);       // rows that the short part's registers hold
   const u64 rows = (u64)max_q * G;
   if (rows <= most) { p.ct = rows <= 16 ? 1 : most / 16; p.short_rows = 16 * p.ct; }
   else {
@@ -140,14 +133,13 @@ static PagedPlan paged_plan(u32 hd, u32 nq, u32 nkv, u32 n_seqs, u32 n_tokens, u
     p.prompt = true;
     if (G <= 16 && n_tokens < (u64)n_seqs * max_q) { p.ct = 1; p.short_rows = 16; }
   }
-  p.short_wgs = n_cu;
-  p.prompt_wgs = n_cu;
+  p.wgs = n_cu;
   // parts of 256 keys at least, where the items are too few for the chip
-  const bool few = (u64)n_tokens * G / PROMPT_ROWS * nkv < p.prompt_wgs;
+  const bool few = (u64)n_tokens * G / PROMPT_ROWS * nkv < p.wgs;
   p.n_splits = p.prompt && few ? std::max(1u, key_steps / 4) : 1u;
   p.ctr_bytes = (((u64)n_seqs * nkv + 2) * 4 + 255) / 256 * 256;
-  const u64 short_part = p.ct ? 2ull * p.short_wgs * p.ct * (128 + 16 * hd) * 4 : 0, prompt_part = p.prompt ? (u64)p.prompt_wgs * PROMPT_SLOT(hd) * 4 : 0;
-  p.part_bytes = std::max(short_part, prompt_part);
+  p.part_bytes = 2ull * p.wgs * p.ct * (128 + 16 * hd) * 4;
+  p.prompt_bytes = p.prompt ? (u64)p.wgs * PROMPT_SLOT(hd) * 4 : 0;
   return p;
 }
 static int paged_check(const blink_kv_cache& c, u32 nq, u32 n_seqs, u32 max_q) {
@@ -164,30 +156,17 @@ extern "C" int blink_attention_workspace_bytes(int32_t device, const blink_kv_ca
   if (int rc = paged_check(*c, n_q_heads, n_seqs, max_q)) return rc;
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  // (n_tokens below n_seqs * max_q: the larger of the two kinds of launches)
+  // (n_tokens below n_seqs * max_q: the larger of the two kinds of launches; and what a smaller max_q would need)
   const PagedPlan p = paged_plan(c->head_dim, n_q_heads, c->n_kv_heads, n_seqs, 0, max_q, 1, n_cu);
-  *bytes = p.ctr_bytes + p.part_bytes;
+  *bytes = p.ctr_bytes + std::max<u64>(p.part_bytes + p.prompt_bytes, 2ull * p.wgs * SHORT_MORE(c->head_dim) * (128 + 16 * c->head_dim) * 4);
   return BLINK_OK;
 }
 
 template <int HD, int BITS>
-static hipError_t launch_short(const PagedArgs& p, u32 ct, u32 grid, hipStream_t st) {
-  constexpr int MORE = HD == 64 ? 4 : 2;
-  return ct == 1 ? launch(k_paged_short<HD, BITS, 1>, grid, 512, st, p) : launch(k_paged_short<HD, BITS, MORE>, grid, 512, st, p);
-}
-static hipError_t launch_paged(const PagedArgs& args, const PagedPlan& plan, u32 hd, u32 bits, hipStream_t st) {
-  if (plan.ct) {
-    const hipError_t e = hd == 64 ? (bits == 16 ? launch_short<64, 16>(args, plan.ct, plan.short_wgs, st) : launch_short<64, 4>(args, plan.ct, plan.short_wgs, st))
-                                  : (bits == 16 ? launch_short<128, 16>(args, plan.ct, plan.short_wgs, st) : launch_short<128, 4>(args, plan.ct, plan.short_wgs, st));
-    if (e != hipSuccess) return e;
-  }
-  if (plan.prompt) {
-    const hipError_t e = hd == 64 ? (bits == 16 ? launch(k_paged_prompt<64, 16>, plan.prompt_wgs, 512, st, args) : launch(k_paged_prompt<64, 4>, plan.prompt_wgs, 512, st, args))
-                                  : (bits == 16 ? launch(k_paged_prompt<128, 16>, plan.prompt_wgs, 512, st, args) : launch(k_paged_prompt<128, 4>, plan.prompt_wgs, 512, st, args));
-    if (e != hipSuccess) return e;
-    if (plan.n_splits > 1) return hd == 64 ? launch(k_paged_merge<64>, plan.prompt_wgs, 512, st, args, plan.prompt_wgs) : launch(k_paged_merge<128>, plan.prompt_wgs, 512, st, args, plan.prompt_wgs);
-  }
-  return hipSuccess;
+static hipError_t launch_paged(const PagedArgs& args, const PagedPlan& plan, hipStream_t st) {
+  if (!plan.prompt) return plan.ct == 1 ? launch(k_paged_short<HD, BITS, 1>, plan.wgs, 512, st, args) : launch(k_paged_short<HD, BITS, SHORT_MORE(HD)>, plan.wgs, 512, st, args);
+  const hipError_t e = plan.ct ? launch(k_paged_both<HD, BITS>, plan.wgs, 512, st, args) : launch(k_paged_prompt<HD, BITS>, plan.wgs, 512, st, args);
+  return e == hipSuccess && plan.n_splits > 1 ? launch(k_paged_merge<HD>, plan.wgs, 512, st, args, plan.wgs) : e;
 }
 
 extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention_args* a, void* stream) {
@@ -212,8 +191,8 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   const u64 reach = a->window ? (u64)a->window + a->max_q + a->sinks : ~0ull;
   const u32 key_steps = (u32)std::min<u64>(a->max_blocks / 4 + 1, reach / 64 + 3);
   const PagedPlan plan = paged_plan(hd, a->n_q_heads, nkv, a->n_seqs, a->n_tokens, a->max_q, key_steps, n_cu);
-  if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.ctr_bytes + plan.part_bytes)
-    return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)(plan.ctr_bytes + plan.part_bytes));
+  if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.ctr_bytes + plan.part_bytes + plan.prompt_bytes)
+    return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)(plan.ctr_bytes + plan.part_bytes + plan.prompt_bytes));
   OnDevice on(device);
   HIPCHK(on.err);
   PagedArgs p{};
@@ -221,7 +200,9 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   p.tables = (const u32*)a->block_tables; p.cache = a->cache.data; p.n_blocks = a->cache.n_blocks; p.max_blocks = a->max_blocks;
   p.nq = a->n_q_heads; p.nkv = nkv; p.G = p.nq / nkv; p.n_seqs = a->n_seqs; p.n_tokens = a->n_tokens; p.max_q = a->max_q;
   p.window = a->window; p.sinks = a->sinks; p.c = a->scale * 1.44269504088896340736f; p.short_rows = plan.short_rows; p.n_splits = plan.n_splits;
-  p.ctr = (u32*)a->workspace; p.part = (float*)((char*)a->workspace + plan.ctr_bytes);
-  HIPCHK(launch_paged(p, plan, hd, a->cache.bits, (hipStream_t)stream));
+  p.ctr = (u32*)a->workspace; p.part = (float*)((char*)a->workspace + plan.ctr_bytes); p.prompt_part = p.part + plan.part_bytes / 4;
+  const hipStream_t st = (hipStream_t)stream;
+  HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_paged<64, 16>(p, plan, st) : launch_paged<64, 4>(p, plan, st))
+                  : (a->cache.bits == 16 ? launch_paged<128, 16>(p, plan, st) : launch_paged<128, 4>(p, plan, st)));
   return BLINK_OK;
 }

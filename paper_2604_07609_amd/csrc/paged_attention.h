@@ -31,7 +31,7 @@ struct PagedArgs {
   u32 short_rows;                 // sequences with at most so many rows are the short part's
   u32 n_splits;                   // most parts of a prompt item's keys
   u32* ctr;                       // zeros between launches: [n_seqs][nkv] pieces done; then next prompt item, workgroups done
-  float* part;                    // partial results
+  float *part, *prompt_part;      // partial results of the short and of the prompt part
 };
 
 // One sequence: its tokens, where its queries stand, and which blocks they see
@@ -614,7 +614,7 @@ __device__ __forceinline__ PromptItem prompt_item(const PagedArgs& a, const u32*
 }
 
 template <int HD, int BITS>
-__device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& sh, u32 wg, u32 nwg) {
+__device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& sh, u32 wg, u32 nwg, bool behind_short) {
   constexpr int CT = PROMPT_CT;
   constexpr u32 BLK = 16 * HD * 2, NB = 4, STAGE = 2 * NB * BLK, NS = BITS == 4 ? 2 : (PROMPT_RING / STAGE > 6 ? 6 : PROMPT_RING / STAGE), TPW = BLK / 1024;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
@@ -632,7 +632,15 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
   const u32 k_at[2] = {(lc >> 3) * BLK + lg * 256 + (lc >> 3) * 128 + (lc & 7) * 16, (lc >> 3) * BLK + lg * 256 + ((lc >> 3) ^ 1u) * 128 + (lc & 7) * 16};
   const u32 v_at = NB * BLK + (lg >> 1) * BLK + (lg & 1) * 256 + lc * 16;
   typedef const __attribute__((address_space(4))) u32 const_u32;
-  for (u32 turn = wg; turn < total;) {
+  // (behind the short part a workgroup may come late: then its first item comes from the counter too)
+  u32 turn = wg;
+  if (behind_short && total) {
+    if (threadIdx.x == 0) sh.next_item = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item);
+    __syncthreads();
+  }
+  while (turn < total) {
     const u32 item = turn / parts, part = turn - item * parts;
     PromptItem it = prompt_item(a, sh.pre, item);
     it.s = (u32)__builtin_amdgcn_readfirstlane(it.s); it.g = (u32)__builtin_amdgcn_readfirstlane(it.g); it.r0 = (u32)__builtin_amdgcn_readfirstlane(it.r0);
@@ -861,7 +869,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
           }
       }
     }
-    if (threadIdx.x == 0) sh.next_item = nwg + __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) sh.next_item = (behind_short ? 0u : nwg) + __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const float sum = quad_sum(l[c]);
@@ -876,7 +884,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
           }
         }
       } else if (colv[c]) {
-        float* const slot = a.part + (u64)turn * PROMPT_SLOT(HD);
+        float* const slot = a.prompt_part + (u64)turn * PROMPT_SLOT(HD);
         const u32 r = wr + c * 16 + lc;
         if (lg == 0) *(float2*)(slot + 2 * r) = make_float2(m[c], sum);
 #pragma unroll
@@ -889,7 +897,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
     __syncthreads();                                           // (read by everyone before it is written again)
   }
   // the last workgroup out leaves the counters as it found them
-  if (threadIdx.x == 0 && __hip_atomic_fetch_add(ctr + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == nwg - 1) {
+  if (total && threadIdx.x == 0 && __hip_atomic_fetch_add(ctr + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == nwg - 1) {
     __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(ctr + 1, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
@@ -906,7 +914,7 @@ __device__ __forceinline__ void prompt_merge(const PagedArgs& a, PromptMergeShar
     const u32 item = i / PROMPT_ROWS, r = i % PROMPT_ROWS;
     const PromptItem it = prompt_item(a, sh.pre, item);
     if (r >= it.rows) continue;
-    const float* const base = a.part + (u64)item * parts * PROMPT_SLOT(HD);
+    const float* const base = a.prompt_part + (u64)item * parts * PROMPT_SLOT(HD);
     float M = -INFINITY, L = 0.f, O[HD / 64];
 #pragma unroll
     for (int d = 0; d < HD / 64; ++d) O[d] = 0.f;
@@ -923,4 +931,13 @@ __device__ __forceinline__ void prompt_merge(const PagedArgs& a, PromptMergeShar
 #pragma unroll
     for (int d = 0; d < HD / 64; ++d) *out_at(a, it.t0 + tok, (it.g * a.G + h) * HD + d * 64 + lane) = (f16_t)half_pair(L == 0.f ? 0.f : O[d] / L, 0.f);
   }
+}
+
+// Batches that may hold both: every workgroup first its runs of the few rows' tiles, then prompt items from the counter.
+template <int HD, int CT> union PagedShared { ShortShared<HD, CT> s; PromptShared p; };
+template <int HD, int BITS, int CT, int NT>
+__device__ __forceinline__ void paged_both(const PagedArgs& a, PagedShared<HD, CT>& sh, u32 wg, u32 nwg) {
+  paged_short<HD, BITS, CT, NT>(a, sh.s, wg, nwg);
+  __syncthreads();
+  paged_prompt<HD, BITS>(a, sh.p, wg, nwg, true);
 }

@@ -1,10 +1,19 @@
-// The kernels of the paged-cache operators, defined in kernels/kv_store.hip, paged_short.hip and paged_prompt.hip.
+// The kernels of the paged-cache operators, defined in kernels/kv_store.hip, paged_short.hip, paged_prompt.hip and paged_both.hip, and
+// those of an engine's phases that are the same operators (kernels/paged_phases.hip).
 #pragma once
 #include "paged_attention.h"
 
 #define STORE_UNROLL 2                                 // rows of a lane group on their way at a time
+// Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold), and tiles of keys on their way
+#define SHORT_MORE(HD) ((HD) == 64 ? 4 : 2)
+#define SHORT_AHEAD(HD, BITS, CT) ((CT) == 1 || (BITS) == 4 ? 4 : 2)
+#define PAGED_BOUNDS __launch_bounds__(512) __attribute__((amdgpu_num_vgpr(120)))       // (see PHASE_KERNEL8)
+
 template <typename T, int HD, int BITS> __global__ void k_kv_store(StoreArgs a);
 __global__ void k_kv_read(ReadArgs a, u32 hd);
 template <int HD, int BITS, int CT> __global__ void k_paged_short(PagedArgs a);
 template <int HD, int BITS> __global__ void k_paged_prompt(PagedArgs a);
+template <int HD, int BITS> __global__ void k_paged_both(PagedArgs a);
 template <int HD> __global__ void k_paged_merge(PagedArgs a, u32 nwg_prompt);
+template <int HD, int BITS> __global__ void k_store_phase(DevCtx c, u32 layer);
+template <int HD, int BITS, int CT> __global__ void k_attention_phase(DevCtx c, u32 layer);

@@ -25,6 +25,7 @@
 
 PHASE_KERNEL_DECL(k_embed)
 PHASE_KERNEL_DECL(k_qkv)
+PHASE_KERNEL_DECL(k_qkv_plain)
 PHASE_KERNEL_DECL(k_attention)
 PHASE_KERNEL_DECL(k_oproj)
 PHASE_KERNEL_DECL(k_gateup)

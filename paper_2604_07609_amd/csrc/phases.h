@@ -18,7 +18,8 @@ enum {
   PH_ATTN_COMBINE,  // bf16 path only, directly after PH_ATTN of the same layer
   PH_UNUSED13, PH_UNUSED14, PH_UNUSED15,   // (no kernels)
   PH_ROUTER, PH_ROUTE, PH_MOE_GATEUP, PH_MOE_DOWN, PH_MOE_COMBINE,  // mixture of experts: in place of PH_GATEUP and PH_DOWN
-  PH_MOE_PERMUTE                                                    // (runs between PH_ROUTE and PH_MOE_GATEUP)
+  PH_MOE_PERMUTE,                                                   // (runs between PH_ROUTE and PH_MOE_GATEUP)
+  PH_QKV_PLAIN                                                      // the kernel of PH_QKV where PH_ROPE has one of its own
 };
 #define PH_LAYER_FIRST PH_NORM1
 #define PH_LAYER_LAST PH_DOWN
@@ -28,6 +29,7 @@ enum {
 struct NoShared {};
 template <int PH, bool F32> struct PhaseSharedOf { typedef NoShared type; };
 template <> struct PhaseSharedOf<PH_QKV, false> { typedef GemmShared8 type; };
+template <> struct PhaseSharedOf<PH_QKV_PLAIN, false> { typedef GemmShared8 type; };
 template <> struct PhaseSharedOf<PH_OPROJ, false> { typedef GemmShared8 type; };
 template <> struct PhaseSharedOf<PH_GATEUP, false> { typedef GemmShared8 type; };
 template <> struct PhaseSharedOf<PH_DOWN, false> { typedef GemmShared8 type; };
@@ -111,6 +113,10 @@ __device__ __forceinline__ void run_phase_bf16(const DevCtx& c, u32 layer, typen
       a.nq = c.nq; a.nkv = c.nkv; a.hd = c.hd; a.bs = c.bs;
       gemm_bf16<EPI_QKV_ROPE>(a, m->plan & 0xffu, *(GemmShared8*)&sh, wg, nwg);
       break;
+    case PH_QKV_PLAIN:
+      a.Wp = P->wqkv; a.Xp = c.xq; a.N = c.qkv_n; a.K = c.d; a.ssq_in = c.ssq; a.out = c.qkv; a.ldo = c.qkv_n;
+      gemm_bf16<EPI_SCALED_STORE>(a, m->plan & 0xffu, *(GemmShared8*)&sh, wg, nwg);
+      break;
     case PH_ATTN: phase_attention_mfma(c, layer, *(AttnShared8*)&sh, wg, nwg); break;
     case PH_ATTN_COMBINE: attn_decode_combine(c, wg, nwg); break;
     case PH_ROUTER:     // router logits of every token; its first workgroup also clears the experts' counters for this layer
@@ -148,7 +154,7 @@ __device__ __forceinline__ void run_phase_bf16(const DevCtx& c, u32 layer, typen
       if (c.spec_k) phase_sample_publish_spec(c, *(SamplerShared*)&sh, wg, nwg);
       else phase_sample_publish(c, *(SamplerShared*)&sh, wg, nwg);
       break;
-    default: break;   // the norms and the rotary / KV-write step are fused into the GEMMs
+    default: break;   // the norms and the rotary / KV-write step are fused into the GEMMs (or are kernels/paged_phases.hip)
   }
 }
 

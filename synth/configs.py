@@ -45,6 +45,17 @@ MODEL_CONFIGS = {
     # sixteen experts, four active, wide enough that a prefill iteration gives an expert more than 64 tokens
     "mini_moe16": dict(n_layers=2, d_model=512, n_q_heads=8, n_kv_heads=2, head_dim=64, d_ffn=160, n_experts=16, n_active=4,
                        vocab=2100, dtype=1, rms_eps=1e-5, rope_theta=10000.0),
+    # per-head norms, a window with sinks, a 4-bit cache (blink_attention_options), apart and together
+    "mini_norm": dict(n_layers=3, d_model=384, n_q_heads=6, n_kv_heads=2, head_dim=64, d_ffn=832, qk_norm=1,
+                      vocab=2500, dtype=1, rms_eps=1e-5, rope_theta=500000.0),
+    "mini_window": dict(n_layers=2, d_model=512, n_q_heads=4, n_kv_heads=1, head_dim=128, d_ffn=640, window=48, sinks=4,
+                        vocab=1900, dtype=1, rms_eps=1e-5, rope_theta=10000.0),
+    "mini_kv4": dict(n_layers=2, d_model=512, n_q_heads=8, n_kv_heads=2, head_dim=64, d_ffn=768, kv_bits=4,
+                     vocab=2100, dtype=1, rms_eps=1e-5, rope_theta=500000.0),
+    "mini_long": dict(n_layers=2, d_model=512, n_q_heads=8, n_kv_heads=2, head_dim=128, d_ffn=768, qk_norm=1, window=80,
+                      sinks=16, kv_bits=4, vocab=2100, dtype=1, rms_eps=1e-6, rope_theta=1000000.0),
+    "mini_long_moe": dict(n_layers=2, d_model=512, n_q_heads=8, n_kv_heads=2, head_dim=128, d_ffn=160, n_experts=16, n_active=4, qk_norm=1, window=80,
+                          sinks=16, vocab=2100, dtype=1, rms_eps=1e-6, rope_theta=1000000.0),
     # the shape of the paper's mixture-of-experts model (30 B parameters, 3 B active per token): 128 experts of width 768, 8 active
     "moe_30b_a3b": dict(n_layers=48, d_model=2048, n_q_heads=32, n_kv_heads=4, head_dim=128, d_ffn=768, n_experts=128, n_active=8,
                         vocab=151936, dtype=1, rms_eps=1e-6, rope_theta=1000000.0),
@@ -83,6 +94,16 @@ ENGINE_CONFIGS = {
                      max_prefill_tokens=256, ring_slots=32, eos_token_id=-1),
     "mini_moe16": dict(kv_block_size=16, kv_num_blocks=400, max_batch=48, max_seq_len=700,
                        max_prefill_tokens=900, ring_slots=128, eos_token_id=-1),
+    "mini_norm": dict(kv_block_size=16, kv_num_blocks=96, max_batch=6, max_seq_len=160,
+                      max_prefill_tokens=256, ring_slots=32, eos_token_id=-1),
+    "mini_window": dict(kv_block_size=16, kv_num_blocks=128, max_batch=6, max_seq_len=700,
+                        max_prefill_tokens=700, ring_slots=32, eos_token_id=-1),
+    "mini_kv4": dict(kv_block_size=16, kv_num_blocks=128, max_batch=6, max_seq_len=700,
+                     max_prefill_tokens=700, ring_slots=32, eos_token_id=-1),
+    "mini_long": dict(kv_block_size=16, kv_num_blocks=400, max_batch=48, max_seq_len=700,
+                      max_prefill_tokens=900, ring_slots=128, eos_token_id=-1),
+    "mini_long_moe": dict(kv_block_size=16, kv_num_blocks=400, max_batch=48, max_seq_len=700,
+                          max_prefill_tokens=900, ring_slots=128, eos_token_id=-1),
     "moe_30b_a3b": dict(kv_block_size=16, kv_num_blocks=32768, max_batch=256, max_seq_len=4096 + 1024,
                         max_prefill_tokens=8192, ring_slots=2048, eos_token_id=-1),
 }
