@@ -1,6 +1,7 @@
 """ctypes binding of include/blink.h. Same names as the C ABI, numpy arrays in and out."""
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -54,6 +55,10 @@ class PagedAttentionArgs(C.Structure):
     _fields_ = [("cache", CacheDesc)] + [(n, C.c_uint32) for n in ("n_q_heads", "n_seqs", "n_tokens", "max_q", "max_blocks", "window", "sinks")] + [
         ("scale", C.c_float), ("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_uint64), ("out_stride", C.c_uint64)] + [
         (n, C.c_void_p) for n in ("cu_seqlens", "seq_lens", "block_tables", "workspace")] + [("workspace_bytes", C.c_uint64)]
+
+
+# the same three as `struct` packs them (fields in order, native alignment)
+_CACHE, _QK_NORM_ROPE, _PAGED_ATTENTION = struct.Struct("@P4I"), struct.Struct("@P4I4I3P3Q6PQ2f"), struct.Struct("@P4I7If2P2Q4PQ")
 
 
 class Stats(C.Structure):
@@ -156,44 +161,34 @@ def sample_rows_static(logits, params, token_index, device=0):
     return _sample_rows("blink_sample_rows_static", logits, params, token_index, device)
 
 
-# ---- operators on device memory: any tensors with data_ptr(), shape, stride(), dtype and device (torch's, for instance) ----
-_TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}
+# ---- operators on device memory: any tensors with data_ptr(), get_device(), shape, stride(), dtype and is_contiguous() as torch's have them ----
+# A call on a few tokens is over in microseconds, so what it asks of every tensor is kept short, and its arguments are packed at once.
+_FLOAT, _HALF, _BF16, _INT, _OTHER = range(5)          # the first three: BLINK_TYPE_*
+_KINDS = {"torch.float32": _FLOAT, "torch.float16": _HALF, "torch.bfloat16": _BF16, "torch.int32": _INT}
+_kind_of = {}                                          # the same by dtype object, as they come
 
 
-def _tensor(name, t, device, dtypes, shape):
-    """Address of a device tensor whose dimensions behind the first are dense. `shape`: its sizes, None for any."""
-    if t.device.type != "cuda" or (t.device.index or 0) != device:
-        raise ValueError(f"{name} is on {t.device}, not on device {device}")
-    if str(t.dtype) not in dtypes:
-        raise ValueError(f"{name} is {t.dtype}, not one of {', '.join(dtypes)}")
-    if len(t.shape) != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
-        raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {shape}")
-    dense = 1
-    for n, s in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if s != dense and n != 1:
-            raise ValueError(f"{name}: the dimensions of a row must be contiguous")
-        dense *= n
-    if t.shape[0] > 1 and t.stride()[0] < dense:
-        raise ValueError(f"{name}: rows overlap")
+def _kind(t):
+    k = _kind_of.get(t.dtype)
+    if k is None:
+        k = _kind_of[t.dtype] = _KINDS.get(str(t.dtype), _OTHER)
+    return k
+
+
+def _dense(name, t, kind, shape, device):
+    """Address of a contiguous tensor."""
+    if t.get_device() != device or _kind(t) != kind or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {[n for n, k in _KINDS.items() if k == kind][0]} of the shape {tuple(shape)} on device {device}; "
+                         f"it is {t.dtype}, {tuple(t.shape)}, strides {tuple(t.stride())}, on device {t.get_device()}")
     return t.data_ptr()
 
 
-def _row_stride(t):
-    """Elements from one row to the next (of a single row: its length)."""
-    if t.shape[0] > 1:
-        return t.stride()[0]
-    n = 1
-    for m in t.shape[1:]:
-        n *= m
-    return n
-
-
-def _dense(name, t):
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-
-
-_HALF, _INT = ("torch.float16",), ("torch.int32",)
+def _rows(name, t, shape, device):
+    """Address of a tensor [tokens, heads, hd] whose rows [heads, hd] are contiguous, and the elements from one row to the next."""
+    st, width = t.stride(), shape[1] * shape[2]
+    if t.get_device() != device or t.shape != shape or (st[2] != 1 and shape[2] != 1) or (st[1] != shape[2] and shape[1] != 1) or (shape[0] > 1 and st[0] < width):
+        raise ValueError(f"{name} must have the shape {tuple(shape)} with contiguous rows, on device {device}; it has {tuple(t.shape)}, strides {tuple(st)}, on device {t.get_device()}")
+    return t.data_ptr(), st[0] if shape[0] > 1 else width
 
 
 def kv_cache_bytes(n_blocks, n_kv_heads, head_dim, bits=16):
@@ -208,47 +203,45 @@ class KVCache:
 
     def __init__(self, data, n_blocks, n_kv_heads, head_dim, bits=16):
         need = kv_cache_bytes(n_blocks, n_kv_heads, head_dim, bits)
-        if data.device.type != "cuda":
+        if data.get_device() < 0:
             raise ValueError(f"data is on {data.device}")
-        _dense("data", data)
-        if data.numel() * data.element_size() != need:
-            raise ValueError(f"data has {data.numel() * data.element_size()} bytes, the cache {need}")
-        self.data, self.device = data, data.device.index or 0
+        if not data.is_contiguous() or data.numel() * data.element_size() != need:
+            raise ValueError(f"data must be contiguous and have {need} bytes; it has {data.numel() * data.element_size()}, strides {tuple(data.stride())}")
+        self.data, self.device = data, data.get_device()
         self.desc = CacheDesc(data.data_ptr(), n_blocks, n_kv_heads, head_dim, bits)
+        self.n_kv_heads, self.head_dim, self._packed = n_kv_heads, head_dim, (data.data_ptr(), n_blocks, n_kv_heads, head_dim, bits)
 
 
 def qk_norm_rope(q, k, v, positions, slots, rope_table, cache, q_out, q_gain=None, k_gain=None, eps=1e-6, q_scale=1.0, stream=0):
     """blink_qk_norm_rope: q [tokens, q heads, hd], k and v [tokens, kv heads, hd] (float32, float16 or bfloat16, rows may be parts
     of wider ones), int32 positions and slots [tokens], float32 rope_table [rows, hd / 2, 2] -> q_out float16 like q, keys and
     values into `cache`. Gains: float32 [hd] or None. stream: a stream's handle."""
-    lib, d, dev = load_library(), cache.desc, cache.device
-    T, hd, nkv = q.shape[0], d.head_dim, d.n_kv_heads
-    a = QkNormRopeArgs(cache=d, n_tokens=T, q_scale=q_scale, eps=eps)
-    a.q = _tensor("q", q, dev, _TYPES, (T, None, hd))
-    same = (str(q.dtype),)
-    a.k, a.v = _tensor("k", k, dev, same, (T, nkv, hd)), _tensor("v", v, dev, same, (T, nkv, hd))
-    a.n_q_heads, a.in_type, a.rope_rows = q.shape[1], _TYPES[same[0]], rope_table.shape[0]
-    a.q_out = _tensor("q_out", q_out, dev, _HALF, (T, q.shape[1], hd))
-    a.q_stride, a.k_stride, a.v_stride, a.q_out_stride = _row_stride(q), _row_stride(k), _row_stride(v), _row_stride(q_out)
-    a.positions, a.slots = _tensor("positions", positions, dev, _INT, (T,)), _tensor("slots", slots, dev, _INT, (T,))
-    a.rope_table = _tensor("rope_table", rope_table, dev, ("torch.float32",), (None, hd // 2, 2))
-    for name, t in (("positions", positions), ("slots", slots), ("rope_table", rope_table)):
-        _dense(name, t)
-    for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
-        if t is not None:
-            setattr(a, name, _tensor(name, t, dev, ("torch.float32",), (hd,)))
-            _dense(name, t)
-    _check(lib, lib.blink_qk_norm_rope(dev, C.byref(a), stream))
+    lib, dev, hd, nkv = _lib or load_library(), cache.device, cache.head_dim, cache.n_kv_heads
+    if len(q.shape) != 3:
+        raise ValueError(f"q must have three dimensions; it has {tuple(q.shape)}")
+    T, nq, kind = q.shape[0], q.shape[1], _kind(q)
+    if kind > _BF16 or _kind(k) != kind or _kind(v) != kind or _kind(q_out) != _HALF:
+        raise ValueError(f"q, k and v must be of one type, float32, float16 or bfloat16, and q_out float16; they are {q.dtype}, {k.dtype}, {v.dtype}, {q_out.dtype}")
+    qp, qs = _rows("q", q, (T, nq, hd), dev)
+    kp, ks = _rows("k", k, (T, nkv, hd), dev)
+    vp, vs = _rows("v", v, (T, nkv, hd), dev)
+    op, os_ = _rows("q_out", q_out, (T, nq, hd), dev)
+    rows = rope_table.shape[0]
+    a = _QK_NORM_ROPE.pack(*cache._packed, nq, T, kind, rows, qp, kp, vp, qs, ks, vs,
+                           0 if q_gain is None else _dense("q_gain", q_gain, _FLOAT, (hd,), dev), 0 if k_gain is None else _dense("k_gain", k_gain, _FLOAT, (hd,), dev),
+                           _dense("positions", positions, _INT, (T,), dev), _dense("slots", slots, _INT, (T,), dev),
+                           _dense("rope_table", rope_table, _FLOAT, (rows, hd // 2, 2), dev), op, os_, eps, q_scale)
+    rc = lib.blink_qk_norm_rope(dev, a, stream)
+    if rc:
+        _check(lib, rc)
 
 
 def kv_cache_read(cache, slots, k_out, v_out, stream=0):
     """blink_kv_cache_read: the tokens at int32 slots [tokens] into k_out, v_out, contiguous float16 [tokens, kv heads, hd]."""
-    lib, d, dev = load_library(), cache.desc, cache.device
-    shape = (slots.shape[0], d.n_kv_heads, d.head_dim)
-    at = [_tensor("slots", slots, dev, _INT, shape[:1]), _tensor("k_out", k_out, dev, _HALF, shape), _tensor("v_out", v_out, dev, _HALF, shape)]
-    for name, t in (("slots", slots), ("k_out", k_out), ("v_out", v_out)):
-        _dense(name, t)
-    _check(lib, lib.blink_kv_cache_read(dev, C.byref(d), at[0], shape[0], at[1], at[2], stream))
+    lib, dev = _lib or load_library(), cache.device
+    shape = (slots.shape[0], cache.n_kv_heads, cache.head_dim)
+    _check(lib, lib.blink_kv_cache_read(dev, _CACHE.pack(*cache._packed), _dense("slots", slots, _INT, shape[:1], dev), shape[0],
+                                        _dense("k_out", k_out, _HALF, shape, dev), _dense("v_out", v_out, _HALF, shape, dev), stream))
 
 
 def attention_workspace_bytes(n_q_heads, cache, n_seqs, max_q=1):
@@ -261,20 +254,23 @@ def attention_workspace_bytes(n_q_heads, cache, n_seqs, max_q=1):
 def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q=1, window=0, sinks=0, scale=1.0, stream=0):
     """blink_paged_attention: q, out float16 [tokens, q heads, hd]; int32 block_tables [seqs, blocks], seq_lens [seqs], cu_seqlens
     [seqs + 1]; workspace: a contiguous tensor of attention_workspace_bytes(...) bytes. stream: a stream's handle."""
-    lib, d, dev = load_library(), cache.desc, cache.device
-    T, S = q.shape[0], seq_lens.shape[0]
-    a = PagedAttentionArgs(cache=d, n_q_heads=q.shape[1], n_seqs=S, n_tokens=T, max_q=max_q, max_blocks=block_tables.shape[-1], window=window, sinks=sinks, scale=scale)
-    a.q = _tensor("q", q, dev, _HALF, (T, None, d.head_dim))
-    a.out = _tensor("out", out, dev, _HALF, (T, q.shape[1], d.head_dim))
-    a.q_stride, a.out_stride = _row_stride(q), _row_stride(out)
-    a.block_tables, a.seq_lens = _tensor("block_tables", block_tables, dev, _INT, (S, None)), _tensor("seq_lens", seq_lens, dev, _INT, (S,))
-    a.cu_seqlens = _tensor("cu_seqlens", cu_seqlens, dev, _INT, (S + 1,))
-    for name, t in (("block_tables", block_tables), ("seq_lens", seq_lens), ("cu_seqlens", cu_seqlens), ("workspace", workspace)):
-        _dense(name, t)
-    if workspace.device.type != "cuda" or (workspace.device.index or 0) != dev:
-        raise ValueError(f"workspace is on {workspace.device}, not on device {dev}")
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(lib, lib.blink_paged_attention(dev, C.byref(a), stream))
+    lib, dev, hd = _lib or load_library(), cache.device, cache.head_dim
+    if len(q.shape) != 3 or len(block_tables.shape) != 2:
+        raise ValueError(f"q must have three dimensions and block_tables two; they have {tuple(q.shape)} and {tuple(block_tables.shape)}")
+    T, nq = q.shape[0], q.shape[1]
+    S, width = block_tables.shape
+    if _kind(q) != _HALF or _kind(out) != _HALF:
+        raise ValueError(f"q and out must be float16; they are {q.dtype} and {out.dtype}")
+    qp, qs = _rows("q", q, (T, nq, hd), dev)
+    op, os_ = _rows("out", out, (T, nq, hd), dev)
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on device {dev}; it is on device {workspace.get_device()}")
+    a = _PAGED_ATTENTION.pack(*cache._packed, nq, S, T, max_q, width, window, sinks, scale, qp, op, qs, os_, _dense("cu_seqlens", cu_seqlens, _INT, (S + 1,), dev),
+                              _dense("seq_lens", seq_lens, _INT, (S,), dev), _dense("block_tables", block_tables, _INT, (S, width), dev), workspace.data_ptr(),
+                              workspace.numel() * workspace.element_size())
+    rc = lib.blink_paged_attention(dev, a, stream)
+    if rc:
+        _check(lib, rc)
 
 
 class Engine:

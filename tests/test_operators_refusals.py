@@ -106,6 +106,19 @@ def test_struct_sizes_match_header(tmp_path):
     assert got == [C.sizeof(M.CacheDesc), C.sizeof(M.QkNormRopeArgs), M.QkNormRopeArgs.eps.offset, C.sizeof(M.PagedAttentionArgs), M.PagedAttentionArgs.workspace.offset]
 
 
+@pytest.mark.parametrize("kind, form", [(M.CacheDesc, "_CACHE"), (M.QkNormRopeArgs, "_QK_NORM_ROPE"), (M.PagedAttentionArgs, "_PAGED_ATTENTION")])
+def test_packed_arguments_are_the_structures(kind, form):
+    """The binding packs its arguments with `struct`: every field where the structure has it."""
+    packer = getattr(M, form)
+    n = len(packer.unpack(bytes(packer.size)))
+    got = kind.from_buffer_copy(packer.pack(*range(1, n + 1)).ljust(C.sizeof(kind), b"\0"))
+    flat = []
+    for name, _ in kind._fields_:
+        x = getattr(got, name)
+        flat += [getattr(x, f) for f, _ in x._fields_] if isinstance(x, C.Structure) else [x]
+    assert [int(x) for x in flat] == list(range(1, n + 1)) and packer.size <= C.sizeof(kind)
+
+
 def test_tensors_of_the_wrong_kind():
     """The binding's own checks, on host tensors: they are on no device of the library's."""
     torch = pytest.importorskip("torch")
