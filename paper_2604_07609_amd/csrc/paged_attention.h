@@ -339,21 +339,31 @@ __device__ __forceinline__ void add_past_caches(const float* slot, ShortAcc<HD, 
       for (int i = 0; i < 4; ++i) acc[c].o[d][i] = acc[c].o[d][i] * mine + __uint_as_float((u32)(v[d][i >> 1] >> (32 * (i & 1)))) * other;
   }
 }
-// takes the values that are not finite out of a tile that some row does not see as a whole, and gives them to the rows that see them
-template <int HD, int BITS, int CT>
-__device__ __forceinline__ void strange_values(typename CacheTile<HD, BITS>::Values& val, ShortAcc<HD, BITS> (&acc)[CT], const u32 (&vis)[CT]) {
+// whether a tile has a value that is not finite (then those are taken out of it)
+template <int HD, int BITS>
+__device__ __forceinline__ bool take_strange_out(typename CacheTile<HD, BITS>::Values& val) {
   typedef CacheTile<HD, BITS> Tile;
   const float zero[4] = {0.f, 0.f, 0.f, 0.f};
   const typename Tile::Probs none = Tile::probs(zero);
   floatx4_t z = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int v = 0; v < Tile::NV; ++v) z = Tile::product(val.w[v], none, 0, z);       // 0 unless something is not finite
-  if (!any_nan(z)) return;
+  if (!any_nan(z)) return false;
+#pragma unroll
+  for (int v = 0; v < Tile::NV; ++v)
+#pragma unroll
+    for (int k = 0; k < Tile::NW; ++k) Tile::word(val, v, k) = only_finite(Tile::word(val, v, k));
+  return true;
+}
+// ... and given to the rows that see them
+template <int HD, int BITS, int CT>
+__device__ __forceinline__ void give_strange(const typename CacheTile<HD, BITS>::Values& val, ShortAcc<HD, BITS> (&acc)[CT], const u32 (&vis)[CT]) {
+  typedef CacheTile<HD, BITS> Tile;
 #pragma unroll
   for (int d = 0; d < HD / 16; ++d) {
-    typename Tile::Values odd;
+    typename Tile::Values odd = val;
 #pragma unroll
-    for (int k = 0; k < Tile::NW; ++k) Tile::word(odd, Tile::of(d), k) = strange_codes(Tile::word(val, Tile::of(d), k));
+    for (int k = 0; k < Tile::NW; ++k) Tile::word(odd, Tile::of(d), k) = strange_codes(Tile::word(odd, Tile::of(d), k));
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const float see[4] = {vis[c] & 1u ? 1.f : 0.f, vis[c] & 2u ? 1.f : 0.f, vis[c] & 4u ? 1.f : 0.f, vis[c] & 8u ? 1.f : 0.f};
@@ -363,10 +373,6 @@ __device__ __forceinline__ void strange_values(typename CacheTile<HD, BITS>::Val
     }
     __builtin_amdgcn_sched_barrier(0);               // (rare: no registers for it)
   }
-#pragma unroll
-  for (int v = 0; v < Tile::NV; ++v)
-#pragma unroll
-    for (int k = 0; k < Tile::NW; ++k) Tile::word(val, v, k) = only_finite(Tile::word(val, v, k));
 }
 
 __device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqView& v) {     // tiles of a sequence and kv head; 0: not this part's, 1 at least else
@@ -377,23 +383,31 @@ __device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqVie
 __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { return a.out_tbs ? a.out + packed_off(tok, k, a.out_tbs) : a.out + (u64)tok * a.os + k; }
 
 // All tiles of all (sequence, kv head) pairs are one line of units, cut into equal runs, one per wave: whatever the lengths, every
-// wave reads the same number of bytes, with NT tiles on their way across the borders between pairs, and waits for nobody until its run ends.
+// wave reads the same number of bytes, with NT tiles on their way, and waits for nobody until its run ends.
 // A pair inside a run is finished where it is. One that several waves of a workgroup share is added up by the wave it begins in (in
 // LDS, after the one barrier); one that several workgroups share leaves a result of each in the workspace, and the workgroup that comes
 // last adds them up, its waves an eighth of them each. All sums in the order of the runs: results do not depend on who comes when.
+// Few short pairs (half as many as workgroups, SHORT_CAP tiles a workgroup) are dealt out whole instead, a workgroup or several to each: no
+// result then crosses workgroups up to SHORT_CAP tiles, which would take longer than the tiles do.
+// The loop over tiles is written out NT times for its registers, so all that is rare stands outside of it, once.
 #define SHORT_QUANTUM 4u
+#define SHORT_CAP 64u
 template <int HD, int BITS, int CT, int NT>
 __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, CT>& sh, u32 wg, u32 nwg) {
   typedef CacheTile<HD, BITS> Tile;
   constexpr u32 NW = PAGED_WAVES;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
   auto scalar = [](u32 x) { return (u32)__builtin_amdgcn_readfirstlane(x); };
-  prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return short_unit_count(a, sh.view[s] = seq_view(a, s)) * a.nkv; });
-  const u32 U = scalar(sh.pre[a.n_seqs]);
-  const u32 quantum = max(SHORT_QUANTUM, (U + nwg * NW - 1) / (nwg * NW)), wg_units = quantum * NW;
-  if (wg * wg_units >= U) return;                    // (all its waves: the counts below are of workgroups with units)
+  bool whole = a.n_seqs * a.nkv <= nwg / 2;          // pairs dealt out whole: then `pre` counts workgroups, else units
+  if (whole) {
+    prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return (short_unit_count(a, sh.view[s] = seq_view(a, s)) + SHORT_CAP - 1) / SHORT_CAP * a.nkv; });
+    whole = scalar(sh.pre[a.n_seqs]) <= nwg;
+    if (!whole) __syncthreads();
+  }
+  if (!whole) prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return short_unit_count(a, sh.view[s] = seq_view(a, s)) * a.nkv; });
+  const u32 U = scalar(sh.pre[a.n_seqs]), wg_units = max(SHORT_QUANTUM, (U + nwg * NW - 1) / (nwg * NW)) * NW;
+  if (whole ? wg >= U : wg * wg_units >= U) return;
   if (threadIdx.x < 2) sh.last[threadIdx.x] = 0;
-  const u32 u0 = min((wg * NW + w) * quantum, U), u1 = min(u0 + quantum, U);
   typedef const __attribute__((address_space(4))) u32 const_u32;
   // a pair of a sequence and a kv head: its first unit and number of tiles, its rows, and which tiles those are
   struct Pair { u32 s, g, first, nv, t0, n, row, zb, wlo; i32 pos0; };
@@ -404,11 +418,11 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     p.t0 = scalar(v.t0); p.n = scalar(v.n); p.pos0 = (i32)scalar((u32)v.pos0);
     const Seen e = seen_tiles<16>(a, p.pos0, p.pos0 + (i32)p.n - 1);
     p.zb = scalar(e.zb); p.wlo = scalar(e.wlo); p.nv = scalar(max(1u, e.n));
-    p.first = scalar(sh.pre[s]) + g * p.nv;
+    p.first = whole ? 0u : scalar(sh.pre[s]) + g * p.nv;
     p.row = a.table_row ? scalar(a.table_row[s]) : s;
     return p;
   };
-  auto pair_at = [&](u32 u) {
+  auto pair_at = [&](u32 u) {                        // (whole pairs: u = the workgroup)
     const u32 s = scalar(last_at_most(sh.pre, a.n_seqs, u)), in = u - scalar(sh.pre[s]);
     return pair_of(s, in / (scalar(sh.pre[s + 1] - sh.pre[s]) / a.nkv));
   };
@@ -418,6 +432,17 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     while (scalar(sh.pre[s + 1]) == scalar(sh.pre[s])) ++s;
     return pair_of(s, 0);
   };
+  // the workgroup's run, and this wave's share of it
+  Pair cur = pair_at(whole ? wg : wg * wg_units);
+  u32 wg0 = wg * wg_units, wg1 = min(wg0 + wg_units, U), from = 0;         // from: the first workgroup of the pair (whole pairs)
+  if (whole) {
+    const u32 per = (cur.nv + SHORT_CAP - 1) / SHORT_CAP;
+    from = scalar(sh.pre[cur.s]) + cur.g * per;
+    wg0 = (wg - from) * SHORT_CAP; wg1 = min(wg0 + SHORT_CAP, cur.nv);
+  }
+  const u32 quantum = (wg1 - wg0 + NW - 1) / NW, u0 = min(wg0 + w * quantum, wg1), u1 = min(u0 + quantum, wg1);
+  auto first_wg = [&](const Pair& p) { return whole ? from : p.first / wg_units; };
+  auto n_wgs = [&](const Pair& p) { return whole ? (p.nv + SHORT_CAP - 1) / SHORT_CAP : (p.first + p.nv - 1) / wg_units - p.first / wg_units + 1; };
   f16x8_t q[CT][HD / 32];
   i32 qpos[CT];                                      // position of the lane's row (no row: before every key)
   auto load_q = [&](const Pair& p) {
@@ -456,22 +481,27 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
       }
     }
   };
-  Pair cur{};
+  auto key_of = [&](const Pair& p, u32 u) { const u32 l = u - p.first; return (l < p.zb ? l : p.wlo + l - p.zb) * 16; };    // first key of the unit's tile
+  auto block_of = [&](const Pair& p, u32 key) {      // (a pair without keys has no block either)
+    return p.pos0 + (i32)p.n > 0 ? ((const_u32*)(u64)uniform_ptr(a.tables + (u64)p.row * a.max_blocks))[key / 16] : ~0u;
+  };
+  auto edge_of = [&](const Pair& p, u32 key, bool in_cache) {      // some row does not see the whole tile
+    const i32 k = (i32)key, p1 = p.pos0 + (i32)p.n - 1;
+    return !(k + 15 <= p.pos0 && in_cache && (!a.window || k > p1 - (i32)a.window || key + 16 <= a.sinks));
+  };
+  auto see = [&](u32 key, bool in_cache, u32 (&vis)[CT]) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) vis[c] = in_cache ? sees(a, qpos[c], (i32)(key + lg * 4)) : 0u;
+  };
+  clear();
   if (u0 < u1) {
-    cur = pair_at(u0);
+    if (u0 != wg0 && !whole) cur = pair_at(u0);
     // the tile to ask for next: its unit, pair and block id (asked for a tile ahead)
     Pair ap = cur;
-    u32 au = u0, aid = 0, ak = 0;
-    auto next_id = [&]() {
-      const u32 l = au - ap.first;
-      const u32 t = l < ap.zb ? l : ap.wlo + l - ap.zb;
-      ak = t * 16;
-      aid = ~0u;                                     // (a pair without keys has no block either)
-      if (ap.pos0 + (i32)ap.n > 0) aid = ((const_u32*)(u64)uniform_ptr(a.tables + (u64)ap.row * a.max_blocks))[t];
-    };
+    u32 au = u0, ak = key_of(ap, au), aid = block_of(ap, ak);
     Tile tile[NT];
     u32 k0[NT];
-    bool in_cache[NT];
+    bool in_cache[NT], strange = false;
     auto ask = [&](int j) {                          // into slot j, unless the run has been asked for
       if (au >= u1) return;
       k0[j] = ak;
@@ -479,53 +509,65 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
       tile[j].load(a, min(aid, a.n_blocks - 1), ap.g);
       if (++au < u1) {
         if (au == ap.first + ap.nv) ap = pair_after(ap);
-        next_id();
+        ak = key_of(ap, au);
+        aid = block_of(ap, ak);
       }
     };
     load_q(cur);
-    next_id();
 #pragma unroll
     for (int j = 0; j < NT; ++j) ask(j);
-    clear();
-    for (u32 u = u0; u < u1;) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        if (u >= u1) break;
-        const i32 p1 = cur.pos0 + (i32)cur.n - 1;
-        if (p1 >= 0) {
-          const typename Tile::Keys key = tile[j].keys();
-          typename Tile::Values val = tile[j].values();
-          const i32 k = (i32)k0[j];
-          const bool edge = !(k + 15 <= cur.pos0 && in_cache[j] && (!a.window || k > p1 - (i32)a.window || (u32)k + 16 <= a.sinks));
-          u32 vis[CT];
-#pragma unroll
-          for (int c = 0; c < CT; ++c) vis[c] = 0;
-          if (edge) {
-            if (in_cache[j]) {
-#pragma unroll
-              for (int c = 0; c < CT; ++c) vis[c] = sees(a, qpos[c], k + (i32)(lg * 4));
-            }
-            strange_values<HD, BITS, CT>(val, acc, vis);
-          }
-#pragma unroll
-          for (int c = 0; c < CT; ++c) acc[c].add(key, val, q[c], a.c, edge, vis[c]);
+    u32 u = u0;
+    auto step = [&](int j) {                         // the tile of slot j; whether its pair, or the run, ends with it
+      if (cur.pos0 + (i32)cur.n > 0) {
+        const typename Tile::Keys key = tile[j].keys();
+        typename Tile::Values val = tile[j].values();
+        const bool edge = edge_of(cur, k0[j], in_cache[j]);
+        u32 vis[CT] = {};
+        if (edge) {
+          see(k0[j], in_cache[j], vis);
+          strange |= take_strange_out<HD, BITS>(val);
         }
-        ask(j);
-        ++u;
-        if (u == cur.first + cur.nv) {               // the pair ends: finished here, or its beginning is another wave's
-          if (cur.first >= u0) finish(cur);
-          else leave_in_lds<HD, BITS, CT>(sh, w, acc);
-          if (u < u1) { cur = pair_after(cur); load_q(cur); }
-          clear();
-        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[c].add(key, val, q[c], a.c, edge, vis[c]);
       }
+      ask(j);
+      ++u;
+      return u == u1 || u == cur.first + cur.nv;
+    };
+    for (u32 j = 0;;) {
+      bool ends;
+      switch (j) {
+        case 0: ends = step(0); j = 1; if (ends) break; [[fallthrough]];
+        case 1: ends = step(1); j = 2 % NT; if (ends || NT == 2) break; [[fallthrough]];
+        case 2: ends = step(2 % NT); j = 3 % NT; if (ends || NT == 3) break; [[fallthrough]];
+        default: ends = step(3 % NT); j = 0;
+      }
+      if (!ends) continue;
+      if (strange) {                                 // (an edge tile had values that are not finite: they go to the rows that see them)
+        for (u32 x = max(u0, cur.first); x < u; ++x) {
+          const u32 key = key_of(cur, x), b = block_of(cur, key);
+          if (!edge_of(cur, key, b < a.n_blocks)) continue;
+          Tile t;
+          t.load(a, min(b, a.n_blocks - 1), cur.g);
+          u32 vis[CT];
+          see(key, b < a.n_blocks, vis);
+          give_strange<HD, BITS, CT>(t.values(), acc, vis);
+        }
+        strange = false;
+      }
+      const bool done = u == cur.first + cur.nv;
+      if (done && cur.first >= u0) finish(cur);                             // the pair is this wave's alone
+      else if (cur.first < u0) leave_in_lds<HD, BITS, CT>(sh, w, acc);      // its beginning is another wave's
+      if (u == u1) break;                                                   // (a pair that begins here and goes on: in acc)
+      cur = pair_after(cur);
+      load_q(cur);
+      clear();
+      wait_loads();      // (the compiler does not know any more which slot's loads are the oldest: it would wait for all of them at every turn)
     }
-    if (u1 < cur.first + cur.nv && cur.first < u0) leave_in_lds<HD, BITS, CT>(sh, w, acc);      // (the whole run inside a pair)
   }
   __syncthreads();
   // The rest is a workgroup's end, once per launch. This wave's pair that goes on behind its run, if it began there; wave 0 also the
   // pair that the workgroup's run begins inside of.
-  const u32 wg0 = wg * wg_units, wg1 = min(wg0 + wg_units, U);
   auto others = [&](const Pair& p, u32 x) {          // what the waves from x on have of the pair
 #pragma unroll 1
     for (; x < NW && wg0 + x * quantum < min(p.first + p.nv, wg1); ++x) add_from_lds<HD, BITS, CT>(sh, x, acc);
@@ -533,8 +575,8 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   auto hand_on = [&](const Pair& p, u32 which) {     // the workgroup's share of the pair to the workspace; who comes last is told
     leave_past_caches<HD, BITS, CT>(a.part + (u64)(2 * wg + which) * short_slot<HD, CT>(), acc, p.n * a.G);
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-    const u32 np = (p.first + p.nv - 1) / wg_units - p.first / wg_units + 1;
     if (lane == 0) {
+      const u32 np = n_wgs(p);
       u32* const ctr = a.ctr + (u64)p.s * a.nkv + p.g;
       const u32 before = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       sh.last[which] = before == np - 1;
@@ -546,7 +588,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     if (cur.first + cur.nv <= wg1) finish(cur); else hand_on(cur, 1);
   }
   if (w == 0) {
-    const Pair p = pair_at(wg0);
+    const Pair p = whole ? cur : pair_at(wg0);
     if (p.first < wg0) {
       clear();
       others(p, 0);
@@ -557,8 +599,8 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 #pragma unroll 1
   for (u32 which = 0; which < 2; ++which) {
     if (!scalar(sh.last[which])) continue;
-    const Pair p = pair_at(which ? wg1 - 1 : wg0);
-    const u32 w0 = p.first / wg_units, np = (p.first + p.nv - 1) / wg_units - w0 + 1, per = (np + NW - 1) / NW;
+    const Pair p = pair_at(whole ? wg : which ? wg1 - 1 : wg0);
+    const u32 w0 = first_wg(p), np = n_wgs(p), per = (np + NW - 1) / NW;
     clear();
 #pragma unroll 1
     for (u32 x = w * per; x < min(np, (w + 1) * per); ++x)

@@ -6,7 +6,7 @@
 #define STORE_UNROLL 2                                 // rows of a lane group on their way at a time
 // Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold), and tiles of keys on their way
 #define SHORT_MORE(HD) ((HD) == 64 ? 4 : 2)
-#define SHORT_AHEAD(HD, BITS, CT) ((CT) == 1 || (BITS) == 4 ? 4 : 2)
+#define SHORT_AHEAD(HD, BITS, CT) ((CT) > 1 ? 2 : (HD) == 128 && (BITS) == 16 ? 3 : 4)
 #define PAGED_BOUNDS __launch_bounds__(512) __attribute__((amdgpu_num_vgpr(120)))       // (see PHASE_KERNEL8)
 
 template <typename T, int HD, int BITS> __global__ void k_kv_store(StoreArgs a);
