@@ -120,10 +120,10 @@ struct PagedPlan {
   u32 ct;                 // row tiles of the short part (0: there is none)
   u32 short_rows;         // sequences with at most so many rows are its
   bool prompt;            // there is a prompt part (with a short one: in one launch)
-  u32 wgs, n_splits;
+  u32 wgs, threads, n_splits;
   u64 ctr_bytes, part_bytes, prompt_bytes;
 };
-static PagedPlan paged_plan(u32 hd, u32 nq, u32 nkv, u32 n_seqs, u32 n_tokens, u32 max_q, u32 key_steps, u32 n_cu) {
+static PagedPlan paged_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_seqs, u32 n_tokens, u32 max_q, u32 key_steps, u32 n_cu) {
   PagedPlan p{};
   const u32 G = nq / nkv, most = 16u * SHORT_MORE(hd);       // rows that the short part's registers hold
   const u64 rows = (u64)max_q * G;
@@ -133,7 +133,8 @@ static PagedPlan paged_plan(u32 hd, u32 nq, u32 nkv, u32 n_seqs, u32 n_tokens, u
     p.prompt = true;
     if (G <= 16 && n_tokens < (u64)n_seqs * max_q) { p.ct = 1; p.short_rows = 16; }
   }
-  p.wgs = n_cu;
+  p.wgs = n_cu * (p.prompt ? 1 : SHORT_PER_CU(bits, p.ct));
+  p.threads = 64 * (p.prompt ? PAGED_WAVES : SHORT_WAVES(bits, p.ct));
   // parts of 256 keys at least, where the items are too few for the chip
   const bool few = (u64)n_tokens * G / PROMPT_ROWS * nkv < p.wgs;
   p.n_splits = p.prompt && few ? std::max(1u, key_steps / 4) : 1u;
@@ -157,14 +158,14 @@ extern "C" int blink_attention_workspace_bytes(int32_t device, const blink_kv_ca
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
   // (n_tokens below n_seqs * max_q: the larger of the two kinds of launches; and what a smaller max_q would need)
-  const PagedPlan p = paged_plan(c->head_dim, n_q_heads, c->n_kv_heads, n_seqs, 0, max_q, 1, n_cu);
-  *bytes = p.ctr_bytes + std::max<u64>(p.part_bytes + p.prompt_bytes, 2ull * p.wgs * SHORT_MORE(c->head_dim) * (128 + 16 * c->head_dim) * 4);
+  const PagedPlan p = paged_plan(c->head_dim, c->bits, n_q_heads, c->n_kv_heads, n_seqs, 0, max_q, 1, n_cu);
+  *bytes = p.ctr_bytes + std::max<u64>(p.part_bytes + p.prompt_bytes, 2ull * n_cu * std::max(SHORT_MORE(c->head_dim), SHORT_PER_CU(c->bits, 1)) * (128 + 16 * c->head_dim) * 4);
   return BLINK_OK;
 }
 
 template <int HD, int BITS>
 static hipError_t launch_paged(const PagedArgs& args, const PagedPlan& plan, hipStream_t st) {
-  if (!plan.prompt) return plan.ct == 1 ? launch(k_paged_short<HD, BITS, 1>, plan.wgs, 512, st, args) : launch(k_paged_short<HD, BITS, SHORT_MORE(HD)>, plan.wgs, 512, st, args);
+  if (!plan.prompt) return plan.ct == 1 ? launch(k_paged_short<HD, BITS, 1>, plan.wgs, plan.threads, st, args) : launch(k_paged_short<HD, BITS, SHORT_MORE(HD)>, plan.wgs, plan.threads, st, args);
   const hipError_t e = plan.ct ? launch(k_paged_both<HD, BITS>, plan.wgs, 512, st, args) : launch(k_paged_prompt<HD, BITS>, plan.wgs, 512, st, args);
   return e == hipSuccess && plan.n_splits > 1 ? launch(k_paged_merge<HD>, plan.wgs, 512, st, args, plan.wgs) : e;
 }
@@ -190,7 +191,7 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   if (int rc = compute_units(device, &n_cu)) return rc;
   const u64 reach = a->window ? (u64)a->window + a->max_q + a->sinks : ~0ull;
   const u32 key_steps = (u32)std::min<u64>(a->max_blocks / 4 + 1, reach / 64 + 3);
-  const PagedPlan plan = paged_plan(hd, a->n_q_heads, nkv, a->n_seqs, a->n_tokens, a->max_q, key_steps, n_cu);
+  const PagedPlan plan = paged_plan(hd, a->cache.bits, a->n_q_heads, nkv, a->n_seqs, a->n_tokens, a->max_q, key_steps, n_cu);
   if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.ctr_bytes + plan.part_bytes + plan.prompt_bytes)
     return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)(plan.ctr_bytes + plan.part_bytes + plan.prompt_bytes));
   OnDevice on(device);

@@ -6,7 +6,10 @@
 //
 // Rows of a sequence and kv head are its queries times the G query heads that share the head: row = query * G + head. Sixteen of
 // them are the columns of the matrix products S[key][row] = K q and O^T[dim][row] = V^T P^T; the accumulator of S (column = lane % 16, keys
-// 4 (lane / 16) + i) is the operand P^T as it stands. In 4 bits a lane holds 8 neighbouring dimensions of 4 keys, so a register pair of
+// 4 (lane / 16) + i) is the operand P^T as it stands. With a 4-bit cache few rows' scores are products of the codes themselves
+// (v_mfma_scale_f32_16x16x128_f8f6f4, which takes a scale per 32 of them as they are stored): the query is the exact sum of three
+// e4m3 numbers of four bits each, so three such products give what one with converted keys would, and the vector instructions that converted them, which
+// bound the kernel, are gone. Of the values a lane holds 8 neighbouring dimensions of 4 keys, so a register pair of
 // the converted values is two dimensions of one key, and each of the two products that take it has zeros for the other one's dimension
 // in its P: twice the matrix instructions, which decode has to spare, in place of exchanging halves between registers, which it has not.
 #pragma once
@@ -56,6 +59,7 @@ __device__ __forceinline__ Seen seen_tiles(const PagedArgs& a, i32 p0, i32 p1) {
 }
 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef i32 i32x8_t __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ u32 f16x2_bits(f16x2_t v) { return *(const u32*)&v; }
 __device__ __forceinline__ f16x8_t f16x8_of(u32 a, u32 b, u32 c, u32 d) { const uint4 v = make_uint4(a, b, c, d); return *(const f16x8_t*)&v; }
 // Values that are not finite, where some row of the tile must not see them (0 times one would not be 0): the products take the finite ones
@@ -84,78 +88,146 @@ __device__ __forceinline__ u32 sees(const PagedArgs& a, i32 p, i32 k) {
 
 // ---- few rows: decoding sequences, drafted tokens --------------------------------------------------------------------------
 // A wave's tile: 16 keys and values of a kv head.
+// A lane's offsets in a tile, as numbers the compiler cannot take apart: it would keep each of their parts as 64-bit addresses, in registers
+// that the loop has no room for, where a uniform base and 32 bits per lane are all that a load takes.
 template <int HD, int BITS> struct CacheTile;
+struct TileLane { u32 k, v, ks, vs; };
+__device__ __forceinline__ u32 opaque(u32 x) { asm volatile("" : "+v"(x)); return x; }
+typedef u32 u32x4_t __attribute__((ext_vector_type(4)));
+typedef u32 u32x2_t __attribute__((ext_vector_type(2)));
+typedef const __attribute__((address_space(1))) unsigned char global_byte;
+template <typename T> __device__ __forceinline__ T from_global(global_byte* p) { return *(const __attribute__((address_space(1))) T*)p; }
+__device__ __forceinline__ global_byte* uniform_global(const void* p) { return (global_byte*)(u64)uniform_ptr((const unsigned char*)p); }
 template <int HD>
 struct CacheTile<HD, 16> {
   f16x8_t k[HD / 32];
   uint2 v[HD / 16];
-  __device__ __forceinline__ void load(const PagedArgs& a, u32 id, u32 g) {
+  static __device__ __forceinline__ TileLane lane_offsets() {
     const u32 lane = threadIdx.x & 63, lg = lane >> 4, lc = lane & 15;
-    const f16_t* kp = (const f16_t*)a.cache + ((u64)id * a.nkv + g) * (16 * HD);
-    const f16_t* vp = kp + (u64)a.n_blocks * a.nkv * (16 * HD);
-#pragma unroll
-    for (int s = 0; s < HD / 32; ++s) k[s] = ld_tile(kp + lc * HD + s * 32 + lg * 8);
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) v[d] = *(const uint2*)(vp + (d * 16 + lc) * 16 + lg * 4);
+    return {opaque(lc * (2 * HD) + lg * 16), opaque(lc * 32 + lg * 8), 0, 0};
   }
-  // dimension of a query's operand, step s
-  static __device__ __forceinline__ u32 q_dim(u32 s, u32 lg) { return s * 32 + lg * 8; }
-  struct Keys { f16x8_t k[HD / 32]; };
-  __device__ __forceinline__ Keys keys() const {
-    Keys r;
+  __device__ __forceinline__ void load(const PagedArgs& a, const TileLane& at, u32 id, u32 g) {
+    const f16_t* const first = (const f16_t*)a.cache + ((u64)id * a.nkv + g) * (16 * HD);
+    global_byte *const kp = uniform_global(first), *const vp = uniform_global(first + (u64)a.n_blocks * a.nkv * (16 * HD));
 #pragma unroll
-    for (int s = 0; s < HD / 32; ++s) r.k[s] = k[s];
-    return r;
+    for (int s = 0; s < HD / 32; ++s) { const u32x4_t x = from_global<u32x4_t>(kp + at.k + s * 64); k[s] = *(const f16x8_t*)&x; }
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) { const u32x2_t x = from_global<u32x2_t>(vp + at.v + d * 512); v[d] = make_uint2(x[0], x[1]); }
+  }
+  struct Query { f16x8_t q[HD / 32]; };
+  static __device__ __forceinline__ void load_query(const f16_t* row, Query& r) {
+    const u32 lg = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int s = 0; s < HD / 32; ++s) r.q[s] = ld_tile(row + s * 32 + lg * 8);
+  }
+  __device__ __forceinline__ floatx4_t scores(const Query& r) const {
+    floatx4_t x = floatx4_t{0.f, 0.f, 0.f, 0.f}, y = x;              // two chains
+#pragma unroll
+    for (int s = 0; s < HD / 32; s += 2) {
+      x = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[s], r.q[s], x, 0, 0, 0);
+      y = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[s + 1], r.q[s + 1], y, 0, 0, 0);
+    }
+    return x + y;
   }
   struct Probs { f16x4_t p; };
   static __device__ __forceinline__ Probs probs(const float (&p)[4]) { return {f16x4_t{(_Float16)p[0], (_Float16)p[1], (_Float16)p[2], (_Float16)p[3]}}; }
-  static __device__ __forceinline__ floatx4_t product(const uint2& w, const Probs& p, int, const floatx4_t& o) { return __builtin_amdgcn_mfma_f32_16x16x16f16(*(const f16x4_t*)&w, p.p, o, 0, 0, 0); }
-  struct Values { uint2 w[HD / 16]; };
-  __device__ __forceinline__ Values values() const {
-    Values r;
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) r.w[d] = v[d];
-    return r;
-  }
-  static constexpr int NW = 2, NV = HD / 16;                         // words of an operand of values, operands
+  struct Operand { u32 w[2]; };                                      // values of 16 dimensions
+  static constexpr int NV = HD / 16;                                 // operands of a tile's values
+  __device__ __forceinline__ Operand operand(int i) const { return {{v[i].x, v[i].y}}; }
   static __device__ __forceinline__ constexpr int of(int d) { return d; }          // operand of the dimensions' tile d
-  static __device__ __forceinline__ u32& word(Values& r, int d, int k) { return k ? r.w[d].y : r.w[d].x; }
+  static __device__ __forceinline__ floatx4_t product(const Operand& x, const Probs& p, int, const floatx4_t& o) {
+    const uint2 w = make_uint2(x.w[0], x.w[1]);
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(*(const f16x4_t*)&w, p.p, o, 0, 0, 0);
+  }
+  // whether some value is not finite (then those are taken out)
+  __device__ __forceinline__ bool take_strange_out() {
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+    const Probs none = probs(zero);
+    floatx4_t z = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) z = product(operand(d), none, 0, z);       // 0 unless something is not finite
+    if (!any_nan(z)) return false;
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) v[d] = make_uint2(only_finite(v[d].x), only_finite(v[d].y));
+    return true;
+  }
   // the 4 dimensions of accumulator tile d, or 4 of the 8 (or 4) neighbouring ones: register i of tile d is dimension
   static __device__ __forceinline__ u32 o_dim(int d, u32 lg, int i) { return d * 16 + lg * 4 + i; }
 };
 template <int HD>
 struct CacheTile<HD, 4> {
-  u32 k[HD / 32];                 // HD / 4 dimensions of a key: lane % 16, dimensions lane / 16 * HD / 4 ..
+  u32 k[4];                       // 32 dimensions of a key: lane % 16, dimensions 32 (lane / 16) .. (heads of 64: of lane / 16 % 2)
   u32 v[HD / 32];                 // HD / 16 dimensions of 4 values
   u32 ks, vs;                     // scale of the key's dimensions; of the 4 values'
-  __device__ __forceinline__ void load(const PagedArgs& a, u32 id, u32 g) {
-    const u32 lane = threadIdx.x & 63, lg = lane >> 4, lc = lane & 15;
-    const unsigned char* r = (const unsigned char*)a.cache + ((u64)id * a.nkv + g) * (17 * HD);
-    if constexpr (HD == 128) {
-      const uint4 x = *(const uint4*)(r + lane_key_off(lc, lg)), y = *(const uint4*)(r + 8 * HD + (lg * 16 + lc) * 16);
-      k[0] = x.x; k[1] = x.y; k[2] = x.z; k[3] = x.w;
-      v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w;
-      ks = r[16 * HD + lg * 16 + lc];
-      vs = *(const u32*)(r + 16 * HD + HD / 2 + (lc >> 2) * 16 + lg * 4);
-    } else {
-      const uint2 x = *(const uint2*)(r + lane_key_off(lc, lg)), y = *(const uint2*)(r + 8 * HD + (lg * 16 + lc) * 8);
-      k[0] = x.x; k[1] = x.y;
-      v[0] = y.x; v[1] = y.y;
-      ks = r[16 * HD + (lg >> 1) * 16 + lc];
-      vs = *(const u32*)(r + 16 * HD + HD / 2 + (lc >> 3) * 16 + lg * 4);
-    }
+  static __device__ __forceinline__ TileLane lane_offsets() {
+    const u32 lane = threadIdx.x & 63, lg = lane >> 4, lc = lane & 15, kg = lg % (HD / 32);
+    return {opaque(lc * (HD / 2) + kg * 16), opaque((lg * 16 + lc) * (HD / 8)), opaque(kg * 16 + lc), opaque(lc / (HD == 128 ? 4 : 8) * 16 + lg * 4)};
   }
-  static __device__ __forceinline__ u32 lane_key_off(u32 lc, u32 lg) { return lc * (HD / 2) + lg * (HD / 8); }
-  static __device__ __forceinline__ u32 q_dim(u32 s, u32 lg) { return lg * (HD / 4) + s * 8; }
-  struct Keys { f16x8_t k[HD / 32]; };
-  __device__ __forceinline__ Keys keys() const {
-    const float sc = __uint_as_float(ks << 23);
-    Keys r;
+  __device__ __forceinline__ void load(const PagedArgs& a, const TileLane& at, u32 id, u32 g) {
+    global_byte* const r = uniform_global((const unsigned char*)a.cache + ((u64)id * a.nkv + g) * (17 * HD));
+    const u32x4_t x = from_global<u32x4_t>(r + at.k);
+    k[0] = x[0]; k[1] = x[1]; k[2] = x[2]; k[3] = x[3];
+    if constexpr (HD == 128) {
+      const u32x4_t y = from_global<u32x4_t>(r + at.v + 8 * HD);
+      v[0] = y[0]; v[1] = y[1]; v[2] = y[2]; v[3] = y[3];
+    } else {
+      const u32x2_t y = from_global<u32x2_t>(r + at.v + 8 * HD);
+      v[0] = y[0]; v[1] = y[1];
+    }
+    ks = *(r + at.ks + 16 * HD);
+    vs = from_global<u32>(r + at.vs + (16 * HD + HD / 2));
+  }
+  // The product's B operand holds the elements 16 g .. and 64 + 16 g .. of its 128 in lane group g, its scales (like A's) are those of the
+  // elements 32 g .. in lane group g. Parts: with the row's largest magnitude in [128, 256), e4m3(x), e4m3(16 (x - that)) and so on: each
+  // takes four bits off a half's eleven, down to 2^-26 of the largest. Heads of 64: A holds a key's codes twice, and the
+  // second part meets the upper ones.
+  static constexpr int NP = HD == 128 ? 3 : 2;
+  struct Query { i32x8_t part[NP]; u32 scale; };     // scale: byte i for product i
+  static __device__ __forceinline__ void load_query(const f16_t* row, Query& r) {
+    const u32 lg = (threadIdx.x & 63) >> 4;
+    float x[HD / 4];
 #pragma unroll
-    for (int s = 0; s < HD / 32; ++s)
-      r.k[s] = f16x8_of(f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(k[s], sc, 0)), f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(k[s], sc, 1)),
-                        f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(k[s], sc, 2)), f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(k[s], sc, 3)));
-    return r;
+    for (int h = 0; h < HD / 64; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) load_n<_Float16, 8>((const _Float16*)row + h * 64 + lg * 16 + i * 8, x + h * 16 + i * 8);
+    u32 top = 0;
+#pragma unroll
+    for (int i = 0; i < HD / 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    top = max(top, (u32)__shfl_xor((int)top, 16));
+    top = max(top, (u32)__shfl_xor((int)top, 32));
+    const bool fine = top < 0x7F800000u;
+    const i32 e = top ? (i32)(top >> 23) - 127 - 7 : 0;              // (a half is a normal float)
+    const float up = __uint_as_float((u32)(127 - (fine ? e : 0)) << 23);
+#pragma unroll
+    for (int i = 0; i < HD / 4; ++i) x[i] = fine ? x[i] * up : 0.f;
+    i32 part[4][HD / 16] = {};
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) {
+        i32 w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j], x[4 * j + 1], 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j + 2], x[4 * j + 3], w, true);
+        part[p][j] = w;
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+        x[4 * j] = (x[4 * j] - lo[0]) * 16.f; x[4 * j + 1] = (x[4 * j + 1] - lo[1]) * 16.f;
+        x[4 * j + 2] = (x[4 * j + 2] - hi[0]) * 16.f; x[4 * j + 3] = (x[4 * j + 3] - hi[1]) * 16.f;
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r.part[p][j] = HD == 128 ? part[p][j] : part[2 * p + j / 4][j % (HD / 16)];
+    // (a row with an infinity or NaN: its scores are not a number)
+    const u32 s0 = (u32)(127 + e) - (HD == 64 && lg >= 2 ? 4u : 0u);
+    r.scale = !fine ? 0xFFFFFFu : HD == 128 ? s0 | (s0 - 4) << 8 | (s0 - 8) << 16 : s0 | (s0 - 8) << 8;
+  }
+  __device__ __forceinline__ floatx4_t scores(const Query& r) const {
+    const i32x8_t a = {(i32)k[0], (i32)k[1], (i32)k[2], (i32)k[3], 0, 0, 0, 0};
+    floatx4_t x = floatx4_t{0.f, 0.f, 0.f, 0.f};                     // (formats: A e2m1 = 4, B e4m3 = 0)
+    x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, r.part[0], x, 4, 0, 0, (i32)ks, 0, (i32)r.scale);
+    x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, r.part[1], x, 4, 0, 0, (i32)ks, 1, (i32)r.scale);
+    if constexpr (NP == 3) x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, r.part[NP - 1], x, 4, 0, 0, (i32)ks, 2, (i32)r.scale);
+    return x;
   }
   struct Probs { f16x8_t even, odd; };                               // the probability at the lower, at the upper half of each word
   static __device__ __forceinline__ Probs probs(const float (&p)[4]) {
@@ -164,47 +236,49 @@ struct CacheTile<HD, 4> {
     for (int i = 0; i < 4; ++i) { const _Float16 h = (_Float16)p[i]; e[i] = *(const uint16_t*)&h; }
     return {f16x8_of(e[0], e[1], e[2], e[3]), f16x8_of(e[0] << 16, e[1] << 16, e[2] << 16, e[3] << 16)};
   }
-  struct Values { u32 w[HD / 32][4]; };                              // [pair of dimensions][value]
-  __device__ __forceinline__ Values values() const {
-    Values r;
+  struct Operand { u32 w[4]; };                                      // a pair of dimensions' tiles, of 4 values
+  static constexpr int NV = HD / 32;
+  __device__ __forceinline__ Operand operand(int i) const {
+    Operand r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float sc = __uint_as_float((vs >> (8 * i) & 0xFFu) << 23);
-      if constexpr (HD == 128) {
-        r.w[0][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[i], sc, 0)); r.w[1][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[i], sc, 1));
-        r.w[2][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[i], sc, 2)); r.w[3][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v[i], sc, 3));
-      } else {
-        const u32 w = i & 1 ? v[i / 2] >> 16 : v[i / 2];
-        r.w[0][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 0)); r.w[1][i] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 1));
-      }
+    for (int t = 0; t < 4; ++t) {
+      const float sc = __uint_as_float((vs >> (8 * t) & 0xFFu) << 23);
+      const u32 w = HD == 128 ? v[t] : t & 1 ? v[t / 2] >> 16 : v[t / 2];
+      r.w[t] = f16x2_bits(i == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 0) : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 1)
+                        : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 2) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 3));
     }
     return r;
   }
-  static __device__ __forceinline__ floatx4_t product(const u32 (&w)[4], const Probs& p, int d, const floatx4_t& o) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(w[0], w[1], w[2], w[3]), d & 1 ? p.odd : p.even, o, 0, 0, 0);
-  }
-  static constexpr int NW = 4, NV = HD / 32;
   static __device__ __forceinline__ constexpr int of(int d) { return d / 2; }
-  static __device__ __forceinline__ u32& word(Values& r, int d, int k) { return r.w[d][k]; }
+  static __device__ __forceinline__ floatx4_t product(const Operand& x, const Probs& p, int d, const floatx4_t& o) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(x.w[0], x.w[1], x.w[2], x.w[3]), d & 1 ? p.odd : p.even, o, 0, 0, 0);
+  }
+  __device__ __forceinline__ bool take_strange_out() {               // (only a scale of 255 is not a number)
+    const u32 odd = ((vs & 0x7F7F7F7Fu) + 0x01010101u) & vs & 0x80808080u;
+    if (!__ballot(odd != 0)) return false;
+    vs &= ~((odd >> 7) * 0xFFu);
+    return true;
+  }
   static __device__ __forceinline__ u32 o_dim(int d, u32 lg, int i) { return (lg * 4 + i) * (HD / 16) + d; }
 };
 
-#define PAGED_WAVES 8
+#define PAGED_WAVES 8              // waves of a workgroup of the prompt part
 #define PAGED_MAX_SEQS 1024u       // sequences whose views a workgroup keeps in LDS
-template <int HD, int CT>
+template <int HD, int CT, int NW>
 struct ShortShared {
-  floatx4_t o[PAGED_WAVES][CT][HD / 16][64];         // a result that one wave leaves for another, as its registers hold it
-  float m[PAGED_WAVES][CT][16], l[PAGED_WAVES][CT][16];
-  SeqView view[PAGED_MAX_SEQS];
-  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], last[2];
+  floatx4_t o[NW][CT][HD / 16][64];                  // a result that one wave leaves for another, as its registers hold it
+  float m[NW][CT][16], l[NW][CT][16];
+  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[NW], last[2];
+  i32 pos0[PAGED_MAX_SEQS];
+  unsigned char n[PAGED_MAX_SEQS];                   // (a short sequence has at most 64 rows)
 };
 
-// exclusive prefix sums of f(0 .. n) into pre[0 .. n], by eight waves
-template <typename F>
+// exclusive prefix sums of f(0 .. n) into pre[0 .. n], by a workgroup of NW waves
+template <u32 NW, typename F>
 __device__ __forceinline__ void prefix_sums(u32* pre, u32* wave_sum, u32 n, F f) {
   const u32 lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   u32 base = 0;
-  for (u32 i0 = 0; i0 < n; i0 += 64 * PAGED_WAVES) {
+  for (u32 i0 = 0; i0 < n; i0 += 64 * NW) {
     const u32 i = i0 + threadIdx.x;
     u32 v = i < n ? f(i) : 0u;
 #pragma unroll
@@ -213,7 +287,7 @@ __device__ __forceinline__ void prefix_sums(u32* pre, u32* wave_sum, u32 n, F f)
     if (lane == 63) wave_sum[w] = v;
     __syncthreads();
     u32 before = base;
-    for (u32 k = 0; k < PAGED_WAVES; ++k) { if (k < w) before += wave_sum[k]; base += wave_sum[k]; }
+    for (u32 k = 0; k < NW; ++k) { if (k < w) before += wave_sum[k]; base += wave_sum[k]; }
     if (i < n) pre[i + 1] = before + v;
   }
   if (threadIdx.x == 0) pre[0] = 0;
@@ -247,19 +321,14 @@ struct ShortAcc {
     m = mn;
   }
   // vis: bit i of the lane's four keys seen by the lane's row (used where `edge`)
-  __device__ __forceinline__ void add(const typename Tile::Keys& key, const typename Tile::Values& val, const f16x8_t (&q)[HD / 32], float c, bool edge, u32 vis) {
-    floatx4_t s = floatx4_t{0.f, 0.f, 0.f, 0.f}, s2 = s;             // two chains
-#pragma unroll
-    for (int i = 0; i < HD / 32; i += 2) {
-      s = __builtin_amdgcn_mfma_f32_16x16x32_f16(key.k[i], q[i], s, 0, 0, 0);
-      s2 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key.k[i + 1], q[i + 1], s2, 0, 0, 0);
-    }
-    s = (s + s2) * c;
+  __device__ __forceinline__ void add(const Tile& t, const typename Tile::Query& q, float c, bool edge, u32 vis) {
+    floatx4_t s = t.scores(q);
     if (edge) {
+      asm volatile("" ::: "memory");                                 // (a branch: few tiles are)
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[i] = vis >> i & 1u ? s[i] : -INFINITY;
     }
-    float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * c;
     if (__ballot(top > m + 8.f)) {
       top = quad_max(top);
       const float mn = fmaxf(m, top);
@@ -269,17 +338,17 @@ struct ShortAcc {
       for (int d = 0; d < HD / 16; ++d) o[d] *= f;
       m = mn;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
+    const float ref = m == -INFINITY ? 0.f : -m;
     float p[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { p[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += p[i]; }      // exp2(-inf) = 0
+    for (int i = 0; i < 4; ++i) { p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, ref)); l += p[i]; }      // exp2(-inf) = 0
     const typename Tile::Probs pp = Tile::probs(p);
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d) o[d] = Tile::product(val.w[Tile::of(d)], pp, d, o[d]);
+    for (int d = 0; d < HD / 16; ++d) o[d] = Tile::product(t.operand(Tile::of(d)), pp, d, o[d]);
   }
 };
-template <int HD, int BITS, int CT>
-__device__ __forceinline__ void leave_in_lds(ShortShared<HD, CT>& sh, u32 at, const ShortAcc<HD, BITS> (&acc)[CT]) {
+template <int HD, int BITS, int CT, int NW>
+__device__ __forceinline__ void leave_in_lds(ShortShared<HD, CT, NW>& sh, u32 at, const ShortAcc<HD, BITS> (&acc)[CT]) {
   const u32 lane = threadIdx.x & 63;
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -289,8 +358,8 @@ __device__ __forceinline__ void leave_in_lds(ShortShared<HD, CT>& sh, u32 at, co
     for (int d = 0; d < HD / 16; ++d) sh.o[at][c][d][lane] = acc[c].o[d];
   }
 }
-template <int HD, int BITS, int CT>
-__device__ __forceinline__ void add_from_lds(const ShortShared<HD, CT>& sh, u32 at, ShortAcc<HD, BITS> (&acc)[CT]) {
+template <int HD, int BITS, int CT, int NW>
+__device__ __forceinline__ void add_from_lds(const ShortShared<HD, CT, NW>& sh, u32 at, ShortAcc<HD, BITS> (&acc)[CT]) {
   const u32 lane = threadIdx.x & 63;
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -339,39 +408,27 @@ __device__ __forceinline__ void add_past_caches(const float* slot, ShortAcc<HD, 
       for (int i = 0; i < 4; ++i) acc[c].o[d][i] = acc[c].o[d][i] * mine + __uint_as_float((u32)(v[d][i >> 1] >> (32 * (i & 1)))) * other;
   }
 }
-// whether a tile has a value that is not finite (then those are taken out of it)
-template <int HD, int BITS>
-__device__ __forceinline__ bool take_strange_out(typename CacheTile<HD, BITS>::Values& val) {
-  typedef CacheTile<HD, BITS> Tile;
-  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-  const typename Tile::Probs none = Tile::probs(zero);
-  floatx4_t z = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int v = 0; v < Tile::NV; ++v) z = Tile::product(val.w[v], none, 0, z);       // 0 unless something is not finite
-  if (!any_nan(z)) return false;
-#pragma unroll
-  for (int v = 0; v < Tile::NV; ++v)
-#pragma unroll
-    for (int k = 0; k < Tile::NW; ++k) Tile::word(val, v, k) = only_finite(Tile::word(val, v, k));
-  return true;
-}
-// ... and given to the rows that see them
+// what CacheTile::take_strange_out has taken out, given to the rows that see it
 template <int HD, int BITS, int CT>
-__device__ __forceinline__ void give_strange(const typename CacheTile<HD, BITS>::Values& val, ShortAcc<HD, BITS> (&acc)[CT], const u32 (&vis)[CT]) {
+__device__ __forceinline__ void give_strange(const CacheTile<HD, BITS>& t, ShortAcc<HD, BITS> (&acc)[CT], const u32 (&vis)[CT]) {
   typedef CacheTile<HD, BITS> Tile;
+  constexpr int PER = HD / 16 / Tile::NV;            // tiles of dimensions per operand
 #pragma unroll
-  for (int d = 0; d < HD / 16; ++d) {
-    typename Tile::Values odd = val;
+  for (int v = 0; v < Tile::NV; ++v) {
+    typename Tile::Operand x = t.operand(v);
 #pragma unroll
-    for (int k = 0; k < Tile::NW; ++k) Tile::word(odd, Tile::of(d), k) = strange_codes(Tile::word(odd, Tile::of(d), k));
+    for (u32& w : x.w) w = strange_codes(w);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const float see[4] = {vis[c] & 1u ? 1.f : 0.f, vis[c] & 2u ? 1.f : 0.f, vis[c] & 4u ? 1.f : 0.f, vis[c] & 8u ? 1.f : 0.f};
-      const floatx4_t n = Tile::product(odd.w[Tile::of(d)], Tile::probs(see), d, floatx4_t{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[c].o[d][i] += strange_sum(n[i]);
+      for (int d = v * PER; d < (v + 1) * PER; ++d) {
+        const floatx4_t n = Tile::product(x, Tile::probs(see), d, floatx4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[c].o[d][i] += strange_sum(n[i]);
+        __builtin_amdgcn_sched_barrier(0);           // (rare: no registers for it)
+      }
     }
-    __builtin_amdgcn_sched_barrier(0);               // (rare: no registers for it)
   }
 }
 
@@ -387,24 +444,28 @@ __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { r
 // A pair inside a run is finished where it is. One that several waves of a workgroup share is added up by the wave it begins in (in
 // LDS, after the one barrier); one that several workgroups share leaves a result of each in the workspace, and the workgroup that comes
 // last adds them up, its waves an eighth of them each. All sums in the order of the runs: results do not depend on who comes when.
-// Few short pairs (half as many as workgroups, SHORT_CAP tiles a workgroup) are dealt out whole instead, a workgroup or several to each: no
-// result then crosses workgroups up to SHORT_CAP tiles, which would take longer than the tiles do.
+// Few short pairs (half as many as workgroups, eight tiles a wave) are dealt out whole instead, a workgroup or several to each: up to that
+// length no result then crosses workgroups, which would take longer than the tiles do.
 // The loop over tiles is written out NT times for its registers, so all that is rare stands outside of it, once.
 #define SHORT_QUANTUM 4u
-#define SHORT_CAP 64u
-template <int HD, int BITS, int CT, int NT>
-__device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, CT>& sh, u32 wg, u32 nwg) {
+template <int HD, int BITS, int CT, int NT, int NW>
+__device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, CT, NW>& sh, u32 wg, u32 nwg) {
   typedef CacheTile<HD, BITS> Tile;
-  constexpr u32 NW = PAGED_WAVES;
+  constexpr u32 CAP = 8 * NW;                        // tiles of a workgroup's share of a pair that is dealt out whole
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
   auto scalar = [](u32 x) { return (u32)__builtin_amdgcn_readfirstlane(x); };
+  auto units = [&](u32 s) {
+    const SeqView v = seq_view(a, s);
+    sh.pos0[s] = v.pos0; sh.n[s] = (unsigned char)v.n;
+    return short_unit_count(a, v);
+  };
   bool whole = a.n_seqs * a.nkv <= nwg / 2;          // pairs dealt out whole: then `pre` counts workgroups, else units
   if (whole) {
-    prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return (short_unit_count(a, sh.view[s] = seq_view(a, s)) + SHORT_CAP - 1) / SHORT_CAP * a.nkv; });
+    prefix_sums<NW>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return (units(s) + CAP - 1) / CAP * a.nkv; });
     whole = scalar(sh.pre[a.n_seqs]) <= nwg;
     if (!whole) __syncthreads();
   }
-  if (!whole) prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return short_unit_count(a, sh.view[s] = seq_view(a, s)) * a.nkv; });
+  if (!whole) prefix_sums<NW>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return units(s) * a.nkv; });
   const u32 U = scalar(sh.pre[a.n_seqs]), wg_units = max(SHORT_QUANTUM, (U + nwg * NW - 1) / (nwg * NW)) * NW;
   if (whole ? wg >= U : wg * wg_units >= U) return;
   if (threadIdx.x < 2) sh.last[threadIdx.x] = 0;
@@ -413,9 +474,9 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   struct Pair { u32 s, g, first, nv, t0, n, row, zb, wlo; i32 pos0; };
   auto pair_of = [&](u32 s, u32 g) {
     Pair p;
-    const SeqView v = sh.view[s];
     p.s = s; p.g = g;
-    p.t0 = scalar(v.t0); p.n = scalar(v.n); p.pos0 = (i32)scalar((u32)v.pos0);
+    p.t0 = (u32)max(0, min((i32)((const_u32*)(u64)uniform_ptr((const u32*)a.cu))[s], (i32)a.n_tokens));
+    p.n = scalar(sh.n[s]); p.pos0 = (i32)scalar((u32)sh.pos0[s]);
     const Seen e = seen_tiles<16>(a, p.pos0, p.pos0 + (i32)p.n - 1);
     p.zb = scalar(e.zb); p.wlo = scalar(e.wlo); p.nv = scalar(max(1u, e.n));
     p.first = whole ? 0u : scalar(sh.pre[s]) + g * p.nv;
@@ -436,23 +497,22 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   Pair cur = pair_at(whole ? wg : wg * wg_units);
   u32 wg0 = wg * wg_units, wg1 = min(wg0 + wg_units, U), from = 0;         // from: the first workgroup of the pair (whole pairs)
   if (whole) {
-    const u32 per = (cur.nv + SHORT_CAP - 1) / SHORT_CAP;
+    const u32 per = (cur.nv + CAP - 1) / CAP;
     from = scalar(sh.pre[cur.s]) + cur.g * per;
-    wg0 = (wg - from) * SHORT_CAP; wg1 = min(wg0 + SHORT_CAP, cur.nv);
+    wg0 = (wg - from) * CAP; wg1 = min(wg0 + CAP, cur.nv);
   }
   const u32 quantum = (wg1 - wg0 + NW - 1) / NW, u0 = min(wg0 + w * quantum, wg1), u1 = min(u0 + quantum, wg1);
   auto first_wg = [&](const Pair& p) { return whole ? from : p.first / wg_units; };
-  auto n_wgs = [&](const Pair& p) { return whole ? (p.nv + SHORT_CAP - 1) / SHORT_CAP : (p.first + p.nv - 1) / wg_units - p.first / wg_units + 1; };
-  f16x8_t q[CT][HD / 32];
+  auto n_wgs = [&](const Pair& p) { return whole ? (p.nv + CAP - 1) / CAP : (p.first + p.nv - 1) / wg_units - p.first / wg_units + 1; };
+  const TileLane at = Tile::lane_offsets();
+  typename Tile::Query q[CT];
   i32 qpos[CT];                                      // position of the lane's row (no row: before every key)
   auto load_q = [&](const Pair& p) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const u32 r = c * 16 + lc, rr = min(r, p.n * a.G - 1), tok = rr / a.G, h = rr - tok * a.G;
       qpos[c] = r < p.n * a.G ? p.pos0 + (i32)tok : -1;
-      const f16_t* qp = a.q + (u64)(p.t0 + tok) * a.qs + (u64)(p.g * a.G + h) * HD;
-#pragma unroll
-      for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(qp + Tile::q_dim(s, lg));
+      Tile::load_query(a.q + (u64)(p.t0 + tok) * a.qs + (u64)(p.g * a.G + h) * HD, q[c]);
     }
   };
   ShortAcc<HD, BITS> acc[CT];
@@ -506,7 +566,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
       if (au >= u1) return;
       k0[j] = ak;
       in_cache[j] = aid < a.n_blocks;
-      tile[j].load(a, min(aid, a.n_blocks - 1), ap.g);
+      tile[j].load(a, at, min(aid, a.n_blocks - 1), ap.g);
       if (++au < u1) {
         if (au == ap.first + ap.nv) ap = pair_after(ap);
         ak = key_of(ap, au);
@@ -519,16 +579,14 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     u32 u = u0;
     auto step = [&](int j) {                         // the tile of slot j; whether its pair, or the run, ends with it
       if (cur.pos0 + (i32)cur.n > 0) {
-        const typename Tile::Keys key = tile[j].keys();
-        typename Tile::Values val = tile[j].values();
         const bool edge = edge_of(cur, k0[j], in_cache[j]);
         u32 vis[CT] = {};
         if (edge) {
           see(k0[j], in_cache[j], vis);
-          strange |= take_strange_out<HD, BITS>(val);
+          strange |= tile[j].take_strange_out();
         }
 #pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c].add(key, val, q[c], a.c, edge, vis[c]);
+        for (int c = 0; c < CT; ++c) acc[c].add(tile[j], q[c], a.c, edge, vis[c]);
       }
       ask(j);
       ++u;
@@ -548,16 +606,25 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
           const u32 key = key_of(cur, x), b = block_of(cur, key);
           if (!edge_of(cur, key, b < a.n_blocks)) continue;
           Tile t;
-          t.load(a, min(b, a.n_blocks - 1), cur.g);
+          t.load(a, at, min(b, a.n_blocks - 1), cur.g);
           u32 vis[CT];
           see(key, b < a.n_blocks, vis);
-          give_strange<HD, BITS, CT>(t.values(), acc, vis);
+          give_strange<HD, BITS, CT>(t, acc, vis);
         }
         strange = false;
+        if (u < u1) {                                // (the tiles on their way are asked for again: none of them stays in registers over this)
+          ap = u == cur.first + cur.nv ? pair_after(cur) : cur;
+          au = u;
+          ak = key_of(ap, au);
+          aid = block_of(ap, ak);
+#pragma unroll
+          for (int x = 0; x < NT; ++x) ask(x);
+          j = 0;
+        }
       }
       const bool done = u == cur.first + cur.nv;
       if (done && cur.first >= u0) finish(cur);                             // the pair is this wave's alone
-      else if (cur.first < u0) leave_in_lds<HD, BITS, CT>(sh, w, acc);      // its beginning is another wave's
+      else if (cur.first < u0) leave_in_lds<HD, BITS, CT, NW>(sh, w, acc);      // its beginning is another wave's
       if (u == u1) break;                                                   // (a pair that begins here and goes on: in acc)
       cur = pair_after(cur);
       load_q(cur);
@@ -570,7 +637,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   // pair that the workgroup's run begins inside of.
   auto others = [&](const Pair& p, u32 x) {          // what the waves from x on have of the pair
 #pragma unroll 1
-    for (; x < NW && wg0 + x * quantum < min(p.first + p.nv, wg1); ++x) add_from_lds<HD, BITS, CT>(sh, x, acc);
+    for (; x < NW && wg0 + x * quantum < min(p.first + p.nv, wg1); ++x) add_from_lds<HD, BITS, CT, NW>(sh, x, acc);
   };
   auto hand_on = [&](const Pair& p, u32 which) {     // the workgroup's share of the pair to the workspace; who comes last is told
     leave_past_caches<HD, BITS, CT>(a.part + (u64)(2 * wg + which) * short_slot<HD, CT>(), acc, p.n * a.G);
@@ -605,12 +672,12 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 #pragma unroll 1
     for (u32 x = w * per; x < min(np, (w + 1) * per); ++x)
       add_past_caches<HD, BITS, CT>(a.part + (u64)(2 * (w0 + x) + (x ? 0u : 1u)) * short_slot<HD, CT>(), acc, p.n * a.G);
-    leave_in_lds<HD, BITS, CT>(sh, w, acc);
+    leave_in_lds<HD, BITS, CT, NW>(sh, w, acc);
     __syncthreads();
     if (w == 0) {
       clear();
 #pragma unroll 1
-      for (u32 x = 0; x < NW; ++x) add_from_lds<HD, BITS, CT>(sh, x, acc);
+      for (u32 x = 0; x < NW; ++x) add_from_lds<HD, BITS, CT, NW>(sh, x, acc);
       finish(p);
     }
     __syncthreads();
@@ -660,7 +727,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
   constexpr int CT = PROMPT_CT;
   constexpr u32 BLK = 16 * HD * 2, NB = 4, STAGE = 2 * NB * BLK, NS = BITS == 4 ? 2 : (PROMPT_RING / STAGE > 6 ? 6 : PROMPT_RING / STAGE), TPW = BLK / 1024;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
-  prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return prompt_items(a, s); });
+  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return prompt_items(a, s); });
   const u32 items = (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]) * a.nkv, parts = prompt_parts(a, items, nwg), total = items * parts;
   u32* const ctr = a.ctr + (u64)a.n_seqs * a.nkv;
   const u32 lds0 = (u32)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sh.ring;
@@ -949,7 +1016,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
 struct PromptMergeShared { u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES]; };
 template <int HD>
 __device__ __forceinline__ void prompt_merge(const PagedArgs& a, PromptMergeShared& sh, u32 wg, u32 nwg, u32 nwg_prompt) {
-  prefix_sums(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return prompt_items(a, s); });
+  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return prompt_items(a, s); });
   const u32 items = sh.pre[a.n_seqs] * a.nkv, parts = prompt_parts(a, items, nwg_prompt), lane = threadIdx.x & 63;
   if (parts < 2) return;
   for (u32 i = wg * PAGED_WAVES + (threadIdx.x >> 6); i < items * PROMPT_ROWS; i += nwg * PAGED_WAVES) {
@@ -976,10 +1043,10 @@ __device__ __forceinline__ void prompt_merge(const PagedArgs& a, PromptMergeShar
 }
 
 // Batches that may hold both: every workgroup first its runs of the few rows' tiles, then prompt items from the counter.
-template <int HD, int CT> union PagedShared { ShortShared<HD, CT> s; PromptShared p; };
+template <int HD, int CT> union PagedShared { ShortShared<HD, CT, PAGED_WAVES> s; PromptShared p; };
 template <int HD, int BITS, int CT, int NT>
 __device__ __forceinline__ void paged_both(const PagedArgs& a, PagedShared<HD, CT>& sh, u32 wg, u32 nwg) {
-  paged_short<HD, BITS, CT, NT>(a, sh.s, wg, nwg);
+  paged_short<HD, BITS, CT, NT, PAGED_WAVES>(a, sh.s, wg, nwg);
   __syncthreads();
   paged_prompt<HD, BITS>(a, sh.p, wg, nwg, true);
 }

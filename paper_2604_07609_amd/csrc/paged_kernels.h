@@ -6,8 +6,12 @@
 #define STORE_UNROLL 2                                 // rows of a lane group on their way at a time
 // Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold), and tiles of keys on their way
 #define SHORT_MORE(HD) ((HD) == 64 ? 4 : 2)
-#define SHORT_AHEAD(HD, BITS, CT) ((CT) > 1 ? 2 : (HD) == 128 && (BITS) == 16 ? 3 : 4)
+#define SHORT_AHEAD(HD, BITS, CT) ((CT) > 1 ? 2 : (HD) == 128 || (BITS) == 4 ? 3 : 4)
 #define PAGED_BOUNDS __launch_bounds__(512) __attribute__((amdgpu_num_vgpr(120)))       // (see PHASE_KERNEL8)
+// One row tile over a 4-bit cache is bound by instructions: three workgroups of four waves on a compute unit, else one of eight
+#define SHORT_SMALL(BITS, CT) ((BITS) == 4 && (CT) == 1)
+#define SHORT_WAVES(BITS, CT) (SHORT_SMALL(BITS, CT) ? 4 : 8)
+#define SHORT_PER_CU(BITS, CT) (SHORT_SMALL(BITS, CT) ? 3 : 1)
 
 template <typename T, int HD, int BITS> __global__ void k_kv_store(StoreArgs a);
 __global__ void k_kv_read(ReadArgs a, u32 hd);
