@@ -336,7 +336,7 @@ struct DevCtx {
   // norms, rotates and stores them, and the attention is that of paged_attention.h
   u32 paged, window, sinks, kv_bits;
   u64 kv_layer_bytes;   // of the KV pool
-  u32* paged_ctr;       // [max_batch][nkv] + 2 (zeros between launches)
+  u32* paged_ctr;       // counters of its launches (zeros between them)
   float* paged_part;    // results of sequences that several workgroups share
   u32* attn_merge_ctr;  // [max_batch][nkv] chunks of a context that are done, where the attention kernel merges them itself (zeros between launches)
 };

@@ -138,8 +138,8 @@ static PagedPlan paged_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_seqs, u32 n
   // parts of 256 keys at least, where the items are too few for the chip
   const bool few = (u64)n_tokens * G / PROMPT_ROWS * nkv < p.wgs;
   p.n_splits = p.prompt && few ? std::max(1u, key_steps / 4) : 1u;
-  p.ctr_bytes = (((u64)n_seqs * nkv + 2) * 4 + 255) / 256 * 256;
-  p.part_bytes = 2ull * p.wgs * p.ct * (128 + 16 * hd) * 4;
+  p.ctr_bytes = (paged_counters((u64)n_seqs * nkv, p.wgs) * 4 + 255) / 256 * 256;
+  p.part_bytes = p.ct ? short_floats(p.wgs, hd, p.ct) * 4 : 0;
   p.prompt_bytes = p.prompt ? (u64)p.wgs * PROMPT_SLOT(hd) * 4 : 0;
   return p;
 }
@@ -159,7 +159,9 @@ extern "C" int blink_attention_workspace_bytes(int32_t device, const blink_kv_ca
   if (int rc = compute_units(device, &n_cu)) return rc;
   // (n_tokens below n_seqs * max_q: the larger of the two kinds of launches; and what a smaller max_q would need)
   const PagedPlan p = paged_plan(c->head_dim, c->bits, n_q_heads, c->n_kv_heads, n_seqs, 0, max_q, 1, n_cu);
-  *bytes = p.ctr_bytes + std::max<u64>(p.part_bytes + p.prompt_bytes, 2ull * n_cu * std::max(SHORT_MORE(c->head_dim), SHORT_PER_CU(c->bits, 1)) * (128 + 16 * c->head_dim) * 4);
+  const u32 one = n_cu * SHORT_PER_CU(c->bits, 1), more = SHORT_MORE(c->head_dim);
+  const u64 least = std::max(short_floats(one, c->head_dim, 1), short_floats(n_cu, c->head_dim, more)) * 4;
+  *bytes = (paged_counters((u64)n_seqs * c->n_kv_heads, one) * 4 + 255) / 256 * 256 + std::max(p.part_bytes + p.prompt_bytes, least);
   return BLINK_OK;
 }
 

@@ -443,11 +443,17 @@ __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { r
 // wave reads the same number of bytes, with NT tiles on their way, and waits for nobody until its run ends.
 // A pair inside a run is finished where it is. One that several waves of a workgroup share is added up by the wave it begins in (in
 // LDS, after the one barrier); one that several workgroups share leaves a result of each in the workspace, and the workgroup that comes
-// last adds them up, its waves an eighth of them each. All sums in the order of the runs: results do not depend on who comes when.
+// last adds them up, its waves a part of them each. Of more than SHORT_GROUP such results, those of every SHORT_GROUP workgroups are added up
+// by the last of these first (65531 keys of one sequence, 4-bit, 171 results a pair: 53 us in one go). All sums in the order of the
+// runs: results do not depend on who comes when.
 // Few short pairs (half as many as workgroups, eight tiles a wave) are dealt out whole instead, a workgroup or several to each: up to that
 // length no result then crosses workgroups, which would take longer than the tiles do.
 // The loop over tiles is written out NT times for its registers, so all that is rare stands outside of it, once.
 #define SHORT_QUANTUM 4u
+#define SHORT_GROUP 16u
+// 32-bit counters of a launch of nwg workgroups (pairs; two for the prompt part; groups) and floats of its results
+__host__ __device__ __forceinline__ u64 paged_counters(u64 pairs, u32 nwg) { return pairs + 2 + 2 * ((nwg + SHORT_GROUP - 1) / SHORT_GROUP); }
+__host__ __device__ __forceinline__ u64 short_floats(u32 nwg, u32 hd, u32 ct) { return 2ull * (nwg + (nwg + SHORT_GROUP - 1) / SHORT_GROUP) * ct * (128 + 16 * hd); }
 template <int HD, int BITS, int CT, int NT, int NW>
 __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, CT, NW>& sh, u32 wg, u32 nwg) {
   typedef CacheTile<HD, BITS> Tile;
@@ -639,16 +645,28 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 #pragma unroll 1
     for (; x < NW && wg0 + x * quantum < min(p.first + p.nv, wg1); ++x) add_from_lds<HD, BITS, CT, NW>(sh, x, acc);
   };
-  auto hand_on = [&](const Pair& p, u32 which) {     // the workgroup's share of the pair to the workspace; who comes last is told
-    leave_past_caches<HD, BITS, CT>(a.part + (u64)(2 * wg + which) * short_slot<HD, CT>(), acc, p.n * a.G);
+  // a pair's results and those of its groups: which of a workgroup's (group's) two slots, by whether the pair begins before it
+  const u32 group = wg / SHORT_GROUP, group0 = group * SHORT_GROUP;
+  auto piece = [&](u32 x, u32 first) { return a.part + (u64)(2 * x + (x == first ? 1u : 0u)) * short_slot<HD, CT>(); };
+  auto group_piece = [&](u32 x, u32 first) { return a.part + (u64)(2 * (nwg + x) + (x == first / SHORT_GROUP ? 1u : 0u)) * short_slot<HD, CT>(); };
+  // counts one result more; whether it was the last of n
+  auto count = [&](u32* ctr, u32 n) {
+    u32 before = 0;
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
     if (lane == 0) {
-      const u32 np = n_wgs(p);
-      u32* const ctr = a.ctr + (u64)p.s * a.nkv + p.g;
-      const u32 before = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      sh.last[which] = before == np - 1;
-      if (before == np - 1) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      before = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (before == n - 1) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    return scalar(before) == n - 1;
+  };
+  u32* const group_ctr = a.ctr + (u64)a.n_seqs * a.nkv + 2;
+  auto hand_on = [&](const Pair& p, u32 which) {     // the workgroup's share of the pair to the workspace; who comes last is told
+    leave_past_caches<HD, BITS, CT>(a.part + (u64)(2 * wg + which) * short_slot<HD, CT>(), acc, p.n * a.G);
+    const u32 f = first_wg(p), np = n_wgs(p);
+    u32 last;
+    if (np <= SHORT_GROUP) last = count(a.ctr + (u64)p.s * a.nkv + p.g, np);
+    else last = count(group_ctr + 2 * group + (f >= group0 ? 1u : 0u), min(f + np, group0 + SHORT_GROUP) - max(f, group0));
+    if (lane == 0) sh.last[which] = last;
   };
   if (u0 < u1 && cur.first >= u0 && u1 < cur.first + cur.nv) {
     others(cur, w + 1);
@@ -667,20 +685,33 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   for (u32 which = 0; which < 2; ++which) {
     if (!scalar(sh.last[which])) continue;
     const Pair p = pair_at(whole ? wg : which ? wg1 - 1 : wg0);
-    const u32 w0 = first_wg(p), np = n_wgs(p), per = (np + NW - 1) / NW;
-    clear();
+    const u32 f = first_wg(p), np = n_wgs(p), rows = p.n * a.G;
+    const bool grouped = np > SHORT_GROUP;
+    // of one level: results x0 .. x1, the waves a run of them each, then wave 0 the waves'
+    u32 x0 = grouped ? max(f, group0) : f, x1 = grouped ? min(f + np, group0 + SHORT_GROUP) : f + np;
 #pragma unroll 1
-    for (u32 x = w * per; x < min(np, (w + 1) * per); ++x)
-      add_past_caches<HD, BITS, CT>(a.part + (u64)(2 * (w0 + x) + (x ? 0u : 1u)) * short_slot<HD, CT>(), acc, p.n * a.G);
-    leave_in_lds<HD, BITS, CT, NW>(sh, w, acc);
-    __syncthreads();
-    if (w == 0) {
+    for (u32 level = grouped ? 0u : 1u;; ++level) {
+      const u32 per = (x1 - x0 + NW - 1) / NW, mine = min(x1, x0 + w * per), end = min(x1, mine + per);
       clear();
 #pragma unroll 1
-      for (u32 x = 0; x < NW; ++x) add_from_lds<HD, BITS, CT, NW>(sh, x, acc);
-      finish(p);
+      for (u32 x = mine; x < end; ++x) add_past_caches<HD, BITS, CT>(level && grouped ? group_piece(x, f) : piece(x, f), acc, rows);
+      leave_in_lds<HD, BITS, CT, NW>(sh, w, acc);
+      __syncthreads();
+      if (w == 0) {
+        clear();
+#pragma unroll 1
+        for (u32 x = 0; x < NW; ++x) add_from_lds<HD, BITS, CT, NW>(sh, x, acc);
+        if (level) finish(p);
+        else {
+          leave_past_caches<HD, BITS, CT>(a.part + (u64)(2 * (nwg + group) + (f >= group0 ? 1u : 0u)) * short_slot<HD, CT>(), acc, rows);
+          const bool last = count(a.ctr + (u64)p.s * a.nkv + p.g, (f + np - 1) / SHORT_GROUP - f / SHORT_GROUP + 1);
+          if (lane == 0) sh.last[which] = last;
+        }
+      }
+      __syncthreads();
+      if (level || !scalar(sh.last[which])) break;
+      x0 = f / SHORT_GROUP; x1 = (f + np - 1) / SHORT_GROUP + 1;
     }
-    __syncthreads();
   }
 }
 

@@ -198,7 +198,7 @@ def run_attention(cache, tables, lens, cu, q, max_q, window=0, sinks=0, scale=1.
     out = torch.full(q.shape, fill, dtype=torch.float16, device="cuda")
     B.paged_attention(dev(q), cache, dev(tables), dev(lens), dev(cu), out, workspace, max_q=max_q, window=window, sinks=sinks, scale=scale,
                       stream=torch.cuda.current_stream().cuda_stream)
-    counters = (len(lens) * cache.desc.n_kv_heads + 2) * 4
+    counters = (len(lens) * cache.desc.n_kv_heads + 2) * 4      # (and more)
     assert not workspace[:counters].any()
     return out.double().cpu().numpy()
 
@@ -265,6 +265,23 @@ def test_attention_group_sizes(nq, nkv, bits):
 def test_attention_split_along_the_keys(n, q, bits):
     b = make_batch([n], [q], 4, 1, 64, bits, seed=7)
     check_attention(run_attention(*b[:1], *b[2:], max_q=q), *b)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("lens, runs", [([40000], [1]), ([23000, 100, 9000], [3, 1, 1])])
+def test_attention_of_more_results_than_one_workgroup_adds_up(lens, runs, bits):
+    """Contexts that dozens of workgroups share: their results are added up in groups. (The table repeats a few blocks: what is
+    compared is long, the cache is not.)"""
+    nkv, nq, hd, few = 2, 6, 64, 40
+    cache, c, _, _, _, _ = make_batch([few * 16], [1], nq, nkv, hd, bits, seed=17, spare=0)
+    rng = np.random.default_rng(18)
+    width = (max(lens) + 15) // 16
+    tables = rng.integers(0, few, (len(lens), width)).astype(np.int32)
+    cu = np.concatenate(([0], np.cumsum(runs))).astype(np.int32)
+    q = (rng.standard_normal((int(cu[-1]), nq, hd)) / 8).astype(np.float16)
+    got = run_attention(cache, tables, np.int32(lens), cu, q, max(runs))
+    check_attention(got, cache, c, tables, np.int32(lens), cu, q)
+    assert np.array_equal(got, run_attention(cache, tables, np.int32(lens), cu, q, max(runs)))
 
 
 @pytest.mark.parametrize("bits", [16, 4])
