@@ -62,12 +62,13 @@ typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef i32 i32x8_t __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ u32 f16x2_bits(f16x2_t v) { return *(const u32*)&v; }
 __device__ __forceinline__ f16x8_t f16x8_of(u32 a, u32 b, u32 c, u32 d) { const uint4 v = make_uint4(a, b, c, d); return *(const f16x8_t*)&v; }
-// Values that are not finite, where some row of the tile must not see them (0 times one would not be 0): the products take the finite ones
-// (only_finite), and a product of strange_codes with the mask (1 where a row sees a key) tells per row and dimension what else it sees:
-// 1 for every +inf, 64 for every -inf, both for NaN (exact: at most 32 keys a product). Tiles that no mask touches need none of it.
+// Values that are not finite, where some row of the tile must not see them (0 times one would not be 0): the products take the largest finite
+// ones in their place (only_finite; where a row does see them, what is added next swallows those), and a product of strange_codes with the
+// mask (1 where a row sees a key) tells per row and dimension what it sees: 1 for every +inf, 64 for every -inf, both for NaN (exact: at
+// most 32 keys a product). Tiles that no mask touches need none of it.
 __device__ __forceinline__ u32 only_finite(u32 w) {
-  const u32 lo = (w & 0x7C00u) == 0x7C00u ? 0u : w & 0xFFFFu, hi = (w & 0x7C000000u) == 0x7C000000u ? 0u : w & 0xFFFF0000u;
-  return lo | hi;
+  const f16x2_t top = {(_Float16)65504.f, (_Float16)65504.f};
+  return f16x2_bits(__builtin_elementwise_max(__builtin_elementwise_min(*(const f16x2_t*)&w, top), -top));      // (of a number and NaN: the number)
 }
 __device__ __forceinline__ u32 strange_codes(u32 w) {
   auto one = [&](u32 h) { return (h & 0x7C00u) != 0x7C00u ? 0u : (h & 0x3FFu) ? 0x5410u : h >> 15 ? 0x5400u : 0x3C00u; };      // 65, 64, 1
@@ -408,26 +409,25 @@ __device__ __forceinline__ void add_past_caches(const float* slot, ShortAcc<HD, 
       for (int i = 0; i < 4; ++i) acc[c].o[d][i] = acc[c].o[d][i] * mine + __uint_as_float((u32)(v[d][i >> 1] >> (32 * (i & 1)))) * other;
   }
 }
-// what CacheTile::take_strange_out has taken out, given to the rows that see it
-template <int HD, int BITS, int CT>
-__device__ __forceinline__ void give_strange(const CacheTile<HD, BITS>& t, ShortAcc<HD, BITS> (&acc)[CT], const u32 (&vis)[CT]) {
+// What CacheTile::take_strange_out has taken out of a tile, given to the rows that see it (vis: bits of the lane's four keys). Rare, and
+// so one step after the other: there are no registers for it.
+template <int HD, int BITS>
+__device__ __forceinline__ void give_strange(const CacheTile<HD, BITS>& t, floatx4_t (&o)[HD / 16], u32 vis) {
   typedef CacheTile<HD, BITS> Tile;
   constexpr int PER = HD / 16 / Tile::NV;            // tiles of dimensions per operand
+  const float see[4] = {vis & 1u ? 1.f : 0.f, vis & 2u ? 1.f : 0.f, vis & 4u ? 1.f : 0.f, vis & 8u ? 1.f : 0.f};
+  const typename Tile::Probs p = Tile::probs(see);
 #pragma unroll
   for (int v = 0; v < Tile::NV; ++v) {
     typename Tile::Operand x = t.operand(v);
 #pragma unroll
     for (u32& w : x.w) w = strange_codes(w);
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      const float see[4] = {vis[c] & 1u ? 1.f : 0.f, vis[c] & 2u ? 1.f : 0.f, vis[c] & 4u ? 1.f : 0.f, vis[c] & 8u ? 1.f : 0.f};
+    for (int d = v * PER; d < (v + 1) * PER; ++d) {
+      const floatx4_t n = Tile::product(x, p, d, floatx4_t{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-      for (int d = v * PER; d < (v + 1) * PER; ++d) {
-        const floatx4_t n = Tile::product(x, Tile::probs(see), d, floatx4_t{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[c].o[d][i] += strange_sum(n[i]);
-        __builtin_amdgcn_sched_barrier(0);           // (rare: no registers for it)
-      }
+      for (int i = 0; i < 4; ++i) o[d][i] += strange_sum(n[i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 }
@@ -615,7 +615,8 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
           t.load(a, at, min(b, a.n_blocks - 1), cur.g);
           u32 vis[CT];
           see(key, b < a.n_blocks, vis);
-          give_strange<HD, BITS, CT>(t, acc, vis);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) give_strange<HD, BITS>(t, acc[c].o, vis[c]);
         }
         strange = false;
         if (u < u1) {                                // (the tiles on their way are asked for again: none of them stays in registers over this)
@@ -729,7 +730,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 #define PROMPT_SLOT(HD) (PROMPT_ROWS * ((HD) + 2u))      // floats of a part's result: maximum and sum of every row, then its output
 struct PromptShared {
   alignas(256) unsigned char ring[PROMPT_RING];
-  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], next_item;
+  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], next_item, strange;      // strange: some step of the item had values that are not finite
 };
 __device__ __forceinline__ u32 prompt_items(const PagedArgs& a, u32 s) {
   const SeqView v = seq_view(a, s);
@@ -753,6 +754,33 @@ __device__ __forceinline__ PromptItem prompt_item(const PagedArgs& a, const u32*
   return it;
 }
 
+// Values of one block that are not finite, given to the rows that see them (vis: bits of the lane's four keys 4 (lane / 16) ..).
+template <int HD, int BITS, int CT>
+__device__ __forceinline__ void give_strange_block(const PagedArgs& a, u32 id, u32 g, const u32 (&vis)[CT], floatx4_t (&o)[CT][HD / 16]) {
+  const TileLane at = CacheTile<HD, BITS>::lane_offsets();
+  CacheTile<HD, BITS> t;
+  t.load(a, at, id, g);
+  if constexpr (BITS == 16) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) give_strange<HD, 16>(t, o[c], vis[c]);
+  } else {
+    // a scale of 255 makes 32 dimensions of a key's value NaN: which of its scales, and for whom
+    global_byte* const sc = uniform_global((const unsigned char*)a.cache + ((u64)id * a.nkv + g) * (17 * HD)) + opaque((threadIdx.x & 63) >> 4) * 4 + 16 * HD + HD / 2;
+#pragma unroll
+    for (int k = 0; k < HD / 32; ++k) {
+      u32 odd = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd |= (sc[k * 16 + i] == 255 ? 1u : 0u) << i;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const float nan = quad_max(odd & vis[c] ? 1.f : 0.f) > 0.f ? __uint_as_float(0x7FC00000u) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { o[c][2 * k][i] += nan; o[c][2 * k + 1][i] += nan; }
+      }
+    }
+  }
+}
+
 template <int HD, int BITS>
 __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& sh, u32 wg, u32 nwg, bool behind_short) {
   constexpr int CT = PROMPT_CT;
@@ -771,6 +799,10 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
   for (u32 r = 0; r < TPW; ++r) voff[r] = fk ? k_tok * (HD * 2) + r * 64 + lg * 16 : (r * 32 + (lg >> 1) * 16 + lc) * 32 + (lg & 1) * 16;
   const u32 k_at[2] = {(lc >> 3) * BLK + lg * 256 + (lc >> 3) * 128 + (lc & 7) * 16, (lc >> 3) * BLK + lg * 256 + ((lc >> 3) ^ 1u) * 128 + (lc & 7) * 16};
   const u32 v_at = NB * BLK + (lg >> 1) * BLK + (lg & 1) * 256 + lc * 16;
+  // a lane's places in a 4-bit record (values: tokens 8 th ..), and where its four dimensions of 8 values lie in a block of the ring
+  const u32 th = lg & 1, d4 = HD == 128 ? lc * 8 + (lane >> 5) * 4 : lc * 4;
+  const TileLane at4 = {opaque(k_tok * (HD / 2) + lg * 4), opaque((th * 32 + lc) * (HD / 8)), opaque(k_tok), opaque(lc / (HD == 128 ? 4 : 8) * 16 + th * 8)};
+  const u32 to4 = opaque(d4 / 32 * 1024 + (d4 % 32 / 16 * 2 + th) * 256 + d4 % 16 * 16);
   typedef const __attribute__((address_space(4))) u32 const_u32;
   // (behind the short part a workgroup may come late: then its first item comes from the counter too)
   u32 turn = wg;
@@ -782,6 +814,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
   }
   while (turn < total) {
     const u32 item = turn / parts, part = turn - item * parts;
+    if (threadIdx.x == 0) sh.strange = 0;                       // (seen behind the first step's barrier)
     PromptItem it = prompt_item(a, sh.pre, item);
     it.s = (u32)__builtin_amdgcn_readfirstlane(it.s); it.g = (u32)__builtin_amdgcn_readfirstlane(it.g); it.r0 = (u32)__builtin_amdgcn_readfirstlane(it.r0);
     it.rows = (u32)__builtin_amdgcn_readfirstlane(it.rows); it.t0 = (u32)__builtin_amdgcn_readfirstlane(it.t0);
@@ -799,17 +832,13 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
     const bool live = wr < it.rows;
     const i32 wp0 = it.p0 + (i32)((it.r0 % a.G + wr) / a.G), wp1 = it.p0 + (i32)((it.r0 % a.G + min(wr + 16 * CT, it.rows) - 1) / a.G);
     f16x8_t q[CT][HD / 32];
-    i32 qpos[CT];
-    u32 otok[CT], ocol[CT];
-    bool colv[CT];
+    i32 qpos[CT];                                    // position of the lane's row (no row: before every key)
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const u32 r = wr + c * 16 + lc, rr = it.r0 + min(r, it.rows - 1), tok = rr / a.G, h = rr - tok * a.G;
-      colv[c] = r < it.rows;
-      qpos[c] = colv[c] ? it.p0 - (i32)(it.r0 / a.G) + (i32)tok : -1;
-      otok[c] = it.t0 + tok; ocol[c] = (it.g * a.G + h) * HD;
+      qpos[c] = r < it.rows ? it.p0 - (i32)(it.r0 / a.G) + (i32)tok : -1;
 #pragma unroll
-      for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(a.q + (u64)otok[c] * a.qs + ocol[c] + s * 32 + lg * 8);
+      for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(a.q + (u64)(it.t0 + tok) * a.qs + (it.g * a.G + h) * HD + s * 32 + lg * 8);
     }
     floatx4_t o[CT][HD / 16];
     float m[CT], l[CT];
@@ -819,6 +848,9 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) o[c][d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     }
+    auto needed = [&](u32 k0) { return live && (i32)k0 <= wp1 && !(a.window && (i32)k0 + 63 <= wp0 - (i32)a.window && k0 >= a.sinks); };      // by some row of this wave
+    auto item_edge = [&](u32 k0, u32 bad) { return (i32)k0 + 63 > it.p0 || bad || (a.window && (i32)k0 <= it.p1 - (i32)a.window && k0 + 64 > a.sinks); };      // not seen as a whole by every row of the item
+    auto edge_of = [&](u32 k0, u32 bad) { return (i32)k0 + 63 > wp0 || wr + 16 * CT > it.rows || bad || (a.window && (i32)k0 <= wp1 - (i32)a.window && k0 + 64 > a.sinks); };      // nor by every one of this wave
     u32 id[NB], bad_ahead = 0;                       // ids of the stage to fetch next; which blocks of the stages in the ring are outside the cache, 4 bits each
 #pragma unroll
     for (u32 b = 0; b < NB; ++b) id[b] = block_id(s_lo, b);
@@ -837,24 +869,25 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
     // 4 bits: waves 0-3 a block's values each, waves 4-7 its keys
     u32 raw[8], raw_s[4];
     auto fetch4 = [&](u32 s) {
-      const unsigned char* rec = (const unsigned char*)uniform_ptr((const unsigned char*)a.cache + ((u64)my_block() * a.nkv + it.g) * (17 * HD));
-      const u32 th = (lane >> 4) & 1;                // tokens 8 th ..
+      global_byte* const rec = uniform_global((const unsigned char*)a.cache + ((u64)my_block() * a.nkv + it.g) * (17 * HD));
       if (!fk) {
 #pragma unroll
         for (u32 r = 0; r < HD / 32; ++r) {
-          raw[r] = *(const u32*)(rec + k_tok * (HD / 2) + r * 16 + lg * 4);
-          raw_s[r] = rec[16 * HD + r * 16 + k_tok];
+          raw[r] = from_global<u32>(rec + at4.k + r * 16);
+          raw_s[r] = *(rec + at4.ks + 16 * HD + r * 16);
         }
-      } else if constexpr (HD == 128) {
-        const uint4 x = *(const uint4*)(rec + 8 * HD + (th * 32 + lc) * 16), y = *(const uint4*)(rec + 8 * HD + (th * 32 + 16 + lc) * 16);
-        raw[0] = x.x; raw[1] = x.y; raw[2] = x.z; raw[3] = x.w; raw[4] = y.x; raw[5] = y.y; raw[6] = y.z; raw[7] = y.w;
-        const uint2 z = *(const uint2*)(rec + 16 * HD + HD / 2 + (lc >> 2) * 16 + th * 8);
-        raw_s[0] = z.x; raw_s[1] = z.y;
       } else {
-        const uint2 x = *(const uint2*)(rec + 8 * HD + (th * 32 + lc) * 8), y = *(const uint2*)(rec + 8 * HD + (th * 32 + 16 + lc) * 8);
-        raw[0] = x.x; raw[1] = x.y; raw[2] = y.x; raw[3] = y.y;
-        const uint2 z = *(const uint2*)(rec + 16 * HD + HD / 2 + (lc >> 3) * 16 + th * 8);
-        raw_s[0] = z.x; raw_s[1] = z.y;
+        if constexpr (HD == 128) {
+          const u32x4_t x = from_global<u32x4_t>(rec + at4.v + 8 * HD), y = from_global<u32x4_t>(rec + at4.v + 8 * HD + 256);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { raw[i] = x[i]; raw[4 + i] = y[i]; }
+        } else {
+          const u32x2_t x = from_global<u32x2_t>(rec + at4.v + 8 * HD), y = from_global<u32x2_t>(rec + at4.v + 8 * HD + 128);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) { raw[i] = x[i]; raw[2 + i] = y[i]; }
+        }
+        const u32x2_t z = from_global<u32x2_t>(rec + at4.vs + 16 * HD + HD / 2);
+        raw_s[0] = z[0]; raw_s[1] = z[1];
       }
       next_ids(s + 1);
     };
@@ -870,23 +903,22 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
         }
       } else if (HD == 128 || lane < 32) {
         // a lane: 8 tokens x 4 dimensions (of heads of 128 the lower or upper 4 of 8)
-        const u32 th = (lane >> 4) & 1, dq = lane >> 5;
         u32 pr[8][2];                                // [token][pair of dimensions]
 #pragma unroll
         for (u32 i = 0; i < 8; ++i) {
           const float sc = __uint_as_float((raw_s[i / 4] >> (8 * (i % 4)) & 0xFFu) << 23);
-          const u32 x = HD == 128 ? (dq ? raw[i] >> 16 : raw[i]) : (i & 1 ? raw[i / 2] >> 16 : raw[i / 2]);
+          const u32 x = HD == 128 ? (lane >= 32 ? raw[i] >> 16 : raw[i]) : (i & 1 ? raw[i / 2] >> 16 : raw[i / 2]);
           pr[i][0] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 0));
           pr[i][1] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 1));
         }
+        unsigned char* const to = st + (NB + fb) * BLK + to4;
 #pragma unroll
         for (u32 x = 0; x < 4; ++x) {
-          const u32 D = HD == 128 ? lc * 8 + dq * 4 + x : lc * 4 + x;
           const u32 sel = x & 1 ? 0x07060302u : 0x05040100u;
           u32 v[4];
 #pragma unroll
           for (u32 i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(pr[2 * i + 1][x / 2], pr[2 * i][x / 2], sel);
-          *(uint4*)(st + (NB + fb) * BLK + (D / 32) * 1024 + (((D % 32) / 16 * 2 + th) * 16 + D % 16) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+          *(uint4*)(to + x * 16) = make_uint4(v[0], v[1], v[2], v[3]);
         }
       }
     };
@@ -910,33 +942,55 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
       }
       const u32 k0 = tile_of(s) * 64;
-      if (!live || (i32)k0 > wp1 || (a.window && (i32)k0 + 63 <= wp0 - (i32)a.window && k0 >= a.sinks)) continue;
+      if (item_edge(k0, bad)) {
+        // values that are not finite: taken out (0 times one would not be 0), and given to the rows that see them at the end
+        unsigned char* const v = sh.ring + (s % NS) * STAGE + NB * BLK + w * (NB * BLK / 8) + lane * 16;
+#pragma unroll
+        for (u32 r = 0; r < NB * BLK / 8192; ++r) {
+          const uint4 x = *(const uint4*)(v + r * 1024), y = make_uint4(only_finite(x.x), only_finite(x.y), only_finite(x.z), only_finite(x.w));
+          if (__ballot(x.x != y.x || x.y != y.y || x.z != y.z || x.w != y.w)) {
+            *(uint4*)(v + r * 1024) = y;
+            sh.strange = 1;
+          }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+      }
+      if (!needed(k0)) continue;
       const unsigned char* const st0 = sh.ring + (s % NS) * STAGE;
       floatx4_t sc[CT][NB];
+      {
+        // operands a block ahead of the products
+        f16x8_t ka[2][HD / 32];
+        auto ask = [&](u32 b) {
 #pragma unroll
-      for (u32 b = 0; b < NB; ++b) {
-        f16x8_t ka[HD / 32];
+          for (int st = 0; st < HD / 32; ++st) ka[b & 1][st] = as_f16x8(*(const uint4*)(st0 + (b & 2) * BLK + st * 1024 + k_at[b & 1]));
+        };
+        ask(0);
 #pragma unroll
-        for (int st = 0; st < HD / 32; ++st) ka[st] = as_f16x8(*(const uint4*)(st0 + (b & 2) * BLK + st * 1024 + k_at[b & 1]));
+        for (u32 b = 0; b < NB; ++b) {
+          if (b + 1 < NB) ask(b + 1);
 #pragma unroll
-        for (int c = 0; c < CT; ++c) sc[c][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[0], q[c][0], floatx4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          for (int c = 0; c < CT; ++c) sc[c][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[b & 1][0], q[c][0], floatx4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-        for (int st = 1; st < HD / 32; ++st)
+          for (int st = 1; st < HD / 32; ++st)
 #pragma unroll
-          for (int c = 0; c < CT; ++c) sc[c][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[st], q[c][st], sc[c][b], 0, 0, 0);
+            for (int c = 0; c < CT; ++c) sc[c][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[b & 1][st], q[c][st], sc[c][b], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      const bool edge = (i32)k0 + 63 > wp0 || wr + 16 * CT > it.rows || bad || (a.window && (i32)k0 <= wp1 - (i32)a.window && k0 + 64 > a.sinks);
-      u32 vis[CT] = {};                                        // bit 8 h + i: this lane's row sees its key i of the step's pair of blocks h
+      const bool edge = edge_of(k0, bad);
       if (edge) {
+        asm volatile("" ::: "memory");                         // (a branch: few steps are)
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
+          u32 vis = 0;                                         // bit 8 h + i: this lane's row sees its key i of the step's pair of blocks h
 #pragma unroll
           for (u32 h = 0; h < NB / 2; ++h)
-            if (!(bad >> (NB - 1 - (2 * h + (lg >> 1))) & 1u)) vis[c] |= sees(a, qpos[c], (i32)(k0 + h * 32 + lg * 8)) << (8 * h);
+            if (!(bad >> (NB - 1 - (2 * h + (lg >> 1))) & 1u)) vis |= sees(a, qpos[c], (i32)(k0 + h * 32 + lg * 8)) << (8 * h);
 #pragma unroll
           for (u32 b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sc[c][b][i] = vis[c] >> (b * 4 + i) & 1u ? sc[c][b][i] : -INFINITY;
+            for (int i = 0; i < 4; ++i) sc[c][b][i] = vis >> (b * 4 + i) & 1u ? sc[c][b][i] : -INFINITY;
         }
       }
       f16x8_t pb[CT][NB / 2];
@@ -969,66 +1023,70 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
       }
       const unsigned char* const sv = st0 + v_at;
       auto value_bits = [&](int d, u32 h) { return *(const uint4*)(sv + 2 * h * BLK + (d >> 1) * 1024 + (d & 1) * 512); };
-      bool strange = false;                                    // some value of the step is not finite
-      if (edge) {
-        const f16x8_t none = f16x8_of(0, 0, 0, 0);
-        floatx4_t z = floatx4_t{0.f, 0.f, 0.f, 0.f};
+      {
+        // operands two tiles of dimensions ahead of the products, and no further: all at once they take the queries' registers
+        f16x8_t va[2][2][NB / 2];
+        auto ask = [&](int d) {
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d)
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (u32 h = 0; h < NB / 2; ++h) z = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_f16x8(value_bits(d, h)), none, z, 0, 0, 0);
-        strange = any_nan(z);
-      }
-      if (!strange) {
+            for (u32 h = 0; h < NB / 2; ++h) va[d / 2 % 2][x][h] = as_f16x8(value_bits(d + x, h));
+        };
+        ask(0);
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d)
+        for (int d = 0; d < HD / 16; d += 2) {
+          if (d + 2 < HD / 16) ask(d + 2);
 #pragma unroll
-          for (u32 h = 0; h < NB / 2; ++h) {
-            const f16x8_t va = as_f16x8(value_bits(d, h));
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int c = 0; c < CT; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pb[c][h], o[c][d], 0, 0, 0);
-          }
-      } else {
+            for (u32 h = 0; h < NB / 2; ++h)
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d)
-#pragma unroll
-          for (u32 h = 0; h < NB / 2; ++h) {
-            const uint4 x = value_bits(d, h);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-              o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(only_finite(x.x), only_finite(x.y), only_finite(x.z), only_finite(x.w)), pb[c][h], o[c][d], 0, 0, 0);
-              u32 see[4];
-#pragma unroll
-              for (u32 k = 0; k < 4; ++k) see[k] = (vis[c] >> (8 * h + 2 * k) & 1u ? 0x3C00u : 0u) | (vis[c] >> (8 * h + 2 * k + 1) & 1u ? 0x3C000000u : 0u);
-              const floatx4_t n = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(strange_codes(x.x), strange_codes(x.y), strange_codes(x.z), strange_codes(x.w)),
-                                                                         f16x8_of(see[0], see[1], see[2], see[3]), floatx4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[c][d][i] += strange_sum(n[i]);
-              __builtin_amdgcn_sched_barrier(0);     // (rare: no registers for it)
-            }
-          }
+              for (int c = 0; c < CT; ++c) o[c][d + x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d / 2 % 2][x][h], pb[c][h], o[c][d + x], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    if ((u32)__builtin_amdgcn_readfirstlane(sh.strange)) {
+#pragma unroll 1
+      for (u32 s = s_lo; s < s_hi; ++s) {
+        const u32 k0 = tile_of(s) * 64;
+        if (!needed(k0)) continue;
+        u32 bad = 0;
+        for (u32 b = 0; b < NB; ++b) bad = bad << 1 | (block_id(s, b) < a.n_blocks ? 0u : 1u);
+        if (!item_edge(k0, bad)) continue;
+#pragma unroll 1
+        for (u32 b = 0; b < NB; ++b) {
+          if (bad >> (NB - 1 - b) & 1u) continue;
+          u32 vis[CT];
+#pragma unroll
+          for (int c = 0; c < CT; ++c) vis[c] = sees(a, qpos[c], (i32)(k0 + b * 16 + lg * 4)) & 15u;
+          give_strange_block<HD, BITS, CT>(a, block_id(s, b), it.g, vis, o);
+        }
+      }
+      wait_loads();
+    }
     if (threadIdx.x == 0) sh.next_item = (behind_short ? 0u : nwg) + __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // (where a row goes is worked out here: the compiler must not keep it through the loop)
+    const u32 at_end = opaque(lane), lc_end = at_end & 15, lg_end = at_end >> 4;
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const float sum = quad_sum(l[c]);
+      const u32 r = wr + c * 16 + lc_end;
+      if (r >= it.rows) continue;
       if (parts == 1) {
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        if (colv[c]) {
+        const u32 rr = it.r0 + r, tok = rr / a.G, k = (it.g * a.G + rr - tok * a.G) * HD + lg_end * 4;
+        f16_t* const to = out_at(a, it.t0 + tok, k);
+        const u32 step = a.out_tbs ? (u32)(packed_off(0, 32, a.out_tbs) - packed_off(0, 0, a.out_tbs)) : 32u, half = a.out_tbs ? 256u : 16u;      // 32 and 16 dimensions on
 #pragma unroll
-          for (int d = 0; d < HD / 16; ++d) {
-            const u32 k = ocol[c] + d * 16 + lg * 4;
-            f16_t* to = a.out_tbs ? a.out + packed_off(otok[c], k, a.out_tbs) : a.out + (u64)otok[c] * a.os + k;
-            *(uint2*)to = make_uint2(half_pair(o[c][d][0] * inv, o[c][d][1] * inv), half_pair(o[c][d][2] * inv, o[c][d][3] * inv));
-          }
-        }
-      } else if (colv[c]) {
+        for (int d = 0; d < HD / 16; ++d)
+          *(uint2*)(to + (u64)(d / 2) * step + d % 2 * half) = make_uint2(half_pair(o[c][d][0] * inv, o[c][d][1] * inv), half_pair(o[c][d][2] * inv, o[c][d][3] * inv));
+      } else {
         float* const slot = a.prompt_part + (u64)turn * PROMPT_SLOT(HD);
-        const u32 r = wr + c * 16 + lc;
-        if (lg == 0) *(float2*)(slot + 2 * r) = make_float2(m[c], sum);
+        if (lg_end == 0) *(float2*)(slot + 2 * r) = make_float2(m[c], sum);
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(slot + 2 * PROMPT_ROWS + r * HD + d * 16 + lg * 4) = o[c][d];
+        for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(slot + 2 * PROMPT_ROWS + r * HD + d * 16 + lg_end * 4) = o[c][d];
       }
     }
     if constexpr (BITS == 16) wait_dma_barrier<0>();           // no fetch of this item is on its way any more, and next_item is there
