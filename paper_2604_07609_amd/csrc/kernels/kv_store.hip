@@ -4,7 +4,7 @@
 #define STORE_KERNEL(T, HD, BITS)                                                                                 \
   template <> __global__ void __launch_bounds__(BLK_THREADS) k_kv_store<T, HD, BITS>(StoreArgs a) {               \
     __shared__ ValueShared<HD> sh;                                                                                \
-    kv_store<T, HD, BITS, STORE_UNROLL>(a, sh, blockIdx.x);                                                       \
+    kv_store<T, HD, BITS>(a, sh, blockIdx.x);                                                       \
   }
 #define STORE_KERNELS(T) STORE_KERNEL(T, 64, 16) STORE_KERNEL(T, 128, 16) STORE_KERNEL(T, 64, 4) STORE_KERNEL(T, 128, 4)
 STORE_KERNELS(float)

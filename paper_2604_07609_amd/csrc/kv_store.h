@@ -10,8 +10,11 @@
 //             number. The layout is what a lane of the attention reads with one load: 16 bytes of a key (one scale), and
 //             of a value the same 8 dimensions of 4 tokens.
 //
-// Bound by bytes: each projection is read once, each output written once. What is between is 32-bit arithmetic, with one exception: keys that go
-// into 4 bits are normed and rotated in 64 bits, because a sum in another order would move the few values next to a border
+// Bound by bytes: each projection is read once, each output written once. 8191 tokens of 32 query and 8 key heads of 128, 206 MB, take
+// 43 us (4.8 TB/s, what a plain copy of as much reaches), into 4 bits 43 us for 176 MB. It took 67 us with two rows a lane and 8-byte
+// loads, 56 with 17 and not 34 KB of LDS a workgroup, 51 with one row a lane (64 registers: 8 waves a SIMD) and 16-byte loads, 47 with
+// non-temporal loads, and 43 with keys apart from queries. Few tokens are bound by their chain (place and position, table, store) and
+// the launch: 3 us. What is between the bytes is 32-bit arithmetic, with one exception: keys that go into 4 bits are normed and rotated in 64 bits, because a sum in another order would move the few values next to a border
 // between two codes by half their size. (Values are not computed on: their codes are exact either way.)
 #pragma once
 #include "blink_device.h"
@@ -33,7 +36,7 @@ struct StoreArgs {
   float eps, q_scale;
   u32 group;                      // tokens of a wave in the values' part (<= STORE_GROUP)
 };
-#define STORE_GROUP 32u
+#define STORE_GROUP 16u
 
 __device__ __forceinline__ float half_range(float a) {     // saturates at the largest half; NaN stays
   const float r = __builtin_fminf(__builtin_fmaxf(a, -65504.f), 65504.f);
@@ -55,14 +58,12 @@ __device__ __forceinline__ void unpack2(const _Float16*, u32 w, float* o) {
   o[0] = (float)h[0]; o[1] = (float)h[1];
 }
 __device__ __forceinline__ void unpack2(const __bf16*, u32 w, float* o) { o[0] = __uint_as_float(w << 16); o[1] = __uint_as_float(w & 0xFFFF0000u); }
+// (inputs are read once: non-temporal loads leave the caches to what is written)
 template <typename T, int N> __device__ __forceinline__ void load_n(const T* p, float* o) {
-  if constexpr (N == 4) {
-    const uint2 v = *(const uint2*)p;
-    unpack2(p, v.x, o); unpack2(p, v.y, o + 2);
-  } else {
-    const uint4 v = *(const uint4*)p;
-    unpack2(p, v.x, o); unpack2(p, v.y, o + 2); unpack2(p, v.z, o + 4); unpack2(p, v.w, o + 6);
-  }
+  typedef u32 words __attribute__((ext_vector_type(N / 2)));
+  const words v = __builtin_nontemporal_load((const words*)p);
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) unpack2(p, v[i], o + 2 * i);
 }
 
 // scale exponent of a group from the bits of its largest magnitude (fp32): m 2^E -> E - 2, one more from m > 1.75 on, so that the
@@ -92,127 +93,118 @@ template <int HD> __device__ __forceinline__ f16_t* k16(const StoreArgs& a, u32 
 template <int HD> __device__ __forceinline__ f16_t* v16(const StoreArgs& a, u32 blk, u32 h) { return (f16_t*)a.cache + (((u64)a.n_blocks + blk) * a.nkv + h) * (16 * HD); }
 template <int HD> __device__ __forceinline__ unsigned char* rec4(const StoreArgs& a, u32 blk, u32 h) { return (unsigned char*)a.cache + ((u64)blk * a.nkv + h) * (17 * HD); }
 
-// One row (a token's query or key head) by HD/8 lanes, a lane with dimensions 4j .. 4j+3 and hd/2 + 4j .. + 3: the pairs of its rotation.
-template <typename T, int HD, int BITS>
+// One row (a head of a token: of its queries, or KEY of its keys) by HD / (2 N) lanes, a lane with dimensions N j .. N j + N - 1 and
+// those hd/2 further: the pairs of its rotation. A lane has one row and 16-byte loads and stores, except for keys on their way to 4 bits, whose
+// 64-bit arithmetic takes twice the registers (N = 4).
+template <typename T, int HD, int BITS, bool KEY>
 struct StoreRow {
-  float x[8], g[8];
-  float4 cs[2];
-  u32 h;
+  static constexpr int N = KEY && BITS == 4 ? 4 : 8;
+  static constexpr u32 LR = HD / (2 * N);
+  float x[2 * N], cs[2 * N];
+  u32 h, t;
   i32 pos, slot;
   bool live;
-  u32 t;
-  __device__ __forceinline__ void load(const StoreArgs& a, u32 row, u32 rows) {
-    constexpr u32 LR = HD / 8;
-    const u32 j = threadIdx.x % LR, heads = a.nq + a.nkv;
-    live = row < rows;
-    row = min(row, rows - 1);
+  __device__ __forceinline__ void load(const StoreArgs& a, u32 row) {
+    const u32 j = threadIdx.x % LR, heads = KEY ? a.nkv : a.nq;
     t = row / heads; h = row % heads;
+    live = t < a.T;
+    t = min(t, a.T - 1);
     pos = a.pos[t];
-    slot = a.slot[t];
+    slot = KEY ? a.slot[t] : 0;
     live = live && (u32)pos < a.rows;
-    const bool key = h >= a.nq;
-    const T* p = key ? (const T*)a.k + (u64)t * a.ks + (u64)(h - a.nq) * HD : (const T*)a.q + (u64)t * a.qs + (u64)h * HD;
-    load_n<T, 4>(p + 4 * j, x);
-    load_n<T, 4>(p + HD / 2 + 4 * j, x + 4);
-    const float4* c = (const float4*)(a.tab + (u64)((u32)pos < a.rows ? (u32)pos : 0u) * (HD / 2) + 4 * j);
-    cs[0] = c[0]; cs[1] = c[1];
-    const float* gp = key ? a.kg : a.qg;
-    if (gp) {
-      const float4 lo = *(const float4*)(gp + 4 * j), hi = *(const float4*)(gp + HD / 2 + 4 * j);
-      g[0] = lo.x; g[1] = lo.y; g[2] = lo.z; g[3] = lo.w; g[4] = hi.x; g[5] = hi.y; g[6] = hi.z; g[7] = hi.w;
-    }
+    const T* p = KEY ? (const T*)a.k + (u64)t * a.ks + (u64)h * HD : (const T*)a.q + (u64)t * a.qs + (u64)h * HD;
+    load_n<T, N>(p + N * j, x);
+    load_n<T, N>(p + HD / 2 + N * j, x + N);
+    const float* const c = (const float*)(a.tab + (u64)((u32)pos < a.rows ? (u32)pos : 0u) * (HD / 2) + N * j);
+    load_n<float, N>(c, cs);
+    load_n<float, N>(c + N, cs + N);
   }
   template <typename F>
-  __device__ __forceinline__ void turn(const StoreArgs& a, F (&y)[8], const float* gp, F scale) const {
-    constexpr u32 LR = HD / 8;
+  __device__ __forceinline__ void turn(const StoreArgs& a, F (&y)[2 * N], const float* gp, F scale) const {
+    const u32 j = threadIdx.x % LR;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (F)x[i];
+    for (int i = 0; i < 2 * N; ++i) y[i] = (F)x[i];
     if (gp) {
+      float g[2 * N];
+      load_n<float, N>(gp + N * j, g);
+      load_n<float, N>(gp + HD / 2 + N * j, g + N);
       F ss = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss += y[i] * y[i];
+      for (int i = 0; i < 2 * N; ++i) ss += y[i] * y[i];
 #pragma unroll
       for (u32 o = 1; o < LR; o <<= 1) ss += __shfl_xor(ss, (int)o, (int)LR);
       const F ms = ss * (F)(1.0 / HD) + (F)a.eps;
       F r;
       if constexpr (sizeof(F) == 8) r = 1.0 / sqrt(ms); else r = 1.0f / sqrtf(ms);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = y[i] * r * (F)g[i];
+      for (int i = 0; i < 2 * N; ++i) y[i] = y[i] * r * (F)g[i];
     }
-    const float c[4] = {cs[0].x, cs[0].z, cs[1].x, cs[1].z}, s[4] = {cs[0].y, cs[0].w, cs[1].y, cs[1].w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const F p = y[i] * (F)c[i] - y[i + 4] * (F)s[i], q = y[i + 4] * (F)c[i] + y[i] * (F)s[i];
-      y[i] = p * scale; y[i + 4] = q * scale;
+    for (int i = 0; i < N; ++i) {
+      const F p = y[i] * (F)cs[2 * i] - y[i + N] * (F)cs[2 * i + 1], q = y[i + N] * (F)cs[2 * i] + y[i] * (F)cs[2 * i + 1];
+      y[i] = p * scale; y[i + N] = q * scale;
+    }
+  }
+  static __device__ __forceinline__ void put(f16_t* o, const float (&y)[2 * N]) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      u32 w[N / 2];
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) w[i] = half_pair(y[u * N + 2 * i], y[u * N + 2 * i + 1]);
+      if constexpr (N == 8) *(uint4*)(o + u * (HD / 2)) = make_uint4(w[0], w[1], w[2], w[3]);
+      else *(uint2*)(o + u * (HD / 2)) = make_uint2(w[0], w[1]);
     }
   }
   __device__ __forceinline__ void store(const StoreArgs& a) const {
-    constexpr u32 LR = HD / 8;
     const u32 j = threadIdx.x % LR;
     // (a row is spread over neighbouring lanes of one wave, which agree on every condition here)
-    if (h < a.nq) {
-      float y[8];
+    if constexpr (!KEY) {
+      float y[2 * N];
       turn<float>(a, y, a.qg, a.q_scale);
-      if (live) {
-        f16_t* o = a.qo + (u64)t * a.qos + (u64)h * HD + 4 * j;
-        *(uint2*)o = make_uint2(half_pair(y[0], y[1]), half_pair(y[2], y[3]));
-        *(uint2*)(o + HD / 2) = make_uint2(half_pair(y[4], y[5]), half_pair(y[6], y[7]));
-      }
+      if (live) put(a.qo + (u64)t * a.qos + (u64)h * HD + N * j, y);
       return;
     }
     const bool in = live && slot >= 0 && (u32)slot / 16 < a.n_blocks;
     const u32 blk = in ? (u32)slot / 16 : 0u, off = (u32)slot % 16;
     if constexpr (BITS == 16) {
-      float y[8];
+      float y[2 * N];
       turn<float>(a, y, a.kg, 1.0f);
-      if (in) {
-        f16_t* o = k16<HD>(a, blk, h - a.nq) + off * HD + 4 * j;
-        *(uint2*)o = make_uint2(half_pair(y[0], y[1]), half_pair(y[2], y[3]));
-        *(uint2*)(o + HD / 2) = make_uint2(half_pair(y[4], y[5]), half_pair(y[6], y[7]));
-      }
+      if (in) put(k16<HD>(a, blk, h) + off * HD + N * j, y);
     } else {
-      double y[8];
+      double y[2 * N];
       turn<double>(a, y, a.kg, 1.0);
-      u64 top[2] = {0, 0};                       // eight lanes hold the 32 dimensions of a group, each half of the row by itself
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top[i / 4] = max(top[i / 4], (u64)__double_as_longlong(y[i]) & 0x7FFFFFFFFFFFFFFFull);
-#pragma unroll
-      for (u32 o = 1; o < 8; o <<= 1) {
-        top[0] = max(top[0], (u64)__shfl_xor((unsigned long long)top[0], (int)o, 8));
-        top[1] = max(top[1], (u64)__shfl_xor((unsigned long long)top[1], (int)o, 8));
-      }
-      unsigned char* rec = rec4<HD>(a, blk, h - a.nq);
+      unsigned char* rec = rec4<HD>(a, blk, h);
+      constexpr u32 LG = 32 / N;                 // lanes that hold the 32 dimensions of a group, each half of the row by itself
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const bool fine = (top[u] >> 52) != 0x7FFull;
-        const i32 e = scale_exponent(top[u]);
+        u64 top = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) top = max(top, (u64)__double_as_longlong(y[u * N + i]) & 0x7FFFFFFFFFFFFFFFull);
+#pragma unroll
+        for (u32 o = 1; o < LG; o <<= 1) top = max(top, (u64)__shfl_xor((unsigned long long)top, (int)o, (int)LG));
+        const bool fine = (top >> 52) != 0x7FFull;
+        const i32 e = scale_exponent(top);
         const float sc = __uint_as_float((u32)(e + 127) << 23);
-        u32 c = codes2<0>(0u, odd_float(y[4 * u]), odd_float(y[4 * u + 1]), sc);
-        c = codes2<1>(c, odd_float(y[4 * u + 2]), odd_float(y[4 * u + 3]), sc);
+        u32 c = codes2<0>(0u, odd_float(y[u * N]), odd_float(y[u * N + 1]), sc);
+        c = codes2<1>(c, odd_float(y[u * N + 2]), odd_float(y[u * N + 3]), sc);
+        if constexpr (N == 8) {
+          c = codes2<2>(c, odd_float(y[u * N + 4]), odd_float(y[u * N + 5]), sc);
+          c = codes2<3>(c, odd_float(y[u * N + 6]), odd_float(y[u * N + 7]), sc);
+        }
         if (in) {
-          *(uint16_t*)(rec + off * (HD / 2) + u * (HD / 4) + 2 * j) = fine ? (uint16_t)c : (uint16_t)0;
-          if (j % 8 == 0) rec[16 * HD + (u * (HD / 64) + j / 8) * 16 + off] = fine ? (unsigned char)(e + 127) : (unsigned char)255;
+          unsigned char* o = rec + off * (HD / 2) + u * (HD / 4) + N / 2 * j;
+          if constexpr (N == 8) *(u32*)o = fine ? c : 0u;
+          else *(uint16_t*)o = fine ? (uint16_t)c : (uint16_t)0;
+          if (j % LG == 0) rec[16 * HD + (u * (HD / 64) + j / LG) * 16 + off] = fine ? (unsigned char)(e + 127) : (unsigned char)255;
         }
       }
     }
   }
 };
 
-// The rows' part: U rows of a lane group at a time, all loads first.
-template <typename T, int HD, int BITS, int U>
-__device__ __forceinline__ void store_rows(const StoreArgs& a, u32 wg) {
-  constexpr u32 LR = HD / 8, RPW = 256 / LR;
-  const u32 rows = a.T * (a.nq + a.nkv), r0 = wg * (RPW * U) + threadIdx.x / LR;
-  StoreRow<T, HD, BITS> r[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) r[u].load(a, r0 + u * RPW, rows);
-#pragma unroll
-  for (int u = 0; u < U; ++u) r[u].store(a);
-}
-
-// Values into halves: they lie with the tokens next to each other, so a wave takes up to 32 tokens of a head through LDS and writes
+// Values into halves: they lie with the tokens next to each other, so a wave takes up to 16 tokens of a head through LDS and writes
 // what fills an aligned run of four places of a block as 8 bytes (four of them are a row of the block, 16 rows a store), the rest
-// as single halves. Written 2 bytes at a time whatever the places, a prefill's store took as long as all the other stores together.
+// as single halves.
 template <int HD>
 struct ValueShared { f16_t v[4][STORE_GROUP][HD + 2]; i32 slot[4][STORE_GROUP + 4]; };
 template <typename T, int HD>
@@ -222,6 +214,7 @@ __device__ __forceinline__ void store_values16(const StoreArgs& a, ValueShared<H
   const bool live = item < groups * a.nkv;
   const u32 h = live ? item % a.nkv : 0u, t0 = live ? item / a.nkv * group : 0u, n = live ? min(group, a.T - t0) : 0u;
   constexpr u32 LR = HD / 8, RP = 64 / LR;       // lanes of a row, rows of a load
+  constexpr u32 RUNS = STORE_GROUP / 4;
   i32 sl = -1;
   if (lane < n) {
     sl = a.slot[t0 + lane];
@@ -241,11 +234,11 @@ __device__ __forceinline__ void store_values16(const StoreArgs& a, ValueShared<H
   const bool first = sl >= 0 && (sl & 3) == 0 && s1 == sl + 1 && s2 == sl + 2 && s3 == sl + 3;
   const u64 runs = __ballot(first), taken = runs | runs << 1 | runs << 2 | runs << 3, single = __ballot(sl >= 0) & ~taken;
   u64 m8 = runs;
-  for (u32 k = lane % 8; k; --k) m8 &= m8 - 1;   // this lane's run: number lane % 8
+  for (u32 k = lane % RUNS; k; --k) m8 &= m8 - 1; // this lane's run: number lane % RUNS
   if (m8) {
     const u32 t = (u32)__builtin_ctzll(m8), s = (u32)sh.slot[w][t];
     f16_t* o = v16<HD>(a, s / 16, h) + s % 16;
-    for (u32 d = lane / 8; d < HD; d += 8) {
+    for (u32 d = lane / RUNS; d < HD; d += 64 / RUNS) {
       const u32 lo = (u32)sh.v[w][t][d] | (u32)sh.v[w][t + 1][d] << 16, hi = (u32)sh.v[w][t + 2][d] | (u32)sh.v[w][t + 3][d] << 16;
       *(uint2*)(o + d * 16) = make_uint2(lo, hi);
     }
@@ -261,10 +254,9 @@ __device__ __forceinline__ void store_values16(const StoreArgs& a, ValueShared<H
 template <typename T, int HD>
 __device__ __forceinline__ void store_values4(const StoreArgs& a, u32 wg) {
   constexpr u32 LR = HD / 8, RPW = 256 / LR;
-  const u32 rows = a.T * a.nkv, row0 = wg * RPW + threadIdx.x / LR, row = min(row0, rows - 1), j = threadIdx.x % LR;
-  const u32 t = row / a.nkv, h = row % a.nkv;
+  const u32 row = wg * RPW + threadIdx.x / LR, t0 = row / a.nkv, h = row % a.nkv, t = min(t0, a.T - 1), j = threadIdx.x % LR;
   const i32 slot = a.slot[t];
-  const bool in = row0 < rows && slot >= 0 && (u32)slot / 16 < a.n_blocks && (u32)a.pos[t] < a.rows;
+  const bool in = t0 < a.T && slot >= 0 && (u32)slot / 16 < a.n_blocks && (u32)a.pos[t] < a.rows;
   float x[8];
   load_n<T, 8>((const T*)a.v + (u64)t * a.vs + (u64)h * HD + 8 * j, x);
   u32 top = 0;
@@ -302,18 +294,30 @@ __host__ __device__ __forceinline__ u32 store_group(u32 T, u32 nkv, u32 n_cu) {
 __host__ __device__ __forceinline__ u32 store_value_wgs(u32 T, u32 nkv, u32 hd, u32 bits, u32 group) {
   return bits == 16 ? ((T + group - 1) / group * nkv + 3) / 4 : (T * nkv + 2048 / hd - 1) / (2048 / hd);
 }
-__host__ __device__ __forceinline__ u32 store_row_wgs(u32 T, u32 heads, u32 hd, u32 unroll) {
-  const u32 per = 2048 / hd * unroll;
-  return (T * heads + per - 1) / per;
+__host__ __device__ __forceinline__ u32 store_key_wgs(u32 T, u32 nkv, u32 hd, u32 bits) {
+  const u32 per = (bits == 16 ? 4096 : 2048) / hd;
+  return (T * nkv + per - 1) / per;
+}
+__host__ __device__ __forceinline__ u32 store_query_wgs(u32 T, u32 nq, u32 hd) { return (T * nq + 4096 / hd - 1) / (4096 / hd); }
+__host__ __device__ __forceinline__ u32 store_wgs(u32 T, u32 nq, u32 nkv, u32 hd, u32 bits, u32 group) {
+  return store_value_wgs(T, nkv, hd, bits, group) + store_key_wgs(T, nkv, hd, bits) + store_query_wgs(T, nq, hd);
 }
 
-template <typename T, int HD, int BITS, int U>
+template <typename T, int HD, int BITS>
 __device__ __forceinline__ void kv_store(const StoreArgs& a, ValueShared<HD>& sh, u32 wg) {
-  const u32 nv = store_value_wgs(a.T, a.nkv, HD, BITS, a.group);
+  const u32 nv = store_value_wgs(a.T, a.nkv, HD, BITS, a.group), nk = store_key_wgs(a.T, a.nkv, HD, BITS);
   if (wg < nv) {
     if constexpr (BITS == 16) store_values16<T, HD>(a, sh, wg);
     else store_values4<T, HD>(a, wg);
-  } else store_rows<T, HD, BITS, U>(a, wg - nv);
+  } else if (wg < nv + nk) {
+    StoreRow<T, HD, BITS, true> r;
+    r.load(a, ((wg - nv) * 256 + threadIdx.x) / r.LR);
+    r.store(a);
+  } else {
+    StoreRow<T, HD, BITS, false> r;
+    r.load(a, ((wg - nv - nk) * 256 + threadIdx.x) / r.LR);
+    r.store(a);
+  }
 }
 
 // ---- tokens read back as halves ---------------------------------------------------------------------------------------------

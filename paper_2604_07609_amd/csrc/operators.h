@@ -88,7 +88,7 @@ extern "C" int blink_qk_norm_rope(int32_t device, const blink_qk_norm_rope_args*
   s.qg = a->q_gain; s.kg = a->k_gain; s.pos = a->positions; s.slot = a->slots; s.tab = (const float2*)a->rope_table; s.rows = a->rope_rows;
   s.qo = (f16_t*)a->q_out; s.qos = a->q_out_stride; s.cache = a->cache.data; s.n_blocks = a->cache.n_blocks; s.nq = a->n_q_heads; s.nkv = nkv; s.T = a->n_tokens;
   s.eps = a->eps; s.q_scale = a->q_scale; s.group = store_group(s.T, nkv, n_cu);
-  const u32 grid = store_value_wgs(s.T, nkv, hd, a->cache.bits, s.group) + store_row_wgs(s.T, s.nq + nkv, hd, STORE_UNROLL);
+  const u32 grid = store_wgs(s.T, s.nq, nkv, hd, a->cache.bits, s.group);
   const hipStream_t st = (hipStream_t)stream;
   HIPCHK(a->in_type == BLINK_TYPE_FLOAT ? launch_store<float>(s, hd, a->cache.bits, grid, st)
          : a->in_type == BLINK_TYPE_HALF ? launch_store<_Float16>(s, hd, a->cache.bits, grid, st) : launch_store<__bf16>(s, hd, a->cache.bits, grid, st));

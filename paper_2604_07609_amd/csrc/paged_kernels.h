@@ -3,7 +3,6 @@
 #pragma once
 #include "paged_attention.h"
 
-#define STORE_UNROLL 2                                 // rows of a lane group on their way at a time
 // Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold), and tiles of keys on their way
 #define SHORT_MORE(HD) ((HD) == 64 ? 4 : 2)
 #define SHORT_AHEAD(HD, BITS, CT) ((CT) > 1 ? 2 : (HD) == 128 || (BITS) == 4 ? 3 : 4)

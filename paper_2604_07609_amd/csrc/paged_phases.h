@@ -15,8 +15,8 @@ __device__ __forceinline__ void store_phase(const DevCtx& c, u32 layer, ValueSha
   a.qg = L->gq; a.kg = L->gk; a.pos = c.positions; a.slot = c.slot_mapping; a.tab = c.rope_tab; a.rows = c.max_seq_len;
   a.qo = c.qbuf; a.qos = (u64)c.nq * HD; a.cache = (char*)c.kv + layer * c.kv_layer_bytes; a.n_blocks = c.n_blocks; a.nq = c.nq; a.nkv = c.nkv; a.T = m->n_tokens;
   a.eps = c.eps; a.q_scale = 1.0f / sqrtf((float)HD); a.group = store_group(a.T, c.nkv, c.n_cu);
-  const u32 total = store_value_wgs(a.T, a.nkv, HD, BITS, a.group) + store_row_wgs(a.T, a.nq + a.nkv, HD, STORE_UNROLL);
-  for (u32 x = wg; x < total; x += nwg) kv_store<float, HD, BITS, STORE_UNROLL>(a, sh, x);      // (a wave's part of the LDS is its own)
+  const u32 total = store_wgs(a.T, a.nq, a.nkv, HD, BITS, a.group);
+  for (u32 x = wg; x < total; x += nwg) kv_store<float, HD, BITS>(a, sh, x);      // (a wave's part of the LDS is its own)
 }
 template <int HD, int BITS, int CT>
 __device__ __forceinline__ void attention_phase(const DevCtx& c, u32 layer, PagedShared<HD, CT>& sh, u32 wg, u32 nwg) {
