@@ -389,26 +389,74 @@ __device__ __forceinline__ void leave_past_caches(float* slot, const ShortAcc<HD
     }
   }
 }
-template <int HD, int BITS, int CT>
-__device__ __forceinline__ void add_past_caches(const float* slot, ShortAcc<HD, BITS> (&acc)[CT], u32 rows) {
-  const u32 lane = threadIdx.x & 63;
+// Results of other workgroups added up by a whole workgroup: a wave has T of the tiles of dimensions, of all results, and asks for those of
+// eight results at a time (a wave with all dimensions of every NWth result, one after the other, took three times as long)
+template <int HD, int BITS, int CT, int NW>
+struct ShortMerge {
+  static constexpr int TILES = CT * (HD / 16), T = TILES > NW ? TILES / NW : 1, AT_ONCE = 8;
+  u32 c, d0;                                         // row tile, first tile of dimensions
+  bool live;                                         // the lane has a row, the wave tiles
+  floatx4_t o[T];
+  float m, l;
+  template <typename F>
+  __device__ __forceinline__ void sum(u32 x0, u32 x1, u32 rows, F result) {      // results x0 .. x1
+    const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    c = w * T / (HD / 16); d0 = w * T % (HD / 16);
+    live = w * T < (u32)TILES && c * 16 + (lane & 15) < rows;
+    m = -INFINITY; l = 0.f;
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    if (c * 16 + (lane & 15) >= rows) continue;
-    const float* const p = slot + c * (128 + HD * 16);
-    u64 v[HD / 16][2];
+    for (int t = 0; t < T; ++t) o[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    if (!live) return;
+#pragma unroll 1
+    for (u32 x = x0; x < x1; x += AT_ONCE) {
+      float ms[AT_ONCE], ls[AT_ONCE];
+      u64 v[AT_ONCE][T][2];
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d)
+      for (int b = 0; b < AT_ONCE; ++b) {
+        ms[b] = -INFINITY; ls[b] = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) v[d][h] = __hip_atomic_load((const u64*)(p + 128 + (d * 64 + lane) * 4) + h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    float mine, other;
-    acc[c].join(ld_past_caches(p + lane), ld_past_caches(p + 64 + lane), mine, other);
+        for (int t = 0; t < T; ++t) v[b][t][0] = v[b][t][1] = 0;
+        if (x + b < x1) {
+          const float* const p = result(x + b) + c * (128 + HD * 16);
+          ms[b] = ld_past_caches(p + lane); ls[b] = ld_past_caches(p + 64 + lane);
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d)
+          for (int t = 0; t < T; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[c].o[d][i] = acc[c].o[d][i] * mine + __uint_as_float((u32)(v[d][i >> 1] >> (32 * (i & 1)))) * other;
+            for (int h = 0; h < 2; ++h) v[b][t][h] = __hip_atomic_load((const u64*)(p + 128 + ((d0 + t) * 64 + lane) * 4) + h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+      }
+      float mn = m;
+#pragma unroll
+      for (int b = 0; b < AT_ONCE; ++b) mn = fmaxf(mn, ms[b]);
+      const float ref = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m - ref);
+      l *= f;
+#pragma unroll
+      for (int t = 0; t < T; ++t) o[t] *= f;
+#pragma unroll
+      for (int b = 0; b < AT_ONCE; ++b) {
+        const float g = __builtin_amdgcn_exp2f(ms[b] - ref);
+        l += ls[b] * g;
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[t][i] += __uint_as_float((u32)(v[b][t][i >> 1] >> (32 * (i & 1)))) * g;
+      }
+      m = mn;
+    }
   }
-}
+  __device__ __forceinline__ void leave(float* result) const {
+    const u32 lane = threadIdx.x & 63;
+    if (!live) return;
+    float* const p = result + c * (128 + HD * 16);
+    if (d0 == 0) { st_past_caches(p + lane, m); st_past_caches(p + 64 + lane, l); }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        __hip_atomic_store((u64*)(p + 128 + ((d0 + t) * 64 + lane) * 4) + h, ((u64)__float_as_uint(o[t][2 * h + 1]) << 32) | __float_as_uint(o[t][2 * h]), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+  }
+};
 // What CacheTile::take_strange_out has taken out of a tile, given to the rows that see it (vis: bits of the lane's four keys). Rare, and
 // so one step after the other: there are no registers for it.
 template <int HD, int BITS>
@@ -687,31 +735,35 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     if (!scalar(sh.last[which])) continue;
     const Pair p = pair_at(whole ? wg : which ? wg1 - 1 : wg0);
     const u32 f = first_wg(p), np = n_wgs(p), rows = p.n * a.G;
-    const bool grouped = np > SHORT_GROUP;
-    // of one level: results x0 .. x1, the waves a run of them each, then wave 0 the waves'
-    u32 x0 = grouped ? max(f, group0) : f, x1 = grouped ? min(f + np, group0 + SHORT_GROUP) : f + np;
-#pragma unroll 1
-    for (u32 level = grouped ? 0u : 1u;; ++level) {
-      const u32 per = (x1 - x0 + NW - 1) / NW, mine = min(x1, x0 + w * per), end = min(x1, mine + per);
-      clear();
-#pragma unroll 1
-      for (u32 x = mine; x < end; ++x) add_past_caches<HD, BITS, CT>(level && grouped ? group_piece(x, f) : piece(x, f), acc, rows);
-      leave_in_lds<HD, BITS, CT, NW>(sh, w, acc);
+    ShortMerge<HD, BITS, CT, NW> all;
+    if (np > SHORT_GROUP) {                          // this workgroup's group, then, if it is the last of them, the groups
+      all.sum(max(f, group0), min(f + np, group0 + SHORT_GROUP), rows, [&](u32 x) { return piece(x, f); });
+      all.leave(group_piece(group, f));
+      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
       __syncthreads();
       if (w == 0) {
-        clear();
-#pragma unroll 1
-        for (u32 x = 0; x < NW; ++x) add_from_lds<HD, BITS, CT, NW>(sh, x, acc);
-        if (level) finish(p);
-        else {
-          leave_past_caches<HD, BITS, CT>(a.part + (u64)(2 * (nwg + group) + (f >= group0 ? 1u : 0u)) * short_slot<HD, CT>(), acc, rows);
-          const bool last = count(a.ctr + (u64)p.s * a.nkv + p.g, (f + np - 1) / SHORT_GROUP - f / SHORT_GROUP + 1);
-          if (lane == 0) sh.last[which] = last;
-        }
+        const bool last = count(a.ctr + (u64)p.s * a.nkv + p.g, (f + np - 1) / SHORT_GROUP - f / SHORT_GROUP + 1);
+        if (lane == 0) sh.last[which] = last;
       }
       __syncthreads();
-      if (level || !scalar(sh.last[which])) break;
-      x0 = f / SHORT_GROUP; x1 = (f + np - 1) / SHORT_GROUP + 1;
+      if (!scalar(sh.last[which])) continue;
+      all.sum(f / SHORT_GROUP, (f + np - 1) / SHORT_GROUP + 1, rows, [&](u32 x) { return group_piece(x, f); });
+    } else all.sum(f, f + np, rows, [&](u32 x) { return piece(x, f); });
+    const float l = quad_sum(all.l), inv = l == 0.f ? 0.f : 1.0f / l;
+    const u32 r = all.c * 16 + lc, tok = r / a.G, k = (p.g * a.G + r - tok * a.G) * HD;
+    if (!all.live) continue;
+    if constexpr (BITS == 16) {
+#pragma unroll
+      for (int t = 0; t < all.T; ++t)
+        *(uint2*)out_at(a, p.t0 + tok, k + (all.d0 + t) * 16 + lg * 4) =
+            make_uint2(half_pair(all.o[t][0] * inv, all.o[t][1] * inv), half_pair(all.o[t][2] * inv, all.o[t][3] * inv));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f16_t* const x = out_at(a, p.t0 + tok, k + Tile::o_dim((int)all.d0, lg, i));
+        const u32 pair = half_pair(all.o[0][i] * inv, all.o[all.T - 1][i] * inv);
+        if constexpr (all.T == 2) *(u32*)x = pair; else *x = (f16_t)pair;
+      }
     }
   }
 }
