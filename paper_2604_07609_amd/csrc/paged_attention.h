@@ -267,9 +267,12 @@ struct CacheTile<HD, 4> {
 #define PAGED_MAX_SEQS 1024u       // sequences whose views a workgroup keeps in LDS
 template <int HD, int CT, int NW>
 struct ShortShared {
-  floatx4_t o[NW][CT][HD / 16][64];                  // a result that one wave leaves for another, as its registers hold it
-  float m[NW][CT][16], l[NW][CT][16];
-  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[NW], last[2];
+  // a result that one wave leaves for others, as its registers hold it: of the pair that its run begins inside of; at NW, of the pair
+  // that goes on in other workgroups, by the wave that it begins in
+  floatx4_t o[NW + 1][CT][HD / 16][64];
+  float m[NW + 1][CT][16], l[NW + 1][CT][16];
+  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[NW], last[2], need[2];      // need: results of the pair, last: this is the last one
+  u32* ctr[2];
   i32 pos0[PAGED_MAX_SEQS];
   unsigned char n[PAGED_MAX_SEQS];                   // (a short sequence has at most 64 rows)
 };
@@ -294,13 +297,14 @@ __device__ __forceinline__ void prefix_sums(u32* pre, u32* wave_sum, u32 n, F f)
   if (threadIdx.x == 0) pre[0] = 0;
   __syncthreads();
 }
-__device__ __forceinline__ u32 last_at_most(const u32* pre, u32 n, u32 x) {     // last s < n with pre[s] <= x
-  u32 lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const u32 mid = (lo + hi) / 2;
-    if (pre[mid] <= x) lo = mid; else hi = mid;
-  }
-  return lo;
+// last s < n (at most PAGED_MAX_SEQS) with pre[s] <= x, x the same in the whole wave, whose lanes look at 64 places at a time (two
+// readings of LDS one after the other, and not ten)
+__device__ __forceinline__ u32 last_at_most(const u32* pre, u32 n, u32 x) {
+  if (n == 1) return 0;
+  const u32 lane = threadIdx.x & 63, step = (n + 63) / 64;
+  auto below = [&](u32 i, u32 end) { return (u32)__popcll(__ballot(i < end && pre[i < end ? i : 0u] <= x)); };
+  const u32 lo = (below(lane * step, n) - 1) * step;
+  return lo + below(lo + lane, min(lo + step, n)) - 1;
 }
 
 // running maximum, sum and output of one tile of 16 rows, and one tile of keys and values added to them
@@ -372,25 +376,28 @@ __device__ __forceinline__ void add_from_lds(const ShortShared<HD, CT, NW>& sh, 
 }
 // a result in global memory, for another workgroup (see merge_chunks for why past the caches): maxima, sums, outputs as registers hold them
 template <int HD, int CT> __device__ __forceinline__ constexpr u32 short_slot() { return CT * (128 + HD * 16); }     // floats
-template <int HD, int BITS, int CT>
-__device__ __forceinline__ void leave_past_caches(float* slot, const ShortAcc<HD, BITS> (&acc)[CT], u32 rows) {
-  const u32 lane = threadIdx.x & 63;
-#pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    if (c * 16 + (lane & 15) >= rows) continue;
-    float* const p = slot + c * (128 + HD * 16);
-    st_past_caches(p + lane, acc[c].m); st_past_caches(p + 64 + lane, acc[c].l);
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) {
-      u64* const q = (u64*)(p + 128 + (d * 64 + lane) * 4);
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        __hip_atomic_store(q + h, ((u64)__float_as_uint(acc[c].o[d][2 * h + 1]) << 32) | __float_as_uint(acc[c].o[d][2 * h]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+// A result in LDS or in the workspace: the lane's maximum and sum of a row tile, its tile d of dimensions
+template <int HD, int CT, int NW>
+struct LdsResult {
+  const ShortShared<HD, CT, NW>& sh;
+  u32 at;
+  __device__ __forceinline__ float m(u32 c, u32 lane) const { return sh.m[at][c][lane & 15]; }
+  __device__ __forceinline__ float l(u32 c, u32 lane) const { return lane < 16 ? sh.l[at][c][lane] : 0.f; }       // (the row's four lanes' added up)
+  __device__ __forceinline__ floatx4_t o(u32 c, u32 d, u32 lane) const { return sh.o[at][c][d][lane]; }
+};
+template <int HD>
+struct FarResult {
+  const float* p;
+  __device__ __forceinline__ float m(u32 c, u32 lane) const { return ld_past_caches(p + c * (128 + HD * 16) + lane); }
+  __device__ __forceinline__ float l(u32 c, u32 lane) const { return ld_past_caches(p + c * (128 + HD * 16) + 64 + lane); }
+  __device__ __forceinline__ floatx4_t o(u32 c, u32 d, u32 lane) const {
+    const u64* const q = (const u64*)(p + c * (128 + HD * 16) + 128 + (d * 64 + lane) * 4);
+    const u64 x = __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), y = __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return floatx4_t{__uint_as_float((u32)x), __uint_as_float((u32)(x >> 32)), __uint_as_float((u32)y), __uint_as_float((u32)(y >> 32))};
   }
-}
-// Results of other workgroups added up by a whole workgroup: a wave has T of the tiles of dimensions, of all results, and asks for those of
-// eight results at a time (a wave with all dimensions of every NWth result, one after the other, took three times as long)
+};
+// Results added up by a whole workgroup: a wave has T of the tiles of dimensions, of all results, and asks for those of eight results at a
+// time. (A wave with all dimensions of every NWth result, one after the other, took three times as long.)
 template <int HD, int BITS, int CT, int NW>
 struct ShortMerge {
   static constexpr int TILES = CT * (HD / 16), T = TILES > NW ? TILES / NW : 1, AT_ONCE = 8;
@@ -410,19 +417,17 @@ struct ShortMerge {
 #pragma unroll 1
     for (u32 x = x0; x < x1; x += AT_ONCE) {
       float ms[AT_ONCE], ls[AT_ONCE];
-      u64 v[AT_ONCE][T][2];
+      floatx4_t v[AT_ONCE][T];
 #pragma unroll
       for (int b = 0; b < AT_ONCE; ++b) {
         ms[b] = -INFINITY; ls[b] = 0.f;
 #pragma unroll
-        for (int t = 0; t < T; ++t) v[b][t][0] = v[b][t][1] = 0;
+        for (int t = 0; t < T; ++t) v[b][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
         if (x + b < x1) {
-          const float* const p = result(x + b) + c * (128 + HD * 16);
-          ms[b] = ld_past_caches(p + lane); ls[b] = ld_past_caches(p + 64 + lane);
+          const auto r = result(x + b);
+          ms[b] = r.m(c, lane); ls[b] = r.l(c, lane);
 #pragma unroll
-          for (int t = 0; t < T; ++t)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) v[b][t][h] = __hip_atomic_load((const u64*)(p + 128 + ((d0 + t) * 64 + lane) * 4) + h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          for (int t = 0; t < T; ++t) v[b][t] = r.o(c, d0 + t, lane);
         }
       }
       float mn = m;
@@ -437,13 +442,12 @@ struct ShortMerge {
         const float g = __builtin_amdgcn_exp2f(ms[b] - ref);
         l += ls[b] * g;
 #pragma unroll
-        for (int t = 0; t < T; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[t][i] += __uint_as_float((u32)(v[b][t][i >> 1] >> (32 * (i & 1)))) * g;
+        for (int t = 0; t < T; ++t) o[t] += v[b][t] * g;
       }
       m = mn;
     }
   }
+  // into the workspace (see merge_chunks for why past the caches)
   __device__ __forceinline__ void leave(float* result) const {
     const u32 lane = threadIdx.x & 63;
     if (!live) return;
@@ -490,8 +494,8 @@ __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { r
 // All tiles of all (sequence, kv head) pairs are one line of units, cut into equal runs, one per wave: whatever the lengths, every
 // wave reads the same number of bytes, with NT tiles on their way, and waits for nobody until its run ends.
 // A pair inside a run is finished where it is. One that several waves of a workgroup share is added up by the wave it begins in (in
-// LDS, after the one barrier); one that several workgroups share leaves a result of each in the workspace, and the workgroup that comes
-// last adds them up, its waves a part of them each. Of more than SHORT_GROUP such results, those of every SHORT_GROUP workgroups are added up
+// LDS, after the one barrier); of one that several workgroups share, each adds up its waves' results and leaves one in the workspace, and
+// the workgroup that comes last adds those up, its waves a part of the dimensions each. Of more than SHORT_GROUP such results, those of every SHORT_GROUP workgroups are added up
 // by the last of these first (65531 keys of one sequence, 4-bit, 171 results a pair: 53 us in one go). All sums in the order of the
 // runs: results do not depend on who comes when.
 // Few short pairs (half as many as workgroups, eight tiles a wave) are dealt out whole instead, a workgroup or several to each: up to that
@@ -522,7 +526,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   if (!whole) prefix_sums<NW>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return units(s) * a.nkv; });
   const u32 U = scalar(sh.pre[a.n_seqs]), wg_units = max(SHORT_QUANTUM, (U + nwg * NW - 1) / (nwg * NW)) * NW;
   if (whole ? wg >= U : wg * wg_units >= U) return;
-  if (threadIdx.x < 2) sh.last[threadIdx.x] = 0;
+  if (threadIdx.x < 2) sh.last[threadIdx.x] = sh.need[threadIdx.x] = 0;
   typedef const __attribute__((address_space(4))) u32 const_u32;
   // a pair of a sequence and a kv head: its first unit and number of tiles, its rows, and which tiles those are
   struct Pair { u32 s, g, first, nv, t0, n, row, zb, wlo; i32 pos0; };
@@ -553,7 +557,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   if (whole) {
     const u32 per = (cur.nv + CAP - 1) / CAP;
     from = scalar(sh.pre[cur.s]) + cur.g * per;
-    wg0 = (wg - from) * CAP; wg1 = min(wg0 + CAP, cur.nv);
+    wg0 = cur.nv * (wg - from) / per; wg1 = cur.nv * (wg - from + 1) / per;
   }
   const u32 quantum = (wg1 - wg0 + NW - 1) / NW, u0 = min(wg0 + w * quantum, wg1), u1 = min(u0 + quantum, wg1);
   auto first_wg = [&](const Pair& p) { return whole ? from : p.first / wg_units; };
@@ -687,71 +691,21 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
       wait_loads();      // (the compiler does not know any more which slot's loads are the oldest: it would wait for all of them at every turn)
     }
   }
+  // The rest is a workgroup's end, once per launch.
+  const bool goes_on = u0 < u1 && cur.first >= u0 && u1 < cur.first + cur.nv;
+  if (goes_on && (whole || cur.first + cur.nv > wg1)) leave_in_lds<HD, BITS, CT, NW>(sh, NW, acc);
   __syncthreads();
-  // The rest is a workgroup's end, once per launch. This wave's pair that goes on behind its run, if it began there; wave 0 also the
-  // pair that the workgroup's run begins inside of.
-  auto others = [&](const Pair& p, u32 x) {          // what the waves from x on have of the pair
-#pragma unroll 1
-    for (; x < NW && wg0 + x * quantum < min(p.first + p.nv, wg1); ++x) add_from_lds<HD, BITS, CT, NW>(sh, x, acc);
-  };
-  // a pair's results and those of its groups: which of a workgroup's (group's) two slots, by whether the pair begins before it
+  // pairs that other workgroups share, all waves at each: the one that the run begins inside of (0), the one that begins in it (1)
   const u32 group = wg / SHORT_GROUP, group0 = group * SHORT_GROUP;
+  u32* const group_ctr = a.ctr + (u64)a.n_seqs * a.nkv + 2;
+  // a pair's results and those of its groups: which of a workgroup's (group's) two slots, by whether the pair begins before it
   auto piece = [&](u32 x, u32 first) { return a.part + (u64)(2 * x + (x == first ? 1u : 0u)) * short_slot<HD, CT>(); };
   auto group_piece = [&](u32 x, u32 first) { return a.part + (u64)(2 * (nwg + x) + (x == first / SHORT_GROUP ? 1u : 0u)) * short_slot<HD, CT>(); };
-  // counts one result more; whether it was the last of n
-  auto count = [&](u32* ctr, u32 n) {
-    u32 before = 0;
-    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-    if (lane == 0) {
-      before = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (before == n - 1) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    return scalar(before) == n - 1;
-  };
-  u32* const group_ctr = a.ctr + (u64)a.n_seqs * a.nkv + 2;
-  auto hand_on = [&](const Pair& p, u32 which) {     // the workgroup's share of the pair to the workspace; who comes last is told
-    leave_past_caches<HD, BITS, CT>(a.part + (u64)(2 * wg + which) * short_slot<HD, CT>(), acc, p.n * a.G);
-    const u32 f = first_wg(p), np = n_wgs(p);
-    u32 last;
-    if (np <= SHORT_GROUP) last = count(a.ctr + (u64)p.s * a.nkv + p.g, np);
-    else last = count(group_ctr + 2 * group + (f >= group0 ? 1u : 0u), min(f + np, group0 + SHORT_GROUP) - max(f, group0));
-    if (lane == 0) sh.last[which] = last;
-  };
-  if (u0 < u1 && cur.first >= u0 && u1 < cur.first + cur.nv) {
-    others(cur, w + 1);
-    if (cur.first + cur.nv <= wg1) finish(cur); else hand_on(cur, 1);
-  }
-  if (w == 0) {
-    const Pair p = whole ? cur : pair_at(wg0);
-    if (p.first < wg0) {
-      clear();
-      others(p, 0);
-      hand_on(p, 0);
-    }
-  }
-  __syncthreads();
-#pragma unroll 1
-  for (u32 which = 0; which < 2; ++which) {
-    if (!scalar(sh.last[which])) continue;
-    const Pair p = pair_at(whole ? wg : which ? wg1 - 1 : wg0);
-    const u32 f = first_wg(p), np = n_wgs(p), rows = p.n * a.G;
-    ShortMerge<HD, BITS, CT, NW> all;
-    if (np > SHORT_GROUP) {                          // this workgroup's group, then, if it is the last of them, the groups
-      all.sum(max(f, group0), min(f + np, group0 + SHORT_GROUP), rows, [&](u32 x) { return piece(x, f); });
-      all.leave(group_piece(group, f));
-      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-      __syncthreads();
-      if (w == 0) {
-        const bool last = count(a.ctr + (u64)p.s * a.nkv + p.g, (f + np - 1) / SHORT_GROUP - f / SHORT_GROUP + 1);
-        if (lane == 0) sh.last[which] = last;
-      }
-      __syncthreads();
-      if (!scalar(sh.last[which])) continue;
-      all.sum(f / SHORT_GROUP, (f + np - 1) / SHORT_GROUP + 1, rows, [&](u32 x) { return group_piece(x, f); });
-    } else all.sum(f, f + np, rows, [&](u32 x) { return piece(x, f); });
+  ShortMerge<HD, BITS, CT, NW> all;
+  auto finish_all = [&](const Pair& p) {
     const float l = quad_sum(all.l), inv = l == 0.f ? 0.f : 1.0f / l;
     const u32 r = all.c * 16 + lc, tok = r / a.G, k = (p.g * a.G + r - tok * a.G) * HD;
-    if (!all.live) continue;
+    if (!all.live) return;
     if constexpr (BITS == 16) {
 #pragma unroll
       for (int t = 0; t < all.T; ++t)
@@ -765,6 +719,55 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
         if constexpr (all.T == 2) *(u32*)x = pair; else *x = (f16_t)pair;
       }
     }
+  };
+#pragma unroll 1
+  for (u32 which = 0; which < 2; ++which) {
+    const Pair p = pair_at(whole ? wg : which ? wg1 - 1 : wg0);
+    const u32 end = p.first + p.nv, f = first_wg(p), np = n_wgs(p);
+    if (which ? p.first < wg0 || end <= (whole ? quantum : wg1) : p.first >= wg0) continue;      // (a pair in one run: its wave has finished it)
+    const u32 x0 = which ? (p.first - wg0) / quantum : 0u, x1 = (min(end, wg1) - wg0 + quantum - 1) / quantum;
+    all.sum(x0, x1, p.n * a.G, [&](u32 x) { return LdsResult<HD, CT, NW>{sh, which && x == x0 ? (u32)NW : x}; });
+    if (np == 1) { finish_all(p); continue; }
+    all.leave(a.part + (u64)(2 * wg + which) * short_slot<HD, CT>());
+    if (threadIdx.x == 0) {
+      const bool grouped = np > SHORT_GROUP;
+      sh.ctr[which] = grouped ? group_ctr + 2 * group + (f >= group0 ? 1u : 0u) : a.ctr + (u64)p.s * a.nkv + p.g;
+      sh.need[which] = grouped ? min(f + np, group0 + SHORT_GROUP) - max(f, group0) : np;
+    }
+  }
+  if (goes_on && !whole && cur.first + cur.nv <= wg1) {
+#pragma unroll 1
+    for (u32 x = w + 1; x < NW && wg0 + x * quantum < cur.first + cur.nv; ++x) add_from_lds<HD, BITS, CT, NW>(sh, x, acc);
+    finish(cur);
+  }
+  // counts one result more, of lane i for pair i, when all waves' are in memory; whether it was the last one
+  auto count = [&](bool mine, u32* ctr, u32 n) {
+    if (!mine) return;
+    const bool last = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
+    if (last) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    sh.last[lane] = last;
+  };
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+  __syncthreads();
+  if (threadIdx.x < 2) count(sh.need[lane] != 0, sh.ctr[lane], sh.need[lane]);
+  __syncthreads();
+#pragma unroll 1
+  for (u32 which = 0; which < 2; ++which) {
+    if (!scalar(sh.last[which])) continue;
+    const Pair p = pair_at(whole ? wg : which ? wg1 - 1 : wg0);
+    const u32 f = first_wg(p), np = n_wgs(p), rows = p.n * a.G;
+    auto of_wg = [&](u32 x) { return FarResult<HD>{piece(x, f)}; };
+    if (np > SHORT_GROUP) {                          // this workgroup's group, then, if it is the last of them, the groups
+      all.sum(max(f, group0), min(f + np, group0 + SHORT_GROUP), rows, of_wg);
+      all.leave(group_piece(group, f));
+      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      __syncthreads();
+      if (threadIdx.x < 2) count(lane == which, a.ctr + (u64)p.s * a.nkv + p.g, (f + np - 1) / SHORT_GROUP - f / SHORT_GROUP + 1);
+      __syncthreads();
+      if (!scalar(sh.last[which])) continue;
+      all.sum(f / SHORT_GROUP, (f + np - 1) / SHORT_GROUP + 1, rows, [&](u32 x) { return FarResult<HD>{group_piece(x, f)}; });
+    } else all.sum(f, f + np, rows, of_wg);
+    finish_all(p);
   }
 }
 
