@@ -780,6 +780,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 // wave skips the steps that none of its own rows see. Items come from a counter, the last queries first. With fewer items than workgroups the
 // keys of each are cut into parts, whose results a second kernel adds up.
 #define PROMPT_CT 2u
+#define PROMPT_PIPE 3             // groups of operands on their way from LDS and in use
 #define PROMPT_ROWS (128u * PROMPT_CT)
 #define PROMPT_RING (128u * 1024u)
 #define PROMPT_SLOT(HD) (PROMPT_ROWS * ((HD) + 2u))      // floats of a part's result: maximum and sum of every row, then its output
@@ -836,6 +837,13 @@ __device__ __forceinline__ void give_strange_block(const PagedArgs& a, u32 id, u
   }
 }
 
+// (nothing is moved over either: the products belong on one side)
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+template <int N> __device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 template <int HD, int BITS>
 __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& sh, u32 wg, u32 nwg, bool behind_short) {
   constexpr int CT = PROMPT_CT;
@@ -847,18 +855,23 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
   const u32 lds0 = (u32)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sh.ring;
   // fetching halves: waves 0-3 the K of a block each, waves 4-7 the V (places in LDS: attn_prompt)
   const bool fk = w < 4;
+  const u32 ahead = fk ? NS - 1 : NS - 2;          // stages that a wave's fetches are ahead of its scores
   const u32 fb = w & 3u, f_lds = lds0 + w * BLK;
   const u32 k_tok = (lc & 4) * 2 + (lc & 3) + (((lc >> 3) ^ fb) & 1u) * 4;    // the key that lies at this lane's place of a K tile
-  u32 voff[TPW];
-#pragma unroll
-  for (u32 r = 0; r < TPW; ++r) voff[r] = fk ? k_tok * (HD * 2) + r * 64 + lg * 16 : (r * 32 + (lg >> 1) * 16 + lc) * 32 + (lg & 1) * 16;
+  const u32 voff = fk ? k_tok * (HD * 2) + lg * 16 : ((lg >> 1) * 16 + lc) * 32 + (lg & 1) * 16, vstep = fk ? 64 : 1024;
   const u32 k_at[2] = {(lc >> 3) * BLK + lg * 256 + (lc >> 3) * 128 + (lc & 7) * 16, (lc >> 3) * BLK + lg * 256 + ((lc >> 3) ^ 1u) * 128 + (lc & 7) * 16};
   const u32 v_at = NB * BLK + (lg >> 1) * BLK + (lg & 1) * 256 + lc * 16;
-  // a lane's places in a 4-bit record (values: tokens 8 th ..), and where its four dimensions of 8 values lie in a block of the ring
-  const u32 th = lg & 1, d4 = HD == 128 ? lc * 8 + (lane >> 5) * 4 : lc * 4;
-  const TileLane at4 = {opaque(k_tok * (HD / 2) + lg * 4), opaque((th * 32 + lc) * (HD / 8)), opaque(k_tok), opaque(lc / (HD == 128 ? 4 : 8) * 16 + th * 8)};
-  const u32 to4 = opaque(d4 / 32 * 1024 + (d4 % 32 / 16 * 2 + th) * 256 + d4 % 16 * 16);
+  // A lane's places in a 4-bit record, and where its four dimensions of 8 values (tokens 8 th ..) lie in a block of the ring: it writes them in
+  // an order of its own (x ^ turn, with the bytes of `pick` and `odd`), so that 16 lanes write to all banks at a time (all in one order they meet in an
+  // eighth of them: a third of the kernel's LDS time)
+  const u32 vl = HD == 128 ? lane >> 1 & 15 : lc, vh = HD == 128 ? lane & 1 : 0u, th = HD == 128 ? lane >> 5 : lg & 1, turn4 = HD == 128 ? vl >> 1 & 3 : vl >> 2 & 3;
+  const u32 d4 = HD == 128 ? vl * 8 + vh * 4 : vl * 4;
+  const TileLane at4 = {opaque(k_tok * (HD / 2) + lg * 4), opaque((th * 32 + vl) * (HD / 8)), opaque(k_tok), opaque(vl / (HD == 128 ? 4 : 8) * 16 + th * 8)};
+  const u32 to4 = opaque(d4 / 32 * 1024 + (d4 % 32 / 16 * 2 + th) * 256 + d4 % 16 * 16 + turn4 * 16);
+  const u32 pick = opaque((turn4 & 2 ? 0x0C0C0001u : 0x0C0C0100u) + vh * 0x0202u), odd = opaque(turn4 & 1 ? 0x02020202u : 0u);
   typedef const __attribute__((address_space(4))) u32 const_u32;
+  if (threadIdx.x == 0) sh.strange = 0;
+  __syncthreads();
   // (behind the short part a workgroup may come late: then its first item comes from the counter too)
   u32 turn = wg;
   if (behind_short && total) {
@@ -869,7 +882,6 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
   }
   while (turn < total) {
     const u32 item = turn / parts, part = turn - item * parts;
-    if (threadIdx.x == 0) sh.strange = 0;                       // (seen behind the first step's barrier)
     PromptItem it = prompt_item(a, sh.pre, item);
     it.s = (u32)__builtin_amdgcn_readfirstlane(it.s); it.g = (u32)__builtin_amdgcn_readfirstlane(it.g); it.r0 = (u32)__builtin_amdgcn_readfirstlane(it.r0);
     it.rows = (u32)__builtin_amdgcn_readfirstlane(it.rows); it.t0 = (u32)__builtin_amdgcn_readfirstlane(it.t0);
@@ -903,29 +915,49 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) o[c][d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     }
-    auto needed = [&](u32 k0) { return live && (i32)k0 <= wp1 && !(a.window && (i32)k0 + 63 <= wp0 - (i32)a.window && k0 >= a.sinks); };      // by some row of this wave
-    auto item_edge = [&](u32 k0, u32 bad) { return (i32)k0 + 63 > it.p0 || bad || (a.window && (i32)k0 <= it.p1 - (i32)a.window && k0 + 64 > a.sinks); };      // not seen as a whole by every row of the item
-    auto edge_of = [&](u32 k0, u32 bad) { return (i32)k0 + 63 > wp0 || wr + 16 * CT > it.rows || bad || (a.window && (i32)k0 <= wp1 - (i32)a.window && k0 + 64 > a.sinks); };      // nor by every one of this wave
-    u32 id[NB], bad_ahead = 0;                       // ids of the stage to fetch next; which blocks of the stages in the ring are outside the cache, 4 bits each
+    // bounds on a step's first key (few scalar instructions in a step: they are in the way of the others)
+    const i32 none = INT32_MIN, need_hi = live ? wp1 : -1, need_lo = a.window ? wp0 - (i32)a.window - 63 : none;
+    const i32 edge_hi = wr + 16 * CT > it.rows ? none : wp0 - 63, edge_lo = a.window ? wp1 - (i32)a.window : none;
+    const i32 item_hi = it.p0 - 63, item_lo = a.window ? it.p1 - (i32)a.window : none;
+    auto needed = [&](u32 k0) { return ((i32)k0 <= need_hi) & (((i32)k0 > need_lo) | (k0 < a.sinks)); };                              // by some row of this wave
+    auto item_edge = [&](u32 k0, u32 bad) { return ((i32)k0 > item_hi) | (bad != 0) | (((i32)k0 <= item_lo) & (k0 + 64 > a.sinks)); };      // not seen as a whole by every row of the item
+    auto edge_of = [&](u32 k0, u32 bad) { return ((i32)k0 > edge_hi) | (bad != 0) | (((i32)k0 <= edge_lo) & (k0 + 64 > a.sinks)); };        // nor by every one of this wave
+    u32 id[NB], my_id = 0, bad_ahead = 0;            // ids of the stage to fetch next, and of this wave's block; which blocks of the stages in the ring are outside the cache, 4 bits each
+    auto next_ids = [&](u32 s) {
+      const u32 first = NB * tile_of(min(s, n_steps ? n_steps - 1 : 0u));
+      my_id = bt[min(first + fb, last_block)];
+      if (first + NB - 1 <= last_block) {
 #pragma unroll
-    for (u32 b = 0; b < NB; ++b) id[b] = block_id(s_lo, b);
-    auto next_ids = [&](u32 s) {                     // notes the stage being fetched, asks for the ids of stage s
+        for (u32 b = 0; b < NB; ++b) id[b] = bt[first + b];
+      } else {
 #pragma unroll
-      for (u32 b = 0; b < NB; ++b) { bad_ahead = bad_ahead << 1 | (id[b] < a.n_blocks ? 0u : 1u); id[b] = block_id(s, b); }
+        for (u32 b = 0; b < NB; ++b) id[b] = bt[min(first + b, last_block)];
+      }
     };
-    auto my_block = [&]() { return min(fb == 0 ? id[0] : fb == 1 ? id[1] : fb == 2 ? id[2] : id[3], a.n_blocks - 1); };
-    auto fetch = [&](u32 s) {                        // stage s (past the last: that one again, not used) into its place of the ring
-      const unsigned char* src = (const unsigned char*)uniform_ptr((const f16_t*)a.cache + (((u64)(fk ? 0u : a.n_blocks) + my_block()) * a.nkv + it.g) * (16 * HD));
-      const u32 at = f_lds + (s % NS) * STAGE;
+    auto note_bad = [&]() {                          // of the stage being fetched
+      bad_ahead <<= 4;
+      if (max(max(id[0], id[1]), max(id[2], id[3])) >= a.n_blocks) {
 #pragma unroll
-      for (u32 r = 0; r < TPW; ++r) dma_tile<false>(at + r * 1024, src, voff[r]);
-      next_ids(s + 1);
+        for (u32 b = 0; b < NB; ++b) bad_ahead |= (id[b] < a.n_blocks ? 0u : 1u) << (NB - 1 - b);
+      }
     };
-    // 4 bits: waves 0-3 a block's values each, waves 4-7 its keys
+    const unsigned char* const item_cache = (const unsigned char*)uniform_ptr((const unsigned char*)a.cache + (BITS == 16 ? ((u64)(fk ? 0u : a.n_blocks) * a.nkv + it.g) * BLK : (u64)it.g * (17 * HD)));
+    const u32 block_bytes = a.nkv * (BITS == 16 ? BLK : 17 * HD);
+    auto my_block = [&]() { return item_cache + (u64)min(my_id, a.n_blocks - 1) * block_bytes; };
+    // stage s (past the last: that one again, not used) into its place of the ring, a piece after the other
+    const unsigned char* f_src = nullptr;
+    u32 f_at = 0;
+    auto fetch_from = [&](u32 s) {
+      f_src = my_block();
+      f_at = f_lds + (s % NS) * STAGE;
+      note_bad();
+    };
+    auto fetch_piece = [&](u32 r) { dma_tile<false>(f_at + r * 1024, f_src + r * vstep, voff); };
+    // 4 bits: waves 0-3 a block's keys each, waves 4-7 its values, by way of registers
     u32 raw[8], raw_s[4];
-    auto fetch4 = [&](u32 s) {
-      global_byte* const rec = uniform_global((const unsigned char*)a.cache + ((u64)my_block() * a.nkv + it.g) * (17 * HD));
-      if (!fk) {
+    auto fetch4 = [&]() {
+      global_byte* const rec = uniform_global(my_block());
+      if (fk) {
 #pragma unroll
         for (u32 r = 0; r < HD / 32; ++r) {
           raw[r] = from_global<u32>(rec + at4.k + r * 16);
@@ -944,11 +976,11 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
         const u32x2_t z = from_global<u32x2_t>(rec + at4.vs + 16 * HD + HD / 2);
         raw_s[0] = z[0]; raw_s[1] = z[1];
       }
-      next_ids(s + 1);
+      note_bad();
     };
     auto convert4 = [&](u32 s) {                     // what fetch4 brought, as halves into the ring
       unsigned char* const st = sh.ring + (s % NS) * STAGE;
-      if (!fk) {
+      if (fk) {
         unsigned char* const to = st + fb * BLK + lane * 16;
 #pragma unroll
         for (u32 r = 0; r < HD / 32; ++r) {
@@ -962,77 +994,122 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
 #pragma unroll
         for (u32 i = 0; i < 8; ++i) {
           const float sc = __uint_as_float((raw_s[i / 4] >> (8 * (i % 4)) & 0xFFu) << 23);
-          const u32 x = HD == 128 ? (lane >= 32 ? raw[i] >> 16 : raw[i]) : (i & 1 ? raw[i / 2] >> 16 : raw[i / 2]);
+          const u32 r = HD == 128 ? raw[i] : raw[i / 2], x = __builtin_amdgcn_perm(0u, r, HD == 64 && i & 1 ? pick + 0x0202u : pick);
           pr[i][0] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 0));
           pr[i][1] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 1));
         }
-        unsigned char* const to = st + (NB + fb) * BLK + to4;
+        unsigned char* const to = st + (NB + fb) * BLK;
 #pragma unroll
         for (u32 x = 0; x < 4; ++x) {
-          const u32 sel = x & 1 ? 0x07060302u : 0x05040100u;
+          const u32 sel = (x & 1 ? 0x07060302u : 0x05040100u) ^ odd;
           u32 v[4];
 #pragma unroll
           for (u32 i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(pr[2 * i + 1][x / 2], pr[2 * i][x / 2], sel);
-          *(uint4*)(to + x * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+          *(uint4*)(to + (to4 ^ x * 16)) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+      }
+    };
+    // values of a stage that are not finite: taken out (0 times one would not be 0) by the wave that brought them, where some row of the
+    // item must not see them, and given to the rows that see them at the end
+    auto take_strange_out = [&](u32 s, u32 bad) {
+      if (fk || s >= s_hi || !item_edge(tile_of(s) * 64, bad)) return;
+      unsigned char* const v = sh.ring + (s % NS) * STAGE + (NB + fb) * BLK + lane * 16;
+#pragma unroll
+      for (u32 r = 0; r < BLK / 1024; ++r) {
+        const uint4 x = *(const uint4*)(v + r * 1024), y = make_uint4(only_finite(x.x), only_finite(x.y), only_finite(x.z), only_finite(x.w));
+        if (__ballot(x.x != y.x || x.y != y.y || x.z != y.z || x.w != y.w)) {
+          *(uint4*)(v + r * 1024) = y;
+          sh.strange = 1;
         }
       }
     };
     if constexpr (BITS == 16) {
 #pragma unroll 1
-      for (u32 s = 0; s < NS - 1; ++s) fetch(s_lo + s);
+      for (u32 s = 0; s < ahead; ++s) {
+        next_ids(s_lo + s);
+        fetch_from(s_lo + s);
+#pragma unroll
+        for (u32 r = 0; r < TPW; ++r) fetch_piece(r);
+      }
+      next_ids(s_lo + ahead);
+      fetch_from(s_lo + ahead);
       wait_loads();      // (left to the compiler, the wait for the queries stands in the loop and empties the ring in every step)
     } else {
-      fetch4(s_lo);
+      next_ids(s_lo);
+      fetch4();
+      convert4(s_lo);
+      take_strange_out(s_lo, bad_ahead & 15u);
+      next_ids(s_lo + 1);
+      fetch4();
     }
-    for (u32 s = s_lo; s < s_hi; ++s) {
-      u32 bad;
-      if constexpr (BITS == 16) {
-        wait_dma_barrier<(int)((NS - 2) * TPW)>();             // stage s is in LDS for everyone, stage s - 1 has been read by everyone
-        bad = bad_ahead >> (4 * (NS - 2)) & 15u;
-        fetch(s + NS - 1);
-      } else {
-        bad = bad_ahead & 15u;
-        convert4(s);                                           // (everyone has read what lay there, step s - 2, before the last barrier)
-        fetch4(s + 1);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
-      }
-      const u32 k0 = tile_of(s) * 64;
-      if (item_edge(k0, bad)) {
-        // values that are not finite: taken out (0 times one would not be 0), and given to the rows that see them at the end
-        unsigned char* const v = sh.ring + (s % NS) * STAGE + NB * BLK + w * (NB * BLK / 8) + lane * 16;
+    lds_barrier();
+    if (!fk) lds_barrier();
+    floatx4_t sc[CT][NB];
+    f16x8_t pb[CT][NB / 2];
+    // The products of a step, in groups of two operands (2 CT products): those of the step before's probabilities with a tile of dimensions,
+    // then this step's scores. The operands come PROMPT_PIPE - 1 groups ahead, in one pipe, and a piece of a fetch now and then.
+    constexpr int NPV = HD / 16, PER = HD / 64, NG = NPV + (int)NB * PER;
+    f16x8_t x[PROMPT_PIPE][2];
+    auto ask = [&](u32 s, int i) {
+      const unsigned char *const sv = sh.ring + ((s - 1) % NS) * STAGE + v_at, *const st0 = sh.ring + (s % NS) * STAGE;
 #pragma unroll
-        for (u32 r = 0; r < NB * BLK / 8192; ++r) {
-          const uint4 x = *(const uint4*)(v + r * 1024), y = make_uint4(only_finite(x.x), only_finite(x.y), only_finite(x.z), only_finite(x.w));
-          if (__ballot(x.x != y.x || x.y != y.y || x.z != y.z || x.w != y.w)) {
-            *(uint4*)(v + r * 1024) = y;
-            sh.strange = 1;
+      for (int j = 0; j < 2; ++j) {
+        if (i < NPV) x[i % PROMPT_PIPE][j] = as_f16x8(*(const uint4*)(sv + 2 * j * BLK + (i >> 1) * 1024 + (i & 1) * 512));
+        else x[i % PROMPT_PIPE][j] = as_f16x8(*(const uint4*)(st0 + ((i - NPV) / PER & 2) * BLK + ((i - NPV) % PER * 2 + j) * 1024 + k_at[(i - NPV) / PER & 1]));
+      }
+    };
+    auto products = [&](u32 s, int i, bool more) {
+      if (more) ask(s, i + PROMPT_PIPE - 1);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          if (i < NPV) o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i % PROMPT_PIPE][j], pb[c][j], o[c][i], 0, 0, 0);
+          else {
+            floatx4_t& y = sc[c][(i - NPV) / PER];
+            const int at = (i - NPV) % PER * 2 + j;
+            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i % PROMPT_PIPE][j], q[c][at], at ? y : floatx4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
           }
         }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+      if constexpr (BITS == 16) {
+        if (i >= NPV && (i - NPV) % 2 && (i - NPV) / 2 < (int)TPW) fetch_piece((i - NPV) / 2);
       }
-      if (!needed(k0)) continue;
-      const unsigned char* const st0 = sh.ring + (s % NS) * STAGE;
-      floatx4_t sc[CT][NB];
-      {
-        // operands a block ahead of the products
-        f16x8_t ka[2][HD / 32];
-        auto ask = [&](u32 b) {
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    bool scored = false;                                       // of the step before: probabilities that wait for their values
+    for (u32 s = s_lo;; ++s) {
+      u32 bad = 0;
+      if (s < s_hi) bad = bad_ahead >> (4 * (BITS == 16 ? ahead : 1u)) & 15u;
+      if (scored) {
 #pragma unroll
-          for (int st = 0; st < HD / 32; ++st) ka[b & 1][st] = as_f16x8(*(const uint4*)(st0 + (b & 2) * BLK + st * 1024 + k_at[b & 1]));
-        };
-        ask(0);
+        for (int i = 0; i < PROMPT_PIPE - 1; ++i) ask(s, i);
 #pragma unroll
-        for (u32 b = 0; b < NB; ++b) {
-          if (b + 1 < NB) ask(b + 1);
+        for (int i = 0; i < NPV; ++i) products(s, i, true);
+      } else {
 #pragma unroll
-          for (int c = 0; c < CT; ++c) sc[c][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[b & 1][0], q[c][0], floatx4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        for (int i = 0; i < PROMPT_PIPE - 1; ++i) ask(s, NPV + i);
+      }
+      if (s == s_hi) break;
+      const u32 k0 = tile_of(s) * 64;
+      const bool scores = needed(k0);
+      if (scores) {
 #pragma unroll
-          for (int st = 1; st < HD / 32; ++st)
+        for (int i = NPV; i < NG; ++i) products(s, i, i + PROMPT_PIPE - 1 < NG);
+      } else if constexpr (BITS == 16) {
 #pragma unroll
-            for (int c = 0; c < CT; ++c) sc[c][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[b & 1][st], q[c][st], sc[c][b], 0, 0, 0);
-          __builtin_amdgcn_sched_barrier(0);
+        for (u32 r = 0; r < TPW; ++r) fetch_piece(r);
+      }
+      scored = scores;
+      if constexpr (BITS == 16) {
+        if (!fk) {
+          wait_dma<(int)((NS - 2) * TPW)>();                     // this wave's values of the step
+          take_strange_out(s, bad);
         }
       }
+      lds_barrier();
+      // (asked for here: with them on their way a wait for an operand from LDS would be one for them too)
+      next_ids(s + (BITS == 16 ? ahead + 1 : 2u));
+      if (scored) {
       const bool edge = edge_of(k0, bad);
       if (edge) {
         asm volatile("" ::: "memory");                         // (a branch: few steps are)
@@ -1048,7 +1125,6 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
             for (int i = 0; i < 4; ++i) sc[c][b][i] = vis >> (b * 4 + i) & 1u ? sc[c][b][i] : -INFINITY;
         }
       }
-      f16x8_t pb[CT][NB / 2];
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
         float top = -INFINITY;
@@ -1076,32 +1152,19 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
           }
         l[c] += ps;
       }
-      const unsigned char* const sv = st0 + v_at;
-      auto value_bits = [&](int d, u32 h) { return *(const uint4*)(sv + 2 * h * BLK + (d >> 1) * 1024 + (d & 1) * 512); };
-      {
-        // operands two tiles of dimensions ahead of the products, and no further: all at once they take the queries' registers
-        f16x8_t va[2][2][NB / 2];
-        auto ask = [&](int d) {
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (u32 h = 0; h < NB / 2; ++h) va[d / 2 % 2][x][h] = as_f16x8(value_bits(d + x, h));
-        };
-        ask(0);
-#pragma unroll
-        for (int d = 0; d < HD / 16; d += 2) {
-          if (d + 2 < HD / 16) ask(d + 2);
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (u32 h = 0; h < NB / 2; ++h)
-#pragma unroll
-              for (int c = 0; c < CT; ++c) o[c][d + x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d / 2 % 2][x][h], pb[c][h], o[c][d + x], 0, 0, 0);
-          __builtin_amdgcn_sched_barrier(0);
-        }
       }
+      if constexpr (BITS == 16) {
+        fetch_from(s + 1 + ahead);
+        if (fk) wait_dma<(int)((NS - 2) * TPW)>();               // this wave's keys of the next step
+      } else {
+        convert4(s + 1);
+        take_strange_out(s + 1, bad_ahead & 15u);
+        fetch4();
+      }
+      lds_barrier();
     }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    if (fk) lds_barrier();
+    lds_barrier();
     if ((u32)__builtin_amdgcn_readfirstlane(sh.strange)) {
 #pragma unroll 1
       for (u32 s = s_lo; s < s_hi; ++s) {
@@ -1147,6 +1210,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
     if constexpr (BITS == 16) wait_dma_barrier<0>();           // no fetch of this item is on its way any more, and next_item is there
     else __syncthreads();
     turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item);
+    if (threadIdx.x == 0) sh.strange = 0;
     __syncthreads();                                           // (read by everyone before it is written again)
   }
   // the last workgroup out leaves the counters as it found them
