@@ -786,7 +786,10 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 #define PROMPT_SLOT(HD) (PROMPT_ROWS * ((HD) + 2u))      // floats of a part's result: maximum and sum of every row, then its output
 struct PromptShared {
   alignas(256) unsigned char ring[PROMPT_RING];
-  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], next_item, strange;      // strange: some step of the item had values that are not finite
+  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES];
+  // the item after this one, and whether some step of it had values that are not finite: by the item's number among the workgroup's, so that no
+  // wave has to wait at its end for those that read them
+  u32 next_item[2], strange[3];
 };
 __device__ __forceinline__ u32 prompt_items(const PagedArgs& a, u32 s) {
   const SeqView v = seq_view(a, s);
@@ -870,18 +873,22 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
   const u32 to4 = opaque(d4 / 32 * 1024 + (d4 % 32 / 16 * 2 + th) * 256 + d4 % 16 * 16 + turn4 * 16);
   const u32 pick = opaque((turn4 & 2 ? 0x0C0C0001u : 0x0C0C0100u) + vh * 0x0202u), odd = opaque(turn4 & 1 ? 0x02020202u : 0u);
   typedef const __attribute__((address_space(4))) u32 const_u32;
-  if (threadIdx.x == 0) sh.strange = 0;
+  if (threadIdx.x < 3) sh.strange[threadIdx.x] = 0;
   __syncthreads();
   // (behind the short part a workgroup may come late: then its first item comes from the counter too)
   u32 turn = wg;
   if (behind_short && total) {
-    if (threadIdx.x == 0) sh.next_item = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) sh.next_item[1] = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item);
-    __syncthreads();
+    turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item[1]);
   }
-  while (turn < total) {
-    const u32 item = turn / parts, part = turn - item * parts;
+  for (u32 nth = 0; turn < total; ++nth) {
+    u32 after = 0, *const strange = sh.strange + nth % 3;
+    if (threadIdx.x == 0) {
+      after = (behind_short ? 0u : nwg) + __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      sh.strange[(nth + 1) % 3] = 0;                            // (read last two items ago)
+    }
+    const u32 this_turn = turn, item = turn / parts, part = turn - item * parts;
     PromptItem it = prompt_item(a, sh.pre, item);
     it.s = (u32)__builtin_amdgcn_readfirstlane(it.s); it.g = (u32)__builtin_amdgcn_readfirstlane(it.g); it.r0 = (u32)__builtin_amdgcn_readfirstlane(it.r0);
     it.rows = (u32)__builtin_amdgcn_readfirstlane(it.rows); it.t0 = (u32)__builtin_amdgcn_readfirstlane(it.t0);
@@ -1019,7 +1026,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
         const uint4 x = *(const uint4*)(v + r * 1024), y = make_uint4(only_finite(x.x), only_finite(x.y), only_finite(x.z), only_finite(x.w));
         if (__ballot(x.x != y.x || x.y != y.y || x.z != y.z || x.w != y.w)) {
           *(uint4*)(v + r * 1024) = y;
-          sh.strange = 1;
+          *strange = 1;
         }
       }
     };
@@ -1042,6 +1049,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
       next_ids(s_lo + 1);
       fetch4();
     }
+    if (threadIdx.x == 0) sh.next_item[nth & 1] = after;
     lds_barrier();
     if (!fk) lds_barrier();
     floatx4_t sc[CT][NB];
@@ -1163,9 +1171,11 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
       }
       lds_barrier();
     }
+    if constexpr (BITS == 16) wait_dma<0>();                   // (no fetch of this item is on its way any more)
     if (fk) lds_barrier();
     lds_barrier();
-    if ((u32)__builtin_amdgcn_readfirstlane(sh.strange)) {
+    turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item[nth & 1]);
+    if ((u32)__builtin_amdgcn_readfirstlane(*strange)) {
 #pragma unroll 1
       for (u32 s = s_lo; s < s_hi; ++s) {
         const u32 k0 = tile_of(s) * 64;
@@ -1184,7 +1194,6 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
       }
       wait_loads();
     }
-    if (threadIdx.x == 0) sh.next_item = (behind_short ? 0u : nwg) + __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     // (where a row goes is worked out here: the compiler must not keep it through the loop)
     const u32 at_end = opaque(lane), lc_end = at_end & 15, lg_end = at_end >> 4;
 #pragma unroll
@@ -1201,17 +1210,12 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
         for (int d = 0; d < HD / 16; ++d)
           *(uint2*)(to + (u64)(d / 2) * step + d % 2 * half) = make_uint2(half_pair(o[c][d][0] * inv, o[c][d][1] * inv), half_pair(o[c][d][2] * inv, o[c][d][3] * inv));
       } else {
-        float* const slot = a.prompt_part + (u64)turn * PROMPT_SLOT(HD);
+        float* const slot = a.prompt_part + (u64)this_turn * PROMPT_SLOT(HD);
         if (lg_end == 0) *(float2*)(slot + 2 * r) = make_float2(m[c], sum);
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(slot + 2 * PROMPT_ROWS + r * HD + d * 16 + lg_end * 4) = o[c][d];
       }
     }
-    if constexpr (BITS == 16) wait_dma_barrier<0>();           // no fetch of this item is on its way any more, and next_item is there
-    else __syncthreads();
-    turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item);
-    if (threadIdx.x == 0) sh.strange = 0;
-    __syncthreads();                                           // (read by everyone before it is written again)
   }
   // the last workgroup out leaves the counters as it found them
   if (total && threadIdx.x == 0 && __hip_atomic_fetch_add(ctr + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == nwg - 1) {
