@@ -14,8 +14,9 @@
 // 43 us (4.8 TB/s, what a plain copy of as much reaches), into 4 bits 43 us for 176 MB. It took 67 us with two rows a lane and 8-byte
 // loads, 56 with 17 and not 34 KB of LDS a workgroup, 51 with one row a lane (64 registers: 8 waves a SIMD) and 16-byte loads, 47 with
 // non-temporal loads, and 43 with keys apart from queries. Few tokens are bound by their chain (place and position, table, store) and
-// the launch: 3 us. What is between the bytes is 32-bit arithmetic, with one exception: keys that go into 4 bits are normed and rotated in 64 bits, because a sum in another order would move the few values next to a border
-// between two codes by half their size. (Values are not computed on: their codes are exact either way.)
+// the launch: 3 us. What is between the bytes is 32-bit arithmetic, with one exception: keys that go into 4 bits are normed and
+// rotated in 64 bits, because a sum in another order would move the few values next to a border between two codes by half their
+// size. (Values are not computed on: their codes are exact either way.)
 #pragma once
 #include "blink_device.h"
 
@@ -311,11 +312,11 @@ __device__ __forceinline__ void kv_store(const StoreArgs& a, ValueShared<HD>& sh
     else store_values4<T, HD>(a, wg);
   } else if (wg < nv + nk) {
     StoreRow<T, HD, BITS, true> r;
-    r.load(a, ((wg - nv) * 256 + threadIdx.x) / r.LR);
+    r.load(a, (wg - nv) * (256 / r.LR) + threadIdx.x / r.LR);
     r.store(a);
   } else {
     StoreRow<T, HD, BITS, false> r;
-    r.load(a, ((wg - nv - nk) * 256 + threadIdx.x) / r.LR);
+    r.load(a, (wg - nv - nk) * (256 / r.LR) + threadIdx.x / r.LR);
     r.store(a);
   }
 }

@@ -32,7 +32,7 @@ def new_cache(n_blocks, nkv, hd, bits):
     return B.KVCache(data, n_blocks, nkv, hd, bits)
 
 
-def oracle_cache(c, bits=None):
+def oracle_cache(c):
     d = c.desc
     return P.Cache(c.data.cpu().numpy().copy(), d.n_blocks, d.n_kv_heads, d.head_dim, d.bits)
 
@@ -203,7 +203,7 @@ def run_attention(cache, tables, lens, cu, q, max_q, window=0, sinks=0, scale=1.
     return out.double().cpu().numpy()
 
 
-def check_attention(got, cache, c, tables, lens, cu, q, window=0, sinks=0, scale=1.0, rows=None, fill=9.0):
+def check_attention(got, cache, c, tables, lens, cu, q, window=0, sinks=0, scale=1.0, fill=9.0):
     want, spread = P.attention(q.astype(np.float64), c, tables, lens, cu, window, sinks, scale)
     hd = q.shape[2]
     # scores: hd products in 32 bits of at most |q| |k| in all: off by hd 2^-24 of that; a probability by as much (twice: numerator and
@@ -441,3 +441,132 @@ def test_results_do_not_depend_on_the_rest_of_the_batch_by_more_than_rounding():
     again = run_attention(*one[:1], *one[2:], max_q=1)
     assert np.array_equal(a, again)
     check_attention(a, *one)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_more_prompts_than_workgroups_with_strange_values(bits):
+    """Workgroups that take several prompts one after the other; in some of those, values that are not finite and not seen by all."""
+    S, n, nq, nkv, hd = 96, 130, 8, 8, 64
+    cache, c, tables, lens, cu, q = make_batch([n] * S, [n] * S, nq, nkv, hd, bits, seed=20)
+    rng = np.random.default_rng(21)
+    for s in range(0, S, 5):
+        j, g = int(rng.integers(0, n)), int(rng.integers(0, nkv))
+        k, v = rng.standard_normal((2, nkv, hd))
+        v[g, 7] = (np.inf, -np.inf, np.nan)[s % 3]
+        c.put(int(tables[s, j // 16]) * 16 + j % 16, k, v)
+        if bits == 16 and s % 3 < 2:
+            c.v[tables[s, j // 16], g, 7, j % 16] = np.float16((np.inf, -np.inf)[s % 3])
+    cache.data.copy_(torch.from_numpy(c.data))
+    got = run_attention(cache, tables, lens, cu, q, n, 50, 3)
+    check_attention(got, cache, c, tables, lens, cu, q, 50, 3)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("hd, window, sinks", [(128, 200, 20), (64, 0, 0), (64, 333, 1)])
+def test_chunks_of_several_items_behind_a_context(hd, window, sinks, bits):
+    b = make_batch([1500, 901, 64], [1300, 500, 1], 8, 2, hd, bits, seed=22)
+    got = run_attention(*b[:1], *b[2:], max_q=1300, window=window, sinks=sinks)
+    check_attention(got, *b, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_the_largest_number_of_sequences(bits):
+    rng = np.random.default_rng(23)
+    lens = [int(x) for x in rng.integers(0, 70, 1024)]
+    runs = [1] * 1024
+    lens[700], runs[700] = 300, 290
+    b = make_batch(lens, runs, 2, 1, 64, bits, seed=23)
+    for max_q in (290, 1):                               # (max_q 1: of the long one, the first)
+        got = run_attention(*b[:1], *b[2:], max_q=max_q, window=40, sinks=2)
+        if max_q == 1:
+            at = int(b[4][700])
+            assert (got[at + 1:at + 290] == 9.0).all()
+            keep = np.r_[0:at + 1, at + 290:len(got)]
+            assert np.allclose(got[keep], full[keep], atol=1e-2)
+        else:
+            check_attention(got, *b, window=40, sinks=2)
+            full = got
+
+
+def test_more_sequences_are_refused():
+    b = make_batch([1], [1], 2, 1, 64, 16, seed=24)
+    lens, cu, tables = np.ones(1025, np.int32), np.arange(1026, dtype=np.int32), np.zeros((1025, 1), np.int32)
+    with pytest.raises(RuntimeError):
+        run_attention(b[0], tables, lens, cu, np.zeros((1025, 2, 64), np.float16), 1, workspace=torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_places_behind_4_gib_of_cache(bits):
+    """The same tokens in a small cache and in one whose blocks lie beyond 32 bits of bytes: the same results, to the bit."""
+    nq, nkv, hd = 16, 8, 128
+    lens, runs = np.int32([100, 300, 33]), [1, 200, 3]
+    need = (lens + 15) // 16
+    few, many = int(need.sum()), 150000 if bits == 16 else 320000      # 9.8 and 5.6 GB
+    caches = [B.KVCache(torch.empty(P.cache_bytes(n, nkv, hd, bits), dtype=torch.uint8, device="cuda"), n, nkv, hd, bits) for n in (few, many)]
+    T = int(lens.sum())
+    g = torch.Generator().manual_seed(25)
+    q, k, v = (torch.randn(T, n, hd, generator=g).cuda() for n in (nq, nkv, nkv))
+    pos = dev(np.concatenate([np.arange(n) for n in lens]).astype(np.int32))
+    table = dev(rope_table(300, hd))
+    rng = np.random.default_rng(25)
+    results = []
+    for cache, n in zip(caches, (few, many)):
+        cache.data[:1 << 20].fill_(GARBAGE)
+        blocks = (rng.permutation(few) if n == few else n - 1 - 7 * rng.permutation(few)).astype(np.int32)
+        tables = np.zeros((3, int(need.max())), np.int32)
+        tables[0, :need[0]], tables[1, :need[1]], tables[2, :need[2]] = np.split(blocks, np.cumsum(need)[:-1])
+        slots = np.concatenate([tables[s, np.arange(m) // 16] * 16 + np.arange(m) % 16 for s, m in enumerate(lens)]).astype(np.int32)
+        turned = torch.empty(T, nq, hd, dtype=torch.float16, device="cuda")
+        st = torch.cuda.current_stream().cuda_stream
+        B.qk_norm_rope(q, k, v, pos, dev(slots), table, cache, turned, q_scale=hd ** -0.5, stream=st)
+        back = torch.zeros(2, T, nkv, hd, dtype=torch.float16, device="cuda")
+        B.kv_cache_read(cache, dev(slots), back[0], back[1], stream=st)
+        last = np.concatenate([np.arange(e - r, e) for e, r in zip(np.cumsum(lens), runs)])
+        rows = turned[dev(last)].contiguous()
+        cu = dev(np.concatenate(([0], np.cumsum(runs))).astype(np.int32))
+        one = dev(np.int32([0, 1, 2, 3]))
+        outs = []
+        for qq, c, max_q in ((rows, cu, max(runs)), (rows[:3].contiguous(), one, 1)):
+            out = torch.zeros_like(qq)
+            work = torch.zeros(B.attention_workspace_bytes(nq, cache, 3, max_q), dtype=torch.uint8, device="cuda")
+            B.paged_attention(qq, cache, dev(tables), dev(lens), c, out, work, max_q=max_q, stream=st)
+            outs.append(out)
+        torch.cuda.synchronize()
+        results.append([turned.clone(), back, *outs])
+    assert bool(torch.isfinite(results[0][2]).all()) and float(results[0][3].abs().max()) > 0
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_prompts_and_single_tokens_in_a_graph(bits):
+    """A mixed batch and one long prompt whose keys are cut into parts (two kernels), captured and replayed beside eager calls of their own."""
+    mixed = make_batch([400, 90, 300, 5], [150, 1, 300, 1], 8, 2, 64, bits, seed=26)
+    long = make_batch([2500], [60], 8, 2, 64, bits, seed=27)
+    calls = []
+    for b, max_q in ((mixed, 300), (long, 60)):
+        args = [dev(x) for x in (b[5], *b[2:5])]
+        out = torch.zeros(b[5].shape, dtype=torch.float16, device="cuda")
+        works = [torch.zeros(B.attention_workspace_bytes(8, b[0], len(b[3]), max_q), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        calls.append((b, args, out, works, max_q))
+
+    def step(which):
+        for b, args, out, works, max_q in calls:
+            B.paged_attention(args[0], b[0], *args[1:], out, works[which], max_q=max_q, window=70, sinks=4, stream=torch.cuda.current_stream().cuda_stream)
+
+    step(0)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(0)
+    for _ in range(4):
+        for c in calls:
+            c[2].zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        first = [c[2].clone() for c in calls]
+        step(1)
+        torch.cuda.synchronize()
+        for (b, _, out, _, _), x in zip(calls, first):
+            assert torch.equal(x, out)
+            check_attention(x.double().cpu().numpy(), *b, window=70, sinks=4)
