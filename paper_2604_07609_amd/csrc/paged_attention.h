@@ -277,6 +277,12 @@ struct ShortShared {
   unsigned char n[PAGED_MAX_SEQS];                   // (a short sequence has at most 64 rows)
 };
 
+__device__ __forceinline__ u32 wave_sums(u32 v) {     // inclusive prefix sums over the wave
+  const u32 lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) { const u32 x = __shfl_up(v, o); if (lane >= (u32)o) v += x; }
+  return v;
+}
 // exclusive prefix sums of f(0 .. n) into pre[0 .. n], by a workgroup of NW waves
 template <u32 NW, typename F>
 __device__ __forceinline__ void prefix_sums(u32* pre, u32* wave_sum, u32 n, F f) {
@@ -284,9 +290,7 @@ __device__ __forceinline__ void prefix_sums(u32* pre, u32* wave_sum, u32 n, F f)
   u32 base = 0;
   for (u32 i0 = 0; i0 < n; i0 += 64 * NW) {
     const u32 i = i0 + threadIdx.x;
-    u32 v = i < n ? f(i) : 0u;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const u32 x = __shfl_up(v, o); if (lane >= (u32)o) v += x; }
+    const u32 v = wave_sums(i < n ? f(i) : 0u);
     __syncthreads();
     if (lane == 63) wave_sum[w] = v;
     __syncthreads();
@@ -501,30 +505,57 @@ __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { r
 // Few short pairs (half as many as workgroups, eight tiles a wave) are dealt out whole instead, a workgroup or several to each: up to that
 // length no result then crosses workgroups, which would take longer than the tiles do.
 // The loop over tiles is written out NT times for its registers, so all that is rare stands outside of it, once.
-#define SHORT_QUANTUM 4u
-#define SHORT_GROUP 16u
+#define SHORT_GROUP 8u
 // 32-bit counters of a launch of nwg workgroups (pairs; two for the prompt part; groups) and floats of its results
 __host__ __device__ __forceinline__ u64 paged_counters(u64 pairs, u32 nwg) { return pairs + 2 + 2 * ((nwg + SHORT_GROUP - 1) / SHORT_GROUP); }
 __host__ __device__ __forceinline__ u64 short_floats(u32 nwg, u32 hd, u32 ct) { return 2ull * (nwg + (nwg + SHORT_GROUP - 1) / SHORT_GROUP) * ct * (128 + 16 * hd); }
 template <int HD, int BITS, int CT, int NT, int NW>
 __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, CT, NW>& sh, u32 wg, u32 nwg) {
   typedef CacheTile<HD, BITS> Tile;
-  constexpr u32 CAP = 8 * NW;                        // tiles of a workgroup's share of a pair that is dealt out whole
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
   auto scalar = [](u32 x) { return (u32)__builtin_amdgcn_readfirstlane(x); };
-  auto units = [&](u32 s) {
+  auto count_tiles = [&](u32 s) {
     const SeqView v = seq_view(a, s);
-    sh.pos0[s] = v.pos0; sh.n[s] = (unsigned char)v.n;
-    return short_unit_count(a, v);
+    const u32 n = short_unit_count(a, v);
+    sh.pos0[s] = v.pos0; sh.n[s] = n ? (unsigned char)v.n : (unsigned char)0;
+    return n;
   };
-  bool whole = a.n_seqs * a.nkv <= nwg / 2;          // pairs dealt out whole: then `pre` counts workgroups, else units
-  if (whole) {
-    prefix_sums<NW>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return (units(s) + CAP - 1) / CAP * a.nkv; });
-    whole = scalar(sh.pre[a.n_seqs]) <= nwg;
-    if (!whole) __syncthreads();
+  // Pairs dealt out whole: `cap` tiles of one at most to a workgroup, as few as there are workgroups for, but 32; then `pre` counts
+  // workgroups, else units.
+  const u32 pairs = a.n_seqs * a.nkv;
+  u32 U, cap;
+  bool whole;
+  auto choose = [&](u32 units, u32 of) {             // (of = nwg - pairs: these are always enough)
+    cap = pairs <= nwg / 2 ? max(32u, (units + of - 1) / of) : ~0u;
+    whole = cap <= 64;
+  };
+  if (a.n_seqs <= 64) {                              // every wave for itself, all the same: nobody waits
+    const u32 n = lane < a.n_seqs ? count_tiles(lane) : 0u;
+    u32 sum = wave_sums(n * a.nkv);
+    const u32 units = U = (u32)__builtin_amdgcn_readlane((i32)sum, 63);
+#pragma unroll 1
+    for (u32 of = nwg;; of = nwg - pairs) {
+      choose(units, of);
+      if (!whole) break;
+      const u32 x = wave_sums((n + cap - 1) / cap * a.nkv), wgs = (u32)__builtin_amdgcn_readlane((i32)x, 63);
+      if (wgs <= nwg) { sum = x; U = wgs; break; }
+    }
+    if (lane < a.n_seqs) sh.pre[lane + 1] = sum;
+    if (lane == 0) sh.pre[0] = 0;
+    __builtin_amdgcn_wave_barrier();
+  } else {
+    prefix_sums<NW>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return count_tiles(s) * a.nkv; });
+    choose(scalar(sh.pre[a.n_seqs]), nwg - pairs);
+    if (whole) {
+      __syncthreads();
+      prefix_sums<NW>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) {
+        const i32 p0 = sh.pos0[s], n = (i32)sh.n[s];
+        return n ? (max(1u, seen_tiles<16>(a, p0, p0 + n - 1).n) + cap - 1) / cap * a.nkv : 0u;
+      });
+    }
+    U = scalar(sh.pre[a.n_seqs]);
   }
-  if (!whole) prefix_sums<NW>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return units(s) * a.nkv; });
-  const u32 U = scalar(sh.pre[a.n_seqs]), wg_units = max(SHORT_QUANTUM, (U + nwg * NW - 1) / (nwg * NW)) * NW;
+  const u32 wg_units = max(1u, (U + nwg * NW - 1) / (nwg * NW)) * NW;
   if (whole ? wg >= U : wg * wg_units >= U) return;
   if (threadIdx.x < 2) sh.last[threadIdx.x] = sh.need[threadIdx.x] = 0;
   typedef const __attribute__((address_space(4))) u32 const_u32;
@@ -555,13 +586,13 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   Pair cur = pair_at(whole ? wg : wg * wg_units);
   u32 wg0 = wg * wg_units, wg1 = min(wg0 + wg_units, U), from = 0;         // from: the first workgroup of the pair (whole pairs)
   if (whole) {
-    const u32 per = (cur.nv + CAP - 1) / CAP;
+    const u32 per = (cur.nv + cap - 1) / cap;
     from = scalar(sh.pre[cur.s]) + cur.g * per;
     wg0 = cur.nv * (wg - from) / per; wg1 = cur.nv * (wg - from + 1) / per;
   }
   const u32 quantum = (wg1 - wg0 + NW - 1) / NW, u0 = min(wg0 + w * quantum, wg1), u1 = min(u0 + quantum, wg1);
   auto first_wg = [&](const Pair& p) { return whole ? from : p.first / wg_units; };
-  auto n_wgs = [&](const Pair& p) { return whole ? (p.nv + CAP - 1) / CAP : (p.first + p.nv - 1) / wg_units - p.first / wg_units + 1; };
+  auto n_wgs = [&](const Pair& p) { return whole ? (p.nv + cap - 1) / cap : (p.first + p.nv - 1) / wg_units - p.first / wg_units + 1; };
   const TileLane at = Tile::lane_offsets();
   typename Tile::Query q[CT];
   i32 qpos[CT];                                      // position of the lane's row (no row: before every key)
