@@ -8,10 +8,11 @@
 // them are the columns of the matrix products S[key][row] = K q and O^T[dim][row] = V^T P^T; the accumulator of S (column = lane % 16, keys
 // 4 (lane / 16) + i) is the operand P^T as it stands. With a 4-bit cache few rows' scores are products of the codes themselves
 // (v_mfma_scale_f32_16x16x128_f8f6f4, which takes a scale per 32 of them as they are stored): the query is the exact sum of three
-// e4m3 numbers of four bits each, so three such products give what one with converted keys would, and the vector instructions that converted them, which
-// bound the kernel, are gone. Of the values a lane holds 8 neighbouring dimensions of 4 keys, so a register pair of
-// the converted values is two dimensions of one key, and each of the two products that take it has zeros for the other one's dimension
-// in its P: twice the matrix instructions, which decode has to spare, in place of exchanging halves between registers, which it has not.
+// e4m3 numbers of four bits each, so three such products give what one with converted keys would, and the vector instructions that
+// converted them, which bound the kernel, are gone. Of the values a lane holds 8 neighbouring dimensions of 4 keys, so a register
+// pair of the converted values is two dimensions of one key, and each of the two products that take it has zeros for the other
+// one's dimension in its P: twice the matrix instructions, which decode has to spare, in place of exchanging halves between registers,
+// which it has not.
 #pragma once
 #include "attention_mfma.h"
 #include "kv_store.h"
@@ -495,15 +496,22 @@ __device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqVie
 
 __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { return a.out_tbs ? a.out + packed_off(tok, k, a.out_tbs) : a.out + (u64)tok * a.os + k; }
 
+// Bound by bytes where there are many: 256 sequences of up to 1028 visible keys (8 kv heads of 128, halves) 574 MB in 122 us, 4.7 TB/s,
+// 1.05 GB of long contexts 5.6; 128 sequences of 3000 to 16384 in 4 bits 1.10 GB in 207 us, 5.3 TB/s. What is left of
+// 6.3 is the start (7 us to the first tile: lengths, ids, tile, one after the other), the end (8 us: a workgroup's results joined and
+// handed on) and XCDs that are up to a tenth slower than others, another one in every launch. Few keys are bound by those latencies.
+//
 // All tiles of all (sequence, kv head) pairs are one line of units, cut into equal runs, one per wave: whatever the lengths, every
 // wave reads the same number of bytes, with NT tiles on their way, and waits for nobody until its run ends.
 // A pair inside a run is finished where it is. One that several waves of a workgroup share is added up by the wave it begins in (in
-// LDS, after the one barrier); of one that several workgroups share, each adds up its waves' results and leaves one in the workspace, and
-// the workgroup that comes last adds those up, its waves a part of the dimensions each. Of more than SHORT_GROUP such results, those of every SHORT_GROUP workgroups are added up
-// by the last of these first (65531 keys of one sequence, 4-bit, 171 results a pair: 53 us in one go). All sums in the order of the
-// runs: results do not depend on who comes when.
-// Few short pairs (half as many as workgroups, eight tiles a wave) are dealt out whole instead, a workgroup or several to each: up to that
-// length no result then crosses workgroups, which would take longer than the tiles do.
+// LDS, after the one barrier); of one that several workgroups share, each adds up its waves' results and leaves one in the
+// workspace, and the workgroup that comes last adds those up, its waves a part of the dimensions each. Of more than SHORT_GROUP such
+// results, those of every SHORT_GROUP workgroups are added up by the last of these first: of one sequence of 65531 keys in 4
+// bits, 128 results a pair, 53 us in one go, 24 in groups of 16 or 8; of 16384 keys, 32 results, 20.6, 18.1 and 16.3. All sums in the
+// order of the runs: results do not depend on who comes when.
+// Few short pairs (half as many as workgroups) are dealt out whole instead, a workgroup or several to each, 32 to 64 tiles a
+// workgroup: 3 sequences of 100 keys 8.4 us and not 18, 12 of 1500 20 and not 23, 48 x 5 drafted tokens 20 and not 26. With up to 32 tiles one
+// workgroup has a pair for itself: two, of 16 sequences of 500 keys in 4 bits, take 12.0 us in place of 11.3.
 // The loop over tiles is written out NT times for its registers, so all that is rare stands outside of it, once.
 #define SHORT_GROUP 8u
 // 32-bit counters of a launch of nwg workgroups (pairs; two for the prompt part; groups) and floats of its results
@@ -804,12 +812,19 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 
 // ---- many rows: prompts and their chunks -------------------------------------------------------------------------------------
 // One workgroup (eight waves of CT tiles of 16 rows) per (sequence, kv head, 128 CT rows): keys and values come once per workgroup, 64
-// keys a step, into a ring in LDS that every wave reads its operands from (order in LDS, products and why: attn_prompt). Halves are
-// fetched straight into the ring, three steps ahead. 4-bit tiles come into registers a step ahead, and half of the
-// waves each turn keys and values into halves in that same order, so that a value is converted once per workgroup and not once per wave.
+// keys a step, into a ring in LDS that every wave reads its operands from (order in LDS: attn_prompt). Halves are fetched straight
+// into the ring, keys by waves 0-3 and values by waves 4-7, three and two steps ahead. 4-bit tiles come into registers a step ahead,
+// and the same waves turn keys and values into halves in that same order, so that a value is converted once per workgroup.
+// Waves 4-7 are half a step behind waves 0-3 (a barrier more at the start, one less at the end): of the two waves of a SIMD one has
+// its products, those of the last step's probabilities with the values and this step's scores, while the other one has its softmax. Operands come
+// PROMPT_PIPE - 1 groups ahead. What stands between is kept short: a step's 40 scalar instructions for block ids, bounds and addresses cost a tenth of the time when they
+// were 120, and block ids on their way (scalar loads, the same counter as LDS) make every wait for an operand one for them.
 // The keys of a step: those of the sinks, then from the first one that the item's first query sees to the last one of its last; a
-// wave skips the steps that none of its own rows see. Items come from a counter, the last queries first. With fewer items than workgroups the
-// keys of each are cut into parts, whose results a second kernel adds up.
+// wave skips the steps that none of its own rows see. Items come from a counter, the last queries first, each asked for an item
+// ahead. With fewer items than workgroups the keys of each are cut into parts, whose results a second kernel adds up.
+// Bound by the instructions of the softmax (32 exponentials and 87 others a lane and step) and the products in turn: 2048 queries at 16384 keys
+// in 4 bits (32 q, 8 kv heads of 128) 560 us, 0.92 PFLOP/s, where the library's largest products reach 1.08; two prompts of 4000
+// behind a window of 1024 168 us, 0.70 PFLOP/s: an item is 17 steps, and its start (queries, ids, the first tiles) and end another 4.
 #define PROMPT_CT 2u
 #define PROMPT_PIPE 3             // groups of operands on their way from LDS and in use
 #define PROMPT_ROWS (128u * PROMPT_CT)

@@ -3,11 +3,14 @@
 #pragma once
 #include "paged_attention.h"
 
-// Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold), and tiles of keys on their way
+// Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold; 8 sequences of 4000 keys with 32
+// rows take 30 us and 60 as prompts, 30 of 2000 in 4 bits with 40 rows 24 and 47), and tiles of keys on their way (two where there are
+// more rows: registers; 4 bits with three 122 us, with two 124)
 #define SHORT_MORE(HD) ((HD) == 64 ? 4 : 2)
 #define SHORT_AHEAD(HD, BITS, CT) ((CT) > 1 ? 2 : (HD) == 128 || (BITS) == 4 ? 3 : 4)
 #define PAGED_BOUNDS __launch_bounds__(512) __attribute__((amdgpu_num_vgpr(120)))       // (see PHASE_KERNEL8)
-// One row tile over a 4-bit cache is bound by instructions: three workgroups of four waves on a compute unit, else one of eight
+// One row tile over a 4-bit cache is bound by instructions: three workgroups of four waves on a compute unit, else one of eight (128
+// sequences of 4096 keys, heads of 128: 122 us and not 131; of 64: 87 and not 100)
 #define SHORT_SMALL(BITS, CT) ((BITS) == 4 && (CT) == 1)
 #define SHORT_WAVES(BITS, CT) (SHORT_SMALL(BITS, CT) ? 4 : 8)
 #define SHORT_PER_CU(BITS, CT) (SHORT_SMALL(BITS, CT) ? 3 : 1)
