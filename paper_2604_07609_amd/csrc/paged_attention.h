@@ -824,7 +824,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 // ahead. With fewer items than workgroups the keys of each are cut into parts, whose results a second kernel adds up.
 // Bound by the instructions of the softmax (32 exponentials and 87 others a lane and step) and the products in turn: 2048 queries at 16384 keys
 // in 4 bits (32 q, 8 kv heads of 128) 560 us, 0.92 PFLOP/s, where the library's largest products reach 1.08; two prompts of 4000
-// behind a window of 1024 168 us, 0.70 PFLOP/s: an item is 17 steps, and its start (queries, ids, the first tiles) and end another 4.
+// behind a window of 1024 165 us, 0.71 PFLOP/s: an item is 17 steps, and its start (queries, ids, the first tiles) and end another 3.
 #define PROMPT_CT 2u
 #define PROMPT_PIPE 3             // groups of operands on their way from LDS and in use
 #define PROMPT_ROWS (128u * PROMPT_CT)
@@ -836,21 +836,22 @@ struct PromptShared {
   // the item after this one, and whether some step of it had values that are not finite: by the item's number among the workgroup's, so that no
   // wave has to wait at its end for those that read them
   u32 next_item[2], strange[3];
+  SeqView view[PAGED_MAX_SEQS];      // (an item begins without asking memory for them: two prompts of 4000 behind a window, four items a workgroup: 169 us -> 165)
 };
-__device__ __forceinline__ u32 prompt_items(const PagedArgs& a, u32 s) {
-  const SeqView v = seq_view(a, s);
+__device__ __forceinline__ u32 prompt_items(const PagedArgs& a, const SeqView& v) {
   return v.n * a.G <= a.short_rows ? 0u : (v.n * a.G + PROMPT_ROWS - 1) / PROMPT_ROWS;
 }
 // parts of every item's keys: as many as there are workgroups for
 __device__ __forceinline__ u32 prompt_parts(const PagedArgs& a, u32 items, u32 nwg) { return items && items < nwg ? max(1u, min(a.n_splits, nwg / items)) : 1u; }
 
 struct PromptItem { u32 s, g, r0, rows, t0; i32 p0, p1; };   // rows r0 .. r0 + rows of the sequence's, queries at positions p0 .. p1
-__device__ __forceinline__ PromptItem prompt_item(const PagedArgs& a, const u32* pre, u32 item) {
+template <typename F>
+__device__ __forceinline__ PromptItem prompt_item(const PagedArgs& a, const u32* pre, u32 item, F view) {
   PromptItem it;
   const u32 gi = pre[a.n_seqs] - 1 - item / a.nkv;             // the last queries (the longest walks) first
   it.g = item % a.nkv;
   it.s = last_at_most(pre, a.n_seqs, gi);
-  const SeqView v = seq_view(a, it.s);
+  const SeqView v = view(it.s);
   it.r0 = (gi - pre[it.s]) * PROMPT_ROWS;
   it.rows = min(PROMPT_ROWS, v.n * a.G - it.r0);
   it.t0 = v.t0;
@@ -898,7 +899,10 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
   constexpr int CT = PROMPT_CT;
   constexpr u32 BLK = 16 * HD * 2, NB = 4, STAGE = 2 * NB * BLK, NS = BITS == 4 ? 2 : (PROMPT_RING / STAGE > 6 ? 6 : PROMPT_RING / STAGE), TPW = BLK / 1024;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
-  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return prompt_items(a, s); });
+  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) {
+    sh.view[s] = seq_view(a, s);
+    return prompt_items(a, sh.view[s]);
+  });
   const u32 items = (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]) * a.nkv, parts = prompt_parts(a, items, nwg), total = items * parts;
   u32* const ctr = a.ctr + (u64)a.n_seqs * a.nkv;
   const u32 lds0 = (u32)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sh.ring;
@@ -935,7 +939,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
       sh.strange[(nth + 1) % 3] = 0;                            // (read last two items ago)
     }
     const u32 this_turn = turn, item = turn / parts, part = turn - item * parts;
-    PromptItem it = prompt_item(a, sh.pre, item);
+    PromptItem it = prompt_item(a, sh.pre, item, [&](u32 s) { return sh.view[s]; });
     it.s = (u32)__builtin_amdgcn_readfirstlane(it.s); it.g = (u32)__builtin_amdgcn_readfirstlane(it.g); it.r0 = (u32)__builtin_amdgcn_readfirstlane(it.r0);
     it.rows = (u32)__builtin_amdgcn_readfirstlane(it.rows); it.t0 = (u32)__builtin_amdgcn_readfirstlane(it.t0);
     it.p0 = __builtin_amdgcn_readfirstlane(it.p0); it.p1 = __builtin_amdgcn_readfirstlane(it.p1);
@@ -1274,12 +1278,12 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
 struct PromptMergeShared { u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES]; };
 template <int HD>
 __device__ __forceinline__ void prompt_merge(const PagedArgs& a, PromptMergeShared& sh, u32 wg, u32 nwg, u32 nwg_prompt) {
-  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return prompt_items(a, s); });
+  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return prompt_items(a, seq_view(a, s)); });
   const u32 items = sh.pre[a.n_seqs] * a.nkv, parts = prompt_parts(a, items, nwg_prompt), lane = threadIdx.x & 63;
   if (parts < 2) return;
   for (u32 i = wg * PAGED_WAVES + (threadIdx.x >> 6); i < items * PROMPT_ROWS; i += nwg * PAGED_WAVES) {
     const u32 item = i / PROMPT_ROWS, r = i % PROMPT_ROWS;
-    const PromptItem it = prompt_item(a, sh.pre, item);
+    const PromptItem it = prompt_item(a, sh.pre, item, [&](u32 s) { return seq_view(a, s); });
     if (r >= it.rows) continue;
     const float* const base = a.prompt_part + (u64)item * parts * PROMPT_SLOT(HD);
     float M = -INFINITY, L = 0.f, O[HD / 64];
