@@ -816,14 +816,15 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 // into the ring, keys by waves 0-3 and values by waves 4-7, three and two steps ahead. 4-bit tiles come into registers a step ahead,
 // and the same waves turn keys and values into halves in that same order, so that a value is converted once per workgroup.
 // Waves 4-7 are half a step behind waves 0-3 (a barrier more at the start, one less at the end): of the two waves of a SIMD one has
-// its products, those of the last step's probabilities with the values and this step's scores, while the other one has its softmax. Operands come
-// PROMPT_PIPE - 1 groups ahead. What stands between is kept short: a step's 40 scalar instructions for block ids, bounds and addresses cost a tenth of the time when they
-// were 120, and block ids on their way (scalar loads, the same counter as LDS) make every wait for an operand one for them.
+// its products, those of the last step's probabilities with the values and this step's scores, while the other one has its
+// softmax. Operands come PROMPT_PIPE - 1 groups ahead. What stands between is kept short: a step's 40 scalar instructions for
+// block ids, bounds and addresses cost a tenth of the time when they were 120, and block ids on their way (scalar loads, the
+// same counter as LDS) make every wait for an operand one for them.
 // The keys of a step: those of the sinks, then from the first one that the item's first query sees to the last one of its last; a
 // wave skips the steps that none of its own rows see. Items come from a counter, the last queries first, each asked for an item
 // ahead. With fewer items than workgroups the keys of each are cut into parts, whose results a second kernel adds up.
-// Bound by the instructions of the softmax (32 exponentials and 87 others a lane and step) and the products in turn: 2048 queries at 16384 keys
-// in 4 bits (32 q, 8 kv heads of 128) 560 us, 0.92 PFLOP/s, where the library's largest products reach 1.08; two prompts of 4000
+// Bound by the instructions of the softmax (32 exponentials and 87 others a lane and step) and the products in turn: 2048 queries at
+// 16384 keys in 4 bits (32 q, 8 kv heads of 128) 560 us, 0.92 PFLOP/s, where the library's largest products reach 1.08; two prompts of 4000
 // behind a window of 1024 165 us, 0.71 PFLOP/s: an item is 17 steps, and its start (queries, ids, the first tiles) and end another 3.
 #define PROMPT_CT 2u
 #define PROMPT_PIPE 3             // groups of operands on their way from LDS and in use
@@ -915,8 +916,8 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
   const u32 k_at[2] = {(lc >> 3) * BLK + lg * 256 + (lc >> 3) * 128 + (lc & 7) * 16, (lc >> 3) * BLK + lg * 256 + ((lc >> 3) ^ 1u) * 128 + (lc & 7) * 16};
   const u32 v_at = NB * BLK + (lg >> 1) * BLK + (lg & 1) * 256 + lc * 16;
   // A lane's places in a 4-bit record, and where its four dimensions of 8 values (tokens 8 th ..) lie in a block of the ring: it writes them in
-  // an order of its own (x ^ turn, with the bytes of `pick` and `odd`), so that 16 lanes write to all banks at a time (all in one order they meet in an
-  // eighth of them: a third of the kernel's LDS time)
+  // an order of its own (x ^ turn4, with the bytes of `pick` and `odd`), so that 16 lanes write to all banks at a time (all in one
+  // order they meet in an eighth of them: two fifths of the kernel's LDS cycles)
   const u32 vl = HD == 128 ? lane >> 1 & 15 : lc, vh = HD == 128 ? lane & 1 : 0u, th = HD == 128 ? lane >> 5 : lg & 1, turn4 = HD == 128 ? vl >> 1 & 3 : vl >> 2 & 3;
   const u32 d4 = HD == 128 ? vl * 8 + vh * 4 : vl * 4;
   const TileLane at4 = {opaque(k_tok * (HD / 2) + lg * 4), opaque((th * 32 + vl) * (HD / 8)), opaque(k_tok), opaque(vl / (HD == 128 ? 4 : 8) * 16 + th * 8)};
@@ -1136,7 +1137,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
     };
     bool scored = false;                                       // of the step before: probabilities that wait for their values
     for (u32 s = s_lo;; ++s) {
-      u32 bad = 0;
+      u32 bad = 0;                                             // (asked first: a loop that begins with its products is turned around by the compiler, which then spills)
       if (s < s_hi) bad = bad_ahead >> (4 * (BITS == 16 ? ahead : 1u)) & 15u;
       if (scored) {
 #pragma unroll
@@ -1168,48 +1169,48 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
       // (asked for here: with them on their way a wait for an operand from LDS would be one for them too)
       next_ids(s + (BITS == 16 ? ahead + 1 : 2u));
       if (scored) {
-      const bool edge = edge_of(k0, bad);
-      if (edge) {
-        asm volatile("" ::: "memory");                         // (a branch: few steps are)
+        const bool edge = edge_of(k0, bad);
+        if (edge) {
+          asm volatile("" ::: "memory");                         // (a branch: few steps are)
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            u32 vis = 0;                                         // bit 8 h + i: this lane's row sees its key i of the step's pair of blocks h
+#pragma unroll
+            for (u32 h = 0; h < NB / 2; ++h)
+              if (!(bad >> (NB - 1 - (2 * h + (lg >> 1))) & 1u)) vis |= sees(a, qpos[c], (i32)(k0 + h * 32 + lg * 8)) << (8 * h);
+#pragma unroll
+            for (u32 b = 0; b < NB; ++b)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) sc[c][b][i] = vis >> (b * 4 + i) & 1u ? sc[c][b][i] : -INFINITY;
+          }
+        }
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-          u32 vis = 0;                                         // bit 8 h + i: this lane's row sees its key i of the step's pair of blocks h
+          float top = -INFINITY;
 #pragma unroll
-          for (u32 h = 0; h < NB / 2; ++h)
-            if (!(bad >> (NB - 1 - (2 * h + (lg >> 1))) & 1u)) vis |= sees(a, qpos[c], (i32)(k0 + h * 32 + lg * 8)) << (8 * h);
+          for (u32 b = 0; b < NB; ++b) top = fmaxf(top, fmaxf(fmaxf(sc[c][b][0], sc[c][b][1]), fmaxf(sc[c][b][2], sc[c][b][3])));
+          top *= a.c;
+          if (__ballot(top > m[c] + 8.f)) {
+            top = quad_max(top);
+            const float mn = fmaxf(m[c], top);
+            const float f = mn == m[c] || m[c] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[c] - mn);
+            l[c] *= f;
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) o[c][d] *= f;
+            m[c] = mn;
+          }
+          const float nm = m[c] == -INFINITY ? 0.f : -m[c];
+          float ps = 0.f;
 #pragma unroll
           for (u32 b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sc[c][b][i] = vis >> (b * 4 + i) & 1u ? sc[c][b][i] : -INFINITY;
+            for (int i = 0; i < 4; ++i) {
+              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][b][i], a.c, nm));
+              ps += p;
+              pb[c][b / 2][(b & 1) * 4 + i] = (_Float16)p;
+            }
+          l[c] += ps;
         }
-      }
-#pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        float top = -INFINITY;
-#pragma unroll
-        for (u32 b = 0; b < NB; ++b) top = fmaxf(top, fmaxf(fmaxf(sc[c][b][0], sc[c][b][1]), fmaxf(sc[c][b][2], sc[c][b][3])));
-        top *= a.c;
-        if (__ballot(top > m[c] + 8.f)) {
-          top = quad_max(top);
-          const float mn = fmaxf(m[c], top);
-          const float f = mn == m[c] || m[c] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[c] - mn);
-          l[c] *= f;
-#pragma unroll
-          for (int d = 0; d < HD / 16; ++d) o[c][d] *= f;
-          m[c] = mn;
-        }
-        const float nm = m[c] == -INFINITY ? 0.f : -m[c];
-        float ps = 0.f;
-#pragma unroll
-        for (u32 b = 0; b < NB; ++b)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][b][i], a.c, nm));
-            ps += p;
-            pb[c][b / 2][(b & 1) * 4 + i] = (_Float16)p;
-          }
-        l[c] += ps;
-      }
       }
       if constexpr (BITS == 16) {
         fetch_from(s + 1 + ahead);
