@@ -824,7 +824,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 // wave skips the steps that none of its own rows see. Items come from a counter, the last queries first, each asked for an item
 // ahead. With fewer items than workgroups the keys of each are cut into parts, whose results a second kernel adds up.
 // Bound by the instructions of the softmax (32 exponentials and 87 others a lane and step) and the products in turn: 2048 queries at
-// 16384 keys in 4 bits (32 q, 8 kv heads of 128) 560 us, 0.92 PFLOP/s, where the library's largest products reach 1.08; two prompts of 4000
+// 16384 keys in 4 bits (32 q, 8 kv heads of 128) 549 us, 0.94 PFLOP/s, where the library's largest products reach 1.08; two prompts of 4000
 // behind a window of 1024 165 us, 0.71 PFLOP/s: an item is 17 steps, and its start (queries, ids, the first tiles) and end another 3.
 #define PROMPT_CT 2u
 #define PROMPT_PIPE 3             // groups of operands on their way from LDS and in use
@@ -1036,34 +1036,33 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
       }
       note_bad();
     };
-    auto convert4 = [&](u32 s) {                     // what fetch4 brought, as halves into the ring
+    auto convert4 = [&](u32 s, u32 half) {           // half of what fetch4 brought, as halves into the ring
       unsigned char* const st = sh.ring + (s % NS) * STAGE;
       if (fk) {
         unsigned char* const to = st + fb * BLK + lane * 16;
 #pragma unroll
-        for (u32 r = 0; r < HD / 32; ++r) {
+        for (u32 r = half * (HD / 64); r < (half + 1) * (HD / 64); ++r) {
           const float sc = __uint_as_float(raw_s[r] << 23);
           *(uint4*)(to + r * 1024) = make_uint4(f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[r], sc, 0)), f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[r], sc, 1)),
                                                 f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[r], sc, 2)), f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[r], sc, 3)));
         }
       } else if (HD == 128 || lane < 32) {
         // a lane: 8 tokens x 4 dimensions (of heads of 128 the lower or upper 4 of 8)
-        u32 pr[8][2];                                // [token][pair of dimensions]
+        u32 pr[8];                                   // [token], a pair of dimensions
 #pragma unroll
         for (u32 i = 0; i < 8; ++i) {
           const float sc = __uint_as_float((raw_s[i / 4] >> (8 * (i % 4)) & 0xFFu) << 23);
           const u32 r = HD == 128 ? raw[i] : raw[i / 2], x = __builtin_amdgcn_perm(0u, r, HD == 64 && i & 1 ? pick + 0x0202u : pick);
-          pr[i][0] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 0));
-          pr[i][1] = f16x2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 1));
+          pr[i] = f16x2_bits(half ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 1) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, sc, 0));
         }
         unsigned char* const to = st + (NB + fb) * BLK;
 #pragma unroll
-        for (u32 x = 0; x < 4; ++x) {
+        for (u32 x = 0; x < 2; ++x) {
           const u32 sel = (x & 1 ? 0x07060302u : 0x05040100u) ^ odd;
           u32 v[4];
 #pragma unroll
-          for (u32 i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(pr[2 * i + 1][x / 2], pr[2 * i][x / 2], sel);
-          *(uint4*)(to + (to4 ^ x * 16)) = make_uint4(v[0], v[1], v[2], v[3]);
+          for (u32 i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(pr[2 * i + 1], pr[2 * i], sel);
+          *(uint4*)(to + (to4 ^ (2 * half + x) * 16)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
       }
     };
@@ -1095,10 +1094,12 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
     } else {
       next_ids(s_lo);
       fetch4();
-      convert4(s_lo);
+      convert4(s_lo, 0);
+      convert4(s_lo, 1);
       take_strange_out(s_lo, bad_ahead & 15u);
       next_ids(s_lo + 1);
       fetch4();
+      next_ids(s_lo + 2);
     }
     if (threadIdx.x == 0) sh.next_item[nth & 1] = after;
     lds_barrier();
@@ -1166,8 +1167,14 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
         }
       }
       lds_barrier();
+      if constexpr (BITS == 4) {                               // (behind the softmax, the barrier waits for these writes: 566 us and not 549)
+        convert4(s + 1, 0);
+        convert4(s + 1, 1);
+        take_strange_out(s + 1, bad_ahead & 15u);
+        fetch4();
+      }
       // (asked for here: with them on their way a wait for an operand from LDS would be one for them too)
-      next_ids(s + (BITS == 16 ? ahead + 1 : 2u));
+      next_ids(s + (BITS == 16 ? ahead + 1 : 3u));
       if (scored) {
         const bool edge = edge_of(k0, bad);
         if (edge) {
@@ -1215,10 +1222,6 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
       if constexpr (BITS == 16) {
         fetch_from(s + 1 + ahead);
         if (fk) wait_dma<(int)((NS - 2) * TPW)>();               // this wave's keys of the next step
-      } else {
-        convert4(s + 1);
-        take_strange_out(s + 1, bad_ahead & 15u);
-        fetch4();
       }
       lds_barrier();
     }
