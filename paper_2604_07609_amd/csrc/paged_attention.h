@@ -191,7 +191,11 @@ struct CacheTile<HD, 4> {
 #pragma unroll
     for (int h = 0; h < HD / 64; ++h)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) load_n<_Float16, 8>((const _Float16*)row + h * 64 + lg * 16 + i * 8, x + h * 16 + i * 8);
+      for (int i = 0; i < 2; ++i) {
+        const f16x8_t y = ld_tile(row + h * 64 + lg * 16 + i * 8);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[h * 16 + i * 8 + j] = (float)y[j];
+      }
     u32 top = 0;
 #pragma unroll
     for (int i = 0; i < HD / 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
