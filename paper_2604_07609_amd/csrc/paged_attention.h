@@ -532,13 +532,14 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     sh.pos0[s] = v.pos0; sh.n[s] = n ? (unsigned char)v.n : (unsigned char)0;
     return n;
   };
-  // Pairs dealt out whole: `cap` tiles of one at most to a workgroup, as few as there are workgroups for, but 32; then `pre` counts
-  // workgroups, else units.
+  // Pairs dealt out whole: `cap` tiles of one at most to a workgroup, as few as there are workgroups for, but 32, and more (up to 64)
+  // where results would be more than groups of groups take (65531 keys in 4 bits: 21.9 us with 64 results a pair, 23.2 with 128; 16384
+  // keys: 19.3 with 16, 16.5 with 32). Then `pre` counts workgroups, else units.
   const u32 pairs = a.n_seqs * a.nkv;
   u32 U, cap;
   bool whole;
   auto choose = [&](u32 units, u32 of) {             // (of = nwg - pairs: these are always enough)
-    cap = pairs <= nwg / 2 ? max(32u, (units + of - 1) / of) : ~0u;
+    cap = pairs <= nwg / 2 ? max(max(32u, (units + of - 1) / of), min(64u, units / (pairs * (SHORT_GROUP * SHORT_GROUP)))) : ~0u;
     whole = cap <= 64;
   };
   if (a.n_seqs <= 64) {                              // every wave for itself, all the same: nobody waits
