@@ -381,7 +381,8 @@ int blink_kv_cache_read(int32_t device, const blink_kv_cache* cache, const int32
  * max_q: no sequence has more queries than this (further ones are not computed). Single tokens, drafts and prompts may be mixed; calls whose
  * sequences have few queries (max_q n_q_heads / n_kv_heads <= 16) are the fastest for those. Rows of `out` that no sequence has stay as they are.
  * Block ids outside the cache: their keys are not seen. Results do not depend on how the work falls on the chip.
- * The workspace holds zeros before its first call and is left so that the next one can use it; two calls that may run at the same time (two
+ * The first 8 KiB of the workspace hold zeros before its first call, and again after every one; what is behind them does not matter. So calls of any
+ * shapes, caches and heads can share a workspace that is large enough for each of them, one after the other; two that may run at the same time (two
  * streams, two graphs in flight) need one each. BLINK_ERR_TOO_LARGE with more than 1024 sequences, or 2^31 blocks of keys. */
 typedef struct {
   blink_kv_cache cache;

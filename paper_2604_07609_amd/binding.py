@@ -245,7 +245,8 @@ def kv_cache_read(cache, slots, k_out, v_out, stream=0):
 
 
 def attention_workspace_bytes(n_q_heads, cache, n_seqs, max_q=1):
-    """Bytes of the workspace of paged_attention for up to n_seqs sequences of up to max_q queries. It holds zeros before its first call."""
+    """Bytes of the workspace of paged_attention for up to n_seqs sequences of up to max_q queries. Its first 8 KiB hold zeros
+    before its first call; calls of any shapes may share one in turn."""
     lib, n = load_library(), C.c_uint64()
     _check(lib, lib.blink_attention_workspace_bytes(cache.device, C.byref(cache.desc), n_q_heads, n_seqs, max_q, C.byref(n)))
     return n.value

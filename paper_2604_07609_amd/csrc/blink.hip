@@ -723,7 +723,7 @@ static int init_impl(const blink_config* cfg, const blink_attention_options& opt
   }
   if (c.paged) {
     if (int rc = dalloc(e, &c.qkv, (u64)c.maxT * c.qkv_n, false)) return rc;
-    if (int rc = dalloc(e, &c.paged_ctr, paged_counters((u64)c.max_batch * c.nkv, (u32)e->n_cu))) return rc;
+    if (int rc = dalloc(e, &c.paged_ctr, paged_counters((u32)e->n_cu))) return rc;
     if (int rc = dalloc(e, &c.paged_part, short_floats((u32)e->n_cu, c.hd, SHORT_MORE(c.hd)), false)) return rc;
   }
   if (int rc = dalloc(e, &e->calib_src, e->calib_bytes)) return rc;

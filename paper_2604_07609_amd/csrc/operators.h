@@ -115,13 +115,18 @@ extern "C" int blink_kv_cache_read(int32_t device, const blink_kv_cache* c, cons
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------
+// The workspace: the counters, then results of the short part, then those of the prompt part. The counters are zeros between calls and results
+// are anything, so where the ones end must be the same in every call, whatever its batch, heads, bits and plan: the counters of
+// the launch with the most workgroups, in whole 8 KiB.
+static u64 paged_ctr_bytes(u32 n_cu) { return (paged_counters(n_cu * SHORT_PER_CU(4, 1)) * 4ull + 8191) / 8192 * 8192; }
 // Which kernels a call takes, from what the host knows: its longest run of queries, and not which sequences have it.
 struct PagedPlan {
   u32 ct;                 // row tiles of the short part (0: there is none)
   u32 short_rows;         // sequences with at most so many rows are its
   bool prompt;            // there is a prompt part (with a short one: in one launch)
   u32 wgs, threads, n_splits;
-  u64 ctr_bytes, part_bytes, prompt_bytes;
+  u64 part_bytes, prompt_bytes;
+  u64 bytes(u32 n_cu) const { return paged_ctr_bytes(n_cu) + part_bytes + prompt_bytes; }
 };
 static PagedPlan paged_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_seqs, u32 n_tokens, u32 max_q, u32 key_steps, u32 n_cu) {
   PagedPlan p{};
@@ -139,7 +144,6 @@ static PagedPlan paged_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_seqs, u32 n
   // part 212; parts of 128 gain nothing and need twice the adding up)
   const bool few = (u64)n_tokens * G / PROMPT_ROWS * nkv < p.wgs;
   p.n_splits = p.prompt && few ? std::max(1u, key_steps / 4) : 1u;
-  p.ctr_bytes = (paged_counters((u64)n_seqs * nkv, p.wgs) * 4 + 255) / 256 * 256;
   p.part_bytes = p.ct ? short_floats(p.wgs, hd, p.ct) * 4 : 0;
   p.prompt_bytes = p.prompt ? (u64)p.wgs * PROMPT_SLOT(hd) * 4 : 0;
   return p;
@@ -162,7 +166,7 @@ extern "C" int blink_attention_workspace_bytes(int32_t device, const blink_kv_ca
   const PagedPlan p = paged_plan(c->head_dim, c->bits, n_q_heads, c->n_kv_heads, n_seqs, 0, max_q, 1, n_cu);
   const u32 one = n_cu * SHORT_PER_CU(c->bits, 1), more = SHORT_MORE(c->head_dim);
   const u64 least = std::max(short_floats(one, c->head_dim, 1), short_floats(n_cu, c->head_dim, more)) * 4;
-  *bytes = (paged_counters((u64)n_seqs * c->n_kv_heads, one) * 4 + 255) / 256 * 256 + std::max(p.part_bytes + p.prompt_bytes, least);
+  *bytes = std::max(p.bytes(n_cu), paged_ctr_bytes(n_cu) + least);
   return BLINK_OK;
 }
 
@@ -195,8 +199,8 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   const u64 reach = a->window ? (u64)a->window + a->max_q + a->sinks : ~0ull;
   const u32 key_steps = (u32)std::min<u64>(a->max_blocks / 4 + 1, reach / 64 + 3);
   const PagedPlan plan = paged_plan(hd, a->cache.bits, a->n_q_heads, nkv, a->n_seqs, a->n_tokens, a->max_q, key_steps, n_cu);
-  if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.ctr_bytes + plan.part_bytes + plan.prompt_bytes)
-    return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)(plan.ctr_bytes + plan.part_bytes + plan.prompt_bytes));
+  if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.bytes(n_cu))
+    return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)plan.bytes(n_cu));
   OnDevice on(device);
   HIPCHK(on.err);
   PagedArgs p{};
@@ -204,7 +208,7 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   p.tables = (const u32*)a->block_tables; p.cache = a->cache.data; p.n_blocks = a->cache.n_blocks; p.max_blocks = a->max_blocks;
   p.nq = a->n_q_heads; p.nkv = nkv; p.G = p.nq / nkv; p.n_seqs = a->n_seqs; p.n_tokens = a->n_tokens; p.max_q = a->max_q;
   p.window = a->window; p.sinks = a->sinks; p.c = a->scale * 1.44269504088896340736f; p.short_rows = plan.short_rows; p.n_splits = plan.n_splits;
-  p.ctr = (u32*)a->workspace; p.part = (float*)((char*)a->workspace + plan.ctr_bytes); p.prompt_part = p.part + plan.part_bytes / 4;
+  p.ctr = (u32*)a->workspace; p.part = (float*)((char*)a->workspace + paged_ctr_bytes(n_cu)); p.prompt_part = p.part + plan.part_bytes / 4;
   const hipStream_t st = (hipStream_t)stream;
   HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_paged<64, 16>(p, plan, st) : launch_paged<64, 4>(p, plan, st))
                   : (a->cache.bits == 16 ? launch_paged<128, 16>(p, plan, st) : launch_paged<128, 4>(p, plan, st)));

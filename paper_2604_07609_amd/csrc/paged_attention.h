@@ -34,7 +34,7 @@ struct PagedArgs {
   float c;                        // scale of the scores * log2(e)
   u32 short_rows;                 // sequences with at most so many rows are the short part's
   u32 n_splits;                   // most parts of a prompt item's keys
-  u32* ctr;                       // zeros between launches: [n_seqs][nkv] pieces done; then next prompt item, workgroups done
+  u32* ctr;                       // zeros between launches (paged_counters): next prompt item, workgroups done, then the short part's
   float *part, *prompt_part;      // partial results of the short and of the prompt part
 };
 
@@ -518,8 +518,9 @@ __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { r
 // workgroup has a pair for itself: two, of 16 sequences of 500 keys in 4 bits, take 12.0 us in place of 11.3.
 // The loop over tiles is written out NT times for its registers, so all that is rare stands outside of it, once.
 #define SHORT_GROUP 8u
-// 32-bit counters of a launch of nwg workgroups (pairs; two for the prompt part; groups) and floats of its results
-__host__ __device__ __forceinline__ u64 paged_counters(u64 pairs, u32 nwg) { return pairs + 2 + 2 * ((nwg + SHORT_GROUP - 1) / SHORT_GROUP); }
+// 32-bit counters of a launch of nwg workgroups and floats of its results. The counters: two for the prompt part, one per workgroup (of the
+// pair that begins in it and goes on in others: one at most), two per group. They do not depend on the batch.
+__host__ __device__ __forceinline__ u32 paged_counters(u32 nwg) { return 2 + nwg + 2 * ((nwg + SHORT_GROUP - 1) / SHORT_GROUP); }
 __host__ __device__ __forceinline__ u64 short_floats(u32 nwg, u32 hd, u32 ct) { return 2ull * (nwg + (nwg + SHORT_GROUP - 1) / SHORT_GROUP) * ct * (128 + 16 * hd); }
 template <int HD, int BITS, int CT, int NT, int NW>
 __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, CT, NW>& sh, u32 wg, u32 nwg) {
@@ -741,7 +742,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   __syncthreads();
   // pairs that other workgroups share, all waves at each: the one that the run begins inside of (0), the one that begins in it (1)
   const u32 group = wg / SHORT_GROUP, group0 = group * SHORT_GROUP;
-  u32* const group_ctr = a.ctr + (u64)a.n_seqs * a.nkv + 2;
+  u32 *const pair_ctr = a.ctr + 2, *const group_ctr = pair_ctr + nwg;        // (pairs by their first workgroup)
   // a pair's results and those of its groups: which of a workgroup's (group's) two slots, by whether the pair begins before it
   auto piece = [&](u32 x, u32 first) { return a.part + (u64)(2 * x + (x == first ? 1u : 0u)) * short_slot<HD, CT>(); };
   auto group_piece = [&](u32 x, u32 first) { return a.part + (u64)(2 * (nwg + x) + (x == first / SHORT_GROUP ? 1u : 0u)) * short_slot<HD, CT>(); };
@@ -775,7 +776,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     all.leave(a.part + (u64)(2 * wg + which) * short_slot<HD, CT>());
     if (threadIdx.x == 0) {
       const bool grouped = np > SHORT_GROUP;
-      sh.ctr[which] = grouped ? group_ctr + 2 * group + (f >= group0 ? 1u : 0u) : a.ctr + (u64)p.s * a.nkv + p.g;
+      sh.ctr[which] = grouped ? group_ctr + 2 * group + (f >= group0 ? 1u : 0u) : pair_ctr + f;
       sh.need[which] = grouped ? min(f + np, group0 + SHORT_GROUP) - max(f, group0) : np;
     }
   }
@@ -806,7 +807,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
       all.leave(group_piece(group, f));
       asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
       __syncthreads();
-      if (threadIdx.x < 2) count(lane == which, a.ctr + (u64)p.s * a.nkv + p.g, (f + np - 1) / SHORT_GROUP - f / SHORT_GROUP + 1);
+      if (threadIdx.x < 2) count(lane == which, pair_ctr + f, (f + np - 1) / SHORT_GROUP - f / SHORT_GROUP + 1);
       __syncthreads();
       if (!scalar(sh.last[which])) continue;
       all.sum(f / SHORT_GROUP, (f + np - 1) / SHORT_GROUP + 1, rows, [&](u32 x) { return FarResult<HD>{group_piece(x, f)}; });
@@ -910,7 +911,7 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
     return prompt_items(a, sh.view[s]);
   });
   const u32 items = (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]) * a.nkv, parts = prompt_parts(a, items, nwg), total = items * parts;
-  u32* const ctr = a.ctr + (u64)a.n_seqs * a.nkv;
+  u32* const ctr = a.ctr;
   const u32 lds0 = (u32)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sh.ring;
   // fetching halves: waves 0-3 the K of a block each, waves 4-7 the V (places in LDS: attn_prompt)
   const bool fk = w < 4;
