@@ -335,7 +335,8 @@ enum { BLINK_TYPE_FLOAT = 0, BLINK_TYPE_HALF = 1, BLINK_TYPE_BF16 = 2 };
  * [token % 4][head_dim / 32], where the pair (j, m) holds the dimensions 2 (j head_dim / 32 + m) and the next, scales of the keys
  * [head_dim / 32][token], scales of the values [head_dim / 32][token]. A code is an e2m1 number (0 0.5 1 1.5 2 3 4 6, bit 3: the sign),
  * the lower half of a byte the lower dimension. A scale byte is 127 + the exponent of the power of two that 32 neighbouring dimensions of one
- * token share, -23 .. 13 (every value is a half, exactly); 255: not a number. */
+ * token share, -23 .. 13 (every value is a half, exactly); 255: not a number. What other bytes
+ * stand for is not defined: where a query does not see them (memory that nothing was stored in), they do not matter. */
 typedef struct {
   void* data;
   uint32_t n_blocks, n_kv_heads;

@@ -141,8 +141,8 @@ struct CacheTile<HD, 16> {
     const uint2 w = make_uint2(x.w[0], x.w[1]);
     return __builtin_amdgcn_mfma_f32_16x16x16f16(*(const f16x4_t*)&w, p.p, o, 0, 0, 0);
   }
-  // whether some value is not finite (then those are taken out)
-  __device__ __forceinline__ bool take_strange_out() {
+  // whether some value is not finite (then those are taken out); vis: bits of the lane's four keys, seen by the lane's rows
+  __device__ __forceinline__ bool take_strange_out(u32) {
     const float zero[4] = {0.f, 0.f, 0.f, 0.f};
     const Probs none = probs(zero);
     floatx4_t z = floatx4_t{0.f, 0.f, 0.f, 0.f};
@@ -259,8 +259,15 @@ struct CacheTile<HD, 4> {
   static __device__ __forceinline__ floatx4_t product(const Operand& x, const Probs& p, int d, const floatx4_t& o) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(x.w[0], x.w[1], x.w[2], x.w[3]), d & 1 ? p.odd : p.even, o, 0, 0, 0);
   }
-  __device__ __forceinline__ bool take_strange_out() {               // (only a scale of 255 is not a number)
-    const u32 odd = ((vs & 0x7F7F7F7Fu) + 0x01010101u) & vs & 0x80808080u;
+  // (Keys that no row sees, in places that may hold anything, become zeros. With scales from 141 on values leave the halves, and 255 is
+  // not a number: the other scales give finite ones.)
+  __device__ __forceinline__ bool take_strange_out(u32 vis) {
+    vis |= (u32)__builtin_amdgcn_update_dpp(0, (i32)vis, 0x128, 0xF, 0xF, false);      // the 16 lanes of the same keys: row_ror 8, 4, 2, 1
+    vis |= (u32)__builtin_amdgcn_update_dpp(0, (i32)vis, 0x124, 0xF, 0xF, false);
+    vis |= (u32)__builtin_amdgcn_update_dpp(0, (i32)vis, 0x122, 0xF, 0xF, false);
+    vis |= (u32)__builtin_amdgcn_update_dpp(0, (i32)vis, 0x121, 0xF, 0xF, false);
+    vs &= ((vis & 15u) * 0x00204081u & 0x01010101u) * 0xFFu;
+    const u32 odd = ((vs & 0x7F7F7F7Fu) + (0x80u - KV_E_MAX) * 0x01010101u) & vs & 0x80808080u;      // from 128 + KV_E_MAX on
     if (!__ballot(odd != 0)) return false;
     vs &= ~((odd >> 7) * 0xFFu);
     return true;
@@ -686,7 +693,10 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
         u32 vis[CT] = {};
         if (edge) {
           see(k0[j], in_cache[j], vis);
-          strange |= tile[j].take_strange_out();
+          u32 any = 0;
+#pragma unroll
+          for (int c = 0; c < CT; ++c) any |= vis[c];
+          strange |= tile[j].take_strange_out(any);
         }
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[c].add(tile[j], q[c], a.c, edge, vis[c]);
