@@ -136,7 +136,28 @@ struct StoreRow {
       for (u32 o = 1; o < LR; o <<= 1) ss += __shfl_xor(ss, (int)o, (int)LR);
       const F ms = ss * (F)(1.0 / HD) + (F)a.eps;
       F r;
-      if constexpr (sizeof(F) == 8) r = 1.0 / sqrt(ms); else r = 1.0f / sqrtf(ms);
+      if constexpr (sizeof(F) == 8) r = 1.0 / sqrt(ms);
+      else {
+        r = 1.0f / sqrtf(ms);
+        // (squares of floats and bf16 numbers can leave the range, at both ends: such a row is first divided by the power of two of its largest
+        // magnitude 2^e, and eps by 4^e; where that overflows, the row's results are below 2^-64 and zeros as halves)
+        if constexpr (!__is_same(T, _Float16)) {
+          if (!(ms >= 0x1p-90f && ms < INFINITY)) {
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2 * N; ++i) top = fmaxf(top, fabsf(y[i]));
+#pragma unroll
+            for (u32 o = 1; o < LR; o <<= 1) top = fmaxf(top, __shfl_xor(top, (int)o, (int)LR));
+            const i32 e = (i32)(__float_as_uint(top) >> 23) - 127;
+            ss = 0;
+#pragma unroll
+            for (int i = 0; i < 2 * N; ++i) { y[i] = ldexpf(y[i], -e); ss += y[i] * y[i]; }
+#pragma unroll
+            for (u32 o = 1; o < LR; o <<= 1) ss += __shfl_xor(ss, (int)o, (int)LR);
+            r = 1.0f / sqrtf(ss * (1.0f / HD) + ldexpf(a.eps, -2 * e));
+          }
+        }
+      }
 #pragma unroll
       for (int i = 0; i < 2 * N; ++i) y[i] = y[i] * r * (F)g[i];
     }
