@@ -7,8 +7,9 @@
 // Rows of a sequence and kv head are its queries times the G query heads that share the head: row = query * G + head. Sixteen of
 // them are the columns of the matrix products S[key][row] = K q and O^T[dim][row] = V^T P^T; the accumulator of S (column = lane % 16, keys
 // 4 (lane / 16) + i) is the operand P^T as it stands. With a 4-bit cache few rows' scores are products of the codes themselves
-// (v_mfma_scale_f32_16x16x128_f8f6f4, which takes a scale per 32 of them as they are stored): the query is the exact sum of three
-// e4m3 numbers of four bits each, so three such products give what one with converted keys would, and the vector instructions that
+// (v_mfma_scale_f32_16x16x128_f8f6f4, which takes a scale per 32 of them as they are stored): the query is the sum of three e4m3
+// numbers of four bits each, with a scale per 32 dimensions as well: exactly, or (below 2^-14 of the largest of those 32) to within 2^-25 of that
+// largest. So three such products give in 32 bits what one with converted keys would, and the vector instructions that
 // converted them, which bound the kernel, are gone. Of the values a lane holds 8 neighbouring dimensions of 4 keys, so a register
 // pair of the converted values is two dimensions of one key, and each of the two products that take it has zeros for the other
 // one's dimension in its P: twice the matrix instructions, which decode has to spare, in place of exchanging halves between registers,
@@ -180,9 +181,9 @@ struct CacheTile<HD, 4> {
     vs = from_global<u32>(r + at.vs + (16 * HD + HD / 2));
   }
   // The product's B operand holds the elements 16 g .. and 64 + 16 g .. of its 128 in lane group g, its scales (like A's) are those of the
-  // elements 32 g .. in lane group g. Parts: with the row's largest magnitude in [128, 256), e4m3(x), e4m3(16 (x - that)) and so on: each
-  // takes four bits off a half's eleven, down to 2^-26 of the largest. Heads of 64: A holds a key's codes twice, and the
-  // second part meets the upper ones.
+  // elements 32 g .. in lane group g. Parts: with the largest magnitude of 32 dimensions (those that share a scale, as a key's do) in
+  // [128, 256), e4m3(x), e4m3(16 (x - that)) and so on: each takes four bits off a half's eleven, down to 2^-25 of that largest. Heads of
+  // 64: A holds a key's codes twice, and the second part meets the upper ones.
   static constexpr int NP = HD == 128 ? 3 : 2;
   struct Query { i32x8_t part[NP]; u32 scale; };     // scale: byte i for product i
   static __device__ __forceinline__ void load_query(const f16_t* row, Query& r) {
@@ -196,16 +197,20 @@ struct CacheTile<HD, 4> {
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[h * 16 + i * 8 + j] = (float)y[j];
       }
-    u32 top = 0;
+    u32 scale[HD / 64];                                              // of the lane's 16 of the dimensions 64 h .., which two lane groups share
 #pragma unroll
-    for (int i = 0; i < HD / 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-    top = max(top, (u32)__shfl_xor((int)top, 16));
-    top = max(top, (u32)__shfl_xor((int)top, 32));
-    const bool fine = top < 0x7F800000u;
-    const i32 e = top ? (i32)(top >> 23) - 127 - 7 : 0;              // (a half is a normal float)
-    const float up = __uint_as_float((u32)(127 - (fine ? e : 0)) << 23);
+    for (int h = 0; h < HD / 64; ++h) {
+      u32 top = 0;
 #pragma unroll
-    for (int i = 0; i < HD / 4; ++i) x[i] = fine ? x[i] * up : 0.f;
+      for (int i = h * 16; i < h * 16 + 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+      top = max(top, (u32)__shfl_xor((int)top, 16));
+      const bool fine = top < 0x7F800000u;
+      const i32 e = top ? (i32)(top >> 23) - 127 - 7 : 0;            // (a half is a normal float)
+      const float up = __uint_as_float((u32)(127 - (fine ? e : 0)) << 23);
+#pragma unroll
+      for (int i = h * 16; i < h * 16 + 16; ++i) x[i] = fine ? x[i] * up : 0.f;
+      scale[h] = fine ? (u32)(127 + e) : 255u;                       // (with an infinity or NaN: the row's scores are not a number)
+    }
     i32 part[4][HD / 16] = {};
 #pragma unroll
     for (int p = 0; p < 3; ++p) {
@@ -223,8 +228,12 @@ struct CacheTile<HD, 4> {
     for (int p = 0; p < NP; ++p)
 #pragma unroll
       for (int j = 0; j < 8; ++j) r.part[p][j] = HD == 128 ? part[p][j] : part[2 * p + j / 4][j % (HD / 16)];
-    // (a row with an infinity or NaN: its scores are not a number)
-    const u32 s0 = (u32)(127 + e) - (HD == 64 && lg >= 2 ? 4u : 0u);
+    // the scale that this lane group gives: that of dimensions 32 lg .. (heads of 64: 32 (lg % 2) .., of the second part where lg / 2)
+    const int from = (int)((lg & 1) * 32 + (threadIdx.x & 15));
+    u32 s0 = (u32)__shfl((int)scale[0], from);
+    if constexpr (HD == 128) { const u32 s1 = (u32)__shfl((int)scale[1], from); s0 = lg >= 2 ? s1 : s0; }
+    const bool fine = s0 != 255;
+    if (HD == 64 && lg >= 2) s0 -= 4;
     r.scale = !fine ? 0xFFFFFFu : HD == 128 ? s0 | (s0 - 4) << 8 | (s0 - 8) << 16 : s0 | (s0 - 8) << 8;
   }
   __device__ __forceinline__ floatx4_t scores(const Query& r) const {
