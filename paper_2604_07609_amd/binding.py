@@ -2,6 +2,7 @@
 import ctypes as C
 import os
 import struct
+import sys
 
 import numpy as np
 
@@ -191,6 +192,15 @@ def _rows(name, t, shape, device):
     return t.data_ptr(), st[0] if shape[0] > 1 else width
 
 
+def _stream(stream, t, device):
+    """Handle of the stream that a call goes to. None: the one its tensors are used on, torch's current one of the device (the null stream for
+    other libraries' tensors)."""
+    if stream is None:
+        torch = sys.modules.get("torch")
+        return torch.cuda.current_stream(device).cuda_stream if torch and isinstance(t, torch.Tensor) else 0
+    return stream
+
+
 def kv_cache_bytes(n_blocks, n_kv_heads, head_dim, bits=16):
     """Bytes of one layer of a paged cache with `n_blocks` blocks of 16 tokens."""
     lib, n = load_library(), C.c_uint64()
@@ -212,10 +222,10 @@ class KVCache:
         self.n_kv_heads, self.head_dim, self._packed = n_kv_heads, head_dim, (data.data_ptr(), n_blocks, n_kv_heads, head_dim, bits)
 
 
-def qk_norm_rope(q, k, v, positions, slots, rope_table, cache, q_out, q_gain=None, k_gain=None, eps=1e-6, q_scale=1.0, stream=0):
+def qk_norm_rope(q, k, v, positions, slots, rope_table, cache, q_out, q_gain=None, k_gain=None, eps=1e-6, q_scale=1.0, stream=None):
     """blink_qk_norm_rope: q [tokens, q heads, hd], k and v [tokens, kv heads, hd] (float32, float16 or bfloat16, rows may be parts
     of wider ones), int32 positions and slots [tokens], float32 rope_table [rows, hd / 2, 2] -> q_out float16 like q, keys and
-    values into `cache`. Gains: float32 [hd] or None. stream: a stream's handle."""
+    values into `cache`. Gains: float32 [hd] or None. stream: a stream's handle, None: torch's current stream."""
     lib, dev, hd, nkv = _lib or load_library(), cache.device, cache.head_dim, cache.n_kv_heads
     if len(q.shape) != 3:
         raise ValueError(f"q must have three dimensions; it has {tuple(q.shape)}")
@@ -231,17 +241,18 @@ def qk_norm_rope(q, k, v, positions, slots, rope_table, cache, q_out, q_gain=Non
                            0 if q_gain is None else _dense("q_gain", q_gain, _FLOAT, (hd,), dev), 0 if k_gain is None else _dense("k_gain", k_gain, _FLOAT, (hd,), dev),
                            _dense("positions", positions, _INT, (T,), dev), _dense("slots", slots, _INT, (T,), dev),
                            _dense("rope_table", rope_table, _FLOAT, (rows, hd // 2, 2), dev), op, os_, eps, q_scale)
-    rc = lib.blink_qk_norm_rope(dev, a, stream)
+    rc = lib.blink_qk_norm_rope(dev, a, _stream(stream, q, dev))
     if rc:
         _check(lib, rc)
 
 
-def kv_cache_read(cache, slots, k_out, v_out, stream=0):
-    """blink_kv_cache_read: the tokens at int32 slots [tokens] into k_out, v_out, contiguous float16 [tokens, kv heads, hd]."""
+def kv_cache_read(cache, slots, k_out, v_out, stream=None):
+    """blink_kv_cache_read: the tokens at int32 slots [tokens] into k_out, v_out, contiguous float16 [tokens, kv heads, hd].
+    stream: as for qk_norm_rope."""
     lib, dev = _lib or load_library(), cache.device
     shape = (slots.shape[0], cache.n_kv_heads, cache.head_dim)
     _check(lib, lib.blink_kv_cache_read(dev, _CACHE.pack(*cache._packed), _dense("slots", slots, _INT, shape[:1], dev), shape[0],
-                                        _dense("k_out", k_out, _HALF, shape, dev), _dense("v_out", v_out, _HALF, shape, dev), stream))
+                                        _dense("k_out", k_out, _HALF, shape, dev), _dense("v_out", v_out, _HALF, shape, dev), _stream(stream, slots, dev)))
 
 
 def attention_workspace_bytes(n_q_heads, cache, n_seqs, max_q=1):
@@ -252,9 +263,9 @@ def attention_workspace_bytes(n_q_heads, cache, n_seqs, max_q=1):
     return n.value
 
 
-def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q=1, window=0, sinks=0, scale=1.0, stream=0):
+def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q=1, window=0, sinks=0, scale=1.0, stream=None):
     """blink_paged_attention: q, out float16 [tokens, q heads, hd]; int32 block_tables [seqs, blocks], seq_lens [seqs], cu_seqlens
-    [seqs + 1]; workspace: a contiguous tensor of attention_workspace_bytes(...) bytes. stream: a stream's handle."""
+    [seqs + 1]; workspace: a contiguous tensor of attention_workspace_bytes(...) bytes. stream: as for qk_norm_rope."""
     lib, dev, hd = _lib or load_library(), cache.device, cache.head_dim
     if len(q.shape) != 3 or len(block_tables.shape) != 2:
         raise ValueError(f"q must have three dimensions and block_tables two; they have {tuple(q.shape)} and {tuple(block_tables.shape)}")
@@ -269,7 +280,7 @@ def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace
     a = _PAGED_ATTENTION.pack(*cache._packed, nq, S, T, max_q, width, window, sinks, scale, qp, op, qs, os_, _dense("cu_seqlens", cu_seqlens, _INT, (S + 1,), dev),
                               _dense("seq_lens", seq_lens, _INT, (S,), dev), _dense("block_tables", block_tables, _INT, (S, width), dev), workspace.data_ptr(),
                               workspace.numel() * workspace.element_size())
-    rc = lib.blink_paged_attention(dev, a, stream)
+    rc = lib.blink_paged_attention(dev, a, _stream(stream, q, dev))
     if rc:
         _check(lib, rc)
 
