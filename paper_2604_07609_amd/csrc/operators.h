@@ -183,7 +183,8 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   if (int rc = check_heads(a->cache, a->n_q_heads)) return rc;
   if (int rc = paged_check(a->cache, a->n_q_heads, a->n_seqs, a->max_q)) return rc;
   const u32 hd = a->cache.head_dim, nkv = a->cache.n_kv_heads;
-  if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return fail(BLINK_ERR_INVAL, "scale must be positive and finite");
+  const float scale2 = a->scale * 1.44269504088896340736f;      // (scores as powers of two)
+  if (!(a->scale > 0.f) || !(scale2 < INFINITY)) return fail(BLINK_ERR_INVAL, "scale must be positive, and finite times log2(e)");
   if (a->sinks && !a->window) return fail(BLINK_ERR_INVAL, "sinks without a window");
   if (a->window > (1u << 30) || a->sinks > (1u << 30)) return fail(BLINK_ERR_INVAL, "window and sinks must be at most 2^30");
   if (a->n_seqs == 0 || a->n_tokens == 0) return BLINK_OK;
@@ -207,7 +208,7 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   p.q = (const f16_t*)a->q; p.qs = a->q_stride; p.out = (f16_t*)a->out; p.os = a->out_stride; p.cu = a->cu_seqlens; p.lens = a->seq_lens;
   p.tables = (const u32*)a->block_tables; p.cache = a->cache.data; p.n_blocks = a->cache.n_blocks; p.max_blocks = a->max_blocks;
   p.nq = a->n_q_heads; p.nkv = nkv; p.G = p.nq / nkv; p.n_seqs = a->n_seqs; p.n_tokens = a->n_tokens; p.max_q = a->max_q;
-  p.window = a->window; p.sinks = a->sinks; p.c = a->scale * 1.44269504088896340736f; p.short_rows = plan.short_rows; p.n_splits = plan.n_splits;
+  p.window = a->window; p.sinks = a->sinks; p.c = scale2; p.short_rows = plan.short_rows; p.n_splits = plan.n_splits;
   p.ctr = (u32*)a->workspace; p.part = (float*)((char*)a->workspace + paged_ctr_bytes(n_cu)); p.prompt_part = p.part + plan.part_bytes / 4;
   const hipStream_t st = (hipStream_t)stream;
   HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_paged<64, 16>(p, plan, st) : launch_paged<64, 4>(p, plan, st))
