@@ -353,7 +353,8 @@ int blink_kv_cache_bytes(uint32_t n_blocks, uint32_t n_kv_heads, uint32_t head_d
  * computed in 32 bits, keys on their way to 4 bits in 64 (their codes do not depend on an order of summation). A group of 32 with an
  * infinity or NaN reads as NaN from 4 bits.
  * A token whose position is not in [0, rope_rows) is skipped: none of its rows is written. One whose slot lies outside the
- * cache (-1, padding) leaves the cache alone. The same slot twice: what that place then holds is not defined. */
+ * cache (-1, padding) leaves the cache alone. The same slot twice: what that place then holds is not defined.
+ * BLINK_ERR_TOO_LARGE (here and for blink_kv_cache_read): more tokens than one launch of 2^32 threads takes. */
 typedef struct {
   blink_kv_cache cache;
   uint32_t n_q_heads, n_tokens;

@@ -48,6 +48,8 @@ static int check_rows(const char* name, const void* p, u64 stride, u64 width, u3
   return BLINK_OK;
 }
 
+constexpr u32 LAUNCH_WGS = 0xFFFFFFFFu / BLK_THREADS;     // workgroups of a launch, whose threads are counted in 32 bits
+
 extern "C" int blink_kv_cache_bytes(uint32_t n_blocks, uint32_t n_kv_heads, uint32_t head_dim, uint32_t bits, uint64_t* bytes) {
   g_err.clear();
   if (!bytes) return fail(BLINK_ERR_INVAL, "null argument");
@@ -71,6 +73,8 @@ extern "C" int blink_qk_norm_rope(int32_t device, const blink_qk_norm_rope_args*
   if (!(a->eps >= 0.f)) return fail(BLINK_ERR_INVAL, "eps must not be negative");
   if (a->n_tokens == 0) return BLINK_OK;
   if ((u64)a->n_tokens * (a->n_q_heads + 2ull * nkv) >= (1ull << 31)) return fail(BLINK_ERR_TOO_LARGE, "2^31 rows or more");
+  // (so many tokens have the largest groups, whatever the number of compute units)
+  if (store_wgs(a->n_tokens, a->n_q_heads, nkv, hd, a->cache.bits, STORE_GROUP) > LAUNCH_WGS) return fail(BLINK_ERR_TOO_LARGE, "too many tokens for one call");
   if (int rc = check_rows("q", a->q, a->q_stride, (u64)a->n_q_heads * hd, es)) return rc;
   if (int rc = check_rows("k", a->k, a->k_stride, (u64)nkv * hd, es)) return rc;
   if (int rc = check_rows("v", a->v, a->v_stride, (u64)nkv * hd, es)) return rc;
@@ -104,7 +108,7 @@ extern "C" int blink_kv_cache_read(int32_t device, const blink_kv_cache* c, cons
   if (int rc = check_rows("k_out", k_out, width, width, 2)) return rc;
   if (int rc = check_rows("v_out", v_out, width, width, 2)) return rc;
   if (!slots || (u64)slots % 4) return fail(BLINK_ERR_INVAL, "slots is null or not aligned");
-  if (n >= (1ull << 31) * BLK_THREADS) return fail(BLINK_ERR_TOO_LARGE, "too many tokens for one call");
+  if (n > (u64)LAUNCH_WGS * BLK_THREADS) return fail(BLINK_ERR_TOO_LARGE, "too many tokens for one call");
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
   OnDevice on(device);
