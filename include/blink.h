@@ -281,7 +281,7 @@ int blink_debug_read(blink_engine* e, uint32_t what, void* buf, uint64_t cap_byt
  * chunks (13 to 15: no kernels); a mixture-of-experts model runs, in place of 7 and 8: 16 router GEMM, 17 expert selection, 18 grouped gate/up GEMMs,
  * 19 grouped down GEMMs, 20 weighted sum + residual, and 21 (between 17 and 18) the experts' operand gathered by
  * expert; -1 none). There
- * are no kernels for phases 1, 6 and 9, and for 3 only with blink_init_attention's options (fused into the GEMMs; their time is 0). While a phase is selected, the loop
+ * are no kernels for phases 1, 6 and 9, nor for 3 without blink_init_attention's options (fused into the GEMMs; their time is 0). While a phase is selected, the loop
  * brackets every launch of that phase's kernel with HIP events on the compute stream. After the loop has
  * stopped, blink_get_phase_times returns, per iteration enqueued in the last window and in enqueue order, the
  * summed duration in milliseconds of that kernel's launches (one per layer for per-layer phases). */
@@ -379,7 +379,8 @@ int blink_kv_cache_read(int32_t device, const blink_kv_cache* cache, const int32
  * seq_lens[s] tokens, which lie in the blocks block_tables[s][0 ..]. A query at position p sees the keys j <= p with j > p - window or
  * j < sinks (window 0: all j <= p): out = softmax(scale q.k) v over those, query head h with kv head h / (n_q_heads / n_kv_heads). A query that sees no
  * key (an unused batch slot: a token and a length of 0) gives zeros; what lies in masked places, in unused places of the last
- * block or in no block's place does not matter, infinities and NaN included. Scores, maxima and sums in 32 bits, probabilities as halves.
+ * block or in no block's place does not matter, infinities and NaN included. Scores, maxima and sums in 32 bits, probabilities as halves;
+ * outputs are rounded to nearest halves (beyond 65504: that).
  * max_q: no sequence has more queries than this (further ones are not computed). Single tokens, drafts and prompts may be mixed; calls whose
  * sequences have few queries (max_q n_q_heads / n_kv_heads <= 16) are the fastest for those. Rows of `out` that no sequence has stay as they are.
  * Block ids outside the cache: their keys are not seen. Results do not depend on how the work falls on the chip.

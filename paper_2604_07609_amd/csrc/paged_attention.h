@@ -517,7 +517,7 @@ __device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqVie
 __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { return a.out_tbs ? a.out + packed_off(tok, k, a.out_tbs) : a.out + (u64)tok * a.os + k; }
 
 // Bound by bytes where there are many: 256 sequences of up to 1028 visible keys (8 kv heads of 128, halves) 574 MB in 122 us, 4.7 TB/s,
-// 1.05 GB of long contexts 5.6; 128 sequences of 3000 to 16384 in 4 bits 1.10 GB in 207 us, 5.3 TB/s. What is left of
+// 1.05 GB of long contexts 5.6; 128 sequences of 3000 to 16384 in 4 bits 1.10 GB in 209 us, 5.3 TB/s. What is left of
 // 6.3 is the start (7 us to the first tile: lengths, ids, tile, one after the other), the end (8 us: a workgroup's results joined and
 // handed on) and XCDs that are up to a tenth slower than others, another one in every launch. Few keys are bound by those latencies.
 //
@@ -849,8 +849,8 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 // wave skips the steps that none of its own rows see. Items come from a counter, the last queries first, each asked for an item
 // ahead. With fewer items than workgroups the keys of each are cut into parts, whose results a second kernel adds up.
 // Bound by the instructions of the softmax (32 exponentials and 87 others a lane and step) and the products in turn: 2048 queries at
-// 16384 keys in 4 bits (32 q, 8 kv heads of 128) 549 us, 0.94 PFLOP/s, where the library's largest products reach 1.08; two prompts of 4000
-// behind a window of 1024 165 us, 0.71 PFLOP/s: an item is 17 steps, and its start (queries, ids, the first tiles) and end another 3.
+// 16384 keys in 4 bits (32 q, 8 kv heads of 128) 547 us, 0.94 PFLOP/s, where the library's largest products reach 1.08; two prompts of 4000
+// behind a window of 1024 168 us, 0.70 PFLOP/s: an item is 17 steps, and its start (queries, ids, the first tiles) and end another 3.
 #define PROMPT_CT 2u
 #define PROMPT_PIPE 3             // groups of operands on their way from LDS and in use
 #define PROMPT_ROWS (128u * PROMPT_CT)
