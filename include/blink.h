@@ -375,6 +375,12 @@ int blink_qk_norm_rope(int32_t device, const blink_qk_norm_rope_args* args, void
  * stay as they are. */
 int blink_kv_cache_read(int32_t device, const blink_kv_cache* cache, const int32_t* slots, uint32_t n_tokens, void* k_out, void* v_out, void* stream);
 
+/* Blocks copied within caches, of all layers in one call: block to_blocks[i] becomes what block from_blocks[i] is, keys and values of its 16 places, in each of
+ * the n_caches caches (host array of descriptions, all of one shape and kind). For a continuation that begins inside a block which others go on to use. A copy
+ * with an id outside the caches is none. A block may be copied any number of times; one that is both copied and written to in a call, or
+ * written to twice: what it then holds is not defined. */
+int blink_kv_cache_copy(int32_t device, const blink_kv_cache* caches, uint32_t n_caches, const int32_t* from_blocks, const int32_t* to_blocks, uint32_t n_copies, void* stream);
+
 /* Attention over the cache. Sequence s has the tokens cu_seqlens[s] .. cu_seqlens[s + 1] of q, the last ones of its context of
  * seq_lens[s] tokens, which lie in the blocks block_tables[s][0 ..]. A query at position p sees the keys j <= p with j > p - window or
  * j < sinks (window 0: all j <= p): out = softmax(scale q.k) v over those, query head h with kv head h / (n_q_heads / n_kv_heads). A query that sees no
@@ -405,6 +411,34 @@ typedef struct {
 int blink_paged_attention(int32_t device, const blink_paged_attention_args* args, void* stream);
 /* What blink_paged_attention needs for any call with these numbers (and any smaller max_q or n_seqs). */
 int blink_attention_workspace_bytes(int32_t device, const blink_kv_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t max_q, uint64_t* bytes);
+
+/* Log probabilities of given tokens, the entropy and the most probable tokens, from rows of logits x (device memory, where blink_sample_rows' rows are the
+ * host's). With z = x inverse_temperature[row]: log p = z - log sum exp(z). Of row r, for each of the n_given tokens: logprobs = log p, ranks = how
+ * many tokens come before it, larger logits first, of equal ones the lower id (the most probable one: 0). A token outside [0, vocab), as in
+ * a padded batch: 0 and -1. entropy = - sum p log p. top_ids, top_logprobs: the first k tokens of that order. All sums in 32 bits.
+ * Logits of -inf are tokens of probability 0. A row with NaN or +inf, with nothing above -inf, or whose inverse temperature is not positive or not
+ * finite (also times log2(e)) has NaN for its log probabilities and entropy; ranks and ids are there, with NaN in the place of -inf.
+ * The first 8 KiB of the workspace are zeros before its first call and again after every one, and it can be shared with other calls' in turn,
+ * as that of blink_paged_attention can. Results do not depend on how the work falls on the chip. */
+typedef struct {
+  uint32_t type;               /* BLINK_TYPE_* of the logits */
+  uint32_t n_rows, vocab;      /* vocab: at most 2^30 */
+  uint32_t n_given, k;         /* at most 64 each; either may be 0 */
+  const void* logits;          /* [n_rows][vocab], aligned to an element */
+  uint64_t stride;             /* elements from row to row */
+  const int32_t* tokens;       /* [n_rows][n_given] */
+  const float* inverse_temperature;        /* [n_rows], null: 1 */
+  float* logprobs;             /* [n_rows][n_given] */
+  int32_t* ranks;              /* the same, or null */
+  float* entropy;              /* [n_rows], or null */
+  int32_t* top_ids;            /* [n_rows][k] */
+  float* top_logprobs;         /* [n_rows][k] */
+  void* workspace;             /* aligned to 256 bytes */
+  uint64_t workspace_bytes;
+} blink_token_logprobs_args;
+int blink_token_logprobs(int32_t device, const blink_token_logprobs_args* args, void* stream);
+/* What blink_token_logprobs needs for any call with these numbers, and any smaller n_rows, n_given or k. */
+int blink_token_logprobs_workspace_bytes(int32_t device, uint32_t n_rows, uint32_t vocab, uint32_t n_given, uint32_t k, uint64_t* bytes);
 
 /* Message of the last error on the calling thread ("" if none). The pointer stays valid until the next call. */
 const char* blink_last_error(void);

@@ -16,7 +16,7 @@ EVENT_FIRST, EVENT_LAST = 1, 2
 EXPORTS = ["blink_init", "blink_init_attention", "blink_submit", "blink_run", "blink_set_exit_when_idle", "blink_wait", "blink_stop", "blink_poll_outputs", "blink_shutdown",
            "blink_get_trace", "blink_get_stats", "blink_debug_read", "blink_time_phase", "blink_get_phase_times", "blink_calibration_copy",
            "blink_calibration_rates", "blink_clock_sync", "blink_sample_rows", "blink_sample_rows_static", "blink_kv_cache_bytes", "blink_qk_norm_rope",
-           "blink_kv_cache_read", "blink_paged_attention", "blink_attention_workspace_bytes", "blink_last_error"]
+           "blink_kv_cache_read", "blink_kv_cache_copy", "blink_token_logprobs", "blink_token_logprobs_workspace_bytes", "blink_paged_attention", "blink_attention_workspace_bytes", "blink_last_error"]
 
 
 class DBG:
@@ -58,8 +58,14 @@ class PagedAttentionArgs(C.Structure):
         (n, C.c_void_p) for n in ("cu_seqlens", "seq_lens", "block_tables", "workspace")] + [("workspace_bytes", C.c_uint64)]
 
 
-# the same three as `struct` packs them (fields in order, native alignment)
+class TokenLogprobsArgs(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "n_rows", "vocab", "n_given", "k")] + [("logits", C.c_void_p), ("stride", C.c_uint64)] + [
+        (n, C.c_void_p) for n in ("tokens", "inverse_temperature", "logprobs", "ranks", "entropy", "top_ids", "top_logprobs", "workspace")] + [("workspace_bytes", C.c_uint64)]
+
+
+# the same four as `struct` packs them (fields in order, native alignment)
 _CACHE, _QK_NORM_ROPE, _PAGED_ATTENTION = struct.Struct("@P4I"), struct.Struct("@P4I4I3P3Q6PQ2f"), struct.Struct("@P4I7If2P2Q4PQ")
+_TOKEN_LOGPROBS = struct.Struct("@5IPQ8PQ")
 
 
 class Stats(C.Structure):
@@ -125,6 +131,9 @@ def load_library():
     lib.blink_kv_cache_bytes.argtypes = [u32, u32, u32, u32, C.POINTER(u64)]
     lib.blink_qk_norm_rope.argtypes = [C.c_int32, vp, vp]
     lib.blink_kv_cache_read.argtypes = [C.c_int32, vp, vp, u32, vp, vp, vp]
+    lib.blink_kv_cache_copy.argtypes = [C.c_int32, vp, u32, vp, vp, u32, vp]
+    lib.blink_token_logprobs.argtypes = [C.c_int32, vp, vp]
+    lib.blink_token_logprobs_workspace_bytes.argtypes = [C.c_int32, u32, u32, u32, u32, C.POINTER(u64)]
     lib.blink_paged_attention.argtypes = [C.c_int32, vp, vp]
     lib.blink_attention_workspace_bytes.argtypes = [C.c_int32, vp, u32, u32, u32, C.POINTER(u64)]
     lib.blink_last_error.restype = C.c_char_p
@@ -219,6 +228,7 @@ class KVCache:
             raise ValueError(f"data must be contiguous and have {need} bytes; it has {data.numel() * data.element_size()}, strides {tuple(data.stride())}")
         self.data, self.device = data, data.get_device()
         self.desc = CacheDesc(data.data_ptr(), n_blocks, n_kv_heads, head_dim, bits)
+        self._bytes = bytes(self.desc)
         self.n_kv_heads, self.head_dim, self._packed = n_kv_heads, head_dim, (data.data_ptr(), n_blocks, n_kv_heads, head_dim, bits)
 
 
@@ -255,6 +265,20 @@ def kv_cache_read(cache, slots, k_out, v_out, stream=None):
                                         _dense("k_out", k_out, _HALF, shape, dev), _dense("v_out", v_out, _HALF, shape, dev), _stream(stream, slots, dev)))
 
 
+def kv_cache_copy(caches, from_blocks, to_blocks, stream=None):
+    """blink_kv_cache_copy: in every cache (a KVCache, or a list of them: layers of one shape) block to_blocks[i] becomes what from_blocks[i] is, int32
+    [copies] both. stream: as for qk_norm_rope."""
+    lib = _lib or load_library()
+    caches = (caches,) if isinstance(caches, KVCache) else caches
+    if not caches:
+        return
+    dev, shape = caches[0].device, (from_blocks.shape[0],)
+    if any(c.device != dev for c in caches):
+        raise ValueError(f"the caches must be on one device; they are on {sorted({c.device for c in caches})}")
+    _check(lib, lib.blink_kv_cache_copy(dev, b"".join([c._bytes for c in caches]), len(caches), _dense("from_blocks", from_blocks, _INT, shape, dev),
+                                        _dense("to_blocks", to_blocks, _INT, shape, dev), shape[0], _stream(stream, from_blocks, dev)))
+
+
 def attention_workspace_bytes(n_q_heads, cache, n_seqs, max_q=1):
     """Bytes of the workspace of paged_attention for up to n_seqs sequences of up to max_q queries. Its first 8 KiB hold zeros
     before its first call; calls of any shapes may share one in turn."""
@@ -281,6 +305,52 @@ def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace
                               _dense("seq_lens", seq_lens, _INT, (S,), dev), _dense("block_tables", block_tables, _INT, (S, width), dev), workspace.data_ptr(),
                               workspace.numel() * workspace.element_size())
     rc = lib.blink_paged_attention(dev, a, _stream(stream, q, dev))
+    if rc:
+        _check(lib, rc)
+
+
+def token_logprobs_workspace_bytes(n_rows, vocab, n_given=1, k=0, device=0):
+    """Bytes of the workspace of token_logprobs for up to n_rows rows. Its first 8 KiB hold zeros before its first call; it may be
+    shared with paged_attention's, in turn."""
+    lib, n = load_library(), C.c_uint64()
+    _check(lib, lib.blink_token_logprobs_workspace_bytes(device, n_rows, vocab, n_given, k, C.byref(n)))
+    return n.value
+
+
+def token_logprobs(logits, workspace, tokens=None, logprobs=None, ranks=None, entropy=None, top_ids=None, top_logprobs=None, inverse_temperature=None, stream=None):
+    """blink_token_logprobs: of logits [rows, vocab] (float32, float16 or bfloat16, rows may be parts of wider ones): of int32 tokens [rows, given]
+    logprobs float32 and ranks int32 (or None) of that shape; entropy float32 [rows]; top_ids int32 and top_logprobs float32 [rows, k]. What is
+    None is not computed. inverse_temperature: float32 [rows]. workspace: a contiguous tensor of token_logprobs_workspace_bytes(...) bytes.
+    stream: as for qk_norm_rope."""
+    lib, dev, kind = _lib or load_library(), logits.get_device(), _kind(logits)
+    if len(logits.shape) != 2 or kind > _BF16:
+        raise ValueError(f"logits must have two dimensions and be float32, float16 or bfloat16; they have {tuple(logits.shape)} and are {logits.dtype}")
+    R, V = logits.shape
+    st = logits.stride()
+    if dev < 0 or (st[1] != 1 and V != 1) or (R > 1 and st[0] < V):
+        raise ValueError(f"logits must have contiguous rows, on a GPU; they have strides {tuple(st)}, on device {dev}")
+    if (tokens is None) != (logprobs is None) or (ranks is not None and tokens is None):
+        raise ValueError("tokens and logprobs belong together, and ranks to them")
+    if (top_ids is None) != (top_logprobs is None):
+        raise ValueError("top_ids and top_logprobs belong together")
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on device {dev}; it is on device {workspace.get_device()}")
+    G = k = 0
+    at = [0] * 7
+    if tokens is not None:
+        G = tokens.shape[-1]
+        at[0], at[2] = _dense("tokens", tokens, _INT, (R, G), dev), _dense("logprobs", logprobs, _FLOAT, (R, G), dev)
+        if ranks is not None:
+            at[3] = _dense("ranks", ranks, _INT, (R, G), dev)
+    if inverse_temperature is not None:
+        at[1] = _dense("inverse_temperature", inverse_temperature, _FLOAT, (R,), dev)
+    if entropy is not None:
+        at[4] = _dense("entropy", entropy, _FLOAT, (R,), dev)
+    if top_ids is not None:
+        k = top_ids.shape[-1]
+        at[5], at[6] = _dense("top_ids", top_ids, _INT, (R, k), dev), _dense("top_logprobs", top_logprobs, _FLOAT, (R, k), dev)
+    rc = lib.blink_token_logprobs(dev, _TOKEN_LOGPROBS.pack(kind, R, V, G, k, logits.data_ptr(), st[0] if R > 1 else V, *at, workspace.data_ptr(),
+                                                            workspace.numel() * workspace.element_size()), _stream(stream, logits, dev))
     if rc:
         _check(lib, rc)
 

@@ -1,4 +1,4 @@
-// norms, rotation and storage of queries, keys and values; tokens read back
+// norms, rotation and storage of queries, keys and values; tokens read back; blocks copied
 #include "../paged_kernels.h"
 
 #define STORE_KERNEL(T, HD, BITS)                                                                                 \
@@ -15,3 +15,4 @@ __global__ void __launch_bounds__(BLK_THREADS) k_kv_read(ReadArgs a, u32 hd) {
   const u64 i = (u64)blockIdx.x * BLK_THREADS + threadIdx.x;
   if (hd == 64) kv_read<64>(a, i); else kv_read<128>(a, i);
 }
+__global__ void __launch_bounds__(BLK_THREADS) k_kv_copy(CopyArgs a) { kv_copy(a, blockIdx.x); }

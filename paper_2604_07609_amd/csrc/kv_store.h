@@ -386,3 +386,29 @@ __device__ __forceinline__ void kv_read(const ReadArgs& a, u64 i) {      // eigh
   *(uint4*)(a.ko + o) = make_uint4(k[0], k[1], k[2], k[3]);
   *(uint4*)(a.vo + o) = make_uint4(v[0], v[1], v[2], v[3]);
 }
+
+// ---- blocks copied ------------------------------------------------------------------------------------------------------------
+// A block is one piece of memory in a cache of 4 bits, two (its keys, its values) in one of 16. A workgroup copies COPY_WORDS words of 16 bytes
+// of a piece at most, four of a lane on their way at a time.
+#define COPY_CACHES 128u           // caches of a launch
+#define COPY_WORDS (4u * BLK_THREADS)
+struct CopyArgs {
+  u32 n_caches, n_copies, n_blocks, words;      // words: of a piece
+  u32 pieces, wgs;                // of a block; workgroups of a piece
+  const i32 *from, *to;           // a copy with an id outside the caches is none
+  void* cache[COPY_CACHES];
+};
+__device__ __forceinline__ void kv_copy(const CopyArgs& a, u32 wg) {
+  const u32 at = wg % a.wgs * COPY_WORDS + threadIdx.x, p = wg / a.wgs, piece = p % a.pieces, n = p / a.pieces % a.n_copies, c = p / a.pieces / a.n_copies;
+  const i32 from = a.from[n], to = a.to[n];
+  if (from < 0 || to < 0 || (u32)from >= a.n_blocks || (u32)to >= a.n_blocks) return;
+  typedef u32 word_t __attribute__((ext_vector_type(4)));
+  word_t* const base = (word_t*)a.cache[c];
+  const word_t* const x = base + ((u64)piece * a.n_blocks + (u32)from) * a.words;
+  word_t* const y = base + ((u64)piece * a.n_blocks + (u32)to) * a.words;
+  word_t v[4];
+#pragma unroll
+  for (u32 i = 0; i < 4; ++i) if (at + i * BLK_THREADS < a.words) v[i] = x[at + i * BLK_THREADS];
+#pragma unroll
+  for (u32 i = 0; i < 4; ++i) if (at + i * BLK_THREADS < a.words) y[at + i * BLK_THREADS] = v[i];
+}

@@ -118,6 +118,93 @@ extern "C" int blink_kv_cache_read(int32_t device, const blink_kv_cache* c, cons
   return BLINK_OK;
 }
 
+extern "C" int blink_kv_cache_copy(int32_t device, const blink_kv_cache* caches, uint32_t n_caches, const int32_t* from_blocks, const int32_t* to_blocks, uint32_t n_copies, void* stream) {
+  g_err.clear();
+  if (!caches && n_caches) return fail(BLINK_ERR_INVAL, "null argument");
+  for (u32 i = 0; i < n_caches; ++i) {
+    const blink_kv_cache &c = caches[i], &d = caches[0];
+    if (int rc = check_heads(c, c.n_kv_heads)) return rc;
+    if (c.n_blocks != d.n_blocks || c.n_kv_heads != d.n_kv_heads || c.head_dim != d.head_dim || c.bits != d.bits) return fail(BLINK_ERR_INVAL, "cache %u is not like the first one", i);
+  }
+  if (n_copies == 0 || n_caches == 0) return BLINK_OK;
+  if (!from_blocks || !to_blocks || (u64)from_blocks % 4 || (u64)to_blocks % 4) return fail(BLINK_ERR_INVAL, "from_blocks or to_blocks is null or not aligned");
+  CopyArgs a{};
+  a.n_copies = n_copies; a.n_blocks = caches[0].n_blocks; a.from = from_blocks; a.to = to_blocks;
+  a.pieces = caches[0].bits == 16 ? 2 : 1;
+  a.words = caches[0].n_kv_heads * caches[0].head_dim * (caches[0].bits == 16 ? 32 : 17) / 16;
+  a.wgs = (a.words + COPY_WORDS - 1) / COPY_WORDS;
+  if ((u64)std::min(n_caches, COPY_CACHES) * n_copies * a.pieces * a.wgs > LAUNCH_WGS) return fail(BLINK_ERR_TOO_LARGE, "too many copies for one call");
+  u32 n_cu;
+  if (int rc = compute_units(device, &n_cu)) return rc;
+  OnDevice on(device);
+  HIPCHK(on.err);
+  for (u32 done = 0; done < n_caches; done += a.n_caches) {
+    a.n_caches = std::min(n_caches - done, COPY_CACHES);
+    for (u32 i = 0; i < a.n_caches; ++i) a.cache[i] = caches[done + i].data;
+    HIPCHK(launch(k_kv_copy, a.n_caches * n_copies * a.pieces * a.wgs, BLK_THREADS, (hipStream_t)stream, a));
+  }
+  return BLINK_OK;
+}
+
+// ---- log probabilities ----------------------------------------------------------------------------------------------------------
+// workgroups of a row: LP_PER_CU for every compute unit in all, a tile each at least
+static u32 logprob_parts(u32 rows, u32 vocab, u32 n_cu) {
+  const u32 tiles = (vocab + LP_TILE - 1) / LP_TILE;
+  const u64 want = ((u64)LP_PER_CU * n_cu + rows - 1) / rows;
+  return rows > LP_CTR_BYTES / 4 ? 1u : (u32)std::min<u64>({want, tiles, LP_MAX_PARTS});
+}
+static int check_logprobs(u32 rows, u32 vocab, u32 given, u32 k) {
+  if (!vocab || vocab > (1u << 30)) return fail(BLINK_ERR_INVAL, "vocab must be in [1, 2^30]");
+  if (given > LP_MOST || k > LP_MOST || k > vocab) return fail(BLINK_ERR_INVAL, "at most %u given tokens, and %u most probable ones of %u", LP_MOST, LP_MOST, vocab);
+  if (rows > LAUNCH_WGS) return fail(BLINK_ERR_TOO_LARGE, "too many rows for one call");
+  return BLINK_OK;
+}
+static u64 logprob_bytes(u32 rows, u32 given, u32 k, u32 parts) { return LP_CTR_BYTES + (parts > 1 ? (u64)rows * parts * lp_words(given, k) * 4 : 0); }
+
+extern "C" int blink_token_logprobs_workspace_bytes(int32_t device, uint32_t n_rows, uint32_t vocab, uint32_t n_given, uint32_t k, uint64_t* bytes) {
+  g_err.clear();
+  if (!bytes) return fail(BLINK_ERR_INVAL, "null argument");
+  if (int rc = check_logprobs(n_rows, vocab, n_given, k)) return rc;
+  u32 n_cu;
+  if (int rc = compute_units(device, &n_cu)) return rc;
+  // (and any smaller call's: rows times parts of each are about as many as workgroups are wanted, or fewer)
+  const u64 most = std::min<u64>(std::min<u64>(n_rows, LP_CTR_BYTES / 4) * LP_MAX_PARTS, (u64)LP_PER_CU * n_cu + std::min<u64>(n_rows, LP_CTR_BYTES / 4));
+  *bytes = LP_CTR_BYTES + most * lp_words(n_given, k) * 4;
+  return BLINK_OK;
+}
+
+template <typename T>
+static hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t st) {
+  return a.k ? launch(k_token_logprobs<T, true>, a.rows * a.parts, BLK_THREADS, st, a) : launch(k_token_logprobs<T, false>, a.rows * a.parts, BLK_THREADS, st, a);
+}
+extern "C" int blink_token_logprobs(int32_t device, const blink_token_logprobs_args* a, void* stream) {
+  g_err.clear();
+  if (!a) return fail(BLINK_ERR_INVAL, "null argument");
+  if (a->type > BLINK_TYPE_BF16) return fail(BLINK_ERR_INVAL, "type must be BLINK_TYPE_FLOAT, BLINK_TYPE_HALF or BLINK_TYPE_BF16");
+  if (int rc = check_logprobs(a->n_rows, a->vocab, a->n_given, a->k)) return rc;
+  if (a->n_rows == 0) return BLINK_OK;
+  if (!a->logits || (u64)a->logits % (a->type == BLINK_TYPE_FLOAT ? 4 : 2)) return fail(BLINK_ERR_INVAL, "logits is null or not aligned to its elements");
+  if (a->stride < a->vocab) return fail(BLINK_ERR_INVAL, "a stride of %llu elements, rows are %u long", (unsigned long long)a->stride, a->vocab);
+  if (a->n_given && (!a->tokens || !a->logprobs)) return fail(BLINK_ERR_INVAL, "tokens and logprobs must not be null");
+  if (a->k && (!a->top_ids || !a->top_logprobs)) return fail(BLINK_ERR_INVAL, "top_ids and top_logprobs must not be null");
+  const void* const words[] = {a->tokens, a->inverse_temperature, a->logprobs, a->ranks, a->entropy, a->top_ids, a->top_logprobs};
+  for (const void* p : words) if ((u64)p % 4) return fail(BLINK_ERR_INVAL, "tokens, inverse_temperature and the results must be aligned to 4 bytes");
+  u32 n_cu;
+  if (int rc = compute_units(device, &n_cu)) return rc;
+  LogprobArgs l{};
+  l.parts = logprob_parts(a->n_rows, a->vocab, n_cu);
+  const u64 need = logprob_bytes(a->n_rows, a->n_given, a->k, l.parts);
+  if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < need) return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)need);
+  OnDevice on(device);
+  HIPCHK(on.err);
+  l.x = a->logits; l.stride = a->stride; l.rows = a->n_rows; l.V = a->vocab; l.given = a->n_given; l.k = a->k; l.tokens = a->tokens; l.inverse = a->inverse_temperature;
+  l.logprobs = a->logprobs; l.ranks = a->n_given ? a->ranks : nullptr; l.entropy = a->entropy; l.top_ids = a->top_ids; l.top_logprobs = a->top_logprobs;
+  l.ctr = (u32*)a->workspace; l.results = (u32*)((char*)a->workspace + LP_CTR_BYTES);
+  const hipStream_t st = (hipStream_t)stream;
+  HIPCHK(a->type == BLINK_TYPE_FLOAT ? launch_logprobs<float>(l, st) : a->type == BLINK_TYPE_HALF ? launch_logprobs<_Float16>(l, st) : launch_logprobs<__bf16>(l, st));
+  return BLINK_OK;
+}
+
 // ---- attention ------------------------------------------------------------------------------------------------------------------
 // The workspace: the counters, then results of the short part, then those of the prompt part. The counters are zeros between calls and results
 // are anything, so where the ones end must be the same in every call, whatever its batch, heads, bits and plan: the counters of

@@ -1,6 +1,8 @@
-// The kernels of the paged-cache operators, defined in kernels/kv_store.hip, paged_short.hip, paged_prompt.hip and paged_both.hip, and
+// The kernels of the paged-cache operators, defined in kernels/kv_store.hip, paged_short.hip, paged_prompt.hip and paged_both.hip, of the log
+// probabilities (kernels/logprobs.hip), and
 // those of an engine's phases that are the same operators (kernels/paged_phases.hip).
 #pragma once
+#include "logprobs.h"
 #include "paged_attention.h"
 
 // Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold; 8 sequences of 4000 keys with 32
@@ -17,6 +19,8 @@
 
 template <typename T, int HD, int BITS> __global__ void k_kv_store(StoreArgs a);
 __global__ void k_kv_read(ReadArgs a, u32 hd);
+__global__ void k_kv_copy(CopyArgs a);
+template <typename T, bool TOP> __global__ void k_token_logprobs(LogprobArgs a);
 template <int HD, int BITS, int CT> __global__ void k_paged_short(PagedArgs a);
 template <int HD, int BITS> __global__ void k_paged_prompt(PagedArgs a);
 template <int HD, int BITS> __global__ void k_paged_both(PagedArgs a);
