@@ -3,7 +3,7 @@
 
 #define LOGPROBS_KERNEL(T, TOP)                                                                                   \
   template <> __global__ void __launch_bounds__(BLK_THREADS, 4) k_token_logprobs<T, TOP>(LogprobArgs a) {         \
-    __shared__ LogprobShared sh;                                                                                  \
+    __shared__ LogprobShared<TOP> sh;                                                                                \
     token_logprobs<T, TOP>(a, sh, blockIdx.x);                                                                    \
   }
 #define LOGPROBS_KERNELS(T) LOGPROBS_KERNEL(T, false) LOGPROBS_KERNEL(T, true)

@@ -1,24 +1,27 @@
 // Log probabilities of given tokens with their ranks, the entropy and the most probable tokens, from rows of logits that are read once.
-// With z = x * inverse temperature, m the row's maximum and S = sum exp(z - m): log p = z - m - log S, entropy = log S - sum (z - m) exp(z - m) / S.
-// Both sums are of y = (x - m) c, c = inverse temperature * log2(e), and 2^y: y 2^y is at most 0.54 whatever the temperature. Every lane keeps its own running maximum and sums of the logits it reads, so nobody waits for anybody until the end.
+// With z = x * inverse temperature, c = inverse temperature * log2(e), y = x c - M for a number M near the largest x c, and S = sum 2^y:
+// log p = ln 2 (y - log2 S), entropy = ln 2 (log2 S - sum y 2^y / S). M may be any number: it is one for a wave, of the largest logit of its first tile, and
+// another one only where a later tile's is 2 above it, so that a logit costs one fused multiply-add ahead of its exponential; the difference of x c
+// and M is rounded once, so M's own rounding falls out.
 //
 // Order: larger logits first, of equal ones the lower id; a key of 64 bits (the logit's bits turned into a whole number, then the id
-// downwards) makes every place of it distinct. The k first ones of a tile: the lanes' largest keys, in groups of neighbouring lanes, are ranked
-// against each other; at least k logits are not below the kth of them, T, and those are in the k groups whose largest are not, so they are
-// few and fit in LDS whatever the row holds. Later tiles add what is above T. What comes together is thinned out the same way and at last ranked,
-// every key against every other.
+// downwards) makes every place of it distinct. The kth largest of the first tiles' largest logits, one of every few lanes, is a bound: what is
+// below it, or equal and in a later tile, is not among the k first. The keys of the others come together in LDS, each wave's apart; of more than LP_FEW (a
+// wave adds a tile at most) the kth is searched for bit by bit, and what is below it thrown away. At last all are ranked, every
+// one against every other.
 #pragma once
 #include "blink_device.h"
 
-#define LP_VALS 32u                // logits of a lane in a tile
-#define LP_TILE (BLK_THREADS * LP_VALS)
-#define LP_MOST 64u                // given tokens, most probable tokens
-#define LP_NEW (LP_MOST * LP_VALS) // keys that a tile adds at most once T is its own
-#define LP_FEW 512u                // keys that are ranked as they are
-#define LP_CAP (LP_FEW + LP_NEW)
+#define LP_VALS 16u                // logits of a lane in a tile
+#define LP_TILE (64u * LP_VALS)    // a wave's
+#define LP_WAVES (BLK_THREADS / 64u)
+#define LP_MOST 64u                // given tokens (a lane each), most probable tokens
+#define LP_FEW 160u                // keys that a wave keeps from tile to tile at most
+#define LP_CAP (LP_FEW + LP_TILE + 4)      // (and zeros behind them)
 #define LP_MAX_PARTS 32u           // workgroups of a row (LP_MAX_PARTS LP_MOST keys at most are joined)
 #define LP_PER_CU 4u               // workgroups that a call has for every compute unit, where its rows have the tiles
 #define LP_LOWEST -3.4028235e38f
+#define LP_LN2 0.69314718055994530942f
 #define LP_CTR_BYTES 8192u         // of the workspace: a counter per row whose parts are joined
 
 struct LogprobArgs {
@@ -35,232 +38,322 @@ struct LogprobArgs {
   u32* ctr;
   u32* results;                   // of the parts: lp_words(given, k) words each
 };
-// a part's result: maximum and sums, logits before each given one, then keys
+// a part's result: m and sums, logits before each given one, then keys
 __host__ __device__ __forceinline__ u32 lp_key_word(u32 given) { return (4 + given + 1) & ~1u; }
 __host__ __device__ __forceinline__ u32 lp_words(u32 given, u32 k) { return lp_key_word(given) + 2 * k; }
 
+template <bool TOP>
 struct LogprobShared {
-  u64 cand[LP_CAP], spare[LP_MOST * ((LP_CAP + BLK_THREADS - 1) / BLK_THREADS)], group[BLK_THREADS], top[LP_MOST], T;
-  u32 cnt[BLK_THREADS], n, last;
-  float m[4], s[4], t[4], given[LP_MOST];
-  i32 token[LP_MOST];
-  u32 before[LP_MOST];
+  alignas(16) u64 cand[TOP ? LP_WAVES * LP_CAP : 1];
+  u64 top[LP_MOST];
+  alignas(16) u32 group[TOP ? BLK_THREADS : 1];
+  u32 kth, before[LP_WAVES][LP_MOST], n[LP_WAVES], last;
+  float m[LP_WAVES], s[LP_WAVES], t[LP_WAVES];
 };
 
 __device__ __forceinline__ float lp_ordered(float x) { return fmaxf(x, -INFINITY); }      // NaN: as -inf
-__device__ __forceinline__ u64 lp_key(float x, u32 id) {
+__device__ __forceinline__ u32 lp_high(float x) {
   const u32 b = __float_as_uint(lp_ordered(x) + 0.0f);                                    // (-0: as 0)
-  return (u64)(b ^ ((i32)b < 0 ? 0xFFFFFFFFu : 0x80000000u)) << 32 | (0xFFFFFFFFu - id);
+  return b ^ ((i32)b < 0 ? 0xFFFFFFFFu : 0x80000000u);
 }
+__device__ __forceinline__ u64 lp_key(float x, u32 id) { return (u64)lp_high(x) << 32 | (0xFFFFFFFFu - id); }
 __device__ __forceinline__ u32 lp_id(u64 key) { return 0xFFFFFFFFu - (u32)key; }
-__device__ __forceinline__ float lp_value(u64 key) { const u32 u = (u32)(key >> 32); return __uint_as_float(u ^ ((i32)u < 0 ? 0x80000000u : 0xFFFFFFFFu)); }
-__device__ __forceinline__ u64 lp_shfl_xor(u64 v, int o) { return (u64)(u32)__shfl_xor((int)(v >> 32), o) << 32 | (u32)__shfl_xor((int)v, o); }
+__device__ __forceinline__ float lp_value(u32 high) { return __uint_as_float(high ^ ((i32)high < 0 ? 0x80000000u : 0xFFFFFFFFu)); }
+__device__ __forceinline__ u32 lp_below(u64 mask) { return __builtin_amdgcn_mbcnt_hi((u32)(mask >> 32), __builtin_amdgcn_mbcnt_lo((u32)mask, 0)); }     // bits of lower lanes
+// what lanes of a wave write to LDS for one another (in order in hardware; the compiler is told)
+__device__ __forceinline__ void lp_wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
-// The kth largest of the groups' largest keys (0: there are fewer), n = BLK_THREADS / lanes groups; `mine`: the lane's largest key.
-__device__ __forceinline__ u64 lp_kth(LogprobShared& sh, u64 mine, u32 k, u32 lanes) {
-  for (u32 o = 1; o < lanes; o <<= 1) { const u64 x = lp_shfl_xor(mine, (int)o); mine = x > mine ? x : mine; }
-  const u32 n = BLK_THREADS / lanes, i = threadIdx.x & (n - 1), per = n * n / BLK_THREADS;
-  __syncthreads();
+// A number that k keys of those the lanes have are not below, into sh.kth: the kth largest of the largest upper halves of groups of 16, 4 or 1 neighbouring
+// lanes, two groups at least for each of the k; `mine`: the lane's largest, 0 if it has none.
+template <typename Shared>
+__device__ __forceinline__ void lp_kth(Shared& sh, u32 mine, u32 k) {
+  u32 lanes = 1;
+#pragma unroll 1
+  while (lanes < 16 && 8 * k * lanes <= BLK_THREADS) {
+    mine = max(mine, (u32)__shfl_xor((int)mine, (int)lanes));
+    mine = max(mine, (u32)__shfl_xor((int)mine, (int)(2 * lanes)));
+    lanes *= 4;
+  }
+  const u32 n = BLK_THREADS / lanes;
   if (threadIdx.x % lanes == 0) sh.group[threadIdx.x / lanes] = mine;
-  sh.cnt[threadIdx.x] = 0;
-  if (threadIdx.x == 0) sh.T = 0;
+  if (threadIdx.x == 0) sh.kth = 0;
   __syncthreads();
-  const u64 key = sh.group[i];
-  if (per) {                                         // every lane a part of the comparisons
-    const u32 j0 = threadIdx.x / n * per;
-    u32 c = 0;
-    for (u32 j = j0; j < j0 + per; ++j) c += sh.group[j] > key ? 1u : 0u;
-    if (c) atomicAdd(&sh.cnt[i], c);
-  } else if (threadIdx.x < n * n && sh.group[threadIdx.x / n] > key) atomicAdd(&sh.cnt[i], 1u);
+  if (threadIdx.x < n) {
+    mine = sh.group[threadIdx.x];
+    u32 above = 0, not_below = 0;
+#pragma unroll 4
+    for (u32 j = 0; j < n; j += 4) {
+      const uint4 x = *(const uint4*)(sh.group + j);
+      above += (x.x > mine ? 1u : 0u) + (x.y > mine ? 1u : 0u) + (x.z > mine ? 1u : 0u) + (x.w > mine ? 1u : 0u);
+      not_below += (x.x >= mine ? 1u : 0u) + (x.y >= mine ? 1u : 0u) + (x.z >= mine ? 1u : 0u) + (x.w >= mine ? 1u : 0u);
+    }
+    if (above < k && not_below >= k) sh.kth = mine;  // (the same one from every lane that finds it)
+  }
   __syncthreads();
-  if (threadIdx.x < n && sh.cnt[threadIdx.x] == k - 1 && key) sh.T = key;
-  __syncthreads();
-  return sh.T;
 }
-// The min(k, n) largest of cand[0 .. n), in order, into top; 0 behind them.
-__device__ __forceinline__ void lp_select(LogprobShared& sh, u32 n, u32 k) {
-  while (n > LP_FEW) {
-    u64 best = 0;
-    for (u32 i = threadIdx.x; i < n; i += BLK_THREADS) best = sh.cand[i] > best ? sh.cand[i] : best;
-    const u64 T = lp_kth(sh, best, k, 1);
-    if (threadIdx.x == 0) sh.n = 0;
-    __syncthreads();
-    for (u32 i = threadIdx.x; i < n; i += BLK_THREADS)
-      if (sh.cand[i] >= T) sh.spare[atomicAdd(&sh.n, 1u)] = sh.cand[i];      // (of k lanes)
-    __syncthreads();
-    n = sh.n;
-    for (u32 i = threadIdx.x; i < n; i += BLK_THREADS) sh.cand[i] = sh.spare[i];
-    __syncthreads();
-  }
-  __syncthreads();
-  if (threadIdx.x < k) sh.top[threadIdx.x] = 0;
-  __syncthreads();
-  for (u32 i = threadIdx.x; i < n; i += BLK_THREADS) {
-    const u64 key = sh.cand[i];
+// Of the n <= LP_CAP keys of a wave's list those that are not below the kth, in the order they had; where more than LP_FEW have its logit or a larger
+// one, the k first. The kth one's upper half.
+__device__ __forceinline__ u32 lp_thin(u64* cand, u32& n, u32 k) {
+  constexpr u32 R = (LP_CAP + 63) / 64;
+  const u32 lane = threadIdx.x & 63;
+  lp_wave_sync();
+  u32 h[R];
+#pragma unroll
+  for (u32 r = 0; r < R; ++r) h[r] = r * 64 + lane < n ? (u32)(cand[r * 64 + lane] >> 32) : 0u;
+  u32 high = 0, low = 0, with = n;
+#pragma unroll 1
+  for (u32 b = 1u << 31; b; b >>= 1) {
+    const u32 up = high | b;
     u32 c = 0;
-    for (u32 j = 0; j < n; ++j) c += sh.cand[j] > key ? 1u : 0u;
-    if (c < k) sh.top[c] = key;
+#pragma unroll
+    for (u32 r = 0; r < R; ++r) c += (u32)__popcll(__ballot(h[r] >= up));
+    if (c >= k) { high = up; with = c; }
   }
-  __syncthreads();
+  if (with > LP_FEW) {
+    u32 need = k;
+#pragma unroll
+    for (u32 r = 0; r < R; ++r) need -= (u32)__popcll(__ballot(h[r] > high));
+#pragma unroll 1
+    for (u32 b = 1u << 31; b; b >>= 1) {
+      u32 c = 0;
+#pragma unroll 1
+      for (u32 i = lane; i - lane < n; i += 64) c += (u32)__popcll(__ballot(i < n && (u32)(cand[i] >> 32) == high && (u32)cand[i] >= (low | b)));
+      if (c >= need) low |= b;
+    }
+  }
+  const u64 least = (u64)high << 32 | low;
+  u32 m = 0;
+#pragma unroll 1
+  for (u32 i = lane; i - lane < n; i += 64) {
+    const u64 x = i < n ? cand[i] : 0;
+    const u64 mask = __ballot(i < n && x >= least);
+    if (i < n && x >= least) cand[m + lp_below(mask)] = x;       // (not behind what has been read)
+    m += (u32)__popcll(mask);
+  }
+  lp_wave_sync();
+  n = m;
+  return high;
 }
 
+// Sums about M = m c, or, where that is not finite and m is (a row with nothing but a mask's lowest values, for one), about m: y = (x - m) c.
 struct LpSums {
-  float m, s, t;                                     // maximum, sum 2^y, sum y 2^y of y = (x - m) c
-  __device__ __forceinline__ void to(float mn, float c) {      // the same with mn >= m for the maximum
-    if (m == -INFINITY) { m = mn; return; }          // (nothing yet: sums of 0, or NaN)
-    const float y = (m - mn) * c, f = __builtin_amdgcn_exp2f(y);
-    t = f > 0.f ? f * __builtin_fmaf(y, s, t) : 0.f; // (y may be -inf)
-    s *= f;
-    m = mn;
+  float m, s, t;                                     // sum 2^y, sum y 2^y
+  static __device__ __forceinline__ bool near(float M) { return fabsf(M) < INFINITY; }
+  __device__ __forceinline__ void to(float m2, float c) {      // the same about another m
+    if (m != -INFINITY && m2 != m) {                 // (nothing yet: sums of 0, or NaN)
+      const float M = m * c, M2 = m2 * c, y = near(M) && near(M2) ? M - M2 : (m - m2) * c, f = __builtin_amdgcn_exp2f(y);
+      t = f > 0.f ? f * __builtin_fmaf(y, s, t) : 0.f;         // (y may be -inf)
+      s *= f;
+    }
+    m = m2;
   }
-  __device__ __forceinline__ void add(float m2, float s2, float t2, float c) {
-    LpSums o = {m2, s2, t2};
-    const float mn = fmaxf(m, m2);
-    to(mn, c); o.to(mn, c);
+  __device__ __forceinline__ void add(LpSums o, float c) {
+    const float m2 = fmaxf(m, o.m);
+    to(m2, c); o.to(m2, c);
     s += o.s; t += o.t;
   }
 };
-
-template <typename T>
-__device__ __forceinline__ void lp_load(float (&x)[LP_VALS], const T* base, u32 at, u32 begin, u32 end, bool whole) {
-  constexpr u32 VEC = 16 / sizeof(T), NV = LP_VALS / VEC;
-  typedef T vec_t __attribute__((ext_vector_type(VEC)));
+__device__ __forceinline__ float lp_wave_max(float v) {
 #pragma unroll
-  for (u32 v = 0; v < NV; ++v) {
-    const u32 i = at + (v * BLK_THREADS + threadIdx.x) * VEC;
-    if (whole || (i >= begin && i + VEC <= end)) {
-      const vec_t y = __builtin_nontemporal_load((const vec_t*)(base + i));
+  for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+__device__ __forceinline__ float lp_wave_sum(float v) {
 #pragma unroll
-      for (u32 j = 0; j < VEC; ++j) x[v * VEC + j] = (float)y[j];
-    } else {
-#pragma unroll
-      for (u32 j = 0; j < VEC; ++j) x[v * VEC + j] = i + j >= begin && i + j < end ? (float)base[i + j] : -INFINITY;
-    }
-  }
+  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+  return v;
 }
 
+// A tile as it lies in memory: 16 bytes a lane, then the next 64 times 16.
+template <typename T>
+struct LpTile {
+  static constexpr u32 VEC = 16 / sizeof(T), NV = LP_VALS / VEC;
+  typedef T vec_t __attribute__((ext_vector_type(VEC)));
+  vec_t v[NV];
+  static __device__ __forceinline__ u32 element(u32 j) { return (j / VEC * 64 + (threadIdx.x & 63)) * VEC + j % VEC; }
+  __device__ __forceinline__ void load(const T* base, u32 at, u32 begin, u32 end) {
+    if (at >= begin && at + LP_TILE <= end) {
+#pragma unroll
+      for (u32 i = 0; i < NV; ++i) v[i] = __builtin_nontemporal_load((const vec_t*)(base + at + element(i * VEC)));
+    } else {                                         // elements outside [begin, end) are not read: -inf
+#pragma unroll
+      for (u32 i = 0; i < NV; ++i) {
+        const u32 e = at + element(i * VEC);
+#pragma unroll
+        for (u32 j = 0; j < VEC; ++j) v[i][j] = e + j >= begin && e + j < end ? base[e + j] : (T)-INFINITY;
+      }
+    }
+  }
+  __device__ __forceinline__ float get(u32 j) const { return (float)v[j / VEC][j % VEC]; }
+};
+
 template <typename T, bool TOP>
-__device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShared& sh, u32 wg) {
-  constexpr u32 VEC = 16 / sizeof(T);
-  const u32 row = wg / a.parts, part = wg - row * a.parts, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+__device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShared<TOP>& sh, u32 wg) {
+  typedef LpTile<T> Tile;
+  const u32 row = wg / a.parts, part = wg - row * a.parts, lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // the row's elements are [shift, end) of what begins at the 16 bytes its first one lies in
   const T* const first = (const T*)a.x + (u64)row * a.stride;
   const u32 shift = (u32)((u64)first % 16 / sizeof(T)), end = shift + a.V;
   const T* const base = first - shift;
-  const u32 tiles = (end + LP_TILE - 1) / LP_TILE, tile0 = (u32)((u64)tiles * part / a.parts), tile1 = (u32)((u64)tiles * (part + 1) / a.parts);
+  const u32 tiles = (end + LP_TILE - 1) / LP_TILE, tile0 = (u32)((u64)tiles * part / a.parts) + w, tile1 = (u32)((u64)tiles * (part + 1) / a.parts);
+  Tile ahead;
+  if (tile0 < tile1) ahead.load(base, tile0 * LP_TILE, shift, end);
   const float inverse = a.inverse ? a.inverse[row] : 1.f;
   float c = inverse * 1.44269504088896340736f;
   if (!(inverse > 0.f) || !(c < INFINITY)) c = __uint_as_float(0x7FC00000u);
-  if (threadIdx.x < a.given) {
-    const i32 t = a.tokens[(u64)row * a.given + threadIdx.x];
-    const bool in = t >= 0 && (u32)t < a.V;
-    sh.token[threadIdx.x] = in ? t : -1;
-    sh.given[threadIdx.x] = in ? lp_ordered((float)first[t]) : 0.f;
-    sh.before[threadIdx.x] = 0;
+  i32 token = -1;                                    // the lane's given token, its logit, and how many come before it
+  float given = 0.f;
+  u32 before = 0;
+  if (lane < a.given) {
+    const i32 t = a.tokens[(u64)row * a.given + lane];
+    if (t >= 0 && (u32)t < a.V) { token = t; given = lp_ordered((float)first[t]); }
   }
-  if (threadIdx.x == 0) sh.n = 0;
-  __syncthreads();
-  LpSums sum = {-INFINITY, 0.f, 0.f};
-  u32 lanes = 1;                                     // of a group, so that no tile adds more than LP_NEW keys
-  while (TOP && 2 * lanes * a.k <= LP_MOST) lanes *= 2;
-  u64 least = 0;                                     // k keys at least are not below this one
-  float over = 0.f;                                  // its logit
+  LpSums sum = {-INFINITY, 0.f, 0.f};                // (m: the wave's, sums: the lane's)
+  u64* const cand = sh.cand + (TOP ? w * LP_CAP : 0);
   u32 n = 0;                                         // keys in cand
+  float over = -INFINITY;                            // a bound: k logits of earlier tiles at least are not below it
+  if constexpr (TOP) {
+    float most = -INFINITY;
+    if (tile0 < tile1) {
+#pragma unroll
+      for (u32 j = 0; j < LP_VALS; ++j) most = fmaxf(most, ahead.get(j));
+    }
+    lp_kth(sh, lp_high(most), a.k);
+    over = sh.kth ? lp_value(sh.kth) : -INFINITY;
+  }
 #pragma unroll 1
-  for (u32 tile = tile0; tile < tile1; ++tile) {
+  for (u32 tile = tile0; tile < tile1; tile += LP_WAVES) {
     const u32 at = tile * LP_TILE;
     const bool whole = at >= shift && at + LP_TILE <= end;
     float x[LP_VALS];
-    lp_load<T>(x, base, at, shift, end, whole);
-    auto id = [&](u32 j) { return at + (j / VEC * BLK_THREADS + threadIdx.x) * VEC + j % VEC - shift; };
+#pragma unroll
+    for (u32 j = 0; j < LP_VALS; ++j) x[j] = ahead.get(j);
+    if (tile + LP_WAVES < tile1) ahead.load(base, at + LP_WAVES * LP_TILE, shift, end);
+    auto id = [&](u32 j) { return at + Tile::element(j) - shift; };
     auto valid = [&](u32 j) { return whole || id(j) < a.V; };      // (before the row: beyond 2^31)
     float most = -INFINITY;
 #pragma unroll
     for (u32 j = 0; j < LP_VALS; ++j) most = fmaxf(most, x[j]);
-    sum.to(fmaxf(sum.m, most), c);
-    const float ref = sum.m == -INFINITY ? 0.f : sum.m;
-#pragma unroll
-    for (u32 j = 0; j < LP_VALS; ++j) {
-      const float y = (x[j] - ref) * c, e = __builtin_amdgcn_exp2f(y);
-      sum.s += e;
-      sum.t = __builtin_fmaf(fmaxf(y, LP_LOWEST), e, sum.t);         // (0 times -inf is to be 0)
+    float M = sum.m * c;
+    if (__ballot(LpSums::near(M) ? most * c > M + 2.f : most > sum.m)) {
+      sum.to(fmaxf(sum.m, lp_wave_max(most)), c);
+      M = sum.m * c;
     }
+    float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};      // (chains of a few sums: a row of one probable token loses little to rounding)
+    auto add = [&](u32 j, float y) {
+      const float e = __builtin_amdgcn_exp2f(y);
+      s[j & 3] += e;
+      t[j & 3] = __builtin_fmaf(fmaxf(y, LP_LOWEST), e, t[j & 3]);     // (0 times -inf is to be 0)
+    };
+    if (LpSums::near(M)) {
+#pragma unroll
+      for (u32 j = 0; j < LP_VALS; ++j) add(j, __builtin_fmaf(x[j], c, -M));
+    } else {
+      const float m = sum.m == -INFINITY ? 0.f : sum.m;
+#pragma unroll
+      for (u32 j = 0; j < LP_VALS; ++j) add(j, (x[j] - m) * c);
+    }
+    sum.s += (s[0] + s[1]) + (s[2] + s[3]);
+    sum.t += (t[0] + t[1]) + (t[2] + t[3]);
     if (a.ranks) {
 #pragma unroll 1
       for (u32 g = 0; g < a.given; ++g) {
-        const u32 t = (u32)__builtin_amdgcn_readfirstlane(sh.token[g]);
-        const float y = __uint_as_float((u32)__builtin_amdgcn_readfirstlane((i32)__float_as_uint(sh.given[g])));
-        u32 before = 0;
-        if (!whole || (t + shift >= at && t + shift < at + LP_TILE)) {
+        const u32 tk = (u32)__builtin_amdgcn_readlane(token, (int)g);
+        const float y = __uint_as_float((u32)__builtin_amdgcn_readlane((i32)__float_as_uint(given), (int)g));
+        u32 mine = 0;
+        if (!whole || y == -INFINITY || (tk + shift >= at && tk + shift < at + LP_TILE)) {
 #pragma unroll
-          for (u32 j = 0; j < LP_VALS; ++j) { const float o = lp_ordered(x[j]); before += (u32)__popcll(__ballot(valid(j) && (o > y || (o == y && id(j) < t)))); }
-        } else if (t + shift < at) {
+          for (u32 j = 0; j < LP_VALS; ++j) { const float o = lp_ordered(x[j]); mine += valid(j) && (o > y || (o == y && id(j) < tk)) ? 1u : 0u; }
+        } else if (tk + shift < at) {
 #pragma unroll
-          for (u32 j = 0; j < LP_VALS; ++j) before += (u32)__popcll(__ballot(x[j] > y));
+          for (u32 j = 0; j < LP_VALS; ++j) mine += x[j] > y ? 1u : 0u;
         } else {
 #pragma unroll
-          for (u32 j = 0; j < LP_VALS; ++j) before += (u32)__popcll(__ballot(lp_ordered(x[j]) >= y));
+          for (u32 j = 0; j < LP_VALS; ++j) mine += x[j] >= y ? 1u : 0u;
         }
-        if (lane == 0) atomicAdd(&sh.before[g], before);
+        u32 more = 0;                                // of the wave: at most 16 each, bit by bit
+#pragma unroll
+        for (u32 b = 0; b < 5; ++b) more += (u32)__popcll(__ballot(mine >> b & 1u)) << b;
+        before += lane == g ? more : 0u;
       }
     }
     if constexpr (TOP) {
-      // the keys of this tile that `take` names, behind the first n of cand; how many there are then (more than fit: none of the rest is there)
-      auto append = [&](auto take) {
-        u32 mine = 0;
-#pragma unroll
-        for (u32 j = 0; j < LP_VALS; ++j) mine += take(j) ? 1u : 0u;
-        if (mine) {
-          u32 to = atomicAdd(&sh.n, mine);
-#pragma unroll
-          for (u32 j = 0; j < LP_VALS; ++j)
-            if (take(j)) { if (to < LP_CAP) sh.cand[to] = lp_key(x[j], id(j)); ++to; }
-        }
-        __syncthreads();
-        return sh.n;
+      auto append = [&](u32 j, bool take) {
+        const u64 mask = __ballot(take);
+        if (!mask) return;
+        if (take) cand[n + lp_below(mask)] = lp_key(x[j], id(j));
+        n += (u32)__popcll(mask);
       };
-      u32 now = LP_CAP + 1;
-      if (tile != tile0) now = append([&](u32 j) { return x[j] > over; });      // (equal ones have the higher ids)
-      if (now > LP_CAP) {
-        u64 best = 0;
+      if (tile == tile0) {
 #pragma unroll
-        for (u32 j = 0; j < LP_VALS; ++j)
-          if (lp_ordered(x[j]) == most && valid(j) && !best) best = lp_key(x[j], id(j));
-        const u64 kth = lp_kth(sh, best, a.k, lanes);
-        least = kth > least ? kth : least;
-        over = lp_value(least);
-        if (threadIdx.x == 0) sh.n = n;
-        __syncthreads();
-        now = append([&](u32 j) { return valid(j) && lp_key(x[j], id(j)) >= least; });
+        for (u32 j = 0; j < LP_VALS; ++j) append(j, valid(j) && lp_ordered(x[j]) >= over);
+      } else {
+#pragma unroll
+        for (u32 j = 0; j < LP_VALS; ++j) append(j, x[j] > over);
       }
-      n = now;
-      if (n > LP_FEW && tile + 1 < tile1) {
-        lp_select(sh, n, a.k);
-        n = a.k;
-        for (u32 i = threadIdx.x; i < n; i += BLK_THREADS) sh.cand[i] = sh.top[i];
-        least = sh.top[a.k - 1];
-        over = lp_value(least);
-        if (threadIdx.x == 0) sh.n = n;
-      }
-      __syncthreads();                               // (before the next tile adds to sh.n)
+      if (n > LP_FEW) over = lp_value(lp_thin(cand, n, a.k));
     }
   }
-  // the workgroup's sums
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) sum.add(__shfl_xor(sum.m, o), __shfl_xor(sum.s, o), __shfl_xor(sum.t, o), c);
+  // the workgroup's: sums of its waves, keys ranked
+  sum.s = lp_wave_sum(sum.s); sum.t = lp_wave_sum(sum.t);
   if (lane == 0) { sh.m[w] = sum.m; sh.s[w] = sum.s; sh.t[w] = sum.t; }
-  if constexpr (TOP) lp_select(sh, n, a.k);
+  if (lane < a.given) sh.before[w][lane] = before;
   __syncthreads();
   sum = {sh.m[0], sh.s[0], sh.t[0]};
 #pragma unroll
-  for (int i = 1; i < 4; ++i) sum.add(sh.m[i], sh.s[i], sh.t[i], c);
+  for (u32 i = 1; i < LP_WAVES; ++i) sum.add({sh.m[i], sh.s[i], sh.t[i]}, c);
+  if (lane < a.given) {
+    before = 0;
+#pragma unroll
+    for (u32 i = 0; i < LP_WAVES; ++i) before += sh.before[i][lane];
+  }
+  // the first k of all waves' lists, in order, into top; 0 behind them
+  auto first_k = [&]() {
+    u32 best = 0;
+#pragma unroll 1
+    for (u32 i = lane; i < n; i += 64) best = max(best, (u32)(cand[i] >> 32));
+    lp_kth(sh, best, a.k);
+    u32 m = 0;
+    const u32 kth = sh.kth;
+#pragma unroll 1
+    for (u32 i = lane; i - lane < n; i += 64) {
+      const u64 x = i < n ? cand[i] : 0, mask = __ballot(x && (u32)(x >> 32) >= kth);
+      if (x && (u32)(x >> 32) >= kth) cand[m + lp_below(mask)] = x;
+      m += (u32)__popcll(mask);
+    }
+    if (lane < 4) cand[m + lane] = 0;
+    if (lane == 0) sh.n[w] = m;
+    if (threadIdx.x < LP_MOST) sh.top[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (u32 i = lane; i < m; i += 64) {
+      const u64 key = cand[i];
+      u32 place = 0;
+#pragma unroll 1
+      for (u32 l = 0; l < LP_WAVES; ++l) {
+        const u64* const x = sh.cand + l * LP_CAP;
+        const u32 end = sh.n[l];
+#pragma unroll 1
+        for (u32 j = 0; j < end; j += 4) {
+#pragma unroll
+          for (u32 h = 0; h < 4; ++h) place += x[j + h] > key ? 1u : 0u;
+        }
+      }
+      if (place < a.k) sh.top[place] = key;
+    }
+    __syncthreads();
+  };
+  if constexpr (TOP) first_k();
   if (a.parts > 1) {
     // a part's result past the caches (other workgroups' caches are not this one's); the last part to come adds them up, in their order
     const u32 words = lp_words(a.given, a.k), key0 = lp_key_word(a.given);
     u32* const mine = a.results + (u64)wg * words;
     auto put = [&](u32 i, u32 v) { __hip_atomic_store(mine + i, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
     if (threadIdx.x == 0) { put(0, __float_as_uint(sum.m)); put(1, __float_as_uint(sum.s)); put(2, __float_as_uint(sum.t)); }
-    if (threadIdx.x < a.given) put(4 + threadIdx.x, sh.before[threadIdx.x]);
+    if (threadIdx.x < a.given) put(4 + threadIdx.x, before);
     if (TOP && threadIdx.x < a.k) __hip_atomic_store((u64*)(mine + key0) + threadIdx.x, sh.top[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
     __syncthreads();
@@ -273,35 +366,38 @@ __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShar
     if (!sh.last) return;
     const u32* const all = a.results + (u64)row * a.parts * words;
     auto get = [&](u32 p, u32 i) { return __hip_atomic_load(all + (u64)p * words + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-    // (a lane a part, added up as the lanes of a wave are)
-    sum = {-INFINITY, 0.f, 0.f};
+    if constexpr (TOP) {
+      // (a quarter of the keys a wave)
+      const u32 per = (a.parts * a.k + LP_WAVES - 1) / LP_WAVES, i0 = min(w * per, a.parts * a.k), i1 = min(i0 + per, a.parts * a.k);
+      n = i1 - i0;
+      for (u32 i = lane; i < n; i += 64) {
+        const u32 p = (i0 + i) / a.k;
+        cand[i] = __hip_atomic_load((const u64*)(all + (u64)p * words + key0) + (i0 + i - p * a.k), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    }
+    sum = {-INFINITY, 0.f, 0.f};                     // (a lane a part)
     if (lane < a.parts) sum = {__uint_as_float(get(lane, 0)), __uint_as_float(get(lane, 1)), __uint_as_float(get(lane, 2))};
     if (threadIdx.x < a.given) {
-      u32 before = 0;
+      before = 0;
       for (u32 p = 0; p < a.parts; ++p) before += get(p, 4 + threadIdx.x);
-      sh.before[threadIdx.x] = before;
     }
-    if constexpr (TOP) {
-      n = a.parts * a.k;
-      for (u32 i = threadIdx.x; i < n; i += BLK_THREADS)
-        sh.cand[i] = __hip_atomic_load((const u64*)(all + (u64)(i / a.k) * words + key0) + i % a.k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum.add(__shfl_xor(sum.m, o), __shfl_xor(sum.s, o), __shfl_xor(sum.t, o), c);
-    __syncthreads();
-    if constexpr (TOP) lp_select(sh, n, a.k);
+    sum.to(lp_wave_max(sum.m), c);
+    sum.s = lp_wave_sum(sum.s); sum.t = lp_wave_sum(sum.t);
+    if constexpr (TOP) first_k();
   }
-  const float log_sum = logf(sum.s);
-  auto logprob = [&](float x) { return __builtin_fmaf(x - sum.m, inverse, -log_sum); };
-  if (threadIdx.x == 0 && a.entropy) a.entropy[row] = log_sum - 0.69314718055994530942f * sum.t / sum.s;
+  const float log_sum = log2f(sum.s), M = sum.m * c;
+  auto logprob = [&](float x) {
+    const float y = LpSums::near(M) ? __builtin_fmaf(x, c, -M) : (x - sum.m) * c;
+    return y == -INFINITY ? (x - sum.m) * inverse - LP_LN2 * log_sum : LP_LN2 * (y - log_sum);      // (a mask's lowest value may overflow in y)
+  };
+  if (threadIdx.x == 0 && a.entropy) a.entropy[row] = LP_LN2 * (log_sum - sum.t / sum.s);
   if (threadIdx.x < a.given) {
-    const i32 t = sh.token[threadIdx.x];
-    a.logprobs[(u64)row * a.given + threadIdx.x] = t < 0 ? 0.f : logprob(sh.given[threadIdx.x]);
-    if (a.ranks) a.ranks[(u64)row * a.given + threadIdx.x] = t < 0 ? -1 : (i32)sh.before[threadIdx.x];
+    a.logprobs[(u64)row * a.given + threadIdx.x] = token < 0 ? 0.f : logprob(given);
+    if (a.ranks) a.ranks[(u64)row * a.given + threadIdx.x] = token < 0 ? -1 : (i32)before;
   }
   if (TOP && threadIdx.x < a.k) {
     const u64 key = sh.top[threadIdx.x];
     a.top_ids[(u64)row * a.k + threadIdx.x] = (i32)lp_id(key);
-    a.top_logprobs[(u64)row * a.k + threadIdx.x] = logprob(lp_value(key));
+    a.top_logprobs[(u64)row * a.k + threadIdx.x] = logprob(lp_value((u32)(key >> 32)));
   }
 }

@@ -147,9 +147,9 @@ extern "C" int blink_kv_cache_copy(int32_t device, const blink_kv_cache* caches,
 }
 
 // ---- log probabilities ----------------------------------------------------------------------------------------------------------
-// workgroups of a row: LP_PER_CU for every compute unit in all, a tile each at least
+// workgroups of a row: LP_PER_CU for every compute unit in all, a tile for each of their waves at least
 static u32 logprob_parts(u32 rows, u32 vocab, u32 n_cu) {
-  const u32 tiles = (vocab + LP_TILE - 1) / LP_TILE;
+  const u32 tiles = (vocab + LP_WAVES * LP_TILE - 1) / (LP_WAVES * LP_TILE);
   const u64 want = ((u64)LP_PER_CU * n_cu + rows - 1) / rows;
   return rows > LP_CTR_BYTES / 4 ? 1u : (u32)std::min<u64>({want, tiles, LP_MAX_PARTS});
 }
