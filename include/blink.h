@@ -412,6 +412,24 @@ int blink_paged_attention(int32_t device, const blink_paged_attention_args* args
 /* What blink_paged_attention needs for any call with these numbers (and any smaller max_q or n_seqs). */
 int blink_attention_workspace_bytes(int32_t device, const blink_kv_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t max_q, uint64_t* bytes);
 
+/* blink_paged_attention of a batch in which the sequences of a group have their first blocks in common (samples and beams of one prompt, a system prompt
+ * that a prefix cache holds once): the keys in those are read and multiplied once for the group, with the queries of all of its sequences as rows. Group i
+ * is the sequences group_starts[i] .. group_starts[i + 1] (not decreasing; those before the first and behind the last one are in none), whose
+ * block tables agree in the blocks of the first shared_lens[i] tokens. Everything else is as for blink_paged_attention, and so are the
+ * results, but for the order of summation: a group saves work, and changes nothing. A sequence whose queries do not all stand behind the
+ * shared tokens, or do not see all of them (a window), or which has many queries, is taken by itself. What comes out where tables do not agree,
+ * or group_starts decrease, is not defined; nothing outside the tensors is read or written then either. BLINK_ERR_TOO_LARGE with more than
+ * 1024 sequences and groups together. */
+typedef struct {
+  blink_paged_attention_args attention;
+  uint32_t n_groups;           /* 0: blink_paged_attention */
+  const int32_t *group_starts, *shared_lens;             /* [n_groups + 1], [n_groups] */
+} blink_shared_attention_args;
+int blink_shared_attention(int32_t device, const blink_shared_attention_args* args, void* stream);
+/* What blink_shared_attention needs for any call with these numbers, and any smaller n_seqs, n_groups, n_tokens or max_q. */
+int blink_shared_attention_workspace_bytes(int32_t device, const blink_kv_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t n_groups, uint32_t n_tokens, uint32_t max_q,
+                                           uint64_t* bytes);
+
 /* Log probabilities of given tokens, the entropy and the most probable tokens, from rows of logits x (device memory, where blink_sample_rows' rows are the
  * host's). With z = x inverse_temperature[row]: log p = z - log sum exp(z). Of row r, for each of the n_given tokens: logprobs = log p, ranks = how
  * many tokens come before it, larger logits first, of equal ones the lower id (the most probable one: 0). A token outside [0, vocab), as in

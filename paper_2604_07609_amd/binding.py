@@ -16,7 +16,8 @@ EVENT_FIRST, EVENT_LAST = 1, 2
 EXPORTS = ["blink_init", "blink_init_attention", "blink_submit", "blink_run", "blink_set_exit_when_idle", "blink_wait", "blink_stop", "blink_poll_outputs", "blink_shutdown",
            "blink_get_trace", "blink_get_stats", "blink_debug_read", "blink_time_phase", "blink_get_phase_times", "blink_calibration_copy",
            "blink_calibration_rates", "blink_clock_sync", "blink_sample_rows", "blink_sample_rows_static", "blink_kv_cache_bytes", "blink_qk_norm_rope",
-           "blink_kv_cache_read", "blink_kv_cache_copy", "blink_token_logprobs", "blink_token_logprobs_workspace_bytes", "blink_paged_attention", "blink_attention_workspace_bytes", "blink_last_error"]
+           "blink_kv_cache_read", "blink_kv_cache_copy", "blink_token_logprobs", "blink_token_logprobs_workspace_bytes", "blink_paged_attention", "blink_attention_workspace_bytes",
+           "blink_shared_attention", "blink_shared_attention_workspace_bytes", "blink_last_error"]
 
 
 class DBG:
@@ -58,13 +59,18 @@ class PagedAttentionArgs(C.Structure):
         (n, C.c_void_p) for n in ("cu_seqlens", "seq_lens", "block_tables", "workspace")] + [("workspace_bytes", C.c_uint64)]
 
 
+class SharedAttentionArgs(C.Structure):
+    _fields_ = [("attention", PagedAttentionArgs), ("n_groups", C.c_uint32), ("group_starts", C.c_void_p), ("shared_lens", C.c_void_p)]
+
+
 class TokenLogprobsArgs(C.Structure):
     _fields_ = [(n, C.c_uint32) for n in ("type", "n_rows", "vocab", "n_given", "k")] + [("logits", C.c_void_p), ("stride", C.c_uint64)] + [
         (n, C.c_void_p) for n in ("tokens", "inverse_temperature", "logprobs", "ranks", "entropy", "top_ids", "top_logprobs", "workspace")] + [("workspace_bytes", C.c_uint64)]
 
 
-# the same four as `struct` packs them (fields in order, native alignment)
+# the same five as `struct` packs them (fields in order, native alignment)
 _CACHE, _QK_NORM_ROPE, _PAGED_ATTENTION = struct.Struct("@P4I"), struct.Struct("@P4I4I3P3Q6PQ2f"), struct.Struct("@P4I7If2P2Q4PQ")
+_GROUPS = struct.Struct("@I2P")                        # of _SHARED_ATTENTION, behind _PAGED_ATTENTION
 _TOKEN_LOGPROBS = struct.Struct("@5IPQ8PQ")
 
 
@@ -135,6 +141,8 @@ def load_library():
     lib.blink_token_logprobs.argtypes = [C.c_int32, vp, vp]
     lib.blink_token_logprobs_workspace_bytes.argtypes = [C.c_int32, u32, u32, u32, u32, C.POINTER(u64)]
     lib.blink_paged_attention.argtypes = [C.c_int32, vp, vp]
+    lib.blink_shared_attention.argtypes = [C.c_int32, vp, vp]
+    lib.blink_shared_attention_workspace_bytes.argtypes = [C.c_int32, vp, u32, u32, u32, u32, u32, C.POINTER(u64)]
     lib.blink_attention_workspace_bytes.argtypes = [C.c_int32, vp, u32, u32, u32, C.POINTER(u64)]
     lib.blink_last_error.restype = C.c_char_p
     for n in EXPORTS[:-1]:
@@ -287,10 +295,9 @@ def attention_workspace_bytes(n_q_heads, cache, n_seqs, max_q=1):
     return n.value
 
 
-def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q=1, window=0, sinks=0, scale=1.0, stream=None):
-    """blink_paged_attention: q, out float16 [tokens, q heads, hd]; int32 block_tables [seqs, blocks], seq_lens [seqs], cu_seqlens
-    [seqs + 1]; workspace: a contiguous tensor of attention_workspace_bytes(...) bytes. stream: as for qk_norm_rope."""
-    lib, dev, hd = _lib or load_library(), cache.device, cache.head_dim
+def _attention_args(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q, window, sinks, scale):
+    """The packed blink_paged_attention_args."""
+    dev, hd = cache.device, cache.head_dim
     if len(q.shape) != 3 or len(block_tables.shape) != 2:
         raise ValueError(f"q must have three dimensions and block_tables two; they have {tuple(q.shape)} and {tuple(block_tables.shape)}")
     T, nq = q.shape[0], q.shape[1]
@@ -301,10 +308,38 @@ def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace
     op, os_ = _rows("out", out, (T, nq, hd), dev)
     if workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous and on device {dev}; it is on device {workspace.get_device()}")
-    a = _PAGED_ATTENTION.pack(*cache._packed, nq, S, T, max_q, width, window, sinks, scale, qp, op, qs, os_, _dense("cu_seqlens", cu_seqlens, _INT, (S + 1,), dev),
-                              _dense("seq_lens", seq_lens, _INT, (S,), dev), _dense("block_tables", block_tables, _INT, (S, width), dev), workspace.data_ptr(),
-                              workspace.numel() * workspace.element_size())
+    return _PAGED_ATTENTION.pack(*cache._packed, nq, S, T, max_q, width, window, sinks, scale, qp, op, qs, os_, _dense("cu_seqlens", cu_seqlens, _INT, (S + 1,), dev),
+                                 _dense("seq_lens", seq_lens, _INT, (S,), dev), _dense("block_tables", block_tables, _INT, (S, width), dev), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size())
+
+
+def paged_attention(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q=1, window=0, sinks=0, scale=1.0, stream=None):
+    """blink_paged_attention: q, out float16 [tokens, q heads, hd]; int32 block_tables [seqs, blocks], seq_lens [seqs], cu_seqlens
+    [seqs + 1]; workspace: a contiguous tensor of attention_workspace_bytes(...) bytes. stream: as for qk_norm_rope."""
+    lib, dev = _lib or load_library(), cache.device
+    a = _attention_args(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q, window, sinks, scale)
     rc = lib.blink_paged_attention(dev, a, _stream(stream, q, dev))
+    if rc:
+        _check(lib, rc)
+
+
+def shared_attention_workspace_bytes(n_q_heads, cache, n_seqs, n_groups, n_tokens, max_q=1):
+    """Bytes of the workspace of shared_attention for up to n_seqs sequences in n_groups groups with n_tokens queries in all, up to max_q each. Its
+    first 8 KiB hold zeros before its first call; calls of any shapes, paged_attention's too, may share one in turn."""
+    lib, n = load_library(), C.c_uint64()
+    _check(lib, lib.blink_shared_attention_workspace_bytes(cache.device, C.byref(cache.desc), n_q_heads, n_seqs, n_groups, n_tokens, max_q, C.byref(n)))
+    return n.value
+
+
+def shared_attention(q, cache, block_tables, seq_lens, cu_seqlens, group_starts, shared_lens, out, workspace, max_q=1, window=0, sinks=0, scale=1.0, stream=None):
+    """blink_shared_attention: paged_attention of a batch whose sequences group_starts[i] .. group_starts[i + 1] have the blocks of their first shared_lens[i]
+    tokens in common; int32 group_starts [groups + 1], shared_lens [groups]; workspace: a contiguous tensor of
+    shared_attention_workspace_bytes(...) bytes. stream: as for qk_norm_rope."""
+    lib, dev = _lib or load_library(), cache.device
+    n = shared_lens.shape[0]
+    a = _attention_args(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q, window, sinks, scale) + _GROUPS.pack(
+        n, _dense("group_starts", group_starts, _INT, (n + 1,), dev), _dense("shared_lens", shared_lens, _INT, (n,), dev))
+    rc = lib.blink_shared_attention(dev, a, _stream(stream, q, dev))
     if rc:
         _check(lib, rc)
 

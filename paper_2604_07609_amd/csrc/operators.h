@@ -268,17 +268,24 @@ static hipError_t launch_paged(const PagedArgs& args, const PagedPlan& plan, hip
   return e == hipSuccess && plan.n_splits > 1 ? launch(k_paged_merge<HD>, plan.wgs, 512, st, args, plan.wgs) : e;
 }
 
-extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention_args* a, void* stream) {
-  g_err.clear();
-  if (!a) return fail(BLINK_ERR_INVAL, "null argument");
+static void fill_paged(PagedArgs& p, const blink_paged_attention_args* a, float scale2, u32 short_rows, u32 n_splits, u32 n_cu) {
+  p.q = (const f16_t*)a->q; p.qs = a->q_stride; p.out = (f16_t*)a->out; p.os = a->out_stride; p.cu = a->cu_seqlens; p.lens = a->seq_lens;
+  p.tables = (const u32*)a->block_tables; p.cache = a->cache.data; p.n_blocks = a->cache.n_blocks; p.max_blocks = a->max_blocks;
+  p.nq = a->n_q_heads; p.nkv = a->cache.n_kv_heads; p.G = p.nq / p.nkv; p.n_seqs = a->n_seqs; p.n_tokens = a->n_tokens; p.max_q = a->max_q;
+  p.window = a->window; p.sinks = a->sinks; p.c = scale2; p.short_rows = short_rows; p.n_splits = n_splits;
+  p.ctr = (u32*)a->workspace; p.part = (float*)((char*)a->workspace + paged_ctr_bytes(n_cu));
+}
+// (nothing: the call has nothing to do)
+static int check_attention(const blink_paged_attention_args* a, float* scale2, bool* nothing) {
   if (int rc = check_heads(a->cache, a->n_q_heads)) return rc;
   if (int rc = paged_check(a->cache, a->n_q_heads, a->n_seqs, a->max_q)) return rc;
   const u32 hd = a->cache.head_dim, nkv = a->cache.n_kv_heads;
-  const float scale2 = a->scale * 1.44269504088896340736f;      // (scores as powers of two)
-  if (!(a->scale > 0.f) || !(scale2 < INFINITY)) return fail(BLINK_ERR_INVAL, "scale must be positive, and finite times log2(e)");
+  *scale2 = a->scale * 1.44269504088896340736f;      // (scores as powers of two)
+  if (!(a->scale > 0.f) || !(*scale2 < INFINITY)) return fail(BLINK_ERR_INVAL, "scale must be positive, and finite times log2(e)");
   if (a->sinks && !a->window) return fail(BLINK_ERR_INVAL, "sinks without a window");
   if (a->window > (1u << 30) || a->sinks > (1u << 30)) return fail(BLINK_ERR_INVAL, "window and sinks must be at most 2^30");
-  if (a->n_seqs == 0 || a->n_tokens == 0) return BLINK_OK;
+  *nothing = a->n_seqs == 0 || a->n_tokens == 0;
+  if (*nothing) return BLINK_OK;
   if (!a->max_blocks || a->max_blocks > (1u << 26)) return fail(BLINK_ERR_INVAL, "max_blocks must be in [1, 2^26]");
   if ((u64)a->n_seqs * a->max_blocks * nkv >= (1ull << 31)) return fail(BLINK_ERR_TOO_LARGE, "2^31 blocks of keys or more in one call");
   if ((u64)a->n_tokens * a->n_q_heads >= (1ull << 31)) return fail(BLINK_ERR_TOO_LARGE, "2^31 rows or more");
@@ -286,6 +293,17 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   if (int rc = check_rows("out", a->out, a->out_stride, (u64)a->n_q_heads * hd, 2)) return rc;
   if (!a->cu_seqlens || !a->seq_lens || !a->block_tables) return fail(BLINK_ERR_INVAL, "cu_seqlens, seq_lens and block_tables must not be null");
   if ((u64)a->cu_seqlens % 4 || (u64)a->seq_lens % 4 || (u64)a->block_tables % 4) return fail(BLINK_ERR_INVAL, "cu_seqlens, seq_lens and block_tables must be aligned to 4 bytes");
+  return BLINK_OK;
+}
+
+extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention_args* a, void* stream) {
+  g_err.clear();
+  if (!a) return fail(BLINK_ERR_INVAL, "null argument");
+  float scale2;
+  bool nothing;
+  if (int rc = check_attention(a, &scale2, &nothing)) return rc;
+  if (nothing) return BLINK_OK;
+  const u32 hd = a->cache.head_dim, nkv = a->cache.n_kv_heads;
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
   const u64 reach = a->window ? (u64)a->window + a->max_q + a->sinks : ~0ull;
@@ -296,13 +314,90 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   OnDevice on(device);
   HIPCHK(on.err);
   PagedArgs p{};
-  p.q = (const f16_t*)a->q; p.qs = a->q_stride; p.out = (f16_t*)a->out; p.os = a->out_stride; p.cu = a->cu_seqlens; p.lens = a->seq_lens;
-  p.tables = (const u32*)a->block_tables; p.cache = a->cache.data; p.n_blocks = a->cache.n_blocks; p.max_blocks = a->max_blocks;
-  p.nq = a->n_q_heads; p.nkv = nkv; p.G = p.nq / nkv; p.n_seqs = a->n_seqs; p.n_tokens = a->n_tokens; p.max_q = a->max_q;
-  p.window = a->window; p.sinks = a->sinks; p.c = scale2; p.short_rows = plan.short_rows; p.n_splits = plan.n_splits;
-  p.ctr = (u32*)a->workspace; p.part = (float*)((char*)a->workspace + paged_ctr_bytes(n_cu)); p.prompt_part = p.part + plan.part_bytes / 4;
+  fill_paged(p, a, scale2, plan.short_rows, plan.n_splits, n_cu);
+  p.prompt_part = p.part + plan.part_bytes / 4;
   const hipStream_t st = (hipStream_t)stream;
   HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_paged<64, 16>(p, plan, st) : launch_paged<64, 4>(p, plan, st))
                   : (a->cache.bits == 16 ? launch_paged<128, 16>(p, plan, st) : launch_paged<128, 4>(p, plan, st)));
+  return BLINK_OK;
+}
+
+// ---- attention of groups --------------------------------------------------------------------------------------------------------
+// Rows of a sequence and of a group are the short part's up to 16 ct. The host knows the longest run of queries, and of a group only that it has
+// no more rows than all tokens have.
+struct SharedPlan {
+  u32 ct, wgs, threads, n_splits;
+  bool prompt;
+  u64 part_bytes, prompt_bytes, row_bytes;
+  u64 bytes(u32 n_cu) const { return paged_ctr_bytes(n_cu) + part_bytes + prompt_bytes + row_bytes; }
+};
+static SharedPlan shared_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_tokens, u32 max_q, u32 key_steps, u32 n_cu) {
+  SharedPlan p{};
+  const u32 G = nq / nkv, most = 16u * SHORT_MORE(hd);
+  const u64 own = (u64)max_q * G, all = (u64)n_tokens * G;
+  p.ct = (all <= most ? all > 16 : own > 16 && own <= most) ? SHORT_MORE(hd) : 1;
+  p.prompt = all > 16u * p.ct;
+  p.wgs = n_cu * (p.prompt ? 1 : SHORT_PER_CU(bits, p.ct));
+  p.threads = 64 * (p.prompt ? PAGED_WAVES : SHORT_WAVES(bits, p.ct));
+  p.n_splits = p.prompt ? std::max(1u, key_steps / 4) : 1;       // (parts of 256 keys at least)
+  p.part_bytes = short_floats(p.wgs, hd, p.ct) * 4;
+  p.prompt_bytes = p.prompt ? (u64)p.wgs * PROMPT_SLOT(hd) * 4 : 0;
+  p.row_bytes = 2ull * n_tokens * nq * ROW_RESULT(hd) * 4;
+  return p;
+}
+static int check_groups(u32 n_seqs, u32 n_groups) {
+  if ((u64)n_seqs + n_groups > PAGED_MAX_SEQS) return fail(BLINK_ERR_TOO_LARGE, "%u sequences and %u groups, at most %u together in one call", n_seqs, n_groups, PAGED_MAX_SEQS);
+  return BLINK_OK;
+}
+
+extern "C" int blink_shared_attention_workspace_bytes(int32_t device, const blink_kv_cache* c, uint32_t n_q_heads, uint32_t n_seqs, uint32_t n_groups, uint32_t n_tokens, uint32_t max_q, uint64_t* bytes) {
+  if (int rc = blink_attention_workspace_bytes(device, c, n_q_heads, n_seqs, max_q, bytes)) return rc;      // (a call without groups)
+  if (int rc = check_groups(n_seqs, n_groups)) return rc;
+  if ((u64)n_tokens * n_q_heads >= (1ull << 31)) return fail(BLINK_ERR_TOO_LARGE, "2^31 rows or more");
+  u32 n_cu;
+  if (int rc = compute_units(device, &n_cu)) return rc;
+  const u32 hd = c->head_dim, more = SHORT_MORE(hd);
+  const u64 part = std::max(short_floats(n_cu * SHORT_PER_CU(c->bits, 1), hd, 1), short_floats(n_cu * SHORT_PER_CU(c->bits, more), hd, more)) * 4;
+  *bytes = std::max<u64>(*bytes, paged_ctr_bytes(n_cu) + part + (u64)n_cu * PROMPT_SLOT(hd) * 4 + 2ull * n_tokens * n_q_heads * ROW_RESULT(hd) * 4);
+  return BLINK_OK;
+}
+
+template <int HD, int BITS>
+static hipError_t launch_shared(const SharedArgs& args, const SharedPlan& plan, u32 n_cu, hipStream_t st) {
+  constexpr int MORE = SHORT_MORE(HD);
+  const hipError_t e = plan.prompt ? (plan.ct == 1 ? launch(k_shared_both<HD, BITS, 1>, plan.wgs, plan.threads, st, args) : launch(k_shared_both<HD, BITS, MORE>, plan.wgs, plan.threads, st, args))
+                                   : (plan.ct == 1 ? launch(k_shared_short<HD, BITS, 1>, plan.wgs, plan.threads, st, args) : launch(k_shared_short<HD, BITS, MORE>, plan.wgs, plan.threads, st, args));
+  const u32 wgs = (u32)std::min<u64>(((u64)args.n_tokens * args.nq + PAGED_WAVES - 1) / PAGED_WAVES, 3 * n_cu);
+  return e == hipSuccess ? launch(k_shared_join<HD>, wgs, 64 * PAGED_WAVES, st, args, plan.prompt ? plan.wgs : 0u) : e;
+}
+
+extern "C" int blink_shared_attention(int32_t device, const blink_shared_attention_args* s, void* stream) {
+  g_err.clear();
+  if (!s) return fail(BLINK_ERR_INVAL, "null argument");
+  const blink_paged_attention_args* const a = &s->attention;
+  float scale2;
+  bool nothing;
+  if (int rc = check_attention(a, &scale2, &nothing)) return rc;
+  if (int rc = check_groups(a->n_seqs, s->n_groups)) return rc;
+  if (nothing) return BLINK_OK;
+  if (s->n_groups == 0) return blink_paged_attention(device, a, stream);
+  const u32 hd = a->cache.head_dim, nkv = a->cache.n_kv_heads;
+  if (((u64)a->n_seqs + s->n_groups) * a->max_blocks * nkv >= (1ull << 31)) return fail(BLINK_ERR_TOO_LARGE, "2^31 blocks of keys or more in one call");
+  if (!s->group_starts || !s->shared_lens || (u64)s->group_starts % 4 || (u64)s->shared_lens % 4) return fail(BLINK_ERR_INVAL, "group_starts or shared_lens is null or not aligned");
+  u32 n_cu;
+  if (int rc = compute_units(device, &n_cu)) return rc;
+  const SharedPlan plan = shared_plan(hd, a->cache.bits, a->n_q_heads, nkv, a->n_tokens, a->max_q, a->max_blocks / 4 + 1, n_cu);
+  if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.bytes(n_cu))
+    return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)plan.bytes(n_cu));
+  OnDevice on(device);
+  HIPCHK(on.err);
+  SharedArgs p{};
+  fill_paged(p, a, scale2, 16 * plan.ct, plan.n_splits, n_cu);
+  p.prompt_part = p.part + plan.part_bytes / 4;
+  p.rows = p.prompt_part + plan.prompt_bytes / 4;
+  p.n_groups = s->n_groups; p.starts = s->group_starts; p.shared = s->shared_lens;
+  const hipStream_t st = (hipStream_t)stream;
+  HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_shared<64, 16>(p, plan, n_cu, st) : launch_shared<64, 4>(p, plan, n_cu, st))
+                  : (a->cache.bits == 16 ? launch_shared<128, 16>(p, plan, n_cu, st) : launch_shared<128, 4>(p, plan, n_cu, st)));
   return BLINK_OK;
 }

@@ -17,6 +17,7 @@
 #pragma once
 #include "attention_mfma.h"
 #include "kv_store.h"
+#include <type_traits>
 
 struct PagedArgs {
   const f16_t* q;                 // [token][q head][hd]
@@ -39,8 +40,31 @@ struct PagedArgs {
   float *part, *prompt_part;      // partial results of the short and of the prompt part
 };
 
+// A call in which sequences of a group have their first blocks in common: those keys are seen once for the group, by the rows of all of its
+// sequences at a time (shared_views). So a call has a view for each sequence and, behind those, one for each group.
+struct SharedArgs : PagedArgs {
+  u32 n_groups;
+  const i32 *starts, *shared;     // first sequence of every group (n_groups + 1), tokens that its sequences share
+  float* rows;                    // results to be joined: [of the group, of the sequence][token][q head] of ROW_RESULT(hd) floats
+};
+#define ROW_RESULT(HD) ((HD) + 4u)                   // maximum, sum, two unused, output
+template <typename A> constexpr bool is_shared = std::is_same<A, SharedArgs>::value;
+__device__ __forceinline__ u32 n_views(const PagedArgs& a) { return a.n_seqs; }
+__device__ __forceinline__ u32 n_views(const SharedArgs& a) { return a.n_seqs + a.n_groups; }
+
 // One sequence: its tokens, where its queries stand, and which blocks they see
-struct SeqView { u32 t0, n; i32 pos0; };
+struct SeqView {
+  u32 t0, n;
+  i32 pos0;
+  __device__ __forceinline__ u32 lo() const { return 0; }
+};
+// The same, and of a group: all its queries stand at its last key. first: the first key seen here (those before it are the group's), a multiple of 64
+struct SharedView {
+  u32 t0, n;
+  i32 pos0;
+  u32 first, row;                                    // row: of the table
+  __device__ __forceinline__ u32 lo() const { return first; }
+};
 __device__ __forceinline__ SeqView seq_view(const PagedArgs& a, u32 s) {
   SeqView v;
   const i32 c0 = max(0, min(a.cu[s], (i32)a.n_tokens)), c1 = max(c0, min(a.cu[s + 1], (i32)a.n_tokens));
@@ -51,11 +75,13 @@ __device__ __forceinline__ SeqView seq_view(const PagedArgs& a, u32 s) {
 }
 // Visible tiles of TK keys of the queries at positions p0 .. p1 (p1 >= 0): the first `zb` ones, then those from `wlo` to `hi`
 struct Seen { u32 zb, wlo, n; };
+// (lo: keys before this multiple of TK are not looked at; not together with a window that begins behind key 0)
 template <u32 TK>
-__device__ __forceinline__ Seen seen_tiles(const PagedArgs& a, i32 p0, i32 p1) {
+__device__ __forceinline__ Seen seen_tiles(const PagedArgs& a, i32 p0, i32 p1, u32 lo = 0) {
   Seen r;
   r.wlo = a.window && p0 >= (i32)a.window ? (u32)(p0 - (i32)a.window + 1) / TK : 0u;
   r.zb = min((a.sinks + TK - 1) / TK, r.wlo);
+  r.wlo += lo / TK;
   r.n = p1 < 0 ? 0u : r.zb + (u32)p1 / TK + 1 - r.wlo;
   return r;
 }
@@ -285,9 +311,13 @@ struct CacheTile<HD, 4> {
 };
 
 #define PAGED_WAVES 8              // waves of a workgroup of the prompt part
-#define PAGED_MAX_SEQS 1024u       // sequences whose views a workgroup keeps in LDS
-template <int HD, int CT, int NW>
-struct ShortShared {
+#define PAGED_MAX_SEQS 1024u       // sequences (and groups) whose views a workgroup keeps in LDS
+#define SHARED_ROWS 256u           // sequences with so many rows fill a prompt item by themselves
+struct NoLinks {};
+struct ViewLinks { uint16_t link[PAGED_MAX_SEQS]; };      // of a sequence: its group, or NO_GROUP; of a group: the sequence whose table it takes
+#define NO_GROUP 0xFFFFu
+template <int HD, int CT, int NW, bool SHARED = false>
+struct ShortShared : std::conditional<SHARED, ViewLinks, NoLinks>::type {
   // a result that one wave leaves for others, as its registers hold it: of the pair that its run begins inside of; at NW, of the pair
   // that goes on in other workgroups, by the wave that it begins in
   floatx4_t o[NW + 1][CT][HD / 16][64];
@@ -377,8 +407,8 @@ struct ShortAcc {
     for (int d = 0; d < HD / 16; ++d) o[d] = Tile::product(t.operand(Tile::of(d)), pp, d, o[d]);
   }
 };
-template <int HD, int BITS, int CT, int NW>
-__device__ __forceinline__ void leave_in_lds(ShortShared<HD, CT, NW>& sh, u32 at, const ShortAcc<HD, BITS> (&acc)[CT]) {
+template <int HD, int BITS, int CT, int NW, typename Shared>
+__device__ __forceinline__ void leave_in_lds(Shared& sh, u32 at, const ShortAcc<HD, BITS> (&acc)[CT]) {
   const u32 lane = threadIdx.x & 63;
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -388,8 +418,8 @@ __device__ __forceinline__ void leave_in_lds(ShortShared<HD, CT, NW>& sh, u32 at
     for (int d = 0; d < HD / 16; ++d) sh.o[at][c][d][lane] = acc[c].o[d];
   }
 }
-template <int HD, int BITS, int CT, int NW>
-__device__ __forceinline__ void add_from_lds(const ShortShared<HD, CT, NW>& sh, u32 at, ShortAcc<HD, BITS> (&acc)[CT]) {
+template <int HD, int BITS, int CT, int NW, typename Shared>
+__device__ __forceinline__ void add_from_lds(const Shared& sh, u32 at, ShortAcc<HD, BITS> (&acc)[CT]) {
   const u32 lane = threadIdx.x & 63;
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -402,9 +432,9 @@ __device__ __forceinline__ void add_from_lds(const ShortShared<HD, CT, NW>& sh, 
 // a result in global memory, for another workgroup (see merge_chunks for why past the caches): maxima, sums, outputs as registers hold them
 template <int HD, int CT> __device__ __forceinline__ constexpr u32 short_slot() { return CT * (128 + HD * 16); }     // floats
 // A result in LDS or in the workspace: the lane's maximum and sum of a row tile, its tile d of dimensions
-template <int HD, int CT, int NW>
+template <typename Shared>
 struct LdsResult {
-  const ShortShared<HD, CT, NW>& sh;
+  const Shared& sh;
   u32 at;
   __device__ __forceinline__ float m(u32 c, u32 lane) const { return sh.m[at][c][lane & 15]; }
   __device__ __forceinline__ float l(u32 c, u32 lane) const { return lane < 16 ? sh.l[at][c][lane] : 0.f; }       // (the row's four lanes' added up)
@@ -509,9 +539,70 @@ __device__ __forceinline__ void give_strange(const CacheTile<HD, BITS>& t, float
   }
 }
 
-__device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqView& v) {     // tiles of a sequence and kv head; 0: not this part's, 1 at least else
+// The views of a call with groups, by a workgroup of NT threads: of every sequence (i, its group or NO_GROUP, view), of every group (n_seqs + its number, the
+// sequence whose table it takes, view), each by some thread. A sequence goes by its group where it gains by that and may: it has fewer rows than a prompt item,
+// all its queries stand behind the shared keys and see every one of them, and it is not the only one. The shared keys are cut to a multiple of 64, what a step of
+// the prompt part takes. room: 4 n_groups + 1 words of LDS.
+template <u32 NT, typename P>
+__device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, P put) {
+  u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const to = from + a.n_groups;
+  for (u32 g = threadIdx.x; g <= a.n_groups; g += NT) {
+    starts[g] = (u32)max(0, min(a.starts[g], (i32)a.n_seqs));
+    if (g == a.n_groups) break;
+    keys[g] = (u32)max(0, min(a.shared[g], (i32)(a.max_blocks * 16))) / 64 * 64;
+    from[g] = ~0u; to[g] = 0;
+  }
+  SeqView v[(PAGED_MAX_SEQS + NT - 1) / NT];         // (asked for before the barrier)
+#pragma unroll
+  for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j)
+    if (threadIdx.x + j * NT < a.n_seqs) v[j] = seq_view(a, threadIdx.x + j * NT);
+  __syncthreads();
+  u32 group[(PAGED_MAX_SEQS + NT - 1) / NT];
+#pragma unroll
+  for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j) {
+    const u32 s = threadIdx.x + j * NT;
+    group[j] = NO_GROUP;
+    if (s >= a.n_seqs || !a.n_groups || s < starts[0]) continue;
+    u32 g = 0;
+    for (u32 step = 1u << (31 - __clz((int)a.n_groups)); step; step >>= 1) if (g + step < a.n_groups && starts[g + step] <= s) g += step;      // the last that begins here or before
+    const i32 p1 = v[j].pos0 + (i32)v[j].n - 1;
+    if (s >= starts[g + 1] || !keys[g] || !v[j].n || v[j].n * a.G >= SHARED_ROWS || v[j].pos0 < (i32)keys[g] || (a.window && p1 >= (i32)a.window)) continue;
+    atomicMin(from + g, s);
+    atomicMax(to + g, s);
+    group[j] = g;
+  }
+  __syncthreads();
+#pragma unroll
+  for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j) {
+    const u32 s = threadIdx.x + j * NT, g = group[j];
+    if (s >= a.n_seqs) continue;
+    const bool in = g != NO_GROUP && from[g] < to[g];
+    put(s, in ? g : NO_GROUP, SharedView{v[j].t0, v[j].n, v[j].pos0, in ? keys[g] : 0u, s});
+  }
+  __syncthreads();
+  for (u32 g = threadIdx.x; g < a.n_groups; g += NT) {
+    SharedView x = {0, 0, -1, 0, 0};
+    if (from[g] < to[g]) {
+      const SeqView b = seq_view(a, from[g]), e = seq_view(a, to[g]);
+      x = {b.t0, e.t0 + e.n > b.t0 ? e.t0 + e.n - b.t0 : 0u, (i32)keys[g] - 1, 0, from[g]};
+    }
+    put(a.n_seqs + g, x.row, x);
+  }
+  __syncthreads();
+}
+
+template <typename View>
+__device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const View& v, i32 p1) {     // tiles of a view and kv head; 0: not this part's, 1 at least else
   if (!v.n || v.n * a.G > a.short_rows) return 0;
-  return max(1u, seen_tiles<16>(a, v.pos0, v.pos0 + (i32)v.n - 1).n);
+  return max(1u, seen_tiles<16>(a, v.pos0, p1, v.lo()).n);
+}
+// whether a view's results are joined with others
+template <typename Shared>
+__device__ __forceinline__ bool is_joined(const SharedArgs& a, const Shared& sh, u32 s) { return s >= a.n_seqs || (u32)__builtin_amdgcn_readfirstlane(sh.link[s]) != NO_GROUP; }
+// a row's result, to be joined with another one (which: 0 the group's, 1 the sequence's)
+template <int HD>
+__device__ __forceinline__ float* row_result(const SharedArgs& a, u32 which, u32 tok, u32 head) {
+  return a.rows + (((u64)which * a.n_tokens + tok) * a.nq + head) * ROW_RESULT(HD);
 }
 
 __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { return a.out_tbs ? a.out + packed_off(tok, k, a.out_tbs) : a.out + (u64)tok * a.os + k; }
@@ -538,29 +629,52 @@ __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { r
 // pair that begins in it and goes on in others: one at most), two per group. They do not depend on the batch.
 __host__ __device__ __forceinline__ u32 paged_counters(u32 nwg) { return 2 + nwg + 2 * ((nwg + SHORT_GROUP - 1) / SHORT_GROUP); }
 __host__ __device__ __forceinline__ u64 short_floats(u32 nwg, u32 hd, u32 ct) { return 2ull * (nwg + (nwg + SHORT_GROUP - 1) / SHORT_GROUP) * ct * (128 + 16 * hd); }
-template <int HD, int BITS, int CT, int NT, int NW>
-__device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, CT, NW>& sh, u32 wg, u32 nwg) {
+template <int HD, int BITS, int CT, int NT, int NW, typename A>
+__device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, is_shared<A>>& sh, u32 wg, u32 nwg) {
+  typedef ShortShared<HD, CT, NW, is_shared<A>> Shared;
+  constexpr bool SHARED = is_shared<A>;
   typedef CacheTile<HD, BITS> Tile;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
   auto scalar = [](u32 x) { return (u32)__builtin_amdgcn_readfirstlane(x); };
-  auto count_tiles = [&](u32 s) {
-    const SeqView v = seq_view(a, s);
-    const u32 n = short_unit_count(a, v);
+  auto note_view = [&](u32 s, const auto& v, i32 p1) {
+    const u32 n = short_unit_count(a, v, p1);
     sh.pos0[s] = v.pos0; sh.n[s] = n ? (unsigned char)v.n : (unsigned char)0;
     return n;
   };
+  // of a view: position of the last query, first key (only where there are groups is it another one than of a sequence's own)
+  auto last_pos = [&](u32 s, i32 p0, i32 n) { return p0 + (SHARED && s >= a.n_seqs ? 1 : n) - 1; };
+  auto first_key = [&](u32 s) {
+    if constexpr (SHARED) return s < a.n_seqs && sh.link[s] != NO_GROUP ? (u32)sh.pos0[a.n_seqs + sh.link[s]] + 1 : 0u;
+    return 0u;
+  };
+  auto count_tiles = [&](u32 s) {
+    if constexpr (SHARED) {
+      const i32 p0 = sh.pos0[s], n = (i32)sh.n[s];
+      return n ? max(1u, seen_tiles<16>(a, p0, last_pos(s, p0, n), first_key(s)).n) : 0u;
+    } else {
+      const SeqView v = seq_view(a, s);
+      const u32 n = short_unit_count(a, v, v.pos0 + (i32)v.n - 1);
+      sh.pos0[s] = v.pos0; sh.n[s] = n ? (unsigned char)v.n : (unsigned char)0;
+      return n;
+    }
+  };
+  if constexpr (SHARED)
+    shared_views<64 * NW>(a, (u32*)sh.o, [&](u32 s, u32 link, const SharedView& v) {
+      sh.link[s] = (uint16_t)link;
+      note_view(s, v, s < a.n_seqs ? v.pos0 + (i32)v.n - 1 : v.pos0);
+    });
   // Pairs dealt out whole: `cap` tiles of one at most to a workgroup, as few as there are workgroups for, but 32, and more (up to 64)
   // where results would be more than groups of groups take (65531 keys in 4 bits: 21.9 us with 64 results a pair, 23.2 with 128; 16384
   // keys: 19.3 with 16, 16.5 with 32). Then `pre` counts workgroups, else units.
-  const u32 pairs = a.n_seqs * a.nkv;
+  const u32 pairs = n_views(a) * a.nkv;
   u32 U, cap;
   bool whole;
   auto choose = [&](u32 units, u32 of) {             // (of = nwg - pairs: these are always enough)
     cap = pairs <= nwg / 2 ? max(max(32u, (units + of - 1) / of), min(64u, units / (pairs * (SHORT_GROUP * SHORT_GROUP)))) : ~0u;
     whole = cap <= 64;
   };
-  if (a.n_seqs <= 64) {                              // every wave for itself, all the same: nobody waits
-    const u32 n = lane < a.n_seqs ? count_tiles(lane) : 0u;
+  if (n_views(a) <= 64) {                                 // every wave for itself, all the same: nobody waits
+    const u32 n = lane < n_views(a) ? count_tiles(lane) : 0u;
     u32 sum = wave_sums(n * a.nkv);
     const u32 units = U = (u32)__builtin_amdgcn_readlane((i32)sum, 63);
 #pragma unroll 1
@@ -570,20 +684,20 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
       const u32 x = wave_sums((n + cap - 1) / cap * a.nkv), wgs = (u32)__builtin_amdgcn_readlane((i32)x, 63);
       if (wgs <= nwg) { sum = x; U = wgs; break; }
     }
-    if (lane < a.n_seqs) sh.pre[lane + 1] = sum;
+    if (lane < n_views(a)) sh.pre[lane + 1] = sum;
     if (lane == 0) sh.pre[0] = 0;
     __builtin_amdgcn_wave_barrier();
   } else {
-    prefix_sums<NW>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) { return count_tiles(s) * a.nkv; });
-    choose(scalar(sh.pre[a.n_seqs]), nwg - pairs);
+    prefix_sums<NW>(sh.pre, sh.wave_sum, n_views(a), [&](u32 s) { return count_tiles(s) * a.nkv; });
+    choose(scalar(sh.pre[n_views(a)]), nwg - pairs);
     if (whole) {
       __syncthreads();
-      prefix_sums<NW>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) {
+      prefix_sums<NW>(sh.pre, sh.wave_sum, n_views(a), [&](u32 s) {
         const i32 p0 = sh.pos0[s], n = (i32)sh.n[s];
-        return n ? (max(1u, seen_tiles<16>(a, p0, p0 + n - 1).n) + cap - 1) / cap * a.nkv : 0u;
+        return n ? (max(1u, seen_tiles<16>(a, p0, last_pos(s, p0, n), first_key(s)).n) + cap - 1) / cap * a.nkv : 0u;
       });
     }
-    U = scalar(sh.pre[a.n_seqs]);
+    U = scalar(sh.pre[n_views(a)]);
   }
   const u32 wg_units = max(1u, (U + nwg * NW - 1) / (nwg * NW)) * NW;
   if (whole ? wg >= U : wg * wg_units >= U) return;
@@ -591,19 +705,22 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   typedef const __attribute__((address_space(4))) u32 const_u32;
   // a pair of a sequence and a kv head: its first unit and number of tiles, its rows, and which tiles those are
   struct Pair { u32 s, g, first, nv, t0, n, row, zb, wlo; i32 pos0; };
+  auto last_of = [&](const Pair& p) { return p.pos0 + (SHARED && p.s >= a.n_seqs ? 1 : (i32)p.n) - 1; };      // position of the last query
   auto pair_of = [&](u32 s, u32 g) {
     Pair p;
     p.s = s; p.g = g;
-    p.t0 = (u32)max(0, min((i32)((const_u32*)(u64)uniform_ptr((const u32*)a.cu))[s], (i32)a.n_tokens));
+    u32 of = s;                                      // the sequence whose table and first token it has
+    if constexpr (SHARED) { if (s >= a.n_seqs) of = scalar(sh.link[s]); }
+    p.t0 = (u32)max(0, min((i32)((const_u32*)(u64)uniform_ptr((const u32*)a.cu))[of], (i32)a.n_tokens));
     p.n = scalar(sh.n[s]); p.pos0 = (i32)scalar((u32)sh.pos0[s]);
-    const Seen e = seen_tiles<16>(a, p.pos0, p.pos0 + (i32)p.n - 1);
+    const Seen e = seen_tiles<16>(a, p.pos0, last_of(p), SHARED ? scalar(first_key(s)) : 0u);
     p.zb = scalar(e.zb); p.wlo = scalar(e.wlo); p.nv = scalar(max(1u, e.n));
     p.first = whole ? 0u : scalar(sh.pre[s]) + g * p.nv;
-    p.row = a.table_row ? scalar(a.table_row[s]) : s;
+    p.row = a.table_row ? scalar(a.table_row[of]) : of;
     return p;
   };
   auto pair_at = [&](u32 u) {                        // (whole pairs: u = the workgroup)
-    const u32 s = scalar(last_at_most(sh.pre, a.n_seqs, u)), in = u - scalar(sh.pre[s]);
+    const u32 s = scalar(last_at_most(sh.pre, n_views(a), u)), in = u - scalar(sh.pre[s]);
     return pair_of(s, in / (scalar(sh.pre[s + 1] - sh.pre[s]) / a.nkv));
   };
   auto pair_after = [&](const Pair& p) {             // (there is one)
@@ -630,7 +747,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const u32 r = c * 16 + lc, rr = min(r, p.n * a.G - 1), tok = rr / a.G, h = rr - tok * a.G;
-      qpos[c] = r < p.n * a.G ? p.pos0 + (i32)tok : -1;
+      qpos[c] = r < p.n * a.G ? (SHARED && p.s >= a.n_seqs ? p.pos0 : p.pos0 + (i32)tok) : -1;
       Tile::load_query(a.q + (u64)(p.t0 + tok) * a.qs + (u64)(p.g * a.G + h) * HD, q[c]);
     }
   };
@@ -640,6 +757,28 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     for (int c = 0; c < CT; ++c) acc[c].init();
   };
   auto finish = [&](const Pair& p) {
+    if constexpr (SHARED) {
+      if (is_joined(a, sh, p.s)) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          const float l = quad_sum(acc[c].l);
+          const u32 r = c * 16 + lc, tok = r / a.G;
+          if (r >= p.n * a.G) continue;
+          float* const x = row_result<HD>(a, p.s < a.n_seqs ? 1u : 0u, p.t0 + tok, p.g * a.G + r - tok * a.G);
+          if (lg == 0) *(float2*)x = make_float2(acc[c].m, l);
+          if constexpr (BITS == 16) {
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(x + 4 + d * 16 + lg * 4) = acc[c].o[d];
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int d = 0; d < HD / 16; d += 4) *(floatx4_t*)(x + 4 + Tile::o_dim(d, lg, i)) = floatx4_t{acc[c].o[d][i], acc[c].o[d + 1][i], acc[c].o[d + 2][i], acc[c].o[d + 3][i]};
+          }
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const float l = quad_sum(acc[c].l), inv = l == 0.f ? 0.f : 1.0f / l;
@@ -665,7 +804,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     return p.pos0 + (i32)p.n > 0 ? ((const_u32*)(u64)uniform_ptr(a.tables + (u64)p.row * a.max_blocks))[key / 16] : ~0u;
   };
   auto edge_of = [&](const Pair& p, u32 key, bool in_cache) {      // some row does not see the whole tile
-    const i32 k = (i32)key, p1 = p.pos0 + (i32)p.n - 1;
+    const i32 k = (i32)key, p1 = last_of(p);
     return !(k + 15 <= p.pos0 && in_cache && (!a.window || k > p1 - (i32)a.window || key + 16 <= a.sinks));
   };
   auto see = [&](u32 key, bool in_cache, u32 (&vis)[CT]) {
@@ -767,6 +906,25 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
   auto group_piece = [&](u32 x, u32 first) { return a.part + (u64)(2 * (nwg + x) + (x == first / SHORT_GROUP ? 1u : 0u)) * short_slot<HD, CT>(); };
   ShortMerge<HD, BITS, CT, NW> all;
   auto finish_all = [&](const Pair& p) {
+    if constexpr (SHARED) {
+      if (is_joined(a, sh, p.s)) {
+        const float sum = quad_sum(all.l);
+        if (!all.live) return;
+        const u32 r = all.c * 16 + lc, tok = r / a.G;
+        float* const x = row_result<HD>(a, p.s < a.n_seqs ? 1u : 0u, p.t0 + tok, p.g * a.G + r - tok * a.G);
+        if (all.d0 == 0 && lg == 0) *(float2*)x = make_float2(all.m, sum);
+        if constexpr (BITS == 16) {
+#pragma unroll
+          for (int t = 0; t < all.T; ++t) *(floatx4_t*)(x + 4 + (all.d0 + t) * 16 + lg * 4) = all.o[t];
+        } else {
+#pragma unroll
+          for (int t = 0; t < all.T; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 + Tile::o_dim((int)all.d0 + t, lg, i)] = all.o[t][i];
+        }
+        return;
+      }
+    }
     const float l = quad_sum(all.l), inv = l == 0.f ? 0.f : 1.0f / l;
     const u32 r = all.c * 16 + lc, tok = r / a.G, k = (p.g * a.G + r - tok * a.G) * HD;
     if (!all.live) return;
@@ -790,7 +948,7 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
     const u32 end = p.first + p.nv, f = first_wg(p), np = n_wgs(p);
     if (which ? p.first < wg0 || end <= (whole ? quantum : wg1) : p.first >= wg0) continue;      // (a pair in one run: its wave has finished it)
     const u32 x0 = which ? (p.first - wg0) / quantum : 0u, x1 = (min(end, wg1) - wg0 + quantum - 1) / quantum;
-    all.sum(x0, x1, p.n * a.G, [&](u32 x) { return LdsResult<HD, CT, NW>{sh, which && x == x0 ? (u32)NW : x}; });
+    all.sum(x0, x1, p.n * a.G, [&](u32 x) { return LdsResult<Shared>{sh, which && x == x0 ? (u32)NW : x}; });
     if (np == 1) { finish_all(p); continue; }
     all.leave(a.part + (u64)(2 * wg + which) * short_slot<HD, CT>());
     if (threadIdx.x == 0) {
@@ -856,33 +1014,46 @@ __device__ __forceinline__ void paged_short(const PagedArgs& a, ShortShared<HD, 
 #define PROMPT_ROWS (128u * PROMPT_CT)
 #define PROMPT_RING (128u * 1024u)
 #define PROMPT_SLOT(HD) (PROMPT_ROWS * ((HD) + 2u))      // floats of a part's result: maximum and sum of every row, then its output
-struct PromptShared {
+template <typename View>
+struct PromptRoom {
   alignas(256) unsigned char ring[PROMPT_RING];
   u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES];
   // the item after this one, and whether some step of it had values that are not finite: by the item's number among the workgroup's, so that no
   // wave has to wait at its end for those that read them
   u32 next_item[2], strange[3];
-  SeqView view[PAGED_MAX_SEQS];      // (an item begins without asking memory for them: two prompts of 4000 behind a window, four items a workgroup: 169 us -> 165)
+  View view[PAGED_MAX_SEQS];         // (an item begins without asking memory for them: two prompts of 4000 behind a window, four items a workgroup: 169 us -> 165)
 };
-__device__ __forceinline__ u32 prompt_items(const PagedArgs& a, const SeqView& v) {
+typedef PromptRoom<SeqView> PromptShared;
+template <typename A> struct PromptKinds { typedef SeqView View; };
+template <> struct PromptKinds<SharedArgs> { typedef SharedView View; };
+template <typename A> using PromptRoomOf = PromptRoom<typename PromptKinds<A>::View>;
+template <typename View>
+__device__ __forceinline__ u32 prompt_items(const PagedArgs& a, const View& v) {
   return v.n * a.G <= a.short_rows ? 0u : (v.n * a.G + PROMPT_ROWS - 1) / PROMPT_ROWS;
 }
 // parts of every item's keys: as many as there are workgroups for
 __device__ __forceinline__ u32 prompt_parts(const PagedArgs& a, u32 items, u32 nwg) { return items && items < nwg ? max(1u, min(a.n_splits, nwg / items)) : 1u; }
 
-struct PromptItem { u32 s, g, r0, rows, t0; i32 p0, p1; };   // rows r0 .. r0 + rows of the sequence's, queries at positions p0 .. p1
-template <typename F>
-__device__ __forceinline__ PromptItem prompt_item(const PagedArgs& a, const u32* pre, u32 item, F view) {
+struct PromptItem { u32 s, g, r0, rows, t0; i32 p0, p1; u32 lo, row; };      // rows r0 .. r0 + rows of the view's, queries at positions p0 .. p1; first key, row of the table
+template <typename A, typename F>
+__device__ __forceinline__ PromptItem prompt_item(const A& a, const u32* pre, u32 item, F view) {
   PromptItem it;
-  const u32 gi = pre[a.n_seqs] - 1 - item / a.nkv;             // the last queries (the longest walks) first
+  const u32 views = n_views(a);
+  const u32 gi = pre[views] - 1 - item / a.nkv;                // the last queries (the longest walks) first
   it.g = item % a.nkv;
-  it.s = last_at_most(pre, a.n_seqs, gi);
-  const SeqView v = view(it.s);
+  it.s = last_at_most(pre, views, gi);
+  const auto v = view(it.s);
   it.r0 = (gi - pre[it.s]) * PROMPT_ROWS;
   it.rows = min(PROMPT_ROWS, v.n * a.G - it.r0);
   it.t0 = v.t0;
   it.p0 = v.pos0 + (i32)(it.r0 / a.G);
   it.p1 = v.pos0 + (i32)((it.r0 + it.rows - 1) / a.G);
+  it.lo = v.lo();
+  it.row = it.s;
+  if constexpr (is_shared<A>) {
+    it.row = v.row;
+    if (it.s >= a.n_seqs) it.p0 = it.p1 = v.pos0;
+  }
   return it;
 }
 
@@ -920,16 +1091,18 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 template <int N> __device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
-template <int HD, int BITS>
-__device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& sh, u32 wg, u32 nwg, bool behind_short) {
+template <int HD, int BITS, typename A>
+__device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u32 wg, u32 nwg, bool behind_short) {
+  constexpr bool SHARED = is_shared<A>;
   constexpr int CT = PROMPT_CT;
   constexpr u32 BLK = 16 * HD * 2, NB = 4, STAGE = 2 * NB * BLK, NS = BITS == 4 ? 2 : (PROMPT_RING / STAGE > 6 ? 6 : PROMPT_RING / STAGE), TPW = BLK / 1024;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
-  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) {
-    sh.view[s] = seq_view(a, s);
+  if constexpr (SHARED) shared_views<64 * PAGED_WAVES>(a, (u32*)sh.ring, [&](u32 s, u32, const SharedView& v) { sh.view[s] = v; });
+  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, n_views(a), [&](u32 s) {
+    if constexpr (!SHARED) sh.view[s] = seq_view(a, s);
     return prompt_items(a, sh.view[s]);
   });
-  const u32 items = (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]) * a.nkv, parts = prompt_parts(a, items, nwg), total = items * parts;
+  const u32 items = (u32)__builtin_amdgcn_readfirstlane(sh.pre[n_views(a)]) * a.nkv, parts = prompt_parts(a, items, nwg), total = items * parts;
   u32* const ctr = a.ctr;
   const u32 lds0 = (u32)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sh.ring;
   // fetching halves: waves 0-3 the K of a block each, waves 4-7 the V (places in LDS: attn_prompt)
@@ -969,24 +1142,26 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
     it.s = (u32)__builtin_amdgcn_readfirstlane(it.s); it.g = (u32)__builtin_amdgcn_readfirstlane(it.g); it.r0 = (u32)__builtin_amdgcn_readfirstlane(it.r0);
     it.rows = (u32)__builtin_amdgcn_readfirstlane(it.rows); it.t0 = (u32)__builtin_amdgcn_readfirstlane(it.t0);
     it.p0 = __builtin_amdgcn_readfirstlane(it.p0); it.p1 = __builtin_amdgcn_readfirstlane(it.p1);
-    const Seen e = seen_tiles<64>(a, it.p0, it.p1);
+    if constexpr (SHARED) { it.lo = (u32)__builtin_amdgcn_readfirstlane(it.lo); it.row = (u32)__builtin_amdgcn_readfirstlane(it.row); }
+    const bool group = SHARED && it.s >= a.n_seqs;              // (all its rows stand at one position)
+    const Seen e = seen_tiles<64>(a, it.p0, it.p1, SHARED ? it.lo : 0u);
     const u32 zb = (u32)__builtin_amdgcn_readfirstlane(e.zb), wlo = (u32)__builtin_amdgcn_readfirstlane(e.wlo), n_steps = (u32)__builtin_amdgcn_readfirstlane(e.n);
     const u32 per = (n_steps + parts - 1) / parts, s_lo = min(part * per, n_steps), s_hi = min(s_lo + per, n_steps);
     const u32 last_block = (u32)max(0, it.p1) / 16;
-    const u32 row = a.table_row ? (u32)__builtin_amdgcn_readfirstlane(a.table_row[it.s]) : it.s;
+    const u32 row = SHARED ? it.row : a.table_row ? (u32)__builtin_amdgcn_readfirstlane(a.table_row[it.s]) : it.s;
     const_u32* const bt = (const_u32*)(u64)uniform_ptr(a.tables + (u64)row * a.max_blocks);
     auto tile_of = [&](u32 s) { return s < zb ? s : wlo + s - zb; };          // 64 keys from 64 times this
     auto block_id = [&](u32 s, u32 b) { return bt[min(NB * tile_of(min(s, n_steps ? n_steps - 1 : 0u)) + b, last_block)]; };
     // this wave's rows
     const u32 wr = w * (16 * CT);
     const bool live = wr < it.rows;
-    const i32 wp0 = it.p0 + (i32)((it.r0 % a.G + wr) / a.G), wp1 = it.p0 + (i32)((it.r0 % a.G + min(wr + 16 * CT, it.rows) - 1) / a.G);
+    const i32 wp0 = group ? it.p0 : it.p0 + (i32)((it.r0 % a.G + wr) / a.G), wp1 = group ? it.p0 : it.p0 + (i32)((it.r0 % a.G + min(wr + 16 * CT, it.rows) - 1) / a.G);
     f16x8_t q[CT][HD / 32];
     i32 qpos[CT];                                    // position of the lane's row (no row: before every key)
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const u32 r = wr + c * 16 + lc, rr = it.r0 + min(r, it.rows - 1), tok = rr / a.G, h = rr - tok * a.G;
-      qpos[c] = r < it.rows ? it.p0 - (i32)(it.r0 / a.G) + (i32)tok : -1;
+      qpos[c] = r < it.rows ? (group ? it.p0 : it.p0 - (i32)(it.r0 / a.G) + (i32)tok) : -1;
 #pragma unroll
       for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(a.q + (u64)(it.t0 + tok) * a.qs + (it.g * a.G + h) * HD + s * 32 + lg * 8);
     }
@@ -1280,7 +1455,17 @@ __device__ __forceinline__ void paged_prompt(const PagedArgs& a, PromptShared& s
       const float sum = quad_sum(l[c]);
       const u32 r = wr + c * 16 + lc_end;
       if (r >= it.rows) continue;
-      if (parts == 1) {
+      bool to_row = false;
+      if constexpr (SHARED) to_row = parts == 1 && (group || it.lo);
+      if (to_row) {
+        if constexpr (SHARED) {
+          const u32 rr = it.r0 + r, tok = rr / a.G;
+          float* const x = row_result<HD>(a, group ? 0u : 1u, it.t0 + tok, it.g * a.G + rr - tok * a.G);
+          if (lg_end == 0) *(float2*)x = make_float2(m[c], sum);
+#pragma unroll
+          for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(x + 4 + d * 16 + lg_end * 4) = o[c][d];
+        }
+      } else if (parts == 1) {
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
         const u32 rr = it.r0 + r, tok = rr / a.G, k = (it.g * a.G + rr - tok * a.G) * HD + lg_end * 4;
         f16_t* const to = out_at(a, it.t0 + tok, k);
@@ -1333,10 +1518,69 @@ __device__ __forceinline__ void prompt_merge(const PagedArgs& a, PromptMergeShar
   }
 }
 
+// Results joined: of a row whose keys are its group's and its sequence's, and of rows whose keys were cut into parts. A wave per row, its lanes along the
+// dimensions. What lies where is worked out as the launch before did (nwg_prompt: its workgroups, 0: without a prompt part).
+struct JoinShared {
+  SharedView view[PAGED_MAX_SEQS];
+  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], room[4 * PAGED_MAX_SEQS + 1];
+  uint16_t group[PAGED_MAX_SEQS];
+};
+template <int HD>
+__device__ __forceinline__ void shared_join(const SharedArgs& a, JoinShared& sh, u32 wg, u32 nwg, u32 nwg_prompt) {
+  const u32 lane = threadIdx.x & 63;
+  shared_views<64 * PAGED_WAVES>(a, sh.room, [&](u32 s, u32 link, const SharedView& v) { sh.view[s] = v; sh.group[s] = (uint16_t)link; });
+  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, n_views(a), [&](u32 s) { return nwg_prompt ? prompt_items(a, sh.view[s]) : 0u; });
+  const u32 item_rows = (u32)__builtin_amdgcn_readfirstlane(sh.pre[n_views(a)]), parts = prompt_parts(a, item_rows * a.nkv, nwg_prompt);
+  for (u32 i = wg * PAGED_WAVES + (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < a.n_tokens * a.nq; i += nwg * PAGED_WAVES) {
+    const u32 t = i / a.nq, head = i - t * a.nq, g = head / a.G;
+    // the sequence: the last that begins at this token or before and has it
+    u32 lo = 0;
+    for (u32 step = 512; step; step >>= 1) if (lo + step < a.n_seqs && sh.view[lo + step].t0 <= t) lo += step;
+    const SharedView v = sh.view[lo];
+    if (t < v.t0 || t - v.t0 >= v.n) continue;       // (no sequence's, or not looked at)
+    const bool in = v.first != 0, prompt = nwg_prompt && prompt_items(a, v) != 0, cut = prompt && parts > 1;
+    if (!in && !cut) continue;                       // (that was its only result)
+    float M = -INFINITY, L = 0.f, O[HD / 64];
+#pragma unroll
+    for (int d = 0; d < HD / 64; ++d) O[d] = 0.f;
+    auto add = [&](float m, float l, const float* o) {
+      const float mn = fmaxf(M, m), ref = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(M - ref), h = __builtin_amdgcn_exp2f(m - ref);
+      L = L * f + l * h;
+#pragma unroll
+      for (int d = 0; d < HD / 64; ++d) O[d] = O[d] * f + o[d * 64 + lane] * h;
+      M = mn;
+    };
+    // a view's result of its row r
+    auto take = [&](u32 which, u32 s, const SharedView& x, u32 r) {
+      if (nwg_prompt && prompt_items(a, x) && parts > 1) {
+        const u32 item = (item_rows - 1 - (sh.pre[s] + r / PROMPT_ROWS)) * a.nkv + g;
+        for (u32 p = 0; p < parts; ++p) {
+          const float* const b = a.prompt_part + ((u64)item * parts + p) * PROMPT_SLOT(HD);
+          const float2 ml = *(const float2*)(b + 2 * (r % PROMPT_ROWS));
+          add(ml.x, ml.y, b + 2 * PROMPT_ROWS + r % PROMPT_ROWS * HD);
+        }
+      } else {
+        const float* const b = row_result<HD>(a, which, t, head);
+        const float2 ml = *(const float2*)b;
+        add(ml.x, ml.y, b + 4);
+      }
+    };
+    const u32 h = head - g * a.G;
+    if (in) {
+      const u32 s = a.n_seqs + sh.group[lo];
+      const SharedView x = sh.view[s];
+      take(0, s, x, (t - x.t0) * a.G + h);
+    }
+    take(1, lo, v, (t - v.t0) * a.G + h);
+#pragma unroll
+    for (int d = 0; d < HD / 64; ++d) *out_at(a, t, head * HD + d * 64 + lane) = (f16_t)half_pair(L == 0.f ? 0.f : O[d] / L, 0.f);
+  }
+}
+
 // Batches that may hold both: every workgroup first its runs of the few rows' tiles, then prompt items from the counter.
-template <int HD, int CT> union PagedShared { ShortShared<HD, CT, PAGED_WAVES> s; PromptShared p; };
-template <int HD, int BITS, int CT, int NT>
-__device__ __forceinline__ void paged_both(const PagedArgs& a, PagedShared<HD, CT>& sh, u32 wg, u32 nwg) {
+template <int HD, int CT, typename A = PagedArgs> union PagedShared { ShortShared<HD, CT, PAGED_WAVES, is_shared<A>> s; PromptRoomOf<A> p; };
+template <int HD, int BITS, int CT, int NT, typename A>
+__device__ __forceinline__ void paged_both(const A& a, PagedShared<HD, CT, A>& sh, u32 wg, u32 nwg) {
   paged_short<HD, BITS, CT, NT, PAGED_WAVES>(a, sh.s, wg, nwg);
   __syncthreads();
   paged_prompt<HD, BITS>(a, sh.p, wg, nwg, true);

@@ -1,4 +1,4 @@
-// The kernels of the paged-cache operators, defined in kernels/kv_store.hip, paged_short.hip, paged_prompt.hip and paged_both.hip, of the log
+// The kernels of the paged-cache operators, defined in kernels/kv_store.hip, paged_short.hip, paged_prompt.hip, paged_both.hip and shared_*.hip, of the log
 // probabilities (kernels/logprobs.hip), and
 // those of an engine's phases that are the same operators (kernels/paged_phases.hip).
 #pragma once
@@ -25,5 +25,8 @@ template <int HD, int BITS, int CT> __global__ void k_paged_short(PagedArgs a);
 template <int HD, int BITS> __global__ void k_paged_prompt(PagedArgs a);
 template <int HD, int BITS> __global__ void k_paged_both(PagedArgs a);
 template <int HD> __global__ void k_paged_merge(PagedArgs a, u32 nwg_prompt);
+template <int HD, int BITS, int CT> __global__ void k_shared_short(SharedArgs a);
+template <int HD, int BITS, int CT> __global__ void k_shared_both(SharedArgs a);
+template <int HD> __global__ void k_shared_join(SharedArgs a, u32 nwg_prompt);
 template <int HD, int BITS> __global__ void k_store_phase(DevCtx c, u32 layer);
 template <int HD, int BITS, int CT> __global__ void k_attention_phase(DevCtx c, u32 layer);

@@ -1,0 +1,270 @@
+"""Attention of groups of sequences that share their first blocks, against the fp64 oracle of the attention without groups."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_07609_amd as B
+from tests.test_gpu_operators import check_attention, dev, new_cache, no_error_of_earlier_tests, oracle_cache, run_attention  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def make_groups(groups, nq, nkv, hd, bits, seed=0, before=(), after=(), extra_rows=0, unlike=False):
+    """groups: (shared tokens, [(context, queries) ...]) each; before, after: (context, queries) of sequences in no group. A filled cache (places of
+    no token hold garbage) and the call's arrays."""
+    rng = np.random.default_rng(seed)
+    seqs, starts, shared = list(before), [len(before)], []
+    for sh, members in groups:
+        seqs += members
+        starts.append(len(seqs))
+        shared.append(sh)
+    seqs += list(after)
+    lens, runs = np.int32([n for n, _ in seqs]), [m for _, m in seqs]
+    width = max(1, max((n + 15) // 16 for n in lens))
+    order = list(rng.permutation(sum((int(n) + 15) // 16 for n in lens) + 3))
+    tables = np.full((len(seqs), width), -1, dtype=np.int32)
+    for g in range(len(groups)):
+        common = [order.pop() for _ in range(min(shared[g], max([int(lens[s]) for s in range(starts[g], starts[g + 1])] + [0])) // 16)]
+        for s in range(starts[g], starts[g + 1]):
+            m = min(len(common), (int(lens[s]) + 15) // 16)
+            tables[s, :m] = common[:m]
+    for s in range(len(seqs)):
+        for j in range((int(lens[s]) + 15) // 16):
+            if tables[s, j] < 0:
+                tables[s, j] = order.pop()
+    cache = new_cache(max(1, int(tables.max()) + 2), nkv, hd, bits)
+    c = oracle_cache(cache)
+    done = set()
+    for s in range(len(seqs)):
+        for j in range(int(lens[s])):
+            place = int(tables[s, j // 16]) * 16 + j % 16
+            if place not in done:
+                done.add(place)
+                c.put(place, *(rng.standard_normal((2, nkv, hd)) * (np.exp(rng.uniform(-3, 3, (2, nkv, 1))) if unlike else 1.0)))
+    cache.data.copy_(torch.from_numpy(c.data))
+    cu = np.concatenate(([0], np.cumsum(runs))).astype(np.int32)
+    q = (rng.standard_normal((int(cu[-1]) + extra_rows, nq, hd)) / np.sqrt(hd)).astype(np.float16)
+    return (cache, c, tables, lens, cu, q), np.int32(starts), np.int32(shared), max(runs)
+
+
+def run_shared(b, starts, shared, max_q, window=0, sinks=0, scale=1.0, workspace=None, fill=9.0):
+    cache, _, tables, lens, cu, q = b
+    if workspace is None:
+        n = B.shared_attention_workspace_bytes(q.shape[1], cache, len(lens), len(shared), q.shape[0], max_q)
+        workspace = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+        workspace[:8192] = 0
+    out = torch.full(q.shape, fill, dtype=torch.float16, device="cuda")
+    B.shared_attention(dev(q), cache, dev(tables), dev(lens), dev(cu), dev(starts), dev(shared), out, workspace, max_q=max_q, window=window, sinks=sinks, scale=scale)
+    assert not workspace[:8192].any()
+    return out.double().cpu().numpy()
+
+
+def check(groups, nq, nkv, hd, bits, window=0, sinks=0, scale=1.0, **k):
+    b, starts, shared, max_q = make_groups(groups, nq, nkv, hd, bits, extra_rows=2, **k)
+    got = run_shared(b, starts, shared, max_q, window, sinks, scale)
+    check_attention(got, *b, window=window, sinks=sinks, scale=scale)
+    assert np.array_equal(got, run_shared(b, starts, shared, max_q, window, sinks, scale))
+    return got
+
+
+HEADS = [(64, 6, 2), (128, 4, 1), (64, 3, 3), (128, 16, 2)]
+ONE = lambda sh, own: (sh, [(sh + n, 1) for n in own])      # noqa: E731   a group that decodes
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("hd, nq, nkv", HEADS)
+@pytest.mark.parametrize("groups", [
+    [ONE(64, [1, 2])],                                       # the fewest
+    [ONE(63, [5, 9])], [ONE(65, [5, 9])], [ONE(127, [16, 1, 40])], [ONE(128, [17, 33])],
+    [ONE(200, [1, 30, 100, 16])],
+    [ONE(80, [3, 4]), ONE(300, [7]), ONE(150, [20, 1, 1])],   # one of them has nobody to share with
+    [ONE(320, [10] * 20)],                                   # more rows than the few-row part holds
+    [ONE(100, [1] * 70), ONE(130, [9] * 5)],
+    [(0, [(40, 1), (50, 1)]), ONE(64, [3, 3])],
+])
+def test_groups_that_decode(groups, hd, nq, nkv, bits):
+    check(groups, nq, nkv, hd, bits, unlike=True)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("hd, nq, nkv", HEADS)
+@pytest.mark.parametrize("groups", [
+    [(100, [(103, 3), (109, 5), (101, 1)])],
+    [(70, [(79, 9)] * 12), (200, [(217, 17), (230, 2)])],
+    [(130, [(190, 60), (140, 1), (200, 70)])],               # rows of prompt items, of sequences and of the group
+    [(130, [(430, 300), (140, 4), (141, 4)])],               # one with so many queries that it goes by itself
+])
+def test_groups_with_drafts_and_continuations(groups, hd, nq, nkv, bits):
+    check(groups, nq, nkv, hd, bits, seed=1)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("groups, before, after", [
+    ([ONE(90, [4, 5])], [(30, 1), (77, 3)], [(0, 1), (0, 1)]),
+    ([(96, [(100, 1), (0, 1), (99, 1), (0, 0)])], [], [(64, 1)]),                # unused slots within the group
+    ([(96, [(100, 4), (60, 2), (96, 1), (110, 20), (97, 2)])], [], []),          # queries inside of the shared tokens, or partly
+    ([(96, [(100, 1), (50, 50), (120, 1)])], [(0, 1)], [(200, 100)]),
+    ([], [(50, 1), (20, 2)], []),
+    ([(64, []), ONE(70, [2, 3]), (64, [])], [], []),
+])
+def test_sequences_in_no_group_unused_and_within_the_shared_tokens(groups, before, after, bits):
+    check(groups, 6, 2, 64, bits, seed=2, before=before, after=after)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("window, sinks", [(1, 0), (40, 5), (90, 0), (109, 3), (110, 3), (111, 0), (500, 16)])
+def test_windows(window, sinks, bits):
+    """Sequences whose window has not been left share, others do not: 105 + 5 tokens on both sides of the border."""
+    check([(100, [(105, 1), (110, 1), (109, 2), (160, 1), (111, 1), (103, 3)])], 4, 2, 64, bits, window=window, sinks=sinks, seed=3)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("nq, nkv", [(24, 1), (12, 1), (20, 4), (33, 1), (64, 1)])
+def test_group_sizes_of_heads(nq, nkv, bits):
+    check([(128, [(130, 1), (140, 2), (150, 3), (129, 1)])], nq, nkv, 64, bits, scale=0.7, seed=nq)
+
+
+def repeated(lens_groups, nq, nkv, hd, bits, few=40, seed=5):
+    """Long contexts over a table that repeats a few blocks."""
+    rng = np.random.default_rng(seed)
+    b, _, _, _ = make_groups([], nq, nkv, hd, bits, seed=seed, before=[(few * 16, 1)])
+    cache, c = b[:2]
+    filled = b[2][0]
+    seqs, starts, shared, rows = [], [0], [], []
+    width = max((n + 15) // 16 for _, m in lens_groups for n, _ in m)
+    for sh, members in lens_groups:
+        first = rng.choice(filled, sh // 16)
+        for n, m in members:
+            seqs.append((n, m))
+            rows.append(np.concatenate((first, rng.choice(filled, width - len(first)))))
+        starts.append(len(seqs))
+        shared.append(sh)
+    cu = np.concatenate(([0], np.cumsum([m for _, m in seqs]))).astype(np.int32)
+    q = (rng.standard_normal((int(cu[-1]), nq, hd)) / np.sqrt(hd)).astype(np.float16)
+    return (cache, c, np.int32(rows), np.int32([n for n, _ in seqs]), cu, q), np.int32(starts), np.int32(shared), max(m for _, m in seqs)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("groups", [
+    [(20000, [(20100, 1), (20001, 1)])],
+    [(9000, [(9100, 1)] * 9)],                               # parts of a prompt item's keys
+    [(9000, [(9100, 3)] * 9), (5000, [(5003, 1), (7000, 1)])],
+    [(6400, [(6500, 30), (6420, 11)])],                      # parts of the group's and of the sequences' keys
+])
+def test_long_shared_contexts(groups, bits):
+    b, starts, shared, max_q = repeated(groups, 6, 2, 64, bits)
+    got = run_shared(b, starts, shared, max_q)
+    check_attention(got, *b)
+    assert np.array_equal(got, run_shared(b, starts, shared, max_q))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("members", [3, 40])
+def test_strange_values_in_the_shared_blocks(members, bits):
+    """Values that are infinite or NaN in shared places reach every row, those behind the shared tokens only the rows of their sequence."""
+    hd, nkv = 64, 2
+    b, starts, shared, max_q = make_groups([(128, [(140, 1)] * members)], 4, nkv, hd, bits, seed=9)
+    cache, c, tables, lens, cu, q = b
+    rng = np.random.default_rng(10)
+    for s, j, what, d in ((0, 20, np.inf, 3), (0, 70, np.nan, 40), (1, 130, -np.inf, 7), (2, 139, np.nan, 8)):
+        k, v = rng.standard_normal((2, nkv, hd))
+        v[1, d] = what
+        c.put(int(tables[s, j // 16]) * 16 + j % 16, k, v)
+    if bits == 16:
+        c.v[tables[0, 2], 0, 3, 5] = np.float16(np.inf)
+        c.v[tables[0, 2], 0, 4, 6] = np.float16(-np.inf)
+    cache.data.copy_(torch.from_numpy(c.data))
+    check_attention(run_shared(b, starts, shared, max_q), *b)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("members", [3, 40])
+def test_block_ids_outside_the_cache(members, bits):
+    b, starts, shared, max_q = make_groups([(192, [(200, 1)] * members)], 4, 2, 64, bits, seed=11)
+    b[2][:, 1], b[2][:, 7] = -1, 2 ** 31 - 1
+    b[2][1, 12] = b[0].desc.n_blocks
+    check_attention(run_shared(b, starts, shared, max_q), *b)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("shared", [[-5, 70], [2 ** 31 - 1, 70], [-2 ** 31, 0], [129, 1000]])
+def test_shared_lengths_that_do_not_fit(shared, bits):
+    """Nothing is shared beyond what every query of a sequence stands behind."""
+    b, starts, _, max_q = make_groups([ONE(128, [4, 30]), ONE(70, [1, 9, 4])], 4, 2, 64, bits, seed=12)
+    check_attention(run_shared(b, starts, np.int32(shared), max_q), *b)
+
+
+@pytest.mark.parametrize("starts", [[-3, 2, 5], [0, 2, 2 ** 31 - 1], [2, 2, 2], [5, 5, 5], [0, 0, 2]])
+def test_groups_that_are_cut_or_empty(starts):
+    b, _, shared, max_q = make_groups([ONE(128, [4, 30]), ONE(70, [1, 9, 4])], 4, 2, 64, 16, seed=13)
+    check_attention(run_shared(b, np.int32(starts), np.int32([64, 64]) if starts[0] == 0 and starts[1] == 0 else shared, max_q), *b)
+
+
+@pytest.mark.parametrize("starts", [[5, 2, 0], [4, 1, 5], [2 ** 31 - 1, -2 ** 31, 3]])
+@pytest.mark.parametrize("members", [2, 40])
+def test_starts_that_decrease_write_nothing_else(starts, members):
+    b, _, shared, max_q = make_groups([ONE(128, [4] * members), ONE(70, [1, 9, 4])], 4, 2, 64, 16, seed=14, extra_rows=3)
+    got = run_shared(b, np.int32(starts), shared, max_q)
+    assert (got[b[4][-1]:] == 9.0).all()
+    lens, cu = np.int32([2 ** 31 - 1, -5] + [40] * (len(b[3]) - 2)), np.int32(b[4][::-1].copy())
+    run_shared((*b[:3], lens, cu, b[5]), np.int32(starts), np.int32([2 ** 31 - 1, -1]), max_q)
+
+
+def test_rows_beyond_max_q_are_not_computed():
+    b, starts, shared, _ = make_groups([(70, [(80, 5), (75, 2), (90, 1)])], 4, 2, 64, 16, seed=15)
+    got = run_shared(b, starts, shared, 3)
+    assert (got[3:5] == 9.0).all()
+    full = run_shared(b, starts, shared, 5)
+    check_attention(full, *b)
+    assert np.allclose(got[:3], full[:3], atol=1e-2) and np.allclose(got[5:], full[5:], atol=1e-2)
+
+
+def test_large_batches():
+    """As many sequences and groups as a call takes."""
+    groups = [(64, [(65 + (i + j) % 20, 1) for j in range(3)]) for i in range(256)]
+    check(groups, 2, 1, 64, 4, seed=16)
+    b, starts, shared, max_q = make_groups([(64, [(66, 1)] * 500), (80, [(82, 1)] * 522)], 2, 1, 64, 16, seed=17)
+    check_attention(run_shared(b, starts, shared, max_q), *b)
+
+
+def test_strided_rows():
+    b, starts, shared, max_q = make_groups([ONE(128, [4, 9, 30])], 4, 2, 64, 16, seed=18)
+    cache, c, tables, lens, cu, q = b
+    T = q.shape[0]
+    wide_q, wide_o = torch.zeros(T, 9, 64, dtype=torch.float16, device="cuda"), torch.full((T, 7, 64), 3.0, dtype=torch.float16, device="cuda")
+    wide_q[:, 2:6] = dev(q)
+    work = torch.zeros(B.shared_attention_workspace_bytes(4, cache, 3, 1, T), dtype=torch.uint8, device="cuda")
+    B.shared_attention(wide_q[:, 2:6], cache, dev(tables), dev(lens), dev(cu), dev(starts), dev(shared), wide_o[:, 1:5], work)
+    o = wide_o.cpu().numpy()
+    check_attention(o[:, 1:5].astype(np.float64), *b)
+    assert (o[:, :1] == 3).all() and (o[:, 5:] == 3).all()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_in_a_graph_whose_groups_change_and_a_workspace_in_turn_with_other_calls(bits):
+    """Captured once, replayed with other groups and lengths; eager calls of other shapes and without groups on the same workspace in between."""
+    b, starts, shared, max_q = make_groups([ONE(200, [40] * 6), ONE(130, [60] * 5)], 8, 2, 128, bits, seed=19)
+    cache, c, tables, lens, cu, q = b
+    T, S = q.shape[0], len(lens)
+    o, os_, osh, omax = make_groups([(70, [(79, 9)] * 6)], 8, 2, 128, bits, seed=20)
+    n = max(B.shared_attention_workspace_bytes(8, cache, S, 2, T), B.shared_attention_workspace_bytes(8, o[0], 6, 1, o[5].shape[0], omax))
+    work = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    args = [dev(x) for x in (q, tables, lens, cu, starts, shared)]
+    out = torch.zeros(q.shape, dtype=torch.float16, device="cuda")
+    call = lambda: B.shared_attention(args[0], cache, *args[1:], out, work)      # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for i, (st, sh) in enumerate((([0, 6, 11], [200, 130]), ([0, 3, 6], [200, 64]), ([0, 0, 0], [0, 0]), ([6, 9, 11], [70, 130]))):
+        now = np.int32(lens - i)
+        args[2].copy_(dev(now)); args[4].copy_(dev(np.int32(st))); args[5].copy_(dev(np.int32(sh)))
+        out.fill_(9.0)
+        g.replay()
+        torch.cuda.synchronize()
+        got = out.double().cpu().numpy()
+        check_attention(got, cache, c, tables, now, cu, q)
+        check_attention(run_attention(cache, tables, lens, cu, q, 1, workspace=work), *b)
+        check_attention(run_shared(o, os_, osh, omax, workspace=work), *o)
+        check_attention(run_shared(b, starts, shared, max_q, workspace=work), *b)
