@@ -323,26 +323,24 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
 }
 
 // ---- attention of groups --------------------------------------------------------------------------------------------------------
-// Rows of a sequence and of a group are the short part's up to 16 ct. The host knows the longest run of queries, and of a group only that it has
-// no more rows than all tokens have.
+// Rows of a sequence and of a group are the few-row part's up to 16 ct: what the sequences with the most queries need, or (where all tokens' rows fit)
+// any group.
 struct SharedPlan {
-  u32 ct, wgs, threads, n_splits;
-  bool prompt;
-  u64 part_bytes, prompt_bytes, row_bytes;
-  u64 bytes(u32 n_cu) const { return paged_ctr_bytes(n_cu) + part_bytes + prompt_bytes + row_bytes; }
+  u32 ct, n_splits;
+  u64 part_bytes, prompt_bytes, flat_bytes, row_bytes, token_bytes;
+  u64 bytes(u32 n_cu) const { return paged_ctr_bytes(n_cu) + part_bytes + prompt_bytes + flat_bytes + row_bytes + token_bytes; }
 };
-static SharedPlan shared_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_tokens, u32 max_q, u32 key_steps, u32 n_cu) {
+static SharedPlan shared_plan(u32 hd, u32 nq, u32 nkv, u32 n_tokens, u32 max_q, u32 key_steps, u32 n_cu) {
   SharedPlan p{};
   const u32 G = nq / nkv, most = 16u * SHORT_MORE(hd);
   const u64 own = (u64)max_q * G, all = (u64)n_tokens * G;
   p.ct = (all <= most ? all > 16 : own > 16 && own <= most) ? SHORT_MORE(hd) : 1;
-  p.prompt = all > 16u * p.ct;
-  p.wgs = n_cu * (p.prompt ? 1 : SHORT_PER_CU(bits, p.ct));
-  p.threads = 64 * (p.prompt ? PAGED_WAVES : SHORT_WAVES(bits, p.ct));
-  p.n_splits = p.prompt ? std::max(1u, key_steps / 4) : 1;       // (parts of 256 keys at least)
-  p.part_bytes = short_floats(p.wgs, hd, p.ct) * 4;
-  p.prompt_bytes = p.prompt ? (u64)p.wgs * PROMPT_SLOT(hd) * 4 : 0;
+  p.n_splits = std::max(1u, key_steps / 4);          // (parts of 256 keys at least)
+  p.part_bytes = short_floats(n_cu, hd, p.ct) * 4;
+  p.prompt_bytes = (u64)n_cu * PROMPT_SLOT(hd) * 4;
+  p.flat_bytes = 2 * p.prompt_bytes;
   p.row_bytes = 2ull * n_tokens * nq * ROW_RESULT(hd) * 4;
+  p.token_bytes = (n_tokens + 1ull) * sizeof(JoinToken);
   return p;
 }
 static int check_groups(u32 n_seqs, u32 n_groups) {
@@ -356,19 +354,18 @@ extern "C" int blink_shared_attention_workspace_bytes(int32_t device, const blin
   if ((u64)n_tokens * n_q_heads >= (1ull << 31)) return fail(BLINK_ERR_TOO_LARGE, "2^31 rows or more");
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  const u32 hd = c->head_dim, more = SHORT_MORE(hd);
-  const u64 part = std::max(short_floats(n_cu * SHORT_PER_CU(c->bits, 1), hd, 1), short_floats(n_cu * SHORT_PER_CU(c->bits, more), hd, more)) * 4;
-  *bytes = std::max<u64>(*bytes, paged_ctr_bytes(n_cu) + part + (u64)n_cu * PROMPT_SLOT(hd) * 4 + 2ull * n_tokens * n_q_heads * ROW_RESULT(hd) * 4);
+  SharedPlan plan = shared_plan(c->head_dim, n_q_heads, c->n_kv_heads, n_tokens, max_q, 1, n_cu);
+  plan.part_bytes = short_floats(n_cu, c->head_dim, SHORT_MORE(c->head_dim)) * 4;
+  *bytes = std::max<u64>(*bytes, plan.bytes(n_cu));
   return BLINK_OK;
 }
 
 template <int HD, int BITS>
-static hipError_t launch_shared(const SharedArgs& args, const SharedPlan& plan, u32 n_cu, hipStream_t st) {
-  constexpr int MORE = SHORT_MORE(HD);
-  const hipError_t e = plan.prompt ? (plan.ct == 1 ? launch(k_shared_both<HD, BITS, 1>, plan.wgs, plan.threads, st, args) : launch(k_shared_both<HD, BITS, MORE>, plan.wgs, plan.threads, st, args))
-                                   : (plan.ct == 1 ? launch(k_shared_short<HD, BITS, 1>, plan.wgs, plan.threads, st, args) : launch(k_shared_short<HD, BITS, MORE>, plan.wgs, plan.threads, st, args));
-  const u32 wgs = (u32)std::min<u64>(((u64)args.n_tokens * args.nq + PAGED_WAVES - 1) / PAGED_WAVES, 3 * n_cu);
-  return e == hipSuccess ? launch(k_shared_join<HD>, wgs, 64 * PAGED_WAVES, st, args, plan.prompt ? plan.wgs : 0u) : e;
+static hipError_t launch_shared(const SharedArgs& args, u32 ct, u32 n_cu, hipStream_t st) {
+  constexpr u32 NT = 64 * PAGED_WAVES;
+  const hipError_t e = ct == 1 ? launch(k_shared_attention<HD, BITS, 1>, n_cu, NT, st, args) : launch(k_shared_attention<HD, BITS, SHORT_MORE(HD)>, n_cu, NT, st, args);
+  const u64 waves = (u64)args.n_tokens * args.nkv * ((args.G + join_heads<HD>() - 1) / join_heads<HD>());
+  return e == hipSuccess ? launch(k_shared_join<HD>, (u32)((waves * 64 + BLK_THREADS - 1) / BLK_THREADS), BLK_THREADS, st, args) : e;
 }
 
 extern "C" int blink_shared_attention(int32_t device, const blink_shared_attention_args* s, void* stream) {
@@ -386,18 +383,20 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   if (!s->group_starts || !s->shared_lens || (u64)s->group_starts % 4 || (u64)s->shared_lens % 4) return fail(BLINK_ERR_INVAL, "group_starts or shared_lens is null or not aligned");
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  const SharedPlan plan = shared_plan(hd, a->cache.bits, a->n_q_heads, nkv, a->n_tokens, a->max_q, a->max_blocks / 4 + 1, n_cu);
+  const SharedPlan plan = shared_plan(hd, a->n_q_heads, nkv, a->n_tokens, a->max_q, a->max_blocks / 4 + 1, n_cu);
   if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.bytes(n_cu))
     return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)plan.bytes(n_cu));
   OnDevice on(device);
   HIPCHK(on.err);
   SharedArgs p{};
   fill_paged(p, a, scale2, 16 * plan.ct, plan.n_splits, n_cu);
-  p.prompt_part = p.part + plan.part_bytes / 4;
-  p.rows = p.prompt_part + plan.prompt_bytes / 4;
+  p.own_part = p.part + plan.part_bytes / 4;
+  p.prompt_part = p.own_part + plan.prompt_bytes / 4;
+  p.rows = p.prompt_part + plan.flat_bytes / 4;
+  p.tokens = (JoinToken*)(p.rows + plan.row_bytes / 4);
   p.n_groups = s->n_groups; p.starts = s->group_starts; p.shared = s->shared_lens;
   const hipStream_t st = (hipStream_t)stream;
-  HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_shared<64, 16>(p, plan, n_cu, st) : launch_shared<64, 4>(p, plan, n_cu, st))
-                  : (a->cache.bits == 16 ? launch_shared<128, 16>(p, plan, n_cu, st) : launch_shared<128, 4>(p, plan, n_cu, st)));
+  HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_shared<64, 16>(p, plan.ct, n_cu, st) : launch_shared<64, 4>(p, plan.ct, n_cu, st))
+                  : (a->cache.bits == 16 ? launch_shared<128, 16>(p, plan.ct, n_cu, st) : launch_shared<128, 4>(p, plan.ct, n_cu, st)));
   return BLINK_OK;
 }

@@ -46,6 +46,8 @@ struct SharedArgs : PagedArgs {
   u32 n_groups;
   const i32 *starts, *shared;     // first sequence of every group (n_groups + 1), tokens that its sequences share
   float* rows;                    // results to be joined: [of the group, of the sequence][token][q head] of ROW_RESULT(hd) floats
+  float* own_part;                // parts of prompt items (prompt_part: of the groups' items)
+  struct JoinToken* tokens;       // what is to be joined of every token, and behind them the units of a workgroup's run (FlatRun)
 };
 #define ROW_RESULT(HD) ((HD) + 4u)                   // maximum, sum, two unused, output
 template <typename A> constexpr bool is_shared = std::is_same<A, SharedArgs>::value;
@@ -62,7 +64,7 @@ struct SeqView {
 struct SharedView {
   u32 t0, n;
   i32 pos0;
-  u32 first, row;                                    // row: of the table
+  u32 first, row;                                    // row: of a group, of the table; of a sequence, its group (first != 0)
   __device__ __forceinline__ u32 lo() const { return first; }
 };
 __device__ __forceinline__ SeqView seq_view(const PagedArgs& a, u32 s) {
@@ -313,6 +315,11 @@ struct CacheTile<HD, 4> {
 #define PAGED_WAVES 8              // waves of a workgroup of the prompt part
 #define PAGED_MAX_SEQS 1024u       // sequences (and groups) whose views a workgroup keeps in LDS
 #define SHARED_ROWS 256u           // sequences with so many rows fill a prompt item by themselves
+// Times on one compute unit, in those of a unit of the groups' shared keys (half a step of 256 rows, 1 us with heads of 128), by which workgroups are
+// dealt out: a tile of few rows; what a pair of a sequence and a kv head takes beside its tiles, in tiles; an item of many rows beside its steps
+#define FEW_COST .25f
+#define FEW_PAIR 2u
+#define FLAT_LEAD 5u
 struct NoLinks {};
 struct ViewLinks { uint16_t link[PAGED_MAX_SEQS]; };      // of a sequence: its group, or NO_GROUP; of a group: the sequence whose table it takes
 #define NO_GROUP 0xFFFFu
@@ -539,12 +546,11 @@ __device__ __forceinline__ void give_strange(const CacheTile<HD, BITS>& t, float
   }
 }
 
-// The views of a call with groups, by a workgroup of NT threads: of every sequence (i, its group or NO_GROUP, view), of every group (n_seqs + its number, the
-// sequence whose table it takes, view), each by some thread. A sequence goes by its group where it gains by that and may: it has fewer rows than a prompt item,
+// The views of a call with groups, by a workgroup of NT threads, in LDS: those of the sequences, then those of the groups. A sequence goes by its group where it gains by that and may: it has fewer rows than a prompt item,
 // all its queries stand behind the shared keys and see every one of them, and it is not the only one. The shared keys are cut to a multiple of 64, what a step of
 // the prompt part takes. room: 4 n_groups + 1 words of LDS.
-template <u32 NT, typename P>
-__device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, P put) {
+template <u32 NT>
+__device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, SharedView* view) {
   u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const to = from + a.n_groups;
   for (u32 g = threadIdx.x; g <= a.n_groups; g += NT) {
     starts[g] = (u32)max(0, min(a.starts[g], (i32)a.n_seqs));
@@ -577,24 +583,27 @@ __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, P p
     const u32 s = threadIdx.x + j * NT, g = group[j];
     if (s >= a.n_seqs) continue;
     const bool in = g != NO_GROUP && from[g] < to[g];
-    put(s, in ? g : NO_GROUP, SharedView{v[j].t0, v[j].n, v[j].pos0, in ? keys[g] : 0u, s});
+    view[s] = SharedView{v[j].t0, v[j].n, v[j].pos0, in ? keys[g] : 0u, g};
   }
   __syncthreads();
   for (u32 g = threadIdx.x; g < a.n_groups; g += NT) {
     SharedView x = {0, 0, -1, 0, 0};
     if (from[g] < to[g]) {
-      const SeqView b = seq_view(a, from[g]), e = seq_view(a, to[g]);
-      x = {b.t0, e.t0 + e.n > b.t0 ? e.t0 + e.n - b.t0 : 0u, (i32)keys[g] - 1, 0, from[g]};
+      const u32 t0 = view[from[g]].t0, end = view[to[g]].t0 + view[to[g]].n;
+      x = {t0, end > t0 ? end - t0 : 0u, (i32)keys[g] - 1, 0, from[g]};
     }
-    put(a.n_seqs + g, x.row, x);
+    view[a.n_seqs + g] = x;
   }
   __syncthreads();
 }
 
-template <typename View>
-__device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const View& v, i32 p1) {     // tiles of a view and kv head; 0: not this part's, 1 at least else
+__device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqView& v) {     // tiles of a sequence and kv head; 0: not this part's, 1 at least else
   if (!v.n || v.n * a.G > a.short_rows) return 0;
-  return max(1u, seen_tiles<16>(a, v.pos0, p1, v.lo()).n);
+  return max(1u, seen_tiles<16>(a, v.pos0, v.pos0 + (i32)v.n - 1).n);
+}
+__device__ __forceinline__ u32 short_unit_count(const SharedArgs& a, const SharedView& v, bool group) {
+  if (!v.n || v.n * a.G > a.short_rows) return 0;
+  return max(1u, seen_tiles<16>(a, v.pos0, group ? v.pos0 : v.pos0 + (i32)v.n - 1, v.first).n);
 }
 // whether a view's results are joined with others
 template <typename Shared>
@@ -636,11 +645,6 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
   typedef CacheTile<HD, BITS> Tile;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
   auto scalar = [](u32 x) { return (u32)__builtin_amdgcn_readfirstlane(x); };
-  auto note_view = [&](u32 s, const auto& v, i32 p1) {
-    const u32 n = short_unit_count(a, v, p1);
-    sh.pos0[s] = v.pos0; sh.n[s] = n ? (unsigned char)v.n : (unsigned char)0;
-    return n;
-  };
   // of a view: position of the last query, first key (only where there are groups is it another one than of a sequence's own)
   auto last_pos = [&](u32 s, i32 p0, i32 n) { return p0 + (SHARED && s >= a.n_seqs ? 1 : n) - 1; };
   auto first_key = [&](u32 s) {
@@ -653,16 +657,11 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
       return n ? max(1u, seen_tiles<16>(a, p0, last_pos(s, p0, n), first_key(s)).n) : 0u;
     } else {
       const SeqView v = seq_view(a, s);
-      const u32 n = short_unit_count(a, v, v.pos0 + (i32)v.n - 1);
+      const u32 n = short_unit_count(a, v);
       sh.pos0[s] = v.pos0; sh.n[s] = n ? (unsigned char)v.n : (unsigned char)0;
       return n;
     }
   };
-  if constexpr (SHARED)
-    shared_views<64 * NW>(a, (u32*)sh.o, [&](u32 s, u32 link, const SharedView& v) {
-      sh.link[s] = (uint16_t)link;
-      note_view(s, v, s < a.n_seqs ? v.pos0 + (i32)v.n - 1 : v.pos0);
-    });
   // Pairs dealt out whole: `cap` tiles of one at most to a workgroup, as few as there are workgroups for, but 32, and more (up to 64)
   // where results would be more than groups of groups take (65531 keys in 4 bits: 21.9 us with 64 results a pair, 23.2 with 128; 16384
   // keys: 19.3 with 16, 16.5 with 32). Then `pre` counts workgroups, else units.
@@ -1024,9 +1023,8 @@ struct PromptRoom {
   View view[PAGED_MAX_SEQS];         // (an item begins without asking memory for them: two prompts of 4000 behind a window, four items a workgroup: 169 us -> 165)
 };
 typedef PromptRoom<SeqView> PromptShared;
-template <typename A> struct PromptKinds { typedef SeqView View; };
-template <> struct PromptKinds<SharedArgs> { typedef SharedView View; };
-template <typename A> using PromptRoomOf = PromptRoom<typename PromptKinds<A>::View>;
+struct SharedRoom : PromptRoom<SharedView> { u32 flat[PAGED_MAX_SEQS + 1], sum[2]; };      // units of the groups before each; of the few rows' tiles, of prompt items' steps
+template <typename A> using PromptRoomOf = typename std::conditional<is_shared<A>, SharedRoom, PromptShared>::type;
 template <typename View>
 __device__ __forceinline__ u32 prompt_items(const PagedArgs& a, const View& v) {
   return v.n * a.G <= a.short_rows ? 0u : (v.n * a.G + PROMPT_ROWS - 1) / PROMPT_ROWS;
@@ -1038,10 +1036,9 @@ struct PromptItem { u32 s, g, r0, rows, t0; i32 p0, p1; u32 lo, row; };      // 
 template <typename A, typename F>
 __device__ __forceinline__ PromptItem prompt_item(const A& a, const u32* pre, u32 item, F view) {
   PromptItem it;
-  const u32 views = n_views(a);
-  const u32 gi = pre[views] - 1 - item / a.nkv;                // the last queries (the longest walks) first
+  const u32 gi = pre[a.n_seqs] - 1 - item / a.nkv;             // the last queries (the longest walks) first
   it.g = item % a.nkv;
-  it.s = last_at_most(pre, views, gi);
+  it.s = last_at_most(pre, a.n_seqs, gi);
   const auto v = view(it.s);
   it.r0 = (gi - pre[it.s]) * PROMPT_ROWS;
   it.rows = min(PROMPT_ROWS, v.n * a.G - it.r0);
@@ -1051,8 +1048,7 @@ __device__ __forceinline__ PromptItem prompt_item(const A& a, const u32* pre, u3
   it.lo = v.lo();
   it.row = it.s;
   if constexpr (is_shared<A>) {
-    it.row = v.row;
-    if (it.s >= a.n_seqs) it.p0 = it.p1 = v.pos0;
+    it.row = it.s;
   }
   return it;
 }
@@ -1091,18 +1087,58 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 template <int N> __device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
-template <int HD, int BITS, typename A>
-__device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u32 wg, u32 nwg, bool behind_short) {
+// The groups with more rows than the few-row part takes: their rows in items of FLAT_ROWS (whole queries), each with all shared keys. All steps of
+// all (group, kv head, item) are one line of units, one or (items of more than 128 rows, which take about twice as long) two a step and FLAT_LEAD ahead of an
+// item's, and every workgroup has an equal run of it. An item inside a run is done there; one that several runs share leaves a result in each.
+__device__ __forceinline__ u32 flat_rows(const PagedArgs& a) { return PROMPT_ROWS / a.G * a.G; }
+struct FlatShape {
+  u32 row_items, steps, weight;
+  __device__ __forceinline__ u32 units() const { return steps * weight + FLAT_LEAD; }      // of an item
+};
+__device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, const SharedView& v) {
+  const u32 rows = v.n * a.G, per = flat_rows(a);
+  return {(rows + per - 1) / per, (u32)(v.pos0 + 1) / 64, min(rows, per) > 128 ? 2u : 1u};
+}
+__device__ __forceinline__ u32 flat_units(const SharedArgs& a, const SharedView& v) {      // of a group
+  if (v.n * a.G <= a.short_rows) return 0;
+  const FlatShape f = flat_shape(a, v);
+  return f.row_items * f.units() * a.nkv;
+}
+struct FlatRun { u32 from, end; };
+struct FlatPiece { u32 s_lo, s_hi, next; bool whole, begins, any; };       // any: has steps (or a half of one)
+template <typename Room>
+__device__ __forceinline__ PromptItem flat_piece(const SharedArgs& a, const Room& sh, u32 u, u32 end, FlatPiece& p) {
+  PromptItem it;
+  const u32 g = last_at_most(sh.flat, a.n_groups, u);
+  const SharedView v = sh.view[a.n_seqs + g];
+  const FlatShape f = flat_shape(a, v);
+  const u32 per = f.units(), x = u - sh.flat[g], item = x / per, off = x - item * per, to = min(per, off + end - u);
+  auto step = [&](u32 at) { return at > FLAT_LEAD ? (at - FLAT_LEAD + f.weight - 1) / f.weight : 0u; };
+  p = {step(off), step(to), u + to - off, off <= FLAT_LEAD && to == per, off <= FLAT_LEAD, to > FLAT_LEAD};
+  it.s = a.n_seqs + g;
+  it.g = item / f.row_items;
+  it.r0 = (item - it.g * f.row_items) * flat_rows(a);
+  it.rows = min(flat_rows(a), v.n * a.G - it.r0);
+  it.t0 = v.t0; it.p0 = it.p1 = v.pos0; it.lo = 0; it.row = v.row;
+  return it;
+}
+
+__device__ __forceinline__ float* own_parts(const PagedArgs& a) { return a.prompt_part; }
+__device__ __forceinline__ float* own_parts(const SharedArgs& a) { return a.own_part; }
+// FLAT: the groups' shared keys in place of prompts, workgroup wg's run of them. All rows see all keys, so what is done for masks falls away, but
+// for blocks outside the cache.
+template <int HD, int BITS, bool FLAT = false, typename A>
+__device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u32 wg, u32 nwg, bool behind_short, FlatRun run = FlatRun{0, 0}) {
   constexpr bool SHARED = is_shared<A>;
   constexpr int CT = PROMPT_CT;
   constexpr u32 BLK = 16 * HD * 2, NB = 4, STAGE = 2 * NB * BLK, NS = BITS == 4 ? 2 : (PROMPT_RING / STAGE > 6 ? 6 : PROMPT_RING / STAGE), TPW = BLK / 1024;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
-  if constexpr (SHARED) shared_views<64 * PAGED_WAVES>(a, (u32*)sh.ring, [&](u32 s, u32, const SharedView& v) { sh.view[s] = v; });
-  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, n_views(a), [&](u32 s) {
-    if constexpr (!SHARED) sh.view[s] = seq_view(a, s);
-    return prompt_items(a, sh.view[s]);
-  });
-  const u32 items = (u32)__builtin_amdgcn_readfirstlane(sh.pre[n_views(a)]) * a.nkv, parts = prompt_parts(a, items, nwg), total = items * parts;
+  if constexpr (!SHARED)                             // (else they are there)
+    prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, a.n_seqs, [&](u32 s) {
+      sh.view[s] = seq_view(a, s);
+      return prompt_items(a, sh.view[s]);
+    });
+  const u32 items = FLAT ? 0u : (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]) * a.nkv, parts = FLAT ? 1u : prompt_parts(a, items, nwg), total = FLAT ? run.end : items * parts;
   u32* const ctr = a.ctr;
   const u32 lds0 = (u32)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sh.ring;
   // fetching halves: waves 0-3 the K of a block each, waves 4-7 the V (places in LDS: attn_prompt)
@@ -1125,8 +1161,8 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
   if (threadIdx.x < 3) sh.strange[threadIdx.x] = 0;
   __syncthreads();
   // (behind the short part a workgroup may come late: then its first item comes from the counter too)
-  u32 turn = wg;
-  if (behind_short && total) {
+  u32 turn = FLAT ? run.from : wg;
+  if (!FLAT && behind_short && total) {
     if (threadIdx.x == 0) sh.next_item[1] = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item[1]);
@@ -1134,19 +1170,25 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
   for (u32 nth = 0; turn < total; ++nth) {
     u32 after = 0, *const strange = sh.strange + nth % 3;
     if (threadIdx.x == 0) {
-      after = (behind_short ? 0u : nwg) + __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if constexpr (!FLAT) after = (behind_short ? 0u : nwg) + __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       sh.strange[(nth + 1) % 3] = 0;                            // (read last two items ago)
     }
     const u32 this_turn = turn, item = turn / parts, part = turn - item * parts;
-    PromptItem it = prompt_item(a, sh.pre, item, [&](u32 s) { return sh.view[s]; });
+    PromptItem it;
+    FlatPiece piece;
+    if constexpr (FLAT) {
+      it = flat_piece(a, sh, turn, total, piece);
+      if (!piece.any) return;                        // (the end of the run, within an item's lead)
+    } else it = prompt_item(a, sh.pre, item, [&](u32 s) { return sh.view[s]; });
     it.s = (u32)__builtin_amdgcn_readfirstlane(it.s); it.g = (u32)__builtin_amdgcn_readfirstlane(it.g); it.r0 = (u32)__builtin_amdgcn_readfirstlane(it.r0);
     it.rows = (u32)__builtin_amdgcn_readfirstlane(it.rows); it.t0 = (u32)__builtin_amdgcn_readfirstlane(it.t0);
     it.p0 = __builtin_amdgcn_readfirstlane(it.p0); it.p1 = __builtin_amdgcn_readfirstlane(it.p1);
     if constexpr (SHARED) { it.lo = (u32)__builtin_amdgcn_readfirstlane(it.lo); it.row = (u32)__builtin_amdgcn_readfirstlane(it.row); }
-    const bool group = SHARED && it.s >= a.n_seqs;              // (all its rows stand at one position)
-    const Seen e = seen_tiles<64>(a, it.p0, it.p1, SHARED ? it.lo : 0u);
-    const u32 zb = (u32)__builtin_amdgcn_readfirstlane(e.zb), wlo = (u32)__builtin_amdgcn_readfirstlane(e.wlo), n_steps = (u32)__builtin_amdgcn_readfirstlane(e.n);
-    const u32 per = (n_steps + parts - 1) / parts, s_lo = min(part * per, n_steps), s_hi = min(s_lo + per, n_steps);
+    Seen e = {0, 0, 0};
+    if constexpr (FLAT) e.n = (u32)(it.p1 + 1) / 64; else e = seen_tiles<64>(a, it.p0, it.p1, SHARED ? it.lo : 0u);
+    const u32 zb = FLAT ? 0u : (u32)__builtin_amdgcn_readfirstlane(e.zb), wlo = FLAT ? 0u : (u32)__builtin_amdgcn_readfirstlane(e.wlo), n_steps = (u32)__builtin_amdgcn_readfirstlane(e.n);
+    u32 per = (n_steps + parts - 1) / parts, s_lo = min(part * per, n_steps), s_hi = min(s_lo + per, n_steps);
+    if constexpr (FLAT) { s_lo = (u32)__builtin_amdgcn_readfirstlane(piece.s_lo); s_hi = (u32)__builtin_amdgcn_readfirstlane(piece.s_hi); }
     const u32 last_block = (u32)max(0, it.p1) / 16;
     const u32 row = SHARED ? it.row : a.table_row ? (u32)__builtin_amdgcn_readfirstlane(a.table_row[it.s]) : it.s;
     const_u32* const bt = (const_u32*)(u64)uniform_ptr(a.tables + (u64)row * a.max_blocks);
@@ -1155,13 +1197,13 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
     // this wave's rows
     const u32 wr = w * (16 * CT);
     const bool live = wr < it.rows;
-    const i32 wp0 = group ? it.p0 : it.p0 + (i32)((it.r0 % a.G + wr) / a.G), wp1 = group ? it.p0 : it.p0 + (i32)((it.r0 % a.G + min(wr + 16 * CT, it.rows) - 1) / a.G);
+    const i32 wp0 = FLAT ? it.p0 : it.p0 + (i32)((it.r0 % a.G + wr) / a.G), wp1 = FLAT ? it.p0 : it.p0 + (i32)((it.r0 % a.G + min(wr + 16 * CT, it.rows) - 1) / a.G);
     f16x8_t q[CT][HD / 32];
     i32 qpos[CT];                                    // position of the lane's row (no row: before every key)
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const u32 r = wr + c * 16 + lc, rr = it.r0 + min(r, it.rows - 1), tok = rr / a.G, h = rr - tok * a.G;
-      qpos[c] = r < it.rows ? (group ? it.p0 : it.p0 - (i32)(it.r0 / a.G) + (i32)tok) : -1;
+      qpos[c] = r < it.rows ? it.p0 - (i32)(it.r0 / a.G) + (i32)tok : -1;
 #pragma unroll
       for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(a.q + (u64)(it.t0 + tok) * a.qs + (it.g * a.G + h) * HD + s * 32 + lg * 8);
     }
@@ -1177,9 +1219,9 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
     const i32 none = INT32_MIN, need_hi = live ? wp1 : -1, need_lo = a.window ? wp0 - (i32)a.window - 63 : none;
     const i32 edge_hi = wr + 16 * CT > it.rows ? none : wp0 - 63, edge_lo = a.window ? wp1 - (i32)a.window : none;
     const i32 item_hi = it.p0 - 63, item_lo = a.window ? it.p1 - (i32)a.window : none;
-    auto needed = [&](u32 k0) { return ((i32)k0 <= need_hi) & (((i32)k0 > need_lo) | (k0 < a.sinks)); };                              // by some row of this wave
-    auto item_edge = [&](u32 k0, u32 bad) { return ((i32)k0 > item_hi) | (bad != 0) | (((i32)k0 <= item_lo) & (k0 + 64 > a.sinks)); };      // not seen as a whole by every row of the item
-    auto edge_of = [&](u32 k0, u32 bad) { return ((i32)k0 > edge_hi) | (bad != 0) | (((i32)k0 <= edge_lo) & (k0 + 64 > a.sinks)); };        // nor by every one of this wave
+    auto needed = [&](u32 k0) { if constexpr (FLAT) return (int)live; return ((i32)k0 <= need_hi) & (((i32)k0 > need_lo) | (k0 < a.sinks)); };                              // by some row of this wave
+    auto item_edge = [&](u32 k0, u32 bad) { if constexpr (FLAT) return (int)(bad != 0); return ((i32)k0 > item_hi) | (bad != 0) | (((i32)k0 <= item_lo) & (k0 + 64 > a.sinks)); };      // not seen as a whole by every row of the item
+    auto edge_of = [&](u32 k0, u32 bad) { if constexpr (FLAT) return (int)(bad != 0); return ((i32)k0 > edge_hi) | (bad != 0) | (((i32)k0 <= edge_lo) & (k0 + 64 > a.sinks)); };        // nor by every one of this wave
     u32 id[NB], my_id = 0, bad_ahead = 0;            // ids of the stage to fetch next, and of this wave's block; which blocks of the stages in the ring are outside the cache, 4 bits each
     auto next_ids = [&](u32 s) {
       const u32 first = NB * tile_of(min(s, n_steps ? n_steps - 1 : 0u));
@@ -1384,7 +1426,7 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
             u32 vis = 0;                                         // bit 8 h + i: this lane's row sees its key i of the step's pair of blocks h
 #pragma unroll
             for (u32 h = 0; h < NB / 2; ++h)
-              if (!(bad >> (NB - 1 - (2 * h + (lg >> 1))) & 1u)) vis |= sees(a, qpos[c], (i32)(k0 + h * 32 + lg * 8)) << (8 * h);
+              if (!(bad >> (NB - 1 - (2 * h + (lg >> 1))) & 1u)) vis |= (FLAT ? 0xFFu : sees(a, qpos[c], (i32)(k0 + h * 32 + lg * 8))) << (8 * h);
 #pragma unroll
             for (u32 b = 0; b < NB; ++b)
 #pragma unroll
@@ -1428,7 +1470,8 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
     if constexpr (BITS == 16) wait_dma<0>();                   // (no fetch of this item is on its way any more)
     if (fk) lds_barrier();
     lds_barrier();
-    turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item[nth & 1]);
+    if constexpr (FLAT) turn = (u32)__builtin_amdgcn_readfirstlane(piece.next);
+    else turn = (u32)__builtin_amdgcn_readfirstlane(sh.next_item[nth & 1]);
     if ((u32)__builtin_amdgcn_readfirstlane(*strange)) {
 #pragma unroll 1
       for (u32 s = s_lo; s < s_hi; ++s) {
@@ -1442,7 +1485,7 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
           if (bad >> (NB - 1 - b) & 1u) continue;
           u32 vis[CT];
 #pragma unroll
-          for (int c = 0; c < CT; ++c) vis[c] = sees(a, qpos[c], (i32)(k0 + b * 16 + lg * 4)) & 15u;
+          for (int c = 0; c < CT; ++c) vis[c] = FLAT ? 15u : sees(a, qpos[c], (i32)(k0 + b * 16 + lg * 4)) & 15u;
           give_strange_block<HD, BITS, CT>(a, block_id(s, b), it.g, vis, o);
         }
       }
@@ -1456,16 +1499,16 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
       const u32 r = wr + c * 16 + lc_end;
       if (r >= it.rows) continue;
       bool to_row = false;
-      if constexpr (SHARED) to_row = parts == 1 && (group || it.lo);
+      if constexpr (SHARED) to_row = FLAT ? piece.whole : parts == 1 && it.lo;
       if (to_row) {
         if constexpr (SHARED) {
           const u32 rr = it.r0 + r, tok = rr / a.G;
-          float* const x = row_result<HD>(a, group ? 0u : 1u, it.t0 + tok, it.g * a.G + rr - tok * a.G);
+          float* const x = row_result<HD>(a, FLAT ? 0u : 1u, it.t0 + tok, it.g * a.G + rr - tok * a.G);
           if (lg_end == 0) *(float2*)x = make_float2(m[c], sum);
 #pragma unroll
           for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(x + 4 + d * 16 + lg_end * 4) = o[c][d];
         }
-      } else if (parts == 1) {
+      } else if (!FLAT && parts == 1) {
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
         const u32 rr = it.r0 + r, tok = rr / a.G, k = (it.g * a.G + rr - tok * a.G) * HD + lg_end * 4;
         f16_t* const to = out_at(a, it.t0 + tok, k);
@@ -1474,7 +1517,7 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
         for (int d = 0; d < HD / 16; ++d)
           *(uint2*)(to + (u64)(d / 2) * step + d % 2 * half) = make_uint2(half_pair(o[c][d][0] * inv, o[c][d][1] * inv), half_pair(o[c][d][2] * inv, o[c][d][3] * inv));
       } else {
-        float* const slot = a.prompt_part + (u64)this_turn * PROMPT_SLOT(HD);
+        float* const slot = (SHARED && !FLAT ? own_parts(a) : a.prompt_part) + (u64)(FLAT ? 2 * wg + (piece.begins ? 1u : 0u) : this_turn) * PROMPT_SLOT(HD);
         if (lg_end == 0) *(float2*)(slot + 2 * r) = make_float2(m[c], sum);
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(slot + 2 * PROMPT_ROWS + r * HD + d * 16 + lg_end * 4) = o[c][d];
@@ -1482,7 +1525,7 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
     }
   }
   // the last workgroup out leaves the counters as it found them
-  if (total && threadIdx.x == 0 && __hip_atomic_fetch_add(ctr + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == nwg - 1) {
+  if (!FLAT && total && threadIdx.x == 0 && __hip_atomic_fetch_add(ctr + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == nwg - 1) {
     __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(ctr + 1, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
@@ -1515,65 +1558,6 @@ __device__ __forceinline__ void prompt_merge(const PagedArgs& a, PromptMergeShar
     const u32 rr = it.r0 + r, tok = rr / a.G, h = rr - tok * a.G;
 #pragma unroll
     for (int d = 0; d < HD / 64; ++d) *out_at(a, it.t0 + tok, (it.g * a.G + h) * HD + d * 64 + lane) = (f16_t)half_pair(L == 0.f ? 0.f : O[d] / L, 0.f);
-  }
-}
-
-// Results joined: of a row whose keys are its group's and its sequence's, and of rows whose keys were cut into parts. A wave per row, its lanes along the
-// dimensions. What lies where is worked out as the launch before did (nwg_prompt: its workgroups, 0: without a prompt part).
-struct JoinShared {
-  SharedView view[PAGED_MAX_SEQS];
-  u32 pre[PAGED_MAX_SEQS + 1], wave_sum[PAGED_WAVES], room[4 * PAGED_MAX_SEQS + 1];
-  uint16_t group[PAGED_MAX_SEQS];
-};
-template <int HD>
-__device__ __forceinline__ void shared_join(const SharedArgs& a, JoinShared& sh, u32 wg, u32 nwg, u32 nwg_prompt) {
-  const u32 lane = threadIdx.x & 63;
-  shared_views<64 * PAGED_WAVES>(a, sh.room, [&](u32 s, u32 link, const SharedView& v) { sh.view[s] = v; sh.group[s] = (uint16_t)link; });
-  prefix_sums<PAGED_WAVES>(sh.pre, sh.wave_sum, n_views(a), [&](u32 s) { return nwg_prompt ? prompt_items(a, sh.view[s]) : 0u; });
-  const u32 item_rows = (u32)__builtin_amdgcn_readfirstlane(sh.pre[n_views(a)]), parts = prompt_parts(a, item_rows * a.nkv, nwg_prompt);
-  for (u32 i = wg * PAGED_WAVES + (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < a.n_tokens * a.nq; i += nwg * PAGED_WAVES) {
-    const u32 t = i / a.nq, head = i - t * a.nq, g = head / a.G;
-    // the sequence: the last that begins at this token or before and has it
-    u32 lo = 0;
-    for (u32 step = 512; step; step >>= 1) if (lo + step < a.n_seqs && sh.view[lo + step].t0 <= t) lo += step;
-    const SharedView v = sh.view[lo];
-    if (t < v.t0 || t - v.t0 >= v.n) continue;       // (no sequence's, or not looked at)
-    const bool in = v.first != 0, prompt = nwg_prompt && prompt_items(a, v) != 0, cut = prompt && parts > 1;
-    if (!in && !cut) continue;                       // (that was its only result)
-    float M = -INFINITY, L = 0.f, O[HD / 64];
-#pragma unroll
-    for (int d = 0; d < HD / 64; ++d) O[d] = 0.f;
-    auto add = [&](float m, float l, const float* o) {
-      const float mn = fmaxf(M, m), ref = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(M - ref), h = __builtin_amdgcn_exp2f(m - ref);
-      L = L * f + l * h;
-#pragma unroll
-      for (int d = 0; d < HD / 64; ++d) O[d] = O[d] * f + o[d * 64 + lane] * h;
-      M = mn;
-    };
-    // a view's result of its row r
-    auto take = [&](u32 which, u32 s, const SharedView& x, u32 r) {
-      if (nwg_prompt && prompt_items(a, x) && parts > 1) {
-        const u32 item = (item_rows - 1 - (sh.pre[s] + r / PROMPT_ROWS)) * a.nkv + g;
-        for (u32 p = 0; p < parts; ++p) {
-          const float* const b = a.prompt_part + ((u64)item * parts + p) * PROMPT_SLOT(HD);
-          const float2 ml = *(const float2*)(b + 2 * (r % PROMPT_ROWS));
-          add(ml.x, ml.y, b + 2 * PROMPT_ROWS + r % PROMPT_ROWS * HD);
-        }
-      } else {
-        const float* const b = row_result<HD>(a, which, t, head);
-        const float2 ml = *(const float2*)b;
-        add(ml.x, ml.y, b + 4);
-      }
-    };
-    const u32 h = head - g * a.G;
-    if (in) {
-      const u32 s = a.n_seqs + sh.group[lo];
-      const SharedView x = sh.view[s];
-      take(0, s, x, (t - x.t0) * a.G + h);
-    }
-    take(1, lo, v, (t - v.t0) * a.G + h);
-#pragma unroll
-    for (int d = 0; d < HD / 64; ++d) *out_at(a, t, head * HD + d * 64 + lane) = (f16_t)half_pair(L == 0.f ? 0.f : O[d] / L, 0.f);
   }
 }
 

@@ -17,6 +17,9 @@
 #define SHORT_WAVES(BITS, CT) (SHORT_SMALL(BITS, CT) ? 4 : 8)
 #define SHORT_PER_CU(BITS, CT) (SHORT_SMALL(BITS, CT) ? 3 : 1)
 
+#include "shared_attention.h"
+
+
 template <typename T, int HD, int BITS> __global__ void k_kv_store(StoreArgs a);
 __global__ void k_kv_read(ReadArgs a, u32 hd);
 __global__ void k_kv_copy(CopyArgs a);
@@ -25,8 +28,7 @@ template <int HD, int BITS, int CT> __global__ void k_paged_short(PagedArgs a);
 template <int HD, int BITS> __global__ void k_paged_prompt(PagedArgs a);
 template <int HD, int BITS> __global__ void k_paged_both(PagedArgs a);
 template <int HD> __global__ void k_paged_merge(PagedArgs a, u32 nwg_prompt);
-template <int HD, int BITS, int CT> __global__ void k_shared_short(SharedArgs a);
-template <int HD, int BITS, int CT> __global__ void k_shared_both(SharedArgs a);
-template <int HD> __global__ void k_shared_join(SharedArgs a, u32 nwg_prompt);
+template <int HD, int BITS, int CT> __global__ void k_shared_attention(SharedArgs a);
+template <int HD> __global__ void k_shared_join(SharedArgs a);
 template <int HD, int BITS> __global__ void k_store_phase(DevCtx c, u32 layer);
 template <int HD, int BITS, int CT> __global__ void k_attention_phase(DevCtx c, u32 layer);

@@ -1,0 +1,210 @@
+// Attention of a batch in which the sequences of a group have their first blocks in common (views, and the groups' shared keys: paged_attention.h): who has
+// which part of the work, and the results joined.
+#pragma once
+#include "paged_attention.h"
+
+// What is to be joined of a token's rows (kinds 0: nothing, its results are in place; 1: a result of its group and one of its sequence; 2: parts of a prompt
+// item's keys). Its group's: units[0] + kv head * units[1] is where its item's line of units[2] begins, row: its first row there. Its sequence's:
+// in rows, or parts of prompt items (parts > 1): items top - (row + head) / PROMPT_ROWS.
+struct JoinToken { u32 kind, units[3], row, own_row, top, parts; };
+
+// The work of a call with groups, by every workgroup all the same: views, who has the groups' shared keys and who the rest. Then notes for the join.
+struct SharedWork { u32 flat_wgs, quota; bool few, prompts; };
+// inclusive prefix sum over the wave, without LDS: sums over rows of 16 lanes, then the rows before
+__device__ __forceinline__ u32 wave_sums_dpp(u32 v) {
+  v += (u32)__builtin_amdgcn_update_dpp(0, (i32)v, 0x111, 0xF, 0xF, true);      // row_shr 1, 2, 4, 8
+  v += (u32)__builtin_amdgcn_update_dpp(0, (i32)v, 0x112, 0xF, 0xF, true);
+  v += (u32)__builtin_amdgcn_update_dpp(0, (i32)v, 0x114, 0xF, 0xF, true);
+  v += (u32)__builtin_amdgcn_update_dpp(0, (i32)v, 0x118, 0xF, 0xF, true);
+  v += (u32)__builtin_amdgcn_update_dpp(0, (i32)v, 0x142, 0xA, 0xF, false);     // row_bcast 15 to rows 1 and 3, 31 to rows 2 and 3
+  v += (u32)__builtin_amdgcn_update_dpp(0, (i32)v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+// Views; items of the prompts before each sequence (pre) and units of the shared keys before each group (flat); sum[0]: cost of all tiles of few rows, sum[1]: of the prompts.
+__device__ __forceinline__ void views_and_sums(const SharedArgs& a, SharedRoom& sh) {
+  constexpr u32 NT = 64 * PAGED_WAVES;
+  const u32 lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  shared_views<NT>(a, (u32*)sh.ring, sh.view);
+  u32 (*const of_wave)[4] = (u32(*)[4])sh.ring;
+  u32 base[4] = {0, 0, 0, 0};
+  for (u32 s0 = 0; s0 < n_views(a); s0 += NT) {
+    const u32 s = s0 + threadIdx.x;
+    u32 v[4] = {0, 0, 0, 0};                         // items, flat units, tiles of few rows, steps of prompt items
+    if (s < n_views(a)) {
+      const SharedView x = sh.view[s];
+      const bool group = s >= a.n_seqs;
+      if (group) v[1] = flat_units(a, x); else v[0] = prompt_items(a, x);
+      const u32 tiles = short_unit_count(a, x, group);
+      v[2] = (tiles ? tiles + FEW_PAIR : 0u) * a.nkv;
+      if (v[0]) v[3] = v[0] * (2 * seen_tiles<64>(a, x.pos0, x.pos0 + (i32)x.n - 1, x.first).n + FLAT_LEAD) * a.nkv;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = wave_sums_dpp(v[k]);
+    if (s0) __syncthreads();
+    if (lane == 63) *(uint4*)of_wave[w] = make_uint4(v[0], v[1], v[2], v[3]);
+    __syncthreads();
+#pragma unroll
+    for (u32 i = 0; i < PAGED_WAVES; ++i) {
+      const uint4 x = *(const uint4*)of_wave[i];
+      if (i < w) { v[0] += x.x; v[1] += x.y; }
+      base[2] += x.z; base[3] += x.w;
+      if (i == PAGED_WAVES - 1) {
+        if (s < a.n_seqs) sh.pre[s + 1] = base[0] + v[0];
+        else if (s < n_views(a)) sh.flat[s - a.n_seqs + 1] = base[1] + v[1];
+      }
+    }
+#pragma unroll
+    for (u32 i = 0; i < PAGED_WAVES; ++i) { base[0] += of_wave[i][0]; base[1] += of_wave[i][1]; }
+  }
+  if (threadIdx.x == 0) { sh.pre[0] = 0; sh.flat[0] = 0; sh.sum[0] = base[2]; sh.sum[1] = base[3]; }
+  __syncthreads();
+}
+template <int HD>
+__device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, SharedRoom& sh, u32 wg, u32 nwg) {
+  constexpr u32 NT = 64 * PAGED_WAVES;
+  views_and_sums(a, sh);
+  SharedWork r;
+  const u32 units = (u32)__builtin_amdgcn_readfirstlane(sh.flat[a.n_groups]);
+  const u32 tiles = (u32)__builtin_amdgcn_readfirstlane(sh.sum[0]), prompts = (u32)__builtin_amdgcn_readfirstlane(sh.sum[1]);
+  r.few = tiles != 0; r.prompts = prompts != 0;
+  const float flat = (float)units, rest = FEW_COST * (float)tiles + (float)prompts;
+  r.flat_wgs = !units ? 0u : rest == 0.f ? nwg : min(nwg - 1, max(1u, (u32)((float)nwg * flat / (flat + rest) + 0.5f)));
+  r.quota = r.flat_wgs ? (units + r.flat_wgs - 1) / r.flat_wgs : 1u;
+  if (wg == 0 && threadIdx.x == 0) *(u32*)(a.tokens + a.n_tokens) = r.quota;
+  // (the parts of prompt items: as the workgroups that take them cut them)
+  const u32 item_rows = (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]), parts = prompt_parts(a, item_rows * a.nkv, nwg - r.flat_wgs);
+  for (u32 t = wg * NT + threadIdx.x; t < a.n_tokens; t += nwg * NT) {
+    u32 s = 0;                                       // the last sequence that begins at this token or before
+    for (u32 step = PAGED_MAX_SEQS / 2; step; step >>= 1) if (s + step < a.n_seqs && sh.view[s + step].t0 <= t) s += step;
+    const SharedView v = sh.view[s];
+    JoinToken j = {};
+    if (t >= v.t0 && t - v.t0 < v.n) {
+      const bool cut = parts > 1 && prompt_items(a, v) != 0;
+      j.own_row = (t - v.t0) * a.G; j.top = item_rows - 1 - sh.pre[s]; j.parts = cut ? parts : 1;
+      j.kind = v.first ? 1 : cut ? 2 : 0;
+      if (v.first) {
+        const SharedView x = sh.view[a.n_seqs + v.row];
+        const u32 r = (t - x.t0) * a.G;
+        if (t - x.t0 < x.n && flat_units(a, x)) {    // (cu_seqlens that decrease may put a token outside its group)
+          const FlatShape f = flat_shape(a, x);
+          const u32 item = r / flat_rows(a), per = f.units();
+          j.units[0] = sh.flat[v.row] + item * per + FLAT_LEAD; j.units[1] = f.row_items * per; j.units[2] = per - FLAT_LEAD;
+          j.row = r - item * flat_rows(a);
+        } else j.units[2] = 1;                       // (by one workgroup, into rows)
+      }
+    }
+    a.tokens[t] = j;
+  }
+  __syncthreads();
+  return r;
+}
+
+// Results joined: of rows whose keys are their group's and their sequence's, and of rows whose keys were cut into parts. A wave per token, kv head and as many
+// of its query heads as it has HD / 4 lanes for.
+template <int HD> __host__ __device__ constexpr u32 join_heads() { return 64 / (HD / 4); }
+template <int HD>
+__device__ __forceinline__ void shared_join(const SharedArgs& a, u32 i) {
+  constexpr u32 LANES = HD / 4, AT_ONCE = 8;
+  const u32 per = (a.G + join_heads<HD>() - 1) / join_heads<HD>(), lane = threadIdx.x & 63, d = lane % LANES * 4;
+  const u32 t = i / (a.nkv * per), g = i / per % a.nkv, h = i % per * join_heads<HD>() + lane / LANES;
+  if (t >= a.n_tokens) return;
+  const JoinToken j = a.tokens[t];
+  if (!j.kind) return;
+  const u32 quota = *(const u32*)(a.tokens + a.n_tokens);
+  if (h < a.G) {
+    float M = -INFINITY, L = 0.f;
+    floatx4_t O = {0.f, 0.f, 0.f, 0.f};
+    // n results, result(x): maximum and sum, output
+    auto take = [&](u32 n, auto ml, auto out) {
+      for (u32 x = 0; x < n; x += AT_ONCE) {
+        float2 v[AT_ONCE];
+        floatx4_t o[AT_ONCE];
+#pragma unroll
+        for (u32 b = 0; b < AT_ONCE; ++b) {
+          v[b] = make_float2(-INFINITY, 0.f);
+          o[b] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+          if (x + b < n) { v[b] = *(const float2*)ml(x + b); o[b] = *(const floatx4_t*)out(x + b); }
+        }
+        float mn = M;
+#pragma unroll
+        for (u32 b = 0; b < AT_ONCE; ++b) mn = fmaxf(mn, v[b].x);
+        const float ref = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(M - ref);
+        L *= f; O *= f;
+#pragma unroll
+        for (u32 b = 0; b < AT_ONCE; ++b) {
+          const float k = __builtin_amdgcn_exp2f(v[b].x - ref);
+          L += v[b].y * k;
+          O += o[b] * k;
+        }
+        M = mn;
+      }
+    };
+    auto of_row = [&](u32 which) {
+      const float* const b = row_result<HD>(a, which, t, g * a.G + h);
+      take(1, [&](u32) { return b; }, [&](u32) { return b + 4 + d; });
+    };
+    if (j.kind == 1) {
+      const u32 begin = j.units[0] + g * j.units[1], w0 = begin / quota, w1 = (begin + j.units[2] - 1) / quota, r = j.row + h;
+      if (w0 == w1) of_row(0);
+      else {
+        auto slot = [&](u32 x) { return a.prompt_part + (u64)(2 * (w0 + x) + (x ? 0u : 1u)) * PROMPT_SLOT(HD); };
+        take(w1 - w0 + 1, [&](u32 x) { return slot(x) + 2 * r; }, [&](u32 x) { return slot(x) + 2 * PROMPT_ROWS + r * HD + d; });
+      }
+    }
+    if (j.parts > 1) {
+      const u32 r = j.own_row + h, item = (j.top - r / PROMPT_ROWS) * a.nkv + g, in = r % PROMPT_ROWS;
+      const float* const first = a.own_part + (u64)item * j.parts * PROMPT_SLOT(HD);
+      take(j.parts, [&](u32 x) { return first + (u64)x * PROMPT_SLOT(HD) + 2 * in; }, [&](u32 x) { return first + (u64)x * PROMPT_SLOT(HD) + 2 * PROMPT_ROWS + in * HD + d; });
+    } else of_row(1);
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    *(uint2*)out_at(a, t, (g * a.G + h) * HD + d) = make_uint2(half_pair(O[0] * inv, O[1] * inv), half_pair(O[2] * inv, O[3] * inv));
+  }
+}
+
+// The kernel's arguments (its first and only ones), loaded anew: each part of the kernel has its own copy, or the compiler would load them once at the
+// start, and keep what is more than the scalar registers hold in vector registers, to be brought back at every tile.
+__device__ __forceinline__ SharedArgs fresh_args() {
+  typedef const __attribute__((address_space(4))) SharedArgs* args_t;
+  u64 p = (u64)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const SharedArgs*)(args_t)p;
+}
+// A call with groups: some workgroups have the groups' shared keys, bound by products, others at the same time the tiles of few rows, bound by bytes,
+// and then the prompts.
+template <int HD, int BITS, int CT>
+__device__ __forceinline__ void shared_attention(const SharedArgs& args, PagedShared<HD, CT, SharedArgs>& sh, u32 wg, u32 nwg) {
+  constexpr u32 NT = 64 * PAGED_WAVES;
+  SharedWork work = shared_work<HD>(args, sh.p, wg, nwg);
+  if (wg < work.flat_wgs) {
+    const SharedArgs a = fresh_args();
+    const u32 units = (u32)__builtin_amdgcn_readfirstlane(sh.p.flat[a.n_groups]), from = min(wg * work.quota, units);
+    paged_prompt<HD, BITS, true>(a, sh.p, wg, work.flat_wgs, false, FlatRun{from, min(from + work.quota, units)});
+    return;
+  }
+  wg -= work.flat_wgs; nwg -= work.flat_wgs;
+  if (work.few) {
+    const SharedArgs a = fresh_args();
+    SharedView v[PAGED_MAX_SEQS / NT];
+#pragma unroll
+    for (u32 j = 0; j < PAGED_MAX_SEQS / NT; ++j) if (threadIdx.x + j * NT < n_views(a)) v[j] = sh.p.view[threadIdx.x + j * NT];
+    __syncthreads();
+#pragma unroll
+    for (u32 j = 0; j < PAGED_MAX_SEQS / NT; ++j) {
+      const u32 s = threadIdx.x + j * NT;
+      if (s >= n_views(a)) continue;
+      const bool group = s >= a.n_seqs;
+      sh.s.pos0[s] = v[j].pos0;
+      sh.s.n[s] = short_unit_count(a, v[j], group) ? (unsigned char)v[j].n : (unsigned char)0;
+      sh.s.link[s] = group || v[j].first ? (uint16_t)v[j].row : (uint16_t)NO_GROUP;
+    }
+    __syncthreads();
+    paged_short<HD, BITS, CT, SHORT_AHEAD(HD, BITS, CT), PAGED_WAVES>(a, sh.s, wg, nwg);
+  }
+  if (!work.prompts) return;
+  const SharedArgs a = fresh_args();
+  if (work.few) {
+    __syncthreads();
+    views_and_sums(a, sh.p);
+  }
+  paged_prompt<HD, BITS>(a, sh.p, wg, nwg, true);
+}
