@@ -60,7 +60,7 @@ class PagedAttentionArgs(C.Structure):
 
 
 class SharedAttentionArgs(C.Structure):
-    _fields_ = [("attention", PagedAttentionArgs), ("n_groups", C.c_uint32), ("group_starts", C.c_void_p), ("shared_lens", C.c_void_p)]
+    _fields_ = [("attention", PagedAttentionArgs), ("n_groups", C.c_uint32), ("share_all", C.c_uint32), ("group_starts", C.c_void_p), ("shared_lens", C.c_void_p)]
 
 
 class TokenLogprobsArgs(C.Structure):
@@ -70,7 +70,7 @@ class TokenLogprobsArgs(C.Structure):
 
 # the same five as `struct` packs them (fields in order, native alignment)
 _CACHE, _QK_NORM_ROPE, _PAGED_ATTENTION = struct.Struct("@P4I"), struct.Struct("@P4I4I3P3Q6PQ2f"), struct.Struct("@P4I7If2P2Q4PQ")
-_GROUPS = struct.Struct("@I2P")                        # of _SHARED_ATTENTION, behind _PAGED_ATTENTION
+_GROUPS = struct.Struct("@2I2P")                       # of _SHARED_ATTENTION, behind _PAGED_ATTENTION
 _TOKEN_LOGPROBS = struct.Struct("@5IPQ8PQ")
 
 
@@ -331,14 +331,15 @@ def shared_attention_workspace_bytes(n_q_heads, cache, n_seqs, n_groups, n_token
     return n.value
 
 
-def shared_attention(q, cache, block_tables, seq_lens, cu_seqlens, group_starts, shared_lens, out, workspace, max_q=1, window=0, sinks=0, scale=1.0, stream=None):
+def shared_attention(q, cache, block_tables, seq_lens, cu_seqlens, group_starts, shared_lens, out, workspace, max_q=1, window=0, sinks=0, scale=1.0, share_all=False,
+                     stream=None):
     """blink_shared_attention: paged_attention of a batch whose sequences group_starts[i] .. group_starts[i + 1] have the blocks of their first shared_lens[i]
     tokens in common; int32 group_starts [groups + 1], shared_lens [groups]; workspace: a contiguous tensor of
-    shared_attention_workspace_bytes(...) bytes. stream: as for qk_norm_rope."""
+    shared_attention_workspace_bytes(...) bytes. share_all: also groups that gain nothing by it. stream: as for qk_norm_rope."""
     lib, dev = _lib or load_library(), cache.device
     n = shared_lens.shape[0]
     a = _attention_args(q, cache, block_tables, seq_lens, cu_seqlens, out, workspace, max_q, window, sinks, scale) + _GROUPS.pack(
-        n, _dense("group_starts", group_starts, _INT, (n + 1,), dev), _dense("shared_lens", shared_lens, _INT, (n,), dev))
+        n, 1 if share_all else 0, _dense("group_starts", group_starts, _INT, (n + 1,), dev), _dense("shared_lens", shared_lens, _INT, (n,), dev))
     rc = lib.blink_shared_attention(dev, a, _stream(stream, q, dev))
     if rc:
         _check(lib, rc)

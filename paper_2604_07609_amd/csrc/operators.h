@@ -380,6 +380,7 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   if (s->n_groups == 0) return blink_paged_attention(device, a, stream);
   const u32 hd = a->cache.head_dim, nkv = a->cache.n_kv_heads;
   if (((u64)a->n_seqs + s->n_groups) * a->max_blocks * nkv >= (1ull << 31)) return fail(BLINK_ERR_TOO_LARGE, "2^31 blocks of keys or more in one call");
+  if (s->share_all > 1) return fail(BLINK_ERR_INVAL, "share_all must be 0 or 1");
   if (!s->group_starts || !s->shared_lens || (u64)s->group_starts % 4 || (u64)s->shared_lens % 4) return fail(BLINK_ERR_INVAL, "group_starts or shared_lens is null or not aligned");
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
@@ -394,7 +395,12 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   p.prompt_part = p.own_part + plan.prompt_bytes / 4;
   p.rows = p.prompt_part + plan.flat_bytes / 4;
   p.tokens = (JoinToken*)(p.rows + plan.row_bytes / 4);
-  p.n_groups = s->n_groups; p.starts = s->group_starts; p.shared = s->shared_lens;
+  // (times on one compute unit, by which workgroups are dealt out. A unit, half a step of 256 rows: 1.03 us with heads of 128, 1.2 over 4 bits, half of that with
+  // heads of 64; a tile of few rows 0.28 us, 0.16 over 4 bits; an item's start and end 5 to 6 us)
+  p.lead = hd == 128 ? 5 : 9;
+  p.light = a->cache.bits == 16 ? 1 : 2;
+  p.few_cost = (a->cache.bits == 16 ? 0.26f : 0.13f) * (plan.ct == 1 ? 1.f : 1.5f);
+  p.n_groups = s->n_groups; p.share_all = s->share_all; p.starts = s->group_starts; p.shared = s->shared_lens;
   const hipStream_t st = (hipStream_t)stream;
   HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_shared<64, 16>(p, plan.ct, n_cu, st) : launch_shared<64, 4>(p, plan.ct, n_cu, st))
                   : (a->cache.bits == 16 ? launch_shared<128, 16>(p, plan.ct, n_cu, st) : launch_shared<128, 4>(p, plan.ct, n_cu, st)));

@@ -43,10 +43,13 @@ struct PagedArgs {
 // A call in which sequences of a group have their first blocks in common: those keys are seen once for the group, by the rows of all of its
 // sequences at a time (shared_views). So a call has a view for each sequence and, behind those, one for each group.
 struct SharedArgs : PagedArgs {
-  u32 n_groups;
+  u32 n_groups, share_all;        // share_all: groups that gain nothing by it too
   const i32 *starts, *shared;     // first sequence of every group (n_groups + 1), tokens that its sequences share
   float* rows;                    // results to be joined: [of the group, of the sequence][token][q head] of ROW_RESULT(hd) floats
   float* own_part;                // parts of prompt items (prompt_part: of the groups' items)
+  u32 light;                      // units of a step of an item of 128 rows or less (of others: 2)
+  u32 lead;                       // time of an item of the groups' shared keys beside its steps, in units (FlatShape)
+  float few_cost;                 // time of a tile of few rows on one compute unit, in units
   struct JoinToken* tokens;       // what is to be joined of every token, and behind them the units of a workgroup's run (FlatRun)
 };
 #define ROW_RESULT(HD) ((HD) + 4u)                   // maximum, sum, two unused, output
@@ -314,12 +317,11 @@ struct CacheTile<HD, 4> {
 
 #define PAGED_WAVES 8              // waves of a workgroup of the prompt part
 #define PAGED_MAX_SEQS 1024u       // sequences (and groups) whose views a workgroup keeps in LDS
+#define PROMPT_CT 2u
+#define PROMPT_ROWS (128u * PROMPT_CT)
 #define SHARED_ROWS 256u           // sequences with so many rows fill a prompt item by themselves
-// Times on one compute unit, in those of a unit of the groups' shared keys (half a step of 256 rows, 1 us with heads of 128), by which workgroups are
-// dealt out: a tile of few rows; what a pair of a sequence and a kv head takes beside its tiles, in tiles; an item of many rows beside its steps
-#define FEW_COST .25f
-#define FEW_PAIR 2u
-#define FLAT_LEAD 5u
+#define SHARED_GAIN 2.f            // units that a group must save
+#define FEW_PAIR 2u                // what a pair of a sequence and a kv head takes beside its tiles, in tiles
 struct NoLinks {};
 struct ViewLinks { uint16_t link[PAGED_MAX_SEQS]; };      // of a sequence: its group, or NO_GROUP; of a group: the sequence whose table it takes
 #define NO_GROUP 0xFFFFu
@@ -546,17 +548,34 @@ __device__ __forceinline__ void give_strange(const CacheTile<HD, BITS>& t, float
   }
 }
 
+// The groups with more rows than the few-row part takes: their rows in items of FLAT_ROWS (whole queries), each with all shared keys. All steps of
+// all (group, kv head, item) are one line of units, one a step (over 4 bits two, whatever the rows) or, for items of more than 128 rows, two, and `lead` ahead of an
+// item's, and every workgroup has an equal run of it. An item inside a run is done there; one that several runs share leaves a result in each.
+__device__ __forceinline__ u32 flat_rows(const PagedArgs& a) { return PROMPT_ROWS / a.G * a.G; }
+struct FlatShape {
+  u32 items, steps, lead, last;                      // items of a kv head; weight of the last one's steps (the others': 2)
+  __device__ __forceinline__ u32 units(u32 item) const { return steps * (item + 1 < items ? 2 : last) + lead; }
+  __device__ __forceinline__ u32 all() const { return (items - 1) * (2 * steps + lead) + last * steps + lead; }
+};
+__device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, u32 rows, u32 keys) {
+  const u32 per = flat_rows(a), items = (rows + per - 1) / per;
+  return {items, keys / 64, a.lead, rows - (items - 1) * per > 128 ? 2u : a.light};
+}
+__device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, const SharedView& v) { return flat_shape(a, v.n * a.G, (u32)v.pos0 + 1); }
+__device__ __forceinline__ u32 flat_units(const SharedArgs& a, const SharedView& v) {      // of a group
+  return v.n * a.G <= a.short_rows ? 0u : flat_shape(a, v).all() * a.nkv;
+}
 // The views of a call with groups, by a workgroup of NT threads, in LDS: those of the sequences, then those of the groups. A sequence goes by its group where it gains by that and may: it has fewer rows than a prompt item,
-// all its queries stand behind the shared keys and see every one of them, and it is not the only one. The shared keys are cut to a multiple of 64, what a step of
-// the prompt part takes. room: 4 n_groups + 1 words of LDS.
+// all its queries stand behind the shared keys and see every one of them, and all of these together take less time with the shared keys apart. The shared keys are cut to a multiple of 64, what a step of
+// the prompt part takes. room: 5 n_groups + 1 words of LDS.
 template <u32 NT>
 __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, SharedView* view) {
-  u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const to = from + a.n_groups;
+  u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const to = from + a.n_groups, *const members = to + a.n_groups;
   for (u32 g = threadIdx.x; g <= a.n_groups; g += NT) {
     starts[g] = (u32)max(0, min(a.starts[g], (i32)a.n_seqs));
     if (g == a.n_groups) break;
     keys[g] = (u32)max(0, min(a.shared[g], (i32)(a.max_blocks * 16))) / 64 * 64;
-    from[g] = ~0u; to[g] = 0;
+    from[g] = ~0u; to[g] = 0; members[g] = 0;
   }
   SeqView v[(PAGED_MAX_SEQS + NT - 1) / NT];         // (asked for before the barrier)
 #pragma unroll
@@ -575,24 +594,27 @@ __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, Sha
     if (s >= starts[g + 1] || !keys[g] || !v[j].n || v[j].n * a.G >= SHARED_ROWS || v[j].pos0 < (i32)keys[g] || (a.window && p1 >= (i32)a.window)) continue;
     atomicMin(from + g, s);
     atomicMax(to + g, s);
+    atomicAdd(members + g, 1u);
+    view[s] = SharedView{v[j].t0, v[j].n, 0, 0, 0};
     group[j] = g;
+  }
+  __syncthreads();
+  for (u32 g = threadIdx.x; g < a.n_groups; g += NT) {
+    SharedView x = {0, 0, -1, 0, 0};
+    if (from[g] < to[g]) {
+      const u32 t0 = view[from[g]].t0, end = view[to[g]].t0 + view[to[g]].n, n = end > t0 ? end - t0 : 0u, tiles = keys[g] / 16;
+      const float together = n * a.G <= a.short_rows ? a.few_cost * (float)(tiles + FEW_PAIR) : (float)flat_shape(a, n * a.G, keys[g]).all();
+      if (a.share_all || (float)members[g] * (float)tiles * a.few_cost > together + SHARED_GAIN) x = {t0, n, (i32)keys[g] - 1, 0, from[g]};
+    }
+    view[a.n_seqs + g] = x;
   }
   __syncthreads();
 #pragma unroll
   for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j) {
     const u32 s = threadIdx.x + j * NT, g = group[j];
     if (s >= a.n_seqs) continue;
-    const bool in = g != NO_GROUP && from[g] < to[g];
+    const bool in = g != NO_GROUP && view[a.n_seqs + g].n != 0;
     view[s] = SharedView{v[j].t0, v[j].n, v[j].pos0, in ? keys[g] : 0u, g};
-  }
-  __syncthreads();
-  for (u32 g = threadIdx.x; g < a.n_groups; g += NT) {
-    SharedView x = {0, 0, -1, 0, 0};
-    if (from[g] < to[g]) {
-      const u32 t0 = view[from[g]].t0, end = view[to[g]].t0 + view[to[g]].n;
-      x = {t0, end > t0 ? end - t0 : 0u, (i32)keys[g] - 1, 0, from[g]};
-    }
-    view[a.n_seqs + g] = x;
   }
   __syncthreads();
 }
@@ -642,6 +664,9 @@ template <int HD, int BITS, int CT, int NT, int NW, typename A>
 __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, is_shared<A>>& sh, u32 wg, u32 nwg) {
   typedef ShortShared<HD, CT, NW, is_shared<A>> Shared;
   constexpr bool SHARED = is_shared<A>;
+  // Units ahead of a pair's that are no tiles, but what the pair takes besides: where most pairs are of a tile or two, and some long, runs of as many tiles
+  // were up to twice as long as others (40 groups of up to four sequences with 9 tokens of their own: 58 us the longest, 34 half of them)
+  constexpr u32 GAP = SHARED ? FEW_PAIR : 0u;
   typedef CacheTile<HD, BITS> Tile;
   const u32 lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lg = lane >> 4, lc = lane & 15;
   auto scalar = [](u32 x) { return (u32)__builtin_amdgcn_readfirstlane(x); };
@@ -654,7 +679,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
   auto count_tiles = [&](u32 s) {
     if constexpr (SHARED) {
       const i32 p0 = sh.pos0[s], n = (i32)sh.n[s];
-      return n ? max(1u, seen_tiles<16>(a, p0, last_pos(s, p0, n), first_key(s)).n) : 0u;
+      return n ? max(1u, seen_tiles<16>(a, p0, last_pos(s, p0, n), first_key(s)).n) + GAP : 0u;
     } else {
       const SeqView v = seq_view(a, s);
       const u32 n = short_unit_count(a, v);
@@ -680,7 +705,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
     for (u32 of = nwg;; of = nwg - pairs) {
       choose(units, of);
       if (!whole) break;
-      const u32 x = wave_sums((n + cap - 1) / cap * a.nkv), wgs = (u32)__builtin_amdgcn_readlane((i32)x, 63);
+      const u32 x = wave_sums((SHARED && n ? n - GAP + cap - 1 : n + cap - 1) / cap * a.nkv), wgs = (u32)__builtin_amdgcn_readlane((i32)x, 63);
       if (wgs <= nwg) { sum = x; U = wgs; break; }
     }
     if (lane < n_views(a)) sh.pre[lane + 1] = sum;
@@ -714,7 +739,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
     p.n = scalar(sh.n[s]); p.pos0 = (i32)scalar((u32)sh.pos0[s]);
     const Seen e = seen_tiles<16>(a, p.pos0, last_of(p), SHARED ? scalar(first_key(s)) : 0u);
     p.zb = scalar(e.zb); p.wlo = scalar(e.wlo); p.nv = scalar(max(1u, e.n));
-    p.first = whole ? 0u : scalar(sh.pre[s]) + g * p.nv;
+    p.first = whole ? 0u : scalar(sh.pre[s]) + g * (p.nv + GAP) + GAP;
     p.row = a.table_row ? scalar(a.table_row[of]) : of;
     return p;
   };
@@ -723,7 +748,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
     return pair_of(s, in / (scalar(sh.pre[s + 1] - sh.pre[s]) / a.nkv));
   };
   auto pair_after = [&](const Pair& p) {             // (there is one)
-    if (p.g + 1 < a.nkv) { Pair q = p; ++q.g; q.first += q.nv; return q; }
+    if (p.g + 1 < a.nkv) { Pair q = p; ++q.g; q.first += q.nv + GAP; return q; }
     u32 s = p.s + 1;
     while (scalar(sh.pre[s + 1]) == scalar(sh.pre[s])) ++s;
     return pair_of(s, 0);
@@ -811,11 +836,12 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
     for (int c = 0; c < CT; ++c) vis[c] = in_cache ? sees(a, qpos[c], (i32)(key + lg * 4)) : 0u;
   };
   clear();
-  if (u0 < u1) {
-    if (u0 != wg0 && !whole) cur = pair_at(u0);
+  if (SHARED && !whole && u0 < u1 && u0 != wg0) cur = pair_at(u0);
+  if (u0 < u1 && (!SHARED || cur.first < u1)) {
+    if (!SHARED && u0 != wg0 && !whole) cur = pair_at(u0);
     // the tile to ask for next: its unit, pair and block id (asked for a tile ahead)
     Pair ap = cur;
-    u32 au = u0, ak = key_of(ap, au), aid = block_of(ap, ak);
+    u32 au = SHARED ? max(u0, cur.first) : u0, ak = key_of(ap, au), aid = block_of(ap, ak);
     Tile tile[NT];
     u32 k0[NT];
     bool in_cache[NT], strange = false;
@@ -825,7 +851,10 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
       in_cache[j] = aid < a.n_blocks;
       tile[j].load(a, at, min(aid, a.n_blocks - 1), ap.g);
       if (++au < u1) {
-        if (au == ap.first + ap.nv) ap = pair_after(ap);
+        if (au == ap.first + ap.nv) {
+          ap = pair_after(ap);
+          if constexpr (SHARED) { au = ap.first; if (au >= u1) return; }
+        }
         ak = key_of(ap, au);
         aid = block_of(ap, ak);
       }
@@ -833,7 +862,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
     load_q(cur);
 #pragma unroll
     for (int j = 0; j < NT; ++j) ask(j);
-    u32 u = u0;
+    u32 u = SHARED ? max(u0, cur.first) : u0;
     auto step = [&](int j) {                         // the tile of slot j; whether its pair, or the run, ends with it
       if (cur.pos0 + (i32)cur.n > 0) {
         const bool edge = edge_of(cur, k0[j], in_cache[j]);
@@ -875,7 +904,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
         strange = false;
         if (u < u1) {                                // (the tiles on their way are asked for again: none of them stays in registers over this)
           ap = u == cur.first + cur.nv ? pair_after(cur) : cur;
-          au = u;
+          au = SHARED ? max(u, ap.first) : u;
           ak = key_of(ap, au);
           aid = block_of(ap, ak);
 #pragma unroll
@@ -887,14 +916,19 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
       if (done && cur.first >= u0) finish(cur);                             // the pair is this wave's alone
       else if (cur.first < u0) leave_in_lds<HD, BITS, CT, NW>(sh, w, acc);      // its beginning is another wave's
       if (u == u1) break;                                                   // (a pair that begins here and goes on: in acc)
-      cur = pair_after(cur);
+      if constexpr (SHARED) {
+        const Pair next = pair_after(cur);
+        if (next.first >= u1) break;
+        cur = next;
+        u = cur.first;
+      } else cur = pair_after(cur);
       load_q(cur);
       clear();
       wait_loads();      // (the compiler does not know any more which slot's loads are the oldest: it would wait for all of them at every turn)
     }
   }
   // The rest is a workgroup's end, once per launch.
-  const bool goes_on = u0 < u1 && cur.first >= u0 && u1 < cur.first + cur.nv;
+  const bool goes_on = u0 < u1 && cur.first >= u0 && u1 < cur.first + cur.nv && (!SHARED || cur.first < u1);
   if (goes_on && (whole || cur.first + cur.nv > wg1)) leave_in_lds<HD, BITS, CT, NW>(sh, NW, acc);
   __syncthreads();
   // pairs that other workgroups share, all waves at each: the one that the run begins inside of (0), the one that begins in it (1)
@@ -946,6 +980,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
     const Pair p = pair_at(whole ? wg : which ? wg1 - 1 : wg0);
     const u32 end = p.first + p.nv, f = first_wg(p), np = n_wgs(p);
     if (which ? p.first < wg0 || end <= (whole ? quantum : wg1) : p.first >= wg0) continue;      // (a pair in one run: its wave has finished it)
+    if (SHARED && !whole && which && p.first >= wg1) continue;           // (it begins behind the run)
     const u32 x0 = which ? (p.first - wg0) / quantum : 0u, x1 = (min(end, wg1) - wg0 + quantum - 1) / quantum;
     all.sum(x0, x1, p.n * a.G, [&](u32 x) { return LdsResult<Shared>{sh, which && x == x0 ? (u32)NW : x}; });
     if (np == 1) { finish_all(p); continue; }
@@ -1008,9 +1043,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
 // Bound by the instructions of the softmax (32 exponentials and 87 others a lane and step) and the products in turn: 2048 queries at
 // 16384 keys in 4 bits (32 q, 8 kv heads of 128) 547 us, 0.94 PFLOP/s, where the library's largest products reach 1.08; two prompts of 4000
 // behind a window of 1024 168 us, 0.70 PFLOP/s: an item is 17 steps, and its start (queries, ids, the first tiles) and end another 3.
-#define PROMPT_CT 2u
 #define PROMPT_PIPE 3             // groups of operands on their way from LDS and in use
-#define PROMPT_ROWS (128u * PROMPT_CT)
 #define PROMPT_RING (128u * 1024u)
 #define PROMPT_SLOT(HD) (PROMPT_ROWS * ((HD) + 2u))      // floats of a part's result: maximum and sum of every row, then its output
 template <typename View>
@@ -1087,23 +1120,6 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 template <int N> __device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
-// The groups with more rows than the few-row part takes: their rows in items of FLAT_ROWS (whole queries), each with all shared keys. All steps of
-// all (group, kv head, item) are one line of units, one or (items of more than 128 rows, which take about twice as long) two a step and FLAT_LEAD ahead of an
-// item's, and every workgroup has an equal run of it. An item inside a run is done there; one that several runs share leaves a result in each.
-__device__ __forceinline__ u32 flat_rows(const PagedArgs& a) { return PROMPT_ROWS / a.G * a.G; }
-struct FlatShape {
-  u32 row_items, steps, weight;
-  __device__ __forceinline__ u32 units() const { return steps * weight + FLAT_LEAD; }      // of an item
-};
-__device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, const SharedView& v) {
-  const u32 rows = v.n * a.G, per = flat_rows(a);
-  return {(rows + per - 1) / per, (u32)(v.pos0 + 1) / 64, min(rows, per) > 128 ? 2u : 1u};
-}
-__device__ __forceinline__ u32 flat_units(const SharedArgs& a, const SharedView& v) {      // of a group
-  if (v.n * a.G <= a.short_rows) return 0;
-  const FlatShape f = flat_shape(a, v);
-  return f.row_items * f.units() * a.nkv;
-}
 struct FlatRun { u32 from, end; };
 struct FlatPiece { u32 s_lo, s_hi, next; bool whole, begins, any; };       // any: has steps (or a half of one)
 template <typename Room>
@@ -1112,12 +1128,13 @@ __device__ __forceinline__ PromptItem flat_piece(const SharedArgs& a, const Room
   const u32 g = last_at_most(sh.flat, a.n_groups, u);
   const SharedView v = sh.view[a.n_seqs + g];
   const FlatShape f = flat_shape(a, v);
-  const u32 per = f.units(), x = u - sh.flat[g], item = x / per, off = x - item * per, to = min(per, off + end - u);
-  auto step = [&](u32 at) { return at > FLAT_LEAD ? (at - FLAT_LEAD + f.weight - 1) / f.weight : 0u; };
-  p = {step(off), step(to), u + to - off, off <= FLAT_LEAD && to == per, off <= FLAT_LEAD, to > FLAT_LEAD};
+  const u32 all = f.all(), x = u - sh.flat[g], head = x / all, full = 2 * f.steps + f.lead, item = min((x - head * all) / full, f.items - 1);
+  const u32 per = f.units(item), off = x - head * all - item * full, to = min(per, off + end - u), weight = item + 1 < f.items ? 2u : f.last;
+  auto step = [&](u32 at) { return at > f.lead ? (at - f.lead + weight - 1) / weight : 0u; };
+  p = {step(off), step(to), u + to - off, off <= f.lead && to == per, off <= f.lead, to > f.lead};
   it.s = a.n_seqs + g;
-  it.g = item / f.row_items;
-  it.r0 = (item - it.g * f.row_items) * flat_rows(a);
+  it.g = head;
+  it.r0 = item * flat_rows(a);
   it.rows = min(flat_rows(a), v.n * a.G - it.r0);
   it.t0 = v.t0; it.p0 = it.p1 = v.pos0; it.lo = 0; it.row = v.row;
   return it;

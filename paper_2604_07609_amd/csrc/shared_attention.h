@@ -36,7 +36,7 @@ __device__ __forceinline__ void views_and_sums(const SharedArgs& a, SharedRoom& 
       if (group) v[1] = flat_units(a, x); else v[0] = prompt_items(a, x);
       const u32 tiles = short_unit_count(a, x, group);
       v[2] = (tiles ? tiles + FEW_PAIR : 0u) * a.nkv;
-      if (v[0]) v[3] = v[0] * (2 * seen_tiles<64>(a, x.pos0, x.pos0 + (i32)x.n - 1, x.first).n + FLAT_LEAD) * a.nkv;
+      if (v[0]) v[3] = v[0] * (2 * seen_tiles<64>(a, x.pos0, x.pos0 + (i32)x.n - 1, x.first).n + a.lead) * a.nkv;
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = wave_sums_dpp(v[k]);
@@ -67,7 +67,7 @@ __device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, SharedRoo
   const u32 units = (u32)__builtin_amdgcn_readfirstlane(sh.flat[a.n_groups]);
   const u32 tiles = (u32)__builtin_amdgcn_readfirstlane(sh.sum[0]), prompts = (u32)__builtin_amdgcn_readfirstlane(sh.sum[1]);
   r.few = tiles != 0; r.prompts = prompts != 0;
-  const float flat = (float)units, rest = FEW_COST * (float)tiles + (float)prompts;
+  const float flat = (float)units, rest = a.few_cost * (float)tiles + (float)prompts;
   r.flat_wgs = !units ? 0u : rest == 0.f ? nwg : min(nwg - 1, max(1u, (u32)((float)nwg * flat / (flat + rest) + 0.5f)));
   r.quota = r.flat_wgs ? (units + r.flat_wgs - 1) / r.flat_wgs : 1u;
   if (wg == 0 && threadIdx.x == 0) *(u32*)(a.tokens + a.n_tokens) = r.quota;
@@ -87,8 +87,8 @@ __device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, SharedRoo
         const u32 r = (t - x.t0) * a.G;
         if (t - x.t0 < x.n && flat_units(a, x)) {    // (cu_seqlens that decrease may put a token outside its group)
           const FlatShape f = flat_shape(a, x);
-          const u32 item = r / flat_rows(a), per = f.units();
-          j.units[0] = sh.flat[v.row] + item * per + FLAT_LEAD; j.units[1] = f.row_items * per; j.units[2] = per - FLAT_LEAD;
+          const u32 item = r / flat_rows(a);
+          j.units[0] = sh.flat[v.row] + item * (2 * f.steps + f.lead) + f.lead; j.units[1] = f.all(); j.units[2] = f.units(item) - f.lead;
           j.row = r - item * flat_rows(a);
         } else j.units[2] = 1;                       // (by one workgroup, into rows)
       }

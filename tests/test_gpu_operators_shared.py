@@ -47,14 +47,14 @@ def make_groups(groups, nq, nkv, hd, bits, seed=0, before=(), after=(), extra_ro
     return (cache, c, tables, lens, cu, q), np.int32(starts), np.int32(shared), max(runs)
 
 
-def run_shared(b, starts, shared, max_q, window=0, sinks=0, scale=1.0, workspace=None, fill=9.0):
+def run_shared(b, starts, shared, max_q, window=0, sinks=0, scale=1.0, workspace=None, fill=9.0, share_all=True):
     cache, _, tables, lens, cu, q = b
     if workspace is None:
         n = B.shared_attention_workspace_bytes(q.shape[1], cache, len(lens), len(shared), q.shape[0], max_q)
         workspace = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
         workspace[:8192] = 0
     out = torch.full(q.shape, fill, dtype=torch.float16, device="cuda")
-    B.shared_attention(dev(q), cache, dev(tables), dev(lens), dev(cu), dev(starts), dev(shared), out, workspace, max_q=max_q, window=window, sinks=sinks, scale=scale)
+    B.shared_attention(dev(q), cache, dev(tables), dev(lens), dev(cu), dev(starts), dev(shared), out, workspace, max_q=max_q, window=window, sinks=sinks, scale=scale, share_all=share_all)
     assert not workspace[:8192].any()
     return out.double().cpu().numpy()
 
@@ -64,7 +64,7 @@ def check(groups, nq, nkv, hd, bits, window=0, sinks=0, scale=1.0, **k):
     got = run_shared(b, starts, shared, max_q, window, sinks, scale)
     check_attention(got, *b, window=window, sinks=sinks, scale=scale)
     assert np.array_equal(got, run_shared(b, starts, shared, max_q, window, sinks, scale))
-    return got
+    check_attention(run_shared(b, starts, shared, max_q, window, sinks, scale, share_all=False), *b, window=window, sinks=sinks, scale=scale)
 
 
 HEADS = [(64, 6, 2), (128, 4, 1), (64, 3, 3), (128, 16, 2)]
@@ -251,7 +251,7 @@ def test_in_a_graph_whose_groups_change_and_a_workspace_in_turn_with_other_calls
     work = torch.zeros(n, dtype=torch.uint8, device="cuda")
     args = [dev(x) for x in (q, tables, lens, cu, starts, shared)]
     out = torch.zeros(q.shape, dtype=torch.float16, device="cuda")
-    call = lambda: B.shared_attention(args[0], cache, *args[1:], out, work)      # noqa: E731
+    call = lambda: B.shared_attention(args[0], cache, *args[1:], out, work, share_all=bits == 4)      # noqa: E731
     call()
     torch.cuda.synchronize()
     g = torch.cuda.CUDAGraph()
