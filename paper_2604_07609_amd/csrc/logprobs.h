@@ -57,6 +57,10 @@ __device__ __forceinline__ u32 lp_high(float x) {
   return b ^ ((i32)b < 0 ? 0xFFFFFFFFu : 0x80000000u);
 }
 __device__ __forceinline__ u64 lp_key(float x, u32 id) { return (u64)lp_high(x) << 32 | (0xFFFFFFFFu - id); }
+__device__ __forceinline__ float lp_next_lower(float x) {      // (of a number, or +inf)
+  const u32 b = __float_as_uint(x);
+  return __uint_as_float(x > 0.f ? b - 1 : x < 0.f ? b + 1 : 0x80000001u);
+}
 __device__ __forceinline__ u32 lp_id(u64 key) { return 0xFFFFFFFFu - (u32)key; }
 __device__ __forceinline__ float lp_value(u32 high) { return __uint_as_float(high ^ ((i32)high < 0 ? 0x80000000u : 0xFFFFFFFFu)); }
 __device__ __forceinline__ u32 lp_below(u64 mask) { return __builtin_amdgcn_mbcnt_hi((u32)(mask >> 32), __builtin_amdgcn_mbcnt_lo((u32)mask, 0)); }     // bits of lower lanes
@@ -211,6 +215,8 @@ __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShar
     const i32 t = a.tokens[(u64)row * a.given + lane];
     if (t >= 0 && (u32)t < a.V) { token = t; given = lp_ordered((float)first[t]); }
   }
+  const u32 token0 = (u32)__builtin_amdgcn_readfirstlane(token);
+  const float given0 = __uint_as_float((u32)__builtin_amdgcn_readfirstlane((i32)__float_as_uint(given)));
   LpSums sum = {-INFINITY, 0.f, 0.f};                // (m: the wave's, sums: the lane's)
   u64* const cand = sh.cand + (TOP ? w * LP_CAP : 0);
   u32 n = 0;                                         // keys in cand
@@ -258,25 +264,31 @@ __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShar
     }
     sum.s += (s[0] + s[1]) + (s[2] + s[3]);
     sum.t += (t[0] + t[1]) + (t[2] + t[3]);
-    if (a.ranks) {
+    // Logits of the tile before the token tk, whose logit is y, by `count`: where the token is not in the tile, those above y or, if the tile is ahead
+    // of the token, not below it: above the next lower number.
+    auto ranked = [&](u32 tk, float y, auto count) {
+      if (!whole || y == -INFINITY || (tk + shift >= at && tk + shift < at + LP_TILE)) {
+        count([&](u32 j) { const float o = lp_ordered(x[j]); return valid(j) && (o > y || (o == y && id(j) < tk)); });
+      } else {
+        const float bound = tk + shift < at ? y : lp_next_lower(y);
+        if (__ballot(most > bound)) count([&](u32 j) { return x[j] > bound; });
+      }
+    };
+    if (a.ranks && a.given == 1) {
+      ranked(token0, given0, [&](auto is) {          // (a lane's own: added up at the end)
+#pragma unroll
+        for (u32 j = 0; j < LP_VALS; ++j) before += is(j) ? 1u : 0u;
+      });
+    } else if (a.ranks) {
 #pragma unroll 1
       for (u32 g = 0; g < a.given; ++g) {
         const u32 tk = (u32)__builtin_amdgcn_readlane(token, (int)g);
         const float y = __uint_as_float((u32)__builtin_amdgcn_readlane((i32)__float_as_uint(given), (int)g));
-        u32 mine = 0;
-        if (!whole || y == -INFINITY || (tk + shift >= at && tk + shift < at + LP_TILE)) {
+        u32 more = 0;
+        ranked(tk, y, [&](auto is) {
 #pragma unroll
-          for (u32 j = 0; j < LP_VALS; ++j) { const float o = lp_ordered(x[j]); mine += valid(j) && (o > y || (o == y && id(j) < tk)) ? 1u : 0u; }
-        } else if (tk + shift < at) {
-#pragma unroll
-          for (u32 j = 0; j < LP_VALS; ++j) mine += x[j] > y ? 1u : 0u;
-        } else {
-#pragma unroll
-          for (u32 j = 0; j < LP_VALS; ++j) mine += x[j] >= y ? 1u : 0u;
-        }
-        u32 more = 0;                                // of the wave: at most 16 each, bit by bit
-#pragma unroll
-        for (u32 b = 0; b < 5; ++b) more += (u32)__popcll(__ballot(mine >> b & 1u)) << b;
+          for (u32 j = 0; j < LP_VALS; ++j) more += (u32)__popcll(__ballot(is(j)));
+        });
         before += lane == g ? more : 0u;
       }
     }
@@ -290,12 +302,16 @@ __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShar
       if (tile == tile0) {
 #pragma unroll
         for (u32 j = 0; j < LP_VALS; ++j) append(j, valid(j) && lp_ordered(x[j]) >= over);
-      } else {
+      } else if (__ballot(most > over)) {
 #pragma unroll
         for (u32 j = 0; j < LP_VALS; ++j) append(j, x[j] > over);
       }
       if (n > LP_FEW) over = lp_value(lp_thin(cand, n, a.k));
     }
+  }
+  if (a.given == 1) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) before += (u32)__shfl_xor((int)before, o);
   }
   // the workgroup's: sums of its waves, keys ranked
   sum.s = lp_wave_sum(sum.s); sum.t = lp_wave_sum(sum.t);
