@@ -17,7 +17,8 @@
 #define LP_WAVES (BLK_THREADS / 64u)
 #define LP_MOST 64u                // given tokens (a lane each), most probable tokens
 #define LP_FEW 160u                // keys that a wave keeps from tile to tile at most
-#define LP_CAP (LP_FEW + LP_TILE + 4)      // (and zeros behind them)
+#define LP_CAP (LP_FEW + LP_TILE + 8)      // (and zeros behind them)
+#define LP_RANKED 96u              // keys of a workgroup that are ranked as they are
 #define LP_MAX_PARTS 32u           // workgroups of a row (LP_MAX_PARTS LP_MOST keys at most are joined)
 #define LP_PER_CU 4u               // workgroups that a call has for every compute unit, where its rows have the tiles
 #define LP_LOWEST -3.4028235e38f
@@ -197,6 +198,7 @@ struct LpTile {
 template <typename T, bool TOP>
 __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShared<TOP>& sh, u32 wg) {
   typedef LpTile<T> Tile;
+  constexpr u32 VEC = Tile::VEC;
   const u32 row = wg / a.parts, part = wg - row * a.parts, lane = threadIdx.x & 63, w = (u32)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // the row's elements are [shift, end) of what begins at the 16 bytes its first one lies in
   const T* const first = (const T*)a.x + (u64)row * a.stride;
@@ -264,21 +266,24 @@ __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShar
     }
     sum.s += (s[0] + s[1]) + (s[2] + s[3]);
     sum.t += (t[0] + t[1]) + (t[2] + t[3]);
-    // Logits of the tile before the token tk, whose logit is y, by `count`: where the token is not in the tile, those above y or, if the tile is ahead
-    // of the token, not below it: above the next lower number.
-    auto ranked = [&](u32 tk, float y, auto count) {
-      if (!whole || y == -INFINITY || (tk + shift >= at && tk + shift < at + LP_TILE)) {
-        count([&](u32 j) { const float o = lp_ordered(x[j]); return valid(j) && (o > y || (o == y && id(j) < tk)); });
-      } else {
-        const float bound = tk + shift < at ? y : lp_next_lower(y);
+    // Logits of the tile that come before the token tk, whose logit is y, by `count`: of those with a lower id the ones that are not below y, of the others those above it.
+    // (y = -inf: all with a lower id, whatever they are; added where the token is.) Elements outside the row, -inf, are never counted.
+    auto ranked = [&](u32 tk, float y, auto count, auto all) {
+      const float lower = y == -INFINITY ? INFINITY : lp_next_lower(y);
+      if (tk + shift < at || tk + shift >= at + LP_TILE) {
+        const float bound = tk + shift < at ? y : lower;
         if (__ballot(most > bound)) count([&](u32 j) { return x[j] > bound; });
+      } else {
+        const i32 mine = (i32)(tk + shift - at) - (i32)Tile::element(0);       // (element(j) is that of j = 0 and a constant more)
+        count([&](u32 j) { return x[j] > ((i32)(j / VEC * 64 * VEC + j % VEC) < mine ? lower : y); });
+        if (y == -INFINITY) all(tk);
       }
     };
     if (a.ranks && a.given == 1) {
       ranked(token0, given0, [&](auto is) {          // (a lane's own: added up at the end)
 #pragma unroll
         for (u32 j = 0; j < LP_VALS; ++j) before += is(j) ? 1u : 0u;
-      });
+      }, [&](u32 n) { before += lane == 0 ? n : 0u; });
     } else if (a.ranks) {
 #pragma unroll 1
       for (u32 g = 0; g < a.given; ++g) {
@@ -288,7 +293,7 @@ __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShar
         ranked(tk, y, [&](auto is) {
 #pragma unroll
           for (u32 j = 0; j < LP_VALS; ++j) more += (u32)__popcll(__ballot(is(j)));
-        });
+        }, [&](u32 n) { more += n; });
         before += lane == g ? more : 0u;
       }
     }
@@ -328,22 +333,28 @@ __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShar
   }
   // the first k of all waves' lists, in order, into top; 0 behind them
   auto first_k = [&]() {
-    u32 best = 0;
-#pragma unroll 1
-    for (u32 i = lane; i < n; i += 64) best = max(best, (u32)(cand[i] >> 32));
-    lp_kth(sh, best, a.k);
-    u32 m = 0;
-    const u32 kth = sh.kth;
-#pragma unroll 1
-    for (u32 i = lane; i - lane < n; i += 64) {
-      const u64 x = i < n ? cand[i] : 0, mask = __ballot(x && (u32)(x >> 32) >= kth);
-      if (x && (u32)(x >> 32) >= kth) cand[m + lp_below(mask)] = x;
-      m += (u32)__popcll(mask);
-    }
-    if (lane < 4) cand[m + lane] = 0;
-    if (lane == 0) sh.n[w] = m;
+    if (lane < 8) cand[n + lane] = 0;
+    if (lane == 0) sh.n[w] = n;
     if (threadIdx.x < LP_MOST) sh.top[threadIdx.x] = 0;
     __syncthreads();
+    u32 m = n;
+    if (sh.n[0] + sh.n[1] + sh.n[2] + sh.n[3] > LP_RANKED) {         // too many to rank all of them: those that are not below a bound
+      u32 best = 0;
+#pragma unroll 1
+      for (u32 i = lane; i < n; i += 64) best = max(best, (u32)(cand[i] >> 32));
+      lp_kth(sh, best, a.k);
+      m = 0;
+      const u32 kth = sh.kth;
+#pragma unroll 1
+      for (u32 i = lane; i - lane < n; i += 64) {
+        const u64 x = i < n ? cand[i] : 0, mask = __ballot(x && (u32)(x >> 32) >= kth);
+        if (x && (u32)(x >> 32) >= kth) cand[m + lp_below(mask)] = x;
+        m += (u32)__popcll(mask);
+      }
+      if (lane < 8) cand[m + lane] = 0;
+      if (lane == 0) sh.n[w] = m;
+      __syncthreads();
+    }
 #pragma unroll 1
     for (u32 i = lane; i < m; i += 64) {
       const u64 key = cand[i];
@@ -353,12 +364,12 @@ __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShar
         const u64* const x = sh.cand + l * LP_CAP;
         const u32 end = sh.n[l];
 #pragma unroll 1
-        for (u32 j = 0; j < end; j += 4) {
+        for (u32 j = 0; j < end; j += 8) {
 #pragma unroll
-          for (u32 h = 0; h < 4; ++h) place += x[j + h] > key ? 1u : 0u;
+          for (u32 h = 0; h < 8; ++h) place += x[j + h] > key ? 1u : 0u;
         }
       }
-      if (place < a.k) sh.top[place] = key;
+      if (place < a.k && key) sh.top[place] = key;
     }
     __syncthreads();
   };
@@ -395,7 +406,14 @@ __device__ __forceinline__ void token_logprobs(const LogprobArgs& a, LogprobShar
     if (lane < a.parts) sum = {__uint_as_float(get(lane, 0)), __uint_as_float(get(lane, 1)), __uint_as_float(get(lane, 2))};
     if (threadIdx.x < a.given) {
       before = 0;
-      for (u32 p = 0; p < a.parts; ++p) before += get(p, 4 + threadIdx.x);
+#pragma unroll 1
+      for (u32 p = 0; p < a.parts; p += 8) {         // (eight on their way)
+        u32 v[8];
+#pragma unroll
+        for (u32 i = 0; i < 8; ++i) v[i] = get(min(p + i, a.parts - 1), 4 + threadIdx.x);
+#pragma unroll
+        for (u32 i = 0; i < 8; ++i) before += p + i < a.parts ? v[i] : 0u;
+      }
     }
     sum.to(lp_wave_max(sum.m), c);
     sum.s = lp_wave_sum(sum.s); sum.t = lp_wave_sum(sum.t);
