@@ -99,19 +99,19 @@ __device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, SharedRoo
   return r;
 }
 
-// Results joined: of rows whose keys are their group's and their sequence's, and of rows whose keys were cut into parts. A wave per token, kv head and as many
-// of its query heads as it has HD / 4 lanes for.
+// Results joined: of rows whose keys are their group's and their sequence's, and of rows whose keys were cut into parts. A wave per token and as many query heads
+// as it has HD / 4 lanes for.
 template <int HD> __host__ __device__ constexpr u32 join_heads() { return 64 / (HD / 4); }
 template <int HD>
 __device__ __forceinline__ void shared_join(const SharedArgs& a, u32 i) {
   constexpr u32 LANES = HD / 4, AT_ONCE = 8;
-  const u32 per = (a.G + join_heads<HD>() - 1) / join_heads<HD>(), lane = threadIdx.x & 63, d = lane % LANES * 4;
-  const u32 t = i / (a.nkv * per), g = i / per % a.nkv, h = i % per * join_heads<HD>() + lane / LANES;
+  const u32 per = (a.nq + join_heads<HD>() - 1) / join_heads<HD>(), lane = threadIdx.x & 63, d = lane % LANES * 4;
+  const u32 t = i / per, head = i % per * join_heads<HD>() + lane / LANES, g = head / a.G, h = head - g * a.G;
   if (t >= a.n_tokens) return;
   const JoinToken j = a.tokens[t];
   if (!j.kind) return;
   const u32 quota = *(const u32*)(a.tokens + a.n_tokens);
-  if (h < a.G) {
+  if (head < a.nq) {
     float M = -INFINITY, L = 0.f;
     floatx4_t O = {0.f, 0.f, 0.f, 0.f};
     // n results, result(x): maximum and sum, output
@@ -140,7 +140,7 @@ __device__ __forceinline__ void shared_join(const SharedArgs& a, u32 i) {
       }
     };
     auto of_row = [&](u32 which) {
-      const float* const b = row_result<HD>(a, which, t, g * a.G + h);
+      const float* const b = row_result<HD>(a, which, t, head);
       take(1, [&](u32) { return b; }, [&](u32) { return b + 4 + d; });
     };
     if (j.kind == 1) {
@@ -157,7 +157,7 @@ __device__ __forceinline__ void shared_join(const SharedArgs& a, u32 i) {
       take(j.parts, [&](u32 x) { return first + (u64)x * PROMPT_SLOT(HD) + 2 * in; }, [&](u32 x) { return first + (u64)x * PROMPT_SLOT(HD) + 2 * PROMPT_ROWS + in * HD + d; });
     } else of_row(1);
     const float inv = L == 0.f ? 0.f : 1.0f / L;
-    *(uint2*)out_at(a, t, (g * a.G + h) * HD + d) = make_uint2(half_pair(O[0] * inv, O[1] * inv), half_pair(O[2] * inv, O[3] * inv));
+    *(uint2*)out_at(a, t, head * HD + d) = make_uint2(half_pair(O[0] * inv, O[1] * inv), half_pair(O[2] * inv, O[3] * inv));
   }
 }
 
