@@ -402,6 +402,9 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   p.lead = hd == 128 ? 5 : 9;
   p.light = a->cache.bits == 16 ? 1 : 2;
   p.few_cost = (a->cache.bits == 16 ? 0.26f : 0.13f) * (plan.ct == 1 ? 1.f : 1.5f);
+  // (what sharing must gain on every compute unit: 8 us for the groups' starts and the join, and what rows' results take to memory and back. 64 sequences in
+  // 4 bits, 1024 shared keys: 26.5 us, 27.8 apart; 253 behind 64: 78.5, 70 apart; 40 groups of 4, heads of 64, behind 64 and 256: 29.8, 37, apart 23.7, 40.4)
+  p.gain = (u32)((hd == 128 ? 1.f : 2.f) * (8.f + (float)a->n_tokens * (float)a->n_q_heads * (float)(16 * ROW_RESULT(hd)) * 2e-7f) * (float)n_cu / (float)nkv);
   p.n_groups = s->n_groups; p.share_all = s->share_all; p.starts = s->group_starts; p.shared = s->shared_lens;
   const hipStream_t st = (hipStream_t)stream;
   HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_shared<64, 16>(p, plan.ct, n_cu, st) : launch_shared<64, 4>(p, plan.ct, n_cu, st))

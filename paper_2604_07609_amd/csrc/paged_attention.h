@@ -50,6 +50,7 @@ struct SharedArgs : PagedArgs {
   u32 light;                      // units of a step of an item of 128 rows or less (of others: 2)
   u32 lead;                       // time of an item of the groups' shared keys beside its steps, in units (FlatShape)
   float few_cost;                 // time of a tile of few rows on one compute unit, in units
+  u32 gain;                       // units that all groups together must save for a kv head
   struct JoinToken* tokens;       // what is to be joined of every token, and behind them the units of a workgroup's run (FlatRun)
 };
 #define ROW_RESULT(HD) ((HD) + 4u)                   // maximum, sum, two unused, output
@@ -321,7 +322,7 @@ struct CacheTile<HD, 4> {
 #define PROMPT_ROWS (128u * PROMPT_CT)
 #define SHARED_ROWS 256u           // sequences with so many rows fill a prompt item by themselves
 #define SHARED_GAIN 2.f            // units that a group must save
-#define FEW_PAIR 3u                // what a pair of a sequence and a kv head takes beside its tiles, in tiles (96 sequences with 5 to 300 keys of their own, in 4 bits: 88 us with 2, 81 with 3 and 4; 253 with 17 to 1000: 98, 99, 100)
+#define FEW_PAIR 3u                // what a pair of a sequence and a kv head takes beside its tiles, in tiles (96 sequences with 5 to 300 keys of their own, in 4 bits: 88 us with 2, 81 with 3 and 4; 253 with 17 to 1000: 105 with none, 99 with 1 to 3)
 struct NoLinks {};
 struct ViewLinks { uint16_t link[PAGED_MAX_SEQS]; };      // of a sequence: its group, or NO_GROUP; of a group: the sequence whose table it takes
 #define NO_GROUP 0xFFFFu
@@ -566,11 +567,12 @@ __device__ __forceinline__ u32 flat_units(const SharedArgs& a, const SharedView&
   return v.n * a.G <= a.short_rows ? 0u : flat_shape(a, v).all() * a.nkv;
 }
 // The views of a call with groups, by a workgroup of NT threads, in LDS: those of the sequences, then those of the groups. A sequence goes by its group where it gains by that and may: it has fewer rows than a prompt item,
-// all its queries stand behind the shared keys and see every one of them, and all of these together take less time with the shared keys apart. The shared keys are cut to a multiple of 64, what a step of
-// the prompt part takes. room: 5 n_groups + 1 words of LDS.
+// all its queries stand behind the shared keys and see every one of them, and all of these together take less time with the shared keys apart; and only if all groups together gain more than
+// what results that are joined take. The shared keys are cut to a multiple of 64, what a step of the prompt part takes. room: 5 n_groups + 2 words of LDS.
 template <u32 NT>
 __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, SharedView* view) {
-  u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const to = from + a.n_groups, *const members = to + a.n_groups;
+  u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const to = from + a.n_groups, *const members = to + a.n_groups, *const saved = members + a.n_groups;
+  if (threadIdx.x == 0) *saved = 0;
   for (u32 g = threadIdx.x; g <= a.n_groups; g += NT) {
     starts[g] = (u32)max(0, min(a.starts[g], (i32)a.n_seqs));
     if (g == a.n_groups) break;
@@ -604,16 +606,22 @@ __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, Sha
     if (from[g] < to[g]) {
       const u32 t0 = view[from[g]].t0, end = view[to[g]].t0 + view[to[g]].n, n = end > t0 ? end - t0 : 0u, tiles = keys[g] / 16;
       const float together = n * a.G <= a.short_rows ? a.few_cost * (float)(tiles + FEW_PAIR) : (float)flat_shape(a, n * a.G, keys[g]).all();
-      if (a.share_all || (float)members[g] * (float)tiles * a.few_cost > together + SHARED_GAIN) x = {t0, n, (i32)keys[g] - 1, 0, from[g]};
+      const float gain = (float)members[g] * (float)tiles * a.few_cost - together;
+      if (a.share_all || gain > SHARED_GAIN) {
+        x = {t0, n, (i32)keys[g] - 1, 0, from[g]};
+        if (!a.share_all) atomicAdd(saved, (u32)min(gain, 1e6f));      // (1024 times that is less than 2^32)
+      }
     }
     view[a.n_seqs + g] = x;
   }
   __syncthreads();
+  const bool share = a.share_all || *saved >= a.gain;
+  if (!share) for (u32 g = threadIdx.x; g < a.n_groups; g += NT) view[a.n_seqs + g] = SharedView{0, 0, -1, 0, 0};
 #pragma unroll
   for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j) {
     const u32 s = threadIdx.x + j * NT, g = group[j];
     if (s >= a.n_seqs) continue;
-    const bool in = g != NO_GROUP && view[a.n_seqs + g].n != 0;
+    const bool in = share && g != NO_GROUP && view[a.n_seqs + g].n != 0;
     view[s] = SharedView{v[j].t0, v[j].n, v[j].pos0, in ? keys[g] : 0u, g};
   }
   __syncthreads();
