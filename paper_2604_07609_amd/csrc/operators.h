@@ -219,7 +219,7 @@ struct PagedPlan {
   u64 part_bytes, prompt_bytes;
   u64 bytes(u32 n_cu) const { return paged_ctr_bytes(n_cu) + part_bytes + prompt_bytes; }
 };
-static PagedPlan paged_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_seqs, u32 n_tokens, u32 max_q, u32 key_steps, u32 n_cu) {
+static PagedPlan paged_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_seqs, u32 n_tokens, u32 max_q, u32 steps, u32 n_cu) {
   PagedPlan p{};
   const u32 G = nq / nkv, most = 16u * SHORT_MORE(hd);       // rows that the short part's registers hold
   const u64 rows = (u64)max_q * G;
@@ -234,7 +234,7 @@ static PagedPlan paged_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_seqs, u32 n
   // parts of 256 keys at least, where the items are too few for the chip (64 queries at 8192 keys: 45 us, of 1024 at least 49, in one
   // part 212; parts of 128 gain nothing and need twice the adding up)
   const bool few = (u64)n_tokens * G / PROMPT_ROWS * nkv < p.wgs;
-  p.n_splits = p.prompt && few ? std::max(1u, key_steps / 4) : 1u;
+  p.n_splits = p.prompt && few ? std::max(1u, steps / 4) : 1u;
   p.part_bytes = p.ct ? short_floats(p.wgs, hd, p.ct) * 4 : 0;
   p.prompt_bytes = p.prompt ? (u64)p.wgs * PROMPT_SLOT(hd) * 4 : 0;
   return p;
@@ -296,6 +296,12 @@ static int check_attention(const blink_paged_attention_args* a, float* scale2, b
   return BLINK_OK;
 }
 
+// steps of 64 keys of a prompt item, at most
+static u32 key_steps(const blink_paged_attention_args* a) {
+  const u64 reach = a->window ? (u64)a->window + a->max_q + a->sinks : ~0ull;
+  return (u32)std::min<u64>(a->max_blocks / 4 + 1, reach / 64 + 3);
+}
+
 extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention_args* a, void* stream) {
   g_err.clear();
   if (!a) return fail(BLINK_ERR_INVAL, "null argument");
@@ -306,9 +312,7 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
   const u32 hd = a->cache.head_dim, nkv = a->cache.n_kv_heads;
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  const u64 reach = a->window ? (u64)a->window + a->max_q + a->sinks : ~0ull;
-  const u32 key_steps = (u32)std::min<u64>(a->max_blocks / 4 + 1, reach / 64 + 3);
-  const PagedPlan plan = paged_plan(hd, a->cache.bits, a->n_q_heads, nkv, a->n_seqs, a->n_tokens, a->max_q, key_steps, n_cu);
+  const PagedPlan plan = paged_plan(hd, a->cache.bits, a->n_q_heads, nkv, a->n_seqs, a->n_tokens, a->max_q, key_steps(a), n_cu);
   if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.bytes(n_cu))
     return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)plan.bytes(n_cu));
   OnDevice on(device);
@@ -332,12 +336,12 @@ struct SharedPlan {
   u64 part_bytes, prompt_bytes, flat_bytes, row_bytes, token_bytes;
   u64 bytes(u32 n_cu) const { return paged_ctr_bytes(n_cu) + part_bytes + prompt_bytes + flat_bytes + row_bytes + token_bytes; }
 };
-static SharedPlan shared_plan(u32 hd, u32 nq, u32 nkv, u32 n_groups, u32 n_tokens, u32 max_q, u32 key_steps, u32 n_cu) {
+static SharedPlan shared_plan(u32 hd, u32 nq, u32 nkv, u32 n_groups, u32 n_tokens, u32 max_q, u32 steps, u32 n_cu) {
   SharedPlan p{};
   const u32 G = nq / nkv, most = 16u * SHORT_MORE(hd);
   const u64 own = (u64)max_q * G, all = (hd == 64 ? ((u64)n_tokens + n_groups - 1) / std::max(n_groups, 1u) : (u64)n_tokens) * G;      // rows of a sequence; of a group, about
   p.ct = (all <= most ? all > 16 : own > 16 && own <= most) ? SHORT_MORE(hd) : 1;
-  p.n_splits = std::max(1u, key_steps / 4);          // (parts of 256 keys at least)
+  p.n_splits = std::max(1u, steps / 4);          // (parts of 256 keys at least)
   p.part_bytes = short_floats(n_cu, hd, p.ct) * 4;
   p.prompt_bytes = (u64)n_cu * PROMPT_SLOT(hd) * 4;
   p.flat_bytes = 2 * p.prompt_bytes;
@@ -345,15 +349,21 @@ static SharedPlan shared_plan(u32 hd, u32 nq, u32 nkv, u32 n_groups, u32 n_token
   p.token_bytes = (n_tokens + 1ull) * sizeof(JoinToken);
   return p;
 }
-static int check_groups(u32 n_seqs, u32 n_groups) {
+// waves of the join: one per token and as many query heads as it has lanes for
+static u64 join_waves(u32 hd, u32 nq, u32 n_tokens) {
+  const u32 heads = hd == 64 ? join_heads<64>() : join_heads<128>();
+  return (u64)n_tokens * ((nq + heads - 1) / heads);
+}
+static int check_groups(const blink_kv_cache& c, u32 nq, u32 n_seqs, u32 n_groups, u32 n_tokens) {
   if ((u64)n_seqs + n_groups > PAGED_MAX_SEQS) return fail(BLINK_ERR_TOO_LARGE, "%u sequences and %u groups, at most %u together in one call", n_seqs, n_groups, PAGED_MAX_SEQS);
+  if (n_groups && join_waves(c.head_dim, nq, n_tokens) * 64 + BLK_THREADS > (1ull << 32)) return fail(BLINK_ERR_TOO_LARGE, "%u tokens of %u heads are too many for one call with groups", n_tokens, nq);
   return BLINK_OK;
 }
 
 extern "C" int blink_shared_attention_workspace_bytes(int32_t device, const blink_kv_cache* c, uint32_t n_q_heads, uint32_t n_seqs, uint32_t n_groups, uint32_t n_tokens, uint32_t max_q, uint64_t* bytes) {
   if (int rc = blink_attention_workspace_bytes(device, c, n_q_heads, n_seqs, max_q, bytes)) return rc;      // (a call without groups)
-  if (int rc = check_groups(n_seqs, n_groups)) return rc;
   if ((u64)n_tokens * n_q_heads >= (1ull << 31)) return fail(BLINK_ERR_TOO_LARGE, "2^31 rows or more");
+  if (int rc = check_groups(*c, n_q_heads, n_seqs, n_groups, n_tokens)) return rc;
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
   SharedPlan plan = shared_plan(c->head_dim, n_q_heads, c->n_kv_heads, n_groups, n_tokens, max_q, 1, n_cu);
@@ -366,7 +376,7 @@ template <int HD, int BITS>
 static hipError_t launch_shared(const SharedArgs& args, u32 ct, u32 n_cu, hipStream_t st) {
   constexpr u32 NT = 64 * PAGED_WAVES;
   const hipError_t e = ct == 1 ? launch(k_shared_attention<HD, BITS, 1>, n_cu, NT, st, args) : launch(k_shared_attention<HD, BITS, SHORT_MORE(HD)>, n_cu, NT, st, args);
-  const u64 waves = (u64)args.n_tokens * ((args.nq + join_heads<HD>() - 1) / join_heads<HD>());
+  const u64 waves = join_waves(HD, args.nq, args.n_tokens);
   return e == hipSuccess ? launch(k_shared_join<HD>, (u32)((waves * 64 + BLK_THREADS - 1) / BLK_THREADS), BLK_THREADS, st, args) : e;
 }
 
@@ -377,7 +387,7 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   float scale2;
   bool nothing;
   if (int rc = check_attention(a, &scale2, &nothing)) return rc;
-  if (int rc = check_groups(a->n_seqs, s->n_groups)) return rc;
+  if (int rc = check_groups(a->cache, a->n_q_heads, a->n_seqs, s->n_groups, a->n_tokens)) return rc;
   if (nothing) return BLINK_OK;
   if (s->n_groups == 0) return blink_paged_attention(device, a, stream);
   const u32 hd = a->cache.head_dim, nkv = a->cache.n_kv_heads;
@@ -386,7 +396,7 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   if (!s->group_starts || !s->shared_lens || (u64)s->group_starts % 4 || (u64)s->shared_lens % 4) return fail(BLINK_ERR_INVAL, "group_starts or shared_lens is null or not aligned");
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  const SharedPlan plan = shared_plan(hd, a->n_q_heads, nkv, s->n_groups, a->n_tokens, a->max_q, a->max_blocks / 4 + 1, n_cu);
+  const SharedPlan plan = shared_plan(hd, a->n_q_heads, nkv, s->n_groups, a->n_tokens, a->max_q, key_steps(a), n_cu);
   if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.bytes(n_cu))
     return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)plan.bytes(n_cu));
   OnDevice on(device);
