@@ -9,6 +9,12 @@
 // below it, or equal and in a later tile, is not among the k first. The keys of the others come together in LDS, each wave's apart; of more than LP_FEW (a
 // wave adds a tile at most) the kth is searched for bit by bit, and what is below it thrown away. At last all are ranked, every
 // one against every other.
+//
+// Bound by the logits' bytes, and for few rows by latencies, one after the other. Waves work on their own, each with its next tile on its way, and meet at a row's end only: tiles
+// of a workgroup, with a barrier or two each, took twice as long (1021 rows of 151936 in 16 bits, no alternatives: 122 us, now 57, 5.4 TB/s). 256 rows of 128256
+// floats take 26 us, 5.1 TB/s, without alternatives and 35 with 20 of them: a microsecond for the bound, two for the keys of the waves, three to five for a row's parts, while
+// nothing is read. Loops over a wave's keys are not unrolled: with four instances (38 KB of code) instructions come from memory once each, and that took 59 us. One row of
+// 32000 with 5 alternatives: 11.3 us (1 to start, 1 the bound, 4 the tile, 2 the keys, 3 the parts).
 #pragma once
 #include "blink_device.h"
 
@@ -16,11 +22,14 @@
 #define LP_TILE (64u * LP_VALS)    // a wave's
 #define LP_WAVES (BLK_THREADS / 64u)
 #define LP_MOST 64u                // given tokens (a lane each), most probable tokens
-#define LP_FEW 160u                // keys that a wave keeps from tile to tile at most
+#define LP_FEW 160u                // keys that a wave keeps from tile to tile at most (256 rows of 128256, 20 alternatives: 36 us; with 96 40, with 256, and so fewer workgroups at a time, 50)
 #define LP_CAP (LP_FEW + LP_TILE + 8)      // (and zeros behind them)
-#define LP_RANKED 96u              // keys of a workgroup that are ranked as they are
-#define LP_MAX_PARTS 32u           // workgroups of a row (LP_MAX_PARTS LP_MOST keys at most are joined)
-#define LP_PER_CU 4u               // workgroups that a call has for every compute unit, where its rows have the tiles
+#define LP_RANKED 96u              // keys of a workgroup that are ranked as they are (the 256 rows: 36 us; with 48 38, with 192 37)
+// workgroups of a row, and keys of theirs that are joined (8 rows of 128256, 5 alternatives: 14.6 us in 32 parts, 13.8 in 16, 15.7 in 8; 64 rows with 64 of them: 48 us with
+// 1024 keys, 34 with 512, 45 with 320, 58 with 128)
+#define LP_MAX_PARTS 16u
+#define LP_JOINED 512u
+#define LP_PER_CU 4u               // workgroups that a call has for every compute unit, where its rows have the tiles (the 256 rows: 36 us; with 2, 3, 6: 46, 36, 48)
 #define LP_LOWEST -3.4028235e38f
 #define LP_LN2 0.69314718055994530942f
 #define LP_CTR_BYTES 8192u         // of the workspace: a counter per row whose parts are joined

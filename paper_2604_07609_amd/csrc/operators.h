@@ -147,11 +147,11 @@ extern "C" int blink_kv_cache_copy(int32_t device, const blink_kv_cache* caches,
 }
 
 // ---- log probabilities ----------------------------------------------------------------------------------------------------------
-// workgroups of a row: LP_PER_CU for every compute unit in all, a tile for each of their waves at least
-static u32 logprob_parts(u32 rows, u32 vocab, u32 n_cu) {
+// workgroups of a row: LP_PER_CU for every compute unit in all, a tile for each of their waves at least, and no more keys to join than LP_JOINED
+static u32 logprob_parts(u32 rows, u32 vocab, u32 k, u32 n_cu) {
   const u32 tiles = (vocab + LP_WAVES * LP_TILE - 1) / (LP_WAVES * LP_TILE);
   const u64 want = ((u64)LP_PER_CU * n_cu + rows - 1) / rows;
-  return rows > LP_CTR_BYTES / 4 ? 1u : (u32)std::min<u64>({want, tiles, LP_MAX_PARTS});
+  return rows > LP_CTR_BYTES / 4 ? 1u : (u32)std::min<u64>({want, tiles, LP_MAX_PARTS, LP_JOINED / std::max(k, 1u)});
 }
 static int check_logprobs(u32 rows, u32 vocab, u32 given, u32 k) {
   if (!vocab || vocab > (1u << 30)) return fail(BLINK_ERR_INVAL, "vocab must be in [1, 2^30]");
@@ -192,7 +192,7 @@ extern "C" int blink_token_logprobs(int32_t device, const blink_token_logprobs_a
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
   LogprobArgs l{};
-  l.parts = logprob_parts(a->n_rows, a->vocab, n_cu);
+  l.parts = logprob_parts(a->n_rows, a->vocab, a->k, n_cu);
   const u64 need = logprob_bytes(a->n_rows, a->n_given, a->k, l.parts);
   if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < need) return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)need);
   OnDevice on(device);
