@@ -408,7 +408,9 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   p.rows = p.prompt_part + plan.flat_bytes / 4;
   p.tokens = (JoinToken*)(p.rows + plan.row_bytes / 4);
   // (times on one compute unit, by which workgroups are dealt out. A unit, half a step of 256 rows: 1.03 us with heads of 128, 1.2 over 4 bits, half of that with
-  // heads of 64; a tile of few rows 0.28 us, 0.16 over 4 bits; an item's start and end 5 to 6 us)
+  // heads of 64; a tile of few rows 0.28 us, 0.16 over 4 bits; an item's start and end 5 to 6 us. A step of 128 rows or less takes half as long, over 4 bits as long as one
+  // of 256, since its keys and values are converted all the same. 16 groups of 8 with 4, 5, 7 units ahead of an item: 58.2, 58.0, 59.9 us, with tiles of 0.24, 0.26, 0.28 us: 60.5, 58.0, 58.4;
+  // 96 sequences with 5 drafts in 4 bits with half units for light steps: 88.5, so 81)
   p.lead = hd == 128 ? 5 : 9;
   p.light = a->cache.bits == 16 ? 1 : 2;
   p.few_cost = (a->cache.bits == 16 ? 0.26f : 0.13f) * (plan.ct == 1 ? 1.f : 1.5f);

@@ -321,7 +321,7 @@ struct CacheTile<HD, 4> {
 #define PROMPT_CT 2u
 #define PROMPT_ROWS (128u * PROMPT_CT)
 #define SHARED_ROWS 256u           // sequences with so many rows fill a prompt item by themselves
-#define SHARED_GAIN 2.f            // units that a group must save
+#define SHARED_GAIN 2.f            // units that a group must save for a kv head: its start and end, two times, beside those of others
 #define FEW_PAIR 3u                // what a pair of a sequence and a kv head takes beside its tiles, in tiles (96 sequences with 5 to 300 keys of their own, in 4 bits: 88 us with 2, 81 with 3 and 4; 253 with 17 to 1000: 105 with none, 99 with 1 to 3)
 struct NoLinks {};
 struct ViewLinks { uint16_t link[PAGED_MAX_SEQS]; };      // of a sequence: its group, or NO_GROUP; of a group: the sequence whose table it takes
