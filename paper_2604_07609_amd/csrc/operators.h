@@ -328,18 +328,19 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
 
 // ---- attention of groups --------------------------------------------------------------------------------------------------------
 // Rows of a sequence and of a group are the few-row part's up to 16 ct: what the sequences with the most queries need or, where that takes all groups' rows,
-// these do (40 groups of up to four sequences with 9 queries, heads of 64: 67 us with the groups' keys as steps of prompt items, 50 as tiles of few rows). With
-// heads of 128 that is asked for only where all tokens' rows are few: 16 groups of 8 sequences of 4 rows took 40.5 us as prompt items, 43 as tiles. (Lengths of groups are known on the
-// device only: their mean stands for them.)
+// these do, by their mean (lengths of groups are known on the device only): a step of a prompt item costs a group of few rows as much as one of 128, over 4 bits as one of 256.
+// 40 groups of up to four sequences with 9 queries, heads of 64: 67 us with the groups' keys as steps of prompt items, 52 as tiles of few rows; 16 groups of 8 behind 2000 and 8000 tokens, heads of 64:
+// 41 and 90, so 32 and 72; heads of 128 over 4 bits: 52 and 132, so 40 and 68. Over halves with heads of 128 the steps are as fast or faster (46 and 117 us, as tiles 47 and 120; behind 500 tokens 31, 36), so
+// there it is asked for only where all tokens' rows are few.
 struct SharedPlan {
   u32 ct, n_splits;
   u64 part_bytes, prompt_bytes, flat_bytes, row_bytes, token_bytes;
   u64 bytes(u32 n_cu) const { return paged_ctr_bytes(n_cu) + part_bytes + prompt_bytes + flat_bytes + row_bytes + token_bytes; }
 };
-static SharedPlan shared_plan(u32 hd, u32 nq, u32 nkv, u32 n_groups, u32 n_tokens, u32 max_q, u32 steps, u32 n_cu) {
+static SharedPlan shared_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_groups, u32 n_tokens, u32 max_q, u32 steps, u32 n_cu) {
   SharedPlan p{};
   const u32 G = nq / nkv, most = 16u * SHORT_MORE(hd);
-  const u64 own = (u64)max_q * G, all = (hd == 64 ? ((u64)n_tokens + n_groups - 1) / std::max(n_groups, 1u) : (u64)n_tokens) * G;      // rows of a sequence; of a group, about
+  const u64 own = (u64)max_q * G, all = (hd == 64 || bits == 4 ? ((u64)n_tokens + n_groups - 1) / std::max(n_groups, 1u) : (u64)n_tokens) * G;      // rows of a sequence; of a group, about
   p.ct = (all <= most ? all > 16 : own > 16 && own <= most) ? SHORT_MORE(hd) : 1;
   p.n_splits = std::max(1u, steps / 4);          // (parts of 256 keys at least)
   p.part_bytes = short_floats(n_cu, hd, p.ct) * 4;
@@ -366,7 +367,7 @@ extern "C" int blink_shared_attention_workspace_bytes(int32_t device, const blin
   if (int rc = check_groups(*c, n_q_heads, n_seqs, n_groups, n_tokens)) return rc;
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  SharedPlan plan = shared_plan(c->head_dim, n_q_heads, c->n_kv_heads, n_groups, n_tokens, max_q, 1, n_cu);
+  SharedPlan plan = shared_plan(c->head_dim, c->bits, n_q_heads, c->n_kv_heads, n_groups, n_tokens, max_q, 1, n_cu);
   plan.part_bytes = short_floats(n_cu, c->head_dim, SHORT_MORE(c->head_dim)) * 4;
   *bytes = std::max<u64>(*bytes, plan.bytes(n_cu));
   return BLINK_OK;
@@ -396,7 +397,7 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   if (!s->group_starts || !s->shared_lens || (u64)s->group_starts % 4 || (u64)s->shared_lens % 4) return fail(BLINK_ERR_INVAL, "group_starts or shared_lens is null or not aligned");
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  const SharedPlan plan = shared_plan(hd, a->n_q_heads, nkv, s->n_groups, a->n_tokens, a->max_q, key_steps(a), n_cu);
+  const SharedPlan plan = shared_plan(hd, a->cache.bits, a->n_q_heads, nkv, s->n_groups, a->n_tokens, a->max_q, key_steps(a), n_cu);
   if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.bytes(n_cu))
     return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)plan.bytes(n_cu));
   OnDevice on(device);

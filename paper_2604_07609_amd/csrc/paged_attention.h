@@ -883,7 +883,8 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
           strange |= tile[j].take_strange_out(any);
         }
 #pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c].add(tile[j], q[c], a.c, edge, vis[c]);
+        for (int c = 0; c < CT; ++c)
+          if (!SHARED || !c || c * 16u < cur.n * a.G) acc[c].add(tile[j], q[c], a.c, edge, vis[c]);
       }
       ask(j);
       ++u;
