@@ -408,16 +408,17 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   p.prompt_part = p.own_part + plan.prompt_bytes / 4;
   p.rows = p.prompt_part + plan.flat_bytes / 4;
   p.tokens = (JoinToken*)(p.rows + plan.row_bytes / 4);
-  // (times on one compute unit, by which workgroups are dealt out. A unit, half a step of 256 rows: 1.03 us with heads of 128, 1.2 over 4 bits, half of that with
-  // heads of 64; a tile of few rows 0.28 us, 0.16 over 4 bits; an item's start and end 5 to 6 us. A step of 128 rows or less takes half as long, over 4 bits as long as one
-  // of 256, since its keys and values are converted all the same. 16 groups of 8 with 4, 5, 7 units ahead of an item: 58.2, 58.0, 59.9 us, with tiles of 0.24, 0.26, 0.28 us: 60.5, 58.0, 58.4;
-  // 96 sequences with 5 drafts in 4 bits with half units for light steps: 88.5, so 81)
-  p.lead = hd == 128 ? 5 : 9;
-  p.light = a->cache.bits == 16 ? 1 : 2;
-  p.few_cost = (a->cache.bits == 16 ? 0.26f : 0.13f) * (plan.ct == 1 ? 1.f : 1.5f);
+  // (times on one compute unit, by which workgroups are dealt out. A unit: a quarter of a step of 256 rows, see FlatShape. Against units of half a step, with one for a step of 128 rows or less
+  // (two over 4 bits): up to 96 sequences with 5 drafts 82 us, so 76 in 4 bits, 82 and 73 over halves; 12 groups of 70 120, 107; 200 sequences of heads of 64 71, 60; three groups of 30 52, 53.
+  // 16 groups of 8 sequences, 32 rows each, 59, and with FLAT_LIGHT for them 63)
+  const bool halves = a->cache.bits == 16;
+  const float unit = hd == 128 ? (halves ? 0.47f : 0.56f) : (halves ? 0.38f : 0.49f);
+  p.lead = hd == 128 ? 13 : halves ? 18 : 9;
+  p.least = halves ? 2 : FLAT_LIGHT;
+  p.few_cost = (halves ? 0.6f : 0.26f) * (plan.ct == 1 ? 1.f : 1.5f);
   // (what sharing must gain on every compute unit: 8 us for the groups' starts and the join, and what rows' results take to memory and back. 64 sequences in
   // 4 bits, 1024 shared keys: 26.5 us, 27.8 apart; 253 behind 64: 78.5, 70 apart; 40 groups of 4, heads of 64, behind 64 and 256: 29.8, 37, apart 23.7, 40.4)
-  p.gain = (u32)((hd == 128 ? 1.f : 2.f) * (8.f + (float)a->n_tokens * (float)a->n_q_heads * (float)(16 * ROW_RESULT(hd)) * 2e-7f) * (float)n_cu / (float)nkv);
+  p.gain = (u32)((8.f + (float)a->n_tokens * (float)a->n_q_heads * (float)(16 * ROW_RESULT(hd)) * 2e-7f) / unit * (float)n_cu / (float)nkv);
   p.n_groups = s->n_groups; p.share_all = s->share_all; p.starts = s->group_starts; p.shared = s->shared_lens;
   const hipStream_t st = (hipStream_t)stream;
   HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_shared<64, 16>(p, plan.ct, n_cu, st) : launch_shared<64, 4>(p, plan.ct, n_cu, st))

@@ -47,7 +47,7 @@ struct SharedArgs : PagedArgs {
   const i32 *starts, *shared;     // first sequence of every group (n_groups + 1), tokens that its sequences share
   float* rows;                    // results to be joined: [of the group, of the sequence][token][q head] of ROW_RESULT(hd) floats
   float* own_part;                // parts of prompt items (prompt_part: of the groups' items)
-  u32 light;                      // units of a step of an item of 128 rows or less (of others: 2)
+  u32 least;                      // units of a step of a group of 32 rows or less in all (of others: FLAT_STEP, of items of 128 rows or less FLAT_LIGHT)
   u32 lead;                       // time of an item of the groups' shared keys beside its steps, in units (FlatShape)
   float few_cost;                 // time of a tile of few rows on one compute unit, in units
   u32 gain;                       // units that all groups together must save for a kv head
@@ -321,7 +321,9 @@ struct CacheTile<HD, 4> {
 #define PROMPT_CT 2u
 #define PROMPT_ROWS (128u * PROMPT_CT)
 #define SHARED_ROWS 256u           // sequences with so many rows fill a prompt item by themselves
-#define SHARED_GAIN 2.f            // units that a group must save for a kv head: its start and end, two times, beside those of others
+#define FLAT_STEP 4u               // units of a step of the groups' shared keys, and of one of an item of 128 rows or less
+#define FLAT_LIGHT 3u
+#define SHARED_GAIN 4.f            // units that a group must save for a kv head: its start and end, two times, beside those of others
 #define FEW_PAIR 3u                // what a pair of a sequence and a kv head takes beside its tiles, in tiles (96 sequences with 5 to 300 keys of their own, in 4 bits: 88 us with 2, 81 with 3 and 4; 253 with 17 to 1000: 105 with none, 99 with 1 to 3)
 struct NoLinks {};
 struct ViewLinks { uint16_t link[PAGED_MAX_SEQS]; };      // of a sequence: its group, or NO_GROUP; of a group: the sequence whose table it takes
@@ -550,17 +552,19 @@ __device__ __forceinline__ void give_strange(const CacheTile<HD, BITS>& t, float
 }
 
 // The groups with more rows than the few-row part takes: their rows in items of FLAT_ROWS (whole queries), each with all shared keys. All steps of
-// all (group, kv head, item) are one line of units, one a step (over 4 bits two, whatever the rows) or, for items of more than 128 rows, two, and `lead` ahead of an
-// item's, and every workgroup has an equal run of it. An item inside a run is done there; one that several runs share leaves a result in each.
+// all (group, kv head, item) are one line of units, FLAT_STEP, FLAT_LIGHT or `least` a step, and `lead` ahead of an item's, and every workgroup has an equal run of it. An item inside a run is
+// done there; one that several runs share leaves a result in each. The units are what workgroups' times fit, to within 1.3 us of 30 to 75: a piece of an item, its start and end, takes
+// 6.3 us (over 4 bits 7.0; with heads of 64: 6.8, 4.4), a step of 256 rows 1.87 (2.25; 1.52, 1.97), one of 128 or less 1.37 (1.68; 1.10, 1.47), of a
+// group of 32 rows over halves 1.17, bound by bytes like the tiles of few rows.
 __device__ __forceinline__ u32 flat_rows(const PagedArgs& a) { return PROMPT_ROWS / a.G * a.G; }
 struct FlatShape {
-  u32 items, steps, lead, last;                      // items of a kv head; weight of the last one's steps (the others': 2)
-  __device__ __forceinline__ u32 units(u32 item) const { return steps * (item + 1 < items ? 2 : last) + lead; }
-  __device__ __forceinline__ u32 all() const { return (items - 1) * (2 * steps + lead) + last * steps + lead; }
+  u32 items, steps, lead, last;                      // items of a kv head; units of the last one's steps (the others': FLAT_STEP)
+  __device__ __forceinline__ u32 units(u32 item) const { return steps * (item + 1 < items ? FLAT_STEP : last) + lead; }
+  __device__ __forceinline__ u32 all() const { return (items - 1) * (FLAT_STEP * steps + lead) + last * steps + lead; }
 };
 __device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, u32 rows, u32 keys) {
   const u32 per = flat_rows(a), items = (rows + per - 1) / per;
-  return {items, keys / 64, a.lead, rows - (items - 1) * per > 128 ? 2u : a.light};
+  return {items, keys / 64, a.lead, rows - (items - 1) * per > 128 ? FLAT_STEP : rows > 32 ? FLAT_LIGHT : a.least};
 }
 __device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, const SharedView& v) { return flat_shape(a, v.n * a.G, (u32)v.pos0 + 1); }
 __device__ __forceinline__ u32 flat_units(const SharedArgs& a, const SharedView& v) {      // of a group
@@ -1130,15 +1134,15 @@ __device__ __forceinline__ void lds_barrier() {
 }
 template <int N> __device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 struct FlatRun { u32 from, end; };
-struct FlatPiece { u32 s_lo, s_hi, next; bool whole, begins, any; };       // any: has steps (or a half of one)
+struct FlatPiece { u32 s_lo, s_hi, next; bool whole, begins, any; };       // any: has units of steps (of steps themselves perhaps none)
 template <typename Room>
 __device__ __forceinline__ PromptItem flat_piece(const SharedArgs& a, const Room& sh, u32 u, u32 end, FlatPiece& p) {
   PromptItem it;
   const u32 g = last_at_most(sh.flat, a.n_groups, u);
   const SharedView v = sh.view[a.n_seqs + g];
   const FlatShape f = flat_shape(a, v);
-  const u32 all = f.all(), x = u - sh.flat[g], head = x / all, full = 2 * f.steps + f.lead, item = min((x - head * all) / full, f.items - 1);
-  const u32 per = f.units(item), off = x - head * all - item * full, to = min(per, off + end - u), weight = item + 1 < f.items ? 2u : f.last;
+  const u32 all = f.all(), x = u - sh.flat[g], head = x / all, full = FLAT_STEP * f.steps + f.lead, item = min((x - head * all) / full, f.items - 1);
+  const u32 per = f.units(item), off = x - head * all - item * full, to = min(per, off + end - u), weight = item + 1 < f.items ? FLAT_STEP : f.last;
   auto step = [&](u32 at) { return at > f.lead ? (at - f.lead + weight - 1) / weight : 0u; };
   p = {step(off), step(to), u + to - off, off <= f.lead && to == per, off <= f.lead, to > f.lead};
   it.s = a.n_seqs + g;

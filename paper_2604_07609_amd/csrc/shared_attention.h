@@ -36,7 +36,8 @@ __device__ __forceinline__ void views_and_sums(const SharedArgs& a, SharedRoom& 
       if (group) v[1] = flat_units(a, x); else v[0] = prompt_items(a, x);
       const u32 tiles = short_unit_count(a, x, group);
       v[2] = (tiles ? tiles + FEW_PAIR : 0u) * a.nkv;
-      if (v[0]) v[3] = v[0] * (2 * seen_tiles<64>(a, x.pos0, x.pos0 + (i32)x.n - 1, x.first).n + a.lead) * a.nkv;
+      // (a time to go by, and that there is some: held to a second's, so that 1024 of them stay within 32 bits)
+      if (v[0]) v[3] = (u32)min((u64)v[0] * (FLAT_STEP * seen_tiles<64>(a, x.pos0, x.pos0 + (i32)x.n - 1, x.first).n + a.lead) * a.nkv, (u64)1 << 21);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = wave_sums_dpp(v[k]);
@@ -88,7 +89,7 @@ __device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, SharedRoo
         if (t - x.t0 < x.n && flat_units(a, x)) {    // (cu_seqlens that decrease may put a token outside its group)
           const FlatShape f = flat_shape(a, x);
           const u32 item = r / flat_rows(a);
-          j.units[0] = sh.flat[v.row] + item * (2 * f.steps + f.lead) + f.lead; j.units[1] = f.all(); j.units[2] = f.units(item) - f.lead;
+          j.units[0] = sh.flat[v.row] + item * (FLAT_STEP * f.steps + f.lead) + f.lead; j.units[1] = f.all(); j.units[2] = f.units(item) - f.lead;
           j.row = r - item * flat_rows(a);
         } else j.units[2] = 1;                       // (by one workgroup, into rows)
       }
