@@ -1093,9 +1093,6 @@ __device__ __forceinline__ PromptItem prompt_item(const A& a, const u32* pre, u3
   it.p1 = v.pos0 + (i32)((it.r0 + it.rows - 1) / a.G);
   it.lo = v.lo();
   it.row = it.s;
-  if constexpr (is_shared<A>) {
-    it.row = it.s;
-  }
   return it;
 }
 
