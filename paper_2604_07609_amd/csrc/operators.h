@@ -327,11 +327,6 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
 }
 
 // ---- attention of groups --------------------------------------------------------------------------------------------------------
-// Rows of a sequence and of a group are the few-row part's up to 16 ct: what the sequences with the most queries need or, where that takes all groups' rows,
-// these do, by their mean (lengths of groups are known on the device only): a step of a prompt item costs a group of few rows as much as one of 128, over 4 bits as one of 256.
-// 40 groups of up to four sequences with 9 queries, heads of 64: 67 us with the groups' keys as steps of prompt items, 52 as tiles of few rows; 16 groups of 8 behind 2000 and 8000 tokens, heads of 64:
-// 41 and 90, so 32 and 72; heads of 128 over 4 bits: 52 and 132, so 40 and 68. Over halves with heads of 128 the steps are as fast or faster (46 and 117 us, as tiles 47 and 120; behind 500 tokens 31, 36), so
-// there it is asked for only where all tokens' rows are few.
 struct SharedPlan {
   u32 ct, n_splits;
   u64 part_bytes, prompt_bytes, flat_bytes, row_bytes, token_bytes;
@@ -339,9 +334,7 @@ struct SharedPlan {
 };
 static SharedPlan shared_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_groups, u32 n_tokens, u32 max_q, u32 steps, u32 n_cu) {
   SharedPlan p{};
-  const u32 G = nq / nkv, most = 16u * SHORT_MORE(hd);
-  const u64 own = (u64)max_q * G, all = (hd == 64 || bits == 4 ? ((u64)n_tokens + n_groups - 1) / std::max(n_groups, 1u) : (u64)n_tokens) * G;      // rows of a sequence; of a group, about
-  p.ct = (all <= most ? all > 16 : own > 16 && own <= most) ? SHORT_MORE(hd) : 1;
+  p.ct = few_row_tiles(hd, bits, nq / nkv, n_tokens, n_groups, max_q);
   p.n_splits = std::max(1u, steps / 4);          // (parts of 256 keys at least)
   p.part_bytes = short_floats(n_cu, hd, p.ct) * 4;
   p.prompt_bytes = (u64)n_cu * PROMPT_SLOT(hd) * 4;
@@ -408,17 +401,7 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   p.prompt_part = p.own_part + plan.prompt_bytes / 4;
   p.rows = p.prompt_part + plan.flat_bytes / 4;
   p.tokens = (JoinToken*)(p.rows + plan.row_bytes / 4);
-  // (times on one compute unit, by which workgroups are dealt out. A unit: a quarter of a step of 256 rows, see FlatShape. Against units of half a step, with one for a step of 128 rows or less
-  // (two over 4 bits): up to 96 sequences with 5 drafts 82 us, so 76 in 4 bits, 82 and 73 over halves; 12 groups of 70 120, 107; 200 sequences of heads of 64 71, 60; three groups of 30 52, 53.
-  // 16 groups of 8 sequences, 32 rows each, 59, and with FLAT_LIGHT for them 63)
-  const bool halves = a->cache.bits == 16;
-  const float unit = hd == 128 ? (halves ? 0.47f : 0.56f) : (halves ? 0.38f : 0.49f);
-  p.lead = hd == 128 ? 13 : halves ? 18 : 9;
-  p.least = halves ? 2 : FLAT_LIGHT;
-  p.few_cost = (halves ? 0.6f : 0.26f) * (plan.ct == 1 ? 1.f : 1.5f);
-  // (what sharing must gain on every compute unit: 8 us for the groups' starts and the join, and what rows' results take to memory and back. 64 sequences in
-  // 4 bits, 1024 shared keys: 26.5 us, 27.8 apart; 253 behind 64: 78.5, 70 apart; 40 groups of 4, heads of 64, behind 64 and 256: 29.8, 37, apart 23.7, 40.4)
-  p.gain = (u32)((8.f + (float)a->n_tokens * (float)a->n_q_heads * (float)(16 * ROW_RESULT(hd)) * 2e-7f) / unit * (float)n_cu / (float)nkv);
+  shared_costs(p, hd, a->cache.bits, plan.ct, n_cu);
   p.n_groups = s->n_groups; p.share_all = s->share_all; p.starts = s->group_starts; p.shared = s->shared_lens;
   const hipStream_t st = (hipStream_t)stream;
   HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_shared<64, 16>(p, plan.ct, n_cu, st) : launch_shared<64, 4>(p, plan.ct, n_cu, st))

@@ -17,80 +17,7 @@
 #pragma once
 #include "attention_mfma.h"
 #include "kv_store.h"
-#include <type_traits>
-
-struct PagedArgs {
-  const f16_t* q;                 // [token][q head][hd]
-  u64 qs;                         // elements between tokens
-  f16_t* out;                     // [token][q head][hd], or packed GEMM operand (out_tbs != 0)
-  u64 os;
-  u32 out_tbs;
-  const i32 *cu, *lens;           // first token of every sequence (n_seqs + 1), its context with them
-  const u32* tables;              // [row][max_blocks] block ids
-  const u32* table_row;           // row of every sequence (null: its number)
-  const void* cache;
-  u32 n_blocks, max_blocks;
-  u32 nq, nkv, G;
-  u32 n_seqs, n_tokens, max_q;    // sequences; tokens of q and out; queries of a sequence that are looked at
-  u32 window, sinks;
-  float c;                        // scale of the scores * log2(e)
-  u32 short_rows;                 // sequences with at most so many rows are the short part's
-  u32 n_splits;                   // most parts of a prompt item's keys
-  u32* ctr;                       // zeros between launches (paged_counters): next prompt item, workgroups done, then the short part's
-  float *part, *prompt_part;      // partial results of the short and of the prompt part
-};
-
-// A call in which sequences of a group have their first blocks in common: those keys are seen once for the group, by the rows of all of its
-// sequences at a time (shared_views). So a call has a view for each sequence and, behind those, one for each group.
-struct SharedArgs : PagedArgs {
-  u32 n_groups, share_all;        // share_all: groups that gain nothing by it too
-  const i32 *starts, *shared;     // first sequence of every group (n_groups + 1), tokens that its sequences share
-  float* rows;                    // results to be joined: [of the group, of the sequence][token][q head] of ROW_RESULT(hd) floats
-  float* own_part;                // parts of prompt items (prompt_part: of the groups' items)
-  u32 least;                      // units of a step of a group of 32 rows or less in all (of others: FLAT_STEP, of items of 128 rows or less FLAT_LIGHT)
-  u32 lead;                       // time of an item of the groups' shared keys beside its steps, in units (FlatShape)
-  float few_cost;                 // time of a tile of few rows on one compute unit, in units
-  u32 gain;                       // units that all groups together must save for a kv head
-  struct JoinToken* tokens;       // what is to be joined of every token, and behind them the units of a workgroup's run (FlatRun)
-};
-#define ROW_RESULT(HD) ((HD) + 4u)                   // maximum, sum, two unused, output
-template <typename A> constexpr bool is_shared = std::is_same<A, SharedArgs>::value;
-__device__ __forceinline__ u32 n_views(const PagedArgs& a) { return a.n_seqs; }
-__device__ __forceinline__ u32 n_views(const SharedArgs& a) { return a.n_seqs + a.n_groups; }
-
-// One sequence: its tokens, where its queries stand, and which blocks they see
-struct SeqView {
-  u32 t0, n;
-  i32 pos0;
-  __device__ __forceinline__ u32 lo() const { return 0; }
-};
-// The same, and of a group: all its queries stand at its last key. first: the first key seen here (those before it are the group's), a multiple of 64
-struct SharedView {
-  u32 t0, n;
-  i32 pos0;
-  u32 first, row;                                    // row: of a group, of the table; of a sequence, its group (first != 0)
-  __device__ __forceinline__ u32 lo() const { return first; }
-};
-__device__ __forceinline__ SeqView seq_view(const PagedArgs& a, u32 s) {
-  SeqView v;
-  const i32 c0 = max(0, min(a.cu[s], (i32)a.n_tokens)), c1 = max(c0, min(a.cu[s + 1], (i32)a.n_tokens));
-  v.t0 = (u32)c0;
-  v.n = min((u32)(c1 - c0), a.max_q);
-  v.pos0 = max(0, min(a.lens[s], (i32)(a.max_blocks * 16))) - (c1 - c0);
-  return v;
-}
-// Visible tiles of TK keys of the queries at positions p0 .. p1 (p1 >= 0): the first `zb` ones, then those from `wlo` to `hi`
-struct Seen { u32 zb, wlo, n; };
-// (lo: keys before this multiple of TK are not looked at; not together with a window that begins behind key 0)
-template <u32 TK>
-__device__ __forceinline__ Seen seen_tiles(const PagedArgs& a, i32 p0, i32 p1, u32 lo = 0) {
-  Seen r;
-  r.wlo = a.window && p0 >= (i32)a.window ? (u32)(p0 - (i32)a.window + 1) / TK : 0u;
-  r.zb = min((a.sinks + TK - 1) / TK, r.wlo);
-  r.wlo += lo / TK;
-  r.n = p1 < 0 ? 0u : r.zb + (u32)p1 / TK + 1 - r.wlo;
-  return r;
-}
+#include "paged_views.h"
 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef i32 i32x8_t __attribute__((ext_vector_type(8)));
@@ -317,17 +244,8 @@ struct CacheTile<HD, 4> {
 };
 
 #define PAGED_WAVES 8              // waves of a workgroup of the prompt part
-#define PAGED_MAX_SEQS 1024u       // sequences (and groups) whose views a workgroup keeps in LDS
-#define PROMPT_CT 2u
-#define PROMPT_ROWS (128u * PROMPT_CT)
-#define SHARED_ROWS 256u           // sequences with so many rows fill a prompt item by themselves
-#define FLAT_STEP 4u               // units of a step of the groups' shared keys, and of one of an item of 128 rows or less
-#define FLAT_LIGHT 3u
-#define SHARED_GAIN 4.f            // units that a group must save for a kv head: its start and end, two times, beside those of others
-#define FEW_PAIR 3u                // what a pair of a sequence and a kv head takes beside its tiles, in tiles (96 sequences with 5 to 300 keys of their own, in 4 bits: 88 us with 2, 81 with 3 and 4; 253 with 17 to 1000: 105 with none, 99 with 1 to 3)
 struct NoLinks {};
 struct ViewLinks { uint16_t link[PAGED_MAX_SEQS]; };      // of a sequence: its group, or NO_GROUP; of a group: the sequence whose table it takes
-#define NO_GROUP 0xFFFFu
 template <int HD, int CT, int NW, bool SHARED = false>
 struct ShortShared : std::conditional<SHARED, ViewLinks, NoLinks>::type {
   // a result that one wave leaves for others, as its registers hold it: of the pair that its run begins inside of; at NW, of the pair
@@ -551,94 +469,6 @@ __device__ __forceinline__ void give_strange(const CacheTile<HD, BITS>& t, float
   }
 }
 
-// The groups with more rows than the few-row part takes: their rows in items of FLAT_ROWS (whole queries), each with all shared keys. All steps of
-// all (group, kv head, item) are one line of units, FLAT_STEP, FLAT_LIGHT or `least` a step, and `lead` ahead of an item's, and every workgroup has an equal run of it. An item inside a run is
-// done there; one that several runs share leaves a result in each. The units are what workgroups' times fit, to within 1.3 us of 30 to 75: a piece of an item, its start and end, takes
-// 6.3 us (over 4 bits 7.0; with heads of 64: 6.8, 4.4), a step of 256 rows 1.87 (2.25; 1.52, 1.97), one of 128 or less 1.37 (1.68; 1.10, 1.47), of a
-// group of 32 rows over halves 1.17, bound by bytes like the tiles of few rows.
-__device__ __forceinline__ u32 flat_rows(const PagedArgs& a) { return PROMPT_ROWS / a.G * a.G; }
-struct FlatShape {
-  u32 items, steps, lead, last;                      // items of a kv head; units of the last one's steps (the others': FLAT_STEP)
-  __device__ __forceinline__ u32 units(u32 item) const { return steps * (item + 1 < items ? FLAT_STEP : last) + lead; }
-  __device__ __forceinline__ u32 all() const { return (items - 1) * (FLAT_STEP * steps + lead) + last * steps + lead; }
-};
-__device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, u32 rows, u32 keys) {
-  const u32 per = flat_rows(a), items = (rows + per - 1) / per;
-  return {items, keys / 64, a.lead, rows - (items - 1) * per > 128 ? FLAT_STEP : rows > 32 ? FLAT_LIGHT : a.least};
-}
-__device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, const SharedView& v) { return flat_shape(a, v.n * a.G, (u32)v.pos0 + 1); }
-__device__ __forceinline__ u32 flat_units(const SharedArgs& a, const SharedView& v) {      // of a group
-  return v.n * a.G <= a.short_rows ? 0u : flat_shape(a, v).all() * a.nkv;
-}
-// The views of a call with groups, by a workgroup of NT threads, in LDS: those of the sequences, then those of the groups. A sequence goes by its group where it gains by that and may: it has fewer rows than a prompt item,
-// all its queries stand behind the shared keys and see every one of them, and all of these together take less time with the shared keys apart; and only if all groups together gain more than
-// what results that are joined take. The shared keys are cut to a multiple of 64, what a step of the prompt part takes. room: 5 n_groups + 2 words of LDS.
-template <u32 NT>
-__device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, SharedView* view) {
-  u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const to = from + a.n_groups, *const members = to + a.n_groups, *const saved = members + a.n_groups;
-  if (threadIdx.x == 0) *saved = 0;
-  for (u32 g = threadIdx.x; g <= a.n_groups; g += NT) {
-    starts[g] = (u32)max(0, min(a.starts[g], (i32)a.n_seqs));
-    if (g == a.n_groups) break;
-    keys[g] = (u32)max(0, min(a.shared[g], (i32)(a.max_blocks * 16))) / 64 * 64;
-    from[g] = ~0u; to[g] = 0; members[g] = 0;
-  }
-  SeqView v[(PAGED_MAX_SEQS + NT - 1) / NT];         // (asked for before the barrier)
-#pragma unroll
-  for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j)
-    if (threadIdx.x + j * NT < a.n_seqs) v[j] = seq_view(a, threadIdx.x + j * NT);
-  __syncthreads();
-  u32 group[(PAGED_MAX_SEQS + NT - 1) / NT];
-#pragma unroll
-  for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j) {
-    const u32 s = threadIdx.x + j * NT;
-    group[j] = NO_GROUP;
-    if (s >= a.n_seqs || !a.n_groups || s < starts[0]) continue;
-    u32 g = 0;
-    for (u32 step = 1u << (31 - __clz((int)a.n_groups)); step; step >>= 1) if (g + step < a.n_groups && starts[g + step] <= s) g += step;      // the last that begins here or before
-    const i32 p1 = v[j].pos0 + (i32)v[j].n - 1;
-    if (s >= starts[g + 1] || !keys[g] || !v[j].n || v[j].n * a.G >= SHARED_ROWS || v[j].pos0 < (i32)keys[g] || (a.window && p1 >= (i32)a.window)) continue;
-    atomicMin(from + g, s);
-    atomicMax(to + g, s);
-    atomicAdd(members + g, 1u);
-    view[s] = SharedView{v[j].t0, v[j].n, 0, 0, 0};
-    group[j] = g;
-  }
-  __syncthreads();
-  for (u32 g = threadIdx.x; g < a.n_groups; g += NT) {
-    SharedView x = {0, 0, -1, 0, 0};
-    if (from[g] < to[g]) {
-      const u32 t0 = view[from[g]].t0, end = view[to[g]].t0 + view[to[g]].n, n = end > t0 ? end - t0 : 0u, tiles = keys[g] / 16;
-      const float together = n * a.G <= a.short_rows ? a.few_cost * (float)(tiles + FEW_PAIR) : (float)flat_shape(a, n * a.G, keys[g]).all();
-      const float gain = (float)members[g] * (float)tiles * a.few_cost - together;
-      if (a.share_all || gain > SHARED_GAIN) {
-        x = {t0, n, (i32)keys[g] - 1, 0, from[g]};
-        if (!a.share_all) atomicAdd(saved, (u32)min(gain, 1e6f));      // (1024 times that is less than 2^32)
-      }
-    }
-    view[a.n_seqs + g] = x;
-  }
-  __syncthreads();
-  const bool share = a.share_all || *saved >= a.gain;
-  if (!share) for (u32 g = threadIdx.x; g < a.n_groups; g += NT) view[a.n_seqs + g] = SharedView{0, 0, -1, 0, 0};
-#pragma unroll
-  for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j) {
-    const u32 s = threadIdx.x + j * NT, g = group[j];
-    if (s >= a.n_seqs) continue;
-    const bool in = share && g != NO_GROUP && view[a.n_seqs + g].n != 0;
-    view[s] = SharedView{v[j].t0, v[j].n, v[j].pos0, in ? keys[g] : 0u, g};
-  }
-  __syncthreads();
-}
-
-__device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqView& v) {     // tiles of a sequence and kv head; 0: not this part's, 1 at least else
-  if (!v.n || v.n * a.G > a.short_rows) return 0;
-  return max(1u, seen_tiles<16>(a, v.pos0, v.pos0 + (i32)v.n - 1).n);
-}
-__device__ __forceinline__ u32 short_unit_count(const SharedArgs& a, const SharedView& v, bool group) {
-  if (!v.n || v.n * a.G > a.short_rows) return 0;
-  return max(1u, seen_tiles<16>(a, v.pos0, group ? v.pos0 : v.pos0 + (i32)v.n - 1, v.first).n);
-}
 // whether a view's results are joined with others
 template <typename Shared>
 __device__ __forceinline__ bool is_joined(const SharedArgs& a, const Shared& sh, u32 s) { return s >= a.n_seqs || (u32)__builtin_amdgcn_readfirstlane(sh.link[s]) != NO_GROUP; }
@@ -1071,14 +901,6 @@ struct PromptRoom {
 typedef PromptRoom<SeqView> PromptShared;
 struct SharedRoom : PromptRoom<SharedView> { u32 flat[PAGED_MAX_SEQS + 1], sum[2]; };      // units of the groups before each; of the few rows' tiles, of prompt items' steps
 template <typename A> using PromptRoomOf = typename std::conditional<is_shared<A>, SharedRoom, PromptShared>::type;
-template <typename View>
-__device__ __forceinline__ u32 prompt_items(const PagedArgs& a, const View& v) {
-  return v.n * a.G <= a.short_rows ? 0u : (v.n * a.G + PROMPT_ROWS - 1) / PROMPT_ROWS;
-}
-// parts of every item's keys: as many as there are workgroups for
-__device__ __forceinline__ u32 prompt_parts(const PagedArgs& a, u32 items, u32 nwg) { return items && items < nwg ? max(1u, min(a.n_splits, nwg / items)) : 1u; }
-
-struct PromptItem { u32 s, g, r0, rows, t0; i32 p0, p1; u32 lo, row; };      // rows r0 .. r0 + rows of the view's, queries at positions p0 .. p1; first key, row of the table
 template <typename A, typename F>
 __device__ __forceinline__ PromptItem prompt_item(const A& a, const u32* pre, u32 item, F view) {
   PromptItem it;
@@ -1130,26 +952,6 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 template <int N> __device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
-struct FlatRun { u32 from, end; };
-struct FlatPiece { u32 s_lo, s_hi, next; bool whole, begins, any; };       // any: has units of steps (of steps themselves perhaps none)
-template <typename Room>
-__device__ __forceinline__ PromptItem flat_piece(const SharedArgs& a, const Room& sh, u32 u, u32 end, FlatPiece& p) {
-  PromptItem it;
-  const u32 g = last_at_most(sh.flat, a.n_groups, u);
-  const SharedView v = sh.view[a.n_seqs + g];
-  const FlatShape f = flat_shape(a, v);
-  const u32 all = f.all(), x = u - sh.flat[g], head = x / all, full = FLAT_STEP * f.steps + f.lead, item = min((x - head * all) / full, f.items - 1);
-  const u32 per = f.units(item), off = x - head * all - item * full, to = min(per, off + end - u), weight = item + 1 < f.items ? FLAT_STEP : f.last;
-  auto step = [&](u32 at) { return at > f.lead ? (at - f.lead + weight - 1) / weight : 0u; };
-  p = {step(off), step(to), u + to - off, off <= f.lead && to == per, off <= f.lead, to > f.lead};
-  it.s = a.n_seqs + g;
-  it.g = head;
-  it.r0 = item * flat_rows(a);
-  it.rows = min(flat_rows(a), v.n * a.G - it.r0);
-  it.t0 = v.t0; it.p0 = it.p1 = v.pos0; it.lo = 0; it.row = v.row;
-  return it;
-}
-
 __device__ __forceinline__ float* own_parts(const PagedArgs& a) { return a.prompt_part; }
 __device__ __forceinline__ float* own_parts(const SharedArgs& a) { return a.own_part; }
 // FLAT: the groups' shared keys in place of prompts, workgroup wg's run of them. All rows see all keys, so what is done for masks falls away, but
@@ -1204,7 +1006,8 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
     PromptItem it;
     FlatPiece piece;
     if constexpr (FLAT) {
-      it = flat_piece(a, sh, turn, total, piece);
+      const u32 of = last_at_most(sh.flat, a.n_groups, turn);
+      it = flat_piece(a, sh.view[a.n_seqs + of], of, sh.flat[of], turn, total, piece);
       if (!piece.any) return;                        // (the end of the run, within an item's lead)
     } else it = prompt_item(a, sh.pre, item, [&](u32 s) { return sh.view[s]; });
     it.s = (u32)__builtin_amdgcn_readfirstlane(it.s); it.g = (u32)__builtin_amdgcn_readfirstlane(it.g); it.r0 = (u32)__builtin_amdgcn_readfirstlane(it.r0);
@@ -1544,7 +1347,7 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
         for (int d = 0; d < HD / 16; ++d)
           *(uint2*)(to + (u64)(d / 2) * step + d % 2 * half) = make_uint2(half_pair(o[c][d][0] * inv, o[c][d][1] * inv), half_pair(o[c][d][2] * inv, o[c][d][3] * inv));
       } else {
-        float* const slot = (SHARED && !FLAT ? own_parts(a) : a.prompt_part) + (u64)(FLAT ? 2 * wg + (piece.begins ? 1u : 0u) : this_turn) * PROMPT_SLOT(HD);
+        float* const slot = (SHARED && !FLAT ? own_parts(a) : a.prompt_part) + (u64)(FLAT ? flat_slot(wg, piece.begins) : this_turn) * PROMPT_SLOT(HD);
         if (lg_end == 0) *(float2*)(slot + 2 * r) = make_float2(m[c], sum);
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(slot + 2 * PROMPT_ROWS + r * HD + d * 16 + lg_end * 4) = o[c][d];

@@ -5,10 +5,7 @@
 #include "logprobs.h"
 #include "paged_attention.h"
 
-// Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold; 8 sequences of 4000 keys with 32
-// rows take 30 us and 60 as prompts, 30 of 2000 in 4 bits with 40 rows 24 and 47), and tiles of keys on their way (two where there are
-// more rows: registers; 4 bits with three 122 us, with two 124)
-#define SHORT_MORE(HD) ((HD) == 64 ? 4 : 2)
+// Tiles of keys on their way: two where there are more rows (registers; 4 bits with three 122 us, with two 124)
 #define SHORT_AHEAD(HD, BITS, CT) ((CT) > 1 ? 2 : (HD) == 128 || (BITS) == 4 ? 3 : 4)
 #define PAGED_BOUNDS __launch_bounds__(512) __attribute__((amdgpu_num_vgpr(120)))       // (see PHASE_KERNEL8)
 // One row tile over a 4-bit cache is bound by instructions: three workgroups of four waves on a compute unit, else one of eight (128
@@ -18,7 +15,6 @@
 #define SHORT_PER_CU(BITS, CT) (SHORT_SMALL(BITS, CT) ? 3 : 1)
 
 #include "shared_attention.h"
-
 
 template <typename T, int HD, int BITS> __global__ void k_kv_store(StoreArgs a);
 __global__ void k_kv_read(ReadArgs a, u32 hd);

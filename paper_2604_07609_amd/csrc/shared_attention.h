@@ -3,13 +3,6 @@
 #pragma once
 #include "paged_attention.h"
 
-// What is to be joined of a token's rows (kinds 0: nothing, its results are in place; 1: a result of its group and one of its sequence; 2: parts of a prompt
-// item's keys). Its group's: units[0] + kv head * units[1] is where its item's line of units[2] begins, row: its first row there. Its sequence's:
-// in rows, or parts of prompt items (parts > 1): items top - (row + head) / PROMPT_ROWS.
-struct JoinToken { u32 kind, units[3], row, own_row, top, parts; };
-
-// The work of a call with groups, by every workgroup all the same: views, who has the groups' shared keys and who the rest. Then notes for the join.
-struct SharedWork { u32 flat_wgs, quota; bool few, prompts; };
 // inclusive prefix sum over the wave, without LDS: sums over rows of 16 lanes, then the rows before
 __device__ __forceinline__ u32 wave_sums_dpp(u32 v) {
   v += (u32)__builtin_amdgcn_update_dpp(0, (i32)v, 0x111, 0xF, 0xF, true);      // row_shr 1, 2, 4, 8
@@ -29,16 +22,8 @@ __device__ __forceinline__ void views_and_sums(const SharedArgs& a, SharedRoom& 
   u32 base[4] = {0, 0, 0, 0};
   for (u32 s0 = 0; s0 < n_views(a); s0 += NT) {
     const u32 s = s0 + threadIdx.x;
-    u32 v[4] = {0, 0, 0, 0};                         // items, flat units, tiles of few rows, steps of prompt items
-    if (s < n_views(a)) {
-      const SharedView x = sh.view[s];
-      const bool group = s >= a.n_seqs;
-      if (group) v[1] = flat_units(a, x); else v[0] = prompt_items(a, x);
-      const u32 tiles = short_unit_count(a, x, group);
-      v[2] = (tiles ? tiles + FEW_PAIR : 0u) * a.nkv;
-      // (a time to go by, and that there is some: held to a second's, so that 1024 of them stay within 32 bits)
-      if (v[0]) v[3] = (u32)min((u64)v[0] * (FLAT_STEP * seen_tiles<64>(a, x.pos0, x.pos0 + (i32)x.n - 1, x.first).n + a.lead) * a.nkv, (u64)1 << 21);
-    }
+    u32 v[4] = {0, 0, 0, 0};
+    if (s < n_views(a)) view_units(a, sh.view[s], s >= a.n_seqs, v);
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = wave_sums_dpp(v[k]);
     if (s0) __syncthreads();
@@ -64,38 +49,13 @@ template <int HD>
 __device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, SharedRoom& sh, u32 wg, u32 nwg) {
   constexpr u32 NT = 64 * PAGED_WAVES;
   views_and_sums(a, sh);
-  SharedWork r;
   const u32 units = (u32)__builtin_amdgcn_readfirstlane(sh.flat[a.n_groups]);
   const u32 tiles = (u32)__builtin_amdgcn_readfirstlane(sh.sum[0]), prompts = (u32)__builtin_amdgcn_readfirstlane(sh.sum[1]);
-  r.few = tiles != 0; r.prompts = prompts != 0;
-  const float flat = (float)units, rest = a.few_cost * (float)tiles + (float)prompts;
-  r.flat_wgs = !units ? 0u : rest == 0.f ? nwg : min(nwg - 1, max(1u, (u32)((float)nwg * flat / (flat + rest) + 0.5f)));
-  r.quota = r.flat_wgs ? (units + r.flat_wgs - 1) / r.flat_wgs : 1u;
+  const SharedWork r = deal_out(a, units, tiles, prompts, nwg);
   if (wg == 0 && threadIdx.x == 0) *(u32*)(a.tokens + a.n_tokens) = r.quota;
   // (the parts of prompt items: as the workgroups that take them cut them)
   const u32 item_rows = (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]), parts = prompt_parts(a, item_rows * a.nkv, nwg - r.flat_wgs);
-  for (u32 t = wg * NT + threadIdx.x; t < a.n_tokens; t += nwg * NT) {
-    u32 s = 0;                                       // the last sequence that begins at this token or before
-    for (u32 step = PAGED_MAX_SEQS / 2; step; step >>= 1) if (s + step < a.n_seqs && sh.view[s + step].t0 <= t) s += step;
-    const SharedView v = sh.view[s];
-    JoinToken j = {};
-    if (t >= v.t0 && t - v.t0 < v.n) {
-      const bool cut = parts > 1 && prompt_items(a, v) != 0;
-      j.own_row = (t - v.t0) * a.G; j.top = item_rows - 1 - sh.pre[s]; j.parts = cut ? parts : 1;
-      j.kind = v.first ? 1 : cut ? 2 : 0;
-      if (v.first) {
-        const SharedView x = sh.view[a.n_seqs + v.row];
-        const u32 r = (t - x.t0) * a.G;
-        if (t - x.t0 < x.n && flat_units(a, x)) {    // (cu_seqlens that decrease may put a token outside its group)
-          const FlatShape f = flat_shape(a, x);
-          const u32 item = r / flat_rows(a);
-          j.units[0] = sh.flat[v.row] + item * (FLAT_STEP * f.steps + f.lead) + f.lead; j.units[1] = f.all(); j.units[2] = f.units(item) - f.lead;
-          j.row = r - item * flat_rows(a);
-        } else j.units[2] = 1;                       // (by one workgroup, into rows)
-      }
-    }
-    a.tokens[t] = j;
-  }
+  for (u32 t = wg * NT + threadIdx.x; t < a.n_tokens; t += nwg * NT) a.tokens[t] = join_token(a, sh.view, sh.pre, sh.flat, parts, t);
   __syncthreads();
   return r;
 }
@@ -141,14 +101,14 @@ __device__ __forceinline__ void shared_join(const SharedArgs& a, u32 i) {
       }
     };
     auto of_row = [&](u32 which) {
-      const float* const b = row_result<HD>(a, which, t, head);
+      const float* const b = row_result<HD>(a, which, j.rows[which], head);
       take(1, [&](u32) { return b; }, [&](u32) { return b + 4 + d; });
     };
     if (j.kind == 1) {
       const u32 begin = j.units[0] + g * j.units[1], w0 = begin / quota, w1 = (begin + j.units[2] - 1) / quota, r = j.row + h;
       if (w0 == w1) of_row(0);
       else {
-        auto slot = [&](u32 x) { return a.prompt_part + (u64)(2 * (w0 + x) + (x ? 0u : 1u)) * PROMPT_SLOT(HD); };
+        auto slot = [&](u32 x) { return a.prompt_part + (u64)flat_slot(w0 + x, x == 0) * PROMPT_SLOT(HD); };
         take(w1 - w0 + 1, [&](u32 x) { return slot(x) + 2 * r; }, [&](u32 x) { return slot(x) + 2 * PROMPT_ROWS + r * HD + d; });
       }
     }
