@@ -1034,8 +1034,10 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
     for (int c = 0; c < CT; ++c) {
       const u32 r = wr + c * 16 + lc, rr = it.r0 + min(r, it.rows - 1), tok = rr / a.G, h = rr - tok * a.G;
       qpos[c] = r < it.rows ? it.p0 - (i32)(it.r0 / a.G) + (i32)tok : -1;
+      u32 token = it.t0 + tok;
+      if constexpr (FLAT) token = group_token(a, sh.view, sh.view[it.s], tok);
 #pragma unroll
-      for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(a.q + (u64)(it.t0 + tok) * a.qs + (it.g * a.G + h) * HD + s * 32 + lg * 8);
+      for (int s = 0; s < HD / 32; ++s) q[c][s] = ld_tile(a.q + (u64)token * a.qs + (it.g * a.G + h) * HD + s * 32 + lg * 8);
     }
     floatx4_t o[CT][HD / 16];
     float m[CT], l[CT];

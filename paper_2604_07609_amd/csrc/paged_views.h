@@ -3,6 +3,19 @@
 #pragma once
 #include <type_traits>
 
+// Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold; 8 sequences of 4000 keys with 32
+// rows take 30 us and 60 as prompts, 30 of 2000 in 4 bits with 40 rows 24 and 47)
+#define SHORT_MORE(HD) ((HD) == 64 ? 4 : 2)
+#define PAGED_MAX_SEQS 1024u       // sequences (and groups) whose views a workgroup keeps in LDS
+#define PROMPT_CT 2u
+#define PROMPT_ROWS (128u * PROMPT_CT)
+#define SHARED_ROWS 256u           // sequences with so many rows fill a prompt item by themselves
+#define FLAT_STEP 4u               // units of a step of the groups' shared keys, and of one of an item of 128 rows or less
+#define FLAT_LIGHT 3u
+#define SHARED_GAIN 4.f            // units that a group must save for a kv head: its start and end, two times, beside those of others
+#define FEW_PAIR 3u                // what a pair of a sequence and a kv head takes beside its tiles, in tiles (96 sequences with 5 to 300 keys of their own, in 4 bits: 88 us with 2, 81 with 3 and 4; 253 with 17 to 1000: 105 with none, 99 with 1 to 3)
+#define NO_GROUP 0xFFFFu
+
 struct PagedArgs {
   const f16_t* q;                 // [token][q head][hd]
   u64 qs;                         // elements between tokens
@@ -48,12 +61,18 @@ struct SeqView {
   i32 pos0;
   __device__ __forceinline__ u32 lo() const { return 0; }
 };
-// The same, and of a group: all its queries stand at its last key. first: the first key seen here (those before it are the group's), a multiple of 64
+// The same, and of a group: the queries of its members, one member's after the other's, t0 the first one's token; all stand at the group's last key. first: the first key seen
+// here (those before it are the group's), a multiple of 64
 struct SharedView {
   u32 t0, n;
   i32 pos0;
-  u32 first, row;                                    // row: of a group, of the table; of a sequence, its group (first != 0)
-  __device__ __forceinline__ u32 group() const { return row; }
+  u32 first, which;
+  // of a sequence (first != 0): its group, and how many queries the members of all groups have before it (less than 2^18; there only where some group has gaps)
+  __device__ __forceinline__ u32 group() const { return which & (PAGED_MAX_SEQS - 1); }
+  __device__ __forceinline__ u32 before() const { return which / PAGED_MAX_SEQS; }
+  // of a group: its first member, whose row of the table it takes, and whether tokens of others lie between its members'
+  __device__ __forceinline__ u32 row() const { return which & (PAGED_MAX_SEQS - 1); }
+  __device__ __forceinline__ bool gaps() const { return which >= PAGED_MAX_SEQS; }
   __device__ __forceinline__ u32 lo() const { return first; }
 };
 __device__ __forceinline__ SeqView seq_view(const PagedArgs& a, u32 s) {
@@ -77,20 +96,7 @@ __device__ __forceinline__ Seen seen_tiles(const PagedArgs& a, i32 p0, i32 p1, u
   return r;
 }
 
-// Row tiles of the short part beyond one (64 rows with heads of 64, 32 of 128: what the registers hold; 8 sequences of 4000 keys with 32
-// rows take 30 us and 60 as prompts, 30 of 2000 in 4 bits with 40 rows 24 and 47)
-#define SHORT_MORE(HD) ((HD) == 64 ? 4 : 2)
-#define PAGED_MAX_SEQS 1024u       // sequences (and groups) whose views a workgroup keeps in LDS
-#define PROMPT_CT 2u
-#define PROMPT_ROWS (128u * PROMPT_CT)
-#define SHARED_ROWS 256u           // sequences with so many rows fill a prompt item by themselves
-#define FLAT_STEP 4u               // units of a step of the groups' shared keys, and of one of an item of 128 rows or less
-#define FLAT_LIGHT 3u
-#define SHARED_GAIN 4.f            // units that a group must save for a kv head: its start and end, two times, beside those of others
-#define FEW_PAIR 3u                // what a pair of a sequence and a kv head takes beside its tiles, in tiles (96 sequences with 5 to 300 keys of their own, in 4 bits: 88 us with 2, 81 with 3 and 4; 253 with 17 to 1000: 105 with none, 99 with 1 to 3)
-#define NO_GROUP 0xFFFFu
-
-// The groups with more rows than the few-row part takes: their rows in items of flat_rows (whole queries), each with all shared keys. All steps of
+// The groups with more rows than the few-row part takes, or with others' tokens between their members' (rows are looked up here, and not there: registers): their rows in items of flat_rows (whole queries), each with all shared keys. All steps of
 // all (group, kv head, item) are one line of units, FLAT_STEP, FLAT_LIGHT or `least` a step, and `lead` ahead of an item's, and every workgroup has an equal run of it. An item inside a run is
 // done there; one that several runs share leaves a result in each. The units are what workgroups' times fit, to within 1.3 us of 30 to 75: a piece of an item, its start and end, takes
 // 6.3 us (over 4 bits 7.0; with heads of 64: 6.8, 4.4), a step of 256 rows 1.87 (2.25; 1.52, 1.97), one of 128 or less 1.37 (1.68; 1.10, 1.47), of a
@@ -107,30 +113,34 @@ __device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, u32 rows, u
 }
 __device__ __forceinline__ FlatShape flat_shape(const SharedArgs& a, const SharedView& v) { return flat_shape(a, v.n * a.G, (u32)v.pos0 + 1); }
 __device__ __forceinline__ u32 flat_units(const SharedArgs& a, const SharedView& v) {      // of a group
-  return v.n * a.G <= a.short_rows ? 0u : flat_shape(a, v).all() * a.nkv;
+  return v.n * a.G <= a.short_rows && !v.gaps() ? 0u : flat_shape(a, v).all() * a.nkv;
 }
 // The views of a call with groups, by a workgroup of NT threads, in LDS: those of the sequences, then those of the groups. A sequence goes by its group where it gains by that and may: it has fewer rows than a prompt item,
 // all its queries stand behind the shared keys and see every one of them, and all of these together take less time with the shared keys apart; and only if all groups together gain more than
-// what results that are joined take. The shared keys are cut to a multiple of 64, what a step of the prompt part takes. room: ROOM_WORDS of LDS.
-#define ROOM_WORDS (5 * PAGED_MAX_SEQS + 2)
+// what results that are joined take. A group's rows are those of its members, wherever in its range of sequences they stand. The shared keys are cut to a multiple of 64, what a step of the
+// prompt part takes. room: ROOM_WORDS of LDS.
+#define ROOM_WORDS (9 * PAGED_MAX_SEQS + 3)
 template <u32 NT>
 __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, SharedView* view) {
-  u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const to = from + a.n_groups, *const members = to + a.n_groups, *const saved = members + a.n_groups;
-  if (threadIdx.x == 0) *saved = 0;
+  constexpr u32 EACH = (PAGED_MAX_SEQS + NT - 1) / NT;
+  // of every group: first sequence, shared keys, then of its members: the first one, how many, their queries, first token and last one + 1
+  u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const members = from + a.n_groups, *const queries = members + a.n_groups;
+  u32 *const t0 = queries + a.n_groups, *const t1 = t0 + a.n_groups, *const saved = t1 + a.n_groups, *const gaps = saved + 1;
+  if (threadIdx.x == 0) *saved = *gaps = 0;
   for (u32 g = threadIdx.x; g <= a.n_groups; g += NT) {
     starts[g] = (u32)max(0, min(a.starts[g], (i32)a.n_seqs));
     if (g == a.n_groups) break;
     keys[g] = (u32)max(0, min(a.shared[g], (i32)(a.max_blocks * 16))) / 64 * 64;
-    from[g] = ~0u; to[g] = 0; members[g] = 0;
+    from[g] = t0[g] = ~0u; members[g] = queries[g] = t1[g] = 0;
   }
-  SeqView v[(PAGED_MAX_SEQS + NT - 1) / NT];         // (asked for before the barrier)
+  SeqView v[EACH];                                   // (asked for before the barrier)
 #pragma unroll
-  for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j)
+  for (u32 j = 0; j < EACH; ++j)
     if (threadIdx.x + j * NT < a.n_seqs) v[j] = seq_view(a, threadIdx.x + j * NT);
   __syncthreads();
-  u32 group[(PAGED_MAX_SEQS + NT - 1) / NT];
+  u32 group[EACH];
 #pragma unroll
-  for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j) {
+  for (u32 j = 0; j < EACH; ++j) {
     const u32 s = threadIdx.x + j * NT;
     group[j] = NO_GROUP;
     if (s >= a.n_seqs || !a.n_groups || s < starts[0]) continue;
@@ -139,20 +149,25 @@ __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, Sha
     const i32 p1 = v[j].pos0 + (i32)v[j].n - 1;
     if (s >= starts[g + 1] || !keys[g] || !v[j].n || v[j].n * a.G >= SHARED_ROWS || v[j].pos0 < (i32)keys[g] || (a.window && p1 >= (i32)a.window)) continue;
     atomicMin(from + g, s);
-    atomicMax(to + g, s);
     atomicAdd(members + g, 1u);
+    atomicAdd(queries + g, v[j].n);
+    atomicMin(t0 + g, v[j].t0);
+    atomicMax(t1 + g, v[j].t0 + v[j].n);
     view[s] = SharedView{v[j].t0, v[j].n, 0, 0, 0};
     group[j] = g;
   }
   __syncthreads();
   for (u32 g = threadIdx.x; g < a.n_groups; g += NT) {
     SharedView x = {0, 0, -1, 0, 0};
-    if (from[g] < to[g]) {
-      const u32 t0 = view[from[g]].t0, end = view[to[g]].t0 + view[to[g]].n, n = end > t0 ? end - t0 : 0u, tiles = keys[g] / 16;
-      const float together = n * a.G <= a.short_rows ? a.few_cost * (float)(tiles + FEW_PAIR) : (float)flat_shape(a, n * a.G, keys[g]).all();
+    // (cu_seqlens that decrease may have the first member's tokens behind another one's, or a token in two members: then the rows from t0 on would not hold them, and there is no group)
+    if (members[g] > 1 && view[from[g]].t0 == t0[g] && queries[g] <= t1[g] - t0[g]) {
+      const u32 n = queries[g], tiles = keys[g] / 16;
+      const bool apart = n < t1[g] - t0[g];
+      const float together = n * a.G <= a.short_rows && !apart ? a.few_cost * (float)(tiles + FEW_PAIR) : (float)flat_shape(a, n * a.G, keys[g]).all();
       const float gain = (float)members[g] * (float)tiles * a.few_cost - together;
       if (a.share_all || gain > SHARED_GAIN) {
-        x = {t0, n, (i32)keys[g] - 1, 0, from[g]};
+        x = {t0[g], n, (i32)keys[g] - 1, 0, from[g] + (apart ? PAGED_MAX_SEQS : 0u)};
+        if (apart) atomicOr(gaps, 1u);
         if (!a.share_all) atomicAdd(saved, (u32)min(gain, 1e6f));      // (1024 times that is less than 2^32)
       }
     }
@@ -161,19 +176,46 @@ __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, Sha
   __syncthreads();
   const bool share = a.share_all || *saved >= a.gain;
   if (!share) for (u32 g = threadIdx.x; g < a.n_groups; g += NT) view[a.n_seqs + g] = SharedView{0, 0, -1, 0, 0};
+  u32 before[EACH] = {};
+  if (share && *gaps) {                              // members' queries before every sequence: sums over 1, 2, 4 .. sequences
+    u32 *sum = gaps + 1, *next = sum + PAGED_MAX_SEQS;
 #pragma unroll
-  for (u32 j = 0; j < (PAGED_MAX_SEQS + NT - 1) / NT; ++j) {
+    for (u32 j = 0; j < EACH; ++j)
+      if (threadIdx.x + j * NT < a.n_seqs) sum[threadIdx.x + j * NT] = group[j] == NO_GROUP ? 0u : v[j].n;
+    __syncthreads();
+    for (u32 step = 1; step < a.n_seqs; step *= 2) {
+      for (u32 s = threadIdx.x; s < a.n_seqs; s += NT) next[s] = sum[s] + (s >= step ? sum[s - step] : 0u);
+      __syncthreads();
+      u32* const x = sum;
+      sum = next; next = x;
+    }
+#pragma unroll
+    for (u32 j = 0; j < EACH; ++j) {
+      const u32 s = threadIdx.x + j * NT;
+      if (s && s < a.n_seqs) before[j] = sum[s - 1];
+    }
+  }
+#pragma unroll
+  for (u32 j = 0; j < EACH; ++j) {
     const u32 s = threadIdx.x + j * NT, g = group[j];
     if (s >= a.n_seqs) continue;
     const bool in = share && g != NO_GROUP && view[a.n_seqs + g].n != 0;
-    view[s] = SharedView{v[j].t0, v[j].n, v[j].pos0, in ? keys[g] : 0u, g};
+    view[s] = SharedView{v[j].t0, v[j].n, v[j].pos0, in ? keys[g] : 0u, (in ? g : 0u) + PAGED_MAX_SEQS * before[j]};
   }
   __syncthreads();
 }
 
 // token of query k of a group, and which of a group's queries is query k of a sequence of its
-__device__ __forceinline__ u32 group_token(const SharedArgs& a, const SharedView* view, const SharedView& group, u32 k) { return group.t0 + k; }
-__device__ __forceinline__ u32 member_query(const SharedArgs& a, const SharedView* view, const SharedView& group, const SharedView& v, u32 k) { return v.t0 + k - group.t0; }
+__device__ __forceinline__ u32 group_token(const SharedArgs& a, const SharedView* view, const SharedView& group, u32 k) {
+  if (!group.gaps()) return group.t0 + k;
+  u32 s = group.row();                               // the last sequence with so many of the group's queries before it, or fewer
+  const u32 base = view[s].before();
+  for (u32 step = PAGED_MAX_SEQS / 2; step; step >>= 1) if (s + step < a.n_seqs && view[s + step].before() - base <= k) s += step;
+  return view[s].t0 + k - (view[s].before() - base);
+}
+__device__ __forceinline__ u32 member_query(const SharedArgs& a, const SharedView* view, const SharedView& group, const SharedView& v, u32 k) {
+  return k + (group.gaps() ? v.before() - view[group.row()].before() : v.t0 - group.t0);
+}
 // the rows of results to be joined, of every query head: how many, and that of a view's query k
 __host__ __device__ __forceinline__ u32 rows_of_call(const SharedArgs& a) { return a.n_tokens; }
 __device__ __forceinline__ u32 row_index(const SharedArgs& a, const SharedView& v, u32 index, u32 k) { return v.t0 + k; }
@@ -183,7 +225,7 @@ __device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqVie
   return max(1u, seen_tiles<16>(a, v.pos0, v.pos0 + (i32)v.n - 1).n);
 }
 __device__ __forceinline__ u32 short_unit_count(const SharedArgs& a, const SharedView& v, bool group) {
-  if (!v.n || v.n * a.G > a.short_rows) return 0;
+  if (!v.n || v.n * a.G > a.short_rows || (group && v.gaps())) return 0;
   return max(1u, seen_tiles<16>(a, v.pos0, group ? v.pos0 : v.pos0 + (i32)v.n - 1, v.first).n);
 }
 template <typename View>
@@ -210,7 +252,7 @@ __device__ __forceinline__ PromptItem flat_piece(const SharedArgs& a, const Shar
   it.g = head;
   it.r0 = item * flat_rows(a);
   it.rows = min(flat_rows(a), v.n * a.G - it.r0);
-  it.t0 = v.t0; it.p0 = it.p1 = v.pos0; it.lo = 0; it.row = v.row;
+  it.t0 = v.t0; it.p0 = it.p1 = v.pos0; it.lo = 0; it.row = v.row();
   return it;
 }
 
@@ -253,7 +295,7 @@ __device__ __forceinline__ JoinToken join_token(const SharedArgs& a, const Share
       const SharedView x = view[a.n_seqs + v.group()];
       const u32 k = member_query(a, view, x, v, t - v.t0), r = k * a.G;
       j.rows[0] = row_index(a, x, a.n_seqs + v.group(), k);
-      if (k < x.n && flat_units(a, x)) {           // (cu_seqlens that decrease may put a token outside its group)
+      if (flat_units(a, x)) {
         const FlatShape f = flat_shape(a, x);
         const u32 item = r / flat_rows(a);
         j.units[0] = flat[v.group()] + item * (FLAT_STEP * f.steps + f.lead) + f.lead; j.units[1] = f.all(); j.units[2] = f.units(item) - f.lead;

@@ -160,7 +160,7 @@ __device__ __forceinline__ void shared_attention(const SharedArgs& args, PagedSh
       const bool group = s >= a.n_seqs;
       sh.s.pos0[s] = v[j].pos0;
       sh.s.n[s] = short_unit_count(a, v[j], group) ? (unsigned char)v[j].n : (unsigned char)0;
-      sh.s.link[s] = group || v[j].first ? (uint16_t)v[j].row : (uint16_t)NO_GROUP;
+      sh.s.link[s] = group ? (uint16_t)v[j].row() : v[j].first ? (uint16_t)v[j].group() : (uint16_t)NO_GROUP;
     }
     __syncthreads();
     paged_short<HD, BITS, CT, SHORT_AHEAD(HD, BITS, CT), PAGED_WAVES>(a, sh.s, wg, nwg);

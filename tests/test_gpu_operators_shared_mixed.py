@@ -1,0 +1,67 @@
+"""Attention of groups in batches that hold other sequences as well: between the members of a group, beside the groups, and with lengths that do not fit."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_07609_amd as B
+from tests.test_gpu_operators import check_attention, dev, no_error_of_earlier_tests  # noqa: F401
+from tests.test_gpu_operators_shared import check, make_groups, run_shared
+from tests.test_shared_plan import DECREASING
+
+pytestmark = pytest.mark.gpu
+
+HEADS = [(64, 6, 2), (128, 4, 1), (64, 33, 1)]
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("hd, nq, nkv", HEADS)
+@pytest.mark.parametrize("groups", [
+    [(130, [(140, 1), (500, 300), (141, 4)])],                                           # a prompt between the only two members
+    [(130, [(500, 300), (140, 2), (100, 30), (150, 1), (20, 20), (135, 3), (430, 280)])],
+    [(200, [(201 + i, 1) if i % 7 else (400, 270 if i % 2 else 150) for i in range(1, 40)])],      # many, with some that have many queries
+    [(128, [(129 + i, 1 + i % 3) for i in range(25)] + [(90, 2)] + [(140, 12)] * 9), (70, [(75, 1), (60, 1), (90, 5)])],
+    [(64, [(70, 1), (66, 3), (20, 1)]), (0, [(33, 2)]), (192, [(200, 2), (0, 1), (0, 0), (194, 1)])],
+])
+def test_sequences_that_may_not_share_between_members(groups, hd, nq, nkv, bits):
+    check(groups, nq, nkv, hd, bits, seed=21)
+
+
+def test_many_sequences_between_members():
+    check([(64, [(66, 1) if i % 11 == 0 else (40, 1) for i in range(700)]), (64, [(200, 1)] + [(60, 2)] * 300 + [(70, 2)])], 2, 1, 64, 16, seed=22)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("hd, nq, nkv", HEADS)
+@pytest.mark.parametrize("times", [1, 30])
+@pytest.mark.parametrize("cu, lens, queries", DECREASING)
+def test_decreasing_tokens_inside_a_group_write_nothing_else(cu, lens, queries, times, hd, nq, nkv, bits):
+    """Results are not defined then, but rows of no sequence and what lies around the workspace stay as they are."""
+    more = 2 * (times - 1)
+    cu = [2 * i for i in range(times - 1)] + [more + x for x in cu]
+    lens = [140] * (times - 1) + lens
+    (cache, c, tables, _, _, q), starts, shared, _ = make_groups([(128, [(200, 1)] * len(lens))], nq, nkv, hd, bits, seed=23)
+    T = max(cu) + 2
+    q = dev((np.random.default_rng(24).standard_normal((T, nq, hd)) / np.sqrt(hd)).astype(np.float16))
+    out = torch.full((T + 2, nq, hd), 9.0, dtype=torch.float16, device="cuda")
+    n = B.shared_attention_workspace_bytes(nq, cache, len(lens), 1, T, 20)
+    work = torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    work[:8192] = 0
+    B.shared_attention(q, cache, dev(tables), dev(np.int32(lens)), dev(np.int32(cu)), dev(starts), dev(shared), out[:T], work[:n], max_q=20, share_all=True)
+    assert (out[max(cu):] == 9.0).all() and (work[n:] == 0xA5).all() and not work[:8192].any()
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("members", [2, 40])
+def test_context_lengths_that_do_not_fit(members, bits):
+    """Contexts beyond the table's width end there, negative ones are empty; the groups' tokens are in order."""
+    b, starts, shared, max_q = make_groups([(128, [(140, 1)] * members), (70, [(80, 2), (75, 1)])], 4, 2, 64, bits, seed=25, extra_rows=2)
+    cache, c, tables, lens, cu, q = b
+    given, seen = lens.copy(), lens.copy()
+    for s, n in ((0, 2 ** 31 - 1), (1, -5), (members, -2 ** 31), (members + 1, 2 ** 31 - 1)):
+        given[s] = n
+        seen[s] = tables.shape[1] * 16 if n > 0 else 0
+    for s in (0, members + 1):                         # (blocks for all of it)
+        tables[s, (lens[s] + 15) // 16:] = tables[s, 0]
+    got = run_shared((cache, c, tables, given, cu, q), starts, shared, max_q)
+    check_attention(got, cache, c, tables, seen, cu, q)

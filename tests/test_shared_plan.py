@@ -115,7 +115,11 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
     if (v.first && !(parts > 1 && prompt_items(a, v)))
       for (u32 k = 0; k < v.n; ++k) for (u32 h = 0; h < a.nkv; ++h) RULE(wrote(1, v, s, k, h));
   }
-  // the join
+  // the join (groups that decrease may have sequences between one another's, cu_seqlens that do may have a token in two sequences: what comes out is not defined then, and
+  // only where it is written and read is looked at)
+  bool ascending = true, groups_ascending = true;
+  for (u32 s = 0; s < a.n_seqs; ++s) ascending &= a.cu[s] >= 0 && a.cu[s] <= a.cu[s + 1];
+  for (u32 g = 0; g < a.n_groups; ++g) groups_ascending &= a.starts[g] <= a.starts[g + 1];
   std::vector<u32> joined(a.n_seqs);
   for (u32 t = 0; t < a.n_tokens; ++t) {
     const JoinToken j = join_token(a, view.data(), pre.data(), flat.data(), parts, t);
@@ -123,7 +127,7 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
     u32 s = 0;
     while (s < a.n_seqs && !(view[s].t0 <= t && t - view[s].t0 < view[s].n)) ++s;
     RULE(s < a.n_seqs);
-    bool one = true;                                 // (cu_seqlens that decrease may have a token in two sequences)
+    bool one = groups_ascending;
     for (u32 o = s + 1; o < a.n_seqs; ++o) if (view[o].t0 <= t && t - view[o].t0 < view[o].n) one = false;
     ++joined[s];
     const SharedView& v = view[s];
@@ -162,8 +166,6 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
       } else if (int rc = row(1, s, query)) return rc;
     }
   }
-  bool ascending = true;
-  for (u32 s = 0; s < a.n_seqs; ++s) ascending &= a.cu[s] >= 0 && a.cu[s] <= a.cu[s + 1];
   for (u32 s = 0; s < a.n_seqs && ascending; ++s)
     RULE(joined[s] == (view[s].first || (parts > 1 && prompt_items(a, view[s])) ? view[s].n : 0u));
   return 0;
@@ -230,3 +232,58 @@ def test_every_row_is_written_where_the_join_reads_it(plan, nq, nkv, hd, bits, n
             continue
         # (a sequence in no group behind its predecessor's: in that one's range of sequences, with blocks that need not agree)
         plan(*batch(seqs), shared, nq, nkv, hd, bits, nwg=nwg, share_all=share_all, window=int(rng.choice([0, 0, 0, 500])))
+
+
+@pytest.mark.parametrize("nq, nkv, hd, bits", HEADS)
+def test_lengths_groups_and_tokens_that_do_not_fit(plan, nq, nkv, hd, bits):
+    """Numbers that come from device memory may be anything: nothing is read or written outside of the call's tensors then."""
+    for seed in range(300):
+        rng = np.random.default_rng(1000 + seed)
+        S, G = int(rng.integers(1, 60)), int(rng.integers(1, 6))
+        any_ = lambda n, lo, hi: np.where(rng.random(n) < 0.1, rng.choice([-2 ** 31, -1, 2 ** 31 - 1], n), rng.integers(lo, hi, n))      # noqa: E731
+        cu = np.where(rng.random(S + 1) < 0.7, np.sort(rng.integers(0, 200, S + 1)), any_(S + 1, 0, 200))
+        plan(cu, any_(S, 0, 3000), any_(G + 1, 0, S + 1), any_(G, 0, 1500), nq, nkv, hd, bits, max_q=int(rng.integers(1, 90)), n_tokens=200, max_blocks=190)
+
+
+# cu_seqlens that decrease between members of one group of (context, queries) behind 128 shared tokens; the queries of the group that is formed all the same (0: none is)
+DECREASING = [
+    ([4, 6, 9, 5, 7], [140, 141, 130, 139], 0),                          # more queries than tokens between the first and the last one
+    ([0, 2, 20, 22, 10, 12], [140, 100, 135, 130, 200], 6),              # one that may not share between them, then an unused one
+    ([0, 1, 3, 5, 3, 5], [140, 100, 135, 130, 200], 5),                  # two members with the same tokens
+    ([10, 12, 2, 4, 6], [140, 130, 150, 160], 0),                        # the first member's tokens behind the others'
+]
+
+
+@pytest.mark.parametrize("cu, lens, queries", DECREASING)
+@pytest.mark.parametrize("times", [1, 30])
+@pytest.mark.parametrize("nq, nkv, hd, bits", HEADS)
+def test_decreasing_tokens_inside_a_group(plan, nq, nkv, hd, bits, times, cu, lens, queries):
+    """Alone and as one of many members, the others ahead of it."""
+    more = 2 * (times - 1)
+    cu = [2 * i for i in range(times - 1)] + [more + x for x in cu]
+    got = plan(cu, [140] * (times - 1) + lens, [0, len(cu) - 1], [128], nq, nkv, hd, bits, n_tokens=max(cu) + 2, max_blocks=16)[1]
+    if times == 1:
+        assert got == [queries]
+
+
+@pytest.mark.parametrize("nq, nkv, hd, bits", HEADS)
+@pytest.mark.parametrize("members, queries", [(24, 1), (64, 1), (150, 1), (30, 3)])
+def test_a_sequence_that_may_not_share_takes_nothing_from_its_neighbours(plan, nq, nkv, hd, bits, members, queries):
+    """A chunk of a prompt, and a sequence whose context lies within the shared tokens: the group is the same wherever in its range they stand."""
+    shared, group = 6000, [(6000 + queries + 7 * i, queries, 0) for i in range(members)]
+    alien = [(9000, 3000, 0), (500, 2, 0)]
+    behind = plan(*batch(group + alien), [shared], nq, nkv, hd, bits)
+    assert behind[1] == [members * queries] and behind[0] == [shared // 64 * 64] * members + [0, 0]
+    for at in (0, 1, members // 2, members - 1):
+        first, n, of_call = plan(*batch(group[:at] + alien + group[at:]), [shared], nq, nkv, hd, bits)
+        assert n == behind[1] and first == [shared // 64 * 64] * at + [0, 0] + [shared // 64 * 64] * (members - at), at
+
+
+def test_units_at_the_largest_sizes(plan):
+    """A chunk of 131072 queries among 4 M shared tokens between two members, 8 kv heads: with its rows the units would not fit 32 bits. Then as many members as there may be."""
+    long = 1 << 22
+    assert plan(*batch([(long + 1, 1, 0), (long, 131072, 0), (long + 5, 1, 0)]), [long])[1] == [2]
+    members = [(4 * 64 + 63, 63, 0)] * 1000
+    assert plan(*batch(members), [4 * 64], nq=32, nkv=8, max_blocks=260000)[1] == [63000]
+    deep = (1 << 31) // (1001 * 8) - 1                   # blocks of each
+    assert plan(*batch([(deep * 16 - 1, 7, 0)] * 1000), [deep * 16 - 64], nq=264, nkv=8, max_blocks=deep)[1] == [7000]
