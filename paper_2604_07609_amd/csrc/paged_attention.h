@@ -955,9 +955,9 @@ template <int N> __device__ __forceinline__ void wait_dma() { asm volatile("s_wa
 __device__ __forceinline__ float* own_parts(const PagedArgs& a) { return a.prompt_part; }
 __device__ __forceinline__ float* own_parts(const SharedArgs& a) { return a.own_part; }
 // FLAT: the groups' shared keys in place of prompts, workgroup wg's run of them. All rows see all keys, so what is done for masks falls away, but
-// for blocks outside the cache.
+// for blocks outside the cache. cut_for: workgroups that few items' keys are cut into parts for, where those are not all (nwg)
 template <int HD, int BITS, bool FLAT = false, typename A>
-__device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u32 wg, u32 nwg, bool behind_short, FlatRun run = FlatRun{0, 0}) {
+__device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u32 wg, u32 nwg, bool behind_short, FlatRun run = FlatRun{0, 0}, u32 cut_for = 0) {
   constexpr bool SHARED = is_shared<A>;
   constexpr int CT = PROMPT_CT;
   constexpr u32 BLK = 16 * HD * 2, NB = 4, STAGE = 2 * NB * BLK, NS = BITS == 4 ? 2 : (PROMPT_RING / STAGE > 6 ? 6 : PROMPT_RING / STAGE), TPW = BLK / 1024;
@@ -967,7 +967,7 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
       sh.view[s] = seq_view(a, s);
       return prompt_items(a, sh.view[s]);
     });
-  const u32 items = FLAT ? 0u : (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]) * a.nkv, parts = FLAT ? 1u : prompt_parts(a, items, nwg), total = FLAT ? run.end : items * parts;
+  const u32 items = FLAT ? 0u : (u32)__builtin_amdgcn_readfirstlane(sh.pre[a.n_seqs]) * a.nkv, parts = FLAT ? 1u : prompt_parts(a, items, cut_for ? cut_for : nwg), total = FLAT ? run.end : items * parts;
   u32* const ctr = a.ctr;
   const u32 lds0 = (u32)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sh.ring;
   // fetching halves: waves 0-3 the K of a block each, waves 4-7 the V (places in LDS: attn_prompt)

@@ -261,18 +261,23 @@ __device__ __forceinline__ void view_units(const SharedArgs& a, const SharedView
   if (group) v[1] = flat_units(a, x); else v[0] = prompt_items(a, x);
   const u32 tiles = short_unit_count(a, x, group);
   v[2] = (tiles ? tiles + FEW_PAIR : 0u) * a.nkv;
-  // (a time to go by, and that there is some: held to a second's, so that 1024 of them stay within 32 bits)
-  if (v[0]) v[3] = (u32)min((u64)v[0] * (FLAT_STEP * seen_tiles<64>(a, x.pos0, x.pos0 + (i32)x.n - 1, x.first).n + a.lead) * a.nkv, (u64)1 << 21);
+  // (a time to go by, and that there is some: an item's, in the middle between the first one's and the last one's, held to a second's, so that 1024 of them stay within 32 bits)
+  if (v[0]) {
+    const i32 p1 = x.pos0 + (i32)x.n - 1, some = (i32)min(x.n, PROMPT_ROWS / a.G) - 1;
+    const u32 steps = seen_tiles<64>(a, x.pos0, x.pos0 + some, x.first).n + seen_tiles<64>(a, p1 - some, p1, x.first).n;
+    v[3] = (u32)min((u64)v[0] * (FLAT_STEP * steps / 2 + a.lead) * a.nkv, (u64)1 << 21);
+  }
 }
 
 // The work of a call with groups, by every workgroup all the same: views, who has the groups' shared keys and who the rest. Then notes for the join.
 struct SharedWork { u32 flat_wgs, quota; bool few, prompts; };
-// Workgroups for the groups' shared keys and for the rest, by their estimated times, and the units of a run of the former
+// Workgroups for the groups' shared keys and for the rest, by their estimated times, and the units of a run of the former. Where there are prompts, whose items come from a counter, the former
+// take some of them at their runs' end, so one too many loses nothing
 __device__ __forceinline__ SharedWork deal_out(const SharedArgs& a, u32 units, u32 tiles, u32 prompts, u32 nwg) {
   SharedWork r;
   r.few = tiles != 0; r.prompts = prompts != 0;
   const float flat = (float)units, rest = a.few_cost * (float)tiles + (float)prompts;
-  r.flat_wgs = !units ? 0u : rest == 0.f ? nwg : min(nwg - 1, max(1u, (u32)((float)nwg * flat / (flat + rest) + 0.5f)));
+  r.flat_wgs = !units ? 0u : rest == 0.f ? nwg : min(nwg - 1, max(1u, (u32)((float)nwg * flat / (flat + rest) + (prompts ? 1.f : 0.5f))));
   r.quota = r.flat_wgs ? (units + r.flat_wgs - 1) / r.flat_wgs : 1u;
   return r;
 }

@@ -133,8 +133,9 @@ __device__ __forceinline__ SharedArgs fresh_args() {
 // A call with groups. A row's keys are its group's and its own: softmax((s1, s2)) v is joined from each part's maximum m, sum l and output o about m, by
 // o = (2^(m1-M) o1 + 2^(m2-M) o2) / (2^(m1-M) l1 + 2^(m2-M) l2). With n members of g rows each the shared keys are read once and not n times, and are products of n g rows:
 // what was bound by bytes becomes bound by products, while the members' own keys stay bound by bytes. So some workgroups have the groups' shared keys, others at the same time
-// the tiles of few rows and then the prompts, as many each as their estimated times ask for (one after the other on all workgroups: 158 us, so 99, for 253 sequences
-// behind 8200 tokens with 17 to 1000 of their own; bytes of all keys that are there 58 us, every sequence by itself 1000).
+// the tiles of few rows, as many each as their estimated times ask for, and whoever is done takes the prompts' items (with one run of all shared keys, and no item behind it, 32 sequences behind
+// 4000 tokens beside a prompt of 8192 took 737 us, so 591, every sequence by itself 628). One after the other on all workgroups: 158 us, so 99, for 253 sequences
+// behind 8200 tokens with 17 to 1000 of their own; bytes of all keys that are there 58 us, every sequence by itself 1000.
 // Of a call's time 3 to 5 us are the views and sums, 4 to 9 the join (a kernel of its own: results of other workgroups are in memory behind it), a workgroup's start and end 5.
 template <int HD, int BITS, int CT>
 __device__ __forceinline__ void shared_attention(const SharedArgs& args, PagedShared<HD, CT, SharedArgs>& sh, u32 wg, u32 nwg) {
@@ -144,10 +145,7 @@ __device__ __forceinline__ void shared_attention(const SharedArgs& args, PagedSh
     const SharedArgs a = fresh_args();
     const u32 units = (u32)__builtin_amdgcn_readfirstlane(sh.p.flat[a.n_groups]), from = min(wg * work.quota, units);
     paged_prompt<HD, BITS, true>(a, sh.p, wg, work.flat_wgs, false, FlatRun{from, min(from + work.quota, units)});
-    return;
-  }
-  wg -= work.flat_wgs; nwg -= work.flat_wgs;
-  if (work.few) {
+  } else if (work.few) {
     const SharedArgs a = fresh_args();
     SharedView v[PAGED_MAX_SEQS / NT];
 #pragma unroll
@@ -163,13 +161,11 @@ __device__ __forceinline__ void shared_attention(const SharedArgs& args, PagedSh
       sh.s.link[s] = group ? (uint16_t)v[j].row() : v[j].first ? (uint16_t)v[j].group() : (uint16_t)NO_GROUP;
     }
     __syncthreads();
-    paged_short<HD, BITS, CT, SHORT_AHEAD(HD, BITS, CT), PAGED_WAVES>(a, sh.s, wg, nwg);
+    paged_short<HD, BITS, CT, SHORT_AHEAD(HD, BITS, CT), PAGED_WAVES>(a, sh.s, wg - work.flat_wgs, nwg - work.flat_wgs);
   }
   if (!work.prompts) return;
   const SharedArgs a = fresh_args();
-  if (work.few) {
-    __syncthreads();
-    views_and_sums(a, sh.p);
-  }
-  paged_prompt<HD, BITS>(a, sh.p, wg, nwg, true);
+  __syncthreads();
+  if (work.few && wg >= work.flat_wgs) views_and_sums(a, sh.p);
+  paged_prompt<HD, BITS>(a, sh.p, wg, nwg, true, FlatRun{0, 0}, nwg - work.flat_wgs);
 }

@@ -65,6 +65,9 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
   const SharedWork w = deal_out(a, (u32)sums[1], (u32)sums[2], (u32)sums[3], c->nwg);
   RULE(w.flat_wgs <= c->nwg && (w.flat_wgs < c->nwg || !(w.few || w.prompts)) && (w.flat_wgs > 0) == (sums[1] > 0));
   RULE((u64)w.quota * std::max(w.flat_wgs, 1u) >= sums[1]);
+  // (beside prompts, whose items whoever is free takes, no run of the shared keys is longer than everyone's share of all the work)
+  const double rest = a.few_cost * (double)sums[2] + (double)sums[3];
+  RULE(!w.flat_wgs || !w.prompts || w.flat_wgs == c->nwg - 1 || (double)sums[1] / w.flat_wgs <= 1.001 * (sums[1] + rest) / c->nwg);
   const u32 items = pre[a.n_seqs] * a.nkv, parts = prompt_parts(a, items, c->nwg - w.flat_wgs);
   RULE(parts == 1 || (u64)items * parts <= c->nwg);
   for (u32 s = 0; s < a.n_seqs; ++s) first[s] = view[s].first;
@@ -277,6 +280,19 @@ def test_a_sequence_that_may_not_share_takes_nothing_from_its_neighbours(plan, n
     for at in (0, 1, members // 2, members - 1):
         first, n, of_call = plan(*batch(group[:at] + alien + group[at:]), [shared], nq, nkv, hd, bits)
         assert n == behind[1] and first == [shared // 64 * 64] * at + [0, 0] + [shared // 64 * 64] * (members - at), at
+
+
+@pytest.mark.parametrize("nq, nkv, hd, bits", HEADS)
+@pytest.mark.parametrize("context, queries", [(2000, 2000), (9000, 4000), (8192, 8192), (40000, 512)])
+def test_prompts_beside_groups(plan, nq, nkv, hd, bits, context, queries):
+    """Units of a prompt's items: those of the steps that each of them has, not of the longest one's; and no long run of shared keys beside it (a rule of the harness)."""
+    G = nq // nkv
+    of_call = plan(*batch([(4100 + i, 1, 0) for i in range(32)] + [(context, queries, None)]), [4000], nq, nkv, hd, bits)[2]
+    rows = [min(256, queries * G - r) + r for r in range(0, queries * G, 256)]
+    steps = [(context - queries + (r - 1) // G) // 64 + 1 for r in rows]
+    want = sum(4 * s + 13 for s in steps) * nkv
+    assert want < 2 ** 21 and abs(of_call[4] - want) < 0.05 * want + 6 * len(steps) * nkv
+    assert of_call[0] >= 1
 
 
 def test_units_at_the_largest_sizes(plan):
