@@ -48,6 +48,7 @@ struct SharedArgs : PagedArgs {
   u32 lead;                       // time of an item of the groups' shared keys beside its steps, in units (FlatShape)
   float few_cost;                 // time of a tile of few rows on one compute unit, in units
   u32 gain;                       // units that all groups together must save for a kv head
+  float row_cost;                 // units that the rows of a member's token, to be joined, take for a kv head
   struct JoinToken* tokens;       // what is to be joined of every token, and behind them the units of a workgroup's run (FlatRun)
 };
 #define ROW_RESULT(HD) ((HD) + 4u)                   // maximum, sum, two unused, output
@@ -164,7 +165,7 @@ __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, Sha
       const u32 n = queries[g], tiles = keys[g] / 16;
       const bool apart = n < t1[g] - t0[g];
       const float together = n * a.G <= a.short_rows && !apart ? a.few_cost * (float)(tiles + FEW_PAIR) : (float)flat_shape(a, n * a.G, keys[g]).all();
-      const float gain = (float)members[g] * (float)tiles * a.few_cost - together;
+      const float gain = (float)members[g] * (float)tiles * a.few_cost - together - a.row_cost * (float)n;
       if (a.share_all || gain > SHARED_GAIN) {
         x = {t0[g], n, (i32)keys[g] - 1, 0, from[g] + (apart ? PAGED_MAX_SEQS : 0u)};
         if (apart) atomicOr(gaps, 1u);
@@ -330,7 +331,9 @@ __host__ inline void shared_costs(SharedArgs& p, u32 hd, u32 bits, u32 ct, u32 n
   p.lead = hd == 128 ? 13 : halves ? 18 : 9;
   p.least = halves ? 2 : FLAT_LIGHT;
   p.few_cost = (halves ? 0.6f : 0.26f) * (ct == 1 ? 1.f : 1.5f);
-  // (what sharing must gain on every compute unit: 8 us for the groups' starts and the join, and what rows' results take to memory and back. 64 sequences in
+  // (what sharing must gain on every compute unit: 8 us for the groups' starts and the join, and what the members' rows take to memory and back: of other tokens nothing is joined. 64 sequences in
   // 4 bits, 1024 shared keys: 26.5 us, 27.8 apart; 253 behind 64: 78.5, 70 apart; 40 groups of 4, heads of 64, behind 64 and 256: 29.8, 37, apart 23.7, 40.4)
-  p.gain = (u32)((8.f + (float)p.n_tokens * (float)p.nq * (float)(16 * ROW_RESULT(hd)) * 2e-7f) / unit * (float)n_cu / (float)p.nkv);
+  const float units = (float)n_cu / (float)p.nkv / unit;      // of a us, for a kv head
+  p.gain = (u32)(8.f * units);
+  p.row_cost = (float)p.nq * (float)(16 * ROW_RESULT(hd)) * 2e-7f * units;
 }

@@ -269,17 +269,20 @@ def test_decreasing_tokens_inside_a_group(plan, nq, nkv, hd, bits, times, cu, le
         assert got == [queries]
 
 
+@pytest.mark.parametrize("share_all", [0, 1])
 @pytest.mark.parametrize("nq, nkv, hd, bits", HEADS)
 @pytest.mark.parametrize("members, queries", [(24, 1), (64, 1), (150, 1), (30, 3)])
-def test_a_sequence_that_may_not_share_takes_nothing_from_its_neighbours(plan, nq, nkv, hd, bits, members, queries):
+def test_a_sequence_that_may_not_share_takes_nothing_from_its_neighbours(plan, nq, nkv, hd, bits, members, queries, share_all):
     """A chunk of a prompt, and a sequence whose context lies within the shared tokens: the group is the same wherever in its range they stand."""
     shared, group = 6000, [(6000 + queries + 7 * i, queries, 0) for i in range(members)]
     alien = [(9000, 3000, 0), (500, 2, 0)]
-    behind = plan(*batch(group + alien), [shared], nq, nkv, hd, bits)
-    assert behind[1] == [members * queries] and behind[0] == [shared // 64 * 64] * members + [0, 0]
+    behind = plan(*batch(group + alien), [shared], nq, nkv, hd, bits, share_all=share_all)
+    keys = behind[0][0]                                # (0 with one kv head and few members: too little work to gain by)
+    assert behind[1] == [members * queries if keys else 0] and behind[0] == [keys] * members + [0, 0]
+    assert keys == shared // 64 * 64 or (nkv == 1 and not share_all)
     for at in (0, 1, members // 2, members - 1):
-        first, n, of_call = plan(*batch(group[:at] + alien + group[at:]), [shared], nq, nkv, hd, bits)
-        assert n == behind[1] and first == [shared // 64 * 64] * at + [0, 0] + [shared // 64 * 64] * (members - at), at
+        first, n, of_call = plan(*batch(group[:at] + alien + group[at:]), [shared], nq, nkv, hd, bits, share_all=share_all)
+        assert n == behind[1] and first == [keys] * at + [0, 0] + [keys] * (members - at), at
 
 
 @pytest.mark.parametrize("nq, nkv, hd, bits", HEADS)
@@ -293,6 +296,16 @@ def test_prompts_beside_groups(plan, nq, nkv, hd, bits, context, queries):
     want = sum(4 * s + 13 for s in steps) * nkv
     assert want < 2 ** 21 and abs(of_call[4] - want) < 0.05 * want + 6 * len(steps) * nkv
     assert of_call[0] >= 1
+
+
+@pytest.mark.parametrize("nq, nkv, hd, bits", HEADS)
+@pytest.mark.parametrize("members, shared", [(2, 70), (4, 1040), (16, 8000), (32, 4000), (64, 2000), (100, 300), (200, 64), (12, 500)])
+def test_whether_groups_share_does_not_depend_on_who_is_beside_them(plan, nq, nkv, hd, bits, members, shared):
+    """Prompts and sequences in no group are not joined, so they change nothing of what sharing gains."""
+    group = [(shared + 1 + i, 1, 0) for i in range(members)]
+    alone = plan(*batch(group), [shared], nq, nkv, hd, bits, share_all=0)
+    for beside in ([(2000, 2000, None)], [(8192, 8192, None)], [(1000 + i, 1, None) for i in range(100)]):
+        assert plan(*batch(group + beside), [shared], nq, nkv, hd, bits, share_all=0)[1] == alone[1]
 
 
 def test_units_at_the_largest_sizes(plan):
