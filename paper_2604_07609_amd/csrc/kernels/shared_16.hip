@@ -3,11 +3,10 @@
 
 #define SHARED_KERNEL(HD, BITS, CT)                                                                    \
   template <> __global__ void PAGED_BOUNDS k_shared_attention<HD, BITS, CT>(SharedArgs a) {            \
-    __shared__ PagedShared<HD, CT, SharedArgs> sh;                                                     \
+    __shared__ SharedKernelRoom<HD, CT> sh;                                                            \
     shared_attention<HD, BITS, CT>(a, sh, blockIdx.x, gridDim.x);                                      \
   }
-SHARED_KERNEL(64, 16, 1)
-SHARED_KERNEL(64, 16, SHORT_MORE(64))
+SHARED_KERNEL(64, 16, ANY_CT)
 SHARED_KERNEL(128, 16, 1)
 SHARED_KERNEL(128, 16, SHORT_MORE(128))
 

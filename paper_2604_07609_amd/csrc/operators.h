@@ -328,15 +328,14 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
 
 // ---- attention of groups --------------------------------------------------------------------------------------------------------
 struct SharedPlan {
-  u32 ct, n_splits;
+  u32 n_splits;
   u64 part_bytes, prompt_bytes, flat_bytes, row_bytes, token_bytes;
   u64 bytes(u32 n_cu) const { return paged_ctr_bytes(n_cu) + part_bytes + prompt_bytes + flat_bytes + row_bytes + token_bytes; }
 };
-static SharedPlan shared_plan(u32 hd, u32 bits, u32 nq, u32 nkv, u32 n_groups, u32 n_tokens, u32 max_q, u32 steps, u32 n_cu) {
+static SharedPlan shared_plan(u32 hd, u32 nq, u32 n_tokens, u32 steps, u32 n_cu) {
   SharedPlan p{};
-  p.ct = few_row_tiles(hd, bits, nq / nkv, n_tokens, n_groups, max_q);
   p.n_splits = std::max(1u, steps / 4);          // (parts of 256 keys at least)
-  p.part_bytes = short_floats(n_cu, hd, p.ct) * 4;
+  p.part_bytes = short_floats(n_cu, hd, SHORT_MORE(hd)) * 4;
   p.prompt_bytes = (u64)n_cu * PROMPT_SLOT(hd) * 4;
   p.flat_bytes = 2 * p.prompt_bytes;
   p.row_bytes = 2ull * n_tokens * nq * ROW_RESULT(hd) * 4;
@@ -360,16 +359,16 @@ extern "C" int blink_shared_attention_workspace_bytes(int32_t device, const blin
   if (int rc = check_groups(*c, n_q_heads, n_seqs, n_groups, n_tokens)) return rc;
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  SharedPlan plan = shared_plan(c->head_dim, c->bits, n_q_heads, c->n_kv_heads, n_groups, n_tokens, max_q, 1, n_cu);
-  plan.part_bytes = short_floats(n_cu, c->head_dim, SHORT_MORE(c->head_dim)) * 4;
-  *bytes = std::max<u64>(*bytes, plan.bytes(n_cu));
+  *bytes = std::max<u64>(*bytes, shared_plan(c->head_dim, n_q_heads, n_tokens, 1, n_cu).bytes(n_cu));
   return BLINK_OK;
 }
 
 template <int HD, int BITS>
-static hipError_t launch_shared(const SharedArgs& args, u32 ct, u32 n_cu, hipStream_t st) {
+static hipError_t launch_shared(const SharedArgs& args, u32 n_cu, hipStream_t st) {
   constexpr u32 NT = 64 * PAGED_WAVES;
-  const hipError_t e = ct == 1 ? launch(k_shared_attention<HD, BITS, 1>, n_cu, NT, st, args) : launch(k_shared_attention<HD, BITS, SHORT_MORE(HD)>, n_cu, NT, st, args);
+  hipError_t e;
+  if constexpr (rows_by_mean(HD, BITS)) e = launch(k_shared_attention<HD, BITS, ANY_CT>, n_cu, NT, st, args);
+  else e = args.short_rows == 16 ? launch(k_shared_attention<HD, BITS, 1>, n_cu, NT, st, args) : launch(k_shared_attention<HD, BITS, SHORT_MORE(HD)>, n_cu, NT, st, args);
   const u64 waves = join_waves(HD, args.nq, args.n_tokens);
   return e == hipSuccess ? launch(k_shared_join<HD>, (u32)((waves * 64 + BLK_THREADS - 1) / BLK_THREADS), BLK_THREADS, st, args) : e;
 }
@@ -390,21 +389,21 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   if (!s->group_starts || !s->shared_lens || (u64)s->group_starts % 4 || (u64)s->shared_lens % 4) return fail(BLINK_ERR_INVAL, "group_starts or shared_lens is null or not aligned");
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  const SharedPlan plan = shared_plan(hd, a->cache.bits, a->n_q_heads, nkv, s->n_groups, a->n_tokens, a->max_q, key_steps(a), n_cu);
+  const SharedPlan plan = shared_plan(hd, a->n_q_heads, a->n_tokens, key_steps(a), n_cu);
   if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.bytes(n_cu))
     return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)plan.bytes(n_cu));
   OnDevice on(device);
   HIPCHK(on.err);
   SharedArgs p{};
-  fill_paged(p, a, scale2, 16 * plan.ct, plan.n_splits, n_cu);
+  fill_paged(p, a, scale2, 0, plan.n_splits, n_cu);
   p.own_part = p.part + plan.part_bytes / 4;
   p.prompt_part = p.own_part + plan.prompt_bytes / 4;
   p.rows = p.prompt_part + plan.flat_bytes / 4;
   p.tokens = (JoinToken*)(p.rows + plan.row_bytes / 4);
-  shared_costs(p, hd, a->cache.bits, plan.ct, n_cu);
+  shared_costs(p, hd, a->cache.bits, n_cu);
   p.n_groups = s->n_groups; p.share_all = s->share_all; p.starts = s->group_starts; p.shared = s->shared_lens;
   const hipStream_t st = (hipStream_t)stream;
-  HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_shared<64, 16>(p, plan.ct, n_cu, st) : launch_shared<64, 4>(p, plan.ct, n_cu, st))
-                  : (a->cache.bits == 16 ? launch_shared<128, 16>(p, plan.ct, n_cu, st) : launch_shared<128, 4>(p, plan.ct, n_cu, st)));
+  HIPCHK(hd == 64 ? (a->cache.bits == 16 ? launch_shared<64, 16>(p, n_cu, st) : launch_shared<64, 4>(p, n_cu, st))
+                  : (a->cache.bits == 16 ? launch_shared<128, 16>(p, n_cu, st) : launch_shared<128, 4>(p, n_cu, st)));
   return BLINK_OK;
 }

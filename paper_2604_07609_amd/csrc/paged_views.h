@@ -13,6 +13,8 @@
 #define FLAT_STEP 4u               // units of a step of the groups' shared keys, and of one of an item of 128 rows or less
 #define FLAT_LIGHT 3u
 #define SHARED_GAIN 4.f            // units that a group must save for a kv head: its start and end, two times, beside those of others
+#define FEW_MORE 1.5f              // time of a tile of few rows in an instance with more than one row tile, in those with one
+#define GROUPS_UNIT (1u << 18)     // (more than the queries of all members: 1023 times 255)
 #define FEW_PAIR 3u                // what a pair of a sequence and a kv head takes beside its tiles, in tiles (96 sequences with 5 to 300 keys of their own, in 4 bits: 88 us with 2, 81 with 3 and 4; 253 with 17 to 1000: 105 with none, 99 with 1 to 3)
 #define NO_GROUP 0xFFFFu
 
@@ -31,7 +33,7 @@ struct PagedArgs {
   u32 n_seqs, n_tokens, max_q;    // sequences; tokens of q and out; queries of a sequence that are looked at
   u32 window, sinks;
   float c;                        // scale of the scores * log2(e)
-  u32 short_rows;                 // sequences with at most so many rows are the short part's
+  u32 short_rows;                 // sequences with at most so many rows are the short part's (of a call with groups by shared_views, where rows_by_mean)
   u32 n_splits;                   // most parts of a prompt item's keys
   u32* ctr;                       // zeros between launches (paged_counters): next prompt item, workgroups done, then the short part's
   float *part, *prompt_part;      // partial results of the short and of the prompt part
@@ -46,7 +48,8 @@ struct SharedArgs : PagedArgs {
   float* own_part;                // parts of prompt items (prompt_part: of the groups' items)
   u32 least;                      // units of a step of a group of 32 rows or less in all (of others: FLAT_STEP, of items of 128 rows or less FLAT_LIGHT)
   u32 lead;                       // time of an item of the groups' shared keys beside its steps, in units (FlatShape)
-  float few_cost;                 // time of a tile of few rows on one compute unit, in units
+  u32 most_rows;                  // rows that the short part's registers hold
+  float few_cost;                 // time of a tile of few rows on one compute unit, in units, with one row tile (with more of them: FEW_MORE times that)
   u32 gain;                       // units that all groups together must save for a kv head
   float row_cost;                 // units that the rows of a member's token, to be joined, take for a kv head
   struct JoinToken* tokens;       // what is to be joined of every token, and behind them the units of a workgroup's run (FlatRun)
@@ -120,14 +123,25 @@ __device__ __forceinline__ u32 flat_units(const SharedArgs& a, const SharedView&
 // all its queries stand behind the shared keys and see every one of them, and all of these together take less time with the shared keys apart; and only if all groups together gain more than
 // what results that are joined take. A group's rows are those of its members, wherever in its range of sequences they stand. The shared keys are cut to a multiple of 64, what a step of the
 // prompt part takes. room: ROOM_WORDS of LDS.
-#define ROOM_WORDS (9 * PAGED_MAX_SEQS + 3)
-template <u32 NT>
-__device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, SharedView* view) {
-  constexpr u32 EACH = (PAGED_MAX_SEQS + NT - 1) / NT;
-  // of every group: first sequence, shared keys, then of its members: the first one, how many, their queries, first token and last one + 1
-  u32 *const starts = room, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const members = from + a.n_groups, *const queries = members + a.n_groups;
-  u32 *const t0 = queries + a.n_groups, *const t1 = t0 + a.n_groups, *const saved = t1 + a.n_groups, *const gaps = saved + 1;
-  if (threadIdx.x == 0) *saved = *gaps = 0;
+//
+// Row tiles of the few-row part (short_rows): more than one where a sequence needs them, and none needs more than it holds (beside a prompt 96 sequences with 5 drafts, 20 rows, take 149 us as prompt
+// items and 169 as two row tiles, in 4 bits 176 and 193), and where the groups' mean does: a step of a prompt item costs a group of few rows as much as one of 128, over 4 bits as one of 256. 40 groups
+// of up to four sequences with 9 queries, heads of 64: 67 us with the groups' keys as steps of prompt items, 52 to 57 as tiles of few rows; 16 groups of 8 behind 2000 and 8000 tokens, heads of 64: 41
+// and 90, so 32 and 72; heads of 128 over 4 bits: 52 and 132, so 40 and 68, and beside 100 sequences in no group 204 and 156. Over halves with heads of 128 the steps are as fast or faster (46 and
+// 117 us, as tiles 47 and 120; behind 500 tokens 31, 36), so there the host says what a call takes, by its longest run of queries, or by all tokens where those are few (shared_costs).
+// The mean is that of the groups that there are: lengths are known here only.
+#define SPREAD 32u                 // places of a sum that many lanes add to
+#define ROOM_WORDS (9 * PAGED_MAX_SEQS + 3 * SPREAD + 16)
+constexpr bool rows_by_mean(int hd, int bits) { return hd == 64 || bits == 4; }
+template <u32 NT, bool BY_MEAN>
+__device__ __forceinline__ void shared_views(SharedArgs& a, u32* room, SharedView* view) {
+  constexpr u32 EACH = (PAGED_MAX_SEQS + NT - 1) / NT, OPTIONS = BY_MEAN ? 2 : 1;
+  // gained[option], sizes: of all groups, in SPREAD places; whether some group has gaps, some sequence more than 16 rows that the few-row part holds, some more than that. Then of every
+  // group: first sequence, shared keys, and of its members: the first one, how many, their queries, first token and last one + 1
+  u32 *const gained = room, *const sizes = gained + 2 * SPREAD, *const gaps = sizes + SPREAD, *const some_rows = gaps + 1, *const many_rows = some_rows + 1;
+  u32 *const starts = gaps + 8, *const keys = starts + a.n_groups + 1, *const from = keys + a.n_groups, *const members = from + a.n_groups, *const queries = members + a.n_groups;
+  u32 *const t0 = queries + a.n_groups, *const t1 = t0 + a.n_groups, *const scratch = t1 + a.n_groups;
+  for (u32 i = threadIdx.x; i < 3 * SPREAD + 3; i += NT) room[i] = 0;
   for (u32 g = threadIdx.x; g <= a.n_groups; g += NT) {
     starts[g] = (u32)max(0, min(a.starts[g], (i32)a.n_seqs));
     if (g == a.n_groups) break;
@@ -144,7 +158,9 @@ __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, Sha
   for (u32 j = 0; j < EACH; ++j) {
     const u32 s = threadIdx.x + j * NT;
     group[j] = NO_GROUP;
-    if (s >= a.n_seqs || !a.n_groups || s < starts[0]) continue;
+    if (s >= a.n_seqs) continue;
+    if (BY_MEAN && v[j].n * a.G > 16) *(v[j].n * a.G > a.most_rows ? many_rows : some_rows) = 1;
+    if (!a.n_groups || s < starts[0]) continue;
     u32 g = 0;
     for (u32 step = 1u << (31 - __clz((int)a.n_groups)); step; step >>= 1) if (g + step < a.n_groups && starts[g + step] <= s) g += step;      // the last that begins here or before
     const i32 p1 = v[j].pos0 + (i32)v[j].n - 1;
@@ -158,28 +174,44 @@ __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, Sha
     group[j] = g;
   }
   __syncthreads();
+  // Every group for both numbers of row tiles, as long as the mean is not known: members[g] becomes the bits of those with which it shares
   for (u32 g = threadIdx.x; g < a.n_groups; g += NT) {
-    SharedView x = {0, 0, -1, 0, 0};
+    u32 shares = 0, which = 0;
     // (cu_seqlens that decrease may have the first member's tokens behind another one's, or a token in two members: then the rows from t0 on would not hold them, and there is no group)
     if (members[g] > 1 && view[from[g]].t0 == t0[g] && queries[g] <= t1[g] - t0[g]) {
       const u32 n = queries[g], tiles = keys[g] / 16;
       const bool apart = n < t1[g] - t0[g];
-      const float together = n * a.G <= a.short_rows && !apart ? a.few_cost * (float)(tiles + FEW_PAIR) : (float)flat_shape(a, n * a.G, keys[g]).all();
-      const float gain = (float)members[g] * (float)tiles * a.few_cost - together - a.row_cost * (float)n;
-      if (a.share_all || gain > SHARED_GAIN) {
-        x = {t0[g], n, (i32)keys[g] - 1, 0, from[g] + (apart ? PAGED_MAX_SEQS : 0u)};
-        if (apart) atomicOr(gaps, 1u);
-        if (!a.share_all) atomicAdd(saved, (u32)min(gain, 1e6f));      // (1024 times that is less than 2^32)
+      if (BY_MEAN) atomicAdd(sizes + g % SPREAD, GROUPS_UNIT + n);
+      for (u32 o = 0; o < OPTIONS; ++o) {
+        const u32 rows = BY_MEAN ? (o ? a.most_rows : 16u) : a.short_rows;
+        const float few_cost = a.few_cost * (rows > 16 ? FEW_MORE : 1.f);
+        const float together = n * a.G <= rows && !apart ? few_cost * (float)(tiles + FEW_PAIR) : (float)flat_shape(a, n * a.G, keys[g]).all();
+        const float gain = (float)members[g] * (float)tiles * few_cost - together - a.row_cost * (float)n;
+        if (!a.share_all && !(gain > SHARED_GAIN)) continue;
+        shares |= 1u << o;
+        if (!a.share_all) atomicAdd(gained + o * SPREAD + g % SPREAD, (u32)min(gain, 1e6f));      // (1024 times that is less than 2^32)
       }
+      which = from[g] + (apart ? PAGED_MAX_SEQS : 0u);
+      if (apart && shares) *gaps = 1;
     }
-    view[a.n_seqs + g] = x;
+    members[g] = shares;
+    view[a.n_seqs + g] = SharedView{t0[g], queries[g], (i32)keys[g] - 1, 0, which};
   }
   __syncthreads();
-  const bool share = a.share_all || *saved >= a.gain;
-  if (!share) for (u32 g = threadIdx.x; g < a.n_groups; g += NT) view[a.n_seqs + g] = SharedView{0, 0, -1, 0, 0};
+  u32 option = 0, all_gained = 0;
+  if (BY_MEAN) {
+    u32 all = 0;
+    for (u32 i = 0; i < SPREAD; ++i) all += sizes[i];
+    const u32 n = all / GROUPS_UNIT, mean = n ? (all % GROUPS_UNIT + n - 1) / n : 0u;
+    option = (*some_rows && !*many_rows) || (mean * a.G > 16 && mean * a.G <= a.most_rows) ? 1 : 0;
+    a.short_rows = option ? a.most_rows : 16u;
+  }
+  for (u32 i = 0; i < SPREAD; ++i) all_gained += gained[option * SPREAD + i];
+  const bool share = a.share_all || all_gained >= a.gain;
+  for (u32 g = threadIdx.x; g < a.n_groups; g += NT) if (!share || !(members[g] >> option & 1u)) view[a.n_seqs + g] = SharedView{0, 0, -1, 0, 0};
   u32 before[EACH] = {};
   if (share && *gaps) {                              // members' queries before every sequence: sums over 1, 2, 4 .. sequences
-    u32 *sum = gaps + 1, *next = sum + PAGED_MAX_SEQS;
+    u32 *sum = scratch, *next = sum + PAGED_MAX_SEQS;
 #pragma unroll
     for (u32 j = 0; j < EACH; ++j)
       if (threadIdx.x + j * NT < a.n_seqs) sum[threadIdx.x + j * NT] = group[j] == NO_GROUP ? 0u : v[j].n;
@@ -200,7 +232,7 @@ __device__ __forceinline__ void shared_views(const SharedArgs& a, u32* room, Sha
   for (u32 j = 0; j < EACH; ++j) {
     const u32 s = threadIdx.x + j * NT, g = group[j];
     if (s >= a.n_seqs) continue;
-    const bool in = share && g != NO_GROUP && view[a.n_seqs + g].n != 0;
+    const bool in = share && g != NO_GROUP && (members[g] >> option & 1u);
     view[s] = SharedView{v[j].t0, v[j].n, v[j].pos0, in ? keys[g] : 0u, (in ? g : 0u) + PAGED_MAX_SEQS * before[j]};
   }
   __syncthreads();
@@ -277,7 +309,7 @@ struct SharedWork { u32 flat_wgs, quota; bool few, prompts; };
 __device__ __forceinline__ SharedWork deal_out(const SharedArgs& a, u32 units, u32 tiles, u32 prompts, u32 nwg) {
   SharedWork r;
   r.few = tiles != 0; r.prompts = prompts != 0;
-  const float flat = (float)units, rest = a.few_cost * (float)tiles + (float)prompts;
+  const float flat = (float)units, rest = a.few_cost * (a.short_rows > 16 ? FEW_MORE : 1.f) * (float)tiles + (float)prompts;
   r.flat_wgs = !units ? 0u : rest == 0.f ? nwg : min(nwg - 1, max(1u, (u32)((float)nwg * flat / (flat + rest) + (prompts ? 1.f : 0.5f))));
   r.quota = r.flat_wgs ? (units + r.flat_wgs - 1) / r.flat_wgs : 1u;
   return r;
@@ -312,25 +344,18 @@ __device__ __forceinline__ JoinToken join_token(const SharedArgs& a, const Share
   return j;
 }
 
-// Row tiles of the few-row part: what the sequences with the most queries need or, where that takes all groups' rows,
-// these do, by their mean (lengths of groups are known on the device only): a step of a prompt item costs a group of few rows as much as one of 128, over 4 bits as one of 256.
-// 40 groups of up to four sequences with 9 queries, heads of 64: 67 us with the groups' keys as steps of prompt items, 52 as tiles of few rows; 16 groups of 8 behind 2000 and 8000 tokens, heads of 64:
-// 41 and 90, so 32 and 72; heads of 128 over 4 bits: 52 and 132, so 40 and 68. Over halves with heads of 128 the steps are as fast or faster (46 and 117 us, as tiles 47 and 120; behind 500 tokens 31, 36), so
-// there it is asked for only where all tokens' rows are few.
-__host__ inline u32 few_row_tiles(u32 hd, u32 bits, u32 G, u32 n_tokens, u32 n_groups, u32 max_q) {
-  const u32 most = 16u * SHORT_MORE(hd);
-  const u64 own = (u64)max_q * G, all = (hd == 64 || bits == 4 ? ((u64)n_tokens + n_groups - 1) / (n_groups ? n_groups : 1u) : (u64)n_tokens) * G;      // rows of a sequence; of a group, about
-  return (all <= most ? all > 16 : own > 16 && own <= most) ? SHORT_MORE(hd) : 1;
-}
 // Times on one compute unit, by which workgroups are dealt out. A unit: a quarter of a step of 256 rows, see FlatShape. Against units of half a step, with one for a step of 128 rows or less
 // (two over 4 bits): up to 96 sequences with 5 drafts 82 us, so 76 in 4 bits, 82 and 73 over halves; 12 groups of 70 120, 107; 200 sequences of heads of 64 71, 60; three groups of 30 52, 53.
 // 16 groups of 8 sequences, 32 rows each, 59, and with FLAT_LIGHT for them 63
-__host__ inline void shared_costs(SharedArgs& p, u32 hd, u32 bits, u32 ct, u32 n_cu) {
+__host__ inline void shared_costs(SharedArgs& p, u32 hd, u32 bits, u32 n_cu) {
   const bool halves = bits == 16;
   const float unit = hd == 128 ? (halves ? 0.47f : 0.56f) : (halves ? 0.38f : 0.49f);
   p.lead = hd == 128 ? 13 : halves ? 18 : 9;
   p.least = halves ? 2 : FLAT_LIGHT;
-  p.few_cost = (halves ? 0.6f : 0.26f) * (ct == 1 ? 1.f : 1.5f);
+  p.most_rows = 16 * SHORT_MORE(hd);
+  const u64 own = (u64)p.max_q * p.G, all = (u64)p.n_tokens * p.G;
+  p.short_rows = (all <= p.most_rows ? all > 16 : own > 16 && own <= p.most_rows) ? p.most_rows : 16u;
+  p.few_cost = halves ? 0.6f : 0.26f;
   // (what sharing must gain on every compute unit: 8 us for the groups' starts and the join, and what the members' rows take to memory and back: of other tokens nothing is joined. 64 sequences in
   // 4 bits, 1024 shared keys: 26.5 us, 27.8 apart; 253 behind 64: 78.5, 70 apart; 40 groups of 4, heads of 64, behind 64 and 256: 29.8, 37, apart 23.7, 40.4)
   const float units = (float)n_cu / (float)p.nkv / unit;      // of a us, for a kv head

@@ -14,10 +14,12 @@ __device__ __forceinline__ u32 wave_sums_dpp(u32 v) {
   return v;
 }
 // Views; items of the prompts before each sequence (pre) and units of the shared keys before each group (flat); sum[0]: cost of all tiles of few rows, sum[1]: of the prompts.
-__device__ __forceinline__ void views_and_sums(const SharedArgs& a, SharedRoom& sh) {
+template <bool BY_MEAN>
+__device__ __forceinline__ void views_and_sums(SharedArgs& a, SharedRoom& sh) {
   constexpr u32 NT = 64 * PAGED_WAVES;
   const u32 lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  shared_views<NT>(a, (u32*)sh.ring, sh.view);
+  shared_views<NT, BY_MEAN>(a, (u32*)sh.ring, sh.view);
+  if (BY_MEAN) a.short_rows = (u32)__builtin_amdgcn_readfirstlane(a.short_rows);
   u32 (*const of_wave)[4] = (u32(*)[4])sh.ring;
   u32 base[4] = {0, 0, 0, 0};
   for (u32 s0 = 0; s0 < n_views(a); s0 += NT) {
@@ -45,10 +47,10 @@ __device__ __forceinline__ void views_and_sums(const SharedArgs& a, SharedRoom& 
   if (threadIdx.x == 0) { sh.pre[0] = 0; sh.flat[0] = 0; sh.sum[0] = base[2]; sh.sum[1] = base[3]; }
   __syncthreads();
 }
-template <int HD>
-__device__ __forceinline__ SharedWork shared_work(const SharedArgs& a, SharedRoom& sh, u32 wg, u32 nwg) {
+template <bool BY_MEAN>
+__device__ __forceinline__ SharedWork shared_work(SharedArgs& a, SharedRoom& sh, u32 wg, u32 nwg) {
   constexpr u32 NT = 64 * PAGED_WAVES;
-  views_and_sums(a, sh);
+  views_and_sums<BY_MEAN>(a, sh);
   const u32 units = (u32)__builtin_amdgcn_readfirstlane(sh.flat[a.n_groups]);
   const u32 tiles = (u32)__builtin_amdgcn_readfirstlane(sh.sum[0]), prompts = (u32)__builtin_amdgcn_readfirstlane(sh.sum[1]);
   const SharedWork r = deal_out(a, units, tiles, prompts, nwg);
@@ -137,35 +139,51 @@ __device__ __forceinline__ SharedArgs fresh_args() {
 // 4000 tokens beside a prompt of 8192 took 737 us, so 591, every sequence by itself 628). One after the other on all workgroups: 158 us, so 99, for 253 sequences
 // behind 8200 tokens with 17 to 1000 of their own; bytes of all keys that are there 58 us, every sequence by itself 1000.
 // Of a call's time 3 to 5 us are the views and sums, 4 to 9 the join (a kernel of its own: results of other workgroups are in memory behind it), a workgroup's start and end 5.
+// the tiles of few rows: views from where the prompt part has them to where the few-row part does, then that part
 template <int HD, int BITS, int CT>
-__device__ __forceinline__ void shared_attention(const SharedArgs& args, PagedShared<HD, CT, SharedArgs>& sh, u32 wg, u32 nwg) {
+__device__ __forceinline__ void few_rows(const SharedArgs& a, const SharedRoom& p, ShortShared<HD, CT, PAGED_WAVES, true>& sh, u32 wg, u32 nwg) {
   constexpr u32 NT = 64 * PAGED_WAVES;
-  SharedWork work = shared_work<HD>(args, sh.p, wg, nwg);
+  SharedView v[PAGED_MAX_SEQS / NT];
+#pragma unroll
+  for (u32 j = 0; j < PAGED_MAX_SEQS / NT; ++j) if (threadIdx.x + j * NT < n_views(a)) v[j] = p.view[threadIdx.x + j * NT];
+  __syncthreads();
+#pragma unroll
+  for (u32 j = 0; j < PAGED_MAX_SEQS / NT; ++j) {
+    const u32 s = threadIdx.x + j * NT;
+    if (s >= n_views(a)) continue;
+    const bool group = s >= a.n_seqs;
+    sh.pos0[s] = v[j].pos0;
+    sh.n[s] = short_unit_count(a, v[j], group) ? (unsigned char)v[j].n : (unsigned char)0;
+    sh.link[s] = group ? (uint16_t)v[j].row() : v[j].first ? (uint16_t)v[j].group() : (uint16_t)NO_GROUP;
+  }
+  __syncthreads();
+  paged_short<HD, BITS, CT, SHORT_AHEAD(HD, BITS, CT), PAGED_WAVES>(a, sh, wg, nwg);
+}
+// CT: row tiles of the few-row part; ANY_CT: one, or SHORT_MORE, by the views
+#define ANY_CT 0
+template <int HD, int CT> union SharedKernelRoom { ShortShared<HD, CT, PAGED_WAVES, true> s; SharedRoom p; };
+template <int HD> union SharedKernelRoom<HD, ANY_CT> { ShortShared<HD, 1, PAGED_WAVES, true> one; ShortShared<HD, SHORT_MORE(HD), PAGED_WAVES, true> more; SharedRoom p; };
+template <int HD, int BITS, int CT>
+__device__ __forceinline__ void shared_attention(const SharedArgs& args, SharedKernelRoom<HD, CT>& sh, u32 wg, u32 nwg) {
+  constexpr bool BY_MEAN = CT == ANY_CT;
+  SharedArgs mine = args;
+  const SharedWork work = shared_work<BY_MEAN>(mine, sh.p, wg, nwg);
+  const u32 short_rows = mine.short_rows;
+  auto part_args = [&]() { SharedArgs a = fresh_args(); if (BY_MEAN) a.short_rows = short_rows; return a; };
   if (wg < work.flat_wgs) {
-    const SharedArgs a = fresh_args();
+    const SharedArgs a = part_args();
     const u32 units = (u32)__builtin_amdgcn_readfirstlane(sh.p.flat[a.n_groups]), from = min(wg * work.quota, units);
     paged_prompt<HD, BITS, true>(a, sh.p, wg, work.flat_wgs, false, FlatRun{from, min(from + work.quota, units)});
   } else if (work.few) {
-    const SharedArgs a = fresh_args();
-    SharedView v[PAGED_MAX_SEQS / NT];
-#pragma unroll
-    for (u32 j = 0; j < PAGED_MAX_SEQS / NT; ++j) if (threadIdx.x + j * NT < n_views(a)) v[j] = sh.p.view[threadIdx.x + j * NT];
-    __syncthreads();
-#pragma unroll
-    for (u32 j = 0; j < PAGED_MAX_SEQS / NT; ++j) {
-      const u32 s = threadIdx.x + j * NT;
-      if (s >= n_views(a)) continue;
-      const bool group = s >= a.n_seqs;
-      sh.s.pos0[s] = v[j].pos0;
-      sh.s.n[s] = short_unit_count(a, v[j], group) ? (unsigned char)v[j].n : (unsigned char)0;
-      sh.s.link[s] = group ? (uint16_t)v[j].row() : v[j].first ? (uint16_t)v[j].group() : (uint16_t)NO_GROUP;
-    }
-    __syncthreads();
-    paged_short<HD, BITS, CT, SHORT_AHEAD(HD, BITS, CT), PAGED_WAVES>(a, sh.s, wg - work.flat_wgs, nwg - work.flat_wgs);
+    const SharedArgs a = part_args();
+    const u32 few_wg = wg - work.flat_wgs, few_wgs = nwg - work.flat_wgs;
+    if constexpr (CT != ANY_CT) few_rows<HD, BITS, CT>(a, sh.p, sh.s, few_wg, few_wgs);
+    else if (short_rows == 16) few_rows<HD, BITS, 1>(a, sh.p, sh.one, few_wg, few_wgs);
+    else few_rows<HD, BITS, SHORT_MORE(HD)>(a, sh.p, sh.more, few_wg, few_wgs);
   }
   if (!work.prompts) return;
-  const SharedArgs a = fresh_args();
+  SharedArgs a = part_args();
   __syncthreads();
-  if (work.few && wg >= work.flat_wgs) views_and_sums(a, sh.p);
+  if (work.few && wg >= work.flat_wgs) views_and_sums<BY_MEAN>(a, sh.p);
   paged_prompt<HD, BITS>(a, sh.p, wg, nwg, true, FlatRun{0, 0}, nwg - work.flat_wgs);
 }

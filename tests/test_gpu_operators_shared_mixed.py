@@ -65,3 +65,15 @@ def test_context_lengths_that_do_not_fit(members, bits):
         tables[s, (lens[s] + 15) // 16:] = tables[s, 0]
     got = run_shared((cache, c, tables, given, cu, q), starts, shared, max_q)
     check_attention(got, cache, c, tables, seen, cu, q)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("hd, nq, nkv", HEADS)
+@pytest.mark.parametrize("before, after", [
+    ([(60, 1)] * 30, [(90, 1)] * 30),                        # in no group
+    ([(333, 333)], [(150, 40), (77, 1)]),                    # prompts, more rows than the few-row part holds
+    ([(50, 3), (70, 5), (20, 1)], [(100, 8)] * 3),           # drafts
+    ([(400, 70)], [(60, 4)] * 20 + [(0, 1)]),
+])
+def test_groups_beside_others(before, after, hd, nq, nkv, bits):
+    check([(130, [(135 + i, 1) for i in range(3)]), (100, [(104, 4), (101, 1)]), (70, [(71, 1)] * 30)], nq, nkv, hd, bits, seed=26, before=before, after=after)

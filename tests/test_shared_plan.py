@@ -43,12 +43,11 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
   a.nq = c->nq; a.nkv = c->nkv; a.G = c->nq / c->nkv; a.n_seqs = c->n_seqs; a.n_tokens = c->n_tokens; a.max_q = c->max_q; a.max_blocks = c->max_blocks;
   a.window = c->window; a.sinks = c->sinks; a.n_groups = c->n_groups; a.share_all = c->share_all; a.n_splits = c->n_splits;
   a.cu = c->cu; a.lens = c->lens; a.starts = c->starts; a.shared = c->shared;
-  const u32 ct = few_row_tiles(c->hd, c->bits, a.G, a.n_tokens, a.n_groups, a.max_q);
-  a.short_rows = 16 * ct;
-  shared_costs(a, c->hd, c->bits, ct, c->nwg);
+  shared_costs(a, c->hd, c->bits, c->nwg);
   std::vector<u32> room(ROOM_WORDS), pre(PAGED_MAX_SEQS + 1), flat(PAGED_MAX_SEQS + 1);
   std::vector<SharedView> view(PAGED_MAX_SEQS);
-  shared_views<1>(a, room.data(), view.data());
+  if (rows_by_mean(c->hd, c->bits)) shared_views<1, true>(a, room.data(), view.data());
+  else shared_views<1, false>(a, room.data(), view.data());
   u64 sums[4] = {0, 0, 0, 0}, all_units = 0;
   for (u32 s = 0; s < n_views(a); ++s) {
     u32 v[4] = {0, 0, 0, 0};
@@ -66,7 +65,7 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
   RULE(w.flat_wgs <= c->nwg && (w.flat_wgs < c->nwg || !(w.few || w.prompts)) && (w.flat_wgs > 0) == (sums[1] > 0));
   RULE((u64)w.quota * std::max(w.flat_wgs, 1u) >= sums[1]);
   // (beside prompts, whose items whoever is free takes, no run of the shared keys is longer than everyone's share of all the work)
-  const double rest = a.few_cost * (double)sums[2] + (double)sums[3];
+  const double rest = a.few_cost * (a.short_rows > 16 ? FEW_MORE : 1.f) * (double)sums[2] + (double)sums[3];
   RULE(!w.flat_wgs || !w.prompts || w.flat_wgs == c->nwg - 1 || (double)sums[1] / w.flat_wgs <= 1.001 * (sums[1] + rest) / c->nwg);
   const u32 items = pre[a.n_seqs] * a.nkv, parts = prompt_parts(a, items, c->nwg - w.flat_wgs);
   RULE(parts == 1 || (u64)items * parts <= c->nwg);
@@ -295,7 +294,6 @@ def test_prompts_beside_groups(plan, nq, nkv, hd, bits, context, queries):
     steps = [(context - queries + (r - 1) // G) // 64 + 1 for r in rows]
     want = sum(4 * s + 13 for s in steps) * nkv
     assert want < 2 ** 21 and abs(of_call[4] - want) < 0.05 * want + 6 * len(steps) * nkv
-    assert of_call[0] >= 1
 
 
 @pytest.mark.parametrize("nq, nkv, hd, bits", HEADS)
@@ -306,6 +304,20 @@ def test_whether_groups_share_does_not_depend_on_who_is_beside_them(plan, nq, nk
     alone = plan(*batch(group), [shared], nq, nkv, hd, bits, share_all=0)
     for beside in ([(2000, 2000, None)], [(8192, 8192, None)], [(1000 + i, 1, None) for i in range(100)]):
         assert plan(*batch(group + beside), [shared], nq, nkv, hd, bits, share_all=0)[1] == alone[1]
+
+
+@pytest.mark.parametrize("nq, nkv, hd, bits, groups, members, queries, rows", [
+    (32, 8, 128, 4, 16, 8, 1, 32), (32, 8, 128, 4, 16, 9, 1, 16), (32, 8, 128, 4, 5, 4, 1, 16), (16, 16, 64, 16, 40, 4, 9, 64), (32, 8, 64, 4, 3, 16, 1, 64),
+    (32, 8, 64, 16, 3, 17, 1, 16), (16, 16, 64, 16, 30, 2, 8, 16), (32, 8, 128, 16, 16, 8, 1, 16)])
+def test_row_tiles_are_those_that_the_groups_need(plan, nq, nkv, hd, bits, groups, members, queries, rows):
+    """Rows of the few-row part: by the mean of the groups there are, whoever is beside them; then by sequences that need more than 16, unless some need more than it holds."""
+    seqs, shared = [(1500 + queries + i, queries, g) for g in range(groups) for i in range(members)], [1500] * groups
+    assert plan(*batch(seqs), shared, nq, nkv, hd, bits)[2][1] == rows
+    for beside in ([(1000 + i, 1, None) for i in range(100)], [(2000, 2000, None)]):
+        assert plan(*batch(seqs + beside), shared, nq, nkv, hd, bits)[2][1] == rows
+    few = [(300, 24 * nkv // nq, None)]                  # 24 rows
+    assert plan(*batch(seqs + few), shared, nq, nkv, hd, bits)[2][1] == (32 if hd == 128 else 64)
+    assert plan(*batch(seqs + few + [(2000, 2000, None)]), shared, nq, nkv, hd, bits)[2][1] == rows
 
 
 def test_units_at_the_largest_sizes(plan):
