@@ -328,18 +328,16 @@ extern "C" int blink_paged_attention(int32_t device, const blink_paged_attention
 
 // ---- attention of groups --------------------------------------------------------------------------------------------------------
 struct SharedPlan {
-  u32 n_splits;
   u64 part_bytes, prompt_bytes, flat_bytes, row_bytes, token_bytes;
   u64 bytes(u32 n_cu) const { return paged_ctr_bytes(n_cu) + part_bytes + prompt_bytes + flat_bytes + row_bytes + token_bytes; }
 };
-static SharedPlan shared_plan(u32 hd, u32 nq, u32 n_tokens, u32 steps, u32 n_cu) {
+static SharedPlan shared_plan(u32 hd, const SharedArgs& a, u32 n_cu) {
   SharedPlan p{};
-  p.n_splits = std::max(1u, steps / 4);          // (parts of 256 keys at least)
   p.part_bytes = short_floats(n_cu, hd, SHORT_MORE(hd)) * 4;
   p.prompt_bytes = (u64)n_cu * PROMPT_SLOT(hd) * 4;
   p.flat_bytes = 2 * p.prompt_bytes;
-  p.row_bytes = 2ull * n_tokens * nq * ROW_RESULT(hd) * 4;
-  p.token_bytes = (n_tokens + 1ull) * sizeof(JoinToken);
+  p.row_bytes = 2ull * a.n_rows * a.nq * ROW_RESULT(hd) * 4;
+  p.token_bytes = (a.n_tokens + 1ull) * sizeof(JoinToken);
   return p;
 }
 // waves of the join: one per token and as many query heads as it has lanes for
@@ -359,7 +357,10 @@ extern "C" int blink_shared_attention_workspace_bytes(int32_t device, const blin
   if (int rc = check_groups(*c, n_q_heads, n_seqs, n_groups, n_tokens)) return rc;
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  *bytes = std::max<u64>(*bytes, shared_plan(c->head_dim, n_q_heads, n_tokens, 1, n_cu).bytes(n_cu));
+  SharedArgs p{};
+  p.nq = n_q_heads; p.G = n_q_heads / c->n_kv_heads; p.n_seqs = n_seqs; p.n_tokens = n_tokens; p.max_q = max_q;
+  rows_of_call(p);
+  *bytes = std::max<u64>(*bytes, shared_plan(c->head_dim, p, n_cu).bytes(n_cu));
   return BLINK_OK;
 }
 
@@ -389,13 +390,14 @@ extern "C" int blink_shared_attention(int32_t device, const blink_shared_attenti
   if (!s->group_starts || !s->shared_lens || (u64)s->group_starts % 4 || (u64)s->shared_lens % 4) return fail(BLINK_ERR_INVAL, "group_starts or shared_lens is null or not aligned");
   u32 n_cu;
   if (int rc = compute_units(device, &n_cu)) return rc;
-  const SharedPlan plan = shared_plan(hd, a->n_q_heads, a->n_tokens, key_steps(a), n_cu);
+  SharedArgs p{};
+  fill_paged(p, a, scale2, 0, std::max(1u, key_steps(a) / 4), n_cu);      // (parts of 256 keys at least)
+  rows_of_call(p);
+  const SharedPlan plan = shared_plan(hd, p, n_cu);
   if (!a->workspace || (u64)a->workspace % 256 || a->workspace_bytes < plan.bytes(n_cu))
     return fail(BLINK_ERR_INVAL, "a workspace of %llu bytes, aligned to 256, is needed", (unsigned long long)plan.bytes(n_cu));
   OnDevice on(device);
   HIPCHK(on.err);
-  SharedArgs p{};
-  fill_paged(p, a, scale2, 0, plan.n_splits, n_cu);
   p.own_part = p.part + plan.part_bytes / 4;
   p.prompt_part = p.own_part + plan.prompt_bytes / 4;
   p.rows = p.prompt_part + plan.flat_bytes / 4;

@@ -472,10 +472,24 @@ __device__ __forceinline__ void give_strange(const CacheTile<HD, BITS>& t, float
 // whether a view's results are joined with others
 template <typename Shared>
 __device__ __forceinline__ bool is_joined(const SharedArgs& a, const Shared& sh, u32 s) { return s >= a.n_seqs || (u32)__builtin_amdgcn_readfirstlane(sh.link[s]) != NO_GROUP; }
+// The kernel's arguments (its first and only ones), loaded anew: each part of the kernel has its own copy, or the compiler would load them once at the
+// start, and keep what is more than the scalar registers hold in vector registers, to be brought back at every tile.
+__device__ __forceinline__ SharedArgs fresh_args() {
+  typedef const __attribute__((address_space(4))) SharedArgs* args_t;
+  u64 p = (u64)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const SharedArgs*)(args_t)p;
+}
 // a row's result, to be joined with another one (which: 0 the group's, 1 the sequence's)
 template <int HD>
-__device__ __forceinline__ float* row_result(const SharedArgs& a, u32 which, u32 tok, u32 head) {
-  return a.rows + (((u64)which * a.n_tokens + tok) * a.nq + head) * ROW_RESULT(HD);
+__device__ __forceinline__ float* row_result(const SharedArgs& a, u32 which, u32 row, u32 head) {
+  return a.rows + (((u64)which * a.n_rows + row) * a.nq + head) * ROW_RESULT(HD);
+}
+// of query k (row_index), with the arguments loaded anew: they would take registers that the loops need (4 sequences: 20.9 us, so 20.5)
+template <int HD>
+__device__ __forceinline__ float* row_result(u32 which, u32 s, u32 t0, u32 k, u32 head) {
+  const SharedArgs a = fresh_args();
+  return row_result<HD>(a, which, row_index(a, s, t0, k), head);
 }
 
 __device__ __forceinline__ f16_t* out_at(const PagedArgs& a, u32 tok, u32 k) { return a.out_tbs ? a.out + packed_off(tok, k, a.out_tbs) : a.out + (u64)tok * a.os + k; }
@@ -630,7 +644,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
           const float l = quad_sum(acc[c].l);
           const u32 r = c * 16 + lc, tok = r / a.G;
           if (r >= p.n * a.G) continue;
-          float* const x = row_result<HD>(a, p.s < a.n_seqs ? 1u : 0u, p.t0 + tok, p.g * a.G + r - tok * a.G);
+          float* const x = row_result<HD>(p.s < a.n_seqs ? 1u : 0u, p.row, p.t0, tok, p.g * a.G + r - tok * a.G);
           if (lg == 0) *(float2*)x = make_float2(acc[c].m, l);
           if constexpr (BITS == 16) {
 #pragma unroll
@@ -787,7 +801,7 @@ __device__ __forceinline__ void paged_short(const A& a, ShortShared<HD, CT, NW, 
         const float sum = quad_sum(all.l);
         if (!all.live) return;
         const u32 r = all.c * 16 + lc, tok = r / a.G;
-        float* const x = row_result<HD>(a, p.s < a.n_seqs ? 1u : 0u, p.t0 + tok, p.g * a.G + r - tok * a.G);
+        float* const x = row_result<HD>(p.s < a.n_seqs ? 1u : 0u, p.row, p.t0, tok, p.g * a.G + r - tok * a.G);
         if (all.d0 == 0 && lg == 0) *(float2*)x = make_float2(all.m, sum);
         if constexpr (BITS == 16) {
 #pragma unroll
@@ -1335,7 +1349,7 @@ __device__ __forceinline__ void paged_prompt(const A& a, PromptRoomOf<A>& sh, u3
       if (to_row) {
         if constexpr (SHARED) {
           const u32 rr = it.r0 + r, tok = rr / a.G;
-          float* const x = row_result<HD>(a, FLAT ? 0u : 1u, it.t0 + tok, it.g * a.G + rr - tok * a.G);
+          float* const x = row_result<HD>(FLAT ? 0u : 1u, it.row, it.t0, tok, it.g * a.G + rr - tok * a.G);
           if (lg_end == 0) *(float2*)x = make_float2(m[c], sum);
 #pragma unroll
           for (int d = 0; d < HD / 16; ++d) *(floatx4_t*)(x + 4 + d * 16 + lg_end * 4) = o[c][d];

@@ -44,7 +44,8 @@ struct PagedArgs {
 struct SharedArgs : PagedArgs {
   u32 n_groups, share_all;        // share_all: groups that gain nothing by it too
   const i32 *starts, *shared;     // first sequence of every group (n_groups + 1), tokens that its sequences share
-  float* rows;                    // results to be joined: [of the group, of the sequence][token][q head] of ROW_RESULT(hd) floats
+  float* rows;                    // results to be joined: [of the group, of the sequence][n_rows][q head] of ROW_RESULT(hd) floats (row_index)
+  u32 n_rows, row_tokens;         // a row per token or, where that is less, row_tokens of them per sequence (0: per token)
   float* own_part;                // parts of prompt items (prompt_part: of the groups' items)
   u32 least;                      // units of a step of a group of 32 rows or less in all (of others: FLAT_STEP, of items of 128 rows or less FLAT_LIGHT)
   u32 lead;                       // time of an item of the groups' shared keys beside its steps, in units (FlatShape)
@@ -249,9 +250,14 @@ __device__ __forceinline__ u32 group_token(const SharedArgs& a, const SharedView
 __device__ __forceinline__ u32 member_query(const SharedArgs& a, const SharedView* view, const SharedView& group, const SharedView& v, u32 k) {
   return k + (group.gaps() ? v.before() - view[group.row()].before() : v.t0 - group.t0);
 }
-// the rows of results to be joined, of every query head: how many, and that of a view's query k
-__host__ __device__ __forceinline__ u32 rows_of_call(const SharedArgs& a) { return a.n_tokens; }
-__device__ __forceinline__ u32 row_index(const SharedArgs& a, const SharedView& v, u32 index, u32 k) { return v.t0 + k; }
+// The row of results to be joined, of every query head, for query k of a sequence whose first token is t0 (a group: its first member's; its members have as many rows as it has queries). A sequence
+// of SHARED_ROWS rows or more, a prompt, has none: what a call needs room for does not grow with its prompts.
+__host__ inline void rows_of_call(SharedArgs& a) {
+  const u32 most = (SHARED_ROWS - 1) / a.G, each = a.max_q < most ? a.max_q : most;
+  a.row_tokens = (u64)a.n_seqs * each < a.n_tokens ? each : 0;
+  a.n_rows = a.row_tokens ? a.n_seqs * each : a.n_tokens;
+}
+__device__ __forceinline__ u32 row_index(const SharedArgs& a, u32 s, u32 t0, u32 k) { return (a.row_tokens ? s * a.row_tokens : t0) + k; }
 
 __device__ __forceinline__ u32 short_unit_count(const PagedArgs& a, const SeqView& v) {     // tiles of a sequence and kv head; 0: not this part's, 1 at least else
   if (!v.n || v.n * a.G > a.short_rows) return 0;
@@ -317,7 +323,7 @@ __device__ __forceinline__ SharedWork deal_out(const SharedArgs& a, u32 units, u
 // What is to be joined of a token's rows (kinds 0: nothing, its results are in place; 1: a result of its group and one of its sequence; 2: parts of a prompt
 // item's keys). Its group's: units[0] + kv head * units[1] is where its item's line of units[2] begins, row: its first row there. Its sequence's:
 // in rows, or parts of prompt items (parts > 1): items top - (row + head) / PROMPT_ROWS. rows: of the group's result and the sequence's, where those are in rows.
-struct JoinToken { u32 kind, units[3], row, own_row, top, parts, rows[2]; };
+struct alignas(16) JoinToken { u32 kind : 2, row : 9, parts : 21, units[3], own_row, top, rows[2]; };
 // Of token t: the views, items of the prompts before each sequence (pre), units before each group (flat), parts of every prompt item
 __device__ __forceinline__ JoinToken join_token(const SharedArgs& a, const SharedView* view, const u32* pre, const u32* flat, u32 parts, u32 t) {
   u32 s = 0;                                       // the last sequence that begins at this token or before
@@ -328,11 +334,11 @@ __device__ __forceinline__ JoinToken join_token(const SharedArgs& a, const Share
     const bool cut = parts > 1 && prompt_items(a, v) != 0;
     j.own_row = (t - v.t0) * a.G; j.top = pre[a.n_seqs] - 1 - pre[s]; j.parts = cut ? parts : 1;
     j.kind = v.first ? 1 : cut ? 2 : 0;
-    j.rows[1] = row_index(a, v, s, t - v.t0);
+    j.rows[1] = row_index(a, s, v.t0, t - v.t0);
     if (v.first) {
       const SharedView x = view[a.n_seqs + v.group()];
       const u32 k = member_query(a, view, x, v, t - v.t0), r = k * a.G;
-      j.rows[0] = row_index(a, x, a.n_seqs + v.group(), k);
+      j.rows[0] = row_index(a, x.row(), x.t0, k);
       if (flat_units(a, x)) {
         const FlatShape f = flat_shape(a, x);
         const u32 item = r / flat_rows(a);

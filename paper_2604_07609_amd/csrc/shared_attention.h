@@ -124,14 +124,6 @@ __device__ __forceinline__ void shared_join(const SharedArgs& a, u32 i) {
   }
 }
 
-// The kernel's arguments (its first and only ones), loaded anew: each part of the kernel has its own copy, or the compiler would load them once at the
-// start, and keep what is more than the scalar registers hold in vector registers, to be brought back at every tile.
-__device__ __forceinline__ SharedArgs fresh_args() {
-  typedef const __attribute__((address_space(4))) SharedArgs* args_t;
-  u64 p = (u64)__builtin_amdgcn_kernarg_segment_ptr();
-  asm volatile("" : "+s"(p));
-  return *(const SharedArgs*)(args_t)p;
-}
 // A call with groups. A row's keys are its group's and its own: softmax((s1, s2)) v is joined from each part's maximum m, sum l and output o about m, by
 // o = (2^(m1-M) o1 + 2^(m2-M) o2) / (2^(m1-M) l1 + 2^(m2-M) l2). With n members of g rows each the shared keys are read once and not n times, and are products of n g rows:
 // what was bound by bytes becomes bound by products, while the members' own keys stay bound by bytes. So some workgroups have the groups' shared keys, others at the same time

@@ -77,3 +77,14 @@ def test_context_lengths_that_do_not_fit(members, bits):
 ])
 def test_groups_beside_others(before, after, hd, nq, nkv, bits):
     check([(130, [(135 + i, 1) for i in range(3)]), (100, [(104, 4), (101, 1)]), (70, [(71, 1)] * 30)], nq, nkv, hd, bits, seed=26, before=before, after=after)
+
+
+def test_workspace_does_not_grow_with_prompts():
+    """Only sequences of fewer than 256 rows have results to be joined: a prompt's tokens take a note of 32 bytes each, and no rows."""
+    cache = make_groups([(64, [(70, 1), (71, 1)])], 32, 8, 128, 16)[0][0]
+    size = lambda seqs, tokens, max_q: B.shared_attention_workspace_bytes(32, cache, seqs, 1, tokens, max_q)      # noqa: E731
+    assert size(33, 65568, 65536) - size(33, 16416, 16384) == 32 * (65568 - 16416)
+    assert size(33, 16416, 16384) - size(33, 33, 1) <= 32 * 16416 + 2 * 33 * 63 * 32 * 132 * 4
+    for seqs, tokens, max_q in ((33, 16416, 16384), (1000, 1000, 1), (40, 400, 17), (7, 3000, 2999)):
+        for fewer in ((seqs - 1, tokens, max_q), (seqs, tokens - 1, max_q), (seqs, tokens, max(1, max_q // 2)), (1, tokens, max_q), (seqs, 1, max_q)):
+            assert size(*fewer) <= size(seqs, tokens, max_q)

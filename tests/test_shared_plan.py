@@ -44,6 +44,8 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
   a.window = c->window; a.sinks = c->sinks; a.n_groups = c->n_groups; a.share_all = c->share_all; a.n_splits = c->n_splits;
   a.cu = c->cu; a.lens = c->lens; a.starts = c->starts; a.shared = c->shared;
   shared_costs(a, c->hd, c->bits, c->nwg);
+  rows_of_call(a);
+  RULE(a.n_rows <= a.n_tokens);
   std::vector<u32> room(ROOM_WORDS), pre(PAGED_MAX_SEQS + 1), flat(PAGED_MAX_SEQS + 1);
   std::vector<SharedView> view(PAGED_MAX_SEQS);
   if (rows_by_mean(c->hd, c->bits)) shared_views<1, true>(a, room.data(), view.data());
@@ -73,15 +75,22 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
   for (u32 g = 0; g < a.n_groups; ++g) queries[g] = view[a.n_seqs + g].n;
   of_call[0] = w.flat_wgs; of_call[1] = a.short_rows; of_call[2] = (u32)sums[1]; of_call[3] = (u32)sums[2]; of_call[4] = (u32)sums[3];
 
+  bool ascending = true, groups_ascending = true;
+  for (u32 s = 0; s < a.n_seqs; ++s) ascending &= a.cu[s] >= 0 && a.cu[s] <= a.cu[s + 1];
+  for (u32 g = 0; g < a.n_groups; ++g) groups_ascending &= a.starts[g] <= a.starts[g + 1];
+  const bool ordered = ascending && groups_ascending;
+
   // what is written: rows by (which, row, kv head) -> (view, query); slots -> (group, kv head, first row)
   struct Written { u32 view, query; };
   std::map<std::vector<u32>, Written> rows;
   struct Slot { u32 g, head, r0, rows, s_lo, s_hi; bool used; };
   std::vector<Slot> slots(2 * c->nwg, Slot{});
   auto wrote = [&](u32 which, const SharedView& v, u32 index, u32 query, u32 head) {
-    const u64 row = row_index(a, v, index, query);
-    if (row >= rows_of_call(a)) return false;
-    rows[{which, (u32)row, head}] = {index, query};
+    const u32 row = row_index(a, which ? index : v.row(), v.t0, query);
+    if (row >= a.n_rows) return false;
+    // (two views' rows at the same place only where what comes out is not defined)
+    if (ordered && rows.count({which, row, head})) return false;
+    rows[{which, row, head}] = {index, query};
     return true;
   };
   for (u32 g = 0; g < a.n_groups; ++g) {
@@ -119,9 +128,6 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
   }
   // the join (groups that decrease may have sequences between one another's, cu_seqlens that do may have a token in two sequences: what comes out is not defined then, and
   // only where it is written and read is looked at)
-  bool ascending = true, groups_ascending = true;
-  for (u32 s = 0; s < a.n_seqs; ++s) ascending &= a.cu[s] >= 0 && a.cu[s] <= a.cu[s + 1];
-  for (u32 g = 0; g < a.n_groups; ++g) groups_ascending &= a.starts[g] <= a.starts[g + 1];
   std::vector<u32> joined(a.n_seqs);
   for (u32 t = 0; t < a.n_tokens; ++t) {
     const JoinToken j = join_token(a, view.data(), pre.data(), flat.data(), parts, t);
@@ -136,7 +142,7 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
     const u32 query = t - v.t0;
     for (u32 h = 0; h < a.nkv; ++h) {
       auto row = [&](u32 which, u32 index, u32 q) {
-        RULE(j.rows[which] < rows_of_call(a));
+        RULE(j.rows[which] < a.n_rows);
         const auto found = rows.find({which, j.rows[which], h});
         if (!one) return 0;
         RULE(found != rows.end() && found->second.view == index && found->second.query == q);
