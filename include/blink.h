@@ -417,9 +417,9 @@ int blink_attention_workspace_bytes(int32_t device, const blink_kv_cache* cache,
  * is the sequences group_starts[i] .. group_starts[i + 1] (not decreasing; those before the first and behind the last one are in none), whose
  * block tables agree in the blocks of the first shared_lens[i] tokens. Everything else is as for blink_paged_attention, and so are the
  * results, but for the order of summation: a group saves work, and changes nothing. A sequence whose queries do not all stand behind the
- * shared tokens, or do not see all of them (a window), or which has many queries, is taken by itself, and so are those of a group so small that
- * sharing takes longer. What comes out where tables do not agree,
- * or group_starts decrease, is not defined; nothing outside the tensors is read or written then either. BLINK_ERR_TOO_LARGE with more than
+ * shared tokens, or do not see all of them (a window), or which has many queries, is taken by itself, wherever in the group it stands, and so are those of a group so
+ * small that sharing takes longer. What comes out where tables do not agree,
+ * or group_starts or cu_seqlens decrease, is not defined; nothing outside the tensors is read or written then either. BLINK_ERR_TOO_LARGE with more than
  * 1024 sequences and groups together. */
 typedef struct {
   blink_paged_attention_args attention;

@@ -88,3 +88,45 @@ def test_workspace_does_not_grow_with_prompts():
     for seqs, tokens, max_q in ((33, 16416, 16384), (1000, 1000, 1), (40, 400, 17), (7, 3000, 2999)):
         for fewer in ((seqs - 1, tokens, max_q), (seqs, tokens - 1, max_q), (seqs, tokens, max(1, max_q // 2)), (1, tokens, max_q), (seqs, 1, max_q)):
             assert size(*fewer) <= size(seqs, tokens, max_q)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("window, sinks", [(150, 0), (190, 5), (191, 0), (260, 17), (500, 16)])
+@pytest.mark.parametrize("hd, nq, nkv", [(64, 4, 2), (128, 8, 2)])
+@pytest.mark.parametrize("members", [
+    [(130 + i, 1) for i in range(40)] + [(400, 1)],          # more rows than the few-row part holds
+    [(170, 40), (260, 70), (189, 61), (190, 1)],             # prompt items behind the shared keys, which end before the window is left, with it and behind it
+    [(190 + i, 1 + 9 * (i % 5)) for i in range(20)],
+])
+def test_windows_behind_groups_of_many_rows(members, hd, nq, nkv, window, sinks, bits):
+    check([(128, members)], nq, nkv, hd, bits, window=window, sinks=sinks, seed=27)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("groups", [
+    [(128, [(140 + i, 1) for i in range(40)])],              # runs of shared keys
+    [(128, [(140, 1), (3000, 40), (2900, 3)])],              # a prompt's parts joined
+    [(128, [(140, 1), (500, 300), (135, 2)])],               # and one without rows among its members
+])
+def test_strided_rows(groups, bits):
+    b, starts, shared, max_q = make_groups(groups, 4, 2, 64, bits, seed=28)
+    cache, c, tables, lens, cu, q = b
+    T = q.shape[0]
+    wide_q, wide_o = torch.zeros(T, 9, 64, dtype=torch.float16, device="cuda"), torch.full((T, 7, 64), 3.0, dtype=torch.float16, device="cuda")
+    wide_q[:, 2:6] = dev(q)
+    work = torch.zeros(B.shared_attention_workspace_bytes(4, cache, len(lens), 1, T, max_q), dtype=torch.uint8, device="cuda")
+    B.shared_attention(wide_q[:, 2:6], cache, dev(tables), dev(lens), dev(cu), dev(starts), dev(shared), wide_o[:, 1:5], work, max_q=max_q, share_all=True)
+    o = wide_o.cpu().numpy()
+    check_attention(o[:, 1:5].astype(np.float64), *b)
+    assert (o[:, :1] == 3).all() and (o[:, 5:] == 3).all()
+
+
+def test_repeated_calls_are_the_same_to_the_last_bit():
+    """Whichever workgroup comes first, sums are in the order of the runs: groups in runs and in parts, drafts, prompts, all in one batch, twenty times."""
+    for bits in (16, 4):
+        b, starts, shared, max_q = make_groups([(400, [(410 + i, 1) for i in range(50)]), (300, [(320, 20), (900, 300), (330, 12)]), (64, [(70, 5), (66, 1)])], 8, 2, 128, bits, seed=29,
+                                               before=[(700, 1)], after=[(500, 120), (30, 1)])
+        got = run_shared(b, starts, shared, max_q)
+        check_attention(got, *b)
+        for _ in range(20):
+            assert np.array_equal(got, run_shared(b, starts, shared, max_q))
