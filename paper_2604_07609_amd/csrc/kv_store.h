@@ -390,7 +390,7 @@ __device__ __forceinline__ void kv_read(const ReadArgs& a, u64 i) {      // eigh
 // ---- blocks copied ------------------------------------------------------------------------------------------------------------
 // A block is one piece of memory in a cache of 4 bits, two (its keys, its values) in one of 16. A workgroup copies COPY_WORDS words of 16 bytes
 // of a piece at most, four of a lane on their way at a time. All layers' copies are one launch. Bound by bytes: 80 layers' 200 blocks
-// of 64 KiB 402 us, 5.2 TB/s; 7 in 32 layers 6.0 us (one layer's 3.2); 2039 blocks of 4 bits (4 kv heads of 128, 35 MB) 6.4 us, 5.5 TB/s. With one, two and eight words of a
+// of 64 KiB 402 us, 5.2 TB/s; 7 in 32 layers 6.0 us (one layer's 3.2); 2039 blocks of 4 bits (4 kv heads of 128, 35 MB) 6.0 to 7.9 us, 4.5 to 5.8 TB/s. With one, two and eight words of a
 // lane at a time those 4-bit blocks, of 544 words, took 7.4, 9.2 and 12.7 us, the 7 in 32 layers 5.8, 5.5 and 7.8.
 #define COPY_CACHES 128u           // caches of a launch
 #define COPY_WORDS (4u * BLK_THREADS)

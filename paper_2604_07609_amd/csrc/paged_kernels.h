@@ -9,7 +9,7 @@
 #define SHORT_AHEAD(HD, BITS, CT) ((CT) > 1 ? 2 : (HD) == 128 || (BITS) == 4 ? 3 : 4)
 #define PAGED_BOUNDS __launch_bounds__(512) __attribute__((amdgpu_num_vgpr(120)))       // (see PHASE_KERNEL8)
 // One row tile over a 4-bit cache is bound by instructions: three workgroups of four waves on a compute unit, else one of eight (128
-// sequences of 4096 keys, heads of 128: 122 us and not 131; of 64: 87 and not 100)
+// sequences of 4096 keys, heads of 128: 122 us and not 131; of 64: 87 and not 100). Not where prompts or groups' shared keys are in the same launch: their ring takes the LDS
 #define SHORT_SMALL(BITS, CT) ((BITS) == 4 && (CT) == 1)
 #define SHORT_WAVES(BITS, CT) (SHORT_SMALL(BITS, CT) ? 4 : 8)
 #define SHORT_PER_CU(BITS, CT) (SHORT_SMALL(BITS, CT) ? 3 : 1)

@@ -101,8 +101,8 @@ __device__ __forceinline__ Seen seen_tiles(const PagedArgs& a, i32 p0, i32 p1, u
   return r;
 }
 
-// The groups with more rows than the few-row part takes, or with others' tokens between their members' (rows are looked up here, and not there: registers): their rows in items of flat_rows (whole queries), each with all shared keys. All steps of
-// all (group, kv head, item) are one line of units, FLAT_STEP, FLAT_LIGHT or `least` a step, and `lead` ahead of an item's, and every workgroup has an equal run of it. An item inside a run is
+// The groups with more rows than the few-row part takes, or with others' tokens between their members' (rows are looked up here, and not there: 60 scalar registers more): their rows in items of
+// flat_rows (whole queries), each with all shared keys. All steps of all (group, kv head, item) are one line of units, FLAT_STEP, FLAT_LIGHT or `least` a step, and `lead` ahead of an item's, and every workgroup has an equal run of it. An item inside a run is
 // done there; one that several runs share leaves a result in each. The units are what workgroups' times fit, to within 1.3 us of 30 to 75: a piece of an item, its start and end, takes
 // 6.3 us (over 4 bits 7.0; with heads of 64: 6.8, 4.4), a step of 256 rows 1.87 (2.25; 1.52, 1.97), one of 128 or less 1.37 (1.68; 1.10, 1.47), of a
 // group of 32 rows over halves 1.17, bound by bytes like the tiles of few rows.
@@ -362,8 +362,8 @@ __host__ inline void shared_costs(SharedArgs& p, u32 hd, u32 bits, u32 n_cu) {
   const u64 own = (u64)p.max_q * p.G, all = (u64)p.n_tokens * p.G;
   p.short_rows = (all <= p.most_rows ? all > 16 : own > 16 && own <= p.most_rows) ? p.most_rows : 16u;
   p.few_cost = halves ? 0.6f : 0.26f;
-  // (what sharing must gain on every compute unit: 8 us for the groups' starts and the join, and what the members' rows take to memory and back: of other tokens nothing is joined. 64 sequences in
-  // 4 bits, 1024 shared keys: 26.5 us, 27.8 apart; 253 behind 64: 78.5, 70 apart; 40 groups of 4, heads of 64, behind 64 and 256: 29.8, 37, apart 23.7, 40.4)
+  // (what sharing must gain on every compute unit: 8 us for the groups' starts and the join, and what the members' rows take to memory and back: of other tokens nothing is joined. Shared and apart in us: 64 sequences in
+  // 4 bits, 1024 shared keys: 30, 28; 253 behind 64: 70, 61; 16 groups of 8 behind 64: 35, 37; 40 groups of 4, heads of 64, behind 64: 26, 25)
   const float units = (float)n_cu / (float)p.nkv / unit;      // of a us, for a kv head
   p.gain = (u32)(8.f * units);
   p.row_cost = (float)p.nq * (float)(16 * ROW_RESULT(hd)) * 2e-7f * units;

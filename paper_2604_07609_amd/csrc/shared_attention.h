@@ -1,5 +1,5 @@
-// Attention of a batch in which the sequences of a group have their first blocks in common (views, and the groups' shared keys: paged_attention.h): who has
-// which part of the work, and the results joined.
+// Attention of a batch in which the sequences of a group have their first blocks in common (views, and who has which part of the work: paged_views.h;
+// the groups' shared keys: paged_attention.h): the parts put together, and the results joined.
 #pragma once
 #include "paged_attention.h"
 
@@ -124,14 +124,8 @@ __device__ __forceinline__ void shared_join(const SharedArgs& a, u32 i) {
   }
 }
 
-// A call with groups. A row's keys are its group's and its own: softmax((s1, s2)) v is joined from each part's maximum m, sum l and output o about m, by
-// o = (2^(m1-M) o1 + 2^(m2-M) o2) / (2^(m1-M) l1 + 2^(m2-M) l2). With n members of g rows each the shared keys are read once and not n times, and are products of n g rows:
-// what was bound by bytes becomes bound by products, while the members' own keys stay bound by bytes. So some workgroups have the groups' shared keys, others at the same time
-// the tiles of few rows, as many each as their estimated times ask for, and whoever is done takes the prompts' items (with one run of all shared keys, and no item behind it, 32 sequences behind
-// 4000 tokens beside a prompt of 8192 took 737 us, so 591, every sequence by itself 628). One after the other on all workgroups: 158 us, so 99, for 253 sequences
-// behind 8200 tokens with 17 to 1000 of their own; bytes of all keys that are there 58 us, every sequence by itself 1000.
-// Of a call's time 3 to 5 us are the views and sums, 4 to 9 the join (a kernel of its own: results of other workgroups are in memory behind it), a workgroup's start and end 5.
-// the tiles of few rows: views from where the prompt part has them to where the few-row part does, then that part
+// The tiles of few rows: views from where the prompt part has them to where the few-row part does, then that part. It has eight waves here, also with one row tile over 4 bits, where three
+// workgroups of four on a compute unit are 7 to 13 % faster (SHORT_SMALL): the prompt part's ring leaves LDS for one workgroup.
 template <int HD, int BITS, int CT>
 __device__ __forceinline__ void few_rows(const SharedArgs& a, const SharedRoom& p, ShortShared<HD, CT, PAGED_WAVES, true>& sh, u32 wg, u32 nwg) {
   constexpr u32 NT = 64 * PAGED_WAVES;
@@ -151,7 +145,16 @@ __device__ __forceinline__ void few_rows(const SharedArgs& a, const SharedRoom& 
   __syncthreads();
   paged_short<HD, BITS, CT, SHORT_AHEAD(HD, BITS, CT), PAGED_WAVES>(a, sh, wg, nwg);
 }
-// CT: row tiles of the few-row part; ANY_CT: one, or SHORT_MORE, by the views
+// A call with groups. A row's keys are its group's and its own: softmax((s1, s2)) v is joined from each part's maximum m, sum l and output o about m, by
+// o = (2^(m1-M) o1 + 2^(m2-M) o2) / (2^(m1-M) l1 + 2^(m2-M) l2). With n members of g rows each the shared keys are read once and not n times, and are products of n g rows:
+// what was bound by bytes becomes bound by products, while the members' own keys stay bound by bytes. So some workgroups have the groups' shared keys, others at the same time
+// the tiles of few rows, as many each as their estimated times ask for, and whoever is done takes the prompts' items (with one run of all shared keys, and no item behind it, 32 sequences behind
+// 4000 tokens beside a prompt of 8192 took 737 us, so 591, every sequence by itself 628). One after the other on all workgroups: 158 us, so 99, for 253 sequences
+// behind 8200 tokens with 17 to 1000 of their own; bytes of all keys that are there 58 us, every sequence by itself 1000.
+// Of a call's time 3 to 5 us are the views and sums, 4 to 9 the join (a kernel of its own: results of other workgroups are in memory behind it), a workgroup's start and end 5.
+// CT: row tiles of the few-row part; ANY_CT: one, or SHORT_MORE, by the views (both instances in one kernel: within 1 us of one alone; the larger one for all calls took 51 and not 40 us for three
+// groups of 30, heads of 64 over 4 bits). Of scalar registers 175 to 292 are spilled, into vector registers, and not in the loops over tiles or steps as far as arguments loaded anew can help it; with
+// heads of 64 over 4 bits 3 vector registers to memory.
 #define ANY_CT 0
 template <int HD, int CT> union SharedKernelRoom { ShortShared<HD, CT, PAGED_WAVES, true> s; SharedRoom p; };
 template <int HD> union SharedKernelRoom<HD, ANY_CT> { ShortShared<HD, 1, PAGED_WAVES, true> one; ShortShared<HD, SHORT_MORE(HD), PAGED_WAVES, true> more; SharedRoom p; };
