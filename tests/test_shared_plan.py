@@ -135,8 +135,7 @@ extern "C" int go_through(const Call* c, u32* first, u32* queries, u32* of_call)
     u32 s = 0;
     while (s < a.n_seqs && !(view[s].t0 <= t && t - view[s].t0 < view[s].n)) ++s;
     RULE(s < a.n_seqs);
-    bool one = groups_ascending;
-    for (u32 o = s + 1; o < a.n_seqs; ++o) if (view[o].t0 <= t && t - view[o].t0 < view[o].n) one = false;
+    const bool one = ordered;
     ++joined[s];
     const SharedView& v = view[s];
     const u32 query = t - v.t0;
